@@ -7,6 +7,7 @@
 #include "hybrid_kernels.h"
 #include "hybrid_tc.h"
 #include "hybrid_train.h"
+#include "softmax_kernels.h"
 
 namespace {
 
@@ -88,6 +89,8 @@ hybrid_status from_cuda(cudaError_t e) { return e == cudaSuccess ? HYBRID_OK : H
 
 namespace hyb {
 std::atomic<unsigned long long> g_armed_wait_ns{0};
+
+unsigned *error_word() { return ::error_word(); }
 }
 
 extern "C" {
@@ -396,7 +399,7 @@ hybrid_status hybrid_check(cudaStream_t stream)
             return HYBRID_ERR_CUDA;
     }
     if (word & hyb::ERR_WAIT_TIMEOUT) return HYBRID_ERR_TIMEOUT;
-    if (word & hyb::ERR_BAD_STATE_PTR) return HYBRID_ERR_DEVICE;
+    if (word & (hyb::ERR_BAD_STATE_PTR | hyb::ERR_BAD_INDEX)) return HYBRID_ERR_DEVICE;
     return HYBRID_OK;
 }
 

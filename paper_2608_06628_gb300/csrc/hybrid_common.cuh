@@ -17,6 +17,7 @@ namespace hyb {
 enum : unsigned {
     ERR_BAD_STATE_PTR = 1u,   // null or misaligned entry in d_state_ptrs
     ERR_WAIT_TIMEOUT = 2u,    // a bounded mbarrier / flag wait gave up
+    ERR_BAD_INDEX = 4u,       // a page, slot, length or row out of range, or too few free pages
 };
 
 __device__ __forceinline__ void raise_error(unsigned *err, unsigned bit)

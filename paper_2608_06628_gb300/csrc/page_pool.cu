@@ -1,0 +1,311 @@
+// page_pool.cu -- block tables and slot maps from request lengths, and the ring
+// of free pages (hybrid_page_append, hybrid_page_release).
+//
+// Append: with P = page_size, request r needs
+//     need_r = ceil((len_r + new_r) / P) - ceil(len_r / P)
+// pages; exclusive sums of need and of new give its first page in the ring and
+// its first slot.  A token at position p lies in page p / P, which is either in
+// the table already (p / P < ceil(len_r / P)) or the ring's entry
+// head + first_r + p / P - ceil(len_r / P).
+//
+// The work is a scan over requests (a few KB, in L2) and two ints written per
+// token: latency at decoding sizes, and the write of slots for prompts.  One
+// launch: every block scans all requests itself, 1024 at a time in shared
+// memory, and writes the slots of its own range; a block-to-block scan would
+// cost a second launch, about as long as the whole call at these sizes.
+// Nothing a block reads is written by another one (table entries of new pages
+// are only written, the ring and lengths are read from one array and written to
+// another), so no block waits on another.
+#include "hybrid_common.cuh"
+#include "softmax_kernels.h"
+
+namespace hyb {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kPer = 4;                     // requests per thread in a chunk
+constexpr int kChunk = kThreads * kPer;
+
+struct Scan2 {
+    long long a, b;
+};
+
+// Exclusive scan of (a, b) over the block in thread order; `total` gets the sums.
+__device__ Scan2 block_scan(Scan2 v, Scan2 &total, Scan2 *warp_sums)
+{
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    Scan2 inc = v;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const long long a = __shfl_up_sync(0xffffffffu, inc.a, o), b = __shfl_up_sync(0xffffffffu, inc.b, o);
+        if (lane >= o) {
+            inc.a += a;
+            inc.b += b;
+        }
+    }
+    __syncthreads();                        // warp_sums free for reuse
+    if (lane == 31) warp_sums[warp] = inc;
+    __syncthreads();
+    Scan2 before{0, 0};
+    total = {0, 0};
+#pragma unroll
+    for (int w = 0; w < kThreads / 32; ++w) {
+        if (w < warp) {
+            before.a += warp_sums[w].a;
+            before.b += warp_sums[w].b;
+        }
+        total.a += warp_sums[w].a;
+        total.b += warp_sums[w].b;
+    }
+    return {before.a + inc.a - v.a, before.b + inc.b - v.b};
+}
+
+// The ring's head and count, or an empty ring if they are out of range.
+__device__ bool load_ring(const int *ring, int n_pages, int &head, int &count)
+{
+    head = ring[0];
+    count = ring[1];
+    if (head >= 0 && head < n_pages && count >= 0 && count <= n_pages) return true;
+    head = count = 0;
+    return false;
+}
+
+struct AppendArgs {
+    const int *lens, *n_new, *free_pages, *ring_in;
+    int *table, *slots, *positions, *tok_offsets, *lens_out, *ring_out;
+    int n_req, n_slots, P, n_pages, max_pages;
+    unsigned *err;
+};
+
+__global__ __launch_bounds__(kThreads) void k_page_append(const AppendArgs a)
+{
+    __shared__ int s_tok[kChunk + 1];       // first slot of each request, capped at n_slots
+    __shared__ int s_len[kChunk], s_page[kChunk];
+    __shared__ bool s_served[kChunk];
+    __shared__ Scan2 s_warp[kThreads / 32];
+    __shared__ int s_taken;
+    const int tid = threadIdx.x;
+    int head, count;
+    const bool ring_ok = load_ring(a.ring_in, a.n_pages, head, count);
+    bool bad = !ring_ok;
+    // this block's slots
+    const long long per = (a.n_slots + (long long)gridDim.x - 1) / gridDim.x;
+    const long long lo = per * blockIdx.x;
+    const long long hi = lo + per < a.n_slots ? lo + per : a.n_slots;
+    long long tok0 = 0, page0 = 0;          // tokens and pages of the chunks before
+    if (tid == 0) s_taken = 0;
+    for (int r0 = 0, chunk = 0; r0 < a.n_req; r0 += kChunk, ++chunk) {
+        const int nr = a.n_req - r0 < kChunk ? a.n_req - r0 : kChunk;
+        const bool mine = chunk % gridDim.x == blockIdx.x;   // writes the per-request outputs
+        int len[kPer], nw[kPer], need[kPer];
+        bool valid[kPer];
+        Scan2 sum{0, 0};
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            const int r = r0 + tid * kPer + i;
+            len[i] = nw[i] = need[i] = 0;
+            valid[i] = false;
+            if (r < a.n_req) {
+                len[i] = a.lens[r];
+                nw[i] = a.n_new[r];
+                const long long end = (long long)len[i] + nw[i];
+                valid[i] = len[i] >= 0 && nw[i] >= 0 && end <= (long long)a.max_pages * a.P;
+                if (valid[i]) need[i] = (int)((end + a.P - 1) / a.P - ((long long)len[i] + a.P - 1) / a.P);
+                if (nw[i] < 0) nw[i] = 0;
+            }
+            sum.a += nw[i];
+            sum.b += need[i];
+        }
+        Scan2 total;
+        Scan2 at = block_scan(sum, total, s_warp);
+        at.a += tok0;
+        at.b += page0;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            const int l = tid * kPer + i, r = r0 + l;
+            if (r < a.n_req) {
+                const bool served =
+                    valid[i] && (need[i] == 0 || at.b + need[i] <= count) && at.a + nw[i] <= a.n_slots;
+                s_tok[l] = (int)(at.a < a.n_slots ? at.a : a.n_slots);
+                s_len[l] = len[i];
+                s_page[l] = served ? (int)at.b : 0;
+                s_served[l] = served;
+                bad |= !served;
+                // the requests that take pages come before all that find too few, so
+                // the pages taken are the first of the ring
+                if (served && need[i] > 0) atomicMax(&s_taken, (int)at.b + need[i]);
+                if (mine) {
+                    a.lens_out[r] = served ? len[i] + nw[i] : len[i];
+                    if (a.tok_offsets) a.tok_offsets[r] = s_tok[l];
+                }
+            }
+            at.a += nw[i];
+            at.b += need[i];
+        }
+        tok0 += total.a;
+        page0 += total.b;
+        if (tid == 0) s_tok[nr] = (int)(tok0 < a.n_slots ? tok0 : a.n_slots);
+        __syncthreads();
+        // the slots of this chunk that lie in this block's range
+        const long long b = s_tok[0] > lo ? s_tok[0] : lo, e = s_tok[nr] < hi ? s_tok[nr] : hi;
+        for (long long t = b + tid; t < e; t += kThreads) {
+            int x = 0, y = nr;              // last request whose first slot is <= t
+            while (y - x > 1) {
+                const int m = (x + y) >> 1;
+                if (s_tok[m] <= t) x = m;
+                else y = m;
+            }
+            const int p = s_len[x] + ((int)t - s_tok[x]);   // of a served request: fits
+            int slot = -1, pos = 0;
+            if (s_served[x]) {
+                pos = p;
+                const int j = p / a.P, old = (s_len[x] + a.P - 1) / a.P;
+                int page;
+                int *entry = a.table + (size_t)(r0 + x) * a.max_pages + j;
+                if (j >= old) {
+                    const long long i = (long long)head + s_page[x] + (j - old);
+                    page = a.free_pages[i < a.n_pages ? i : i - a.n_pages];
+                    if (p % a.P == 0) *entry = page;        // its first token is always a new one
+                } else {
+                    page = *entry;
+                }
+                if (page >= 0 && page < a.n_pages) slot = page * a.P + p % a.P;
+                else bad = true;
+            }
+            a.slots[t] = slot;
+            if (a.positions) a.positions[t] = pos;
+        }
+        __syncthreads();                    // the chunk's arrays are read no more
+    }
+    // beyond the last token
+    for (long long t = (tok0 > lo ? tok0 : lo) + tid; t < hi; t += kThreads) {
+        a.slots[t] = -1;
+        if (a.positions) a.positions[t] = 0;
+    }
+    if (blockIdx.x == 0) {
+        __syncthreads();
+        if (tid == 0) {
+            const long long h = (long long)head + s_taken;
+            a.ring_out[0] = ring_ok ? (int)(h < a.n_pages ? h : h - a.n_pages) : a.ring_in[0];
+            a.ring_out[1] = ring_ok ? count - s_taken : a.ring_in[1];
+            if (a.tok_offsets) a.tok_offsets[a.n_req] = (int)(tok0 < a.n_slots ? tok0 : a.n_slots);
+        }
+    }
+    if (bad) raise_error(a.err, ERR_BAD_INDEX);
+}
+
+struct ReleaseArgs {
+    const int *rows, *lens, *table, *ring_in;
+    int *free_pages, *ring_out;
+    int n_req, n_rows, P, n_pages, max_pages;
+    unsigned *err;
+};
+
+// Page i of all released pages, in order, goes to the ring's entry head + count + i.
+// Blocks take runs of kThreads pages in turn.
+__global__ __launch_bounds__(kThreads) void k_page_release(const ReleaseArgs a)
+{
+    __shared__ int s_row[kChunk];
+    __shared__ long long s_first[kChunk + 1];
+    __shared__ Scan2 s_warp[kThreads / 32];
+    const int tid = threadIdx.x;
+    int head, count;
+    const bool ring_ok = load_ring(a.ring_in, a.n_pages, head, count);
+    const long long room = ring_ok ? a.n_pages - count : 0;
+    bool bad = !ring_ok;
+    long long page0 = 0;
+    for (int i0 = 0; i0 < a.n_rows; i0 += kChunk) {
+        const int nr = a.n_rows - i0 < kChunk ? a.n_rows - i0 : kChunk;
+        int k[kPer];
+        Scan2 sum{0, 0};
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            const int l = tid * kPer + i;
+            k[i] = 0;
+            if (i0 + l < a.n_rows) {
+                const int r = a.rows[i0 + l];
+                const bool row_ok = r >= 0 && r < a.n_req;
+                const int len = row_ok ? a.lens[r] : -1;
+                const bool ok = len >= 0 && len <= (long long)a.max_pages * a.P;
+                if (ok) k[i] = (int)(((long long)len + a.P - 1) / a.P);
+                s_row[l] = ok ? r : 0;
+                bad |= !ok;
+            }
+            sum.a += k[i];
+        }
+        Scan2 total;
+        Scan2 at = block_scan(sum, total, s_warp);
+        at.a += page0;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            const int l = tid * kPer + i;
+            if (l < nr) s_first[l] = at.a;
+            at.a += k[i];
+        }
+        const long long begin = page0;
+        page0 += total.a;
+        if (tid == 0) s_first[nr] = page0;
+        __syncthreads();
+        const long long end = page0 < room ? page0 : room;
+        long long run = begin / kThreads;
+        run += (blockIdx.x + gridDim.x - run % gridDim.x) % gridDim.x;   // first run of this block
+        for (; run * kThreads < end; run += gridDim.x) {
+            const long long i = run * kThreads + tid;
+            if (i >= begin && i < end) {
+                int x = 0, y = nr;
+                while (y - x > 1) {
+                    const int m = (x + y) >> 1;
+                    if (s_first[m] <= i) x = m;
+                    else y = m;
+                }
+                const int page = a.table[(size_t)s_row[x] * a.max_pages + (size_t)(i - s_first[x])];
+                if (page < 0 || page >= a.n_pages) bad = true;
+                a.free_pages[((long long)head + count + i) % a.n_pages] = page;
+            }
+        }
+        __syncthreads();
+    }
+    if (page0 > room) bad = true;
+    if (blockIdx.x == 0 && tid == 0) {
+        a.ring_out[0] = a.ring_in[0];
+        a.ring_out[1] = ring_ok ? count + (int)(page0 < room ? page0 : room) : a.ring_in[1];
+    }
+    if (bad) raise_error(a.err, ERR_BAD_INDEX);
+}
+
+// Enough blocks for about 2048 items each, at most two waves of the GPU.
+int blocks_for(long long items)
+{
+    const long long n = (items + 2047) / 2048;
+    return (int)(n < 1 ? 1 : (n > 304 ? 304 : n));
+}
+
+}  // namespace
+
+cudaError_t launch_page_append(const hybrid_page_cfg &pg, int n_req, const int *lens, const int *n_new,
+                               const int *free_pages, const int *ring_in, int *block_table, int *slots,
+                               int *positions, int n_slots, int *tok_offsets, int *lens_out, int *ring_out,
+                               unsigned *err, cudaStream_t st)
+{
+    AppendArgs a{lens,      n_new,    free_pages, ring_in, block_table,  slots,      positions,    tok_offsets,
+                 lens_out,  ring_out, n_req,      n_slots, pg.page_size, pg.n_pages, pg.max_pages, err};
+    void *args[] = {&a};
+    return cudaLaunchKernel(reinterpret_cast<const void *>(&k_page_append), dim3(blocks_for(n_slots)), dim3(kThreads),
+                            args, 0, st);
+}
+
+cudaError_t launch_page_release(const hybrid_page_cfg &pg, int n_req, const int *rows, int n_rows, const int *lens,
+                                const int *block_table, int *free_pages, const int *ring_in, int *ring_out,
+                                unsigned *err, cudaStream_t st)
+{
+    ReleaseArgs a{rows,     lens,  block_table, ring_in,      free_pages, ring_out,
+                  n_req,    n_rows, pg.page_size, pg.n_pages, pg.max_pages, err};
+    void *args[] = {&a};
+    // at most the pool's pages move
+    long long most = (long long)n_rows * pg.max_pages;
+    if (most > pg.n_pages) most = pg.n_pages;
+    return cudaLaunchKernel(reinterpret_cast<const void *>(&k_page_release), dim3(blocks_for(most)), dim3(kThreads),
+                            args, 0, st);
+}
+
+}  // namespace hyb

@@ -1,0 +1,162 @@
+// paged_plan.cuh -- how one paged-attention call is cut over the GPU, and the
+// format of the partial results.
+//
+// A unit is (request, key head, row tile): M = Hkv * n_gt * n_bt units a request,
+// all with the same visible keys.  The visible keys of a request are cut into
+// tiles of kTile keys; the tiles of all units, in the order (request, unit of the
+// request, tile), are shared out evenly: of C blocks, block c takes the tiles
+// [c T / C, (c + 1) T / C).  So every block reads the same amount of cache
+// whatever the lengths are, and a long request is split over as many blocks as
+// it is worth.  The lengths are on the device, so each block finds its share
+// itself by a scan over the requests (a few KB).
+//
+// A run of tiles of one unit is a segment.  A segment that covers its unit writes
+// the output; any other writes (m, l, O) -- running maximum in units of log2,
+// sum and unnormalised output -- to partial 2 c (segment at the start of the
+// block's share) or 2 c + 1 (a later one: only a block's last segment can be cut
+// there).  A second launch joins them.
+#pragma once
+
+#include "hybrid_common.cuh"
+#include "softmax_kernels.h"
+
+namespace hyb {
+namespace paged {
+
+constexpr int kTile = 128;
+
+// Visible keys of a context of len tokens: [0, sink) and [lo, len), sink <= lo;
+// as tiles: `ns` tiles from 0 (those of the sinks), then `first`, first + 1, ...
+struct Visible {
+    int len, lo, sink;
+    int ns, first, tiles;
+};
+
+__device__ __forceinline__ Visible visible_keys(const PagedArgs &a, int len)
+{
+    Visible v;
+    const long long cap = (long long)a.max_pages * a.page_size;
+    if (len < 0) len = 0;
+    if (len > cap) len = (int)cap;
+    v.len = len;
+    v.lo = a.window > 0 && len > a.window ? len - a.window : 0;
+    v.sink = v.lo > 0 ? (a.sink < v.lo ? a.sink : v.lo) : 0;
+    v.ns = (v.sink + kTile - 1) / kTile;
+    v.first = v.lo / kTile > v.ns ? v.lo / kTile : v.ns;
+    const int last = (int)(((long long)len + kTile - 1) / kTile);
+    v.tiles = v.ns + (last > v.first ? last - v.first : 0);
+    return v;
+}
+__device__ __forceinline__ bool length_ok(const PagedArgs &a, int len)
+{
+    return len >= 0 && len <= (long long)a.max_pages * a.page_size;
+}
+// key tile of the i-th visible tile
+__device__ __forceinline__ int key_tile(const Visible &v, int i) { return i < v.ns ? i : v.first + (i - v.ns); }
+__device__ __forceinline__ bool key_visible(const Visible &v, int j) { return j < v.len && (j >= v.lo || j < v.sink); }
+
+__device__ __forceinline__ int units_per_request(const PagedArgs &a) { return a.Hkv * a.n_gt * a.n_bt; }
+
+// First tile of block c of C.
+__device__ __forceinline__ long long share_start(long long T, int C, int c) { return T * c / C; }
+
+// Scratch of the scan: one long per warp and the answer.
+struct PlanSmem {
+    long long warp[32];
+    long long total;
+    int req;
+    long long before;
+};
+
+// Scan over the requests by the whole block (NT threads, a multiple of 32).
+// Returns T, the number of tiles of all units; then locate() finds the request
+// of a tile.  Each thread holds the requests [q0, q1) and the tiles before them
+// (per unit of a request, that is: without the factor M).
+struct Plan {
+    long long total;       // tiles of all requests, per unit
+    long long before;      // of the requests before this thread's
+    int q0, q1;
+};
+
+template <int NT>
+__device__ __forceinline__ Plan make_plan(const PagedArgs &a, PlanSmem &s)
+{
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int per = (a.n_req + NT - 1) / NT;
+    Plan p;
+    p.q0 = tid * per < a.n_req ? tid * per : a.n_req;
+    p.q1 = p.q0 + per < a.n_req ? p.q0 + per : a.n_req;
+    long long sum = 0;
+    bool bad = false;
+    for (int r = p.q0; r < p.q1; ++r) {
+        const int len = a.lens[r];
+        bad |= !length_ok(a, len);
+        sum += visible_keys(a, len).tiles;
+    }
+    if (bad) raise_error(a.err, ERR_BAD_INDEX);
+    long long inc = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const long long v = __shfl_up_sync(0xffffffffu, inc, o);
+        if (lane >= o) inc += v;
+    }
+    if (lane == 31) s.warp[warp] = inc;
+    __syncthreads();
+    long long before = 0, total = 0;
+#pragma unroll
+    for (int w = 0; w < NT / 32; ++w) {
+        if (w < warp) before += s.warp[w];
+        total += s.warp[w];
+    }
+    p.total = total;
+    p.before = before + inc - sum;
+    return p;
+}
+
+// Request that holds tile `tile` (0 <= tile < total * M) and the tiles per unit
+// of the requests before it; for the whole block.
+__device__ __forceinline__ void locate(const PagedArgs &a, const Plan &p, long long tile, PlanSmem &s, int &req,
+                                       long long &before)
+{
+    const long long M = units_per_request(a);
+    long long b = p.before;
+    for (int r = p.q0; r < p.q1; ++r) {
+        const int n = visible_keys(a, a.lens[r]).tiles;
+        if (tile >= b * M && tile < (b + n) * M) {
+            s.req = r;
+            s.before = b;
+        }
+        b += n;
+    }
+    __syncthreads();
+    req = s.req;
+    before = s.before;
+}
+
+// Unit m of a request: key head, first query head of the group, first token.
+struct Unit {
+    int head, g0, i0;
+    int rows;              // valid rows: row rho is token i0 + rho / Gt, head g0 + rho % Gt
+};
+__device__ __forceinline__ Unit unit_of(const PagedArgs &a, int m)
+{
+    Unit u;
+    u.head = m / (a.n_gt * a.n_bt);
+    const int rest = m % (a.n_gt * a.n_bt);
+    u.g0 = rest / a.n_bt * a.Gt;
+    u.i0 = rest % a.n_bt * a.Bt;
+    return u;
+}
+// Element offset of row rho of a unit in Q and O, and whether the row exists.
+__device__ __forceinline__ bool row_at(const PagedArgs &a, int req, const Unit &u, int rho, size_t &at)
+{
+    const int i = u.i0 + rho / a.Gt, g = u.g0 + rho % a.Gt;
+    at = (((size_t)req * a.B + i) * a.Hq + (size_t)u.head * a.G + g) * a.d;
+    return rho < a.Bt * a.Gt && i < a.B && g < a.G;
+}
+
+// Partial slot s: m[rows], l[rows], O[rows][d], rows = Bt * Gt.
+__host__ __device__ __forceinline__ size_t partial_floats(int rows, int d) { return ((size_t)rows * (d + 2) + 3) / 4 * 4; }
+
+}  // namespace paged
+}  // namespace hyb

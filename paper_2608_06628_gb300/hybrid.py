@@ -1,4 +1,5 @@
-"""Python binding of the block-hybrid attention C ABI (include/hybrid.h).
+"""Python binding of the block-hybrid attention C ABI (include/hybrid.h, and
+include/hybrid_softmax.h for the softmax layers of a hybrid model).
 
 Argument marshalling only: every function here forwards to the entry point of
 ``libhybrid.so`` with the same name.  Tensors are passed as device pointers
@@ -29,7 +30,16 @@ EXPORTED = (
     "hybrid_state_unpack",
     "hybrid_state_pack", "hybrid_train_workspace_bytes", "hybrid_train_forward", "hybrid_train_backward",
     "hybrid_debug_arm_wait_timeout", "hybrid_check", "hybrid_status_str",
+    # the softmax layers of a hybrid model (include/hybrid_softmax.h)
+    "hybrid_page_append", "hybrid_page_release", "hybrid_rope_freqs", "hybrid_qk_norm_rope",
+    "hybrid_qk_norm_rope_cache", "hybrid_qk_norm_rope_workspace_bytes", "hybrid_qk_norm_rope_backward",
+    "hybrid_paged_attn_workspace_bytes", "hybrid_paged_attn",
 )
+
+HYBRID_ROPE_NONE = 0
+HYBRID_ROPE_LINEAR = 1
+HYBRID_ROPE_NTK = 2
+HYBRID_ROPE_YARN = 3
 
 
 class hybrid_cfg(ctypes.Structure):
@@ -45,6 +55,27 @@ class hybrid_cfg(ctypes.Structure):
     def __repr__(self):
         return (f"hybrid_cfg(d={self.head_dim}, F={self.feat_dim}, Hq={self.n_q_heads}, "
                 f"Hkv={self.n_kv_heads}, B={self.block_size}, io_dtype={self.io_dtype})")
+
+
+class hybrid_page_cfg(ctypes.Structure):
+    _fields_ = [("page_size", ctypes.c_int), ("n_pages", ctypes.c_int), ("max_pages", ctypes.c_int)]
+
+    def __repr__(self):
+        return f"hybrid_page_cfg(page_size={self.page_size}, n_pages={self.n_pages}, max_pages={self.max_pages})"
+
+
+class hybrid_rope_cfg(ctypes.Structure):
+    _fields_ = [("rot_dim", ctypes.c_int), ("interleaved", ctypes.c_int), ("scale", ctypes.c_float),
+                ("eps", ctypes.c_float)]
+
+    def __repr__(self):
+        return (f"hybrid_rope_cfg(rot_dim={self.rot_dim}, interleaved={self.interleaved}, scale={self.scale}, "
+                f"eps={self.eps})")
+
+
+class hybrid_rope_scaling(ctypes.Structure):
+    _fields_ = [("kind", ctypes.c_int), ("base", ctypes.c_double), ("factor", ctypes.c_double),
+                ("orig_len", ctypes.c_double), ("beta_fast", ctypes.c_double), ("beta_slow", ctypes.c_double)]
 
 
 class HybridError(RuntimeError):
@@ -88,8 +119,21 @@ def lib(path: str | None = None):
     L.hybrid_check.argtypes = [P]
     L.hybrid_status_str.argtypes = [I]
     L.hybrid_status_str.restype = ctypes.c_char_p
+    pgp, ropep = ctypes.POINTER(hybrid_page_cfg), ctypes.POINTER(hybrid_rope_cfg)
+    L.hybrid_page_append.argtypes = [pgp, I, P, P, P, P, P, P, P, I, P, P, P, P]
+    L.hybrid_page_release.argtypes = [pgp, I, P, I, P, P, P, P, P, P]
+    L.hybrid_rope_freqs.argtypes = [ctypes.POINTER(hybrid_rope_scaling), I, P, ctypes.POINTER(ctypes.c_float)]
+    L.hybrid_qk_norm_rope.argtypes = [cfgp, ropep, P, S, P, S, I, P, P, P, P, P, P, P]
+    L.hybrid_qk_norm_rope_cache.argtypes = [cfgp, ropep, pgp, P, S, P, S, P, S, I, P, P, P, P, P, P, P, P, P]
+    L.hybrid_qk_norm_rope_workspace_bytes.argtypes = [cfgp, I]
+    L.hybrid_qk_norm_rope_workspace_bytes.restype = S
+    L.hybrid_qk_norm_rope_backward.argtypes = [cfgp, ropep, P, S, P, S, P, P, I, P, P, P, P, P, S, P, P, P, P, P]
+    L.hybrid_paged_attn_workspace_bytes.argtypes = [cfgp, pgp, I]
+    L.hybrid_paged_attn_workspace_bytes.restype = S
+    L.hybrid_paged_attn.argtypes = [cfgp, pgp, P, P, P, P, P, I, I, I, P, P, S, P]
     for name in EXPORTED:
-        if name not in ("hybrid_state_bytes", "hybrid_status_str", "hybrid_train_workspace_bytes"):
+        if name not in ("hybrid_state_bytes", "hybrid_status_str", "hybrid_train_workspace_bytes",
+                        "hybrid_qk_norm_rope_workspace_bytes", "hybrid_paged_attn_workspace_bytes"):
             getattr(L, name).restype = ctypes.c_int
     if path == _build.LIB_PATH:
         _lib = L
@@ -226,3 +270,83 @@ def hybrid_debug_arm_wait_timeout(wait_ns, check=True):
 def hybrid_check(stream=None, check=True):
     st = lib().hybrid_check(_stream(stream))
     return _ret(st, "hybrid_check", check)
+
+
+# ---------------------------------------------------------------- softmax layers
+
+def make_page_cfg(page_size, n_pages, max_pages) -> hybrid_page_cfg:
+    return hybrid_page_cfg(int(page_size), int(n_pages), int(max_pages))
+
+
+def make_rope(rot_dim, interleaved=False, eps=1e-6, base=10000.0, kind=HYBRID_ROPE_NONE, factor=1.0, orig_len=4096.0,
+              beta_fast=32.0, beta_slow=1.0, device="cuda"):
+    """The rotation of a model's layers: (hybrid_rope_cfg, freqs), freqs an int64
+    tensor that holds hybrid_rope_freqs' 64-bit fractions.  Made once per model."""
+    import torch
+    arr = (ctypes.c_ulonglong * max(1, int(rot_dim) // 2))()
+    scale = ctypes.c_float(1.0)
+    if rot_dim:
+        sc = hybrid_rope_scaling(int(kind), float(base), float(factor), float(orig_len), float(beta_fast), float(beta_slow))
+        hybrid_rope_freqs(sc, rot_dim, arr, scale)
+    freqs = torch.frombuffer(bytearray(arr), dtype=torch.int64).to(device)
+    return hybrid_rope_cfg(int(rot_dim), int(bool(interleaved)), scale.value, float(eps)), freqs
+
+
+def hybrid_page_append(pg, n_req, lens, n_new, free_pages, ring_in, block_table, slots, positions, n_slots, tok_offsets,
+                       lens_out, ring_out, stream=None, check=True):
+    st = lib().hybrid_page_append(pg, n_req, _ptr(lens), _ptr(n_new), _ptr(free_pages), _ptr(ring_in),
+                                  _ptr(block_table), _ptr(slots), _ptr(positions), n_slots, _ptr(tok_offsets),
+                                  _ptr(lens_out), _ptr(ring_out), _stream(stream))
+    return _ret(st, "hybrid_page_append", check)
+
+
+def hybrid_page_release(pg, n_req, rows, n_rows, lens, block_table, free_pages, ring_in, ring_out, stream=None,
+                        check=True):
+    st = lib().hybrid_page_release(pg, n_req, _ptr(rows), n_rows, _ptr(lens), _ptr(block_table), _ptr(free_pages),
+                                   _ptr(ring_in), _ptr(ring_out), _stream(stream))
+    return _ret(st, "hybrid_page_release", check)
+
+
+def hybrid_rope_freqs(scaling, rot_dim, freqs, scale, check=True):
+    """freqs: a ctypes array of rot_dim / 2 unsigned long long, scale: a ctypes float; both written."""
+    st = lib().hybrid_rope_freqs(ctypes.byref(scaling), int(rot_dim), freqs, ctypes.byref(scale))
+    return _ret(st, "hybrid_rope_freqs", check)
+
+
+def hybrid_qk_norm_rope(cfg, rope, Q, q_stride, K, k_stride, n_tok, wq, wk, positions, freqs, Qo, Ko, stream=None,
+                        check=True):
+    st = lib().hybrid_qk_norm_rope(cfg, rope, _ptr(Q), q_stride, _ptr(K), k_stride, n_tok, _ptr(wq), _ptr(wk),
+                                   _ptr(positions), _ptr(freqs), _ptr(Qo), _ptr(Ko), _stream(stream))
+    return _ret(st, "hybrid_qk_norm_rope", check)
+
+
+def hybrid_qk_norm_rope_cache(cfg, rope, pg, Q, q_stride, K, k_stride, V, v_stride, n_tok, wq, wk, positions, freqs,
+                              slots, Qo, K_cache, V_cache, stream=None, check=True):
+    st = lib().hybrid_qk_norm_rope_cache(cfg, rope, pg, _ptr(Q), q_stride, _ptr(K), k_stride, _ptr(V), v_stride, n_tok,
+                                         _ptr(wq), _ptr(wk), _ptr(positions), _ptr(freqs), _ptr(slots), _ptr(Qo),
+                                         _ptr(K_cache), _ptr(V_cache), _stream(stream))
+    return _ret(st, "hybrid_qk_norm_rope_cache", check)
+
+
+def hybrid_qk_norm_rope_workspace_bytes(cfg, n_tok) -> int:
+    return int(lib().hybrid_qk_norm_rope_workspace_bytes(cfg, n_tok))
+
+
+def hybrid_qk_norm_rope_backward(cfg, rope, Q, q_stride, K, k_stride, dQo, dKo, n_tok, wq, wk, positions, freqs,
+                                 workspace, workspace_bytes, dQ, dK, dwq, dwk, stream=None, check=True):
+    st = lib().hybrid_qk_norm_rope_backward(cfg, rope, _ptr(Q), q_stride, _ptr(K), k_stride, _ptr(dQo), _ptr(dKo),
+                                            n_tok, _ptr(wq), _ptr(wk), _ptr(positions), _ptr(freqs), _ptr(workspace),
+                                            workspace_bytes, _ptr(dQ), _ptr(dK), _ptr(dwq), _ptr(dwk),
+                                            _stream(stream))
+    return _ret(st, "hybrid_qk_norm_rope_backward", check)
+
+
+def hybrid_paged_attn_workspace_bytes(cfg, pg, n_req) -> int:
+    return int(lib().hybrid_paged_attn_workspace_bytes(cfg, pg, n_req))
+
+
+def hybrid_paged_attn(cfg, pg, Q, K_cache, V_cache, block_table, kv_len, n_req, window, n_sink, O, workspace,
+                      workspace_bytes, stream=None, check=True):
+    st = lib().hybrid_paged_attn(cfg, pg, _ptr(Q), _ptr(K_cache), _ptr(V_cache), _ptr(block_table), _ptr(kv_len),
+                                 n_req, window, n_sink, _ptr(O), _ptr(workspace), workspace_bytes, _stream(stream))
+    return _ret(st, "hybrid_paged_attn", check)
