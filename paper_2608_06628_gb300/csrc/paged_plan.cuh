@@ -133,10 +133,47 @@ __device__ __forceinline__ void locate(const PagedArgs &a, const Plan &p, long l
     before = s.before;
 }
 
+// The segments of a block's share, one after another.
+struct Walk {
+    long long t, t1;       // next tile, end of the share
+    long long before;      // tiles per unit of the requests before `req`
+    int req;
+    Visible vis;
+    // the current segment: tiles [i0, i1) of unit m of request req
+    int m, i0, i1;
+    bool at_start;         // it begins the share
+
+    __device__ void begin(const PagedArgs &a, long long t_, long long t1_, int req_, long long before_)
+    {
+        t = t_;
+        t1 = t1_;
+        req = req_;
+        before = before_;
+        vis = visible_keys(a, __ldg(a.lens + req));
+        at_start = true;
+        i1 = -1;
+    }
+    __device__ bool next(const PagedArgs &a, long long M)
+    {
+        if (t >= t1) return false;
+        at_start = i1 < 0;
+        while (t >= (before + vis.tiles) * M) {             // next request with visible keys
+            before += vis.tiles;
+            vis = visible_keys(a, __ldg(a.lens + ++req));
+        }
+        const long long rel = t - before * M;
+        m = (int)(rel / vis.tiles);
+        i0 = (int)(rel % vis.tiles);
+        i1 = vis.tiles - i0 < t1 - t ? vis.tiles : (int)(i0 + (t1 - t));
+        t += i1 - i0;
+        return true;
+    }
+    __device__ bool whole() const { return i0 == 0 && i1 == vis.tiles; }
+};
+
 // Unit m of a request: key head, first query head of the group, first token.
 struct Unit {
-    int head, g0, i0;
-    int rows;              // valid rows: row rho is token i0 + rho / Gt, head g0 + rho % Gt
+    int head, g0, i0;      // row rho is token i0 + rho / Gt, head g0 + rho % Gt
 };
 __device__ __forceinline__ Unit unit_of(const PagedArgs &a, int m)
 {
@@ -155,7 +192,8 @@ __device__ __forceinline__ bool row_at(const PagedArgs &a, int req, const Unit &
     return rho < a.Bt * a.Gt && i < a.B && g < a.G;
 }
 
-// Partial slot s: m[rows], l[rows], O[rows][d], rows = Bt * Gt.
+// Partial slot: m[rows], l[rows], O[d][rows] (feature-major, so that the threads of a
+// warp, one row each, write runs of memory), rows = Bt * Gt.
 __host__ __device__ __forceinline__ size_t partial_floats(int rows, int d) { return ((size_t)rows * (d + 2) + 3) / 4 * 4; }
 
 }  // namespace paged

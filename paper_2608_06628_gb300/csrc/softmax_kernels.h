@@ -58,6 +58,7 @@ struct PagedArgs {
 // Geometry (row tiles, number of blocks) of a call; part and pointers left to the caller.
 void paged_geometry(const hybrid_cfg &c, PagedArgs &a);
 size_t paged_partial_bytes(const PagedArgs &a);
+cudaError_t launch_paged_attn_tc(const PagedArgs &a, cudaStream_t st);   // bfloat16, without the join
 cudaError_t launch_paged_attn(hybrid_dtype dt, const PagedArgs &a, cudaStream_t st);
 
 }  // namespace hyb
