@@ -44,21 +44,14 @@ __global__ __launch_bounds__(kThreads) void k_paged_attn(const PagedArgs a)
     const float to_log2 = pipe::kLog2e * rsqrtf((float)D);
 
     ptx::griddep_launch_dependents();                        // the join may start its scan
-    const Plan plan = make_plan<kThreads>(a, s.plan);
-    const long long M = units_per_request(a), T_all = plan.total * M;
-    const int C = T_all < a.n_cta ? (int)T_all : a.n_cta;
-    if ((int)blockIdx.x >= C) return;
-    const long long t = share_start(T_all, C, blockIdx.x), t1 = share_start(T_all, C, blockIdx.x + 1);
-    int req;
-    long long before;
-    locate(a, plan, t, s.plan, req, before);
-
     Walk w;
-    w.begin(a, t, t1, req, before);
-    while (w.next(a, M)) {
+    Shares sh(0, 1);
+    const bool work = find_share<kThreads>(a, s.plan, w, sh);
+    const long long M = units_per_request(a);
+    while (work && w.next(a, M)) {
         const Visible vis = w.vis;
         const int i0 = w.i0, i1 = w.i1;
-        req = w.req;
+        const int req = w.req;
         const Unit u = unit_of(a, w.m);
         const int *pages = a.table + (size_t)req * a.max_pages;
 
@@ -167,7 +160,7 @@ __global__ __launch_bounds__(kThreads) void k_paged_attn(const PagedArgs a)
             }
         }
         const bool whole = w.whole();
-        float *part = a.part + (size_t)(2 * blockIdx.x + (w.at_start ? 0 : 1)) * partial_floats(rows, D);
+        float *part = a.part + w.slot() * partial_floats(rows, D);
 #pragma unroll
         for (int y = 0; y < kOwn; ++y) {
             const int rho = row0 + y * kRowStep;
@@ -195,110 +188,118 @@ __global__ __launch_bounds__(kThreads) void k_paged_attn(const PagedArgs a)
             }
         }
     }
+    if (tid == 0) write_note(a, work, w, sh);
+    write_empty<float, kThreads>(a, tid);
 }
 
-// Join: block x looks at the boundary between shares x and x + 1.  If it cuts a
-// unit, and is the first one to cut it, the block joins all of the unit's
-// partials; blocks along y take kJoinCols features each.  Where a unit has few
-// rows (decoding) and so may have many partials, groups of threads take every
-// n-th partial and are added in order.  Requests without a visible key get their
-// zeros here, shared over the blocks.  Launched programmatically behind the
-// attention kernel: the scan over the requests overlaps its end.
-constexpr int kJoinCols = 32;
+// Join: block x reads the note of boundary x and, if a unit is cut there for the
+// first time, adds up the unit's partials; blocks along y take COLS features each.
+// Where a unit has few rows (decoding) it may have many partials: then groups of
+// threads take every n-th one, and the groups are added in order.  Launched
+// programmatically behind the attention kernel.
 constexpr int kMaxRows = 128;
+constexpr int kJoinWeights = 2048;      // weights in shared memory at a time
 
-template <typename T, int D>
+template <typename T, int COLS>
 __global__ __launch_bounds__(kThreads) void k_paged_join(const PagedArgs a)
 {
-    __shared__ PlanSmem s_plan;
+    // items per thread, at most (16 features: at most 16 rows)
+    constexpr int kIter = (COLS == 16 ? 16 : kMaxRows) * COLS / kThreads;
     __shared__ float s_base[kMaxRows], s_inv[kMaxRows];
-    __shared__ float s_o[kMaxRows * (kJoinCols + 1)];        // [group][row][kJoinCols + 1]
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, rows = a.Bt * a.Gt;
-    const int col0 = blockIdx.y * kJoinCols;
-    const Plan plan = make_plan<kThreads>(a, s_plan);
-    const long long M = units_per_request(a), T_all = plan.total * M;
-    const int C = T_all < a.n_cta ? (int)T_all : a.n_cta;
-    const int c = blockIdx.x;
-    int req = 0, last = 0;
-    Unit u{};
-    const float *first = nullptr;
-    bool cut_here = false;
-    if (c + 1 < C) {
-        const long long cut = share_start(T_all, C, c + 1);
-        long long before;
-        locate(a, plan, cut, s_plan, req, before);
-        const Visible vis = visible_keys(a, a.lens[req]);
-        const int m = (int)((cut - before * M) / vis.tiles);
-        const long long mine = share_start(T_all, C, c), start = before * M + (long long)m * vis.tiles;
-        cut_here = cut != start && mine <= start;
-        if (cut_here) {
-            last = c + 1;                                    // block of the unit's last tile
-            while (share_start(T_all, C, last + 1) < start + vis.tiles) ++last;
-            u = unit_of(a, m);
-            first = a.part + (size_t)(2 * c + (mine != start)) * partial_floats(rows, D);
-        }
-    }
+    __shared__ float s_w[kJoinWeights];                      // [partial of the chunk][row]
+    __shared__ float s_o[kMaxRows * (COLS + 1)];             // [group][row][COLS + 1]
+    const int tid = threadIdx.x, rows = a.Bt * a.Gt, c = blockIdx.x, col0 = blockIdx.y * COLS;
     ptx::griddep_wait();
-    for (int r = blockIdx.x; r < a.n_req; r += gridDim.x) {
-        if (visible_keys(a, a.lens[r]).tiles > 0) continue;
-        T *out = static_cast<T *>(a.O) + (size_t)r * a.B * a.Hq * D;
-        const int n = a.B * a.Hq * D / 4;
-        for (int x = blockIdx.y * kThreads + tid; x < n; x += gridDim.y * kThreads)
-            store4(out + (size_t)x * 4, make_float4(0.f, 0.f, 0.f, 0.f));
-    }
-    if (!cut_here) return;
-    const size_t size = partial_floats(rows, D);
-    auto part_of = [&](int b) { return b == c ? first : a.part + (size_t)2 * b * size; };
+    const JoinNote note = a.notes[c];
+    if (!note.cut) return;
+    const size_t size = partial_floats(rows, a.d);
+    const int n = note.last - c + 1;                         // partials
+    auto part_of = [&](int i) { return a.part + (size_t)(i == 0 ? note.slot : 2 * (c + i)) * size; };
 
-    // maximum and sum of each row: warp = row, lanes over the partials
-    for (int rho = warp; rho < rows; rho += kThreads / 32) {
-        float mx = -INFINITY;
-        for (int b = c + lane; b <= last; b += 32) mx = fmaxf(mx, part_of(b)[rho]);
-        mx = warp_max(mx);
+    // maximum and sum of each row: L lanes a row
+    int L = 1;
+    while (L < n && L < 32) L *= 2;
+    for (int r0 = 0; r0 < rows; r0 += kThreads / L) {
+        const int rho = r0 + tid / L, y = tid % L;
+        float mx = -INFINITY, l = 0.f;
+        if (rho < rows)
+            for (int i = y; i < n; i += L) mx = fmaxf(mx, part_of(i)[rho]);
+        for (int o = L / 2; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
         const float base = mx == -INFINITY ? 0.f : mx;
-        float l = 0.f;
-        for (int b = c + lane; b <= last; b += 32) l = fmaf(exp2f(part_of(b)[rho] - base), part_of(b)[rows + rho], l);
-        l = warp_sum(l);
-        if (lane == 0) {
+        if (rho < rows)
+            for (int i = y; i < n; i += L) l = fmaf(exp2f(part_of(i)[rho] - base), part_of(i)[rows + rho], l);
+        for (int o = L / 2; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+        if (rho < rows && y == 0) {
             s_base[rho] = base;
             s_inv[rho] = 1.f / l;
         }
     }
-    __syncthreads();
     // sums over the partials; item = (feature, row), row fastest as in memory
-    const int items = rows * kJoinCols, groups = items <= kThreads / 2 ? kThreads / items : 1;
-    const int step = groups > 1 ? items * groups : kThreads;
-    for (int x = tid; x < items * groups; x += step) {
-        const int item = x % items, g = x / items, rho = item % rows, col = item / rows;
-        const float base = s_base[rho];
-        float o = 0.f;
+    const int items = rows * COLS, groups = items <= kThreads / 2 ? kThreads / items : 1;
+    const int g = groups > 1 ? tid / items : 0, item0 = groups > 1 ? tid % items : tid;
+    const int rho0 = item0 % rows, step_row = kThreads % rows;
+    float o[kIter];
+#pragma unroll
+    for (int k = 0; k < kIter; ++k) o[k] = 0.f;
+    const int chunk = kJoinWeights / rows;
+    for (int i0 = 0; i0 < n; i0 += chunk) {
+        const int nc = n - i0 < chunk ? n - i0 : chunk;
+        __syncthreads();
+        for (int x = tid; x < nc * rows; x += kThreads)
+            s_w[x] = exp2f(part_of(i0 + x / rows)[x % rows] - s_base[x % rows]);
+        __syncthreads();
+        if (g >= groups) continue;
 #pragma unroll 4
-        for (int b = c + g; b <= last; b += groups) {
-            const float *p = part_of(b);
-            o = fmaf(exp2f(p[rho] - base), p[2 * rows + (size_t)(col0 + col) * rows + rho], o);
+        for (int i = g; i < nc; i += groups) {
+            const float *p = part_of(i0 + i) + 2 * rows + (size_t)col0 * rows;
+            int rho = rho0;
+#pragma unroll
+            for (int k = 0; k < kIter; ++k) {
+                const int item = item0 + k * kThreads;
+                if (item < items) o[k] = fmaf(s_w[i * rows + rho], p[item], o[k]);
+                rho += step_row;
+                if (rho >= rows) rho -= rows;
+            }
         }
-        s_o[(g * rows + rho) * (kJoinCols + 1) + col] = o;
+    }
+    {
+        int rho = rho0, col = item0 / rows;
+        const int step_col = kThreads / rows;
+#pragma unroll
+        for (int k = 0; k < kIter; ++k) {
+            if (g < groups && item0 + k * kThreads < items) s_o[(g * rows + rho) * (COLS + 1) + col] = o[k];
+            rho += step_row;
+            col += step_col;
+            if (rho >= rows) {
+                rho -= rows;
+                ++col;
+            }
+        }
     }
     __syncthreads();
-    for (int x = tid; x < rows * (kJoinCols / 4); x += kThreads) {
-        const int rho = x / (kJoinCols / 4), col = x % (kJoinCols / 4) * 4;
+    const Unit u = unit_of(a, note.m);
+    for (int x = tid; x < rows * (COLS / 4); x += kThreads) {
+        const int rho = x / (COLS / 4), col = x % (COLS / 4) * 4;
         size_t at;
-        if (!row_at(a, req, u, rho, at)) continue;
-        float o[4] = {0.f, 0.f, 0.f, 0.f};
-        for (int g = 0; g < groups; ++g) {
+        if (!row_at(a, note.req, u, rho, at)) continue;
+        float v[4] = {0.f, 0.f, 0.f, 0.f};
+        for (int y = 0; y < groups; ++y) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) o[i] += s_o[(g * rows + rho) * (kJoinCols + 1) + col + i];
+            for (int i = 0; i < 4; ++i) v[i] += s_o[(y * rows + rho) * (COLS + 1) + col + i];
         }
         const float f = s_inv[rho];
-        store4(static_cast<T *>(a.O) + at + col0 + col, make_float4(o[0] * f, o[1] * f, o[2] * f, o[3] * f));
+        store4(static_cast<T *>(a.O) + at + col0 + col, make_float4(v[0] * f, v[1] * f, v[2] * f, v[3] * f));
     }
 }
 
 // The join of a call whose attention kernel was launched just before.
-template <typename T, int D> cudaError_t launch_join(const PagedArgs &a, cudaStream_t st)
+template <typename T> cudaError_t launch_join(const PagedArgs &a, cudaStream_t st)
 {
+    // many partials of few rows: more blocks of fewer features
+    const bool few = a.Bt * a.Gt <= 16;
+    static_assert(16 * 16 == kThreads, "one item a thread");
     cudaLaunchConfig_t lc = {};
-    lc.gridDim = dim3(a.n_cta, D / kJoinCols);
+    lc.gridDim = dim3(a.n_cta, a.d / (few ? 16 : 32));
     lc.blockDim = dim3(kThreads);
     lc.stream = st;
     cudaLaunchAttribute attr[1];
@@ -306,7 +307,7 @@ template <typename T, int D> cudaError_t launch_join(const PagedArgs &a, cudaStr
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     lc.attrs = attr;
     lc.numAttrs = 1;
-    return cudaLaunchKernelEx(&lc, k_paged_join<T, D>, a);
+    return few ? cudaLaunchKernelEx(&lc, k_paged_join<T, 16>, a) : cudaLaunchKernelEx(&lc, k_paged_join<T, 32>, a);
 }
 
 template <int D> cudaError_t launch_f32(const PagedArgs &a, cudaStream_t st)
@@ -319,7 +320,7 @@ template <int D> cudaError_t launch_f32(const PagedArgs &a, cudaStream_t st)
     if (e != cudaSuccess) return e;
     e = cudaLaunchKernel(f, dim3(a.n_cta), dim3(kThreads), args, sizeof(Smem<D>), st);
     if (e != cudaSuccess) return e;
-    return launch_join<float, D>(a, st);
+    return launch_join<float>(a, st);
 }
 
 }  // namespace
@@ -340,9 +341,15 @@ void paged_geometry(const hybrid_cfg &c, PagedArgs &a)
     a.n_cta = (tc ? 1 : 2) * pipe::sm_count();
 }
 
-size_t paged_partial_bytes(const PagedArgs &a)
+size_t paged_workspace_bytes(const PagedArgs &a)
 {
-    return (size_t)2 * a.n_cta * partial_floats(a.Bt * a.Gt, a.d) * sizeof(float);
+    return (size_t)a.n_cta * sizeof(JoinNote) + (size_t)2 * a.n_cta * partial_floats(a.Bt * a.Gt, a.d) * sizeof(float);
+}
+
+void paged_set_workspace(PagedArgs &a, void *workspace)
+{
+    a.notes = static_cast<JoinNote *>(workspace);
+    a.part = reinterpret_cast<float *>(a.notes + a.n_cta);
 }
 
 cudaError_t launch_paged_attn(hybrid_dtype dt, const PagedArgs &a, cudaStream_t st)
@@ -350,7 +357,7 @@ cudaError_t launch_paged_attn(hybrid_dtype dt, const PagedArgs &a, cudaStream_t 
     if (dt == HYBRID_F32) return a.d == 128 ? launch_f32<128>(a, st) : launch_f32<64>(a, st);
     const cudaError_t e = launch_paged_attn_tc(a, st);
     if (e != cudaSuccess) return e;
-    return a.d == 128 ? launch_join<__nv_bfloat16, 128>(a, st) : launch_join<__nv_bfloat16, 64>(a, st);
+    return launch_join<__nv_bfloat16>(a, st);
 }
 
 }  // namespace hyb

@@ -4,19 +4,22 @@
 // A row tile has up to 128 query rows (tokens x query heads of one key head), the
 // M of the products.  For each tile of 128 keys
 //     S = Q K^T          bf16, accumulator in Tensor Memory (two buffers)
-//     p = 2^(S c - ref)  c = log2(e) / sqrt(d); one thread per row
+//     p = 2^(S c - ref)  c = log2(e) / sqrt(d); two threads per row, 64 keys each
 //     O += P V           P bf16 in Tensor Memory, V as the MN-major operand
 // with a running reference per row instead of the running maximum: ref is the
 // maximum when it was last moved, and O and the sum are rescaled only when a
 // row's maximum exceeds it by more than 8, so p <= 2^8 and most tiles touch O
-// with the products alone.
+// with the products alone.  The two threads of a row lie in different warps (a
+// warp reaches one quarter of Tensor Memory's lanes): they agree by one barrier
+// vote per tile that no reference has to move, and exchange maxima only if one has.
 //
 // The cache is read once per row tile by TMA boxes of one page of one head (64
-// features x page_size rows, 128-byte swizzle), which land in a ring of K and V
-// tiles: 5 or 6 slots of 32 KB for d = 128, so that 160 to 192 KB are in flight or
-// in use per SM.  One block per SM walks its share of all requests' tiles
-// (paged_plan.cuh) without a pause between segments: the producer and the MMA
-// issuer run ahead into the next segment.  With few rows (decoding) the tensor
+// features x page_size rows, 128-byte swizzle), which land in a ring of K tiles
+// and one of V tiles: 5 or 6 slots of 32 KB for d = 128, so that 160 to 192 KB are
+// in flight or in use per SM.  (Two rings, because a wait knows a phase by its
+// parity alone: each issuer must itself have seen every phase of its slots.)  One block per SM walks its share of all requests' tiles
+// (paged_plan.cuh) without a pause between segments: the producer and the issuer
+// of S run ahead into the next segment.  With few rows (decoding) the tensor
 // pipe works on padding, which costs nothing here: a tile's products take about
 // 0.6 us, its bytes 1.5 us at an SM's share of the memory bandwidth.
 //
@@ -25,8 +28,9 @@
 // visible one enter the product, their masked rows zeroed in shared memory, so
 // nothing in those places (NaN included) reaches the output.
 //
-// Warps: 0-3 softmax and epilogue (row = thread; warps beyond the rows idle),
-// 4 producer, 5 MMA issuer.  Every wait is bounded (tc_pipeline.cuh).
+// Warps: 0-7 softmax and epilogue (warp w: rows 32 (w % 4) ..., half w / 4 of the
+// keys and of the output's features; warps beyond the rows idle), 8 producer, 9
+// issuer of S, 10 issuer of O.  Every wait is bounded (tc_pipeline.cuh).
 #include <atomic>
 
 #include "paged_plan.cuh"
@@ -38,17 +42,42 @@ namespace {
 using namespace paged;
 using namespace pipe;
 
-constexpr int kThreads = 192;
+constexpr int kParts = 2;                 // threads per row: each has kTile / kParts keys
+constexpr int kSoftWarps = 4 * kParts;
+constexpr int kThreads = 32 * (kSoftWarps + 3);
+constexpr int kProducer = kSoftWarps, kIssueS = kSoftWarps + 1, kIssueO = kSoftWarps + 2;
 constexpr int kSmemLimit = 232448;
 constexpr int kMaxSlots = 12;
+constexpr uint32_t kBarBytes = 1024;      // barriers, TMEM address, failure flag, the plan's scratch
 constexpr float kSlack = 8.f;             // log2 of the largest p
 
 struct TcArgs {
     CUtensorMap tmQ, tmK, tmV;
     PagedArgs p;
-    int NS;                               // ring slots
+    int NK, NV;                           // slots of the K ring, then of the V ring
     uint32_t q_bytes;                     // one Q buffer
     uint32_t off_ring, off_bar, bytes;
+};
+
+// As wait_bar, but reads the timer only after some tries: its latency would delay
+// the common short wait.
+__device__ __forceinline__ bool wait_soon(uint64_t *bar, uint32_t parity, volatile int *fail)
+{
+    for (int i = 0; i < 32; ++i)
+        if (ptx::mbar_try_wait(bar, parity)) return true;
+    return wait_bar(bar, parity, fail);
+}
+
+// Position in a ring: slot and phase of the next item.
+struct RingPos {
+    uint32_t slot, phase;
+    __device__ void step(uint32_t n_slots)
+    {
+        if (++slot == n_slots) {
+            slot = 0;
+            phase ^= 1u;
+        }
+    }
 };
 
 // Whether the 16 keys from j hold a visible one (for pages, `n` keys from j).
@@ -73,13 +102,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_tc(const __grid_cons
     const PagedArgs &a = ta.p;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, NS = ta.NS;
-    const int rows = a.Bt * a.Gt, n_soft = (rows + 31) / 32;   // warps with rows
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, NK = ta.NK, NV = ta.NV;
+    const int rows = a.Bt * a.Gt, n_quads = (rows + 31) / 32;  // quarters of the lanes with rows
+    const int n_soft = n_quads * kParts;                       // softmax warps at work
 
     uint8_t *ring = smem + ta.off_ring;
     uint64_t *bars = reinterpret_cast<uint64_t *>(smem + ta.off_bar);
-    uint64_t *full = bars;               // [NS] the K or V tile has landed
-    uint64_t *empty = full + kMaxSlots;  // [NS] its products are done
+    uint64_t *full = bars;               // [NK + NV] the K or V tile has landed
+    uint64_t *empty = full + kMaxSlots;  // [NK + NV] its products are done
     uint64_t *qfull = empty + kMaxSlots; // [2]
     uint64_t *qempty = qfull + 2;        // [2] the segment's last S is formed
     uint64_t *sready = qempty + 2;       // [2] S is formed
@@ -87,20 +117,21 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_tc(const __grid_cons
     uint64_t *pready = sfree + 2;        // [2] P is written (and O rescaled, V's masked rows zeroed)
     uint64_t *pvdone = pready + 2;       // [2] O includes the tile's P V
     uint64_t *ofree = pvdone + 2;        // the epilogue has read O
-    uint64_t *drained = ofree + 1;       // every MMA has completed
-    uint32_t *tmem_holder = reinterpret_cast<uint32_t *>(drained + 1);
+    uint64_t *drained = ofree + 1;       // [2] every MMA of an issuer has completed
+    uint32_t *tmem_holder = reinterpret_cast<uint32_t *>(drained + 2);
     volatile int *fail = reinterpret_cast<volatile int *>(tmem_holder + 1);
     PlanSmem *plan_smem = reinterpret_cast<PlanSmem *>(tmem_holder + 2);
+    float *exchange = reinterpret_cast<float *>(smem + ta.off_bar + kBarBytes);   // [kParts][128]
 
-    if (warp == 5) {
+    if (warp == kIssueS) {
         tmem_alloc(tmem_holder, 512);
         tmem_relinquish();
     }
-    if (warp == 4 && lane == 0) {
+    if (warp == kProducer && lane == 0) {
         prefetch_tensormap(&ta.tmQ);
         prefetch_tensormap(&ta.tmK);
         prefetch_tensormap(&ta.tmV);
-        for (int i = 0; i < NS; ++i) {
+        for (int i = 0; i < NK + NV; ++i) {
             mbar_init(&full[i], 1);
             mbar_init(&empty[i], 1);
         }
@@ -113,7 +144,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_tc(const __grid_cons
             mbar_init(&pvdone[i], 1);
         }
         mbar_init(ofree, n_soft);
-        mbar_init(drained, 1);
+        mbar_init(&drained[0], 1);
+        mbar_init(&drained[1], 1);
         *fail = 0;
         fence_mbar_init();
     }
@@ -121,31 +153,24 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_tc(const __grid_cons
     griddep_wait();
     griddep_launch_dependents();
     tc_fence_before();
-    const Plan plan = make_plan<kThreads>(a, *plan_smem);  // synchronises the block
+    Walk w;
+    Shares sh(0, 1);
+    const bool work = find_share<kThreads>(a, *plan_smem, w, sh);   // synchronises the block
     tc_fence_after();
     const uint32_t tmem = *tmem_holder;
-    const long long M = units_per_request(a), T_all = plan.total * M;
-    const int C = T_all < a.n_cta ? (int)T_all : a.n_cta;
-    const bool work = (int)blockIdx.x < C;
-    Walk w;
-    if (work) {
-        const long long t0 = share_start(T_all, C, blockIdx.x), t1 = share_start(T_all, C, blockIdx.x + 1);
-        int req;
-        long long before;
-        locate(a, plan, t0, *plan_smem, req, before);
-        w.begin(a, t0, t1, req, before);
-    }
+    const long long M = units_per_request(a);
 
-    if (work && warp == 4) {
+    if (work && warp == kProducer) {
         // ------------------------------------------------------------- producer
         const int P = a.page_size, per = kTile / P;        // pages of a tile
         const uint32_t page_bytes = (uint32_t)P * D * 2;
-        uint32_t q = 0, ns = 0;                            // ring items and segments issued
+        uint32_t n_k = 0, n_v = 0, ns = 0;                 // K and V tiles and segments issued
+        RingPos pos_k{0, 1}, pos_v{0, 1};                  // phases of `empty`: the first round is free
         bool ok = true;
         while (ok && w.next(a, M)) {
             const Unit u = unit_of(a, w.m);
             const uint32_t qb = ns & 1;
-            ok = wait_bar(&qempty[qb], ((ns >> 1) & 1u) ^ 1u, fail);
+            ok = wait_soon(&qempty[qb], ((ns >> 1) & 1u) ^ 1u, fail);
             if (__any_sync(0xffffffffu, !ok)) break;
             if (lane == 0) {
                 const uint32_t panel = ta.q_bytes / kHalves;
@@ -173,8 +198,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_tc(const __grid_cons
                 const uint32_t bytes = page_bytes * __popc(__ballot_sync(0xffffffffu, page >= 0));
 #pragma unroll 1
                 for (int kv = 0; kv < 2; ++kv) {
-                    const int slot = q % NS;
-                    ok = wait_bar(&empty[slot], ((q / NS) & 1u) ^ 1u, fail);
+                    const int slot = kv ? NK + (int)pos_v.slot : (int)pos_k.slot;
+                    ok = wait_soon(&empty[slot], kv ? pos_v.phase : pos_k.phase, fail);
                     if (__any_sync(0xffffffffu, !ok)) {
                         ok = false;
                         break;
@@ -187,111 +212,133 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_tc(const __grid_cons
                         for (int h = 0; h < kHalves; ++h)
                             tma_load_4d(dst + h * kPanel, kv ? &ta.tmV : &ta.tmK, 64 * h, 0, u.head, page, &full[slot]);
                     }
-                    ++q;
+                    if (kv) {
+                        pos_v.step(NV);
+                        ++n_v;
+                    } else {
+                        pos_k.step(NK);
+                        ++n_k;
+                    }
                 }
                 if (!ok) break;
             }
         }
         if (*fail && lane == 0) {
             // let copies in flight land before the block exits
-            for (int s = 0; s < NS; ++s) {
-                const uint32_t n = q / NS + ((uint32_t)s < q % NS ? 1u : 0u);
-                if (n) mbar_wait(&full[s], (n - 1) & 1u, kWaitNs);
-            }
-            for (uint32_t s = 0; s < 2; ++s) {
-                const uint32_t n = ns / 2 + (s < ns % 2 ? 1u : 0u);
-                if (n) mbar_wait(&qfull[s], (n - 1) & 1u, kWaitNs);
-            }
-        }
-    } else if (work && warp == 5) {
-        // ----------------------------------------------------------- MMA issuer
-        if (lane == 0) {
-            const uint32_t id_s = instr_desc(FMT_BF16, FMT_BF16, false, false, 128, kTile);
-            const uint32_t id_o = instr_desc(FMT_BF16, FMT_BF16, false, true, 128, D);
-            const uint32_t ring_u = smem_u32(ring), q_u = smem_u32(smem), q_panel = ta.q_bytes / kHalves;
-            uint32_t n = 0, seg = 0;                       // tiles and segments whose S was issued
-            // the tile whose P V is still to be issued
-            bool have = false, pv_first = false, pv_last = false;
-            uint32_t pv_n = 0, pv_seg = 0, pv_groups = 0;
-            // O += P V of the pending tile
-            auto issue_pv = [&]() -> bool {
-                const uint32_t b = pv_n & 1, item = 2 * pv_n + 1, slot = item % NS;
-                // O is overwritten by a segment's first product: the last epilogue has read it
-                if (pv_first && pv_seg > 0 && !wait_bar(ofree, (pv_seg - 1) & 1u, fail)) return false;
-                if (!wait_bar(&pready[b], (pv_n >> 1) & 1u, fail)) return false;
-                if (!wait_bar(&full[slot], (item / NS) & 1u, fail)) return false;
-                tc_fence_after();
-                uint32_t acc = pv_first ? 0u : 1u;
-                for (int g = 0; g < kTile / 16; ++g) {
-                    if (!(pv_groups >> g & 1u)) continue;
-                    const uint64_t bv = smem_desc(ring_u + slot * kSlot + g * 2048, kPanel, 1024, SWZ_128B);
-                    mma_bf16_ts(tmem + cO, tmem + cP + 64 * b + 8 * g, bv, id_o, acc);
-                    acc = 1;
+            auto land = [&](uint64_t *bar, uint32_t slots, uint32_t items) {
+                for (uint32_t s = 0; s < slots; ++s) {
+                    const uint32_t n = items / slots + (s < items % slots ? 1u : 0u);
+                    if (n) mbar_wait(&bar[s], (n - 1) & 1u, kWaitNs);
                 }
-                mma_commit(&empty[slot]);
-                mma_commit(&pvdone[b]);
-                return true;
             };
+            land(full, NK, n_k);
+            land(full + NK, NV, n_v);
+            land(qfull, 2, ns);
+        }
+    } else if (work && warp == kIssueS) {
+        // ------------------------------------------------------ issuer of S = Q K^T
+        if (lane == 0) {
+            const uint32_t id = instr_desc(FMT_BF16, FMT_BF16, false, false, 128, kTile);
+            const uint64_t q_desc = smem_desc(smem_u32(smem), 16, 1024, SWZ_128B);
+            const uint64_t k_desc = smem_desc(smem_u32(ring), 16, 1024, SWZ_128B);
+            const uint32_t q_panel = ta.q_bytes / kHalves;
+            uint32_t n = 0, seg = 0;                       // tiles and segments so far
+            RingPos pos{0, 0};
             bool ok = true;
             while (ok && w.next(a, M)) {
                 const uint32_t qb = seg & 1;
-                ok = wait_bar(&qfull[qb], (seg >> 1) & 1u, fail);
-                for (int i = w.i0; ok && i < w.i1; ++i) {
-                    const uint32_t b = n & 1, item = 2 * n, slot = item % NS;
-                    if (!wait_bar(&sfree[b], ((n >> 1) & 1u) ^ 1u, fail) ||
-                        !wait_bar(&full[slot], (item / NS) & 1u, fail)) {
-                        ok = false;
-                        break;
-                    }
+                const uint64_t aq = q_desc + qb * (ta.q_bytes >> 4);
+                ok = wait_soon(&qfull[qb], (seg >> 1) & 1u, fail);
+                for (int i = w.i0; ok && i < w.i1; ++i, ++n) {
+                    const uint32_t b = n & 1;
+                    ok = wait_soon(&sfree[b], ((n >> 1) & 1u) ^ 1u, fail) && wait_soon(&full[pos.slot], pos.phase, fail);
+                    if (!ok) break;
                     tc_fence_after();
+                    const uint64_t bk = k_desc + pos.slot * (kSlot >> 4);
 #pragma unroll
-                    for (int k = 0; k < D / 16; ++k) {
-                        const uint64_t aq =
-                            smem_desc(q_u + qb * ta.q_bytes + (k >> 2) * q_panel + (k & 3) * 32, 16, 1024, SWZ_128B);
-                        const uint64_t bk =
-                            smem_desc(ring_u + slot * kSlot + (k >> 2) * kPanel + (k & 3) * 32, 16, 1024, SWZ_128B);
-                        mma_bf16_ss(tmem + cS + 128 * b, aq, bk, id_s, k > 0);
-                    }
-                    mma_commit(&empty[slot]);
+                    for (int k = 0; k < D / 16; ++k)
+                        mma_bf16_ss(tmem + cS + 128 * b, aq + (k >> 2) * (q_panel >> 4) + (k & 3) * 2,
+                                    bk + (k >> 2) * (kPanel >> 4) + (k & 3) * 2, id, k > 0);
                     mma_commit(&sready[b]);
+                    mma_commit(&empty[pos.slot]);
                     if (i + 1 == w.i1) mma_commit(&qempty[qb]);
-                    if (have) ok = issue_pv();
-                    const int j = key_tile(w.vis, i) * kTile;
-                    pv_groups = 0;
-                    for (int g = 0; g < kTile / 16; ++g)
-                        pv_groups |= (any_visible(w.vis, j + 16 * g, 16) ? 1u : 0u) << g;
-                    have = true;
-                    pv_first = i == w.i0;
-                    pv_n = n++;
-                    pv_seg = seg;
+                    pos.step(NK);
                 }
                 ++seg;
             }
-            if (ok && have) issue_pv();
-            mma_commit(drained);
-            mbar_wait(drained, 0, kWaitNs);
-            (void)pv_last;
+            mma_commit(&drained[0]);
+            mbar_wait(&drained[0], 0, kWaitNs);
         }
-    } else if (work && warp < n_soft) {
+    } else if (work && warp == kIssueO) {
+        // ------------------------------------------------------ issuer of O += P V
+        if (lane == 0) {
+            const uint32_t id = instr_desc(FMT_BF16, FMT_BF16, false, true, 128, D);
+            const uint64_t v_desc = smem_desc(smem_u32(ring), kPanel, 1024, SWZ_128B);
+            uint32_t n = 0, seg = 0;
+            RingPos pos{0, 0};
+            bool ok = true;
+            while (ok && w.next(a, M)) {
+                // O is overwritten by a segment's first product: the last epilogue has read it
+                if (seg > 0) ok = wait_soon(ofree, (seg - 1) & 1u, fail);
+                for (int i = w.i0; ok && i < w.i1; ++i, ++n) {
+                    const uint32_t b = n & 1;
+                    const int j = key_tile(w.vis, i) * kTile;
+                    ok = wait_soon(&full[NK + pos.slot], pos.phase, fail) && wait_soon(&pready[b], (n >> 1) & 1u, fail);
+                    if (!ok) break;
+                    tc_fence_after();
+                    const uint64_t bv = v_desc + (NK + pos.slot) * (kSlot >> 4);
+                    if (all_visible(w.vis, j)) {
+#pragma unroll
+                        for (int g = 0; g < kTile / 16; ++g)
+                            mma_bf16_ts(tmem + cO, tmem + cP + 64 * b + 8 * g, bv + g * (2048 >> 4), id,
+                                        g > 0 || i > w.i0);
+                    } else {
+                        uint32_t acc = i > w.i0;
+                        for (int g = 0; g < kTile / 16; ++g) {
+                            if (!any_visible(w.vis, j + 16 * g, 16)) continue;
+                            mma_bf16_ts(tmem + cO, tmem + cP + 64 * b + 8 * g, bv + g * (2048 >> 4), id, acc);
+                            acc = 1;
+                        }
+                    }
+                    mma_commit(&pvdone[b]);
+                    mma_commit(&empty[NK + pos.slot]);
+                    pos.step(NV);
+                }
+                ++seg;
+            }
+            mma_commit(&drained[1]);
+            mbar_wait(&drained[1], 0, kWaitNs);
+        }
+    } else if (work && (warp & 3) < n_quads) {
         // --------------------------------------------------- softmax, epilogue
-        const int row = tid;
-        const uint32_t lane_off = (uint32_t)(32 * warp) << 16;
+        constexpr int kKeys = kTile / kParts, kFeat = D / kParts;   // this thread's keys and features
+        const int quad = warp & 3, part = warp >> 2, row = 32 * quad + lane;
+        const int worker = 32 * (part * n_quads + quad) + lane;     // among the threads at work
+        const uint32_t lane_off = (uint32_t)(32 * quad) << 16;
+        const uint32_t pair_bar = 1 + quad;                         // the kParts warps of these rows
         const float to_log2 = kLog2e * rsqrtf((float)D);
+        float *mine = exchange + part * 128 + row, *row_x = exchange + row;
         uint32_t n = 0;                                    // tiles so far
-        bool ok = true;
-        while (ok && w.next(a, M)) {
+        bool bad = false;                                  // a wait gave up: leave at the next vote
+        auto wait = [&](uint64_t *bar, uint32_t parity) {
+            bad = __any_sync(0xffffffffu, bad || !wait_soon(bar, parity, fail));
+        };
+        while (w.next(a, M)) {              // left by a vote only, so that the warps of a row stay together
             const Unit u = unit_of(a, w.m);
-            float ref = -INFINITY, l = 0.f;
+            float ref = 0.f, l2[2] = {0.f, 0.f};           // the row's sum over this thread's keys, in two
+            bool left = false;
             for (int i = w.i0; i < w.i1; ++i, ++n) {
                 const uint32_t b = n & 1;
                 const int j0 = key_tile(w.vis, i) * kTile;
-                const bool edge = !all_visible(w.vis, j0);
+                const bool edge = !all_visible(w.vis, j0), first = i == w.i0;
                 if (edge) {
-                    // masked rows of V in the groups that enter the product
-                    const uint32_t item = 2 * n + 1, slot = item % NS;
-                    ok = wait_bar(&full[slot], (item / NS) & 1u, fail);
-                    if (__any_sync(0xffffffffu, !ok)) { ok = false; break; }
-                    for (int c = tid; c < kTile; c += 32 * n_soft) {
+                    // masked rows of V in the groups that enter the product.  (An earlier
+                    // tile's product first, so that the slot's last item has landed and the
+                    // wait cannot take its phase for this one's.)
+                    if (n >= 2) wait(&pvdone[b], ((n - 2) >> 1) & 1u);
+                    const uint32_t slot = NK + n % NV;
+                    wait(&full[slot], (n / NV) & 1u);
+                    for (int c = worker; c < kTile; c += 32 * n_soft) {
                         const int j = j0 + c;
                         if (!key_visible(w.vis, j) && any_visible(w.vis, j & ~15, 16)) {
 #pragma unroll
@@ -302,58 +349,69 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_tc(const __grid_cons
                     }
                     fence_proxy_async_smem();
                 }
-                ok = wait_bar(&sready[b], (n >> 1) & 1u, fail);
-                if (__any_sync(0xffffffffu, !ok)) { ok = false; break; }
+                wait(&sready[b], (n >> 1) & 1u);
                 tc_fence_after();
-                float s[4][32];
+                float s[kKeys / 32][32];
 #pragma unroll
-                for (int x = 0; x < 4; ++x) tmem_ld32(tmem + cS + 128 * b + 32 * x + lane_off, s[x]);
+                for (int x = 0; x < kKeys / 32; ++x)
+                    tmem_ld32(tmem + cS + 128 * b + kKeys * part + 32 * x + lane_off, s[x]);
                 tmem_wait_ld();
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&sfree[b]);
                 if (edge) {
 #pragma unroll
-                    for (int x = 0; x < 4; ++x)
+                    for (int x = 0; x < kKeys / 32; ++x)
 #pragma unroll
                         for (int y = 0; y < 32; ++y)
-                            if (!key_visible(w.vis, j0 + 32 * x + y)) s[x][y] = -INFINITY;
+                            if (!key_visible(w.vis, j0 + kKeys * part + 32 * x + y)) s[x][y] = -INFINITY;
                 }
-                float mx = -INFINITY;
+                float mx4[4] = {s[0][0], s[0][1], s[0][2], s[0][3]};
 #pragma unroll
-                for (int x = 0; x < 4; ++x)
+                for (int x = 0; x < kKeys / 32; ++x)
 #pragma unroll
-                    for (int y = 0; y < 32; ++y) mx = fmaxf(mx, s[x][y]);
-                mx *= to_log2;
+                    for (int y = 0; y < 32; ++y) mx4[y & 3] = fmaxf(mx4[y & 3], s[x][y]);
+                float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])) * to_log2;
+                bool rescale = false;
                 float f = 1.f;
-                if (i == w.i0) {
-                    ref = mx == -INFINITY ? 0.f : mx;
-                } else if (mx > ref + kSlack) {
-                    f = ex2(ref - mx);
-                    ref = mx;
+                if (group_sync_failed(pair_bar, 32 * kParts, bad || first || (row < rows && mx > ref + kSlack))) {
+                    *mine = mx;
+                    if (group_sync_failed(pair_bar, 32 * kParts, bad)) {
+                        left = true;
+                        break;
+                    }
+#pragma unroll
+                    for (int x = 0; x < kParts; ++x) mx = fmaxf(mx, row_x[x * 128]);
+                    if (first) {
+                        ref = mx == -INFINITY ? 0.f : mx;
+                    } else if (mx > ref + kSlack) {
+                        f = ex2(ref - mx);
+                        ref = mx;
+                    }
+                    rescale = __any_sync(0xffffffffu, row < rows && f != 1.f);
                 }
-                const bool rescale = __any_sync(0xffffffffu, row < rows && f != 1.f);
                 // P's buffer is free, and O is at rest, once earlier products are done
                 if (rescale || n >= 2) {
                     const uint32_t k = rescale ? n - 1 : n - 2;
-                    ok = wait_bar(&pvdone[k & 1], (k >> 1) & 1u, fail);
-                    if (__any_sync(0xffffffffu, !ok)) { ok = false; break; }
+                    wait(&pvdone[k & 1], (k >> 1) & 1u);
                     tc_fence_after();
                 }
                 if (rescale) {
-                    l *= f;
+                    l2[0] *= f;
+                    l2[1] *= f;
 #pragma unroll 1
-                    for (int x = 0; x < D / 32; ++x) {
+                    for (int x = 0; x < kFeat / 32; ++x) {
+                        const uint32_t at = tmem + cO + kFeat * part + 32 * x + lane_off;
                         float o[32];
-                        tmem_ld32(tmem + cO + 32 * x + lane_off, o);
+                        tmem_ld32(at, o);
                         tmem_wait_ld();
 #pragma unroll
                         for (int y = 0; y < 32; ++y) o[y] *= f;
-                        tmem_st32(tmem + cO + 32 * x + lane_off, o);
+                        tmem_st32(at, o);
                     }
                 }
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
+                for (int h = 0; h < kKeys / 64; ++h) {
                     float p[32];                           // pairs of bf16
 #pragma unroll
                     for (int x = 0; x < 2; ++x)
@@ -361,39 +419,45 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_tc(const __grid_cons
                         for (int y = 0; y < 32; y += 2) {
                             const float p0 = ex2(fmaf(s[2 * h + x][y], to_log2, -ref));
                             const float p1 = ex2(fmaf(s[2 * h + x][y + 1], to_log2, -ref));
-                            l += p0 + p1;
+                            l2[0] += p0;
+                            l2[1] += p1;
                             p[16 * x + y / 2] = __uint_as_float(pack_bf16x2(p0, p1));
                         }
-                    tmem_st32(tmem + cP + 64 * b + 32 * h + lane_off, p);
+                    tmem_st32(tmem + cP + 64 * b + (kKeys / 2) * part + 32 * h + lane_off, p);
                 }
                 tmem_wait_st();
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&pready[b]);
+                if (lane == 0 && !bad) mbar_arrive(&pready[b]);
             }
-            if (!ok) break;
-            // the segment's output
-            ok = wait_bar(&pvdone[(n - 1) & 1], ((n - 1) >> 1) & 1u, fail);
-            if (__any_sync(0xffffffffu, !ok)) { ok = false; break; }
+            if (left) break;
+            // the segment's output: the row's sum from its threads, then O
+            group_sync_failed(pair_bar, 32 * kParts, false);       // the exchanged maxima have been read
+            *mine = l2[0] + l2[1];
+            group_sync_failed(pair_bar, 32 * kParts, false);
+            float l = 0.f;
+#pragma unroll
+            for (int x = 0; x < kParts; ++x) l += row_x[x * 128];
+            wait(&pvdone[(n - 1) & 1], ((n - 1) >> 1) & 1u);
             tc_fence_after();
             size_t at;
-            const bool live = row_at(a, w.req, u, row, at), whole = w.whole();
-            bf16 *out = static_cast<bf16 *>(a.O) + at;
-            float *part = a.part + (size_t)(2 * blockIdx.x + (w.at_start ? 0 : 1)) * partial_floats(rows, D);
+            const bool live = row_at(a, w.req, u, row, at) && !bad, whole = w.whole();
+            bf16 *out = static_cast<bf16 *>(a.O) + at + kFeat * part;
+            float *partial = a.part + w.slot() * partial_floats(rows, D);
             const float inv = 1.f / l;
-            if (!whole && row < rows) {
-                part[row] = ref;
-                part[rows + row] = l;
+            if (!whole && row < rows && part == 0) {
+                partial[row] = ref;
+                partial[rows + row] = l;
             }
 #pragma unroll 1
-            for (int x = 0; x < D / 32; ++x) {
+            for (int x = 0; x < kFeat / 32; ++x) {
                 float o[32];
-                tmem_ld32(tmem + cO + 32 * x + lane_off, o);
+                tmem_ld32(tmem + cO + kFeat * part + 32 * x + lane_off, o);
                 tmem_wait_ld();
-                if (x == D / 32 - 1) {
+                if (x == kFeat / 32 - 1) {
                     tc_fence_before();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(ofree);
+                    if (lane == 0 && !bad) mbar_arrive(ofree);
                 }
                 if (whole) {
                     if (live) {
@@ -404,16 +468,19 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_tc(const __grid_cons
                                 pack_bf16x2(o[y + 4] * inv, o[y + 5] * inv), pack_bf16x2(o[y + 6] * inv, o[y + 7] * inv));
                     }
                 } else if (row < rows) {
-                    float *po = part + 2 * rows + (size_t)(32 * x) * rows + row;
+                    float *po = partial + 2 * rows + (size_t)(kFeat * part + 32 * x) * rows + row;
 #pragma unroll
                     for (int y = 0; y < 32; ++y) po[(size_t)y * rows] = o[y];
                 }
             }
         }
         if (tid == 0 && *fail) raise_error(a.err, ERR_WAIT_TIMEOUT);
+        if (worker == 0) write_note(a, true, w, sh);
     }
+    if (!work && tid == 0) write_note(a, false, w, sh);
+    write_empty<bf16, kThreads>(a, tid);
     __syncthreads();
-    if (warp == 5) {
+    if (warp == kIssueS) {
         tc_fence_after();
         tmem_dealloc(tmem, 512);
     }
@@ -424,15 +491,16 @@ template <int D> cudaError_t launch(const PagedArgs &a, cudaStream_t st)
     TcArgs ta;
     ta.p = a;
     const int rows = a.Bt * a.Gt;
-    // Q buffers (two), K/V ring, barriers and the plan's scratch
+    // Q buffers (two), K/V ring, barriers, exchange, and 1 KB for alignment
     ta.q_bytes = (uint32_t)((rows + 7) / 8) * 1024 * (D / 64);
-    const uint32_t bar_bytes = 1024, slot = kTile * D * 2;
-    int ns = (int)((kSmemLimit - 1024 - bar_bytes - 2 * ta.q_bytes) / slot);
+    const uint32_t tail = kBarBytes + kParts * 128 * sizeof(float) + 1024, slot = kTile * D * 2;
+    int ns = (int)((kSmemLimit - tail - 2 * ta.q_bytes) / slot);
     if (ns > kMaxSlots) ns = kMaxSlots;
-    ta.NS = ns;
+    ta.NK = (ns + 1) / 2;
+    ta.NV = ns / 2;
     ta.off_ring = 2 * ta.q_bytes;
     ta.off_bar = ta.off_ring + ns * slot;
-    ta.bytes = ta.off_bar + bar_bytes + 1024;
+    ta.bytes = ta.off_bar + tail;
     {
         const cuuint64_t dq[4] = {(cuuint64_t)D, (cuuint64_t)a.Hq, (cuuint64_t)a.B, (cuuint64_t)a.n_req};
         const cuuint64_t sq[3] = {(cuuint64_t)D * 2, (cuuint64_t)a.Hq * D * 2, (cuuint64_t)a.B * a.Hq * D * 2};

@@ -14,7 +14,9 @@
 // the output; any other writes (m, l, O) -- running maximum in units of log2,
 // sum and unnormalised output -- to partial 2 c (segment at the start of the
 // block's share) or 2 c + 1 (a later one: only a block's last segment can be cut
-// there).  A second launch joins them.
+// there).  A second launch joins them, told by notes what to join.
+//
+// Workspace: n_cta notes, then 2 n_cta partials.
 #pragma once
 
 #include "hybrid_common.cuh"
@@ -57,12 +59,39 @@ __device__ __forceinline__ bool key_visible(const Visible &v, int j) { return j 
 
 __device__ __forceinline__ int units_per_request(const PagedArgs &a) { return a.Hkv * a.n_gt * a.n_bt; }
 
-// First tile of block c of C.
-__device__ __forceinline__ long long share_start(long long T, int C, int c) { return T * c / C; }
+// Shares of T tiles over C blocks (C <= T): the first T % C blocks take one more.
+struct Shares {
+    long long per, rem;
+    int C;
+    __device__ Shares(long long T, int n_cta)
+    {
+        C = T < n_cta ? (int)T : n_cta;
+        const bool small = T < 0x7fffffffll;                // the usual case, with 32-bit division
+        per = C == 0 ? 0 : (small ? (long long)((unsigned)T / (unsigned)C) : T / C);
+        rem = T - per * C;
+    }
+    __device__ long long start(int c) const { return per * c + (c < rem ? c : rem); }
+    // block of a tile
+    __device__ int block_of(long long t) const
+    {
+        const long long big = rem * (per + 1);
+        return (int)(t < big ? t / (per + 1) : rem + (t - big) / per);
+    }
+};
+
+// What the join does at the boundary between blocks c and c + 1: written by block c
+// when its last segment is the first part of a unit that later blocks go on with.
+struct JoinNote {
+    int cut;               // 0: nothing to join
+    int req, m;            // the unit
+    int last;              // block of its last tile; blocks c + 1 ... last hold partial 2 b
+    int slot;              // block c's partial
+    int pad[3];
+};
 
 // Scratch of the scan: one long per warp and the answer.
 struct PlanSmem {
-    long long warp[32];
+    long long warp[16];
     long long total;
     int req;
     long long before;
@@ -169,7 +198,50 @@ struct Walk {
         return true;
     }
     __device__ bool whole() const { return i0 == 0 && i1 == vis.tiles; }
+    __device__ int slot() const { return 2 * (int)blockIdx.x + (at_start ? 0 : 1); }
 };
+
+// Find a block's share; false if it has none.  For the whole block.
+template <int NT>
+__device__ __forceinline__ bool find_share(const PagedArgs &a, PlanSmem &s, Walk &w, Shares &sh)
+{
+    const Plan plan = make_plan<NT>(a, s);
+    sh = Shares(plan.total * units_per_request(a), a.n_cta);
+    if ((int)blockIdx.x >= sh.C) return false;
+    const long long t0 = sh.start(blockIdx.x);
+    int req;
+    long long before;
+    locate(a, plan, t0, s, req, before);
+    w.begin(a, t0, sh.start(blockIdx.x + 1), req, before);
+    return true;
+}
+
+// The note of this block, from its last segment (one thread).
+__device__ __forceinline__ void write_note(const PagedArgs &a, bool work, const Walk &w, const Shares &sh)
+{
+    JoinNote n{};
+    if (work && w.i0 == 0 && w.i1 < w.vis.tiles) {
+        n.cut = 1;
+        n.req = w.req;
+        n.m = w.m;
+        n.last = sh.block_of(w.t - w.i1 + w.vis.tiles - 1);
+        n.slot = w.slot();
+    }
+    a.notes[blockIdx.x] = n;
+}
+
+// Zeros for the requests without a visible key, shared over the blocks.
+template <typename T, int NT>
+__device__ __forceinline__ void write_empty(const PagedArgs &a, int thread)
+{
+    for (int r = blockIdx.x; r < a.n_req; r += gridDim.x) {
+        if (visible_keys(a, __ldg(a.lens + r)).tiles > 0) continue;
+        constexpr int kPer = 16 / sizeof(T);
+        uint4 *out = reinterpret_cast<uint4 *>(static_cast<T *>(a.O) + (size_t)r * a.B * a.Hq * a.d);
+        const int n = a.B * a.Hq * a.d / kPer;
+        for (int x = thread; x < n; x += NT) out[x] = make_uint4(0, 0, 0, 0);
+    }
+}
 
 // Unit m of a request: key head, first query head of the group, first token.
 struct Unit {

@@ -242,7 +242,7 @@ size_t hybrid_paged_attn_workspace_bytes(const hybrid_cfg *cfg, const hybrid_pag
     if (cfg->block_size < 1 || cfg->block_size > 128) return 0;
     hyb::PagedArgs a{};
     hyb::paged_geometry(*cfg, a);
-    return hyb::paged_partial_bytes(a);
+    return hyb::paged_workspace_bytes(a);
 }
 
 hybrid_status hybrid_paged_attn(const hybrid_cfg *cfg, const hybrid_page_cfg *pg, const void *Q,
@@ -263,7 +263,7 @@ hybrid_status hybrid_paged_attn(const hybrid_cfg *cfg, const hybrid_page_cfg *pg
         return HYBRID_ERR_INVALID_ARG;
     hyb::PagedArgs a{};
     hyb::paged_geometry(*cfg, a);
-    if (workspace_bytes < hyb::paged_partial_bytes(a)) return HYBRID_ERR_INVALID_ARG;
+    if (workspace_bytes < hyb::paged_workspace_bytes(a)) return HYBRID_ERR_INVALID_ARG;
     unsigned *err = hyb::error_word();
     if (!err) return HYBRID_ERR_CUDA;
     a.Q = Q;
@@ -272,7 +272,7 @@ hybrid_status hybrid_paged_attn(const hybrid_cfg *cfg, const hybrid_page_cfg *pg
     a.table = block_table;
     a.lens = kv_len;
     a.O = O;
-    a.part = static_cast<float *>(workspace);
+    hyb::paged_set_workspace(a, workspace);
     a.n_req = n_req;
     a.page_size = pg->page_size;
     a.n_pages = pg->n_pages;

@@ -43,11 +43,15 @@ cudaError_t launch_qk_norm_rope_backward(hybrid_dtype dt, const RopeArgs &a, cud
 size_t qk_norm_rope_partial_bytes(int d, int n_tok);
 
 // paged_attn.cu (float32, and the join of split requests), paged_attn_tc.cu (bfloat16)
+namespace paged {
+struct JoinNote;
+}
 struct PagedArgs {
     const void *Q, *K, *V;
     const int *table, *lens;
     void *O;
-    float *part;                      // partial results, see paged_plan.cuh
+    paged::JoinNote *notes;           // workspace, see paged_plan.cuh
+    float *part;
     int n_req, B, Hq, Hkv, G, d;
     int page_size, n_pages, max_pages, window, sink;
     // a row tile is Bt tokens x Gt query heads of one key head
@@ -55,9 +59,10 @@ struct PagedArgs {
     int n_cta;                        // blocks that share the tiles
     unsigned *err;
 };
-// Geometry (row tiles, number of blocks) of a call; part and pointers left to the caller.
+// Geometry (row tiles, number of blocks) of a call; pointers left to the caller.
 void paged_geometry(const hybrid_cfg &c, PagedArgs &a);
-size_t paged_partial_bytes(const PagedArgs &a);
+size_t paged_workspace_bytes(const PagedArgs &a);
+void paged_set_workspace(PagedArgs &a, void *workspace);
 cudaError_t launch_paged_attn_tc(const PagedArgs &a, cudaStream_t st);   // bfloat16, without the join
 cudaError_t launch_paged_attn(hybrid_dtype dt, const PagedArgs &a, cudaStream_t st);
 
