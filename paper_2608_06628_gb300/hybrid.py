@@ -148,17 +148,25 @@ def make_cfg(head_dim, feat_dim, n_q_heads, n_kv_heads, block_size, io_dtype) ->
 
 
 def _ptr(x):
-    if x is None:
-        return None
-    if isinstance(x, int):
+    if x is None or type(x) is int:
         return x
     return x.data_ptr()
 
 
+_raw_stream = None
+
+
 def _stream(stream):
+    """The raw stream to launch on; None is torch's current stream of the current device."""
+    global _raw_stream
     if stream is None:
-        import torch
-        return torch.cuda.current_stream().cuda_stream
+        if _raw_stream is None:
+            import torch
+            torch.cuda.current_stream()      # initialises CUDA, or raises without a device
+            get, device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+            # (building torch's stream object would take longer than the launch)
+            _raw_stream = lambda: get(device())  # noqa: E731
+        return _raw_stream()
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
