@@ -18,6 +18,7 @@
 // another), so no block waits on another.
 #include "hybrid_common.cuh"
 #include "softmax_kernels.h"
+#include "tc_pipeline.cuh"
 
 namespace hyb {
 namespace {
@@ -60,6 +61,9 @@ __device__ Scan2 block_scan(Scan2 v, Scan2 &total, Scan2 *warp_sums)
     return {before.a + inc.a - v.a, before.b + inc.b - v.b};
 }
 
+// Pages of a context of len tokens.
+__device__ __forceinline__ long long pages_of(long long len, int lg) { return (len + (1ll << lg) - 1) >> lg; }
+
 // The ring's head and count, or an empty ring if they are out of range.
 __device__ bool load_ring(const int *ring, int n_pages, int &head, int &count)
 {
@@ -73,7 +77,7 @@ __device__ bool load_ring(const int *ring, int n_pages, int &head, int &count)
 struct AppendArgs {
     const int *lens, *n_new, *free_pages, *ring_in;
     int *table, *slots, *positions, *tok_offsets, *lens_out, *ring_out;
-    int n_req, n_slots, P, n_pages, max_pages;
+    int n_req, n_slots, lg, n_pages, max_pages;   // page size 1 << lg
     unsigned *err;
 };
 
@@ -85,6 +89,8 @@ __global__ __launch_bounds__(kThreads) void k_page_append(const AppendArgs a)
     __shared__ Scan2 s_warp[kThreads / 32];
     __shared__ int s_taken;
     const int tid = threadIdx.x;
+    ptx::griddep_wait();
+    ptx::griddep_launch_dependents();
     int head, count;
     const bool ring_ok = load_ring(a.ring_in, a.n_pages, head, count);
     bool bad = !ring_ok;
@@ -109,8 +115,8 @@ __global__ __launch_bounds__(kThreads) void k_page_append(const AppendArgs a)
                 len[i] = a.lens[r];
                 nw[i] = a.n_new[r];
                 const long long end = (long long)len[i] + nw[i];
-                valid[i] = len[i] >= 0 && nw[i] >= 0 && end <= (long long)a.max_pages * a.P;
-                if (valid[i]) need[i] = (int)((end + a.P - 1) / a.P - ((long long)len[i] + a.P - 1) / a.P);
+                valid[i] = len[i] >= 0 && nw[i] >= 0 && end <= ((long long)a.max_pages << a.lg);
+                if (valid[i]) need[i] = (int)(pages_of(end, a.lg) - pages_of(len[i], a.lg));
                 if (nw[i] < 0) nw[i] = 0;
             }
             sum.a += nw[i];
@@ -159,17 +165,17 @@ __global__ __launch_bounds__(kThreads) void k_page_append(const AppendArgs a)
             int slot = -1, pos = 0;
             if (s_served[x]) {
                 pos = p;
-                const int j = p / a.P, old = (s_len[x] + a.P - 1) / a.P;
+                const int j = p >> a.lg, old = (int)pages_of(s_len[x], a.lg), in_page = p & ((1 << a.lg) - 1);
                 int page;
                 int *entry = a.table + (size_t)(r0 + x) * a.max_pages + j;
                 if (j >= old) {
                     const long long i = (long long)head + s_page[x] + (j - old);
                     page = a.free_pages[i < a.n_pages ? i : i - a.n_pages];
-                    if (p % a.P == 0) *entry = page;        // its first token is always a new one
+                    if (in_page == 0) *entry = page;        // its first token is always a new one
                 } else {
                     page = *entry;
                 }
-                if (page >= 0 && page < a.n_pages) slot = page * a.P + p % a.P;
+                if (page >= 0 && page < a.n_pages) slot = (page << a.lg) + in_page;
                 else bad = true;
             }
             a.slots[t] = slot;
@@ -197,7 +203,7 @@ __global__ __launch_bounds__(kThreads) void k_page_append(const AppendArgs a)
 struct ReleaseArgs {
     const int *rows, *lens, *table, *ring_in;
     int *free_pages, *ring_out;
-    int n_req, n_rows, P, n_pages, max_pages;
+    int n_req, n_rows, lg, n_pages, max_pages;
     unsigned *err;
 };
 
@@ -209,6 +215,8 @@ __global__ __launch_bounds__(kThreads) void k_page_release(const ReleaseArgs a)
     __shared__ long long s_first[kChunk + 1];
     __shared__ Scan2 s_warp[kThreads / 32];
     const int tid = threadIdx.x;
+    ptx::griddep_wait();
+    ptx::griddep_launch_dependents();
     int head, count;
     const bool ring_ok = load_ring(a.ring_in, a.n_pages, head, count);
     const long long room = ring_ok ? a.n_pages - count : 0;
@@ -226,8 +234,8 @@ __global__ __launch_bounds__(kThreads) void k_page_release(const ReleaseArgs a)
                 const int r = a.rows[i0 + l];
                 const bool row_ok = r >= 0 && r < a.n_req;
                 const int len = row_ok ? a.lens[r] : -1;
-                const bool ok = len >= 0 && len <= (long long)a.max_pages * a.P;
-                if (ok) k[i] = (int)(((long long)len + a.P - 1) / a.P);
+                const bool ok = len >= 0 && len <= ((long long)a.max_pages << a.lg);
+                if (ok) k[i] = (int)pages_of(len, a.lg);
                 s_row[l] = ok ? r : 0;
                 bad |= !ok;
             }
@@ -260,7 +268,8 @@ __global__ __launch_bounds__(kThreads) void k_page_release(const ReleaseArgs a)
                 }
                 const int page = a.table[(size_t)s_row[x] * a.max_pages + (size_t)(i - s_first[x])];
                 if (page < 0 || page >= a.n_pages) bad = true;
-                a.free_pages[((long long)head + count + i) % a.n_pages] = page;
+                const long long to = (long long)head + count + i;      // < 2 n_pages
+                a.free_pages[to < a.n_pages ? to : to - a.n_pages] = page;
             }
         }
         __syncthreads();
@@ -273,11 +282,18 @@ __global__ __launch_bounds__(kThreads) void k_page_release(const ReleaseArgs a)
     if (bad) raise_error(a.err, ERR_BAD_INDEX);
 }
 
-// Enough blocks for about 2048 items each, at most two waves of the GPU.
+// A thread per item while that takes no more blocks than the GPU holds at once.
 int blocks_for(long long items)
 {
-    const long long n = (items + 2047) / 2048;
-    return (int)(n < 1 ? 1 : (n > 304 ? 304 : n));
+    const long long n = (items + kThreads - 1) / kThreads;
+    return (int)(n < 1 ? 1 : (n > 608 ? 608 : n));
+}
+
+int log2_of(int page_size)
+{
+    int lg = 0;
+    while ((1 << lg) < page_size) ++lg;
+    return lg;
 }
 
 }  // namespace
@@ -288,10 +304,8 @@ cudaError_t launch_page_append(const hybrid_page_cfg &pg, int n_req, const int *
                                unsigned *err, cudaStream_t st)
 {
     AppendArgs a{lens,      n_new,    free_pages, ring_in, block_table,  slots,      positions,    tok_offsets,
-                 lens_out,  ring_out, n_req,      n_slots, pg.page_size, pg.n_pages, pg.max_pages, err};
-    void *args[] = {&a};
-    return cudaLaunchKernel(reinterpret_cast<const void *>(&k_page_append), dim3(blocks_for(n_slots)), dim3(kThreads),
-                            args, 0, st);
+                 lens_out,  ring_out, n_req,      n_slots, log2_of(pg.page_size), pg.n_pages, pg.max_pages, err};
+    return pipe::launch_early(k_page_append, dim3(blocks_for(n_slots)), dim3(kThreads), 0, st, a);
 }
 
 cudaError_t launch_page_release(const hybrid_page_cfg &pg, int n_req, const int *rows, int n_rows, const int *lens,
@@ -299,13 +313,11 @@ cudaError_t launch_page_release(const hybrid_page_cfg &pg, int n_req, const int 
                                 unsigned *err, cudaStream_t st)
 {
     ReleaseArgs a{rows,     lens,  block_table, ring_in,      free_pages, ring_out,
-                  n_req,    n_rows, pg.page_size, pg.n_pages, pg.max_pages, err};
-    void *args[] = {&a};
+                  n_req,    n_rows, log2_of(pg.page_size), pg.n_pages, pg.max_pages, err};
     // at most the pool's pages move
     long long most = (long long)n_rows * pg.max_pages;
     if (most > pg.n_pages) most = pg.n_pages;
-    return cudaLaunchKernel(reinterpret_cast<const void *>(&k_page_release), dim3(blocks_for(most)), dim3(kThreads),
-                            args, 0, st);
+    return pipe::launch_early(k_page_release, dim3(blocks_for(most)), dim3(kThreads), 0, st, a);
 }
 
 }  // namespace hyb

@@ -43,7 +43,8 @@ __global__ __launch_bounds__(kThreads) void k_paged_attn(const PagedArgs a)
     const int rows = a.Bt * a.Gt;
     const float to_log2 = pipe::kLog2e * rsqrtf((float)D);
 
-    ptx::griddep_launch_dependents();                        // the join may start its scan
+    ptx::griddep_wait();
+    ptx::griddep_launch_dependents();
     Walk w;
     Shares sh(0, 1);
     const bool work = find_share<kThreads>(a, s.plan, w, sh);
@@ -298,27 +299,18 @@ template <typename T> cudaError_t launch_join(const PagedArgs &a, cudaStream_t s
     // many partials of few rows: more blocks of fewer features
     const bool few = a.Bt * a.Gt <= 16;
     static_assert(16 * 16 == kThreads, "one item a thread");
-    cudaLaunchConfig_t lc = {};
-    lc.gridDim = dim3(a.n_cta, a.d / (few ? 16 : 32));
-    lc.blockDim = dim3(kThreads);
-    lc.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    lc.attrs = attr;
-    lc.numAttrs = 1;
-    return few ? cudaLaunchKernelEx(&lc, k_paged_join<T, 16>, a) : cudaLaunchKernelEx(&lc, k_paged_join<T, 32>, a);
+    const dim3 grid(a.n_cta, a.d / (few ? 16 : 32));
+    return few ? pipe::launch_early(k_paged_join<T, 16>, grid, dim3(kThreads), 0, st, a)
+               : pipe::launch_early(k_paged_join<T, 32>, grid, dim3(kThreads), 0, st, a);
 }
 
 template <int D> cudaError_t launch_f32(const PagedArgs &a, cudaStream_t st)
 {
     static_assert(sizeof(Smem<D>) < 100 * 1024, "two blocks per multiprocessor");
-    PagedArgs b = a;
-    void *args[] = {&b};
-    const void *f = reinterpret_cast<const void *>(&k_paged_attn<D>);
-    cudaError_t e = cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Smem<D>));
+    cudaError_t e =
+        cudaFuncSetAttribute(k_paged_attn<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Smem<D>));
     if (e != cudaSuccess) return e;
-    e = cudaLaunchKernel(f, dim3(a.n_cta), dim3(kThreads), args, sizeof(Smem<D>), st);
+    e = pipe::launch_early(k_paged_attn<D>, dim3(a.n_cta), dim3(kThreads), sizeof(Smem<D>), st, a);
     if (e != cudaSuccess) return e;
     return launch_join<float>(a, st);
 }

@@ -18,7 +18,7 @@
 // and one of V tiles: 5 or 6 slots of 32 KB for d = 128, so that 160 to 192 KB are
 // in flight or in use per SM.  (Two rings, because a wait knows a phase by its
 // parity alone: each issuer must itself have seen every phase of its slots.)  One block per SM walks its share of all requests' tiles
-// (paged_plan.cuh) without a pause between segments: the producer and the issuer
+// (paged_plan.cuh) without a pause between segments: the producers and the issuer
 // of S run ahead into the next segment.  With few rows (decoding) the tensor
 // pipe works on padding, which costs nothing here: a tile's products take about
 // 0.6 us, its bytes 1.5 us at an SM's share of the memory bandwidth.
@@ -29,8 +29,8 @@
 // nothing in those places (NaN included) reaches the output.
 //
 // Warps: 0-7 softmax and epilogue (warp w: rows 32 (w % 4) ..., half w / 4 of the
-// keys and of the output's features; warps beyond the rows idle), 8 producer, 9
-// issuer of S, 10 issuer of O.  Every wait is bounded (tc_pipeline.cuh).
+// keys and of the output's features; warps beyond the rows idle), 8 and 9
+// producers of K (with Q) and V, 10 and 11 issuers of S and O.  Every wait is bounded (tc_pipeline.cuh).
 #include <atomic>
 
 #include "paged_plan.cuh"
@@ -44,8 +44,8 @@ using namespace pipe;
 
 constexpr int kParts = 2;                 // threads per row: each has kTile / kParts keys
 constexpr int kSoftWarps = 4 * kParts;
-constexpr int kThreads = 32 * (kSoftWarps + 3);
-constexpr int kProducer = kSoftWarps, kIssueS = kSoftWarps + 1, kIssueO = kSoftWarps + 2;
+constexpr int kThreads = 32 * (kSoftWarps + 4);
+constexpr int kLoadK = kSoftWarps, kLoadV = kSoftWarps + 1, kIssueS = kSoftWarps + 2, kIssueO = kSoftWarps + 3;
 constexpr int kSmemLimit = 232448;
 constexpr int kMaxSlots = 12;
 constexpr uint32_t kBarBytes = 1024;      // barriers, TMEM address, failure flag, the plan's scratch
@@ -127,7 +127,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_tc(const __grid_cons
         tmem_alloc(tmem_holder, 512);
         tmem_relinquish();
     }
-    if (warp == kProducer && lane == 0) {
+    if (warp == kLoadK && lane == 0) {
         prefetch_tensormap(&ta.tmQ);
         prefetch_tensormap(&ta.tmK);
         prefetch_tensormap(&ta.tmV);
@@ -149,7 +149,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_tc(const __grid_cons
         *fail = 0;
         fence_mbar_init();
     }
-    // what comes before in the stream is complete from here on; the join may start its scan
+    // what comes before in the stream is complete from here on
     griddep_wait();
     griddep_launch_dependents();
     tc_fence_before();
@@ -160,27 +160,19 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_tc(const __grid_cons
     const uint32_t tmem = *tmem_holder;
     const long long M = units_per_request(a);
 
-    if (work && warp == kProducer) {
-        // ------------------------------------------------------------- producer
+    if (work && (warp == kLoadK || warp == kLoadV)) {
+        // ------------------------------------------- producers: Q and K; V
+        const bool is_v = warp == kLoadV;
         const int P = a.page_size, per = kTile / P;        // pages of a tile
-        const uint32_t page_bytes = (uint32_t)P * D * 2;
-        uint32_t n_k = 0, n_v = 0, ns = 0;                 // K and V tiles and segments issued
-        RingPos pos_k{0, 1}, pos_v{0, 1};                  // phases of `empty`: the first round is free
+        const uint32_t page_bytes = (uint32_t)P * D * 2, n_slots = is_v ? NV : NK;
+        const CUtensorMap *map = is_v ? &ta.tmV : &ta.tmK;
+        uint64_t *my_full = is_v ? full + NK : full, *my_empty = is_v ? empty + NK : empty;
+        uint8_t *my_ring = is_v ? ring + (size_t)NK * kSlot : ring;
+        uint32_t n = 0, ns = 0;                            // tiles and segments issued
+        RingPos pos{0, 1};                                 // phase of `empty`: the first round is free
         bool ok = true;
         while (ok && w.next(a, M)) {
             const Unit u = unit_of(a, w.m);
-            const uint32_t qb = ns & 1;
-            ok = wait_soon(&qempty[qb], ((ns >> 1) & 1u) ^ 1u, fail);
-            if (__any_sync(0xffffffffu, !ok)) break;
-            if (lane == 0) {
-                const uint32_t panel = ta.q_bytes / kHalves;
-                mbar_arrive_expect_tx(&qfull[qb], (uint32_t)rows * D * 2);
-#pragma unroll
-                for (int h = 0; h < kHalves; ++h)
-                    tma_load_4d(smem + qb * ta.q_bytes + h * panel, &ta.tmQ, 64 * h, u.head * a.G + u.g0, u.i0, w.req,
-                                &qfull[qb]);
-            }
-            ++ns;
             const int *pages = a.table + (size_t)w.req * a.max_pages;
             auto page_at = [&](int i) -> int {             // this lane's page of tile i, -1: nothing visible in it
                 if (i >= w.i1 || lane >= per) return -1;
@@ -192,47 +184,50 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_tc(const __grid_cons
                 return 0;
             };
             int next_page = page_at(w.i0);
+            if (!is_v) {
+                const uint32_t qb = ns & 1;
+                ok = wait_soon(&qempty[qb], ((ns >> 1) & 1u) ^ 1u, fail);
+                if (__any_sync(0xffffffffu, !ok)) break;
+                if (lane == 0) {
+                    const uint32_t panel = ta.q_bytes / kHalves;
+                    mbar_arrive_expect_tx(&qfull[qb], (uint32_t)rows * D * 2);
+#pragma unroll
+                    for (int h = 0; h < kHalves; ++h)
+                        tma_load_4d(smem + qb * ta.q_bytes + h * panel, &ta.tmQ, 64 * h, u.head * a.G + u.g0, u.i0,
+                                    w.req, &qfull[qb]);
+                }
+                ++ns;
+            }
             for (int i = w.i0; i < w.i1; ++i) {
                 const int page = next_page;
                 next_page = page_at(i + 1);                // a tile ahead of its use
                 const uint32_t bytes = page_bytes * __popc(__ballot_sync(0xffffffffu, page >= 0));
-#pragma unroll 1
-                for (int kv = 0; kv < 2; ++kv) {
-                    const int slot = kv ? NK + (int)pos_v.slot : (int)pos_k.slot;
-                    ok = wait_soon(&empty[slot], kv ? pos_v.phase : pos_k.phase, fail);
-                    if (__any_sync(0xffffffffu, !ok)) {
-                        ok = false;
-                        break;
-                    }
-                    if (lane == 0) mbar_arrive_expect_tx(&full[slot], bytes);
-                    __syncwarp();
-                    if (page >= 0) {
-                        uint8_t *dst = ring + (size_t)slot * kSlot + lane * P * 128;
-#pragma unroll
-                        for (int h = 0; h < kHalves; ++h)
-                            tma_load_4d(dst + h * kPanel, kv ? &ta.tmV : &ta.tmK, 64 * h, 0, u.head, page, &full[slot]);
-                    }
-                    if (kv) {
-                        pos_v.step(NV);
-                        ++n_v;
-                    } else {
-                        pos_k.step(NK);
-                        ++n_k;
-                    }
+                ok = wait_soon(&my_empty[pos.slot], pos.phase, fail);
+                if (__any_sync(0xffffffffu, !ok)) {
+                    ok = false;
+                    break;
                 }
-                if (!ok) break;
+                if (lane == 0) mbar_arrive_expect_tx(&my_full[pos.slot], bytes);
+                __syncwarp();
+                if (page >= 0) {
+                    uint8_t *dst = my_ring + (size_t)pos.slot * kSlot + lane * P * 128;
+#pragma unroll
+                    for (int h = 0; h < kHalves; ++h)
+                        tma_load_4d(dst + h * kPanel, map, 64 * h, 0, u.head, page, &my_full[pos.slot]);
+                }
+                pos.step(n_slots);
+                ++n;
             }
         }
         if (*fail && lane == 0) {
             // let copies in flight land before the block exits
             auto land = [&](uint64_t *bar, uint32_t slots, uint32_t items) {
                 for (uint32_t s = 0; s < slots; ++s) {
-                    const uint32_t n = items / slots + (s < items % slots ? 1u : 0u);
-                    if (n) mbar_wait(&bar[s], (n - 1) & 1u, kWaitNs);
+                    const uint32_t k = items / slots + (s < items % slots ? 1u : 0u);
+                    if (k) mbar_wait(&bar[s], (k - 1) & 1u, kWaitNs);
                 }
             };
-            land(full, NK, n_k);
-            land(full + NK, NV, n_v);
+            land(my_full, n_slots, n);
             land(qfull, 2, ns);
         }
     } else if (work && warp == kIssueS) {
@@ -524,17 +519,7 @@ template <int D> cudaError_t launch(const PagedArgs &a, cudaStream_t st)
         if (e != cudaSuccess) return e;
         opted.fetch_or(bit, std::memory_order_release);
     }
-    cudaLaunchConfig_t lc = {};
-    lc.gridDim = dim3(a.n_cta);
-    lc.blockDim = dim3(kThreads);
-    lc.dynamicSmemBytes = ta.bytes;
-    lc.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    lc.attrs = attr;
-    lc.numAttrs = 1;
-    return cudaLaunchKernelEx(&lc, k_paged_attn_tc<D>, ta);
+    return pipe::launch_early(k_paged_attn_tc<D>, dim3(a.n_cta), dim3(kThreads), ta.bytes, st, ta);
 }
 
 }  // namespace

@@ -135,11 +135,13 @@ __device__ __forceinline__ void rotate(float (&x)[E], const Rotation<E> &r, bool
 }
 
 template <typename T, int D>
-__global__ __launch_bounds__(kThreads) void k_qk_norm_rope(const RopeArgs a, int parts, int rows_per_part)
+__global__ __launch_bounds__(kThreads, 3) void k_qk_norm_rope(const RopeArgs a, int parts, int rows_per_part)
 {
-    constexpr int E = Vec<T>::E, L = D / E, RPW = 32 / L, U = 4;
+    constexpr int E = Vec<T>::E, L = D / E, RPW = 32 / L, U = E == 8 ? 2 : 4;
     const int lane = threadIdx.x & 31, sub = lane / L, e0 = (lane % L) * E;
     const long long item = (long long)blockIdx.x * kWarps + (threadIdx.x >> 5);
+    ptx::griddep_wait();
+    ptx::griddep_launch_dependents();
     if (item >= (long long)a.n_tok * parts) return;
     const int t = (int)(item / parts), part = (int)(item % parts);
     const int n_rows = a.Hq + (a.slots ? 2 : 1) * a.Hkv;    // q heads, k heads, v heads
@@ -167,21 +169,29 @@ __global__ __launch_bounds__(kThreads) void k_qk_norm_rope(const RopeArgs a, int
     } else {
         Ko = static_cast<T *>(a.Ko) + (size_t)t * a.Hkv * D + e0;
     }
-    const Rotation<E> rot = make_rotation<E>(a, t, e0);
-
-    for (int h0 = begin; h0 < end; h0 += U * RPW) {
-        uint4 raw[U];
+    // U rows a lane group are loaded before the angles are formed, and the next U
+    // while these are worked on
+    uint4 raw[U], next[U];
+    auto load = [&](int h0, uint4 (&r)[U]) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int h = h0 + u * RPW + sub;
-            raw[u] = make_uint4(0, 0, 0, 0);
+            r[u] = make_uint4(0, 0, 0, 0);
             if (h < end) {
                 const T *src = h < a.Hq ? Q + (size_t)h * D
                                         : (h < a.Hq + a.Hkv ? K + (size_t)(h - a.Hq) * D
                                                             : V + (size_t)(h - a.Hq - a.Hkv) * D);
-                raw[u] = *reinterpret_cast<const uint4 *>(src);
+                r[u] = *reinterpret_cast<const uint4 *>(src);
             }
         }
+    };
+    load(begin, next);
+    const Rotation<E> rot = make_rotation<E>(a, t, e0);
+
+    for (int h0 = begin; h0 < end; h0 += U * RPW) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) raw[u] = next[u];
+        if (h0 + U * RPW < end) load(h0 + U * RPW, next);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int h = h0 + u * RPW + sub;
@@ -214,44 +224,100 @@ __global__ __launch_bounds__(kThreads) void k_qk_norm_rope(const RopeArgs a, int
 }
 
 template <typename T, int D>
-__global__ __launch_bounds__(kThreads) void k_qk_norm_rope_backward(const RopeArgs a, int parts, int rows_per_part)
+__global__ __launch_bounds__(kThreads, 2) void k_qk_norm_rope_backward(const RopeArgs a, int parts, int rows_per_part)
 {
-    constexpr int E = Vec<T>::E, L = D / E, RPW = 32 / L;
+    constexpr int E = Vec<T>::E, L = D / E, RPW = 32 / L, U = 2;
     __shared__ float s_dw[kWarps][2][D];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = lane / L, e0 = (lane % L) * E;
     const int n_rows = a.Hq + a.Hkv;
-    float wq[E], wk[E], dwq[E], dwk[E];
+    ptx::griddep_wait();
+    ptx::griddep_launch_dependents();
+    // the weights stay packed: they are unpacked where they are used
+    uint4 wq = make_uint4(0, 0, 0, 0), wk = wq;
+    float dwq[E], dwk[E];
 #pragma unroll
     for (int i = 0; i < E; ++i) dwq[i] = dwk[i] = 0.f;
-    if (a.wq) Vec<T>::unpack(*reinterpret_cast<const uint4 *>(static_cast<const T *>(a.wq) + e0), wq);
-    if (a.wk) Vec<T>::unpack(*reinterpret_cast<const uint4 *>(static_cast<const T *>(a.wk) + e0), wk);
-    const long long items = (long long)a.n_tok * parts;
-    for (long long item = (long long)blockIdx.x * kWarps + warp; item < items; item += (long long)gridDim.x * kWarps) {
-        const int t = (int)(item / parts), part = (int)(item % parts);
-        const int begin = part * rows_per_part;
-        const int end = begin + rows_per_part < n_rows ? begin + rows_per_part : n_rows;
-        const Rotation<E> rot = make_rotation<E>(a, t, e0);
-        for (int h0 = begin; h0 < end; h0 += RPW) {
-            const int h = h0 + sub;
-            const bool live = h < end, is_q = h < a.Hq;
-            const size_t at = is_q ? (size_t)t * a.q_stride + (size_t)h * D + e0
-                                   : (size_t)t * a.k_stride + (size_t)(h - a.Hq) * D + e0;
-            uint4 rx = make_uint4(0, 0, 0, 0), ry = rx;
+    if (a.wq) wq = *reinterpret_cast<const uint4 *>(static_cast<const T *>(a.wq) + e0);
+    if (a.wk) wk = *reinterpret_cast<const uint4 *>(static_cast<const T *>(a.wk) + e0);
+    const long long items = (long long)a.n_tok * parts, stride = (long long)gridDim.x * kWarps;
+
+    // A warp's rows, U lane groups' worth at a time, over all of its tokens: the next
+    // ones are loaded while these are worked on.
+    struct Place {
+        long long item;
+        int h0;             // first row of the batch
+        int end;            // end of the token's rows
+    };
+    auto rows_of = [&](Place &p) {
+        const int begin = (int)(p.item % parts) * rows_per_part;
+        p.h0 = begin;
+        p.end = begin + rows_per_part < n_rows ? begin + rows_per_part : n_rows;
+    };
+    auto step = [&](Place &p) {
+        p.h0 += U * RPW;
+        if (p.h0 < p.end) return;
+        p.item += stride;
+        if (p.item < items) rows_of(p);
+    };
+    auto place_of = [&](const Place &p, int u, bool &live, bool &is_q, size_t &at, size_t &dy) {
+        const int t = (int)(p.item / parts), h = p.h0 + u * RPW + sub;
+        live = h < p.end;
+        is_q = h < a.Hq;
+        at = is_q ? (size_t)t * a.q_stride + (size_t)h * D + e0 : (size_t)t * a.k_stride + (size_t)(h - a.Hq) * D + e0;
+        dy = is_q ? ((size_t)t * a.Hq + h) * D + e0 : ((size_t)t * a.Hkv + (h - a.Hq)) * D + e0;
+    };
+    uint4 nx[U], ny[U];
+    auto load = [&](const Place &p) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            bool live, is_q;
+            size_t at, dy;
+            place_of(p, u, live, is_q, at, dy);
+            nx[u] = ny[u] = make_uint4(0, 0, 0, 0);
             if (live) {
-                rx = *reinterpret_cast<const uint4 *>(static_cast<const T *>(is_q ? a.Q : a.K) + at);
-                const size_t dy = is_q ? ((size_t)t * a.Hq + h) * D + e0 : ((size_t)t * a.Hkv + (h - a.Hq)) * D + e0;
-                ry = *reinterpret_cast<const uint4 *>(static_cast<const T *>(is_q ? a.dQo : a.dKo) + dy);
+                nx[u] = *reinterpret_cast<const uint4 *>(static_cast<const T *>(is_q ? a.Q : a.K) + at);
+                ny[u] = *reinterpret_cast<const uint4 *>(static_cast<const T *>(is_q ? a.dQo : a.dKo) + dy);
             }
-            float x[E], g[E];
-            Vec<T>::unpack(rx, x);
-            Vec<T>::unpack(ry, g);
+        }
+    };
+    Place p{(long long)blockIdx.x * kWarps + warp, 0, 0};
+    if (p.item < items) {
+        rows_of(p);
+        load(p);
+    }
+    long long rotated = -1;                 // token of `rot`
+    Rotation<E> rot;
+    while (p.item < items) {
+        const Place now = p;
+        uint4 rx[U], ry[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            rx[u] = nx[u];
+            ry[u] = ny[u];
+        }
+        step(p);
+        if (p.item < items) load(p);
+        if (now.item / parts != rotated) {
+            rotated = now.item / parts;
+            rot = make_rotation<E>(a, (int)rotated, e0);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (now.h0 + u * RPW >= now.end) break;         // the whole warp
+            bool live, is_q;
+            size_t at, dy;
+            place_of(now, u, live, is_q, at, dy);
+            float x[E], g[E], w[E];
+            Vec<T>::unpack(rx[u], x);
+            Vec<T>::unpack(ry[u], g);
+            Vec<T>::unpack(is_q ? wq : wk, w);
             rotate<E, true>(g, rot, a.interleaved, lane);   // dn
             float xx = 0.f, ux = 0.f;
             const bool norm = is_q ? a.wq != nullptr : a.wk != nullptr;
 #pragma unroll
             for (int i = 0; i < E; ++i) {
                 xx = fmaf(x[i], x[i], xx);
-                ux = fmaf(norm ? g[i] * (is_q ? wq[i] : wk[i]) : 0.f, x[i], ux);
+                ux = fmaf(g[i] * w[i], x[i], ux);
             }
             xx = head_sum<L>(xx);
             ux = head_sum<L>(ux);
@@ -263,7 +329,7 @@ __global__ __launch_bounds__(kThreads) void k_qk_norm_rope_backward(const RopeAr
                     const float xh = x[i] * r, dw = g[i] * xh;
                     if (is_q) dwq[i] += dw;
                     else dwk[i] += dw;
-                    g[i] = r * (g[i] * (is_q ? wq[i] : wk[i]) - xh * m);
+                    g[i] = r * (g[i] * w[i] - xh * m);
                 }
             }
             *reinterpret_cast<uint4 *>(static_cast<T *>(is_q ? a.Qo : a.Ko) + at) = Vec<T>::pack(g);
@@ -296,6 +362,8 @@ __global__ __launch_bounds__(kThreads) void k_qk_norm_rope_backward(const RopeAr
 __global__ __launch_bounds__(kThreads) void k_dw_reduce(const float *partial, int blocks, int d, float *dwq, float *dwk)
 {
     __shared__ float s[8][32];
+    ptx::griddep_wait();
+    ptx::griddep_launch_dependents();
     const int c = blockIdx.x * 32 + (threadIdx.x & 31), y = threadIdx.x >> 5;
     float v = 0.f;
     for (int b = y; b < blocks; b += 8) v += partial[(size_t)b * 2 * d + c];
@@ -329,10 +397,7 @@ template <typename T, int D> cudaError_t forward(const RopeArgs &a, cudaStream_t
     int parts, rpp;
     split_heads(a.n_tok, a.Hq + (a.slots ? 2 : 1) * a.Hkv, RPW, parts, rpp);
     const long long blocks = ((long long)a.n_tok * parts + kWarps - 1) / kWarps;
-    RopeArgs b = a;
-    void *args[] = {&b, &parts, &rpp};
-    return cudaLaunchKernel(reinterpret_cast<const void *>(&k_qk_norm_rope<T, D>), dim3((unsigned)blocks),
-                            dim3(kThreads), args, 0, st);
+    return pipe::launch_early(k_qk_norm_rope<T, D>, dim3((unsigned)blocks), dim3(kThreads), 0, st, a, parts, rpp);
 }
 
 template <typename T, int D> cudaError_t backward(const RopeArgs &a, cudaStream_t st)
@@ -344,18 +409,13 @@ template <typename T, int D> cudaError_t backward(const RopeArgs &a, cudaStream_
         split_heads(a.n_tok, a.Hq + a.Hkv, RPW, parts, rpp);
         const long long want = ((long long)a.n_tok * parts + kWarps - 1) / kWarps;
         blocks = (int)(want < kMaxBackwardBlocks ? want : kMaxBackwardBlocks);
-        RopeArgs b = a;
-        void *args[] = {&b, &parts, &rpp};
-        const cudaError_t e = cudaLaunchKernel(reinterpret_cast<const void *>(&k_qk_norm_rope_backward<T, D>),
-                                               dim3(blocks), dim3(kThreads), args, 0, st);
+        const cudaError_t e =
+            pipe::launch_early(k_qk_norm_rope_backward<T, D>, dim3(blocks), dim3(kThreads), 0, st, a, parts, rpp);
         if (e != cudaSuccess) return e;
     }
     if (!a.dwq && !a.dwk) return cudaSuccess;
-    const float *partial = a.partial;
-    float *dwq = a.dwq, *dwk = a.dwk;
-    int d = D;
-    void *args[] = {&partial, &blocks, &d, &dwq, &dwk};
-    return cudaLaunchKernel(reinterpret_cast<const void *>(&k_dw_reduce), dim3(2 * D / 32), dim3(kThreads), args, 0, st);
+    return pipe::launch_early(k_dw_reduce, dim3(2 * D / 32), dim3(kThreads), 0, st, (const float *)a.partial, blocks, D,
+                              a.dwq, a.dwk);
 }
 
 }  // namespace
