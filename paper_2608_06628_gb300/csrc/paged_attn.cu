@@ -48,7 +48,7 @@ __global__ __launch_bounds__(kThreads) void k_paged_attn(const PagedArgs a)
     Walk w;
     Shares sh(0, 1);
     const bool work = find_share<kThreads>(a, s.plan, w, sh);
-    const long long M = units_per_request(a);
+    const int M = units_per_request(a);
     while (work && w.next(a, M)) {
         const Visible vis = w.vis;
         const int i0 = w.i0, i1 = w.i1;

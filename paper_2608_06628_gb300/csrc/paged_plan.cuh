@@ -37,21 +37,21 @@ struct Visible {
 __device__ __forceinline__ Visible visible_keys(const PagedArgs &a, int len)
 {
     Visible v;
-    const long long cap = (long long)a.max_pages * a.page_size;
+    const int cap = a.max_pages * a.page_size;              // < 2^31 - 255 (the host's check)
     if (len < 0) len = 0;
-    if (len > cap) len = (int)cap;
+    if (len > cap) len = cap;
     v.len = len;
     v.lo = a.window > 0 && len > a.window ? len - a.window : 0;
     v.sink = v.lo > 0 ? (a.sink < v.lo ? a.sink : v.lo) : 0;
     v.ns = (v.sink + kTile - 1) / kTile;
     v.first = v.lo / kTile > v.ns ? v.lo / kTile : v.ns;
-    const int last = (int)(((long long)len + kTile - 1) / kTile);
+    const int last = (len + kTile - 1) / kTile;
     v.tiles = v.ns + (last > v.first ? last - v.first : 0);
     return v;
 }
 __device__ __forceinline__ bool length_ok(const PagedArgs &a, int len)
 {
-    return len >= 0 && len <= (long long)a.max_pages * a.page_size;
+    return len >= 0 && len <= a.max_pages * a.page_size;
 }
 // key tile of the i-th visible tile
 __device__ __forceinline__ int key_tile(const Visible &v, int i) { return i < v.ns ? i : v.first + (i - v.ns); }
@@ -60,22 +60,21 @@ __device__ __forceinline__ bool key_visible(const Visible &v, int j) { return j 
 __device__ __forceinline__ int units_per_request(const PagedArgs &a) { return a.Hkv * a.n_gt * a.n_bt; }
 
 // Shares of T tiles over C blocks (C <= T): the first T % C blocks take one more.
+// T < 2^31 (the host's check).
 struct Shares {
-    long long per, rem;
-    int C;
-    __device__ Shares(long long T, int n_cta)
+    int per, rem, C;
+    __device__ Shares(int T, int n_cta)
     {
-        C = T < n_cta ? (int)T : n_cta;
-        const bool small = T < 0x7fffffffll;                // the usual case, with 32-bit division
-        per = C == 0 ? 0 : (small ? (long long)((unsigned)T / (unsigned)C) : T / C);
+        C = T < n_cta ? T : n_cta;
+        per = C == 0 ? 0 : T / C;
         rem = T - per * C;
     }
-    __device__ long long start(int c) const { return per * c + (c < rem ? c : rem); }
+    __device__ int start(int c) const { return per * c + (c < rem ? c : rem); }
     // block of a tile
-    __device__ int block_of(long long t) const
+    __device__ int block_of(int t) const
     {
-        const long long big = rem * (per + 1);
-        return (int)(t < big ? t / (per + 1) : rem + (t - big) / per);
+        const int big = rem * (per + 1);
+        return t < big ? t / (per + 1) : rem + (t - big) / per;
     }
 };
 
@@ -89,100 +88,23 @@ struct JoinNote {
     int pad[3];
 };
 
-// Scratch of the scan: one long per warp and the answer.
+// Scratch of the search for a block's share.
 struct PlanSmem {
-    long long warp[16];
-    long long total;
-    int req;
-    long long before;
+    int warp[16];
+    int req, before, len;
 };
-
-// Scan over the requests by the whole block (NT threads, a multiple of 32).
-// Returns T, the number of tiles of all units; then locate() finds the request
-// of a tile.  Each thread holds the requests [q0, q1) and the tiles before them
-// (per unit of a request, that is: without the factor M).
-struct Plan {
-    long long total;       // tiles of all requests, per unit
-    long long before;      // of the requests before this thread's
-    int q0, q1;
-};
-
-template <int NT>
-__device__ __forceinline__ Plan make_plan(const PagedArgs &a, PlanSmem &s)
-{
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int per = (a.n_req + NT - 1) / NT;
-    Plan p;
-    p.q0 = tid * per < a.n_req ? tid * per : a.n_req;
-    p.q1 = p.q0 + per < a.n_req ? p.q0 + per : a.n_req;
-    long long sum = 0;
-    bool bad = false;
-    for (int r = p.q0; r < p.q1; ++r) {
-        const int len = a.lens[r];
-        bad |= !length_ok(a, len);
-        sum += visible_keys(a, len).tiles;
-    }
-    if (bad) raise_error(a.err, ERR_BAD_INDEX);
-    long long inc = sum;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const long long v = __shfl_up_sync(0xffffffffu, inc, o);
-        if (lane >= o) inc += v;
-    }
-    if (lane == 31) s.warp[warp] = inc;
-    __syncthreads();
-    long long before = 0, total = 0;
-#pragma unroll
-    for (int w = 0; w < NT / 32; ++w) {
-        if (w < warp) before += s.warp[w];
-        total += s.warp[w];
-    }
-    p.total = total;
-    p.before = before + inc - sum;
-    return p;
-}
-
-// Request that holds tile `tile` (0 <= tile < total * M) and the tiles per unit
-// of the requests before it; for the whole block.
-__device__ __forceinline__ void locate(const PagedArgs &a, const Plan &p, long long tile, PlanSmem &s, int &req,
-                                       long long &before)
-{
-    const long long M = units_per_request(a);
-    long long b = p.before;
-    for (int r = p.q0; r < p.q1; ++r) {
-        const int n = visible_keys(a, a.lens[r]).tiles;
-        if (tile >= b * M && tile < (b + n) * M) {
-            s.req = r;
-            s.before = b;
-        }
-        b += n;
-    }
-    __syncthreads();
-    req = s.req;
-    before = s.before;
-}
 
 // The segments of a block's share, one after another.
 struct Walk {
-    long long t, t1;       // next tile, end of the share
-    long long before;      // tiles per unit of the requests before `req`
+    int t, t1;             // next tile, end of the share
+    int before;            // tiles per unit of the requests before `req`
     int req;
     Visible vis;
     // the current segment: tiles [i0, i1) of unit m of request req
     int m, i0, i1;
     bool at_start;         // it begins the share
 
-    __device__ void begin(const PagedArgs &a, long long t_, long long t1_, int req_, long long before_)
-    {
-        t = t_;
-        t1 = t1_;
-        req = req_;
-        before = before_;
-        vis = visible_keys(a, __ldg(a.lens + req));
-        at_start = true;
-        i1 = -1;
-    }
-    __device__ bool next(const PagedArgs &a, long long M)
+    __device__ bool next(const PagedArgs &a, int M)
     {
         if (t >= t1) return false;
         at_start = i1 < 0;
@@ -190,10 +112,10 @@ struct Walk {
             before += vis.tiles;
             vis = visible_keys(a, __ldg(a.lens + ++req));
         }
-        const long long rel = t - before * M;
-        m = (int)(rel / vis.tiles);
-        i0 = (int)(rel % vis.tiles);
-        i1 = vis.tiles - i0 < t1 - t ? vis.tiles : (int)(i0 + (t1 - t));
+        const int rel = t - before * M;
+        m = (unsigned)rel / (unsigned)vis.tiles;
+        i0 = rel - m * vis.tiles;
+        i1 = vis.tiles - i0 < t1 - t ? vis.tiles : i0 + (t1 - t);
         t += i1 - i0;
         return true;
     }
@@ -201,18 +123,61 @@ struct Walk {
     __device__ int slot() const { return 2 * (int)blockIdx.x + (at_start ? 0 : 1); }
 };
 
-// Find a block's share; false if it has none.  For the whole block.
+// Find the block's share by a scan over the requests, NT threads (a multiple of
+// 32), each with a run of them; false if the block has none.  Synchronises the
+// block (also where it returns false).
 template <int NT>
 __device__ __forceinline__ bool find_share(const PagedArgs &a, PlanSmem &s, Walk &w, Shares &sh)
 {
-    const Plan plan = make_plan<NT>(a, s);
-    sh = Shares(plan.total * units_per_request(a), a.n_cta);
-    if ((int)blockIdx.x >= sh.C) return false;
-    const long long t0 = sh.start(blockIdx.x);
-    int req;
-    long long before;
-    locate(a, plan, t0, s, req, before);
-    w.begin(a, t0, sh.start(blockIdx.x + 1), req, before);
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int M = units_per_request(a), per = (a.n_req + NT - 1) / NT;
+    const int q0 = tid * per < a.n_req ? tid * per : a.n_req, q1 = q0 + per < a.n_req ? q0 + per : a.n_req;
+    int sum = 0;
+    bool bad = false;
+    for (int r = q0; r < q1; ++r) {
+        const int len = __ldg(a.lens + r);
+        bad |= !length_ok(a, len);
+        sum += visible_keys(a, len).tiles;
+    }
+    if (bad) raise_error(a.err, ERR_BAD_INDEX);
+    int inc = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int v = __shfl_up_sync(0xffffffffu, inc, o);
+        if (lane >= o) inc += v;
+    }
+    if (lane == 31) s.warp[warp] = inc;
+    __syncthreads();
+    int b = inc - sum, total = 0;
+#pragma unroll
+    for (int x = 0; x < NT / 32; ++x) {
+        if (x < warp) b += s.warp[x];
+        total += s.warp[x];
+    }
+    sh = Shares(total * M, a.n_cta);
+    const bool work = (int)blockIdx.x < sh.C;
+    const int t0 = sh.start(blockIdx.x);
+    if (work && t0 >= b * M && t0 < (b + sum) * M) {        // one thread's run holds the first tile
+        for (int r = q0; r < q1; ++r) {
+            const int len = __ldg(a.lens + r), n = visible_keys(a, len).tiles;
+            if (t0 < (b + n) * M) {
+                s.req = r;
+                s.before = b;
+                s.len = len;
+                break;
+            }
+            b += n;
+        }
+    }
+    __syncthreads();
+    if (!work) return false;
+    w.t = t0;
+    w.t1 = sh.start(blockIdx.x + 1);
+    w.req = s.req;
+    w.before = s.before;
+    w.vis = visible_keys(a, s.len);
+    w.at_start = true;
+    w.i1 = -1;
     return true;
 }
 
@@ -250,6 +215,11 @@ struct Unit {
 __device__ __forceinline__ Unit unit_of(const PagedArgs &a, int m)
 {
     Unit u;
+    if (a.n_gt * a.n_bt == 1) {             // one row tile per key head
+        u.head = m;
+        u.g0 = u.i0 = 0;
+        return u;
+    }
     u.head = m / (a.n_gt * a.n_bt);
     const int rest = m % (a.n_gt * a.n_bt);
     u.g0 = rest / a.n_bt * a.Gt;

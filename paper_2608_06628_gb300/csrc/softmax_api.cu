@@ -31,8 +31,8 @@ hybrid_status check_pages(const hybrid_page_cfg *p)
     if (p->page_size != 16 && p->page_size != 32 && p->page_size != 64 && p->page_size != 128)
         return HYBRID_ERR_UNSUPPORTED;
     if (p->n_pages < 1 || p->max_pages < 1) return HYBRID_ERR_INVALID_ARG;
-    // slots and positions are ints
-    if ((long long)p->n_pages * p->page_size > 0x7fffffffll || (long long)p->max_pages * p->page_size > 0x7fffffffll)
+    // slots and positions are ints (with room for the end of a tile)
+    if ((long long)p->n_pages * p->page_size > 0x7fffffffll || (long long)p->max_pages * p->page_size > 0x7fffff00ll)
         return HYBRID_ERR_UNSUPPORTED;
     return HYBRID_OK;
 }
@@ -264,6 +264,9 @@ hybrid_status hybrid_paged_attn(const hybrid_cfg *cfg, const hybrid_page_cfg *pg
     hyb::PagedArgs a{};
     hyb::paged_geometry(*cfg, a);
     if (workspace_bytes < hyb::paged_workspace_bytes(a)) return HYBRID_ERR_INVALID_ARG;
+    // the kernels count tiles of 128 keys of all row tiles in an int
+    const long long tiles = ((long long)pg->max_pages * pg->page_size + 127) / 128;
+    if (tiles * n_req > 0x7fffffffll / ((long long)a.Hkv * a.n_gt * a.n_bt)) return HYBRID_ERR_UNSUPPORTED;
     unsigned *err = hyb::error_word();
     if (!err) return HYBRID_ERR_CUDA;
     a.Q = Q;
