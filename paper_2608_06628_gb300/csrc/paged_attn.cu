@@ -195,20 +195,33 @@ __global__ __launch_bounds__(kThreads) void k_paged_attn(const PagedArgs a)
 
 // Join: block x reads the note of boundary x and, if a unit is cut there for the
 // first time, adds up the unit's partials; blocks along y take COLS features each.
-// Where a unit has few rows (decoding) it may have many partials: then groups of
-// threads take every n-th one, and the groups are added in order.  Launched
-// programmatically behind the attention kernel.
+// A thread has one row and every n-th feature; it loads references, sums and
+// outputs of a partial together and merges them into its own (m, l, o), so that two
+// rounds of loads (the note, then the partials) are all the latency.  Where a unit
+// has few rows (decoding) it may have many partials: then groups of threads take
+// every n-th one, and the groups are merged in order.  Launched programmatically
+// behind the attention kernel.
 constexpr int kMaxRows = 128;
-constexpr int kJoinWeights = 2048;      // weights in shared memory at a time
 
-template <typename T, int COLS>
+// (m, l, o) <- (m, l, o) + (mi, li, oi): weights of both in units of the larger reference
+struct Merge {
+    float keep, add;
+    __device__ Merge(float &m, float mi)
+    {
+        const float top = fmaxf(m, mi), base = top == -INFINITY ? 0.f : top;
+        keep = exp2f(m - base);
+        add = exp2f(mi - base);
+        m = top;
+    }
+};
+
+template <typename T, int COLS, int ROWS>
 __global__ __launch_bounds__(kThreads) void k_paged_join(const PagedArgs a)
 {
-    // items per thread, at most (16 features: at most 16 rows)
-    constexpr int kIter = (COLS == 16 ? 16 : kMaxRows) * COLS / kThreads;
-    __shared__ float s_base[kMaxRows], s_inv[kMaxRows];
-    __shared__ float s_w[kJoinWeights];                      // [partial of the chunk][row]
-    __shared__ float s_o[kMaxRows * (COLS + 1)];             // [group][row][COLS + 1]
+    constexpr int kIter = ROWS * COLS > kThreads ? ROWS * COLS / kThreads : 1;   // features per thread, at most
+    constexpr int kOut = ROWS * (COLS + 1) > kThreads ? ROWS * (COLS + 1) : kThreads;
+    __shared__ float s_o[kOut];                              // [row][COLS + 1], or one value a thread
+    __shared__ float s_m[kThreads], s_l[kThreads];
     const int tid = threadIdx.x, rows = a.Bt * a.Gt, c = blockIdx.x, col0 = blockIdx.y * COLS;
     ptx::griddep_wait();
     const JoinNote note = a.notes[c];
@@ -217,91 +230,72 @@ __global__ __launch_bounds__(kThreads) void k_paged_join(const PagedArgs a)
     const int n = note.last - c + 1;                         // partials
     auto part_of = [&](int i) { return a.part + (size_t)(i == 0 ? note.slot : 2 * (c + i)) * size; };
 
-    // maximum and sum of each row: L lanes a row
-    int L = 1;
-    while (L < n && L < 32) L *= 2;
-    for (int r0 = 0; r0 < rows; r0 += kThreads / L) {
-        const int rho = r0 + tid / L, y = tid % L;
-        float mx = -INFINITY, l = 0.f;
-        if (rho < rows)
-            for (int i = y; i < n; i += L) mx = fmaxf(mx, part_of(i)[rho]);
-        for (int o = L / 2; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-        const float base = mx == -INFINITY ? 0.f : mx;
-        if (rho < rows)
-            for (int i = y; i < n; i += L) l = fmaf(exp2f(part_of(i)[rho] - base), part_of(i)[rows + rho], l);
-        for (int o = L / 2; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
-        if (rho < rows && y == 0) {
-            s_base[rho] = base;
-            s_inv[rho] = 1.f / l;
-        }
-    }
-    // sums over the partials; item = (feature, row), row fastest as in memory
-    const int items = rows * COLS, groups = items <= kThreads / 2 ? kThreads / items : 1;
-    const int g = groups > 1 ? tid / items : 0, item0 = groups > 1 ? tid % items : tid;
-    const int rho0 = item0 % rows, step_row = kThreads % rows;
-    float o[kIter];
+    const int rho = tid % rows, lane = tid / rows, lanes = kThreads / rows;   // threads of a row
+    const int groups = lanes >= COLS ? lanes / COLS : 1, step = lanes >= COLS ? COLS : lanes;
+    const int g = lane / step, first = lane % step;          // features first, first + step, ...
+    float m = -INFINITY, l = 0.f, o[kIter];
 #pragma unroll
     for (int k = 0; k < kIter; ++k) o[k] = 0.f;
-    const int chunk = kJoinWeights / rows;
-    for (int i0 = 0; i0 < n; i0 += chunk) {
-        const int nc = n - i0 < chunk ? n - i0 : chunk;
-        __syncthreads();
-        for (int x = tid; x < nc * rows; x += kThreads)
-            s_w[x] = exp2f(part_of(i0 + x / rows)[x % rows] - s_base[x % rows]);
-        __syncthreads();
-        if (g >= groups) continue;
-#pragma unroll 4
-        for (int i = g; i < nc; i += groups) {
-            const float *p = part_of(i0 + i) + 2 * rows + (size_t)col0 * rows;
-            int rho = rho0;
+    if (g < groups) {
+#pragma unroll 2
+        for (int i = g; i < n; i += groups) {
+            const float *p = part_of(i);
+            const float mi = p[rho], li = p[rows + rho];
+            float v[kIter];
 #pragma unroll
             for (int k = 0; k < kIter; ++k) {
-                const int item = item0 + k * kThreads;
-                if (item < items) o[k] = fmaf(s_w[i * rows + rho], p[item], o[k]);
-                rho += step_row;
-                if (rho >= rows) rho -= rows;
+                const int col = first + k * step;
+                v[k] = col < COLS ? p[2 * rows + (size_t)(col0 + col) * rows + rho] : 0.f;
             }
+            const Merge w(m, mi);
+            l = l * w.keep + li * w.add;
+#pragma unroll
+            for (int k = 0; k < kIter; ++k) o[k] = o[k] * w.keep + v[k] * w.add;
         }
     }
-    {
-        int rho = rho0, col = item0 / rows;
-        const int step_col = kThreads / rows;
+    if (groups > 1) {                                        // one feature a thread
+        s_m[tid] = m;
+        s_l[tid] = l;
+        s_o[tid] = o[0];
+        __syncthreads();
+        if (g == 0) {
+            for (int y = 1; y < groups; ++y) {
+                const int other = tid + y * COLS * rows;
+                const Merge w(m, s_m[other]);
+                l = l * w.keep + s_l[other] * w.add;
+                o[0] = o[0] * w.keep + s_o[other] * w.add;
+            }
+        }
+        __syncthreads();
+    }
+    if (g == 0) {
+        const float inv = 1.f / l;
 #pragma unroll
         for (int k = 0; k < kIter; ++k) {
-            if (g < groups && item0 + k * kThreads < items) s_o[(g * rows + rho) * (COLS + 1) + col] = o[k];
-            rho += step_row;
-            col += step_col;
-            if (rho >= rows) {
-                rho -= rows;
-                ++col;
-            }
+            const int col = first + k * step;
+            if (col < COLS) s_o[rho * (COLS + 1) + col] = o[k] * inv;
         }
     }
     __syncthreads();
     const Unit u = unit_of(a, note.m);
     for (int x = tid; x < rows * (COLS / 4); x += kThreads) {
-        const int rho = x / (COLS / 4), col = x % (COLS / 4) * 4;
+        const int r = x / (COLS / 4), col = x % (COLS / 4) * 4;
         size_t at;
-        if (!row_at(a, note.req, u, rho, at)) continue;
-        float v[4] = {0.f, 0.f, 0.f, 0.f};
-        for (int y = 0; y < groups; ++y) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] += s_o[(y * rows + rho) * (COLS + 1) + col + i];
-        }
-        const float f = s_inv[rho];
-        store4(static_cast<T *>(a.O) + at + col0 + col, make_float4(v[0] * f, v[1] * f, v[2] * f, v[3] * f));
+        if (!row_at(a, note.req, u, r, at)) continue;
+        const float *v = s_o + r * (COLS + 1) + col;
+        store4(static_cast<T *>(a.O) + at + col0 + col, make_float4(v[0], v[1], v[2], v[3]));
     }
 }
 
 // The join of a call whose attention kernel was launched just before.
 template <typename T> cudaError_t launch_join(const PagedArgs &a, cudaStream_t st)
 {
-    // many partials of few rows: more blocks of fewer features
-    const bool few = a.Bt * a.Gt <= 16;
-    static_assert(16 * 16 == kThreads, "one item a thread");
-    const dim3 grid(a.n_cta, a.d / (few ? 16 : 32));
-    return few ? pipe::launch_early(k_paged_join<T, 16>, grid, dim3(kThreads), 0, st, a)
-               : pipe::launch_early(k_paged_join<T, 32>, grid, dim3(kThreads), 0, st, a);
+    // many partials of few rows: more blocks of fewer features, with little shared
+    // memory, so that they are in place before the attention kernel ends
+    const int rows = a.Bt * a.Gt;
+    if (rows <= 16)
+        return pipe::launch_early(k_paged_join<T, 16, 16>, dim3(a.n_cta, a.d / 16), dim3(kThreads), 0, st, a);
+    return pipe::launch_early(k_paged_join<T, 32, kMaxRows>, dim3(a.n_cta, a.d / 32), dim3(kThreads), 0, st, a);
 }
 
 template <int D> cudaError_t launch_f32(const PagedArgs &a, cudaStream_t st)

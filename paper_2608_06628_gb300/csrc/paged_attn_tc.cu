@@ -56,6 +56,8 @@ constexpr int kSmemLimit = 232448;
 constexpr int kMaxSlots = 12;
 constexpr uint32_t kBarBytes = 1024;      // barriers, TMEM address, failure flag, the plan's scratch
 constexpr uint32_t kExchange = 1024;      // two floats a row
+// with copies: 64 inverse sums, and 128 rows of 32 + 4 features (a quarter of the rows: 128 + 4)
+constexpr uint32_t kStage = 256 + 128 * 36 * 4;
 constexpr float kSlack = 8.f;             // log2 of the largest p
 
 struct TcArgs {
@@ -140,6 +142,7 @@ __global__ void __launch_bounds__(Roles<kCopies>::kThreads, 1) k_paged_attn_tc(c
     volatile int *fail = reinterpret_cast<volatile int *>(tmem_holder + 1);
     PlanSmem *plan_smem = reinterpret_cast<PlanSmem *>(tmem_holder + 2);
     float *exchange = reinterpret_cast<float *>(smem + ta.off_bar + kBarBytes);   // [2][128]
+    float *inv_of = exchange + 256;                        // [64], with copies
 
     if (warp == W::kIssueS) {
         tmem_alloc(tmem_holder, 512);
@@ -326,7 +329,7 @@ __global__ void __launch_bounds__(Roles<kCopies>::kThreads, 1) k_paged_attn_tc(c
         const uint32_t lane_off = (uint32_t)(32 * quad) << 16;
         const uint32_t group_bar = kCopies > 1 ? 1 : 1 + quad;
         const float to_log2 = kLog2e * rsqrtf((float)D);
-        float *stage = reinterpret_cast<float *>(smem + ta.off_stage);   // [128][33], with copies
+        float *stage = reinterpret_cast<float *>(smem + ta.off_stage);   // with copies
         uint32_t n = 0;                                    // tiles so far
         bool bad = false;                                  // a wait gave up: leave at the next vote
         auto wait = [&](uint64_t *bar, uint32_t parity) {
@@ -473,6 +476,7 @@ __global__ void __launch_bounds__(Roles<kCopies>::kThreads, 1) k_paged_attn_tc(c
 #pragma unroll
                 for (int c = 0; c < kCopies; ++c)
                     l = fmaf(exchange[128 + c * kCopyRows + row], ex2(exchange[c * kCopyRows + row] - base), l);
+                if (copy == 0) inv_of[row] = 1.f / l;              // read after the next barrier
             } else {
                 group_sync_failed(group_bar, kGroup, false);       // the exchanged maxima have been read
                 exchange[part * 128 + row] = l;
@@ -486,41 +490,82 @@ __global__ void __launch_bounds__(Roles<kCopies>::kThreads, 1) k_paged_attn_tc(c
             }
             wait(&pvdone[(n - 1) & 1], ((n - 1) >> 1) & 1u);
             tc_fence_after();
+            if constexpr (kCopies > 1) {
+                // The copies' rows are added in order, in shared memory, as many features
+                // (32, 64 or 128) at a time as it holds of these rows: [copy][row][width + 4].
+                const int width = rows <= kCopyRows / 4 ? 128 : (rows <= kCopyRows / 2 ? 64 : 32);
+                const int span = width < D ? width : D, pitch = span + 4;
 #pragma unroll 1
-            for (int x = 0; x < kFeat / 32; ++x) {
-                float o[32];
-                tmem_ld32(tmem + cO + kFeat * part + 32 * x + lane_off, o);
-                tmem_wait_ld();
-                if (x == kFeat / 32 - 1) arrive(ofree);
-                constexpr int kCols = 32 / kCopies;        // features of these 32 that this thread writes
-                const int col = kFeat * part + 32 * x + (kCopies > 1 ? copy * kCols : 0);
-                if (kCopies > 1) {
-                    // the copies' rows, added in order
+                for (int x0 = 0; x0 < D; x0 += span) {
+                    float *mine = stage + (copy * rows + row) * pitch;
+#pragma unroll 1
+                    for (int x = 0; x < span; x += 32) {
+                        float o[32];
+                        tmem_ld32(tmem + cO + x0 + x + lane_off, o);
+                        tmem_wait_ld();
+                        if (row < rows) {
 #pragma unroll
-                    for (int y = 0; y < 32; ++y) stage[tid * 33 + y] = o[y] * f;
+                            for (int y = 0; y < 32; y += 4)
+                                *reinterpret_cast<float4 *>(mine + x + y) =
+                                    make_float4(o[y] * f, o[y + 1] * f, o[y + 2] * f, o[y + 3] * f);
+                        }
+                    }
+                    if (x0 + span == D) arrive(ofree);
                     group_sync_failed(group_bar, kGroup, false);
+                    if (!bad) {
+                        if (whole) {                       // eight features of a row
+                            for (int x = tid; x < rows * (span / 8); x += 128) {
+                                const int r = x / (span / 8), col = x % (span / 8) * 8;
+                                const float *src = stage + r * pitch + col;
+                                float4 v0 = make_float4(0.f, 0.f, 0.f, 0.f), v1 = v0;
 #pragma unroll
-                    for (int y = 0; y < kCols; ++y) {
-                        float v = 0.f;
+                                for (int c = 0; c < kCopies; ++c) {
+                                    const float4 s0 = *reinterpret_cast<const float4 *>(src + c * rows * pitch);
+                                    const float4 s1 = *reinterpret_cast<const float4 *>(src + c * rows * pitch + 4);
+                                    v0 = make_float4(v0.x + s0.x, v0.y + s0.y, v0.z + s0.z, v0.w + s0.w);
+                                    v1 = make_float4(v1.x + s1.x, v1.y + s1.y, v1.z + s1.z, v1.w + s1.w);
+                                }
+                                const float k = inv_of[r];
+                                size_t to;
+                                if (row_at(a, w.req, u, r, to))
+                                    *reinterpret_cast<uint4 *>(static_cast<bf16 *>(a.O) + to + x0 + col) = make_uint4(
+                                        pack_bf16x2(v0.x * k, v0.y * k), pack_bf16x2(v0.z * k, v0.w * k),
+                                        pack_bf16x2(v1.x * k, v1.y * k), pack_bf16x2(v1.z * k, v1.w * k));
+                            }
+                        } else {                           // feature-major, as the join reads it
+                            for (int x = tid; x < rows * span; x += 128) {
+                                const int r = x % rows, col = x / rows;
+                                float v = 0.f;
 #pragma unroll
-                        for (int c = 0; c < kCopies; ++c) v += stage[(c * kCopyRows + row) * 33 + copy * kCols + y];
-                        o[y] = v;
+                                for (int c = 0; c < kCopies; ++c) v += stage[(c * rows + r) * pitch + col];
+                                partial[2 * rows + (size_t)x0 * rows + x] = v;
+                            }
+                        }
                     }
                     group_sync_failed(group_bar, kGroup, false);
                 }
-                if (bad) continue;
-                if (whole) {
-                    if (live) {
+            } else {
+#pragma unroll 1
+                for (int x = 0; x < kFeat / 32; ++x) {
+                    float o[32];
+                    tmem_ld32(tmem + cO + kFeat * part + 32 * x + lane_off, o);
+                    tmem_wait_ld();
+                    if (x == kFeat / 32 - 1) arrive(ofree);
+                    if (bad) continue;
+                    const int col = kFeat * part + 32 * x;
+                    if (whole) {
+                        if (live) {
 #pragma unroll
-                        for (int y = 0; y < kCols; y += 8)
-                            *reinterpret_cast<uint4 *>(out + col + y) = make_uint4(
-                                pack_bf16x2(o[y] * inv, o[y + 1] * inv), pack_bf16x2(o[y + 2] * inv, o[y + 3] * inv),
-                                pack_bf16x2(o[y + 4] * inv, o[y + 5] * inv), pack_bf16x2(o[y + 6] * inv, o[y + 7] * inv));
+                            for (int y = 0; y < 32; y += 8)
+                                *reinterpret_cast<uint4 *>(out + col + y) = make_uint4(
+                                    pack_bf16x2(o[y] * inv, o[y + 1] * inv), pack_bf16x2(o[y + 2] * inv, o[y + 3] * inv),
+                                    pack_bf16x2(o[y + 4] * inv, o[y + 5] * inv), pack_bf16x2(o[y + 6] * inv, o[y + 7] * inv));
+                        }
+                    } else if (row < rows) {
+                        float *po = partial + 2 * rows + (size_t)col * rows + row;
+#pragma unroll
+                        for (int y = 0; y < 32; ++y) po[(size_t)y * rows] = o[y];
                     }
-                } else if (row < rows) {
-                    float *po = partial + 2 * rows + (size_t)col * rows + row;
-#pragma unroll
-                    for (int y = 0; y < kCols; ++y) po[(size_t)y * rows] = o[y];
                 }
             }
         }
@@ -538,14 +583,15 @@ template <int D, int kCopies> cudaError_t launch(const PagedArgs &a, cudaStream_
     TcArgs ta;
     ta.p = a;
     // Q, K/V rings, barriers, exchange, stage (with copies), and 1 KB for alignment
-    const uint32_t slot = kTile * D * 2, stage = kCopies > 1 ? 128 * 33 * sizeof(float) : 0;
+    const uint32_t slot = kTile * D * 2, stage = kCopies > 1 ? kStage : 0;
     const uint32_t tail = kBarBytes + kExchange + stage + 1024;
     int ns = (int)((kSmemLimit - tail) / slot) - 1;
     if (ns > kMaxSlots) ns = kMaxSlots;
-    ta.NK = (ns + 1) / 2;
-    ta.NV = ns / 2;
+    // S has two buffers of its own, so V waits longer for its product than K
+    ta.NK = ns / 2;
+    ta.NV = ns - ta.NK;
     ta.off_bar = (1 + ns) * slot;
-    ta.off_stage = ta.off_bar + kBarBytes + kExchange;
+    ta.off_stage = ta.off_bar + kBarBytes + kExchange + 256;
     ta.bytes = ta.off_bar + tail;
     {
         const cuuint64_t dq[4] = {(cuuint64_t)D, (cuuint64_t)a.Hq, (cuuint64_t)a.B, (cuuint64_t)a.n_req};
