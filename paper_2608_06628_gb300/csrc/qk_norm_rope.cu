@@ -9,15 +9,20 @@
 // Forward and backward read each input once and write each output once; memory
 // bounds them.
 //
-// A warp takes one token and a run of its heads.  A head lies across D / E lanes,
-// E = 16 bytes of elements each, so every load and store is 16 bytes a lane and
-// 512 a warp.  The angles depend on the token only: each lane forms the cosines
-// and sines of its own features once and uses them for all heads of the run.  A
-// pair's other member is in the same lane (interleaved) or rot / 2 features away,
-// which is a whole number of lanes because rot is a multiple of 16: one shuffle
-// per feature.  Everything is float32; outputs are rounded once.
-#include <math_constants.h>
-
+// A warp takes one token and a run of its rows (heads of Q, of K, of V), then
+// another token.  A row lies across D / E lanes, E = 16 bytes of elements each: the
+// first members of E / 2 pairs and their second members, so a pair is always in one
+// lane.  With interleaved pairs these are 16 bytes in a row, with the half layout
+// twice 8 bytes (rot is a multiple of 16, so they are aligned, and a lane's pairs
+// are all rotated or all not).  Each thread copies what it will need next into a
+// ring of its own in shared memory (cp.async), kDepth steps ahead, across tokens:
+// that keeps 64 KB and more in flight per SM without holding registers, and needs
+// no barrier, since a thread reads only what it has copied.  The angles depend on
+// the token only: the lanes of a warp form them once, two each at most, and read
+// their own from shared memory.  Beside memory the issue slots count: at the
+// memory's rate an SM has about 170 (backward 260) for the 512 (2 x 512) bytes of a
+// step, so what depends on the kind of row is set where the kind changes, and a
+// step only advances pointers.  Everything is float32; outputs are rounded once.
 #include "hybrid_common.cuh"
 #include "softmax_kernels.h"
 #include "tc_pipeline.cuh"
@@ -27,7 +32,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
-constexpr int kMaxBackwardBlocks = 608;     // partial sums of dw: 4 blocks per SM of 152
+constexpr int kMaxBackwardBlocks = 512;     // partial sums of dw
 
 template <typename T> struct Vec {
     static constexpr int E = 16 / sizeof(T);
@@ -68,271 +73,377 @@ template <int L> __device__ __forceinline__ float head_sum(float v)
     return v;
 }
 
-// What a lane needs to rotate its E features: cos and sin (times scale) of each,
-// and the lane that holds the other member of its pairs (half layout).
-template <int E> struct Rotation {
-    float c[E], s[E];
-    int partner;        // lane offset of the other member
-    bool on;            // the lane's features are rotated
+constexpr int kMaxPairs = 64;
+constexpr int kDepth = 4;           // steps ahead
+
+// Where a lane's features lie in a row: two pieces of E / 2.
+template <int D, int E, bool kInter> struct Pieces {
+    int first, second;              // offsets of the pieces
+    int pair;                       // its first pair
+    bool on;                        // its pairs are rotated
+    __device__ Pieces(const RopeArgs &a, int l)
+    {
+        pair = l * (E / 2);
+        const int half = a.rot >> 1;
+        on = pair < half;
+        if (kInter) {
+            first = l * E;
+            second = first + E / 2;
+        } else if (on) {
+            first = pair;
+            second = half + pair;
+        } else {                    // beyond the rotated part, halves of what is left
+            first = a.rot + (pair - half);
+            second = first + (D / 2 - half);
+        }
+    }
 };
 
+template <int E, bool kInter, typename T>
+__device__ __forceinline__ void copy_async(uint4 *dst, const T *row, int first, int second)
+{
+    if (kInter) {
+        ptx::cp_async16(dst, row + first);
+    } else {
+        asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(ptx::smem_u32(dst)), "l"(row + first) : "memory");
+        asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(ptx::smem_u32(dst) + 8), "l"(row + second)
+                     : "memory");
+    }
+}
+template <int E, bool kInter, typename T>
+__device__ __forceinline__ void store(T *row, int first, int second, const uint4 &v)
+{
+    if (kInter) {
+        *reinterpret_cast<uint4 *>(row + first) = v;
+    } else {
+        *reinterpret_cast<uint2 *>(row + first) = make_uint2(v.x, v.y);
+        *reinterpret_cast<uint2 *>(row + second) = make_uint2(v.z, v.w);
+    }
+}
+template <int E, bool kInter, typename T>
+__device__ __forceinline__ uint4 load(const T *row, int first, int second)
+{
+    if (kInter) return __ldg(reinterpret_cast<const uint4 *>(row + first));
+    const uint2 x = __ldg(reinterpret_cast<const uint2 *>(row + first));
+    const uint2 y = __ldg(reinterpret_cast<const uint2 *>(row + second));
+    return make_uint4(x.x, x.y, y.x, y.y);
+}
+
+// Cosine and sine (times scale) of a lane's E / 2 pairs.
+template <int E> struct Rotation {
+    float c[E / 2], s[E / 2];
+};
+
+// The angles of token t, by the whole warp; `table` is the warp's own.
 template <int E>
-__device__ __forceinline__ Rotation<E> make_rotation(const RopeArgs &a, int t, int e0)
+__device__ __forceinline__ void make_rotation(const RopeArgs &a, int t, int pair0, bool on, float2 *table,
+                                              Rotation<E> &r)
 {
-    Rotation<E> r;
-    const int half = a.rot >> 1;
-    r.on = e0 < a.rot;
-    r.partner = 0;
+    const int lane = threadIdx.x & 31, half = a.rot >> 1;
+    if (half == 0) return;
+    __syncwarp();                                   // the last token's have been read
+    const unsigned long long p = (unsigned long long)(long long)__ldg(a.positions + t);
 #pragma unroll
-    for (int i = 0; i < E; ++i) {
-        r.c[i] = 1.f;
-        r.s[i] = 0.f;
-    }
-    if (!r.on) return r;
-    const unsigned long long p = (unsigned long long)(long long)a.positions[t];
-    const bool second = !a.interleaved && e0 >= half;
-    if (!a.interleaved) r.partner = second ? -(half / E) : half / E;
-#pragma unroll
-    for (int i = 0; i < E; ++i) {
-        if (a.interleaved && (i & 1)) {             // the pair's angle again
-            r.c[i] = r.c[i - 1];
-            r.s[i] = -r.s[i - 1];
-            continue;
+    for (int i = 0; i < kMaxPairs / 32; ++i) {
+        const int pair = lane + 32 * i;
+        if (pair < half) {
+            // fraction of a turn, exact modulo 1, as a signed number of half turns
+            const int frac = (int)(unsigned)((p * __ldg(a.freqs + pair)) >> 32);
+            float s, c;
+            sincospif((float)frac * 0x1p-31f, &s, &c);
+            table[pair] = make_float2(c * a.scale, s * a.scale);
         }
-        const int pair = a.interleaved ? (e0 + i) >> 1 : (second ? e0 - half : e0) + i;
-        // fraction of a turn, exact modulo 1, as a signed number of half turns
-        const int frac = (int)(unsigned)((p * a.freqs[pair]) >> 32);
-        float s, c;
-        sincospif((float)frac * 0x1p-31f, &s, &c);
-        r.c[i] = c * a.scale;
-        // the first member gets -b sin, the second +a sin
-        r.s[i] = (second ? s : -s) * a.scale;
     }
-    return r;
+    __syncwarp();
+    if (on) {
+#pragma unroll
+        for (int i = 0; i < E / 2; ++i) {
+            const float2 v = table[pair0 + i];
+            r.c[i] = v.x;
+            r.s[i] = v.y;
+        }
+    }
 }
 
-// x <- R x (kInverse: R^T x).  All lanes of the warp take part.
-template <int E, bool kInverse>
-__device__ __forceinline__ void rotate(float (&x)[E], const Rotation<E> &r, bool interleaved, int lane)
+// x <- R x (kInverse: R^T x) for a lane whose pairs are rotated.
+template <int E, bool kInter, bool kInverse>
+__device__ __forceinline__ void rotate(float (&x)[E], const Rotation<E> &r)
 {
-    if (interleaved) {
 #pragma unroll
-        for (int i = 0; i < E; i += 2) {
-            const float a = x[i], b = x[i + 1];
-            const float sa = kInverse ? -r.s[i] : r.s[i], sb = kInverse ? -r.s[i + 1] : r.s[i + 1];
-            if (r.on) {
-                x[i] = a * r.c[i] + b * sa;
-                x[i + 1] = b * r.c[i + 1] + a * sb;
+    for (int i = 0; i < E / 2; ++i) {
+        float &a = x[kInter ? 2 * i : i], &b = x[kInter ? 2 * i + 1 : E / 2 + i];
+        const float s = kInverse ? -r.s[i] : r.s[i], a0 = a;
+        a = a0 * r.c[i] - b * s;
+        b = b * r.c[i] + a0 * s;
+    }
+}
+
+// The rows of a token in steps of RPW: kinds 0 (Q), 1 (K) and, with the cache, 2
+// (V), each padded to whole steps.  Part `part` of `parts` takes `run` steps.
+struct Split {
+    unsigned items;                 // tokens * parts
+    int parts, run, steps;          // steps of a token
+    int steps_q, steps_k;
+};
+
+// A warp's place in its rows.
+template <int RPW> struct Cursor {
+    unsigned item;
+    int t, kind, left, h;           // token, kind, steps left in the part, first row of the step
+
+    __device__ bool live(const Split &s) const { return item < s.items; }
+    __device__ void enter(const Split &s)
+    {
+        t = s.parts == 1 ? (int)item : (int)(item / (unsigned)s.parts);
+        int at = s.parts == 1 ? 0 : (int)(item - (unsigned)t * s.parts) * s.run;
+        left = s.steps - at < s.run ? s.steps - at : s.run;
+        kind = 0;
+        if (at >= s.steps_q) {
+            at -= s.steps_q;
+            kind = 1;
+            if (at >= s.steps_k) {
+                at -= s.steps_k;
+                kind = 2;
             }
         }
-    } else {
-#pragma unroll
-        for (int i = 0; i < E; ++i) {
-            const float o = __shfl_sync(0xffffffffu, x[i], lane + r.partner);
-            if (r.on) x[i] = x[i] * r.c[i] + o * (kInverse ? -r.s[i] : r.s[i]);
-        }
+        h = at * RPW;
     }
-}
+    // Advance; true if the rows go on in another kind or token.
+    __device__ bool step(const Split &s, int n_heads, unsigned stride)
+    {
+        h += RPW;
+        if (--left == 0) {
+            item = s.items - item > stride ? item + stride : s.items;
+            if (live(s)) enter(s);
+            return true;
+        }
+        if (h < n_heads) return false;
+        ++kind;
+        h = 0;
+        return true;
+    }
+};
 
-template <typename T, int D>
-__global__ __launch_bounds__(kThreads, 3) void k_qk_norm_rope(const RopeArgs a, int parts, int rows_per_part)
+template <int N> __device__ __forceinline__ void async_wait()
 {
-    constexpr int E = Vec<T>::E, L = D / E, RPW = 32 / L, U = E == 8 ? 2 : 4;
-    const int lane = threadIdx.x & 31, sub = lane / L, e0 = (lane % L) * E;
-    const long long item = (long long)blockIdx.x * kWarps + (threadIdx.x >> 5);
+    asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ void async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+
+template <typename T, int D, bool kInter>
+__global__ __launch_bounds__(kThreads, 4) void k_qk_norm_rope(const RopeArgs a, const Split split)
+{
+    constexpr int E = Vec<T>::E, L = D / E, RPW = 32 / L;
+    __shared__ uint4 s_ring[kDepth][kThreads];
+    __shared__ float2 s_angles[kWarps][kMaxPairs];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, sub = lane / L;
+    const Pieces<D, E, kInter> piece(a, lane % L);
+    const unsigned stride = gridDim.x * kWarps;
     ptx::griddep_wait();
     ptx::griddep_launch_dependents();
-    if (item >= (long long)a.n_tok * parts) return;
-    const int t = (int)(item / parts), part = (int)(item % parts);
-    const int n_rows = a.Hq + (a.slots ? 2 : 1) * a.Hkv;    // q heads, k heads, v heads
-    const int begin = part * rows_per_part;
-    const int end = begin + rows_per_part < n_rows ? begin + rows_per_part : n_rows;
+    Cursor<RPW> at, ahead;
+    at.item = ahead.item = blockIdx.x * kWarps + warp;
+    if (!at.live(split)) return;
+    auto heads = [&](int kind) { return kind == 0 ? a.Hq : a.Hkv; };
 
-    const T *Q = static_cast<const T *>(a.Q) + (size_t)t * a.q_stride + e0;
-    const T *K = static_cast<const T *>(a.K) + (size_t)t * a.k_stride + e0;
-    const T *V = static_cast<const T *>(a.V) + (size_t)t * a.v_stride + e0;
-    T *Qo = static_cast<T *>(a.Qo) + (size_t)t * a.Hq * D + e0;
-    // key head h of the token: base + h * step
-    T *Ko, *Vo = nullptr;
-    size_t step = D;
-    bool write_kv = true;
-    if (a.slots) {
-        const int slot = a.slots[t];
-        const int page = slot / a.page_size;
-        write_kv = slot >= 0 && page < a.n_pages;
-        if (slot >= 0 && !write_kv && lane == 0) raise_error(a.err, ERR_BAD_INDEX);
-        const size_t at =
-            write_kv ? ((size_t)page * a.Hkv * a.page_size + (size_t)(slot % a.page_size)) * D + e0 : 0;
-        step = (size_t)a.page_size * D;
-        Ko = static_cast<T *>(a.K_cache) + at;
-        Vo = static_cast<T *>(a.V_cache) + at;
-    } else {
-        Ko = static_cast<T *>(a.Ko) + (size_t)t * a.Hkv * D + e0;
-    }
-    // U rows a lane group are loaded before the angles are formed, and the next U
-    // while these are worked on
-    uint4 raw[U], next[U];
-    auto load = [&](int h0, uint4 (&r)[U]) {
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int h = h0 + u * RPW + sub;
-            r[u] = make_uint4(0, 0, 0, 0);
-            if (h < end) {
-                const T *src = h < a.Hq ? Q + (size_t)h * D
-                                        : (h < a.Hq + a.Hkv ? K + (size_t)(h - a.Hq) * D
-                                                            : V + (size_t)(h - a.Hq - a.Hkv) * D);
-                r[u] = *reinterpret_cast<const uint4 *>(src);
+    // loads, kDepth steps ahead
+    const T *src = nullptr;                 // this lane group's row of the step
+    auto source = [&]() {
+        const T *base = ahead.kind == 0   ? static_cast<const T *>(a.Q) + (size_t)ahead.t * a.q_stride
+                        : ahead.kind == 1 ? static_cast<const T *>(a.K) + (size_t)ahead.t * a.k_stride
+                                          : static_cast<const T *>(a.V) + (size_t)ahead.t * a.v_stride;
+        src = base + (size_t)(ahead.h + sub) * D;
+    };
+    int ahead_heads = 0;
+    auto issue = [&](int slot) {
+        if (ahead.live(split)) {
+            if (ahead.h + sub < ahead_heads) copy_async<E, kInter>(&s_ring[slot][tid], src, piece.first, piece.second);
+            src += RPW * D;
+            if (ahead.step(split, ahead_heads, stride) && ahead.live(split)) {
+                ahead_heads = heads(ahead.kind);
+                source();
             }
         }
+        async_commit();
     };
-    load(begin, next);
-    const Rotation<E> rot = make_rotation<E>(a, t, e0);
+    ahead.enter(split);
+    ahead_heads = heads(ahead.kind);
+    source();
+#pragma unroll
+    for (int i = 0; i < kDepth; ++i) issue(i);
 
-    for (int h0 = begin; h0 < end; h0 += U * RPW) {
-#pragma unroll
-        for (int u = 0; u < U; ++u) raw[u] = next[u];
-        if (h0 + U * RPW < end) load(h0 + U * RPW, next);
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int h = h0 + u * RPW + sub;
-            if (h0 + u * RPW >= end) break;                 // the whole warp
-            float x[E];
-            Vec<T>::unpack(raw[u], x);
-            const bool is_q = h < a.Hq, is_k = !is_q && h < a.Hq + a.Hkv;
-            const void *w = is_q ? a.wq : (is_k ? a.wk : nullptr);
-            float ss = 0.f;
-#pragma unroll
-            for (int i = 0; i < E; ++i) ss = fmaf(x[i], x[i], ss);
-            ss = head_sum<L>(ss);
-            if (w) {
-                const float r = rsqrtf(ss * (1.f / D) + a.eps);
-                float g[E];
-                Vec<T>::unpack(*reinterpret_cast<const uint4 *>(static_cast<const T *>(w) + e0), g);
-#pragma unroll
-                for (int i = 0; i < E; ++i) x[i] = x[i] * r * g[i];
-            }
-            rotate<E, false>(x, rot, a.interleaved, lane);
-            if (h >= end) continue;
-            if (is_q) {
-                *reinterpret_cast<uint4 *>(Qo + (size_t)h * D) = Vec<T>::pack(x);
-            } else if (write_kv) {
-                if (is_k) *reinterpret_cast<uint4 *>(Ko + (size_t)(h - a.Hq) * step) = Vec<T>::pack(x);
-                else *reinterpret_cast<uint4 *>(Vo + (size_t)(h - a.Hq - a.Hkv) * step) = raw[u];
-            }
-        }
-    }
-}
-
-template <typename T, int D>
-__global__ __launch_bounds__(kThreads, 2) void k_qk_norm_rope_backward(const RopeArgs a, int parts, int rows_per_part)
-{
-    constexpr int E = Vec<T>::E, L = D / E, RPW = 32 / L, U = 2;
-    __shared__ float s_dw[kWarps][2][D];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = lane / L, e0 = (lane % L) * E;
-    const int n_rows = a.Hq + a.Hkv;
-    ptx::griddep_wait();
-    ptx::griddep_launch_dependents();
-    // the weights stay packed: they are unpacked where they are used
-    uint4 wq = make_uint4(0, 0, 0, 0), wk = wq;
-    float dwq[E], dwk[E];
-#pragma unroll
-    for (int i = 0; i < E; ++i) dwq[i] = dwk[i] = 0.f;
-    if (a.wq) wq = *reinterpret_cast<const uint4 *>(static_cast<const T *>(a.wq) + e0);
-    if (a.wk) wk = *reinterpret_cast<const uint4 *>(static_cast<const T *>(a.wk) + e0);
-    const long long items = (long long)a.n_tok * parts, stride = (long long)gridDim.x * kWarps;
-
-    // A warp's rows, U lane groups' worth at a time, over all of its tokens: the next
-    // ones are loaded while these are worked on.
-    struct Place {
-        long long item;
-        int h0;             // first row of the batch
-        int end;            // end of the token's rows
-    };
-    auto rows_of = [&](Place &p) {
-        const int begin = (int)(p.item % parts) * rows_per_part;
-        p.h0 = begin;
-        p.end = begin + rows_per_part < n_rows ? begin + rows_per_part : n_rows;
-    };
-    auto step = [&](Place &p) {
-        p.h0 += U * RPW;
-        if (p.h0 < p.end) return;
-        p.item += stride;
-        if (p.item < items) rows_of(p);
-    };
-    auto place_of = [&](const Place &p, int u, bool &live, bool &is_q, size_t &at, size_t &dy) {
-        const int t = (int)(p.item / parts), h = p.h0 + u * RPW + sub;
-        live = h < p.end;
-        is_q = h < a.Hq;
-        at = is_q ? (size_t)t * a.q_stride + (size_t)h * D + e0 : (size_t)t * a.k_stride + (size_t)(h - a.Hq) * D + e0;
-        dy = is_q ? ((size_t)t * a.Hq + h) * D + e0 : ((size_t)t * a.Hkv + (h - a.Hq)) * D + e0;
-    };
-    uint4 nx[U], ny[U];
-    auto load = [&](const Place &p) {
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            bool live, is_q;
-            size_t at, dy;
-            place_of(p, u, live, is_q, at, dy);
-            nx[u] = ny[u] = make_uint4(0, 0, 0, 0);
-            if (live) {
-                nx[u] = *reinterpret_cast<const uint4 *>(static_cast<const T *>(is_q ? a.Q : a.K) + at);
-                ny[u] = *reinterpret_cast<const uint4 *>(static_cast<const T *>(is_q ? a.dQo : a.dKo) + dy);
-            }
-        }
-    };
-    Place p{(long long)blockIdx.x * kWarps + warp, 0, 0};
-    if (p.item < items) {
-        rows_of(p);
-        load(p);
-    }
-    long long rotated = -1;                 // token of `rot`
     Rotation<E> rot;
-    while (p.item < items) {
-        const Place now = p;
-        uint4 rx[U], ry[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            rx[u] = nx[u];
-            ry[u] = ny[u];
+    float w[E];                             // the kind's weight
+    bool norm = false, write = true;
+    T *dst = nullptr;                       // this lane group's row of the output
+    size_t step = 0;                        // rows RPW apart in the output
+    int n_heads = 0, token = -1, slot_of = -1;
+    auto enter = [&]() {                    // another kind or token
+        n_heads = heads(at.kind);
+        if (at.t != token) {
+            token = at.t;
+            make_rotation<E>(a, token, piece.pair, piece.on, s_angles[warp], rot);
+            if (a.slots) slot_of = __ldg(a.slots + token);
         }
-        step(p);
-        if (p.item < items) load(p);
-        if (now.item / parts != rotated) {
-            rotated = now.item / parts;
-            rot = make_rotation<E>(a, (int)rotated, e0);
+        const void *wp = at.kind == 0 ? a.wq : (at.kind == 1 ? a.wk : nullptr);
+        norm = wp != nullptr;
+        if (norm) Vec<T>::unpack(load<E, kInter>(static_cast<const T *>(wp), piece.first, piece.second), w);
+        write = true;
+        step = (size_t)RPW * D;
+        if (at.kind == 0) {
+            dst = static_cast<T *>(a.Qo) + ((size_t)token * a.Hq + at.h + sub) * D;
+        } else if (!a.slots) {
+            dst = static_cast<T *>(a.Ko) + ((size_t)token * a.Hkv + at.h + sub) * D;
+        } else {
+            const int page = slot_of / a.page_size;
+            write = slot_of >= 0 && page < a.n_pages;
+            if (slot_of >= 0 && !write && lane == 0) raise_error(a.err, ERR_BAD_INDEX);
+            step *= a.page_size;
+            dst = static_cast<T *>(at.kind == 1 ? a.K_cache : a.V_cache);
+            if (write)
+                dst += (((size_t)page * a.Hkv + at.h + sub) * a.page_size + (size_t)(slot_of % a.page_size)) * D;
         }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (now.h0 + u * RPW >= now.end) break;         // the whole warp
-            bool live, is_q;
-            size_t at, dy;
-            place_of(now, u, live, is_q, at, dy);
-            float x[E], g[E], w[E];
-            Vec<T>::unpack(rx[u], x);
-            Vec<T>::unpack(ry[u], g);
-            Vec<T>::unpack(is_q ? wq : wk, w);
-            rotate<E, true>(g, rot, a.interleaved, lane);   // dn
-            float xx = 0.f, ux = 0.f;
-            const bool norm = is_q ? a.wq != nullptr : a.wk != nullptr;
-#pragma unroll
-            for (int i = 0; i < E; ++i) {
-                xx = fmaf(x[i], x[i], xx);
-                ux = fmaf(g[i] * w[i], x[i], ux);
-            }
-            xx = head_sum<L>(xx);
-            ux = head_sum<L>(ux);
-            if (!live) continue;
+    };
+    at.enter(split);
+    enter();
+    for (int slot = 0;; slot = (slot + 1) % kDepth) {
+        async_wait<kDepth - 1>();
+        const uint4 raw = s_ring[slot][tid];
+        uint4 out = raw;
+        if (at.kind < 2) {
+            float x[E];
+            Vec<T>::unpack(raw, x);
             if (norm) {
-                const float r = rsqrtf(xx * (1.f / D) + a.eps), m = r * ux * (1.f / D);   // m = mean(u xh)
+                float ss = 0.f;
+#pragma unroll
+                for (int i = 0; i < E; ++i) ss = fmaf(x[i], x[i], ss);
+                const float r = rsqrtf(head_sum<L>(ss) * (1.f / D) + a.eps);
+#pragma unroll
+                for (int i = 0; i < E; ++i) x[i] = x[i] * r * w[i];
+            }
+            if (piece.on) rotate<E, kInter, false>(x, rot);
+            out = Vec<T>::pack(x);
+        }
+        issue(slot);
+        if (write && at.h + sub < n_heads) store<E, kInter>(dst, piece.first, piece.second, out);
+        dst += step;
+        if (at.step(split, n_heads, stride)) {
+            if (!at.live(split)) break;
+            enter();
+        }
+    }
+}
+
+template <typename T, int D, bool kInter>
+__global__ __launch_bounds__(kThreads, 2) void k_qk_norm_rope_backward(const RopeArgs a, const Split split)
+{
+    constexpr int E = Vec<T>::E, L = D / E, RPW = 32 / L;
+    __shared__ uint4 s_ring[kDepth][2][kThreads];
+    __shared__ float2 s_angles[kWarps][kMaxPairs];
+    __shared__ float s_dw[kWarps][2][D];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, sub = lane / L;
+    const Pieces<D, E, kInter> piece(a, lane % L);
+    const unsigned stride = gridDim.x * kWarps;
+    ptx::griddep_wait();
+    ptx::griddep_launch_dependents();
+    Cursor<RPW> at, ahead;
+    at.item = ahead.item = blockIdx.x * kWarps + warp;
+    const bool work = at.live(split);
+    auto heads = [&](int kind) { return kind == 0 ? a.Hq : a.Hkv; };
+    // start of a token's rows of a kind in Q or K (or its gradient)
+    auto offset = [&](const Cursor<RPW> &c) {
+        return (size_t)c.t * (c.kind == 0 ? a.q_stride : a.k_stride) + (size_t)(c.h + sub) * D;
+    };
+
+    const T *src = nullptr, *src_dy = nullptr;
+    int ahead_heads = 0;
+    auto source = [&]() {
+        ahead_heads = heads(ahead.kind);
+        src = static_cast<const T *>(ahead.kind == 0 ? a.Q : a.K) + offset(ahead);
+        src_dy = static_cast<const T *>(ahead.kind == 0 ? a.dQo : a.dKo) +
+                 ((size_t)ahead.t * ahead_heads + ahead.h + sub) * D;
+    };
+    auto issue = [&](int slot) {
+        if (ahead.live(split)) {
+            if (ahead.h + sub < ahead_heads) {
+                copy_async<E, kInter>(&s_ring[slot][0][tid], src, piece.first, piece.second);
+                copy_async<E, kInter>(&s_ring[slot][1][tid], src_dy, piece.first, piece.second);
+            }
+            src += RPW * D;
+            src_dy += RPW * D;
+            if (ahead.step(split, ahead_heads, stride) && ahead.live(split)) source();
+        }
+        async_commit();
+    };
+    // sums of dw over the rows of the current kind and of the other one
+    float dw[E], dw_other[E];
+#pragma unroll
+    for (int i = 0; i < E; ++i) dw[i] = dw_other[i] = 0.f;
+    int kind = 0;                           // of `dw`
+    if (work) {
+        ahead.enter(split);
+        source();
+#pragma unroll
+        for (int i = 0; i < kDepth; ++i) issue(i);
+
+        Rotation<E> rot;
+        float w[E];
+        bool norm = false;
+        T *dst = nullptr;
+        int n_heads = 0, token = -1;
+        auto enter = [&]() {                // another kind or token
+            n_heads = heads(at.kind);
+            if (at.t != token) {
+                token = at.t;
+                make_rotation<E>(a, token, piece.pair, piece.on, s_angles[warp], rot);
+            }
+            const void *wp = at.kind == 0 ? a.wq : a.wk;
+            norm = wp != nullptr;
+            if (norm) Vec<T>::unpack(load<E, kInter>(static_cast<const T *>(wp), piece.first, piece.second), w);
+            dst = static_cast<T *>(at.kind == 0 ? a.Qo : a.Ko) + offset(at);
+            if (at.kind != kind) {
+                kind = at.kind;
 #pragma unroll
                 for (int i = 0; i < E; ++i) {
-                    const float xh = x[i] * r, dw = g[i] * xh;
-                    if (is_q) dwq[i] += dw;
-                    else dwk[i] += dw;
-                    g[i] = r * (g[i] * w[i] - xh * m);
+                    const float x = dw[i];
+                    dw[i] = dw_other[i];
+                    dw_other[i] = x;
                 }
             }
-            *reinterpret_cast<uint4 *>(static_cast<T *>(is_q ? a.Qo : a.Ko) + at) = Vec<T>::pack(g);
+        };
+        at.enter(split);
+        enter();
+        for (int slot = 0;; slot = (slot + 1) % kDepth) {
+            async_wait<kDepth - 1>();
+            float x[E], g[E];
+            Vec<T>::unpack(s_ring[slot][1][tid], g);
+            if (piece.on) rotate<E, kInter, true>(g, rot);          // dn
+            const bool live = at.h + sub < n_heads;
+            if (norm) {
+                Vec<T>::unpack(s_ring[slot][0][tid], x);
+                float xx = 0.f, ux = 0.f, u[E];
+#pragma unroll
+                for (int i = 0; i < E; ++i) {
+                    u[i] = g[i] * w[i];
+                    xx = fmaf(x[i], x[i], xx);
+                    ux = fmaf(u[i], x[i], ux);
+                }
+                const float r = rsqrtf(head_sum<L>(xx) * (1.f / D) + a.eps);
+                const float m = r * r * head_sum<L>(ux) * (1.f / D);    // r mean(u xh)
+#pragma unroll
+                for (int i = 0; i < E; ++i) {
+                    const float xh = x[i] * r;
+                    if (live) dw[i] = fmaf(g[i], xh, dw[i]);
+                    g[i] = r * u[i] - xh * m;
+                }
+            }
+            issue(slot);
+            if (live) store<E, kInter>(dst, piece.first, piece.second, Vec<T>::pack(g));
+            dst += RPW * D;
+            if (at.step(split, n_heads, stride)) {
+                if (!at.live(split)) break;
+                enter();
+            }
         }
     }
     // heads of the warp, then warps of the block, in a fixed order
@@ -340,12 +451,13 @@ __global__ __launch_bounds__(kThreads, 2) void k_qk_norm_rope_backward(const Rop
     for (int i = 0; i < E; ++i) {
 #pragma unroll
         for (int o = L; o < 32; o <<= 1) {
-            dwq[i] += __shfl_xor_sync(0xffffffffu, dwq[i], o);
-            dwk[i] += __shfl_xor_sync(0xffffffffu, dwk[i], o);
+            dw[i] += __shfl_xor_sync(0xffffffffu, dw[i], o);
+            dw_other[i] += __shfl_xor_sync(0xffffffffu, dw_other[i], o);
         }
         if (sub == 0) {
-            s_dw[warp][0][e0 + i] = dwq[i];
-            s_dw[warp][1][e0 + i] = dwk[i];
+            const int c = i < E / 2 ? piece.first + i : piece.second + i - E / 2;
+            s_dw[warp][kind][c] = dw[i];
+            s_dw[warp][1 - kind][c] = dw_other[i];
         }
     }
     __syncthreads();
@@ -377,45 +489,61 @@ __global__ __launch_bounds__(kThreads) void k_dw_reduce(const float *partial, in
     }
 }
 
-// Heads per warp: all heads of a token when there are enough tokens to fill the
-// GPU, else runs short enough that about 16 warps a multiprocessor have one.
-void split_heads(long long n_tok, int n_rows, int rpw, int &parts, int &rows_per_part)
+// A warp takes all rows of a token when there are enough tokens to fill the GPU,
+// else runs of them short enough that about 16 warps a multiprocessor have one.
+Split split_rows(const RopeArgs &a, int rpw)
 {
-    const long long want = 152 * 16;
-    const int most = (n_rows + rpw - 1) / rpw;              // parts of one row a lane group
-    long long p = (want + n_tok - 1) / n_tok;
-    if (p > most) p = most;
-    if (p < 1) p = 1;
-    rows_per_part = (int)((n_rows + p - 1) / p);
-    rows_per_part = (rows_per_part + rpw - 1) / rpw * rpw;
-    parts = (n_rows + rows_per_part - 1) / rows_per_part;
+    Split s;
+    s.steps_q = (a.Hq + rpw - 1) / rpw;
+    s.steps_k = (a.Hkv + rpw - 1) / rpw;
+    s.steps = s.steps_q + (a.slots ? 2 : 1) * s.steps_k;
+    long long p = (152 * 16 + a.n_tok - 1) / a.n_tok;
+    if (p > s.steps) p = s.steps;
+    s.run = (int)((s.steps + p - 1) / p);
+    s.parts = (s.steps + s.run - 1) / s.run;
+    s.items = (unsigned)a.n_tok * (unsigned)s.parts;        // parts > 1 only for few tokens
+    return s;
 }
 
-template <typename T, int D> cudaError_t forward(const RopeArgs &a, cudaStream_t st)
+int blocks_of(const Split &s, int per_sm)
 {
-    constexpr int RPW = 32 * 16 / (int)sizeof(T) / D;
-    int parts, rpp;
-    split_heads(a.n_tok, a.Hq + (a.slots ? 2 : 1) * a.Hkv, RPW, parts, rpp);
-    const long long blocks = ((long long)a.n_tok * parts + kWarps - 1) / kWarps;
-    return pipe::launch_early(k_qk_norm_rope<T, D>, dim3((unsigned)blocks), dim3(kThreads), 0, st, a, parts, rpp);
+    const long long want = ((long long)s.items + kWarps - 1) / kWarps, held = (long long)per_sm * pipe::sm_count();
+    return (int)(want < held ? want : held);
 }
 
-template <typename T, int D> cudaError_t backward(const RopeArgs &a, cudaStream_t st)
+template <typename T, int D, bool kInter> cudaError_t forward(const RopeArgs &a, cudaStream_t st)
 {
-    constexpr int RPW = 32 * 16 / (int)sizeof(T) / D;
+    const Split s = split_rows(a, 32 * 16 / (int)sizeof(T) / D);
+    return pipe::launch_early(k_qk_norm_rope<T, D, kInter>, dim3(blocks_of(s, 4)), dim3(kThreads), 0, st, a, s);
+}
+
+template <typename T, int D, bool kInter> cudaError_t backward(const RopeArgs &a, cudaStream_t st)
+{
     int blocks = 0;
     if (a.n_tok > 0) {
-        int parts, rpp;
-        split_heads(a.n_tok, a.Hq + a.Hkv, RPW, parts, rpp);
-        const long long want = ((long long)a.n_tok * parts + kWarps - 1) / kWarps;
-        blocks = (int)(want < kMaxBackwardBlocks ? want : kMaxBackwardBlocks);
+        const Split s = split_rows(a, 32 * 16 / (int)sizeof(T) / D);
+        blocks = blocks_of(s, 2);
+        if (blocks > kMaxBackwardBlocks) blocks = kMaxBackwardBlocks;
         const cudaError_t e =
-            pipe::launch_early(k_qk_norm_rope_backward<T, D>, dim3(blocks), dim3(kThreads), 0, st, a, parts, rpp);
+            pipe::launch_early(k_qk_norm_rope_backward<T, D, kInter>, dim3(blocks), dim3(kThreads), 0, st, a, s);
         if (e != cudaSuccess) return e;
     }
     if (!a.dwq && !a.dwk) return cudaSuccess;
     return pipe::launch_early(k_dw_reduce, dim3(2 * D / 32), dim3(kThreads), 0, st, (const float *)a.partial, blocks, D,
                               a.dwq, a.dwk);
+}
+
+template <typename T, int D> cudaError_t either(const RopeArgs &a, bool back, cudaStream_t st)
+{
+    if (back) return a.interleaved ? backward<T, D, true>(a, st) : backward<T, D, false>(a, st);
+    return a.interleaved ? forward<T, D, true>(a, st) : forward<T, D, false>(a, st);
+}
+
+cudaError_t launch(hybrid_dtype dt, const RopeArgs &a, bool back, cudaStream_t st)
+{
+    if (dt == HYBRID_BF16)
+        return a.d == 128 ? either<__nv_bfloat16, 128>(a, back, st) : either<__nv_bfloat16, 64>(a, back, st);
+    return a.d == 128 ? either<float, 128>(a, back, st) : either<float, 64>(a, back, st);
 }
 
 }  // namespace
@@ -426,18 +554,11 @@ size_t qk_norm_rope_partial_bytes(int d, int n_tok)
     return (size_t)kMaxBackwardBlocks * 2 * d * sizeof(float);
 }
 
-cudaError_t launch_qk_norm_rope(hybrid_dtype dt, const RopeArgs &a, cudaStream_t st)
-{
-    if (dt == HYBRID_BF16)
-        return a.d == 128 ? forward<__nv_bfloat16, 128>(a, st) : forward<__nv_bfloat16, 64>(a, st);
-    return a.d == 128 ? forward<float, 128>(a, st) : forward<float, 64>(a, st);
-}
+cudaError_t launch_qk_norm_rope(hybrid_dtype dt, const RopeArgs &a, cudaStream_t st) { return launch(dt, a, false, st); }
 
 cudaError_t launch_qk_norm_rope_backward(hybrid_dtype dt, const RopeArgs &a, cudaStream_t st)
 {
-    if (dt == HYBRID_BF16)
-        return a.d == 128 ? backward<__nv_bfloat16, 128>(a, st) : backward<__nv_bfloat16, 64>(a, st);
-    return a.d == 128 ? backward<float, 128>(a, st) : backward<float, 64>(a, st);
+    return launch(dt, a, true, st);
 }
 
 }  // namespace hyb
