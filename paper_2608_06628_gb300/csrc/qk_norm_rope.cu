@@ -9,8 +9,7 @@
 // Forward and backward read each input once and write each output once; memory
 // bounds them.
 //
-// A warp takes one token and a run of its rows (heads of Q, of K, of V), then
-// another token.  A row lies across D / E lanes, E = 16 bytes of elements each: the
+// A warp takes a run of rows (heads of Q, of K, of V, token by token).  A row lies across D / E lanes, E = 16 bytes of elements each: the
 // first members of E / 2 pairs and their second members, so a pair is always in one
 // lane.  With interleaved pairs these are 16 bytes in a row, with the half layout
 // twice 8 bytes (rot is a multiple of 16, so they are aligned, and a lane's pairs
@@ -179,24 +178,37 @@ __device__ __forceinline__ void rotate(float (&x)[E], const Rotation<E> &r)
 }
 
 // The rows of a token in steps of RPW: kinds 0 (Q), 1 (K) and, with the cache, 2
-// (V), each padded to whole steps.  Part `part` of `parts` takes `run` steps.
+// (V), each padded to whole steps.  The steps of all tokens are shared out evenly:
+// each warp takes a run of them, wherever in a token it begins.
 struct Split {
-    unsigned items;                 // tokens * parts
-    int parts, run, steps;          // steps of a token
-    int steps_q, steps_k;
+    int steps, steps_q, steps_k;    // steps of a token, of its Q and of its K
+    int n_kinds;
+    int warps, run, rem;            // warps with work; the first rem take run + 1 steps
+    bool wide;                      // more than 2^32 steps in all
 };
 
-// A warp's place in its rows.
+// A warp's place in its steps.
 template <int RPW> struct Cursor {
-    unsigned item;
-    int t, kind, left, h;           // token, kind, steps left in the part, first row of the step
+    int t, kind, h;                 // token, kind, first row of the step
+    int left;                       // steps to go
 
-    __device__ bool live(const Split &s) const { return item < s.items; }
-    __device__ void enter(const Split &s)
+    // Start of a warp's run; false if it has none.
+    __device__ bool begin(const Split &s, unsigned warp)
     {
-        t = s.parts == 1 ? (int)item : (int)(item / (unsigned)s.parts);
-        int at = s.parts == 1 ? 0 : (int)(item - (unsigned)t * s.parts) * s.run;
-        left = s.steps - at < s.run ? s.steps - at : s.run;
+        left = 0;
+        if (warp >= (unsigned)s.warps) return false;
+        left = s.run + ((int)warp < s.rem ? 1 : 0);
+        const unsigned extra = warp < (unsigned)s.rem ? warp : (unsigned)s.rem;
+        int at;
+        if (s.wide) {
+            const unsigned long long start = (unsigned long long)s.run * warp + extra;
+            t = (int)(start / (unsigned)s.steps);
+            at = (int)(start - (unsigned long long)t * s.steps);
+        } else {
+            const unsigned start = (unsigned)s.run * warp + extra;
+            t = (int)(start / (unsigned)s.steps);
+            at = (int)(start - (unsigned)t * s.steps);
+        }
         kind = 0;
         if (at >= s.steps_q) {
             at -= s.steps_q;
@@ -207,19 +219,19 @@ template <int RPW> struct Cursor {
             }
         }
         h = at * RPW;
+        return true;
     }
-    // Advance; true if the rows go on in another kind or token.
-    __device__ bool step(const Split &s, int n_heads, unsigned stride)
+    // Advance; true if there is no step left or it is of another kind or token.
+    __device__ bool step(const Split &s, int n_heads)
     {
         h += RPW;
-        if (--left == 0) {
-            item = s.items - item > stride ? item + stride : s.items;
-            if (live(s)) enter(s);
-            return true;
-        }
+        if (--left == 0) return true;
         if (h < n_heads) return false;
-        ++kind;
         h = 0;
+        if (++kind == s.n_kinds) {
+            kind = 0;
+            ++t;
+        }
         return true;
     }
 };
@@ -238,12 +250,11 @@ __global__ __launch_bounds__(kThreads, 4) void k_qk_norm_rope(const RopeArgs a, 
     __shared__ float2 s_angles[kWarps][kMaxPairs];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, sub = lane / L;
     const Pieces<D, E, kInter> piece(a, lane % L);
-    const unsigned stride = gridDim.x * kWarps;
     ptx::griddep_wait();
     ptx::griddep_launch_dependents();
-    Cursor<RPW> at, ahead;
-    at.item = ahead.item = blockIdx.x * kWarps + warp;
-    if (!at.live(split)) return;
+    Cursor<RPW> at;
+    if (!at.begin(split, blockIdx.x * kWarps + warp)) return;
+    Cursor<RPW> ahead = at;
     auto heads = [&](int kind) { return kind == 0 ? a.Hq : a.Hkv; };
 
     // loads, kDepth steps ahead
@@ -256,17 +267,16 @@ __global__ __launch_bounds__(kThreads, 4) void k_qk_norm_rope(const RopeArgs a, 
     };
     int ahead_heads = 0;
     auto issue = [&](int slot) {
-        if (ahead.live(split)) {
+        if (ahead.left > 0) {
             if (ahead.h + sub < ahead_heads) copy_async<E, kInter>(&s_ring[slot][tid], src, piece.first, piece.second);
             src += RPW * D;
-            if (ahead.step(split, ahead_heads, stride) && ahead.live(split)) {
+            if (ahead.step(split, ahead_heads) && ahead.left > 0) {
                 ahead_heads = heads(ahead.kind);
                 source();
             }
         }
         async_commit();
     };
-    ahead.enter(split);
     ahead_heads = heads(ahead.kind);
     source();
 #pragma unroll
@@ -304,7 +314,6 @@ __global__ __launch_bounds__(kThreads, 4) void k_qk_norm_rope(const RopeArgs a, 
                 dst += (((size_t)page * a.Hkv + at.h + sub) * a.page_size + (size_t)(slot_of % a.page_size)) * D;
         }
     };
-    at.enter(split);
     enter();
     for (int slot = 0;; slot = (slot + 1) % kDepth) {
         async_wait<kDepth - 1>();
@@ -327,8 +336,8 @@ __global__ __launch_bounds__(kThreads, 4) void k_qk_norm_rope(const RopeArgs a, 
         issue(slot);
         if (write && at.h + sub < n_heads) store<E, kInter>(dst, piece.first, piece.second, out);
         dst += step;
-        if (at.step(split, n_heads, stride)) {
-            if (!at.live(split)) break;
+        if (at.step(split, n_heads)) {
+            if (at.left == 0) break;
             enter();
         }
     }
@@ -343,12 +352,11 @@ __global__ __launch_bounds__(kThreads, 2) void k_qk_norm_rope_backward(const Rop
     __shared__ float s_dw[kWarps][2][D];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, sub = lane / L;
     const Pieces<D, E, kInter> piece(a, lane % L);
-    const unsigned stride = gridDim.x * kWarps;
     ptx::griddep_wait();
     ptx::griddep_launch_dependents();
-    Cursor<RPW> at, ahead;
-    at.item = ahead.item = blockIdx.x * kWarps + warp;
-    const bool work = at.live(split);
+    Cursor<RPW> at;
+    const bool work = at.begin(split, blockIdx.x * kWarps + warp);
+    Cursor<RPW> ahead = at;
     auto heads = [&](int kind) { return kind == 0 ? a.Hq : a.Hkv; };
     // start of a token's rows of a kind in Q or K (or its gradient)
     auto offset = [&](const Cursor<RPW> &c) {
@@ -364,14 +372,14 @@ __global__ __launch_bounds__(kThreads, 2) void k_qk_norm_rope_backward(const Rop
                  ((size_t)ahead.t * ahead_heads + ahead.h + sub) * D;
     };
     auto issue = [&](int slot) {
-        if (ahead.live(split)) {
+        if (ahead.left > 0) {
             if (ahead.h + sub < ahead_heads) {
                 copy_async<E, kInter>(&s_ring[slot][0][tid], src, piece.first, piece.second);
                 copy_async<E, kInter>(&s_ring[slot][1][tid], src_dy, piece.first, piece.second);
             }
             src += RPW * D;
             src_dy += RPW * D;
-            if (ahead.step(split, ahead_heads, stride) && ahead.live(split)) source();
+            if (ahead.step(split, ahead_heads) && ahead.left > 0) source();
         }
         async_commit();
     };
@@ -381,7 +389,6 @@ __global__ __launch_bounds__(kThreads, 2) void k_qk_norm_rope_backward(const Rop
     for (int i = 0; i < E; ++i) dw[i] = dw_other[i] = 0.f;
     int kind = 0;                           // of `dw`
     if (work) {
-        ahead.enter(split);
         source();
 #pragma unroll
         for (int i = 0; i < kDepth; ++i) issue(i);
@@ -411,7 +418,6 @@ __global__ __launch_bounds__(kThreads, 2) void k_qk_norm_rope_backward(const Rop
                 }
             }
         };
-        at.enter(split);
         enter();
         for (int slot = 0;; slot = (slot + 1) % kDepth) {
             async_wait<kDepth - 1>();
@@ -440,8 +446,8 @@ __global__ __launch_bounds__(kThreads, 2) void k_qk_norm_rope_backward(const Rop
             issue(slot);
             if (live) store<E, kInter>(dst, piece.first, piece.second, Vec<T>::pack(g));
             dst += RPW * D;
-            if (at.step(split, n_heads, stride)) {
-                if (!at.live(split)) break;
+            if (at.step(split, n_heads)) {
+                if (at.left == 0) break;
                 enter();
             }
         }
@@ -489,41 +495,44 @@ __global__ __launch_bounds__(kThreads) void k_dw_reduce(const float *partial, in
     }
 }
 
-// A warp takes all rows of a token when there are enough tokens to fill the GPU,
-// else runs of them short enough that about 16 warps a multiprocessor have one.
-Split split_rows(const RopeArgs &a, int rpw)
+// Shares of the steps: a warp per step while the GPU holds them, per_sm blocks a
+// multiprocessor.  Beyond that, with `waves`, short runs of about 16 to 24 steps
+// (whole tokens where those are short): the blocks at work then keep to a narrow
+// window of memory, which the DRAM serves better than runs that span all of it
+// (20011 tokens of 32 float32 heads: 53 against 62 us; 65536 tokens of 24 bfloat16
+// rows: 142 against 153; runs of 4 steps 62 and 180, for the angles).  Returns the
+// number of blocks.
+int split_rows(const RopeArgs &a, int rpw, int per_sm, bool waves, Split &s)
 {
-    Split s;
     s.steps_q = (a.Hq + rpw - 1) / rpw;
     s.steps_k = (a.Hkv + rpw - 1) / rpw;
-    s.steps = s.steps_q + (a.slots ? 2 : 1) * s.steps_k;
-    long long p = (152 * 16 + a.n_tok - 1) / a.n_tok;
-    if (p > s.steps) p = s.steps;
-    s.run = (int)((s.steps + p - 1) / p);
-    s.parts = (s.steps + s.run - 1) / s.run;
-    s.items = (unsigned)a.n_tok * (unsigned)s.parts;        // parts > 1 only for few tokens
-    return s;
-}
-
-int blocks_of(const Split &s, int per_sm)
-{
-    const long long want = ((long long)s.items + kWarps - 1) / kWarps, held = (long long)per_sm * pipe::sm_count();
-    return (int)(want < held ? want : held);
+    s.n_kinds = a.slots ? 3 : 2;
+    s.steps = s.steps_q + (s.n_kinds - 1) * s.steps_k;
+    const long long total = (long long)a.n_tok * s.steps, held = (long long)per_sm * pipe::sm_count() * kWarps;
+    long long warps = total < held ? total : held;
+    const int run = s.steps >= 16 ? (s.steps < 24 ? s.steps : 24) : (16 + s.steps - 1) / s.steps * s.steps;
+    if (waves && total / run > warps) warps = total / run;
+    s.warps = (int)warps;
+    s.run = (int)(total / warps);
+    s.rem = (int)(total % warps);
+    s.wide = total > 0xffffffffll;
+    return (int)((warps + kWarps - 1) / kWarps);
 }
 
 template <typename T, int D, bool kInter> cudaError_t forward(const RopeArgs &a, cudaStream_t st)
 {
-    const Split s = split_rows(a, 32 * 16 / (int)sizeof(T) / D);
-    return pipe::launch_early(k_qk_norm_rope<T, D, kInter>, dim3(blocks_of(s, 4)), dim3(kThreads), 0, st, a, s);
+    Split s;
+    const int blocks = split_rows(a, 32 * 16 / (int)sizeof(T) / D, 4, true, s);
+    return pipe::launch_early(k_qk_norm_rope<T, D, kInter>, dim3(blocks), dim3(kThreads), 0, st, a, s);
 }
 
 template <typename T, int D, bool kInter> cudaError_t backward(const RopeArgs &a, cudaStream_t st)
 {
     int blocks = 0;
     if (a.n_tok > 0) {
-        const Split s = split_rows(a, 32 * 16 / (int)sizeof(T) / D);
-        blocks = blocks_of(s, 2);
-        if (blocks > kMaxBackwardBlocks) blocks = kMaxBackwardBlocks;
+        Split s;
+        blocks = split_rows(a, 32 * 16 / (int)sizeof(T) / D, 2, false, s);
+        if (blocks > kMaxBackwardBlocks) return cudaErrorInvalidConfiguration;   // a GPU of more than 256 multiprocessors
         const cudaError_t e =
             pipe::launch_early(k_qk_norm_rope_backward<T, D, kInter>, dim3(blocks), dim3(kThreads), 0, st, a, s);
         if (e != cudaSuccess) return e;
