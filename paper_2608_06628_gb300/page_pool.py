@@ -1,0 +1,62 @@
+"""Paged key-value caches of a model's softmax layers, and the tables that all layers share.
+
+The device holds everything: lengths, block table and the ring of free pages are
+int32 tensors that hybrid_page_append and hybrid_page_release read and write (they
+read one copy of lengths and ring and write another; the pool swaps them), so a
+serving loop never waits for the host to count pages.  Rows of the table are the
+requests of the batch; a released row may take a new request at once.
+"""
+from __future__ import annotations
+
+import torch
+
+from . import hybrid as H
+
+
+class PagePool:
+    def __init__(self, cfg: H.hybrid_cfg, n_req: int, n_pages: int, max_len: int, page_size: int = 32, n_layers: int = 1,
+                 device="cuda"):
+        self.cfg, self.n_req, self.n_layers = cfg, n_req, n_layers
+        self.pg = H.make_page_cfg(page_size, n_pages, -(-max_len // page_size))
+        dtype = torch.bfloat16 if cfg.io_dtype == H.HYBRID_BF16 else torch.float32
+        shape = (n_layers, n_pages, cfg.n_kv_heads, page_size, cfg.head_dim)
+        self.k_cache = torch.empty(shape, dtype=dtype, device=device)
+        self.v_cache = torch.empty(shape, dtype=dtype, device=device)
+        self.device = torch.device(device)
+        self.block_table = torch.full((n_req, self.pg.max_pages), -1, dtype=torch.int32, device=device)
+        self.free_pages = torch.arange(n_pages, dtype=torch.int32, device=device)
+        self._lens = [torch.zeros(n_req, dtype=torch.int32, device=device) for _ in range(2)]
+        self._ring = [torch.tensor([0, n_pages], dtype=torch.int32, device=device) for _ in range(2)]
+        self.workspace_bytes = H.hybrid_paged_attn_workspace_bytes(cfg, self.pg, n_req)
+        if self.workspace_bytes == 0:
+            raise ValueError(f"unsupported {cfg} with {self.pg}")
+        self.workspace = torch.empty(self.workspace_bytes, dtype=torch.uint8, device=device)
+
+    @property
+    def lens(self) -> torch.Tensor:
+        """Tokens of each request, int32 [n_req]."""
+        return self._lens[0]
+
+    @property
+    def ring(self) -> torch.Tensor:
+        """{head, count} of the free pages."""
+        return self._ring[0]
+
+    def append(self, n_new: torch.Tensor, n_tok: int, stream=None):
+        """Room for n_new [n_req] (int32, device) more tokens of each request, at most n_tok in all.
+        Returns slots, positions [n_tok] and tok_offsets [n_req + 1] (int32); slots beyond the last
+        token, and of requests that did not fit (see hybrid_check), are -1."""
+        new = lambda n: torch.empty(n, dtype=torch.int32, device=self.device)  # noqa: E731
+        slots, positions, offsets = new(n_tok), new(n_tok), new(self.n_req + 1)
+        H.hybrid_page_append(self.pg, self.n_req, self._lens[0], n_new, self.free_pages, self._ring[0], self.block_table,
+                             slots, positions, n_tok, offsets, self._lens[1], self._ring[1], stream=stream)
+        self._lens.reverse()
+        self._ring.reverse()
+        return slots, positions, offsets
+
+    def release(self, rows: torch.Tensor, stream=None):
+        """Give back the pages of the requests in rows (int32, device, each once); their lengths become 0."""
+        H.hybrid_page_release(self.pg, self.n_req, rows, rows.numel(), self._lens[0], self.block_table, self.free_pages,
+                              self._ring[0], self._ring[1], stream=stream)
+        self._ring.reverse()
+        self._lens[0][rows.long()] = 0

@@ -530,3 +530,75 @@ def test_attention_reports_bad_pages_and_lengths(dt):
         assert H.hybrid_check(check=False) == H.HYBRID_ERR_DEVICE
         assert_parity(o[1:].double().cpu().numpy(), want[1:].cpu().numpy(), dt, "beside a bad length", units="out")
     assert H.hybrid_check(check=False) == H.HYBRID_OK
+
+
+# ------------------------------------------------------------------ together
+
+def test_pool_over_many_blocks():
+    """Requests that grow block by block, finish and give way to others: the pool against the model."""
+    from paper_2608_06628_gb300.page_pool import PagePool
+    rng = random.Random(7)
+    n, P, B = 9, 16, 5
+    pool = PagePool(H.make_cfg(64, 64, 2, 1, B, F32), n, 60, 200, P)
+    model = R.Pool(P, 60, pool.pg.max_pages, range(60), 0, 60, [[-1] * pool.pg.max_pages for _ in range(n)])
+    lens = [0] * n
+    for step in range(40):
+        new = [B if x else rng.choice([0, 0, 1, 30, 90]) for x in lens]
+        room = sum(new) + rng.randint(0, 9)
+        slots, pos, offs = pool.append(i32(new), room)
+        st = H.hybrid_check(check=False)
+        ws, wp, wo, lens, bad = model.append(lens, new, room)
+        assert st == (H.HYBRID_ERR_DEVICE if bad else H.HYBRID_OK)
+        assert (slots.tolist(), pos.tolist(), offs.tolist()) == (ws, wp, wo)
+        rows = [r for r in range(n) if lens[r] > 100 or (lens[r] and rng.random() < 0.1)]
+        if rows:
+            pool.release(i32(rows))
+            H.hybrid_check()
+            model.release(rows, lens)
+            lens = [0 if r in rows else x for r, x in enumerate(lens)]
+        assert pool.lens.tolist() == lens and pool.ring.tolist() == [model.head, model.count]
+        held = sum(-(-x // P) for x in lens)
+        assert held + model.count == 60
+
+
+def test_example_runs_the_operators_together(capsys):
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "hybrid_stack_decode.py")
+    spec = importlib.util.spec_from_file_location("hybrid_stack_decode", path)
+    m = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(m)
+    us, err = m.main(["--requests", "5", "--prompt-max", "300", "--blocks", "2", "--steps", "2"])
+    assert us > 0 and err <= 1e-2
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
+def test_decoding_in_a_graph(dt):
+    """Cache write and attention captured once and replayed on other inputs, one token per request."""
+    n, Hq, Hkv, d, P = 6, 8, 2, 64, 16
+    s = attn_setup(dt, 1, Hq, Hkv, d, P, [40, 1, 129, 500, 16, 33], poison=False)
+    r = rope_setup(n, Hq, Hkv, d, d, dt, seed=2)
+    lens = s["lens"].tolist()
+    slots = i32([int(s["table"][i, (x - 1) // P]) * P + (x - 1) % P for i, x in enumerate(lens)])
+    q, o = torch.empty(n, Hq, d, dtype=dt, device="cuda"), torch.empty(n, 1, Hq, d, dtype=dt, device="cuda")
+    nb = H.hybrid_paged_attn_workspace_bytes(s["cfg"], s["pg"], n)
+    ws = torch.empty(nb, dtype=torch.uint8, device="cuda")
+
+    def step():
+        H.hybrid_qk_norm_rope_cache(r["cfg"], r["rope"], s["pg"], r["q"], r["stride"], r["k"], r["stride"], r["v"],
+                                    r["stride"], n, r["wq"], r["wk"], r["pos"], r["freqs"], slots, q, s["kc"], s["vc"])
+        H.hybrid_paged_attn(s["cfg"], s["pg"], q, s["kc"], s["vc"], s["table"], s["lens"], n, 0, 0, o, ws, nb)
+
+    step()
+    H.hybrid_check()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        step()
+    for seed in (11, 12):
+        for x in ("q", "k", "v"):
+            r[x].copy_(torch.randn(r[x].shape, generator=gen(seed), device="cuda"))
+        g.replay()
+        H.hybrid_check()
+        close_rows(q, want_rope(r, r["q"], r["wq"]), dt, "q")
+        want = R.paged_attention(q[:, None], s["kc"], s["vc"], s["table"], lens, 0, 0)
+        assert_parity(o.double().cpu().numpy(), want.cpu().numpy(), dt, "replay", units="out")
