@@ -3,6 +3,17 @@
 //
 // Per row: running maximum m, sum l and output O over the visible keys, in one
 // pass; scores are kept in units of log2, x = q . k log2(e) / sqrt(d).
+//
+// A block of 8 warps walks its share of the tiles (paged_plan.cuh) in chunks of 64
+// (d = 64) or 32 keys, copied by cp.async one or two chunks ahead, across requests; masked
+// keys are zero-filled, their pages not read.  For the scores a lane has its keys
+// (row pitch d + 4 floats: 16-byte reads of 8 keys do not collide) and a warp every
+// eighth row, so maximum, sum and probabilities of a row stay in one warp's
+// registers; for O a thread has 4 features of every (1024 / d)-th row.  16 rows to a
+// tile where a key head has no more (decoding: bound by memory), else 64, so that
+// each key read from shared memory meets 8 rows (bound by the FMA pipe).
+#include <type_traits>
+
 #include "paged_plan.cuh"
 #include "tc_pipeline.cuh"
 
@@ -10,10 +21,11 @@ namespace hyb {
 namespace {
 
 using namespace paged;
+using ptx::f32x2;
 
 constexpr int kThreads = 256;
-constexpr int kRows = 16;       // rows of a tile
-constexpr int kKeys = 64;       // keys in shared memory at a time
+constexpr int kWarps = kThreads / 32;
+constexpr int kFewRows = 16, kManyRows = 64;    // rows of a tile
 
 __device__ __forceinline__ float4 load4(const float *p) { return *reinterpret_cast<const float4 *>(p); }
 template <typename T> __device__ __forceinline__ void store4(T *p, float4 v);
@@ -22,23 +34,78 @@ template <> __device__ __forceinline__ void store4<__nv_bfloat16>(__nv_bfloat16 
 {
     *reinterpret_cast<uint2 *>(p) = make_uint2(pipe::pack_bf16x2(v.x, v.y), pipe::pack_bf16x2(v.z, v.w));
 }
+// 16 bytes of shared memory as two pairs
+__device__ __forceinline__ void load_pairs(const float *p, f32x2 &a, f32x2 &b)
+{
+    const ulonglong2 v = *reinterpret_cast<const ulonglong2 *>(p);
+    a.v = v.x;
+    b.v = v.y;
+}
 
-template <int D> struct Smem {
-    float q[kRows][D];
-    float k[kKeys][D + 4];      // rows 16 bytes apart modulo 128: a warp's 16-byte reads of 32 keys do not collide
-    float v[kKeys][D];
-    float p[kRows][kKeys];
-    float m[kRows], l[kRows], scale[kRows];
+template <int D, int ROWS> struct Smem {
+    static constexpr int kKeys = D == 64 ? 64 : 32;
+    static constexpr int kStages = ROWS == kFewRows ? 3 : 2;   // chunks in place or on their way
+    float q[ROWS][D];
+    struct {
+        float k[kKeys][D + 4];
+        float v[kKeys][D];
+    } chunk[kStages];
+    float p[ROWS][kKeys];
+    float m[ROWS], l[ROWS], scale[ROWS];
     PlanSmem plan;
 };
 
-// Output columns: thread = 4 columns (tid % (D/4)) of rows tid / (D/4) + i * kRowStep.
-template <int D>
-__global__ __launch_bounds__(kThreads) void k_paged_attn(const PagedArgs a)
+// The chunks of a block's share, those without a visible key left out.
+template <int KEYS> struct Chunks {
+    Walk w;
+    int i, j0;             // tile of the segment, first key
+    bool live;
+
+    __device__ void begin(const PagedArgs &a, const Walk &walk, int M)
+    {
+        w = walk;
+        live = w.next(a, M);
+        if (!live) return;
+        i = w.i0;
+        j0 = key_tile(w.vis, i) * kTile;
+        skip(a, M);
+    }
+    // Advance; true if the chunk is the first of a segment.
+    __device__ bool step(const PagedArgs &a, int M)
+    {
+        j0 += KEYS;
+        return skip(a, M);
+    }
+    __device__ bool skip(const PagedArgs &a, int M)
+    {
+        bool first = false;
+        while (true) {
+            if (j0 < (key_tile(w.vis, i) + 1) * kTile) {
+                if (any_visible(w.vis, j0, KEYS)) return first;
+                j0 += KEYS;
+                continue;
+            }
+            if (++i == w.i1) {
+                first = true;
+                live = w.next(a, M);
+                if (!live) return first;
+                i = w.i0;
+            }
+            j0 = key_tile(w.vis, i) * kTile;
+        }
+    }
+};
+
+template <int D, int ROWS>
+__global__ __launch_bounds__(kThreads) void k_paged_attn(const PagedArgs a, int page_lg)
 {
-    constexpr int kCols = D / 4, kRowStep = kThreads / kCols, kOwn = kRows / kRowStep;
+    using S = Smem<D, ROWS>;
+    constexpr int KEYS = S::kKeys, KL = KEYS / 32, RW = ROWS / kWarps;      // keys of a lane, rows of a warp
+    constexpr int kCols = D / 4, kRowStep = kThreads / kCols;               // O: threads per row, rows at a time
+    constexpr int kOwn = ROWS / kRowStep;                                   // rows of a thread
+    constexpr int kCopies = KEYS * kCols / kThreads;                        // 16-byte copies of K per thread
     extern __shared__ __align__(16) unsigned char raw[];
-    Smem<D> &s = *reinterpret_cast<Smem<D> *>(raw);
+    S &s = *reinterpret_cast<S *>(raw);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int rows = a.Bt * a.Gt;
     const float to_log2 = pipe::kLog2e * rsqrtf((float)D);
@@ -49,145 +116,200 @@ __global__ __launch_bounds__(kThreads) void k_paged_attn(const PagedArgs a)
     Shares sh(0, 1);
     const bool work = find_share<kThreads>(a, s.plan, w, sh);
     const int M = units_per_request(a);
-    while (work && w.next(a, M)) {
-        const Visible vis = w.vis;
-        const int i0 = w.i0, i1 = w.i1;
-        const int req = w.req;
-        const Unit u = unit_of(a, w.m);
-        const int *pages = a.table + (size_t)req * a.max_pages;
-
-        __syncthreads();                                     // the last segment's reads are done
-        for (int x = tid; x < kRows * kCols; x += kThreads) {
-            const int rho = x / kCols, c = x % kCols * 4;
-            size_t at;
-            const bool live = row_at(a, req, u, rho, at);
-            *reinterpret_cast<float4 *>(&s.q[rho][c]) =
-                live ? load4(static_cast<const float *>(a.Q) + at + c) : make_float4(0.f, 0.f, 0.f, 0.f);
-        }
-        if (tid < kRows) {
-            s.m[tid] = -INFINITY;
-            s.l[tid] = 0.f;
-        }
-        float4 o[kOwn];
-#pragma unroll
-        for (int i = 0; i < kOwn; ++i) o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (work) {
         const int col = tid % kCols * 4, row0 = tid / kCols;
-
-        for (int i = i0; i < i1; ++i) {
-            const int tile = key_tile(vis, i);
-#pragma unroll 1
-            for (int half = 0; half < kTile / kKeys; ++half) {
-                const int j0 = tile * kTile + half * kKeys;
-                if (j0 >= vis.len) break;
-                __syncthreads();                             // keys and values free
-                for (int x = tid; x < kKeys * kCols; x += kThreads) {
-                    const int r = x / kCols, c = x % kCols * 4, j = j0 + r;
-                    float4 k = make_float4(0.f, 0.f, 0.f, 0.f), v = k;
-                    if (key_visible(vis, j)) {
-                        int page = pages[j / a.page_size];
+        Chunks<KEYS> at, ahead;
+        at.begin(a, w, M);
+        ahead = at;
+        auto issue = [&](int b) {
+            if (ahead.live) {
+                const int *pages = a.table + (size_t)ahead.w.req * a.max_pages;
+                const int head = unit_of(a, ahead.w.m).head;
+#pragma unroll
+                for (int x = 0; x < kCopies; ++x) {
+                    const int r = row0 + x * kRowStep, j = ahead.j0 + r;
+                    const bool see = key_visible(ahead.w.vis, j);
+                    size_t from = 0;
+                    if (see) {
+                        int page = __ldg(pages + (j >> page_lg));
                         if (page < 0 || page >= a.n_pages) {
                             raise_error(a.err, ERR_BAD_INDEX);
                             page = 0;
                         }
-                        const size_t at =
-                            (((size_t)page * a.Hkv + u.head) * a.page_size + j % a.page_size) * D + c;
-                        k = load4(static_cast<const float *>(a.K) + at);
-                        v = load4(static_cast<const float *>(a.V) + at);
+                        from = ((((size_t)page * a.Hkv + head) << page_lg) + (j & ((1 << page_lg) - 1))) * D + col;
                     }
-                    *reinterpret_cast<float4 *>(&s.k[r][c]) = k;
-                    *reinterpret_cast<float4 *>(&s.v[r][c]) = v;
+                    const int bytes = see ? 16 : 0;          // masked keys are zero-filled
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(
+                                     ptx::smem_u32(&s.chunk[b].k[r][col])),
+                                 "l"(static_cast<const float *>(a.K) + from), "r"(bytes)
+                                 : "memory");
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(
+                                     ptx::smem_u32(&s.chunk[b].v[r][col])),
+                                 "l"(static_cast<const float *>(a.V) + from), "r"(bytes)
+                                 : "memory");
                 }
-                __syncthreads();
-                {   // scores: thread = one key, four rows
-                    const int r = tid % kKeys, g = tid / kKeys * 4;
-                    float acc[4] = {0.f, 0.f, 0.f, 0.f};
-                    if (g < rows) {
-#pragma unroll 8
-                        for (int c = 0; c < D; c += 4) {
-                            const float4 k = *reinterpret_cast<const float4 *>(&s.k[r][c]);
+                ahead.step(a, M);
+            }
+            asm volatile("cp.async.commit_group;" ::: "memory");
+        };
+        constexpr int kAhead = S::kStages - 1;
 #pragma unroll
-                            for (int y = 0; y < 4; ++y) {
-                                const float4 q = *reinterpret_cast<const float4 *>(&s.q[g + y][c]);
-                                acc[y] = fmaf(k.x, q.x, acc[y]);
-                                acc[y] = fmaf(k.y, q.y, acc[y]);
-                                acc[y] = fmaf(k.z, q.z, acc[y]);
-                                acc[y] = fmaf(k.w, q.w, acc[y]);
+        for (int x = 0; x < kAhead; ++x) issue(x);
+        bool first = true;
+        float m[RW], l[RW];                                  // of rows warp + 8 y
+        float4 o[kOwn];                                      // features col ... of rows row0 + y kRowStep
+        Unit u{};
+        for (int b = 0; at.live; b = b + 1 == S::kStages ? 0 : b + 1) {
+            const int req = at.w.req;
+            issue(b == 0 ? kAhead : b - 1);
+            if (first) {
+                u = unit_of(a, at.w.m);
+                for (int x = tid; x < rows * kCols; x += kThreads) {
+                    const int rho = x / kCols, c = x % kCols * 4;
+                    size_t from;
+                    const bool live = row_at(a, req, u, rho, from);
+                    *reinterpret_cast<float4 *>(&s.q[rho][c]) =
+                        live ? load4(static_cast<const float *>(a.Q) + from + c) : make_float4(0.f, 0.f, 0.f, 0.f);
+                }
+#pragma unroll
+                for (int y = 0; y < RW; ++y) {
+                    m[y] = -INFINITY;
+                    l[y] = 0.f;
+                }
+#pragma unroll
+                for (int y = 0; y < kOwn; ++y) o[y] = make_float4(0.f, 0.f, 0.f, 0.f);
+            }
+            asm volatile("cp.async.wait_group %0;" ::"n"(kAhead) : "memory");
+            __syncthreads();
+            {   // scores of keys lane, lane + 32 with rows warp, warp + 8, ...
+                f32x2 acc[KL][RW];
+#pragma unroll
+                for (int x = 0; x < KL; ++x)
+#pragma unroll
+                    for (int y = 0; y < RW; ++y) acc[x][y] = ptx::pair2(0.f, 0.f);
+                auto products = [&](auto full) {
+#pragma unroll 4
+                    for (int c = 0; c < D; c += 4) {
+                        f32x2 k0[KL], k1[KL];
+#pragma unroll
+                        for (int x = 0; x < KL; ++x) load_pairs(&s.chunk[b].k[lane + 32 * x][c], k0[x], k1[x]);
+#pragma unroll
+                        for (int y = 0; y < RW; ++y) {
+                            if (!full && warp + 8 * y >= rows) break;
+                            f32x2 q0, q1;
+                            load_pairs(&s.q[warp + 8 * y][c], q0, q1);
+#pragma unroll
+                            for (int x = 0; x < KL; ++x)
+                                acc[x][y] = ptx::fma2(k1[x], q1, ptx::fma2(k0[x], q0, acc[x][y]));
+                        }
+                    }
+                };
+                // (a full tile without the checks of each row)
+                if (rows == ROWS) products(std::true_type{});
+                else if (warp < rows) products(std::false_type{});
+                bool see[KL];
+#pragma unroll
+                for (int x = 0; x < KL; ++x) see[x] = key_visible(at.w.vis, at.j0 + lane + 32 * x);
+#pragma unroll
+                for (int y = 0; y < RW; ++y) {
+                    const int rho = warp + 8 * y;
+                    if (rho >= rows) break;
+                    float x[KL], mx = -INFINITY, sum = 0.f;
+#pragma unroll
+                    for (int k = 0; k < KL; ++k) {
+                        float lo, hi;
+                        ptx::unpair2(acc[k][y], lo, hi);
+                        x[k] = see[k] ? (lo + hi) * to_log2 : -INFINITY;
+                        mx = fmaxf(mx, x[k]);
+                    }
+                    const float now = fmaxf(m[y], warp_max(mx)), base = now == -INFINITY ? 0.f : now;
+#pragma unroll
+                    for (int k = 0; k < KL; ++k) {
+                        const float p = exp2f(x[k] - base);
+                        s.p[rho][lane + 32 * k] = p;
+                        sum += p;
+                    }
+                    const float f = exp2f(m[y] - base);
+                    l[y] = l[y] * f + warp_sum(sum);
+                    m[y] = now;
+                    if (lane == 0) {
+                        s.scale[rho] = f;
+                        s.m[rho] = now;
+                        s.l[rho] = l[y];
+                    }
+                }
+            }
+            __syncthreads();
+            {   // O <- O scale + P V
+                f32x2 acc[kOwn][2];
+#pragma unroll
+                for (int y = 0; y < kOwn; ++y) {
+                    const int rho = row0 + y * kRowStep;
+                    const float f = rho < rows ? s.scale[rho] : 0.f;
+                    acc[y][0] = ptx::pair2(o[y].x * f, o[y].y * f);
+                    acc[y][1] = ptx::pair2(o[y].z * f, o[y].w * f);
+                }
+                auto products = [&](auto full) {
+#pragma unroll 2
+                    for (int r = 0; r < KEYS; r += 4) {
+                        f32x2 v[4][2];
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) load_pairs(&s.chunk[b].v[r + k][col], v[k][0], v[k][1]);
+#pragma unroll
+                        for (int y = 0; y < kOwn; ++y) {
+                            const int rho = row0 + y * kRowStep;
+                            if (!full && y > 0 && rho >= rows) break;
+                            const float4 p4 = load4(&s.p[rho][r]);
+                            const float p[4] = {p4.x, p4.y, p4.z, p4.w};
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) {
+                                const f32x2 pp = ptx::pair2(p[k], p[k]);
+                                acc[y][0] = ptx::fma2(pp, v[k][0], acc[y][0]);
+                                acc[y][1] = ptx::fma2(pp, v[k][1], acc[y][1]);
                             }
                         }
                     }
-                    const bool see = key_visible(vis, j0 + r);
+                };
+                if (rows == ROWS) products(std::true_type{});
+                else if (row0 < rows) products(std::false_type{});
 #pragma unroll
-                    for (int y = 0; y < 4; ++y) s.p[g + y][r] = see ? acc[y] * to_log2 : -INFINITY;
+                for (int y = 0; y < kOwn; ++y) {
+                    ptx::unpair2(acc[y][0], o[y].x, o[y].y);
+                    ptx::unpair2(acc[y][1], o[y].z, o[y].w);
                 }
-                __syncthreads();
-                // softmax: warp = two rows
-                for (int rho = warp * 2; rho < warp * 2 + 2; ++rho) {
-                    const float x0 = s.p[rho][lane], x1 = s.p[rho][lane + 32];
-                    const float old = s.m[rho], now = fmaxf(old, warp_max(fmaxf(x0, x1)));
-                    const float base = now == -INFINITY ? 0.f : now;
-                    const float p0 = exp2f(x0 - base), p1 = exp2f(x1 - base);
-                    const float sum = warp_sum(p0 + p1), f = exp2f(old - base);
-                    s.p[rho][lane] = p0;
-                    s.p[rho][lane + 32] = p1;
-                    __syncwarp();
-                    if (lane == 0) {
-                        s.m[rho] = now;
-                        s.l[rho] = s.l[rho] * f + sum;
-                        s.scale[rho] = f;
-                    }
-                }
-                __syncthreads();
+            }
+            const Walk here = at.w;
+            first = at.step(a, M);
+            if (first) {                                     // the segment's output
+                const bool whole = here.whole();
+                float *part = a.part + here.slot() * partial_floats(rows, D);
 #pragma unroll
                 for (int y = 0; y < kOwn; ++y) {
                     const int rho = row0 + y * kRowStep;
                     if (rho >= rows) break;
-                    const float f = s.scale[rho];
-                    float4 c = o[y];
-                    c.x *= f;
-                    c.y *= f;
-                    c.z *= f;
-                    c.w *= f;
-#pragma unroll 8
-                    for (int r = 0; r < kKeys; ++r) {
-                        const float4 v = *reinterpret_cast<const float4 *>(&s.v[r][col]);
-                        const float p = s.p[rho][r];
-                        c.x = fmaf(p, v.x, c.x);
-                        c.y = fmaf(p, v.y, c.y);
-                        c.z = fmaf(p, v.z, c.z);
-                        c.w = fmaf(p, v.w, c.w);
+                    size_t to;
+                    const bool live = row_at(a, req, u, rho, to);
+                    const float4 c = o[y];
+                    if (whole) {
+                        const float f = 1.f / s.l[rho];
+                        if (live)
+                            store4(static_cast<float *>(a.O) + to + col, make_float4(c.x * f, c.y * f, c.z * f, c.w * f));
+                    } else {
+                        float *out = part + 2 * rows + (size_t)col * rows + rho;
+                        out[0] = c.x;
+                        out[rows] = c.y;
+                        out[2 * rows] = c.z;
+                        out[3 * rows] = c.w;
+                        if (col == 0) {
+                            part[rho] = s.m[rho];
+                            part[rows + rho] = s.l[rho];
+                        }
                     }
-                    o[y] = c;
                 }
             }
+            __syncthreads();                                 // the chunk, Q and P may be overwritten
         }
-        const bool whole = w.whole();
-        float *part = a.part + w.slot() * partial_floats(rows, D);
-#pragma unroll
-        for (int y = 0; y < kOwn; ++y) {
-            const int rho = row0 + y * kRowStep;
-            if (rho >= rows) break;
-            size_t at;
-            const bool live = row_at(a, req, u, rho, at);
-            float4 c = o[y];
-            if (whole) {
-                const float f = 1.f / s.l[rho];
-                c.x *= f;
-                c.y *= f;
-                c.z *= f;
-                c.w *= f;
-                if (live) store4(static_cast<float *>(a.O) + at + col, c);
-            } else {
-                float *out = part + 2 * rows + (size_t)col * rows + rho;
-                out[0] = c.x;
-                out[rows] = c.y;
-                out[2 * rows] = c.z;
-                out[3 * rows] = c.w;
-                if (col == 0) {
-                    part[rho] = s.m[rho];
-                    part[rows + rho] = s.l[rho];
-                }
-            }
-        }
+        w = at.w;
     }
     if (tid == 0) write_note(a, work, w, sh);
     write_empty<float, kThreads>(a, tid);
@@ -237,7 +359,7 @@ __global__ __launch_bounds__(kThreads) void k_paged_join(const PagedArgs a)
 #pragma unroll
     for (int k = 0; k < kIter; ++k) o[k] = 0.f;
     if (g < groups) {
-#pragma unroll 2
+#pragma unroll 4
         for (int i = g; i < n; i += groups) {
             const float *p = part_of(i);
             const float mi = p[rho], li = p[rows + rho];
@@ -290,23 +412,31 @@ __global__ __launch_bounds__(kThreads) void k_paged_join(const PagedArgs a)
 // The join of a call whose attention kernel was launched just before.
 template <typename T> cudaError_t launch_join(const PagedArgs &a, cudaStream_t st)
 {
-    // many partials of few rows: more blocks of fewer features, with little shared
-    // memory, so that they are in place before the attention kernel ends
+    // few rows: little shared memory, so that the blocks are in place before the
+    // attention kernel ends
     const int rows = a.Bt * a.Gt;
     if (rows <= 16)
         return pipe::launch_early(k_paged_join<T, 16, 16>, dim3(a.n_cta, a.d / 16), dim3(kThreads), 0, st, a);
-    return pipe::launch_early(k_paged_join<T, 32, kMaxRows>, dim3(a.n_cta, a.d / 32), dim3(kThreads), 0, st, a);
+    return pipe::launch_early(k_paged_join<T, 16, kMaxRows>, dim3(a.n_cta, a.d / 16), dim3(kThreads), 0, st, a);
+}
+
+template <int D, int ROWS> cudaError_t launch_f32(const PagedArgs &a, cudaStream_t st)
+{
+    using S = Smem<D, ROWS>;
+    static_assert(sizeof(S) < 113 * 1024, "two blocks per multiprocessor");
+    int lg = 4;
+    while ((1 << lg) < a.page_size) ++lg;
+    cudaError_t e =
+        cudaFuncSetAttribute(k_paged_attn<D, ROWS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(S));
+    if (e != cudaSuccess) return e;
+    e = pipe::launch_early(k_paged_attn<D, ROWS>, dim3(a.n_cta), dim3(kThreads), sizeof(S), st, a, lg);
+    if (e != cudaSuccess) return e;
+    return launch_join<float>(a, st);
 }
 
 template <int D> cudaError_t launch_f32(const PagedArgs &a, cudaStream_t st)
 {
-    static_assert(sizeof(Smem<D>) < 100 * 1024, "two blocks per multiprocessor");
-    cudaError_t e =
-        cudaFuncSetAttribute(k_paged_attn<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Smem<D>));
-    if (e != cudaSuccess) return e;
-    e = pipe::launch_early(k_paged_attn<D>, dim3(a.n_cta), dim3(kThreads), sizeof(Smem<D>), st, a);
-    if (e != cudaSuccess) return e;
-    return launch_join<float>(a, st);
+    return a.Bt * a.Gt <= kFewRows ? launch_f32<D, kFewRows>(a, st) : launch_f32<D, kManyRows>(a, st);
 }
 
 }  // namespace
@@ -314,7 +444,8 @@ template <int D> cudaError_t launch_f32(const PagedArgs &a, cudaStream_t st)
 void paged_geometry(const hybrid_cfg &c, PagedArgs &a)
 {
     const bool tc = c.io_dtype == HYBRID_BF16;
-    const int max_rows = tc ? kMaxRows : kRows;
+    const int group = c.n_q_heads / c.n_kv_heads * c.block_size;            // rows of a key head
+    const int max_rows = tc ? kMaxRows : (group <= kFewRows ? kFewRows : kManyRows);
     a.B = c.block_size;
     a.Hq = c.n_q_heads;
     a.Hkv = c.n_kv_heads;

@@ -88,11 +88,6 @@ struct RingPos {
     }
 };
 
-// Whether the n keys from j hold a visible one.
-__device__ __forceinline__ bool any_visible(const Visible &v, int j, int n)
-{
-    return (j < v.len && j + n > v.lo) || j < v.sink;
-}
 __device__ __forceinline__ bool all_visible(const Visible &v, int j)
 {
     return (j >= v.lo && j + kTile <= v.len) || j + kTile <= v.sink;

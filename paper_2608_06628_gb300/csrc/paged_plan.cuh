@@ -57,6 +57,12 @@ __device__ __forceinline__ bool length_ok(const PagedArgs &a, int len)
 __device__ __forceinline__ int key_tile(const Visible &v, int i) { return i < v.ns ? i : v.first + (i - v.ns); }
 __device__ __forceinline__ bool key_visible(const Visible &v, int j) { return j < v.len && (j >= v.lo || j < v.sink); }
 
+// Whether the n keys from j hold a visible one.
+__device__ __forceinline__ bool any_visible(const Visible &v, int j, int n)
+{
+    return (j < v.len && j + n > v.lo) || j < v.sink;
+}
+
 __device__ __forceinline__ int units_per_request(const PagedArgs &a) { return a.Hkv * a.n_gt * a.n_bt; }
 
 // Shares of T tiles over C blocks (C <= T): the first T % C blocks take one more.
