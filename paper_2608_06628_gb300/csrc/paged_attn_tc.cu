@@ -164,14 +164,15 @@ __global__ void __launch_bounds__(Roles<kCopies>::kThreads, 1) k_paged_attn_tc(c
         *fail = 0;
         fence_mbar_init();
     }
+    tc_fence_before();
+    __syncthreads();                                       // barriers and Tensor Memory are in place
+    tc_fence_after();
     // what comes before in the stream is complete from here on
     griddep_wait();
     griddep_launch_dependents();
-    tc_fence_before();
     Walk w;
     Shares sh(0, 1);
-    const bool work = find_share<kThreads>(a, *plan_smem, w, sh);   // synchronises the block
-    tc_fence_after();
+    const bool work = find_share<kThreads>(a, *plan_smem, w, sh);
     const uint32_t tmem = *tmem_holder;
     const int M = units_per_request(a);
 

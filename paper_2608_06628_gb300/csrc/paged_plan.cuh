@@ -129,12 +129,62 @@ struct Walk {
     __device__ int slot() const { return 2 * (int)blockIdx.x + (at_start ? 0 : 1); }
 };
 
+// The same by each warp for itself, for few requests (kPerLane a lane): no barrier
+// and no shared memory between the lengths and the first use of the share.
+constexpr int kPerLane = 4, kFewRequests = 32 * kPerLane;
+__device__ __forceinline__ bool find_share_warp(const PagedArgs &a, Walk &w, Shares &sh)
+{
+    const int lane = threadIdx.x & 31, M = units_per_request(a);
+    int len[kPerLane], n[kPerLane], sum = 0;
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < kPerLane; ++i) {
+        const int r = lane * kPerLane + i;
+        len[i] = r < a.n_req ? __ldg(a.lens + r) : 0;
+        bad |= !length_ok(a, len[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < kPerLane; ++i) {
+        n[i] = visible_keys(a, len[i]).tiles;
+        sum += n[i];
+    }
+    if (bad) raise_error(a.err, ERR_BAD_INDEX);
+    int inc = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int v = __shfl_up_sync(0xffffffffu, inc, o);
+        if (lane >= o) inc += v;
+    }
+    sh = Shares(__shfl_sync(0xffffffffu, inc, 31) * M, a.n_cta);
+    if ((int)blockIdx.x >= sh.C) return false;
+    const int t0 = sh.start(blockIdx.x);
+    int b = inc - sum, req = lane * kPerLane, length = len[0];
+    const unsigned holder = __ballot_sync(0xffffffffu, t0 >= b * M && t0 < inc * M);
+#pragma unroll
+    for (int i = 0; i + 1 < kPerLane; ++i)
+        if (t0 >= (b + n[i]) * M && req == lane * kPerLane + i) {
+            b += n[i];
+            ++req;
+            length = len[i + 1];
+        }
+    const int from = __ffs(holder) - 1;
+    w.t = t0;
+    w.t1 = sh.start(blockIdx.x + 1);
+    w.req = __shfl_sync(0xffffffffu, req, from);
+    w.before = __shfl_sync(0xffffffffu, b, from);
+    w.vis = visible_keys(a, __shfl_sync(0xffffffffu, length, from));
+    w.at_start = true;
+    w.i1 = -1;
+    return true;
+}
+
 // Find the block's share by a scan over the requests, NT threads (a multiple of
-// 32), each with a run of them; false if the block has none.  Synchronises the
+// 32), each with a run of them; false if the block has none.  May synchronise the
 // block (also where it returns false).
 template <int NT>
 __device__ __forceinline__ bool find_share(const PagedArgs &a, PlanSmem &s, Walk &w, Shares &sh)
 {
+    if (a.n_req <= kFewRequests) return find_share_warp(a, w, sh);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int M = units_per_request(a), per = (a.n_req + NT - 1) / NT;
     const int q0 = tid * per < a.n_req ? tid * per : a.n_req, q1 = q0 + per < a.n_req ? q0 + per : a.n_req;
