@@ -61,22 +61,22 @@ template <int KEYS> struct Chunks {
     int i, j0;             // tile of the segment, first key
     bool live;
 
-    __device__ void begin(const PagedArgs &a, const Walk &walk, int M)
+    __device__ void begin(const PagedArgs &a, const Walk &walk)
     {
         w = walk;
-        live = w.next(a, M);
+        live = w.next(a);
         if (!live) return;
         i = w.i0;
         j0 = key_tile(w.vis, i) * kTile;
-        skip(a, M);
+        skip(a);
     }
     // Advance; true if the chunk is the first of a segment.
-    __device__ bool step(const PagedArgs &a, int M)
+    __device__ bool step(const PagedArgs &a)
     {
         j0 += KEYS;
-        return skip(a, M);
+        return skip(a);
     }
-    __device__ bool skip(const PagedArgs &a, int M)
+    __device__ bool skip(const PagedArgs &a)
     {
         bool first = false;
         while (true) {
@@ -87,7 +87,7 @@ template <int KEYS> struct Chunks {
             }
             if (++i == w.i1) {
                 first = true;
-                live = w.next(a, M);
+                live = w.next(a);
                 if (!live) return first;
                 i = w.i0;
             }
@@ -115,16 +115,15 @@ __global__ __launch_bounds__(kThreads) void k_paged_attn(const PagedArgs a, int 
     Walk w;
     Shares sh(0, 1);
     const bool work = find_share<kThreads>(a, s.plan, w, sh);
-    const int M = units_per_request(a);
     if (work) {
         const int col = tid % kCols * 4, row0 = tid / kCols;
         Chunks<KEYS> at, ahead;
-        at.begin(a, w, M);
+        at.begin(a, w);
         ahead = at;
         auto issue = [&](int b) {
             if (ahead.live) {
                 const int *pages = a.table + (size_t)ahead.w.req * a.max_pages;
-                const int head = unit_of(a, ahead.w.m).head;
+                const int head = ahead.w.head;
 #pragma unroll
                 for (int x = 0; x < kCopies; ++x) {
                     const int r = row0 + x * kRowStep, j = ahead.j0 + r;
@@ -148,7 +147,7 @@ __global__ __launch_bounds__(kThreads) void k_paged_attn(const PagedArgs a, int 
                                  "l"(static_cast<const float *>(a.V) + from), "r"(bytes)
                                  : "memory");
                 }
-                ahead.step(a, M);
+                ahead.step(a);
             }
             asm volatile("cp.async.commit_group;" ::: "memory");
         };
@@ -163,7 +162,7 @@ __global__ __launch_bounds__(kThreads) void k_paged_attn(const PagedArgs a, int 
             const int req = at.w.req;
             issue(b == 0 ? kAhead : b - 1);
             if (first) {
-                u = unit_of(a, at.w.m);
+                u = unit_of(a, at.w.head, at.w.rt);
                 for (int x = tid; x < rows * kCols; x += kThreads) {
                     const int rho = x / kCols, c = x % kCols * 4;
                     size_t from;
@@ -279,7 +278,7 @@ __global__ __launch_bounds__(kThreads) void k_paged_attn(const PagedArgs a, int 
                 }
             }
             const Walk here = at.w;
-            first = at.step(a, M);
+            first = at.step(a);
             if (first) {                                     // the segment's output
                 const bool whole = here.whole();
                 float *part = a.part + here.slot() * partial_floats(rows, D);
@@ -359,20 +358,29 @@ __global__ __launch_bounds__(kThreads) void k_paged_join(const PagedArgs a)
 #pragma unroll
     for (int k = 0; k < kIter; ++k) o[k] = 0.f;
     if (g < groups) {
-#pragma unroll 4
-        for (int i = g; i < n; i += groups) {
-            const float *p = part_of(i);
-            const float mi = p[rho], li = p[rows + rho];
-            float v[kIter];
+        constexpr int kLoad = 4;                             // partials loaded at a time
+        for (int i0 = g; i0 < n; i0 += kLoad * groups) {
+            float mi[kLoad], li[kLoad], v[kLoad][kIter];
 #pragma unroll
-            for (int k = 0; k < kIter; ++k) {
-                const int col = first + k * step;
-                v[k] = col < COLS ? p[2 * rows + (size_t)(col0 + col) * rows + rho] : 0.f;
+            for (int x = 0; x < kLoad; ++x) {
+                const int i = i0 + x * groups;
+                const float *p = part_of(i < n ? i : i0);
+                mi[x] = i < n ? p[rho] : -INFINITY;
+                li[x] = p[rows + rho];
+#pragma unroll
+                for (int k = 0; k < kIter; ++k) {
+                    const int col = first + k * step;
+                    v[x][k] = i < n && col < COLS ? p[2 * rows + (size_t)(col0 + col) * rows + rho] : 0.f;
+                }
             }
-            const Merge w(m, mi);
-            l = l * w.keep + li * w.add;
 #pragma unroll
-            for (int k = 0; k < kIter; ++k) o[k] = o[k] * w.keep + v[k] * w.add;
+            for (int x = 0; x < kLoad; ++x) {
+                if (i0 + x * groups >= n) break;
+                const Merge w(m, mi[x]);
+                l = l * w.keep + li[x] * w.add;
+#pragma unroll
+                for (int k = 0; k < kIter; ++k) o[k] = o[k] * w.keep + v[x][k] * w.add;
+            }
         }
     }
     if (groups > 1) {                                        // one feature a thread
@@ -399,7 +407,7 @@ __global__ __launch_bounds__(kThreads) void k_paged_join(const PagedArgs a)
         }
     }
     __syncthreads();
-    const Unit u = unit_of(a, note.m);
+    const Unit u = unit_of(a, note.head, note.rt);
     for (int x = tid; x < rows * (COLS / 4); x += kThreads) {
         const int r = x / (COLS / 4), col = x % (COLS / 4) * 4;
         size_t at;
@@ -455,6 +463,7 @@ void paged_geometry(const hybrid_cfg &c, PagedArgs &a)
     a.n_gt = (a.G + a.Gt - 1) / a.Gt;
     a.Bt = max_rows / a.Gt < a.B ? max_rows / a.Gt : a.B;
     a.n_bt = (a.B + a.Bt - 1) / a.Bt;
+    a.Bt = (a.B + a.n_bt - 1) / a.n_bt;                                     // row tiles of about equal size
     a.n_cta = (tc ? 1 : 2) * pipe::sm_count();
 }
 

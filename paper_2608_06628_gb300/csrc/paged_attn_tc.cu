@@ -174,7 +174,6 @@ __global__ void __launch_bounds__(Roles<kCopies>::kThreads, 1) k_paged_attn_tc(c
     Shares sh(0, 1);
     const bool work = find_share<kThreads>(a, *plan_smem, w, sh);
     const uint32_t tmem = *tmem_holder;
-    const int M = units_per_request(a);
 
     if (warp == W::kLoadK || warp == W::kLoadV) {
         // ------------------------------------------------------ producers of K and V
@@ -185,11 +184,14 @@ __global__ void __launch_bounds__(Roles<kCopies>::kThreads, 1) k_paged_attn_tc(c
             const CUtensorMap *map = is_v ? &ta.tmV : &ta.tmK;
             uint64_t *my_full = is_v ? full + NK : full, *my_empty = is_v ? empty + NK : empty;
             uint8_t *my_ring = is_v ? ring + (size_t)NK * kSlot : ring;
+            // a cache that is read once need not push tables, lengths and partials out of L2
+            const bool once = row_tiles(a) == 1;
+            const uint64_t policy = policy_evict_first();
             uint32_t n = 0;                                // tiles issued
             RingPos pos{0, 1};                             // phase of `empty`: the first round is free
             bool ok = true;
-            while (ok && w.next(a, M)) {
-                const int head = unit_of(a, w.m).head;
+            while (ok && w.next(a)) {
+                const int head = w.head;
                 const int *pages = a.table + (size_t)w.req * a.max_pages;
                 auto page_at = [&](int i) -> int {         // this lane's page of tile i, -1: nothing visible in it
                     if (i >= w.i1 || lane >= per) return -1;
@@ -216,7 +218,8 @@ __global__ void __launch_bounds__(Roles<kCopies>::kThreads, 1) k_paged_attn_tc(c
                         uint8_t *dst = my_ring + (size_t)pos.slot * kSlot + lane * P * 128;
 #pragma unroll
                         for (int h = 0; h < kHalves; ++h)
-                            tma_load_4d(dst + h * kPanel, map, 64 * h, 0, head, page, &my_full[pos.slot]);
+                            if (once) tma_load_4d_policy(dst + h * kPanel, map, 64 * h, 0, head, page, &my_full[pos.slot], policy);
+                            else tma_load_4d(dst + h * kPanel, map, 64 * h, 0, head, page, &my_full[pos.slot]);
                     }
                     pos.step(n_slots);
                     ++n;
@@ -243,8 +246,8 @@ __global__ void __launch_bounds__(Roles<kCopies>::kThreads, 1) k_paged_attn_tc(c
             uint32_t n = 0, seg = 0;                       // tiles and segments so far
             RingPos pos{0, 0};
             bool ok = true;
-            while (ok && w.next(a, M)) {
-                const Unit u = unit_of(a, w.m);
+            while (ok && w.next(a)) {
+                const Unit u = unit_of(a, w.head, w.rt);
                 if (seg > 0 && !wait_soon(qempty, (seg - 1) & 1u, fail)) break;
                 mbar_arrive_expect_tx(qfull, (uint32_t)(kCopies * rows * D * 2));
 #pragma unroll
@@ -281,7 +284,7 @@ __global__ void __launch_bounds__(Roles<kCopies>::kThreads, 1) k_paged_attn_tc(c
             uint32_t n = 0, seg = 0;
             RingPos pos{0, 0};
             bool ok = true;
-            while (ok && w.next(a, M)) {
+            while (ok && w.next(a)) {
                 // O is overwritten by a segment's first product: the last epilogue has read it
                 if (seg > 0) ok = wait_soon(ofree, (seg - 1) & 1u, fail);
                 for (int i = w.i0; ok && i < w.i1; ++i, ++n) {
@@ -345,7 +348,7 @@ __global__ void __launch_bounds__(Roles<kCopies>::kThreads, 1) k_paged_attn_tc(c
             for (int x = 0; x < 4; ++x) tmem_st32(tmem + cP + 32 * x + lane_off, zero);
             tmem_wait_st();
         }
-        while (w.next(a, M)) {              // left by a vote only, so that the warps of a row stay together
+        while (w.next(a)) {              // left by a vote only, so that the warps of a row stay together
             float ref = -INFINITY, l2[2] = {0.f, 0.f};     // the row's sum over this thread's keys, in two
             bool left = false;
             for (int i = w.i0; i < w.i1; ++i, ++n) {
@@ -451,7 +454,7 @@ __global__ void __launch_bounds__(Roles<kCopies>::kThreads, 1) k_paged_attn_tc(c
             }
             if (left) break;
             // the segment's output
-            const Unit u = unit_of(a, w.m);
+            const Unit u = unit_of(a, w.head, w.rt);
             size_t at;
             const bool live = row_at(a, w.req, u, row, at), whole = w.whole();
             bf16 *out = static_cast<bf16 *>(a.O) + at;

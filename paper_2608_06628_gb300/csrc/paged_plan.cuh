@@ -1,13 +1,15 @@
 // paged_plan.cuh -- how one paged-attention call is cut over the GPU, and the
 // format of the partial results.
 //
-// A unit is (request, key head, row tile): M = Hkv * n_gt * n_bt units a request,
-// all with the same visible keys.  The visible keys of a request are cut into
-// tiles of kTile keys; the tiles of all units, in the order (request, unit of the
-// request, tile), are shared out evenly: of C blocks, block c takes the tiles
+// A unit is (row tile, request, key head): n_gt * n_bt row tiles, all units of a
+// request with the same visible keys.  The visible keys of a request are cut into
+// tiles of kTile keys; the tiles of all units, in the order (row tile, request, key
+// head, tile), are shared out evenly: of C blocks, block c takes the tiles
 // [c T / C, (c + 1) T / C).  So every block reads the same amount of cache
 // whatever the lengths are, and a long request is split over as many blocks as
-// it is worth.  The lengths are on the device, so each block finds its share
+// it is worth.  Where there are several row tiles, the blocks of one are at the
+// same keys as the blocks of another at any time, and all but the first find them
+// in L2.  The lengths are on the device, so each block finds its share
 // itself by a scan over the requests (a few KB).
 //
 // A run of tiles of one unit is a segment.  A segment that covers its unit writes
@@ -63,7 +65,7 @@ __device__ __forceinline__ bool any_visible(const Visible &v, int j, int n)
     return (j < v.len && j + n > v.lo) || j < v.sink;
 }
 
-__device__ __forceinline__ int units_per_request(const PagedArgs &a) { return a.Hkv * a.n_gt * a.n_bt; }
+__device__ __forceinline__ int row_tiles(const PagedArgs &a) { return a.n_gt * a.n_bt; }
 
 // Shares of T tiles over C blocks (C <= T): the first T % C blocks take one more.
 // T < 2^31 (the host's check).
@@ -88,10 +90,10 @@ struct Shares {
 // when its last segment is the first part of a unit that later blocks go on with.
 struct JoinNote {
     int cut;               // 0: nothing to join
-    int req, m;            // the unit
+    int req, head, rt;     // the unit
     int last;              // block of its last tile; blocks c + 1 ... last hold partial 2 b
     int slot;              // block c's partial
-    int pad[3];
+    int pad[2];
 };
 
 // Scratch of the search for a block's share.
@@ -103,24 +105,28 @@ struct PlanSmem {
 // The segments of a block's share, one after another.
 struct Walk {
     int t, t1;             // next tile, end of the share
-    int before;            // tiles per unit of the requests before `req`
-    int req;
+    int base;              // tiles of the row tiles before, and of the requests before `req`
+    int req, rt;           // request and row tile
     Visible vis;
-    // the current segment: tiles [i0, i1) of unit m of request req
-    int m, i0, i1;
+    // the current segment: tiles [i0, i1) of key head `head` of request `req`
+    int head, i0, i1;
     bool at_start;         // it begins the share
 
-    __device__ bool next(const PagedArgs &a, int M)
+    __device__ bool next(const PagedArgs &a)
     {
         if (t >= t1) return false;
         at_start = i1 < 0;
-        while (t >= (before + vis.tiles) * M) {             // next request with visible keys
-            before += vis.tiles;
-            vis = visible_keys(a, __ldg(a.lens + ++req));
+        while (t >= base + vis.tiles * a.Hkv) {             // next request with visible keys
+            base += vis.tiles * a.Hkv;
+            if (++req == a.n_req) {
+                req = 0;
+                ++rt;
+            }
+            vis = visible_keys(a, __ldg(a.lens + req));
         }
-        const int rel = t - before * M;
-        m = (unsigned)rel / (unsigned)vis.tiles;
-        i0 = rel - m * vis.tiles;
+        const int rel = t - base;
+        head = (unsigned)rel / (unsigned)vis.tiles;
+        i0 = rel - head * vis.tiles;
         i1 = vis.tiles - i0 < t1 - t ? vis.tiles : i0 + (t1 - t);
         t += i1 - i0;
         return true;
@@ -129,12 +135,27 @@ struct Walk {
     __device__ int slot() const { return 2 * (int)blockIdx.x + (at_start ? 0 : 1); }
 };
 
-// The same by each warp for itself, for few requests (kPerLane a lane): no barrier
-// and no shared memory between the lengths and the first use of the share.
+// Row tile and tile within it of a block's first tile, and the walk up to the
+// request, which the caller fills in.
+__device__ __forceinline__ int start_walk(const PagedArgs &a, int total, const Shares &sh, Walk &w)
+{
+    const int t0 = sh.start(blockIdx.x), tiles = total * a.Hkv;             // of one row tile
+    w.t = t0;
+    w.t1 = sh.start(blockIdx.x + 1);
+    w.rt = row_tiles(a) == 1 ? 0 : t0 / tiles;
+    w.base = w.rt * tiles;
+    w.at_start = true;
+    w.i1 = -1;
+    return t0 - w.base;
+}
+
+// Find the block's share; false if it has none.  By each warp for itself, for few
+// requests (kPerLane a lane): no barrier and no shared memory between the lengths
+// and the first use of the share.
 constexpr int kPerLane = 4, kFewRequests = 32 * kPerLane;
 __device__ __forceinline__ bool find_share_warp(const PagedArgs &a, Walk &w, Shares &sh)
 {
-    const int lane = threadIdx.x & 31, M = units_per_request(a);
+    const int lane = threadIdx.x & 31, M = a.Hkv;
     int len[kPerLane], n[kPerLane], sum = 0;
     bool bad = false;
 #pragma unroll
@@ -155,38 +176,35 @@ __device__ __forceinline__ bool find_share_warp(const PagedArgs &a, Walk &w, Sha
         const int v = __shfl_up_sync(0xffffffffu, inc, o);
         if (lane >= o) inc += v;
     }
-    sh = Shares(__shfl_sync(0xffffffffu, inc, 31) * M, a.n_cta);
+    const int total = __shfl_sync(0xffffffffu, inc, 31);
+    sh = Shares(total * M * row_tiles(a), a.n_cta);
     if ((int)blockIdx.x >= sh.C) return false;
-    const int t0 = sh.start(blockIdx.x);
+    const int at = start_walk(a, total, sh, w);
     int b = inc - sum, req = lane * kPerLane, length = len[0];
-    const unsigned holder = __ballot_sync(0xffffffffu, t0 >= b * M && t0 < inc * M);
+    const unsigned holder = __ballot_sync(0xffffffffu, at >= b * M && at < inc * M);
 #pragma unroll
     for (int i = 0; i + 1 < kPerLane; ++i)
-        if (t0 >= (b + n[i]) * M && req == lane * kPerLane + i) {
+        if (at >= (b + n[i]) * M && req == lane * kPerLane + i) {
             b += n[i];
             ++req;
             length = len[i + 1];
         }
     const int from = __ffs(holder) - 1;
-    w.t = t0;
-    w.t1 = sh.start(blockIdx.x + 1);
     w.req = __shfl_sync(0xffffffffu, req, from);
-    w.before = __shfl_sync(0xffffffffu, b, from);
+    w.base += M * __shfl_sync(0xffffffffu, b, from);
     w.vis = visible_keys(a, __shfl_sync(0xffffffffu, length, from));
-    w.at_start = true;
-    w.i1 = -1;
     return true;
 }
 
-// Find the block's share by a scan over the requests, NT threads (a multiple of
-// 32), each with a run of them; false if the block has none.  May synchronise the
-// block (also where it returns false).
+// By a scan over the requests with the whole block, NT threads (a multiple of 32),
+// each with a run of them, for any number.  May synchronise the block (also where
+// it returns false).
 template <int NT>
 __device__ __forceinline__ bool find_share(const PagedArgs &a, PlanSmem &s, Walk &w, Shares &sh)
 {
     if (a.n_req <= kFewRequests) return find_share_warp(a, w, sh);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int M = units_per_request(a), per = (a.n_req + NT - 1) / NT;
+    const int M = a.Hkv, per = (a.n_req + NT - 1) / NT;
     const int q0 = tid * per < a.n_req ? tid * per : a.n_req, q1 = q0 + per < a.n_req ? q0 + per : a.n_req;
     int sum = 0;
     bool bad = false;
@@ -210,30 +228,28 @@ __device__ __forceinline__ bool find_share(const PagedArgs &a, PlanSmem &s, Walk
         if (x < warp) b += s.warp[x];
         total += s.warp[x];
     }
-    sh = Shares(total * M, a.n_cta);
+    sh = Shares(total * M * row_tiles(a), a.n_cta);
     const bool work = (int)blockIdx.x < sh.C;
-    const int t0 = sh.start(blockIdx.x);
-    if (work && t0 >= b * M && t0 < (b + sum) * M) {        // one thread's run holds the first tile
-        for (int r = q0; r < q1; ++r) {
-            const int len = __ldg(a.lens + r), n = visible_keys(a, len).tiles;
-            if (t0 < (b + n) * M) {
-                s.req = r;
-                s.before = b;
-                s.len = len;
-                break;
+    if (work) {
+        const int at = start_walk(a, total, sh, w);
+        if (at >= b * M && at < (b + sum) * M) {            // one thread's run holds the first tile
+            for (int r = q0; r < q1; ++r) {
+                const int len = __ldg(a.lens + r), n = visible_keys(a, len).tiles;
+                if (at < (b + n) * M) {
+                    s.req = r;
+                    s.before = b;
+                    s.len = len;
+                    break;
+                }
+                b += n;
             }
-            b += n;
         }
     }
     __syncthreads();
     if (!work) return false;
-    w.t = t0;
-    w.t1 = sh.start(blockIdx.x + 1);
     w.req = s.req;
-    w.before = s.before;
+    w.base += M * s.before;
     w.vis = visible_keys(a, s.len);
-    w.at_start = true;
-    w.i1 = -1;
     return true;
 }
 
@@ -244,7 +260,8 @@ __device__ __forceinline__ void write_note(const PagedArgs &a, bool work, const 
     if (work && w.i0 == 0 && w.i1 < w.vis.tiles) {
         n.cut = 1;
         n.req = w.req;
-        n.m = w.m;
+        n.head = w.head;
+        n.rt = w.rt;
         n.last = sh.block_of(w.t - w.i1 + w.vis.tiles - 1);
         n.slot = w.slot();
     }
@@ -264,22 +281,19 @@ __device__ __forceinline__ void write_empty(const PagedArgs &a, int thread)
     }
 }
 
-// Unit m of a request: key head, first query head of the group, first token.
+// A unit's rows: row rho is token i0 + rho / Gt, query head g0 + rho % Gt of the group.
 struct Unit {
-    int head, g0, i0;      // row rho is token i0 + rho / Gt, head g0 + rho % Gt
+    int head, g0, i0;
 };
-__device__ __forceinline__ Unit unit_of(const PagedArgs &a, int m)
+__device__ __forceinline__ Unit unit_of(const PagedArgs &a, int head, int rt)
 {
     Unit u;
-    if (a.n_gt * a.n_bt == 1) {             // one row tile per key head
-        u.head = m;
-        u.g0 = u.i0 = 0;
-        return u;
+    u.head = head;
+    u.g0 = u.i0 = 0;
+    if (row_tiles(a) > 1) {
+        u.g0 = rt / a.n_bt * a.Gt;
+        u.i0 = rt % a.n_bt * a.Bt;
     }
-    u.head = m / (a.n_gt * a.n_bt);
-    const int rest = m % (a.n_gt * a.n_bt);
-    u.g0 = rest / a.n_bt * a.Gt;
-    u.i0 = rest % a.n_bt * a.Bt;
     return u;
 }
 // Element offset of row rho of a unit in Q and O, and whether the row exists.
