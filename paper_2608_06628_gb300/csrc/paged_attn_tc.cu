@@ -349,7 +349,8 @@ __global__ void __launch_bounds__(Roles<kCopies>::kThreads, 1) k_paged_attn_tc(c
             tmem_wait_st();
         }
         while (w.next(a)) {              // left by a vote only, so that the warps of a row stay together
-            float ref = -INFINITY, l2[2] = {0.f, 0.f};     // the row's sum over this thread's keys, in two
+            float ref = -INFINITY;
+            f32x2 l2 = pair2(0.f, 0.f);                    // the row's sum over this thread's keys, in two
             bool left = false;
             for (int i = w.i0; i < w.i1; ++i, ++n) {
                 const uint32_t b = n & 1;
@@ -422,8 +423,7 @@ __global__ void __launch_bounds__(Roles<kCopies>::kThreads, 1) k_paged_attn_tc(c
                     tc_fence_after();
                 }
                 if (rescale) {
-                    l2[0] *= f;
-                    l2[1] *= f;
+                    l2 = mul2(l2, pair2(f, f));
 #pragma unroll 1
                     for (int x = 0; x < kFeat / 32; ++x) {
                         const uint32_t at = tmem + cO + kFeat * part + 32 * x + lane_off;
@@ -436,15 +436,17 @@ __global__ void __launch_bounds__(Roles<kCopies>::kThreads, 1) k_paged_attn_tc(c
                     }
                 }
                 const float base = ref == -INFINITY ? 0.f : ref;
+                const f32x2 c2 = pair2(to_log2, to_log2), base2 = pair2(-base, -base);
 #pragma unroll
                 for (int x = 0; x < kKeys / 32; ++x) {
                     float p[16];                           // pairs of bf16
 #pragma unroll
                     for (int y = 0; y < 32; y += 2) {
-                        const float p0 = ex2(fmaf(s[x][y], to_log2, -base));
-                        const float p1 = ex2(fmaf(s[x][y + 1], to_log2, -base));
-                        l2[0] += p0;
-                        l2[1] += p1;
+                        float p0, p1;
+                        unpair2(fma2(pair2(s[x][y], s[x][y + 1]), c2, base2), p0, p1);
+                        p0 = ex2(p0);
+                        p1 = ex2(p1);
+                        l2 = add2(l2, pair2(p0, p1));
                         p[y / 2] = __uint_as_float(pack_bf16x2(p0, p1));
                     }
                     tmem_st16(tmem + cP + 64 * b + key0 / 2 + 16 * x + lane_off, p);
@@ -459,7 +461,9 @@ __global__ void __launch_bounds__(Roles<kCopies>::kThreads, 1) k_paged_attn_tc(c
             const bool live = row_at(a, w.req, u, row, at), whole = w.whole();
             bf16 *out = static_cast<bf16 *>(a.O) + at;
             float *partial = a.part + w.slot() * partial_floats(rows, D);
-            float l = l2[0] + l2[1], f = 1.f;
+            float l, l_odd, f = 1.f;
+            unpair2(l2, l, l_odd);
+            l += l_odd;
             if (kCopies > 1) {
                 // reference and sum of the row over its copies
                 exchange[tid] = ref;
