@@ -97,7 +97,7 @@ template <int KEYS> struct Chunks {
 };
 
 template <int D, int ROWS>
-__global__ __launch_bounds__(kThreads) void k_paged_attn(const PagedArgs a, int page_lg)
+__global__ __launch_bounds__(kThreads, 2) void k_paged_attn(const PagedArgs a, int page_lg)
 {
     using S = Smem<D, ROWS>;
     constexpr int KEYS = S::kKeys, KL = KEYS / 32, RW = ROWS / kWarps;      // keys of a lane, rows of a warp
@@ -434,8 +434,8 @@ template <int D, int ROWS> cudaError_t launch_f32(const PagedArgs &a, cudaStream
     static_assert(sizeof(S) < 113 * 1024, "two blocks per multiprocessor");
     int lg = 4;
     while ((1 << lg) < a.page_size) ++lg;
-    cudaError_t e =
-        cudaFuncSetAttribute(k_paged_attn<D, ROWS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(S));
+    static std::atomic<unsigned long long> opted{0};
+    cudaError_t e = pipe::opt_in(reinterpret_cast<const void *>(&k_paged_attn<D, ROWS>), (int)sizeof(S), opted);
     if (e != cudaSuccess) return e;
     e = pipe::launch_early(k_paged_attn<D, ROWS>, dim3(a.n_cta), dim3(kThreads), sizeof(S), st, a, lg);
     if (e != cudaSuccess) return e;

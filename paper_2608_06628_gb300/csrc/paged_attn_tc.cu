@@ -41,8 +41,6 @@
 // Warps: softmax and epilogue (4 with copies, else 8: warp w reaches the lanes
 // 32 (w % 4) ...), producers of K and V, issuers of S (and loads of Q) and of O.
 // Every wait is bounded (tc_pipeline.cuh).
-#include <atomic>
-
 #include "paged_plan.cuh"
 #include "tc_pipeline.cuh"
 
@@ -608,17 +606,9 @@ template <int D, int kCopies> cudaError_t launch(const PagedArgs &a, cudaStream_
             !encode_bf16(&ta.tmV, a.V, 4, dk, sk, bk))
             return cudaErrorInvalidValue;
     }
-    // opt in to the shared memory once per device
     static std::atomic<unsigned long long> opted{0};
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
-    const unsigned long long bit = 1ull << dev;
-    if (!(opted.load(std::memory_order_acquire) & bit)) {
-        const cudaError_t e =
-            cudaFuncSetAttribute(k_paged_attn_tc<D, kCopies>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemLimit);
-        if (e != cudaSuccess) return e;
-        opted.fetch_or(bit, std::memory_order_release);
-    }
+    const cudaError_t e = opt_in(reinterpret_cast<const void *>(&k_paged_attn_tc<D, kCopies>), kSmemLimit, opted);
+    if (e != cudaSuccess) return e;
     return pipe::launch_early(k_paged_attn_tc<D, kCopies>, dim3(a.n_cta), dim3(Roles<kCopies>::kThreads), ta.bytes, st, ta);
 }
 

@@ -9,6 +9,7 @@
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
+#include <atomic>
 #include <mutex>
 
 #include "tc_ptx.cuh"
@@ -206,6 +207,19 @@ inline cudaError_t launch_early(void (*kernel)(Params...), dim3 grid, dim3 block
     lc.attrs = attr;
     lc.numAttrs = 1;
     return cudaLaunchKernelEx(&lc, kernel, args...);
+}
+
+// Opt a kernel in to `bytes` of dynamic shared memory, once per device; `opted` is
+// the kernel's own static word.
+inline cudaError_t opt_in(const void *kernel, int bytes, std::atomic<unsigned long long> &opted)
+{
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
+    const unsigned long long bit = 1ull << dev;
+    if (opted.load(std::memory_order_acquire) & bit) return cudaSuccess;
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == cudaSuccess) opted.fetch_or(bit, std::memory_order_release);
+    return e;
 }
 
 inline int sm_count()

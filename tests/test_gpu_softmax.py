@@ -602,3 +602,13 @@ def test_decoding_in_a_graph(dt):
         close_rows(q, want_rope(r, r["q"], r["wq"]), dt, "q")
         want = R.paged_attention(q[:, None], s["kc"], s["vc"], s["table"], lens, 0, 0)
         assert_parity(o.double().cpu().numpy(), want.cpu().numpy(), dt, "replay", units="out")
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
+def test_attention_row_tiles_of_many_requests(dt):
+    """More query rows than one tile holds, with few and with many requests (which share out their work differently)."""
+    rng = random.Random(2)
+    for n in (3, 128, 129, 400):
+        lens = [rng.choice([0, 1, 127, 128, rng.randint(0, 400)]) for _ in range(n)]
+        check_attn(attn_setup(dt, 40, 14, 2, 64, 32, lens, seed=n), f"{n} requests, 280 rows")
+    check_attn(attn_setup(dt, 128, 8, 1, 128, 16, [3000, 0, 50], 700, 30), "1024 rows, window")
