@@ -42,6 +42,12 @@ __device__ __forceinline__ void load_pairs(const float *p, f32x2 &a, f32x2 &b)
     b.v = v.y;
 }
 
+// 16 bytes to shared memory, `bytes` of them read and the rest zeros
+__device__ __forceinline__ void copy16(uint32_t dst, const float *src, int bytes)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+
 template <int D, int ROWS> struct Smem {
     static constexpr int kKeys = D == 64 ? 64 : 32;
     static constexpr int kStages = ROWS == kFewRows ? 3 : 2;   // chunks in place or on their way
@@ -123,29 +129,40 @@ __global__ __launch_bounds__(kThreads, 2) void k_paged_attn(const PagedArgs a, i
         auto issue = [&](int b) {
             if (ahead.live) {
                 const int *pages = a.table + (size_t)ahead.w.req * a.max_pages;
-                const int head = ahead.w.head;
-#pragma unroll
-                for (int x = 0; x < kCopies; ++x) {
-                    const int r = row0 + x * kRowStep, j = ahead.j0 + r;
-                    const bool see = key_visible(ahead.w.vis, j);
-                    size_t from = 0;
-                    if (see) {
-                        int page = __ldg(pages + (j >> page_lg));
-                        if (page < 0 || page >= a.n_pages) {
-                            raise_error(a.err, ERR_BAD_INDEX);
-                            page = 0;
-                        }
-                        from = ((((size_t)page * a.Hkv + head) << page_lg) + (j & ((1 << page_lg) - 1))) * D + col;
+                // this thread's 16 bytes of a key in the cache, from its page
+                auto in_cache = [&](int j) {
+                    int page = __ldg(pages + (j >> page_lg));
+                    if (page < 0 || page >= a.n_pages) {
+                        raise_error(a.err, ERR_BAD_INDEX);
+                        page = 0;
                     }
-                    const int bytes = see ? 16 : 0;          // masked keys are zero-filled
-                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(
-                                     ptx::smem_u32(&s.chunk[b].k[r][col])),
-                                 "l"(static_cast<const float *>(a.K) + from), "r"(bytes)
-                                 : "memory");
-                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(
-                                     ptx::smem_u32(&s.chunk[b].v[r][col])),
-                                 "l"(static_cast<const float *>(a.V) + from), "r"(bytes)
-                                 : "memory");
+                    return ((((size_t)page * a.Hkv + ahead.w.head) << page_lg) + (j & ((1 << page_lg) - 1))) * D + col;
+                };
+                const uint32_t to_k = ptx::smem_u32(&s.chunk[b].k[row0][col]), to_v = ptx::smem_u32(&s.chunk[b].v[row0][col]);
+                if (ahead.j0 >= ahead.w.vis.lo && ahead.j0 + KEYS <= ahead.w.vis.len) {
+                    // all keys visible: a page is looked up once for 16 keys in a row
+                    constexpr int kRun = 16 / kRowStep > 1 ? 16 / kRowStep : 1;
+#pragma unroll
+                    for (int x = 0; x < kCopies; x += kRun) {
+                        const size_t from = in_cache(ahead.j0 + row0 + x * kRowStep);
+#pragma unroll
+                        for (int y = 0; y < kRun; ++y) {
+                            copy16(to_k + (x + y) * kRowStep * (D + 4) * 4,
+                                   static_cast<const float *>(a.K) + from + y * kRowStep * D, 16);
+                            copy16(to_v + (x + y) * kRowStep * D * 4,
+                                   static_cast<const float *>(a.V) + from + y * kRowStep * D, 16);
+                        }
+                    }
+                } else {
+#pragma unroll 1
+                    for (int x = 0; x < kCopies; ++x) {
+                        const int j = ahead.j0 + row0 + x * kRowStep;
+                        const bool see = key_visible(ahead.w.vis, j);
+                        const size_t from = see ? in_cache(j) : 0;
+                        const int bytes = see ? 16 : 0;      // masked keys are zero-filled
+                        copy16(to_k + x * kRowStep * (D + 4) * 4, static_cast<const float *>(a.K) + from, bytes);
+                        copy16(to_v + x * kRowStep * D * 4, static_cast<const float *>(a.V) + from, bytes);
+                    }
                 }
                 ahead.step(a);
             }
