@@ -19,9 +19,10 @@
 // and a sum of its own, and O is the sum of the copies' rows, formed at the end of a
 // segment.  The products' padding costs nothing here: a tile's products take about
 // 0.6 us, its bytes 1.5 us at an SM's share of the memory bandwidth.  With more
-// rows, two threads share a row (64 keys each, one reference): they lie in different
-// warps, agree by one barrier vote per tile that no reference has to move, and
-// exchange maxima only if one has.
+// rows, two threads share a row, 64 keys of every tile each, with a reference, a sum
+// and an accumulator O of its own; P then takes the place of the S it was made
+// from (Tensor Memory holds two S and two O), and the halves are added at the end of
+// a segment.  So no warp waits for another between the tiles of a segment.
 //
 // The cache is read once per row tile by TMA boxes of one page of one head (64
 // features x page_size rows, 128-byte swizzle), issued by one warp for K and one
@@ -109,8 +110,9 @@ __global__ void __launch_bounds__(Roles<kCopies>::kThreads, 1) k_paged_attn_tc(c
     constexpr uint32_t kPanel = kTile * 128;               // bytes of one panel of a Q, K or V tile
     constexpr uint32_t kSlot = kHalves * kPanel;
     constexpr int kCopyRows = 128 / kCopies;
-    // Tensor Memory columns: S (2 x 128), P (2 x 64), O
-    constexpr uint32_t cS = 0, cP = 256, cO = 384;
+    // Tensor Memory columns: S (2 x 128); with copies P (2 x 64) and O, else the O of
+    // both halves of the keys, and P in the first 32 columns of its half of S
+    constexpr uint32_t cS = 0, cP = 256, cO = kCopies > 1 ? 384 : 256;
     const PagedArgs &a = ta.p;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -124,9 +126,9 @@ __global__ void __launch_bounds__(Roles<kCopies>::kThreads, 1) k_paged_attn_tc(c
     uint64_t *full = bars;               // [NK + NV] the K or V tile has landed
     uint64_t *empty = full + kMaxSlots;  // [NK + NV] its products are done
     uint64_t *sready = empty + kMaxSlots;// [2] S is formed
-    uint64_t *sfree = sready + 2;        // [2] S has been read
-    uint64_t *pready = sfree + 2;        // [2] P is written (and O rescaled, V's masked rows zeroed)
-    uint64_t *pvdone = pready + 2;       // [2] O includes the tile's P V
+    uint64_t *sfree = sready + 2;        // [2] S has been read (with copies; else pvdone tells it)
+    uint64_t *pready = sfree + 2;        // [2][kParts] P is written (and O rescaled, V's masked rows zeroed)
+    uint64_t *pvdone = pready + 4;       // [2] O includes the tile's P V
     uint64_t *qfull = pvdone + 2;
     uint64_t *qempty = qfull + 1;        // the segment's last S is formed
     uint64_t *ofree = qempty + 1;        // the epilogue has read O
@@ -152,7 +154,7 @@ __global__ void __launch_bounds__(Roles<kCopies>::kThreads, 1) k_paged_attn_tc(c
         for (int i = 0; i < 2; ++i) {
             mbar_init(&sready[i], 1);
             mbar_init(&sfree[i], n_soft);
-            mbar_init(&pready[i], n_soft);
+            for (int p = 0; p < kParts; ++p) mbar_init(&pready[i * kParts + p], n_quads);
             mbar_init(&pvdone[i], 1);
             mbar_init(&drained[i], 1);
         }
@@ -256,7 +258,9 @@ __global__ void __launch_bounds__(Roles<kCopies>::kThreads, 1) k_paged_attn_tc(c
                 ++seg;
                 for (int i = w.i0; ok && i < w.i1; ++i, ++n) {
                     const uint32_t b = n & 1;
-                    ok = wait_soon(&sfree[b], ((n >> 1) & 1u) ^ 1u, fail) && wait_soon(&full[pos.slot], pos.phase, fail);
+                    // S's buffer is free: read, or (P being in it) multiplied
+                    ok = wait_soon(kCopies > 1 ? &sfree[b] : &pvdone[b], ((n >> 1) & 1u) ^ 1u, fail) &&
+                         wait_soon(&full[pos.slot], pos.phase, fail);
                     if (!ok) break;
                     tc_fence_after();
                     const uint64_t bk = k_desc + pos.slot * (kSlot >> 4);
@@ -285,26 +289,34 @@ __global__ void __launch_bounds__(Roles<kCopies>::kThreads, 1) k_paged_attn_tc(c
             while (ok && w.next(a)) {
                 // O is overwritten by a segment's first product: the last epilogue has read it
                 if (seg > 0) ok = wait_soon(ofree, (seg - 1) & 1u, fail);
+                uint32_t acc[kParts] = {};                 // whether the segment has written the accumulator
                 for (int i = w.i0; ok && i < w.i1; ++i, ++n) {
                     const uint32_t b = n & 1;
                     const int j = key_tile(w.vis, i) * kTile;
-                    ok = wait_soon(&full[NK + pos.slot], pos.phase, fail) && wait_soon(&pready[b], (n >> 1) & 1u, fail);
-                    if (!ok) break;
-                    tc_fence_after();
+                    const bool all = all_visible(w.vis, j);
+                    constexpr int kSteps = kTile / 16 / kParts;
+                    ok = wait_soon(&full[NK + pos.slot], pos.phase, fail);
                     const uint64_t bv = v_desc + pos.slot * (kSlot >> 4);
-                    if (all_visible(w.vis, j)) {
 #pragma unroll
-                        for (int g = 0; g < kTile / 16; ++g)
-                            mma_bf16_ts(tmem + cO, tmem + cP + 64 * b + 8 * g, bv + g * (2048 >> 4), id,
-                                        g > 0 || i > w.i0);
-                    } else {
-                        uint32_t acc = i > w.i0;
-                        for (int g = 0; g < kTile / 16; ++g) {
-                            if (!any_visible(w.vis, j + 16 * g, 16)) continue;
-                            mma_bf16_ts(tmem + cO, tmem + cP + 64 * b + 8 * g, bv + g * (2048 >> 4), id, acc);
-                            acc = 1;
+                    for (int p = 0; p < kParts; ++p) {
+                        ok = ok && wait_soon(&pready[b * kParts + p], (n >> 1) & 1u, fail);
+                        if (!ok) break;
+                        tc_fence_after();
+                        const uint32_t o = tmem + cO + 128 * p, pa = tmem + (kCopies > 1 ? cP + 64 * b : cS + 128 * b + 64 * p);
+                        if (all) {
+#pragma unroll
+                            for (int g = 0; g < kSteps; ++g)
+                                mma_bf16_ts(o, pa + 8 * g, bv + (p * kSteps + g) * (2048 >> 4), id, acc[p] | (g > 0));
+                            acc[p] = 1;
+                        } else {
+                            for (int g = 0; g < kSteps; ++g) {
+                                if (!any_visible(w.vis, j + 16 * (p * kSteps + g), 16)) continue;
+                                mma_bf16_ts(o, pa + 8 * g, bv + (p * kSteps + g) * (2048 >> 4), id, acc[p]);
+                                acc[p] = 1;
+                            }
                         }
                     }
+                    if (!ok) break;
                     mma_commit(&pvdone[b]);
                     mma_commit(&empty[NK + pos.slot]);
                     pos.step(NV);
@@ -317,7 +329,7 @@ __global__ void __launch_bounds__(Roles<kCopies>::kThreads, 1) k_paged_attn_tc(c
     } else if (work && warp < W::kSoft && (warp & 3) < n_quads) {
         // --------------------------------------------------- softmax, epilogue
         constexpr int kKeys = kTile / (kParts * kCopies);   // keys of a tile of this thread
-        constexpr int kFeat = D / kParts;                   // features of O that it rescales and reads
+        constexpr int kFeat = D / kParts;                   // features of the output that it writes
         constexpr int kGroup = 32 * (kCopies > 1 ? 4 : kParts);   // threads that share rows
         const int quad = warp & 3, part = kCopies > 1 ? 0 : warp >> 2;
         const int copy = kCopies > 1 ? tid / kCopyRows : 0, row = kCopies > 1 ? tid % kCopyRows : 32 * quad + lane;
@@ -325,6 +337,7 @@ __global__ void __launch_bounds__(Roles<kCopies>::kThreads, 1) k_paged_attn_tc(c
         const int worker = kCopies > 1 ? tid : 32 * (part * n_quads + quad) + lane;   // among the threads at work
         const uint32_t lane_off = (uint32_t)(32 * quad) << 16;
         const uint32_t group_bar = kCopies > 1 ? 1 : 1 + quad;
+        const uint32_t my_o = tmem + cO + 128 * part + lane_off;
         const float to_log2 = kLog2e * rsqrtf((float)D);
         float *stage = reinterpret_cast<float *>(smem + ta.off_stage);   // with copies
         uint32_t n = 0;                                    // tiles so far
@@ -346,14 +359,13 @@ __global__ void __launch_bounds__(Roles<kCopies>::kThreads, 1) k_paged_attn_tc(c
             for (int x = 0; x < 4; ++x) tmem_st32(tmem + cP + 32 * x + lane_off, zero);
             tmem_wait_st();
         }
-        while (w.next(a)) {              // left by a vote only, so that the warps of a row stay together
+        while (w.next(a)) {     // left by a vote at a segment's end only, so that the warps of a row stay together
             float ref = -INFINITY;
             f32x2 l2 = pair2(0.f, 0.f);                    // the row's sum over this thread's keys, in two
-            bool left = false;
             for (int i = w.i0; i < w.i1; ++i, ++n) {
                 const uint32_t b = n & 1;
                 const int j0 = key_tile(w.vis, i) * kTile;
-                const bool edge = !all_visible(w.vis, j0), first = i == w.i0;
+                const bool edge = !all_visible(w.vis, j0);
                 if (edge) {
                     // masked rows of V in the groups that enter the product.  (An earlier
                     // tile's product first, so that the slot's last item has landed and the
@@ -379,7 +391,7 @@ __global__ void __launch_bounds__(Roles<kCopies>::kThreads, 1) k_paged_attn_tc(c
                 for (int x = 0; x < kKeys / 32; ++x)
                     tmem_ld32(tmem + cS + 128 * b + key0 + 32 * x + lane_off, s[x]);
                 tmem_wait_ld();
-                arrive(&sfree[b]);
+                if (kCopies > 1) arrive(&sfree[b]);
                 if (edge) {
                     const int k0 = j0 + key0, hi = w.vis.len - k0, lo = w.vis.lo - k0, sink = w.vis.sink - k0;
 #pragma unroll
@@ -396,26 +408,14 @@ __global__ void __launch_bounds__(Roles<kCopies>::kThreads, 1) k_paged_attn_tc(c
 #pragma unroll
                     for (int y = 0; y < 32; ++y) mx4[y & 3] = fmaxf(mx4[y & 3], s[x][y]);
                 float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])) * to_log2;
-                bool moves = row < rows && mx > ref + kSlack;      // from -inf: whenever a key is visible
-                if (kParts > 1) {
-                    moves = group_sync_failed(group_bar, kGroup, bad || moves);
-                    if (moves) {
-                        exchange[part * 128 + row] = mx;
-                        if (group_sync_failed(group_bar, kGroup, bad)) {
-                            left = true;
-                            break;
-                        }
-                        mx = fmaxf(exchange[row], exchange[128 + row]);
-                    }
-                }
                 float f = 1.f;
-                if (moves && mx > ref + kSlack) {
-                    f = ex2(ref - mx);
+                if (mx > ref + kSlack) {                   // from -inf: whenever a key is visible
+                    if (ref != -INFINITY) f = ex2(ref - mx);        // (else O and the sum are zero)
                     ref = mx;
                 }
                 // P's buffer is free, and O is at rest, once earlier products are done
-                const bool rescale = !first && __any_sync(0xffffffffu, f != 1.f && row < rows);
-                if (rescale || n >= 2) {
+                const bool rescale = __any_sync(0xffffffffu, f != 1.f && row < rows);
+                if (rescale || (kCopies > 1 && n >= 2)) {
                     const uint32_t k = rescale ? n - 1 : n - 2;
                     wait(&pvdone[k & 1], (k >> 1) & 1u);
                     tc_fence_after();
@@ -423,14 +423,13 @@ __global__ void __launch_bounds__(Roles<kCopies>::kThreads, 1) k_paged_attn_tc(c
                 if (rescale) {
                     l2 = mul2(l2, pair2(f, f));
 #pragma unroll 1
-                    for (int x = 0; x < kFeat / 32; ++x) {
-                        const uint32_t at = tmem + cO + kFeat * part + 32 * x + lane_off;
+                    for (int x = 0; x < D / 32; ++x) {
                         float o[32];
-                        tmem_ld32(at, o);
+                        tmem_ld32(my_o + 32 * x, o);
                         tmem_wait_ld();
 #pragma unroll
                         for (int y = 0; y < 32; ++y) o[y] *= f;
-                        tmem_st32(at, o);
+                        tmem_st32(my_o + 32 * x, o);
                     }
                 }
                 const float base = ref == -INFINITY ? 0.f : ref;
@@ -447,19 +446,18 @@ __global__ void __launch_bounds__(Roles<kCopies>::kThreads, 1) k_paged_attn_tc(c
                         l2 = add2(l2, pair2(p0, p1));
                         p[y / 2] = __uint_as_float(pack_bf16x2(p0, p1));
                     }
-                    tmem_st16(tmem + cP + 64 * b + key0 / 2 + 16 * x + lane_off, p);
+                    tmem_st16(tmem + lane_off + 16 * x + (kCopies > 1 ? cP + 64 * b + key0 / 2 : cS + 128 * b + 64 * part), p);
                 }
                 tmem_wait_st();
-                arrive(&pready[b]);
+                arrive(&pready[b * kParts + part]);
             }
-            if (left) break;
             // the segment's output
             const Unit u = unit_of(a, w.head, w.rt);
             size_t at;
             const bool live = row_at(a, w.req, u, row, at), whole = w.whole();
             bf16 *out = static_cast<bf16 *>(a.O) + at;
             float *partial = a.part + w.slot() * partial_floats(rows, D);
-            float l, l_odd, f = 1.f;
+            float l, l_odd, f = 1.f, f0 = 0.f, f1 = 0.f;
             unpair2(l2, l, l_odd);
             l += l_odd;
             if (kCopies > 1) {
@@ -479,10 +477,19 @@ __global__ void __launch_bounds__(Roles<kCopies>::kThreads, 1) k_paged_attn_tc(c
                     l = fmaf(exchange[128 + c * kCopyRows + row], ex2(exchange[c * kCopyRows + row] - base), l);
                 if (copy == 0) inv_of[row] = 1.f / l;              // read after the next barrier
             } else {
-                group_sync_failed(group_bar, kGroup, false);       // the exchanged maxima have been read
-                exchange[part * 128 + row] = l;
+                // the same over the two halves of the keys
+                exchange[part * 128 + row] = ref;
+                if (group_sync_failed(group_bar, kGroup, bad)) break;
+                const float r0 = exchange[row], r1 = exchange[128 + row], top = fmaxf(r0, r1);
+                const float base = top == -INFINITY ? 0.f : top;
+                f0 = ex2(r0 - base);
+                f1 = ex2(r1 - base);
+                group_sync_failed(group_bar, kGroup, false);
+                exchange[part * 128 + row] = l * (part == 0 ? f0 : f1);
                 group_sync_failed(group_bar, kGroup, false);
                 l = exchange[row] + exchange[128 + row];
+                group_sync_failed(group_bar, kGroup, false);       // read before the next segment's are written
+                ref = top;
             }
             const float inv = 1.f / l;
             if (!whole && row < rows && (kCopies > 1 ? copy == 0 : part == 0)) {
@@ -548,11 +555,16 @@ __global__ void __launch_bounds__(Roles<kCopies>::kThreads, 1) k_paged_attn_tc(c
             } else {
 #pragma unroll 1
                 for (int x = 0; x < kFeat / 32; ++x) {
-                    float o[32];
-                    tmem_ld32(tmem + cO + kFeat * part + 32 * x + lane_off, o);
+                    const uint32_t from = tmem + cO + kFeat * part + 32 * x + lane_off;
+                    float o[32], o1[32];
+                    tmem_ld32(from, o);
+                    tmem_ld32(from + 128, o1);
                     tmem_wait_ld();
                     if (x == kFeat / 32 - 1) arrive(ofree);
                     if (bad) continue;
+                    // (a half without a visible key in the segment may not have been written)
+#pragma unroll
+                    for (int y = 0; y < 32; ++y) o[y] = (f0 != 0.f ? o[y] * f0 : 0.f) + (f1 != 0.f ? o1[y] * f1 : 0.f);
                     const int col = kFeat * part + 32 * x;
                     if (whole) {
                         if (live) {
