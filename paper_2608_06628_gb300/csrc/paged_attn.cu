@@ -366,7 +366,7 @@ __global__ __launch_bounds__(kThreads) void k_paged_join(const PagedArgs a)
     if (!note.cut) return;
     const size_t size = partial_floats(rows, a.d);
     const int n = note.last - c + 1;                         // partials
-    auto part_of = [&](int i) { return a.part + (size_t)(i == 0 ? note.slot : 2 * (c + i)) * size; };
+    auto part_of = [&](int i) { return a.part + (size_t)(i == 0 ? 2 * c + 1 : 2 * (c + i)) * size; };
 
     const int rho = tid % rows, lane = tid / rows, lanes = kThreads / rows;   // threads of a row
     const int groups = lanes >= COLS ? lanes / COLS : 1, step = lanes >= COLS ? COLS : lanes;
@@ -481,6 +481,7 @@ void paged_geometry(const hybrid_cfg &c, PagedArgs &a)
     a.Bt = max_rows / a.Gt < a.B ? max_rows / a.Gt : a.B;
     a.n_bt = (a.B + a.Bt - 1) / a.Bt;
     a.Bt = (a.B + a.n_bt - 1) / a.n_bt;                                     // row tiles of about equal size
+    a.extra = tc && a.Bt * a.Gt <= 64 ? 2 : 5;
     a.n_cta = (tc ? 1 : 2) * pipe::sm_count();
 }
 

@@ -3,20 +3,23 @@
 //
 // A unit is (row tile, request, key head): n_gt * n_bt row tiles, all units of a
 // request with the same visible keys.  The visible keys of a request are cut into
-// tiles of kTile keys; the tiles of all units, in the order (row tile, request, key
-// head, tile), are shared out evenly: of C blocks, block c takes the tiles
-// [c T / C, (c + 1) T / C).  So every block reads the same amount of cache
-// whatever the lengths are, and a long request is split over as many blocks as
-// it is worth.  Where there are several row tiles, the blocks of one are at the
+// tiles of kTile keys.  Work is counted in quarters of a tile: a unit of n tiles is
+// 4 n + extra quarters, `extra` for what a change of units costs a block (measured
+// at 64 requests of 256-8192 tokens: 0.4 tiles where rows are copied, 1.2 where
+// they fill the product).  The quarters of all units, in the order (row tile, request,
+// key head, tile), are shared out evenly over the blocks, at least four to a block,
+// and a tile belongs to the block that has its first quarter.  So every block is
+// busy for the same time whatever the lengths are, and a long request is split over
+// as many blocks as it is worth.  Where there are several row tiles, the blocks of one are at the
 // same keys as the blocks of another at any time, and all but the first find them
 // in L2.  The lengths are on the device, so each block finds its share
 // itself by a scan over the requests (a few KB).
 //
 // A run of tiles of one unit is a segment.  A segment that covers its unit writes
 // the output; any other writes (m, l, O) -- running maximum in units of log2,
-// sum and unnormalised output -- to partial 2 c (segment at the start of the
-// block's share) or 2 c + 1 (a later one: only a block's last segment can be cut
-// there).  A second launch joins them, told by notes what to join.
+// sum and unnormalised output -- to partial 2 c (the segment goes on with a unit of
+// an earlier block c - 1) or 2 c + 1 (it begins one that later blocks go on with).  A
+// second launch joins them, told by notes what to join.
 //
 // Workspace: n_cta notes, then 2 n_cta partials.
 #pragma once
@@ -67,18 +70,21 @@ __device__ __forceinline__ bool any_visible(const Visible &v, int j, int n)
 
 __device__ __forceinline__ int row_tiles(const PagedArgs &a) { return a.n_gt * a.n_bt; }
 
-// Shares of T tiles over C blocks (C <= T): the first T % C blocks take one more.
+// Quarters of a unit of n tiles.
+__device__ __forceinline__ int unit_quarters(const PagedArgs &a, int tiles) { return tiles > 0 ? 4 * tiles + a.extra : 0; }
+
+// Shares of T quarters over C blocks: the first T % C blocks take one more.
 // T < 2^31 (the host's check).
 struct Shares {
     int per, rem, C;
     __device__ Shares(int T, int n_cta)
     {
-        C = T < n_cta ? T : n_cta;
+        C = T / 4 < n_cta ? T / 4 : n_cta;
         per = C == 0 ? 0 : T / C;
         rem = T - per * C;
     }
     __device__ int start(int c) const { return per * c + (c < rem ? c : rem); }
-    // block of a tile
+    // block of a quarter
     __device__ int block_of(int t) const
     {
         const int big = rem * (per + 1);
@@ -91,9 +97,8 @@ struct Shares {
 struct JoinNote {
     int cut;               // 0: nothing to join
     int req, head, rt;     // the unit
-    int last;              // block of its last tile; blocks c + 1 ... last hold partial 2 b
-    int slot;              // block c's partial
-    int pad[2];
+    int last;              // block of its last tile: partials 2 c + 1, 2 (c + 1), ... 2 last
+    int pad[3];
 };
 
 // Scratch of the search for a block's share.
@@ -104,48 +109,54 @@ struct PlanSmem {
 
 // The segments of a block's share, one after another.
 struct Walk {
-    int t, t1;             // next tile, end of the share
-    int base;              // tiles of the row tiles before, and of the requests before `req`
+    int t, t1;             // next quarter, end of the share
+    int base;              // quarters of the row tiles before, and of the requests before `req`
     int req, rt;           // request and row tile
     Visible vis;
     // the current segment: tiles [i0, i1) of key head `head` of request `req`
     int head, i0, i1;
-    bool at_start;         // it begins the share
 
     __device__ bool next(const PagedArgs &a)
     {
-        if (t >= t1) return false;
-        at_start = i1 < 0;
-        while (t >= base + vis.tiles * a.Hkv) {             // next request with visible keys
-            base += vis.tiles * a.Hkv;
-            if (++req == a.n_req) {
-                req = 0;
-                ++rt;
+        while (t < t1) {
+            int unit = unit_quarters(a, vis.tiles);
+            while (t >= base + unit * a.Hkv) {              // next request with visible keys
+                base += unit * a.Hkv;
+                if (++req == a.n_req) {
+                    req = 0;
+                    ++rt;
+                }
+                vis = visible_keys(a, __ldg(a.lens + req));
+                unit = unit_quarters(a, vis.tiles);
             }
-            vis = visible_keys(a, __ldg(a.lens + req));
+            const int rel = t - base;
+            const int h = (unsigned)rel / (unsigned)unit;
+            const int q0 = rel - h * unit, q1 = unit - q0 < t1 - t ? unit : q0 + (t1 - t);
+            t += q1 - q0;
+            const int first = (q0 + 3) >> 2, end = (q1 + 3) >> 2;       // tiles whose first quarter is here
+            if (first >= vis.tiles) continue;
+            head = h;
+            i0 = first;
+            i1 = end < vis.tiles ? end : vis.tiles;
+            return true;
         }
-        const int rel = t - base;
-        head = (unsigned)rel / (unsigned)vis.tiles;
-        i0 = rel - head * vis.tiles;
-        i1 = vis.tiles - i0 < t1 - t ? vis.tiles : i0 + (t1 - t);
-        t += i1 - i0;
-        return true;
+        return false;
     }
     __device__ bool whole() const { return i0 == 0 && i1 == vis.tiles; }
-    __device__ int slot() const { return 2 * (int)blockIdx.x + (at_start ? 0 : 1); }
+    __device__ int slot() const { return 2 * (int)blockIdx.x + (i0 == 0 ? 1 : 0); }
 };
 
-// Row tile and tile within it of a block's first tile, and the walk up to the
-// request, which the caller fills in.
+// The walk up to the request, which the caller fills in; returns the first quarter's
+// place in its row tile (of `total` quarters per key head).
 __device__ __forceinline__ int start_walk(const PagedArgs &a, int total, const Shares &sh, Walk &w)
 {
-    const int t0 = sh.start(blockIdx.x), tiles = total * a.Hkv;             // of one row tile
+    const int t0 = sh.start(blockIdx.x), row_tile = total * a.Hkv;
     w.t = t0;
     w.t1 = sh.start(blockIdx.x + 1);
-    w.rt = row_tiles(a) == 1 ? 0 : t0 / tiles;
-    w.base = w.rt * tiles;
-    w.at_start = true;
-    w.i1 = -1;
+    w.rt = row_tiles(a) == 1 ? 0 : t0 / row_tile;
+    w.base = w.rt * row_tile;
+    w.i0 = 1;                                               // no segment yet
+    w.i1 = 0;
     return t0 - w.base;
 }
 
@@ -166,7 +177,7 @@ __device__ __forceinline__ bool find_share_warp(const PagedArgs &a, Walk &w, Sha
     }
 #pragma unroll
     for (int i = 0; i < kPerLane; ++i) {
-        n[i] = visible_keys(a, len[i]).tiles;
+        n[i] = unit_quarters(a, visible_keys(a, len[i]).tiles);
         sum += n[i];
     }
     if (bad) raise_error(a.err, ERR_BAD_INDEX);
@@ -211,7 +222,7 @@ __device__ __forceinline__ bool find_share(const PagedArgs &a, PlanSmem &s, Walk
     for (int r = q0; r < q1; ++r) {
         const int len = __ldg(a.lens + r);
         bad |= !length_ok(a, len);
-        sum += visible_keys(a, len).tiles;
+        sum += unit_quarters(a, visible_keys(a, len).tiles);
     }
     if (bad) raise_error(a.err, ERR_BAD_INDEX);
     int inc = sum;
@@ -232,9 +243,9 @@ __device__ __forceinline__ bool find_share(const PagedArgs &a, PlanSmem &s, Walk
     const bool work = (int)blockIdx.x < sh.C;
     if (work) {
         const int at = start_walk(a, total, sh, w);
-        if (at >= b * M && at < (b + sum) * M) {            // one thread's run holds the first tile
+        if (at >= b * M && at < (b + sum) * M) {            // one thread's run holds the first quarter
             for (int r = q0; r < q1; ++r) {
-                const int len = __ldg(a.lens + r), n = visible_keys(a, len).tiles;
+                const int len = __ldg(a.lens + r), n = unit_quarters(a, visible_keys(a, len).tiles);
                 if (at < (b + n) * M) {
                     s.req = r;
                     s.before = b;
@@ -262,8 +273,7 @@ __device__ __forceinline__ void write_note(const PagedArgs &a, bool work, const 
         n.req = w.req;
         n.head = w.head;
         n.rt = w.rt;
-        n.last = sh.block_of(w.t - w.i1 + w.vis.tiles - 1);
-        n.slot = w.slot();
+        n.last = sh.block_of(w.base + w.head * unit_quarters(a, w.vis.tiles) + 4 * (w.vis.tiles - 1));
     }
     a.notes[blockIdx.x] = n;
 }

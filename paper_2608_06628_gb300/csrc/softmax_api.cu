@@ -264,9 +264,9 @@ hybrid_status hybrid_paged_attn(const hybrid_cfg *cfg, const hybrid_page_cfg *pg
     hyb::PagedArgs a{};
     hyb::paged_geometry(*cfg, a);
     if (workspace_bytes < hyb::paged_workspace_bytes(a)) return HYBRID_ERR_INVALID_ARG;
-    // the kernels count tiles of 128 keys of all row tiles in an int
-    const long long tiles = ((long long)pg->max_pages * pg->page_size + 127) / 128;
-    if (tiles * n_req > 0x7fffffffll / ((long long)a.Hkv * a.n_gt * a.n_bt)) return HYBRID_ERR_UNSUPPORTED;
+    // the kernels count quarters of tiles of 128 keys, of all row tiles, in an int
+    const long long quarters = 4 * (((long long)pg->max_pages * pg->page_size + 127) / 128) + a.extra;
+    if (quarters * n_req > 0x7fffffffll / ((long long)a.Hkv * a.n_gt * a.n_bt)) return HYBRID_ERR_UNSUPPORTED;
     unsigned *err = hyb::error_word();
     if (!err) return HYBRID_ERR_CUDA;
     a.Q = Q;

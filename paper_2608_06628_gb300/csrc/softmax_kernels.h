@@ -57,6 +57,7 @@ struct PagedArgs {
     // a row tile is Bt tokens x Gt query heads of one key head
     int Gt, n_gt, Bt, n_bt;
     int n_cta;                        // blocks that share the tiles
+    int extra;                        // quarters of a tile that a unit costs besides its tiles
     unsigned *err;
 };
 // Geometry (row tiles, number of blocks) of a call; pointers left to the caller.
