@@ -434,9 +434,11 @@ __global__ __launch_bounds__(kThreads) void k_paged_join(const PagedArgs a)
     }
 }
 
-// The join of a call whose attention kernel was launched just before.
+// The join of a call whose attention kernel was launched just before; none where no
+// unit can be cut (one block, or contexts of one tile at most).
 template <typename T> cudaError_t launch_join(const PagedArgs &a, cudaStream_t st)
 {
+    if (a.n_cta == 1 || a.max_pages * a.page_size <= kTile) return cudaSuccess;
     // few rows: little shared memory, so that the blocks are in place before the
     // attention kernel ends
     const int rows = a.Bt * a.Gt;
@@ -481,7 +483,7 @@ void paged_geometry(const hybrid_cfg &c, PagedArgs &a)
     a.Bt = max_rows / a.Gt < a.B ? max_rows / a.Gt : a.B;
     a.n_bt = (a.B + a.Bt - 1) / a.Bt;
     a.Bt = (a.B + a.n_bt - 1) / a.n_bt;                                     // row tiles of about equal size
-    a.extra = tc && a.Bt * a.Gt <= 64 ? 2 : 5;
+    a.extra = tc && a.Bt * a.Gt <= 64 ? 3 : 7;
     a.n_cta = (tc ? 1 : 2) * pipe::sm_count();
 }
 

@@ -4,9 +4,10 @@
 // A unit is (row tile, request, key head): n_gt * n_bt row tiles, all units of a
 // request with the same visible keys.  The visible keys of a request are cut into
 // tiles of kTile keys.  Work is counted in quarters of a tile: a unit of n tiles is
-// 4 n + extra quarters, `extra` for what a change of units costs a block (measured
-// at 64 requests of 256-8192 tokens: 0.4 tiles where rows are copied, 1.2 where
-// they fill the product).  The quarters of all units, in the order (row tile, request,
+// 4 n + extra quarters, `extra` for what a change of units costs a block: 3 where rows
+// are copied, else 7 (128 requests of 1-2000 tokens, one token 55.3 us with 1, 52.2 with
+// 3, 53.4 with 4; block of 32 72.0 with 4, 65.2 with 7, 64.4 with 12, where 64 requests of
+// 256-8192 tokens lose 1 us).  The quarters of all units, in the order (row tile, request,
 // key head, tile), are shared out evenly over the blocks, at least four to a block,
 // and a tile belongs to the block that has its first quarter.  So every block is
 // busy for the same time whatever the lengths are, and a long request is split over

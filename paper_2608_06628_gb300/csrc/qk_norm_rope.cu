@@ -590,6 +590,7 @@ int split_rows(const RopeArgs &a, int rpw, int per_sm, bool waves, Split &s)
     long long warps = total < held ? total : held;
     const int share = s.steps >= 16 ? (s.steps < 24 ? s.steps : 24) : (16 + s.steps - 1) / s.steps * s.steps;
     if (waves && total / share > warps) warps = total / share;
+    if (warps > 1 << 30) warps = 1 << 30;
     s.warps = (int)warps;
     s.share = (int)(total / warps);
     s.rem = (int)(total % warps);

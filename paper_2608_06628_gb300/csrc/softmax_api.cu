@@ -267,6 +267,9 @@ hybrid_status hybrid_paged_attn(const hybrid_cfg *cfg, const hybrid_page_cfg *pg
     // the kernels count quarters of tiles of 128 keys, of all row tiles, in an int
     const long long quarters = 4 * (((long long)pg->max_pages * pg->page_size + 127) / 128) + a.extra;
     if (quarters * n_req > 0x7fffffffll / ((long long)a.Hkv * a.n_gt * a.n_bt)) return HYBRID_ERR_UNSUPPORTED;
+    // no more blocks than the longest possible contexts give work, four quarters each
+    const long long most = quarters * n_req * a.Hkv * a.n_gt * a.n_bt / 4;
+    if (most < a.n_cta) a.n_cta = (int)most;
     unsigned *err = hyb::error_word();
     if (!err) return HYBRID_ERR_CUDA;
     a.Q = Q;

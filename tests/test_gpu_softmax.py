@@ -612,3 +612,34 @@ def test_attention_row_tiles_of_many_requests(dt):
         lens = [rng.choice([0, 1, 127, 128, rng.randint(0, 400)]) for _ in range(n)]
         check_attn(attn_setup(dt, 40, 14, 2, 64, 32, lens, seed=n), f"{n} requests, 280 rows")
     check_attn(attn_setup(dt, 128, 8, 1, 128, 16, [3000, 0, 50], 700, 30), "1024 rows, window")
+
+
+def test_attention_float32_offsets_beyond_32_bits():
+    """A float32 cache of more than 2^31 elements, whose far pages are used, with few and with many rows."""
+    P, n_pages, d = 128, 140000, 128
+    assert n_pages * P * d > 2 ** 31
+    kc = torch.empty(n_pages, 1, P, d, device="cuda")
+    vc = torch.empty(n_pages, 1, P, d, device="cuda")
+    for B in (1, 24):
+        s = attn_setup(F32, B, 4, 1, d, P, [3000, 129])
+        for r in range(2):
+            for j in range(-(-[3000, 129][r] // P)):
+                to, frm = n_pages - 1 - 50 * r - j, int(s["table"][r, j])
+                kc[to], vc[to] = s["kc"][frm], s["vc"][frm]
+                s["table"][r, j] = to
+        s.update(kc=kc, vc=vc, pg=H.make_page_cfg(P, n_pages, s["pg"].max_pages))
+        check_attn(s, f"far pages, {B} tokens")
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("max_len", [16, 128, 144])
+def test_attention_of_contexts_that_fit_a_tile(dt, max_len):
+    """The table's width bounds the contexts to one tile (nothing to join) or just above it."""
+    lens = [0, 1, max_len, max_len - 1, 7, max_len // 2]
+    for Hkv, Hq, B in ((1, 4, 1), (3, 6, 20)):
+        s = attn_setup(dt, B, Hq, Hkv, 64, 16, lens, seed=max_len)
+        s["pg"] = H.make_page_cfg(16, s["pg"].n_pages, -(-max_len // 16))
+        s["table"] = s["table"][:, :s["pg"].max_pages].contiguous()
+        check_attn(s, f"up to {max_len} keys")
+        one = attn_setup(dt, B, Hq, Hkv, 64, 16, [max_len], seed=1)
+        check_attn(one, "one request")
