@@ -189,9 +189,9 @@ hybrid_status hybrid_qk_norm_rope_backward(const hybrid_cfg *cfg, const hybrid_r
  * is then unspecified.
  *   workspace  16-byte aligned, >= hybrid_paged_attn_workspace_bytes; need not be
  *              initialised; calls that may overlap on the GPU need one each
- * n_req <= 65536, and n_req * (ceil(max_pages * page_size / 128) + 2) * Hkv * B < 2^29
- * (HYBRID_ERR_UNSUPPORTED above a limit; with blocks of several tokens the second one
- * lies higher). */
+ * n_req <= 65536, and n_req * (ceil(max_pages * page_size / 128) + 2) * Hkv * B *
+ * ceil(Hq / (8 Hkv)) < 2^29 (HYBRID_ERR_UNSUPPORTED above a limit; with several rows to
+ * a tile the second one lies higher). */
 size_t hybrid_paged_attn_workspace_bytes(const hybrid_cfg *cfg, const hybrid_page_cfg *pg, int n_req);
 hybrid_status hybrid_paged_attn(const hybrid_cfg *cfg, const hybrid_page_cfg *pg, const void *Q,
                                 const void *K_cache, const void *V_cache, const int *block_table,

@@ -10,8 +10,8 @@
 // (row pitch d + 4 floats: 16-byte reads of 8 keys do not collide) and a warp every
 // eighth row, so maximum, sum and probabilities of a row stay in one warp's
 // registers; for O a thread has 4 features of every (1024 / d)-th row.  16 rows to a
-// tile where a key head has no more (decoding: bound by memory), else 64, so that
-// each key read from shared memory meets 8 rows (bound by the FMA pipe).
+// tile where a key head has no more, else 64, so that each key read from shared memory
+// meets 8 rows (bound by the FMA pipe).  Up to 8 rows: paged_attn_few.cu.
 #include <type_traits>
 
 #include "paged_plan.cuh"
@@ -456,9 +456,7 @@ template <int D, int ROWS> cudaError_t launch_f32(const PagedArgs &a, cudaStream
     static std::atomic<unsigned long long> opted{0};
     cudaError_t e = pipe::opt_in(reinterpret_cast<const void *>(&k_paged_attn<D, ROWS>), (int)sizeof(S), opted);
     if (e != cudaSuccess) return e;
-    e = pipe::launch_early(k_paged_attn<D, ROWS>, dim3(a.n_cta), dim3(kThreads), sizeof(S), st, a, lg);
-    if (e != cudaSuccess) return e;
-    return launch_join<float>(a, st);
+    return pipe::launch_early(k_paged_attn<D, ROWS>, dim3(a.n_cta), dim3(kThreads), sizeof(S), st, a, lg);
 }
 
 template <int D> cudaError_t launch_f32(const PagedArgs &a, cudaStream_t st)
@@ -468,23 +466,36 @@ template <int D> cudaError_t launch_f32(const PagedArgs &a, cudaStream_t st)
 
 }  // namespace
 
+// Row tiles of at most `most` rows, of about equal size along the tokens.
+static void cut_rows(PagedArgs &a, int most)
+{
+    a.Gt = a.G < most ? a.G : most;
+    a.n_gt = (a.G + a.Gt - 1) / a.Gt;
+    a.Bt = most / a.Gt < a.B ? most / a.Gt : a.B;
+    a.n_bt = (a.B + a.Bt - 1) / a.Bt;
+    a.Bt = (a.B + a.n_bt - 1) / a.n_bt;
+}
+
 void paged_geometry(const hybrid_cfg &c, PagedArgs &a)
 {
     const bool tc = c.io_dtype == HYBRID_BF16;
-    const int group = c.n_q_heads / c.n_kv_heads * c.block_size;            // rows of a key head
-    const int max_rows = tc ? kMaxRows : (group <= kFewRows ? kFewRows : kManyRows);
     a.B = c.block_size;
     a.Hq = c.n_q_heads;
     a.Hkv = c.n_kv_heads;
     a.G = c.n_q_heads / c.n_kv_heads;
     a.d = c.head_dim;
-    a.Gt = a.G < max_rows ? a.G : max_rows;
-    a.n_gt = (a.G + a.Gt - 1) / a.Gt;
-    a.Bt = max_rows / a.Gt < a.B ? max_rows / a.Gt : a.B;
-    a.n_bt = (a.B + a.Bt - 1) / a.Bt;
-    a.Bt = (a.B + a.n_bt - 1) / a.n_bt;                                     // row tiles of about equal size
-    a.extra = tc && a.Bt * a.Gt <= 64 ? 3 : 7;
-    a.n_cta = (tc ? 1 : 2) * pipe::sm_count();
+    if (tc) {
+        cut_rows(a, kMaxRows);
+    } else {
+        // The kernel of paged_attn_few.cu also for two row tiles, but not for three: 64
+        // requests of 256-8192 tokens, 4 key heads, d = 128, 16 rows 425 us against 539
+        // here (d = 64 230 and 292), 15 rows as three times 5 628 against 548.
+        cut_rows(a, kFewestRows);
+        if (a.n_gt * a.n_bt > 2) cut_rows(a, a.G * a.B <= kFewRows ? kFewRows : kManyRows);
+    }
+    const int rows = a.Bt * a.Gt;
+    a.extra = tc && rows <= 64 ? 3 : 7;
+    a.n_cta = (tc || (rows > 4 && rows <= kFewestRows) ? 1 : 2) * pipe::sm_count();   // resident blocks
 }
 
 size_t paged_workspace_bytes(const PagedArgs &a)
@@ -500,10 +511,14 @@ void paged_set_workspace(PagedArgs &a, void *workspace)
 
 cudaError_t launch_paged_attn(hybrid_dtype dt, const PagedArgs &a, cudaStream_t st)
 {
-    if (dt == HYBRID_F32) return a.d == 128 ? launch_f32<128>(a, st) : launch_f32<64>(a, st);
-    const cudaError_t e = launch_paged_attn_tc(a, st);
+    const bool bf16 = dt == HYBRID_BF16;
+    const int rows = a.Bt * a.Gt;
+    cudaError_t e;
+    if (bf16) e = launch_paged_attn_tc(a, st);
+    else if (rows <= kFewestRows) e = launch_paged_attn_few(a, st);
+    else e = a.d == 128 ? launch_f32<128>(a, st) : launch_f32<64>(a, st);
     if (e != cudaSuccess) return e;
-    return launch_join<__nv_bfloat16>(a, st);
+    return bf16 ? launch_join<__nv_bfloat16>(a, st) : launch_join<float>(a, st);
 }
 
 }  // namespace hyb

@@ -643,3 +643,29 @@ def test_attention_of_contexts_that_fit_a_tile(dt, max_len):
         check_attn(s, f"up to {max_len} keys")
         one = attn_setup(dt, B, Hq, Hkv, 64, 16, [max_len], seed=1)
         check_attn(one, "one request")
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("B,G", [(1, 1), (3, 1), (1, 4), (1, 5), (7, 1), (2, 4), (1, 8), (9, 1), (3, 3), (1, 11), (5, 3), (4, 4), (1, 16),
+                                 (17, 1)])
+def test_attention_float32_few_rows(B, G, d):
+    """Row counts at which the float32 kernels and the row tiles change; masks of both kinds, requests that are split."""
+    for window, sink, scale in ((0, 0, 1.0), (300, 5, 4.0)):
+        s = attn_setup(F32, B, 3 * G, 3, d, 16, EDGES + [9000], window, sink, seed=B + 20 * G, k_scale=scale)
+        check_attn(s, f"{B} tokens, {G} heads to a key head, window {window}")
+
+
+@pytest.mark.parametrize("step", [0.0625, 1.0, 32.0])
+def test_attention_float32_rising_scores(step):
+    """Each key's score is above all before it, by less or by more than what moves the running maximum (8, in log2).
+
+    q = 8, k = j step / 512 in 64 features, both exact: q . k / 8 = j step / 8.  The largest score, in log2, is
+    200 * 4 * 1.4427 < 1155, rounded by at most 2^-14 of 1: 6e-5 * ln 2 of a weight, and the weights but the last are below
+    2% of it then; with the smaller steps the scores are below 37 and rounded by 2^-19."""
+    for B in (1, 2):
+        s = attn_setup(F32, B, 4, 1, 64, 128, [200, 129], seed=5)
+        for r, x in enumerate(s["lens"].tolist()):
+            j = torch.arange(x, device="cuda")
+            s["kc"][s["table"][r][j // 128].long(), 0, j % 128] = (j.float() * step / 512.0)[:, None].expand(x, 64)
+        s["q"][:] = 8.0
+        check_attn(s, f"rising by {step / 8}")
