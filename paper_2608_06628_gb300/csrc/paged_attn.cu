@@ -4,14 +4,20 @@
 // Per row: running maximum m, sum l and output O over the visible keys, in one
 // pass; scores are kept in units of log2, x = q . k log2(e) / sqrt(d).
 //
-// A block of 8 warps walks its share of the tiles (paged_plan.cuh) in chunks of 64
-// (d = 64) or 32 keys, copied by cp.async one or two chunks ahead, across requests; masked
-// keys are zero-filled, their pages not read.  For the scores a lane has its keys
-// (row pitch d + 4 floats: 16-byte reads of 8 keys do not collide) and a warp every
-// eighth row, so maximum, sum and probabilities of a row stay in one warp's
-// registers; for O a thread has 4 features of every (1024 / d)-th row.  16 rows to a
-// tile where a key head has no more, else 64, so that each key read from shared memory
-// meets 8 rows (bound by the FMA pipe).  Up to 8 rows: paged_attn_few.cu.
+// A block of 8 warps takes the tiles of its share (paged_plan.cuh) one after another,
+// 64 rows x 128 keys.  For the scores a thread has 8 rows x 4 keys (12 16-byte reads of
+// shared memory for 64 packed FMAs), for O 4 rows x 8 features (the same), with all
+// keys at d = 128 and every second 64 of them at d = 64, added at a segment's end.  K, V
+// and P have one buffer each: K of the next tile comes while P V is computed, V while
+// the scores are; masked keys are zero-filled, their pages not read.  A row's
+// maximum is moved only when a score exceeds it by more than 8, which the block votes
+// on, so that a tile takes three barriers and no reduction; sums are added over the
+// threads at a segment's end.  Row tiles of up to 8 rows: paged_attn_few.cu.
+//
+// Bound by reads of shared memory and the FMA pipe in turn (58% and 57% of their peaks):
+// 64 requests of 256-8192 tokens, blocks of 32, 16 query and 4 key heads, d = 128
+// 1610 us (44 TFLOP/s), d = 64 909 us; with 8 rows x 2 keys and 4 x 4 to a thread,
+// and a maximum of each row found for each tile, 2440 us.
 #include <type_traits>
 
 #include "paged_plan.cuh"
@@ -22,99 +28,49 @@ namespace {
 
 using namespace paged;
 using ptx::f32x2;
+using ptx::pair2;
 
 constexpr int kThreads = 256;
-constexpr int kWarps = kThreads / 32;
-constexpr int kFewRows = 16, kManyRows = 64;    // rows of a tile
+constexpr int kRows = 64;                       // rows of a tile
+constexpr int kPitchP = kTile + 8;              // 4 rows x 8 keys written by a warp meet 32 banks
+constexpr float kSlack = 8.f;
 
-__device__ __forceinline__ float4 load4(const float *p) { return *reinterpret_cast<const float4 *>(p); }
 template <typename T> __device__ __forceinline__ void store4(T *p, float4 v);
 template <> __device__ __forceinline__ void store4<float>(float *p, float4 v) { *reinterpret_cast<float4 *>(p) = v; }
 template <> __device__ __forceinline__ void store4<__nv_bfloat16>(__nv_bfloat16 *p, float4 v)
 {
     *reinterpret_cast<uint2 *>(p) = make_uint2(pipe::pack_bf16x2(v.x, v.y), pipe::pack_bf16x2(v.z, v.w));
 }
-// 16 bytes of shared memory as two pairs
-__device__ __forceinline__ void load_pairs(const float *p, f32x2 &a, f32x2 &b)
-{
-    const ulonglong2 v = *reinterpret_cast<const ulonglong2 *>(p);
-    a.v = v.x;
-    b.v = v.y;
-}
 
-// 16 bytes to shared memory, `bytes` of them read and the rest zeros
-__device__ __forceinline__ void copy16(uint32_t dst, const float *src, int bytes)
-{
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
-}
-
-template <int D, int ROWS> struct Smem {
-    static constexpr int kKeys = D == 64 ? 64 : 32;
-    static constexpr int kStages = ROWS == kFewRows ? 3 : 2;   // chunks in place or on their way
-    float q[ROWS][D];
-    struct {
-        float k[kKeys][D + 4];
-        float v[kKeys][D];
-    } chunk[kStages];
-    float p[ROWS][kKeys];
-    float m[ROWS], l[ROWS], scale[ROWS];
+template <int D> struct Smem {
+    static constexpr int kPitch = D + 4;        // 16-byte reads of 8 keys, or 4 rows, meet 32 banks
+    float q[kRows][kPitch];
+    float k[kTile][kPitch];
+    float v[kTile][D];
+    float p[kRows][kPitchP];
+    float sum[kRows][4], top[kRows][4];         // of a row, by the warps that share it
+    float m[kRows], scale[kRows];
     PlanSmem plan;
 };
 
-// The chunks of a block's share, those without a visible key left out.
-template <int KEYS> struct Chunks {
-    Walk w;
-    int i, j0;             // tile of the segment, first key
-    bool live;
-
-    __device__ void begin(const PagedArgs &a, const Walk &walk)
-    {
-        w = walk;
-        live = w.next(a);
-        if (!live) return;
-        i = w.i0;
-        j0 = key_tile(w.vis, i) * kTile;
-        skip(a);
-    }
-    // Advance; true if the chunk is the first of a segment.
-    __device__ bool step(const PagedArgs &a)
-    {
-        j0 += KEYS;
-        return skip(a);
-    }
-    __device__ bool skip(const PagedArgs &a)
-    {
-        bool first = false;
-        while (true) {
-            if (j0 < (key_tile(w.vis, i) + 1) * kTile) {
-                if (any_visible(w.vis, j0, KEYS)) return first;
-                j0 += KEYS;
-                continue;
-            }
-            if (++i == w.i1) {
-                first = true;
-                live = w.next(a);
-                if (!live) return first;
-                i = w.i0;
-            }
-            j0 = key_tile(w.vis, i) * kTile;
-        }
-    }
-};
-
-template <int D, int ROWS>
-__global__ __launch_bounds__(kThreads, 2) void k_paged_attn(const PagedArgs a, int page_lg)
+template <int D> __global__ __launch_bounds__(kThreads, 1) void k_paged_attn(const PagedArgs a, int page_lg)
 {
-    using S = Smem<D, ROWS>;
-    constexpr int KEYS = S::kKeys, KL = KEYS / 32, RW = ROWS / kWarps;      // keys of a lane, rows of a warp
-    constexpr int kCols = D / 4, kRowStep = kThreads / kCols;               // O: threads per row, rows at a time
-    constexpr int kOwn = ROWS / kRowStep;                                   // rows of a thread
-    constexpr int kCopies = KEYS * kCols / kThreads;                        // 16-byte copies of K per thread
+    using S = Smem<D>;
+    constexpr int kCols = D / 4, kKeyStep = 32 / kCols;     // copies of a warp: 16 bytes of kKeyStep keys at a time
+    constexpr int kOwnKeys = kTile / 8;                     // keys that a warp copies, side by side: of one page
     extern __shared__ __align__(16) unsigned char raw[];
     S &s = *reinterpret_cast<S *>(raw);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int rows = a.Bt * a.Gt;
     const float to_log2 = pipe::kLog2e * rsqrtf((float)D);
+
+    // scores: rows row_s + 8 y, keys key_s + 8 x
+    const int row_s = lane / 8 + 4 * (warp & 1), key_s = lane % 8 + 32 * (warp >> 1);
+    // outputs: rows row_o + 16 y, features col_o + 32 x + (0 ... 3); half of the keys (d = 64)
+    const int row_o = lane / 8 + 4 * (warp & 3), half = warp >> 2;
+    const int col_o = lane % 8 * 4 + (D == 128 ? 64 * half : 0);
+    constexpr int kKeysO = D == 128 ? kTile : kTile / 2;
+    const int key_o = D == 128 ? 0 : half * kKeysO;
 
     ptx::griddep_wait();
     ptx::griddep_launch_dependents();
@@ -122,210 +78,271 @@ __global__ __launch_bounds__(kThreads, 2) void k_paged_attn(const PagedArgs a, i
     Shares sh(0, 1);
     const bool work = find_share<kThreads>(a, s.plan, w, sh);
     if (work) {
-        const int col = tid % kCols * 4, row0 = tid / kCols;
-        Chunks<KEYS> at, ahead;
-        at.begin(a, w);
-        ahead = at;
-        auto issue = [&](int b) {
-            if (ahead.live) {
-                const int *pages = a.table + (size_t)ahead.w.req * a.max_pages;
-                // this thread's 16 bytes of a key in the cache, from its page
-                auto in_cache = [&](int j) {
-                    int page = __ldg(pages + (j >> page_lg));
-                    if (page < 0 || page >= a.n_pages) {
-                        raise_error(a.err, ERR_BAD_INDEX);
-                        page = 0;
-                    }
-                    return ((((size_t)page * a.Hkv + ahead.w.head) << page_lg) + (j & ((1 << page_lg) - 1))) * D + col;
-                };
-                const uint32_t to_k = ptx::smem_u32(&s.chunk[b].k[row0][col]), to_v = ptx::smem_u32(&s.chunk[b].v[row0][col]);
-                if (ahead.j0 >= ahead.w.vis.lo && ahead.j0 + KEYS <= ahead.w.vis.len) {
-                    // all keys visible: a page is looked up once for 16 keys in a row
-                    constexpr int kRun = 16 / kRowStep > 1 ? 16 / kRowStep : 1;
+        // the tile to copy next: segment and tile, and this warp's page
+        Walk ahead = w;
+        int i = 0, page = 0;
+        bool more = ahead.next(a);
+        i = ahead.i0;
+        auto look_up = [&]() {                              // the page of this warp's keys
+            const int j = key_tile(ahead.vis, i) * kTile + warp * kOwnKeys;
+            page = 0;
+            if (more && any_visible(ahead.vis, j, kOwnKeys))
+                page = __ldg(a.table + (size_t)ahead.req * a.max_pages + (j >> page_lg));
+        };
+        auto copy_q = [&]() {
+            const Unit u = unit_of(a, ahead.head, ahead.rt);
+            for (int x = tid; x < kRows * kCols; x += kThreads) {
+                const int rho = x / kCols, c = x % kCols * 4;
+                size_t from;
+                const bool live = row_at(a, ahead.req, u, rho, from);
+                copy16(&s.q[rho][c], static_cast<const float *>(a.Q) + (live ? from + c : 0), live ? 16 : 0);
+            }
+        };
+        // this warp's keys of a tile to shared memory
+        auto copy_tile = [&](const Visible &vis, int tile, size_t from, const void *cache, float *to, int pitch) {
+            const int j0 = key_tile(vis, tile) * kTile + warp * kOwnKeys + lane / kCols, c = lane % kCols * 4;
+            const float *src = static_cast<const float *>(cache) + from + c;
+            float *dst = to + (size_t)(warp * kOwnKeys + lane / kCols) * pitch + c;
+            const int in_page = j0 & ((1 << page_lg) - 1);
 #pragma unroll
-                    for (int x = 0; x < kCopies; x += kRun) {
-                        const size_t from = in_cache(ahead.j0 + row0 + x * kRowStep);
+            for (int x = 0; x < kOwnKeys; x += kKeyStep) {
+                const bool see = key_visible(vis, j0 + x);
+                copy16(dst + x * pitch, see ? src + (in_page + x) * D : static_cast<const float *>(cache), see ? 16 : 0);
+            }
+        };
+        auto from_page = [&]() {
+            if (page < 0 || page >= a.n_pages) {
+                raise_error(a.err, ERR_BAD_INDEX);
+                page = 0;
+            }
+            return (((size_t)page * a.Hkv + ahead.head) << page_lg) * D;
+        };
+        auto commit = [&]() { asm volatile("cp.async.commit_group;" ::: "memory"); };
+
+        size_t from = 0;
+        Visible vis_v{};                                    // of the tile whose values are to be copied
+        int i_v = 0;
+        look_up();
+        if (more) {
+            from = from_page();
+            copy_q();
+            copy_tile(ahead.vis, i, from, a.K, &s.k[0][0], S::kPitch);
+            commit();
+            copy_tile(ahead.vis, i, from, a.V, &s.v[0][0], D);
+        }
+        commit();
+        asm volatile("cp.async.wait_group 1;" ::: "memory");
+        __syncthreads();
+        while (w.next(a)) {
+            const Unit u = unit_of(a, w.head, w.rt);
+            float m[8], l[8];                               // of this thread's rows; its own keys' sum
+            f32x2 o[4][4];
 #pragma unroll
-                        for (int y = 0; y < kRun; ++y) {
-                            copy16(to_k + (x + y) * kRowStep * (D + 4) * 4,
-                                   static_cast<const float *>(a.K) + from + y * kRowStep * D, 16);
-                            copy16(to_v + (x + y) * kRowStep * D * 4,
-                                   static_cast<const float *>(a.V) + from + y * kRowStep * D, 16);
+            for (int y = 0; y < 8; ++y) {
+                m[y] = -INFINITY;
+                l[y] = 0.f;
+            }
+#pragma unroll
+            for (int y = 0; y < 4; ++y)
+#pragma unroll
+                for (int x = 0; x < 4; ++x) o[y][x] = pair2(0.f, 0.f);
+            for (int tile = w.i0; tile < w.i1; ++tile) {
+                // the next tile to copy
+                bool segment = false;
+                if (++i >= ahead.i1) {
+                    more = ahead.next(a);
+                    segment = more;
+                    i = ahead.i0;
+                }
+                look_up();
+                float x[8][4];
+                {
+                    f32x2 acc[8][4];
+#pragma unroll
+                    for (int y = 0; y < 8; ++y)
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) acc[y][k] = pair2(0.f, 0.f);
+                    auto products = [&](auto full) {
+#pragma unroll 2
+                        for (int c = 0; c < D; c += 4) {
+                            f32x2 k0[4], k1[4];
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) load_pairs(&s.k[key_s + 8 * k][c], k0[k], k1[k]);
+#pragma unroll
+                            for (int y = 0; y < 8; ++y) {
+                                if (!full && 8 * y >= rows) break;
+                                f32x2 q0, q1;
+                                load_pairs(&s.q[row_s + 8 * y][c], q0, q1);
+#pragma unroll
+                                for (int k = 0; k < 4; ++k)
+                                    acc[y][k] = ptx::fma2(k1[k], q1, ptx::fma2(k0[k], q0, acc[y][k]));
+                            }
+                        }
+                    };
+                    // (a full tile without the checks of each row)
+                    if (rows > kRows - 8) products(std::true_type{});
+                    else products(std::false_type{});
+                    const int j = key_tile(w.vis, tile) * kTile + key_s;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const bool see = key_visible(w.vis, j + 8 * k);
+#pragma unroll
+                        for (int y = 0; y < 8; ++y) {
+                            float lo, hi;
+                            ptx::unpair2(acc[y][k], lo, hi);
+                            x[y][k] = see ? (lo + hi) * to_log2 : -INFINITY;
                         }
                     }
-                } else {
-#pragma unroll 1
-                    for (int x = 0; x < kCopies; ++x) {
-                        const int j = ahead.j0 + row0 + x * kRowStep;
-                        const bool see = key_visible(ahead.w.vis, j);
-                        const size_t from = see ? in_cache(j) : 0;
-                        const int bytes = see ? 16 : 0;      // masked keys are zero-filled
-                        copy16(to_k + x * kRowStep * (D + 4) * 4, static_cast<const float *>(a.K) + from, bytes);
-                        copy16(to_v + x * kRowStep * D * 4, static_cast<const float *>(a.V) + from, bytes);
+                }
+                bool above = false;
+#pragma unroll
+                for (int y = 0; y < 8; ++y)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) above |= x[y][k] > m[y] + kSlack;
+                const bool moved = __syncthreads_or(above);     // also: K and Q have been read
+                vis_v = ahead.vis;
+                i_v = i;
+                if (more) {
+                    from = from_page();
+                    if (segment) copy_q();
+                    copy_tile(vis_v, i_v, from, a.K, &s.k[0][0], S::kPitch);
+                }
+                commit();
+                if (moved) {
+#pragma unroll
+                    for (int y = 0; y < 8; ++y) {
+                        float t = fmaxf(fmaxf(x[y][0], x[y][1]), fmaxf(x[y][2], x[y][3]));
+#pragma unroll
+                        for (int f = 4; f > 0; f >>= 1) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, f));
+                        if (lane % 8 == 0) s.top[row_s + 8 * y][warp >> 1] = t;
+                    }
+                    __syncthreads();
+#pragma unroll
+                    for (int y = 0; y < 8; ++y) {
+                        const float4 t = *reinterpret_cast<const float4 *>(s.top[row_s + 8 * y]);
+                        const float all = fmaxf(fmaxf(t.x, t.y), fmaxf(t.z, t.w));
+                        const float now = all > m[y] + kSlack ? all : m[y];
+                        const float f = m[y] == -INFINITY ? 1.f : exp2f(m[y] - now);    // (l and O are zero, or NaN)
+                        m[y] = now;
+                        l[y] *= f;
+                        if (lane % 8 == 0 && warp < 2) s.scale[row_s + 8 * y] = f;
                     }
                 }
-                ahead.step(a);
-            }
-            asm volatile("cp.async.commit_group;" ::: "memory");
-        };
-        constexpr int kAhead = S::kStages - 1;
 #pragma unroll
-        for (int x = 0; x < kAhead; ++x) issue(x);
-        bool first = true;
-        float m[RW], l[RW];                                  // of rows warp + 8 y
-        float4 o[kOwn];                                      // features col ... of rows row0 + y kRowStep
-        Unit u{};
-        for (int b = 0; at.live; b = b + 1 == S::kStages ? 0 : b + 1) {
-            const int req = at.w.req;
-            issue(b == 0 ? kAhead : b - 1);
-            if (first) {
-                u = unit_of(a, at.w.head, at.w.rt);
-                for (int x = tid; x < rows * kCols; x += kThreads) {
-                    const int rho = x / kCols, c = x % kCols * 4;
-                    size_t from;
-                    const bool live = row_at(a, req, u, rho, from);
-                    *reinterpret_cast<float4 *>(&s.q[rho][c]) =
-                        live ? load4(static_cast<const float *>(a.Q) + from + c) : make_float4(0.f, 0.f, 0.f, 0.f);
+                for (int y = 0; y < 8; ++y) {
+                    const float base = m[y] == -INFINITY ? 0.f : m[y];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const float p = exp2f(x[y][k] - base);
+                        l[y] += p;
+                        s.p[row_s + 8 * y][key_s + 8 * k] = p;
+                    }
                 }
+                asm volatile("cp.async.wait_group 1;" ::: "memory");
+                __syncthreads();                            // P and V are in place
+                if (moved) {
 #pragma unroll
-                for (int y = 0; y < RW; ++y) {
-                    m[y] = -INFINITY;
-                    l[y] = 0.f;
+                    for (int y = 0; y < 4; ++y) {
+                        const float f = s.scale[row_o + 16 * y];
+                        const f32x2 ff = pair2(f, f);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) o[y][e] = ptx::mul2(o[y][e], ff);
+                    }
                 }
-#pragma unroll
-                for (int y = 0; y < kOwn; ++y) o[y] = make_float4(0.f, 0.f, 0.f, 0.f);
-            }
-            asm volatile("cp.async.wait_group %0;" ::"n"(kAhead) : "memory");
-            __syncthreads();
-            {   // scores of keys lane, lane + 32 with rows warp, warp + 8, ...
-                f32x2 acc[KL][RW];
-#pragma unroll
-                for (int x = 0; x < KL; ++x)
-#pragma unroll
-                    for (int y = 0; y < RW; ++y) acc[x][y] = ptx::pair2(0.f, 0.f);
                 auto products = [&](auto full) {
 #pragma unroll 4
-                    for (int c = 0; c < D; c += 4) {
-                        f32x2 k0[KL], k1[KL];
+                    for (int r = 0; r < kKeysO; r += 4) {
+                        f32x2 v[4][4];
 #pragma unroll
-                        for (int x = 0; x < KL; ++x) load_pairs(&s.chunk[b].k[lane + 32 * x][c], k0[x], k1[x]);
-#pragma unroll
-                        for (int y = 0; y < RW; ++y) {
-                            if (!full && warp + 8 * y >= rows) break;
-                            f32x2 q0, q1;
-                            load_pairs(&s.q[warp + 8 * y][c], q0, q1);
-#pragma unroll
-                            for (int x = 0; x < KL; ++x)
-                                acc[x][y] = ptx::fma2(k1[x], q1, ptx::fma2(k0[x], q0, acc[x][y]));
+                        for (int k = 0; k < 4; ++k) {
+                            const float *at = &s.v[key_o + r + k][col_o];
+                            load_pairs(at, v[k][0], v[k][1]);
+                            load_pairs(at + 32, v[k][2], v[k][3]);
                         }
-                    }
-                };
-                // (a full tile without the checks of each row)
-                if (rows == ROWS) products(std::true_type{});
-                else if (warp < rows) products(std::false_type{});
-                bool see[KL];
 #pragma unroll
-                for (int x = 0; x < KL; ++x) see[x] = key_visible(at.w.vis, at.j0 + lane + 32 * x);
-#pragma unroll
-                for (int y = 0; y < RW; ++y) {
-                    const int rho = warp + 8 * y;
-                    if (rho >= rows) break;
-                    float x[KL], mx = -INFINITY, sum = 0.f;
-#pragma unroll
-                    for (int k = 0; k < KL; ++k) {
-                        float lo, hi;
-                        ptx::unpair2(acc[k][y], lo, hi);
-                        x[k] = see[k] ? (lo + hi) * to_log2 : -INFINITY;
-                        mx = fmaxf(mx, x[k]);
-                    }
-                    const float now = fmaxf(m[y], warp_max(mx)), base = now == -INFINITY ? 0.f : now;
-#pragma unroll
-                    for (int k = 0; k < KL; ++k) {
-                        const float p = exp2f(x[k] - base);
-                        s.p[rho][lane + 32 * k] = p;
-                        sum += p;
-                    }
-                    const float f = exp2f(m[y] - base);
-                    l[y] = l[y] * f + warp_sum(sum);
-                    m[y] = now;
-                    if (lane == 0) {
-                        s.scale[rho] = f;
-                        s.m[rho] = now;
-                        s.l[rho] = l[y];
-                    }
-                }
-            }
-            __syncthreads();
-            {   // O <- O scale + P V
-                f32x2 acc[kOwn][2];
-#pragma unroll
-                for (int y = 0; y < kOwn; ++y) {
-                    const int rho = row0 + y * kRowStep;
-                    const float f = rho < rows ? s.scale[rho] : 0.f;
-                    acc[y][0] = ptx::pair2(o[y].x * f, o[y].y * f);
-                    acc[y][1] = ptx::pair2(o[y].z * f, o[y].w * f);
-                }
-                auto products = [&](auto full) {
-#pragma unroll 2
-                    for (int r = 0; r < KEYS; r += 4) {
-                        f32x2 v[4][2];
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) load_pairs(&s.chunk[b].v[r + k][col], v[k][0], v[k][1]);
-#pragma unroll
-                        for (int y = 0; y < kOwn; ++y) {
-                            const int rho = row0 + y * kRowStep;
-                            if (!full && y > 0 && rho >= rows) break;
-                            const float4 p4 = load4(&s.p[rho][r]);
+                        for (int y = 0; y < 4; ++y) {
+                            if (!full && 16 * y >= rows) break;
+                            const float4 p4 = *reinterpret_cast<const float4 *>(&s.p[row_o + 16 * y][key_o + r]);
                             const float p[4] = {p4.x, p4.y, p4.z, p4.w};
 #pragma unroll
                             for (int k = 0; k < 4; ++k) {
-                                const f32x2 pp = ptx::pair2(p[k], p[k]);
-                                acc[y][0] = ptx::fma2(pp, v[k][0], acc[y][0]);
-                                acc[y][1] = ptx::fma2(pp, v[k][1], acc[y][1]);
+                                const f32x2 pp = pair2(p[k], p[k]);
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) o[y][e] = ptx::fma2(pp, v[k][e], o[y][e]);
                             }
                         }
                     }
                 };
-                if (rows == ROWS) products(std::true_type{});
-                else if (row0 < rows) products(std::false_type{});
+                if (rows > kRows - 16) products(std::true_type{});
+                else products(std::false_type{});
+                asm volatile("cp.async.wait_group 0;" ::: "memory");
+                __syncthreads();                            // the next K and Q are in place, V and P have been read
+                if (more) copy_tile(vis_v, i_v, from, a.V, &s.v[0][0], D);
+                commit();
+            }
+            // the segment's output
 #pragma unroll
-                for (int y = 0; y < kOwn; ++y) {
-                    ptx::unpair2(acc[y][0], o[y].x, o[y].y);
-                    ptx::unpair2(acc[y][1], o[y].z, o[y].w);
+            for (int y = 0; y < 8; ++y) {
+#pragma unroll
+                for (int f = 4; f > 0; f >>= 1) l[y] += __shfl_xor_sync(0xffffffffu, l[y], f);
+                if (lane % 8 == 0) {
+                    s.sum[row_s + 8 * y][warp >> 1] = l[y];
+                    if (warp < 2) s.m[row_s + 8 * y] = m[y];
                 }
             }
-            const Walk here = at.w;
-            first = at.step(a);
-            if (first) {                                     // the segment's output
-                const bool whole = here.whole();
-                float *part = a.part + here.slot() * partial_floats(rows, D);
+            if (D == 64 && half == 1) {
 #pragma unroll
-                for (int y = 0; y < kOwn; ++y) {
-                    const int rho = row0 + y * kRowStep;
+                for (int y = 0; y < 4; ++y)
+#pragma unroll
+                    for (int e = 0; e < 4; e += 2) {
+                        ulonglong2 t;
+                        t.x = o[y][e].v;
+                        t.y = o[y][e + 1].v;
+                        *reinterpret_cast<ulonglong2 *>(&s.p[row_o + 16 * y][col_o + 16 * e]) = t;
+                    }
+            }
+            __syncthreads();
+            if (D == 128 || half == 0) {
+                const bool whole = w.whole();
+                float *part = a.part + w.slot() * partial_floats(rows, D);
+#pragma unroll
+                for (int y = 0; y < 4; ++y) {
+                    const int rho = row_o + 16 * y;
                     if (rho >= rows) break;
+                    const float4 t = *reinterpret_cast<const float4 *>(s.sum[rho]);
+                    const float sum = (t.x + t.y) + (t.z + t.w), f = 1.f / sum;
                     size_t to;
-                    const bool live = row_at(a, req, u, rho, to);
-                    const float4 c = o[y];
-                    if (whole) {
-                        const float f = 1.f / s.l[rho];
-                        if (live)
-                            store4(static_cast<float *>(a.O) + to + col, make_float4(c.x * f, c.y * f, c.z * f, c.w * f));
-                    } else {
-                        float *out = part + 2 * rows + (size_t)col * rows + rho;
-                        out[0] = c.x;
-                        out[rows] = c.y;
-                        out[2 * rows] = c.z;
-                        out[3 * rows] = c.w;
-                        if (col == 0) {
-                            part[rho] = s.m[rho];
-                            part[rows + rho] = s.l[rho];
+                    const bool live = row_at(a, w.req, u, rho, to);
+#pragma unroll
+                    for (int e = 0; e < 4; e += 2) {
+                        const int col = col_o + 16 * e;
+                        if (D == 64) {
+                            f32x2 b0, b1;
+                            load_pairs(&s.p[rho][col], b0, b1);
+                            o[y][e] = ptx::add2(o[y][e], b0);
+                            o[y][e + 1] = ptx::add2(o[y][e + 1], b1);
                         }
+                        float4 c;
+                        ptx::unpair2(o[y][e], c.x, c.y);
+                        ptx::unpair2(o[y][e + 1], c.z, c.w);
+                        if (whole) {
+                            if (live)
+                                store4(static_cast<float *>(a.O) + to + col, make_float4(c.x * f, c.y * f, c.z * f, c.w * f));
+                        } else {
+                            float *out = part + 2 * rows + (size_t)col * rows + rho;
+                            out[0] = c.x;
+                            out[rows] = c.y;
+                            out[2 * rows] = c.z;
+                            out[3 * rows] = c.w;
+                        }
+                    }
+                    if (!whole && col_o == 0) {
+                        part[rho] = s.m[rho];
+                        part[rows + rho] = sum;
                     }
                 }
             }
-            __syncthreads();                                 // the chunk, Q and P may be overwritten
         }
-        w = at.w;
     }
     if (tid == 0) write_note(a, work, w, sh);
     write_empty<float, kThreads>(a, tid);
@@ -447,21 +464,14 @@ template <typename T> cudaError_t launch_join(const PagedArgs &a, cudaStream_t s
     return pipe::launch_early(k_paged_join<T, 16, kMaxRows>, dim3(a.n_cta, a.d / 16), dim3(kThreads), 0, st, a);
 }
 
-template <int D, int ROWS> cudaError_t launch_f32(const PagedArgs &a, cudaStream_t st)
+template <int D> cudaError_t launch_f32(const PagedArgs &a, cudaStream_t st)
 {
-    using S = Smem<D, ROWS>;
-    static_assert(sizeof(S) < 113 * 1024, "two blocks per multiprocessor");
     int lg = 4;
     while ((1 << lg) < a.page_size) ++lg;
     static std::atomic<unsigned long long> opted{0};
-    cudaError_t e = pipe::opt_in(reinterpret_cast<const void *>(&k_paged_attn<D, ROWS>), (int)sizeof(S), opted);
+    const cudaError_t e = pipe::opt_in(reinterpret_cast<const void *>(&k_paged_attn<D>), (int)sizeof(Smem<D>), opted);
     if (e != cudaSuccess) return e;
-    return pipe::launch_early(k_paged_attn<D, ROWS>, dim3(a.n_cta), dim3(kThreads), sizeof(S), st, a, lg);
-}
-
-template <int D> cudaError_t launch_f32(const PagedArgs &a, cudaStream_t st)
-{
-    return a.Bt * a.Gt <= kFewRows ? launch_f32<D, kFewRows>(a, st) : launch_f32<D, kManyRows>(a, st);
+    return pipe::launch_early(k_paged_attn<D>, dim3(a.n_cta), dim3(kThreads), sizeof(Smem<D>), st, a, lg);
 }
 
 }  // namespace
@@ -487,15 +497,17 @@ void paged_geometry(const hybrid_cfg &c, PagedArgs &a)
     if (tc) {
         cut_rows(a, kMaxRows);
     } else {
-        // The kernel of paged_attn_few.cu also for two row tiles, but not for three: 64
-        // requests of 256-8192 tokens, 4 key heads, d = 128, 16 rows 425 us against 539
-        // here (d = 64 230 and 292), 15 rows as three times 5 628 against 548.
+        // The kernel of paged_attn_few.cu also for a few row tiles, if they are about full:
+        // 64 requests of 256-8192 tokens, 4 key heads, d = 128, two tiles of 8 rows 426 us
+        // against 580 here, three 630 and 724, four 825 and 798, but one request of 777
+        // tokens 12.4 and 24.0; three tiles of 5 rows 628 and 580.
         cut_rows(a, kFewestRows);
-        if (a.n_gt * a.n_bt > 2) cut_rows(a, a.G * a.B <= kFewRows ? kFewRows : kManyRows);
+        const int tiles = a.n_gt * a.n_bt;
+        if (tiles > 4 || (tiles > 2 && a.G * a.B < 6 * tiles)) cut_rows(a, kRows);
     }
     const int rows = a.Bt * a.Gt;
     a.extra = tc && rows <= 64 ? 3 : 7;
-    a.n_cta = (tc || (rows > 4 && rows <= kFewestRows) ? 1 : 2) * pipe::sm_count();   // resident blocks
+    a.n_cta = (tc || rows > 4 ? 1 : 2) * pipe::sm_count();   // resident blocks
 }
 
 size_t paged_workspace_bytes(const PagedArgs &a)

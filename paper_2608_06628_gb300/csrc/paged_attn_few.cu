@@ -14,9 +14,9 @@
 // what it alone reads (cp.async, kStages - 1 steps ahead), so the loop has no barrier.
 //
 // Bound by memory with 4 rows: 64 requests of 256-8192 tokens, 4 key heads, d = 128
-// 176 us (6.3 TB/s), d = 64 92 us, where the chunks of paged_attn.cu, with two barriers
-// each and scores through shared memory, take 297 us.  With 8 rows the queries and
-// outputs fill 128 registers: one block to a multiprocessor, 223 us (paged_attn.cu 463).
+// 176 us (6.3 TB/s), d = 64 92 us, where a version with chunks of 32 or 64 keys, two barriers
+// each and scores through shared memory took 297 us.  With 8 rows the queries and
+// outputs fill 128 registers: one block to a multiprocessor, 223 us (that version 463).
 #include "paged_plan.cuh"
 #include "tc_pipeline.cuh"
 
@@ -40,18 +40,6 @@ template <int D, int R> struct Smem {
     float m[kWarps][R], l[kWarps][R];
     PlanSmem plan;
 };
-
-__device__ __forceinline__ void copy16(float4 *dst, const float *src, int bytes)
-{
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(ptx::smem_u32(dst)), "l"(src), "r"(bytes)
-                 : "memory");
-}
-__device__ __forceinline__ void load_pairs(const float4 *p, f32x2 &a, f32x2 &b)
-{
-    const ulonglong2 v = *reinterpret_cast<const ulonglong2 *>(p);
-    a.v = v.x;
-    b.v = v.y;
-}
 
 template <int D, int R>
 __global__ __launch_bounds__(kThreads, R == 4 ? 2 : 1) void k_paged_attn_few(const PagedArgs a, int page_lg)
@@ -132,8 +120,8 @@ __global__ __launch_bounds__(kThreads, R == 4 ? 2 : 1) void k_paged_attn_few(con
             for (int c = 0; c < 4; ++c) q[y][c] = o[y][c] = pair2(0.f, 0.f);
             if (live) {
                 const float *row = static_cast<const float *>(a.Q) + from + 4 * sub;
-                load_pairs(reinterpret_cast<const float4 *>(row), q[y][0], q[y][1]);
-                load_pairs(reinterpret_cast<const float4 *>(row + 4 * LPK), q[y][2], q[y][3]);
+                load_pairs(row, q[y][0], q[y][1]);
+                load_pairs(row + 4 * LPK, q[y][2], q[y][3]);
             }
         }
         float m = -INFINITY, l = 0.f;                       // of row sub % R; l of this lane's keys

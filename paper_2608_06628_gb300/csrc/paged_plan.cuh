@@ -27,6 +27,7 @@
 
 #include "hybrid_common.cuh"
 #include "softmax_kernels.h"
+#include "tc_ptx.cuh"
 
 namespace hyb {
 namespace paged {
@@ -313,6 +314,20 @@ __device__ __forceinline__ bool row_at(const PagedArgs &a, int req, const Unit &
     const int i = u.i0 + rho / a.Gt, g = u.g0 + rho % a.Gt;
     at = (((size_t)req * a.B + i) * a.Hq + (size_t)u.head * a.G + g) * a.d;
     return rho < a.Bt * a.Gt && i < a.B && g < a.G;
+}
+
+// 16 bytes to shared memory by cp.async, `bytes` (16 or 0) of them read and the rest zeros.
+__device__ __forceinline__ void copy16(void *dst, const float *src, int bytes)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(ptx::smem_u32(dst)), "l"(src), "r"(bytes)
+                 : "memory");
+}
+// 16 bytes as two pairs
+__device__ __forceinline__ void load_pairs(const void *p, ptx::f32x2 &a, ptx::f32x2 &b)
+{
+    const ulonglong2 v = *static_cast<const ulonglong2 *>(p);
+    a.v = v.x;
+    b.v = v.y;
 }
 
 // Partial slot: m[rows], l[rows], O[d][rows] (feature-major, so that the threads of a

@@ -64,7 +64,7 @@ struct PagedArgs {
 void paged_geometry(const hybrid_cfg &c, PagedArgs &a);
 size_t paged_workspace_bytes(const PagedArgs &a);
 void paged_set_workspace(PagedArgs &a, void *workspace);
-// Without the join: bfloat16; float32 with at most kFewestRows rows to a key head.
+// Without the join: bfloat16; float32 with row tiles of at most kFewestRows rows.
 cudaError_t launch_paged_attn_tc(const PagedArgs &a, cudaStream_t st);
 constexpr int kFewestRows = 8;
 cudaError_t launch_paged_attn_few(const PagedArgs &a, cudaStream_t st);

@@ -647,7 +647,7 @@ def test_attention_of_contexts_that_fit_a_tile(dt, max_len):
 
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("B,G", [(1, 1), (3, 1), (1, 4), (1, 5), (7, 1), (2, 4), (1, 8), (9, 1), (3, 3), (1, 11), (5, 3), (4, 4), (1, 16),
-                                 (17, 1)])
+                                 (17, 1), (6, 4), (5, 4), (33, 1), (9, 7)])
 def test_attention_float32_few_rows(B, G, d):
     """Row counts at which the float32 kernels and the row tiles change; masks of both kinds, requests that are split."""
     for window, sink, scale in ((0, 0, 1.0), (300, 5, 4.0)):
