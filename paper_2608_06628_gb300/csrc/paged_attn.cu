@@ -5,21 +5,20 @@
 // pass; scores are kept in units of log2, x = q . k log2(e) / sqrt(d).
 //
 // A block of 8 warps takes the tiles of its share (paged_plan.cuh) one after another,
-// 64 rows x 128 keys.  For the scores a thread has 8 rows x 4 keys (12 16-byte reads of
-// shared memory for 64 packed FMAs), for O 4 rows x 8 features (the same), with all
-// keys at d = 128 and every second 64 of them at d = 64, added at a segment's end.  K, V
-// and P have one buffer each: K of the next tile comes while P V is computed, V while
-// the scores are; masked keys are zero-filled, their pages not read.  A row's
-// maximum is moved only when a score exceeds it by more than 8, which the block votes
-// on, so that a tile takes three barriers and no reduction; sums are added over the
-// threads at a segment's end.  Row tiles of up to 8 rows: paged_attn_few.cu.
+// 64 rows x 128 keys (rows beyond the tile's are zeros: checks in the loops cost more).
+// For the scores a thread has 8 rows x 4 keys (12 16-byte reads of shared memory for 64
+// packed FMAs), for O 4 rows x 8 features (the same), with all keys at d = 128 and every
+// second 64 of them at d = 64, added at a segment's end.  K, V and P have one buffer each:
+// K of the next tile comes while P V is computed, V while the scores are; masked keys are
+// zero-filled, their pages not read.  A row's maximum is moved only when a score exceeds
+// it by more than 8, which the block votes on, so that a tile takes three barriers and no
+// reduction; sums are added over the threads at a segment's end.  Row tiles of up to 8
+// rows: paged_attn_few.cu.
 //
-// Bound by reads of shared memory and the FMA pipe in turn (58% and 57% of their peaks):
-// 64 requests of 256-8192 tokens, blocks of 32, 16 query and 4 key heads, d = 128
-// 1610 us (44 TFLOP/s), d = 64 909 us; with 8 rows x 2 keys and 4 x 4 to a thread,
-// and a maximum of each row found for each tile, 2440 us.
-#include <type_traits>
-
+// Bound by reads of shared memory and the FMA pipe in turn (about 60% of the peak of
+// each): 64 requests of 256-8192 tokens, blocks of 32, 16 query and 4 key heads, d = 128
+// 1540 us (46 TFLOP/s), d = 64 852 us; with 8 rows x 2 keys and 4 x 4 to a thread, and a
+// maximum of each row found for each tile, 2440 us.
 #include "paged_plan.cuh"
 #include "tc_pipeline.cuh"
 
@@ -162,26 +161,20 @@ template <int D> __global__ __launch_bounds__(kThreads, 1) void k_paged_attn(con
                     for (int y = 0; y < 8; ++y)
 #pragma unroll
                         for (int k = 0; k < 4; ++k) acc[y][k] = pair2(0.f, 0.f);
-                    auto products = [&](auto full) {
 #pragma unroll 2
-                        for (int c = 0; c < D; c += 4) {
-                            f32x2 k0[4], k1[4];
+                    for (int c = 0; c < D; c += 4) {
+                        f32x2 k0[4], k1[4];
 #pragma unroll
-                            for (int k = 0; k < 4; ++k) load_pairs(&s.k[key_s + 8 * k][c], k0[k], k1[k]);
+                        for (int k = 0; k < 4; ++k) load_pairs(&s.k[key_s + 8 * k][c], k0[k], k1[k]);
 #pragma unroll
-                            for (int y = 0; y < 8; ++y) {
-                                if (!full && 8 * y >= rows) break;
-                                f32x2 q0, q1;
-                                load_pairs(&s.q[row_s + 8 * y][c], q0, q1);
+                        for (int y = 0; y < 8; ++y) {
+                            f32x2 q0, q1;
+                            load_pairs(&s.q[row_s + 8 * y][c], q0, q1);
 #pragma unroll
-                                for (int k = 0; k < 4; ++k)
-                                    acc[y][k] = ptx::fma2(k1[k], q1, ptx::fma2(k0[k], q0, acc[y][k]));
-                            }
+                            for (int k = 0; k < 4; ++k)
+                                acc[y][k] = ptx::fma2(k1[k], q1, ptx::fma2(k0[k], q0, acc[y][k]));
                         }
-                    };
-                    // (a full tile without the checks of each row)
-                    if (rows > kRows - 8) products(std::true_type{});
-                    else products(std::false_type{});
+                    }
                     const int j = key_tile(w.vis, tile) * kTile + key_s;
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
@@ -249,32 +242,27 @@ template <int D> __global__ __launch_bounds__(kThreads, 1) void k_paged_attn(con
                         for (int e = 0; e < 4; ++e) o[y][e] = ptx::mul2(o[y][e], ff);
                     }
                 }
-                auto products = [&](auto full) {
 #pragma unroll 4
-                    for (int r = 0; r < kKeysO; r += 4) {
-                        f32x2 v[4][4];
+                for (int r = 0; r < kKeysO; r += 4) {
+                    f32x2 v[4][4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const float *at = &s.v[key_o + r + k][col_o];
+                        load_pairs(at, v[k][0], v[k][1]);
+                        load_pairs(at + 32, v[k][2], v[k][3]);
+                    }
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) {
+                        const float4 p4 = *reinterpret_cast<const float4 *>(&s.p[row_o + 16 * y][key_o + r]);
+                        const float p[4] = {p4.x, p4.y, p4.z, p4.w};
 #pragma unroll
                         for (int k = 0; k < 4; ++k) {
-                            const float *at = &s.v[key_o + r + k][col_o];
-                            load_pairs(at, v[k][0], v[k][1]);
-                            load_pairs(at + 32, v[k][2], v[k][3]);
-                        }
+                            const f32x2 pp = pair2(p[k], p[k]);
 #pragma unroll
-                        for (int y = 0; y < 4; ++y) {
-                            if (!full && 16 * y >= rows) break;
-                            const float4 p4 = *reinterpret_cast<const float4 *>(&s.p[row_o + 16 * y][key_o + r]);
-                            const float p[4] = {p4.x, p4.y, p4.z, p4.w};
-#pragma unroll
-                            for (int k = 0; k < 4; ++k) {
-                                const f32x2 pp = pair2(p[k], p[k]);
-#pragma unroll
-                                for (int e = 0; e < 4; ++e) o[y][e] = ptx::fma2(pp, v[k][e], o[y][e]);
-                            }
+                            for (int e = 0; e < 4; ++e) o[y][e] = ptx::fma2(pp, v[k][e], o[y][e]);
                         }
                     }
-                };
-                if (rows > kRows - 16) products(std::true_type{});
-                else products(std::false_type{});
+                }
                 asm volatile("cp.async.wait_group 0;" ::: "memory");
                 __syncthreads();                            // the next K and Q are in place, V and P have been read
                 if (more) copy_tile(vis_v, i_v, from, a.V, &s.v[0][0], D);
@@ -497,13 +485,12 @@ void paged_geometry(const hybrid_cfg &c, PagedArgs &a)
     if (tc) {
         cut_rows(a, kMaxRows);
     } else {
-        // The kernel of paged_attn_few.cu also for a few row tiles, if they are about full:
-        // 64 requests of 256-8192 tokens, 4 key heads, d = 128, two tiles of 8 rows 426 us
-        // against 580 here, three 630 and 724, four 825 and 798, but one request of 777
-        // tokens 12.4 and 24.0; three tiles of 5 rows 628 and 580.
+        // The kernel of paged_attn_few.cu also for a few row tiles: 64 requests of 256-8192
+        // tokens, 4 key heads, d = 128, here 786 us for any rows up to 64, there four tiles
+        // of 8 rows 650 us, five 813, six 969 (one request of 777 tokens: 25 us here, 14
+        // there).
         cut_rows(a, kFewestRows);
-        const int tiles = a.n_gt * a.n_bt;
-        if (tiles > 4 || (tiles > 2 && a.G * a.B < 6 * tiles)) cut_rows(a, kRows);
+        if (a.n_gt * a.n_bt > 5) cut_rows(a, kRows);
     }
     const int rows = a.Bt * a.Gt;
     a.extra = tc && rows <= 64 ? 3 : 7;

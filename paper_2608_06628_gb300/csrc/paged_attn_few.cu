@@ -1,11 +1,11 @@
 // paged_attn_few.cu -- attention over the paged cache for row tiles of at most 8 rows,
 // float32 (hybrid_paged_attn): decoding.
 //
-// D / 8 lanes hold the queries of the R = 4 or 8 rows and a step's 8 / R keys, 8 features
+// D / 8 lanes hold the queries of the R = 4 or 8 rows and a step's two keys, 8 features
 // each:
-//     x = q . k log2(e) / sqrt(d)    8 partial products (keys x rows), added over the
-//                                    lanes by halves, so that lane i ends with product i % 8
-//     p = 2^(x - m), l += p          one a lane
+//     x = q . k log2(e) / sqrt(d)    2 R partial products, added over the lanes by halves,
+//                                    so that each lane ends with one (or two) of them
+//     p = 2^(x - m), l += p          by that lane
 //     o += p v                       p from its lane; o as R rows of 8 features a lane
 // A row's maximum is moved, and its output rescaled, only when a score exceeds it by
 // more than 8 (as in paged_attn_tc.cu).  Each group of D / 8 lanes has an m, l and o of
@@ -16,7 +16,8 @@
 // Bound by memory with 4 rows: 64 requests of 256-8192 tokens, 4 key heads, d = 128
 // 176 us (6.3 TB/s), d = 64 92 us, where a version with chunks of 32 or 64 keys, two barriers
 // each and scores through shared memory took 297 us.  With 8 rows the queries and
-// outputs fill 128 registers: one block to a multiprocessor, 223 us (that version 463).
+// outputs fill 128 registers, so one block to a multiprocessor, 177 and 99 us (one key
+// to a step 223 and 121 us: 2 warps to a scheduler, and each step waits for its sums).
 #include "paged_plan.cuh"
 #include "tc_pipeline.cuh"
 
@@ -29,12 +30,12 @@ using ptx::pair2;
 
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
+constexpr int kKeys = 2;                        // of a lane in a step
 constexpr int kRun = kTile / kWarps;            // keys of a warp in a tile, side by side: of one page
 constexpr float kSlack = 8.f;
 
 template <int D, int R> struct Smem {
-    static constexpr int kKeys = 8 / R;         // keys of a lane: 8 products
-    static constexpr int kStages = R == 4 ? 3 : 8;
+    static constexpr int kStages = R == 4 ? 3 : 4;
     float4 ring[kWarps][kStages][4 * kKeys][32];            // [2 key + half]: K, then V
     float o[kWarps][R][D];
     float m[kWarps][R], l[kWarps][R];
@@ -44,10 +45,12 @@ template <int D, int R> struct Smem {
 template <int D, int R>
 __global__ __launch_bounds__(kThreads, R == 4 ? 2 : 1) void k_paged_attn_few(const PagedArgs a, int page_lg)
 {
-    constexpr int kKeys = Smem<D, R>::kKeys, kStages = Smem<D, R>::kStages;
+    constexpr int kStages = Smem<D, R>::kStages;
     constexpr int LPK = D / 8, SLOTS = 32 / LPK;            // lanes of a key, groups of a warp
     constexpr int kSteps = kRun / (kKeys * SLOTS);          // steps of a tile
-    static_assert((kStages - 1) * kKeys < 32, "bits of `seen`");
+    // the products key * R + row of a step: lane i ends with kOwn from kOwn (i % kSpread)
+    constexpr int kProducts = kKeys * R, kSpread = kProducts < LPK ? kProducts : LPK, kOwn = kProducts / kSpread;
+    static_assert(kStages * kKeys < 32, "bits of `seen`");
     extern __shared__ __align__(16) unsigned char raw[];
     Smem<D, R> &s = *reinterpret_cast<Smem<D, R> *>(raw);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -61,56 +64,69 @@ __global__ __launch_bounds__(kThreads, R == 4 ? 2 : 1) void k_paged_attn_few(con
     Walk w;
     Shares sh(0, 1);
     const bool work = find_share<kThreads>(a, s.plan, w, sh);
-    while (work && w.next(a)) {
-        const Unit u = unit_of(a, w.head, w.rt);
-        const int *pages = a.table + (size_t)w.req * a.max_pages;
-        const Visible vis = w.vis;
-        int i = w.i0, at = 0, slot = 0;                     // of the copies: tile, step within it, stage
-        unsigned seen = 0;                                  // a bit for each key, the latest lowest
-        int key = 0, page = 0, ahead;                       // first key of the run, its page, the next run's
-        auto look_up = [&](int tile) {
-            const int j = key_tile(vis, tile) * kTile + warp * kRun;
-            return tile < w.i1 && any_visible(vis, j, kRun) ? __ldg(pages + (j >> page_lg)) : 0;
-        };
-        ahead = look_up(i);
-        auto fetch = [&]() {
-            if (i < w.i1) {
-                if (at == 0) {
-                    key = key_tile(vis, i) * kTile + warp * kRun;
-                    page = ahead;
-                    if (page < 0 || page >= a.n_pages) {
-                        raise_error(a.err, ERR_BAD_INDEX);
-                        page = 0;
-                    }
-                    ahead = look_up(i + 1);
+    bool go = work && w.next(a);
+    // the copies, of the segment w: tile, step within it, stage
+    int i = 0, at = 0, slot = 0;
+    unsigned seen = 0;                                      // a bit for each key, the latest lowest
+    int key = 0, ahead = 0;                                 // this group's first key of the run; page of the next run
+    size_t run = 0;                                         // place of that key in the cache
+    auto look_up = [&](int tile) {
+        ahead = 0;
+        if (tile >= w.i1) return;
+        const int j = key_tile(w.vis, tile) * kTile + warp * kRun;
+        if (any_visible(w.vis, j, kRun)) ahead = __ldg(a.table + (size_t)w.req * a.max_pages + (j >> page_lg));
+    };
+    auto fetch = [&]() {
+        if (i < w.i1) {
+            if (at == 0) {
+                key = key_tile(w.vis, i) * kTile + warp * kRun + group;
+                int page = ahead;
+                if (page < 0 || page >= a.n_pages) {
+                    raise_error(a.err, ERR_BAD_INDEX);
+                    page = 0;
                 }
-                const size_t head = (((size_t)page * a.Hkv + w.head) << page_lg) * D;
-#pragma unroll
-                for (int x = 0; x < kKeys; ++x) {
-                    const int j = key + (kKeys * at + x) * SLOTS + group;
-                    const bool see = key_visible(vis, j);
-                    const int bytes = see ? 16 : 0;         // masked keys and values are zeros
-                    const size_t from = see ? head + (size_t)(j & ((1 << page_lg) - 1)) * D + 4 * sub : 0;
-                    seen = 2 * seen + see;
-#pragma unroll
-                    for (int y = 0; y < 2; ++y) {
-                        const int c = y * 4 * LPK;
-                        copy16(&ring[slot][2 * x + y][lane], static_cast<const float *>(a.K) + from + c, bytes);
-                        copy16(&ring[slot][2 * (kKeys + x) + y][lane], static_cast<const float *>(a.V) + from + c, bytes);
-                    }
-                }
-                if (++at == kSteps) {
-                    at = 0;
-                    ++i;
-                }
-            } else {
-                seen <<= kKeys;
+                run = ((((size_t)page * a.Hkv + w.head) << page_lg) + (key & ((1 << page_lg) - 1))) * D + 4 * sub;
+                look_up(i + 1);
             }
-            slot = slot + 1 == kStages ? 0 : slot + 1;
-            asm volatile("cp.async.commit_group;" ::: "memory");
-        };
+#pragma unroll
+            for (int x = 0; x < kKeys; ++x) {
+                const int step = (kKeys * at + x) * SLOTS;
+                const bool see = key_visible(w.vis, key + step);
+                const int bytes = see ? 16 : 0;             // masked keys and values are zeros
+                const size_t from = see ? run + step * D : 0;
+                seen = 2 * seen + see;
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+                    const int c = y * 4 * LPK;
+                    copy16(&ring[slot][2 * x + y][lane], static_cast<const float *>(a.K) + from + c, bytes);
+                    copy16(&ring[slot][2 * (kKeys + x) + y][lane], static_cast<const float *>(a.V) + from + c, bytes);
+                }
+            }
+            if (++at == kSteps) {
+                at = 0;
+                ++i;
+            }
+        } else {
+            seen <<= kKeys;
+        }
+        slot = slot + 1 == kStages ? 0 : slot + 1;
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    auto first_page = [&]() {
+        i = w.i0;
+        at = slot = 0;
+        look_up(i);
+    };
+    auto first_steps = [&]() {
 #pragma unroll
         for (int x = 0; x < kStages - 1; ++x) fetch();
+    };
+    if (go) {
+        first_page();
+        first_steps();
+    }
+    while (go) {
+        const Unit u = unit_of(a, w.head, w.rt);
         f32x2 q[R][4], o[R][4];
 #pragma unroll
         for (int y = 0; y < R; ++y) {
@@ -124,12 +140,17 @@ __global__ __launch_bounds__(kThreads, R == 4 ? 2 : 1) void k_paged_attn_few(con
                 load_pairs(row + 4 * LPK, q[y][2], q[y][3]);
             }
         }
-        float m = -INFINITY, l = 0.f;                       // of row sub % R; l of this lane's keys
+        float m[kOwn], l[kOwn];                             // of rows kOwn sub % R ...; l of this lane's key
+#pragma unroll
+        for (int e = 0; e < kOwn; ++e) {
+            m[e] = -INFINITY;
+            l[e] = 0.f;
+        }
         const int steps = (w.i1 - w.i0) * kSteps;
         for (int n = 0, b = 0; n < steps; ++n, b = b + 1 == kStages ? 0 : b + 1) {
             fetch();                                        // into the stage of the step before
             asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
-            float x[8];
+            float x[kProducts];
 #pragma unroll
             for (int k = 0; k < kKeys; ++k) {
                 f32x2 c[4];
@@ -143,35 +164,47 @@ __global__ __launch_bounds__(kThreads, R == 4 ? 2 : 1) void k_paged_attn_few(con
                     x[R * k + y] = lo + hi;
                 }
             }
-            // add over the lanes; lane i keeps product i % 8
+            // add over the lanes, each time half of the products to half of the lanes
 #pragma unroll
-            for (int f = 4; f > 0; f >>= 1)
+            for (int f = kSpread / 2; f > 0; f >>= 1)
 #pragma unroll
-                for (int y = 0; y < f; ++y) {
+                for (int y = 0; y < kOwn * f; ++y) {
                     const bool up = sub & f;
-                    const float give = up ? x[y] : x[y + f];
-                    x[y] = (up ? x[y + f] : x[y]) + __shfl_xor_sync(0xffffffffu, give, f);
+                    const float give = up ? x[y] : x[y + kOwn * f];
+                    x[y] = (up ? x[y + kOwn * f] : x[y]) + __shfl_xor_sync(0xffffffffu, give, f);
                 }
 #pragma unroll
-            for (int f = 8; f < LPK; f <<= 1) x[0] += __shfl_xor_sync(0xffffffffu, x[0], f);
-            const bool see = seen >> (kKeys * kStages - 1 - sub % 8 / R) & 1;
-            const float score = see ? x[0] * to_log2 : -INFINITY;
-            if (__any_sync(0xffffffffu, score > m + kSlack)) {
-                float now = score > m + kSlack ? score : m;
-                if (R == 4) now = fmaxf(now, __shfl_xor_sync(0xffffffffu, now, 4));
-                const float f = m == -INFINITY ? 1.f : exp2f(m - now);      // (o and l are zero, or NaN)
-                m = now;
-                l *= f;
+            for (int f = kSpread; f < LPK; f <<= 1) x[0] += __shfl_xor_sync(0xffffffffu, x[0], f);
+            const bool see = seen >> (kKeys * kStages - 1 - sub % kSpread * kOwn / R) & 1;
+            bool above = false;
+#pragma unroll
+            for (int e = 0; e < kOwn; ++e) {
+                x[e] = see ? x[e] * to_log2 : -INFINITY;
+                above |= x[e] > m[e] + kSlack;
+            }
+            if (__any_sync(0xffffffffu, above)) {
+                float f[kOwn];
+#pragma unroll
+                for (int e = 0; e < kOwn; ++e) {
+                    float now = x[e] > m[e] + kSlack ? x[e] : m[e];
+                    now = fmaxf(now, __shfl_xor_sync(0xffffffffu, now, kSpread / 2));   // the lane of the other key
+                    f[e] = m[e] == -INFINITY ? 1.f : exp2f(m[e] - now);                 // (o and l are zero, or NaN)
+                    m[e] = now;
+                    l[e] *= f[e];
+                }
 #pragma unroll
                 for (int y = 0; y < R; ++y) {
-                    const float g = __shfl_sync(0xffffffffu, f, lane0 + y);
+                    const float g = __shfl_sync(0xffffffffu, f[y % kOwn], lane0 + y / kOwn);
                     const f32x2 gg = pair2(g, g);
 #pragma unroll
                     for (int c = 0; c < 4; ++c) o[y][c] = ptx::mul2(o[y][c], gg);
                 }
             }
-            const float p = exp2f(score - (m == -INFINITY ? 0.f : m));
-            l += p;
+#pragma unroll
+            for (int e = 0; e < kOwn; ++e) {
+                x[e] = exp2f(x[e] - (m[e] == -INFINITY ? 0.f : m[e]));
+                l[e] += x[e];
+            }
 #pragma unroll
             for (int k = 0; k < kKeys; ++k) {
                 f32x2 c[4];
@@ -179,29 +212,38 @@ __global__ __launch_bounds__(kThreads, R == 4 ? 2 : 1) void k_paged_attn_few(con
                 load_pairs(&ring[b][2 * (kKeys + k) + 1][lane], c[2], c[3]);
 #pragma unroll
                 for (int y = 0; y < R; ++y) {
-                    const float t = __shfl_sync(0xffffffffu, p, lane0 + R * k + y);
+                    const float t = __shfl_sync(0xffffffffu, x[(R * k + y) % kOwn], lane0 + (R * k + y) / kOwn);
                     const f32x2 tt = pair2(t, t);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) o[y][e] = ptx::fma2(tt, c[e], o[y][e]);
                 }
             }
         }
+        // the segment after this one: its first page, then its first copies, are under way meanwhile
+        const bool whole = w.whole();
+        const int req = w.req;
+        float *part = a.part + w.slot() * partial_floats(rows, D);
+        go = w.next(a);
+        if (go) first_page();
         {   // the groups of the warp
-            float top = m;
+            float f[kOwn];
 #pragma unroll
-            for (int f = LPK; f < 32; f <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, f));
-            const float f = m == -INFINITY ? 0.f : exp2f(m - top);
-            if (R == 4) l += __shfl_xor_sync(0xffffffffu, l, 4);
-            l *= f;
+            for (int e = 0; e < kOwn; ++e) {
+                float top = m[e];
 #pragma unroll
-            for (int x = LPK; x < 32; x <<= 1) l += __shfl_xor_sync(0xffffffffu, l, x);
-            if (lane < R) {
-                s.m[warp][lane] = top;
-                s.l[warp][lane] = l;
+                for (int x = LPK; x < 32; x <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
+                f[e] = m[e] == -INFINITY ? 0.f : exp2f(m[e] - top);
+                l[e] = (l[e] + __shfl_xor_sync(0xffffffffu, l[e], kSpread / 2)) * f[e];
+#pragma unroll
+                for (int x = LPK; x < 32; x <<= 1) l[e] += __shfl_xor_sync(0xffffffffu, l[e], x);
+                if (lane < R / kOwn) {
+                    s.m[warp][lane * kOwn + e] = top;
+                    s.l[warp][lane * kOwn + e] = l[e];
+                }
             }
 #pragma unroll
             for (int y = 0; y < R; ++y) {
-                const float g = __shfl_sync(0xffffffffu, f, lane0 + y);
+                const float g = __shfl_sync(0xffffffffu, f[y % kOwn], lane0 + y / kOwn);
                 float e[8];
 #pragma unroll
                 for (int c = 0; c < 4; ++c) ptx::unpair2(o[y][c], e[2 * c], e[2 * c + 1]);
@@ -217,10 +259,9 @@ __global__ __launch_bounds__(kThreads, R == 4 ? 2 : 1) void k_paged_attn_few(con
                 }
             }
         }
+        if (go) first_steps();
         __syncthreads();
         // the warps
-        const bool whole = w.whole();
-        float *part = a.part + w.slot() * partial_floats(rows, D);
         for (int x = tid; x < rows * D; x += kThreads) {
             const int rho = x / D, c = x % D;
             float top = s.m[0][rho], sum = 0.f, out = 0.f;
@@ -235,7 +276,7 @@ __global__ __launch_bounds__(kThreads, R == 4 ? 2 : 1) void k_paged_attn_few(con
             }
             if (whole) {
                 size_t to;
-                if (row_at(a, w.req, u, rho, to)) static_cast<float *>(a.O)[to + c] = out / sum;
+                if (row_at(a, req, u, rho, to)) static_cast<float *>(a.O)[to + c] = out / sum;
             } else {
                 part[2 * rows + (size_t)c * rows + rho] = out;
                 if (c == 0) {
