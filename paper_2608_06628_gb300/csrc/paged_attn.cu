@@ -337,14 +337,13 @@ template <int D> __global__ __launch_bounds__(kThreads, 1) void k_paged_attn(con
 }
 
 // Join: block x reads the note of boundary x and, if a unit is cut there for the
-// first time, adds up the unit's partials; blocks along y take COLS features each.
-// A thread has one row and every n-th feature; it loads references, sums and
+// first time, adds up the unit's partials; blocks along y take kJoinCols features each.
+// A thread has one row and some of the features; it loads references, sums and
 // outputs of a partial together and merges them into its own (m, l, o), so that two
-// rounds of loads (the note, then the partials) are all the latency.  Where a unit
-// has few rows (decoding) it may have many partials: then groups of threads take
-// every n-th one, and the groups are merged in order.  Launched programmatically
-// behind the attention kernel.
+// rounds of loads (the note, then the partials) are all the latency.  Launched
+// programmatically behind the attention kernel.
 constexpr int kMaxRows = 128;
+constexpr int kJoinCols = 16;
 
 // (m, l, o) <- (m, l, o) + (mi, li, oi): weights of both in units of the larger reference
 struct Merge {
@@ -358,84 +357,124 @@ struct Merge {
     }
 };
 
-template <typename T, int COLS, int ROWS>
-__global__ __launch_bounds__(kThreads) void k_paged_join(const PagedArgs a)
+// At most 16 rows (decoding): a unit may have many partials, so groups of kJoinCols
+// threads a row, one feature each, take every n-th one, and the groups are merged in
+// order.
+template <typename T> __global__ __launch_bounds__(kThreads) void k_paged_join_few(const PagedArgs a)
 {
-    constexpr int kIter = ROWS * COLS > kThreads ? ROWS * COLS / kThreads : 1;   // features per thread, at most
-    constexpr int kOut = ROWS * (COLS + 1) > kThreads ? ROWS * (COLS + 1) : kThreads;
-    __shared__ float s_o[kOut];                              // [row][COLS + 1], or one value a thread
+    constexpr int kPitch = kJoinCols + 1;
+    __shared__ float s_o[16 * kPitch];                       // one value a thread, then [row][kPitch]
     __shared__ float s_m[kThreads], s_l[kThreads];
-    const int tid = threadIdx.x, rows = a.Bt * a.Gt, c = blockIdx.x, col0 = blockIdx.y * COLS;
+    static_assert(16 * kPitch >= kThreads, "a value of each thread");
+    const int tid = threadIdx.x, rows = a.Bt * a.Gt, c = blockIdx.x, col0 = blockIdx.y * kJoinCols;
     ptx::griddep_wait();
     const JoinNote note = a.notes[c];
     if (!note.cut) return;
     const size_t size = partial_floats(rows, a.d);
     const int n = note.last - c + 1;                         // partials
-    auto part_of = [&](int i) { return a.part + (size_t)(i == 0 ? 2 * c + 1 : 2 * (c + i)) * size; };
-
-    const int rho = tid % rows, lane = tid / rows, lanes = kThreads / rows;   // threads of a row
-    const int groups = lanes >= COLS ? lanes / COLS : 1, step = lanes >= COLS ? COLS : lanes;
-    const int g = lane / step, first = lane % step;          // features first, first + step, ...
-    float m = -INFINITY, l = 0.f, o[kIter];
-#pragma unroll
-    for (int k = 0; k < kIter; ++k) o[k] = 0.f;
+    const int rho = tid % rows, lane = tid / rows, groups = kThreads / rows / kJoinCols;
+    const int g = lane / kJoinCols, col = lane % kJoinCols;
+    float m = -INFINITY, l = 0.f, o = 0.f;
     if (g < groups) {
         constexpr int kLoad = 4;                             // partials loaded at a time
         for (int i0 = g; i0 < n; i0 += kLoad * groups) {
-            float mi[kLoad], li[kLoad], v[kLoad][kIter];
+            float mi[kLoad], li[kLoad], v[kLoad];
 #pragma unroll
             for (int x = 0; x < kLoad; ++x) {
                 const int i = i0 + x * groups;
-                const float *p = part_of(i < n ? i : i0);
-                mi[x] = i < n ? p[rho] : -INFINITY;
-                li[x] = p[rows + rho];
-#pragma unroll
-                for (int k = 0; k < kIter; ++k) {
-                    const int col = first + k * step;
-                    v[x][k] = i < n && col < COLS ? p[2 * rows + (size_t)(col0 + col) * rows + rho] : 0.f;
-                }
+                const float *p = a.part + (size_t)(i == 0 ? 2 * c + 1 : 2 * (c + i)) * size + rho;
+                mi[x] = i < n ? p[0] : -INFINITY;
+                li[x] = i < n ? p[rows] : 0.f;
+                v[x] = i < n ? p[(2 + col0 + col) * rows] : 0.f;
             }
 #pragma unroll
             for (int x = 0; x < kLoad; ++x) {
                 if (i0 + x * groups >= n) break;
                 const Merge w(m, mi[x]);
                 l = l * w.keep + li[x] * w.add;
-#pragma unroll
-                for (int k = 0; k < kIter; ++k) o[k] = o[k] * w.keep + v[x][k] * w.add;
+                o = o * w.keep + v[x] * w.add;
             }
         }
     }
-    if (groups > 1) {                                        // one feature a thread
+    if (groups > 1) {
         s_m[tid] = m;
         s_l[tid] = l;
-        s_o[tid] = o[0];
+        s_o[tid] = o;
         __syncthreads();
         if (g == 0) {
             for (int y = 1; y < groups; ++y) {
-                const int other = tid + y * COLS * rows;
+                const int other = tid + y * kJoinCols * rows;
                 const Merge w(m, s_m[other]);
                 l = l * w.keep + s_l[other] * w.add;
-                o[0] = o[0] * w.keep + s_o[other] * w.add;
+                o = o * w.keep + s_o[other] * w.add;
             }
         }
         __syncthreads();
     }
-    if (g == 0) {
-        const float inv = 1.f / l;
-#pragma unroll
-        for (int k = 0; k < kIter; ++k) {
-            const int col = first + k * step;
-            if (col < COLS) s_o[rho * (COLS + 1) + col] = o[k] * inv;
-        }
-    }
+    if (g == 0) s_o[rho * kPitch + col] = o / l;
     __syncthreads();
     const Unit u = unit_of(a, note.head, note.rt);
-    for (int x = tid; x < rows * (COLS / 4); x += kThreads) {
-        const int r = x / (COLS / 4), col = x % (COLS / 4) * 4;
+    for (int x = tid; x < rows * (kJoinCols / 4); x += kThreads) {
+        const int r = x / (kJoinCols / 4), at_col = x % (kJoinCols / 4) * 4;
         size_t at;
         if (!row_at(a, note.req, u, r, at)) continue;
-        const float *v = s_o + r * (COLS + 1) + col;
-        store4(static_cast<T *>(a.O) + at + col0 + col, make_float4(v[0], v[1], v[2], v[3]));
+        const float *v = s_o + r * kPitch + at_col;
+        store4(static_cast<T *>(a.O) + at + col0 + at_col, make_float4(v[0], v[1], v[2], v[3]));
+    }
+}
+
+// More than 16 rows: kJoinCols / FEAT threads to a row, each with FEAT features side by
+// side, which it writes itself; two partials at a time, as most units have, so that five
+// blocks are in place on a multiprocessor.  (Four partials at a time and the output by way
+// of shared memory, three blocks: blocks of 32 tokens for 64 requests 104 us, here 100.)
+template <typename T, int FEAT> __global__ __launch_bounds__(kThreads, 4) void k_paged_join_many(const PagedArgs a)
+{
+    constexpr int kSpan = kThreads * FEAT / kJoinCols;       // rows
+    const int rows = a.Bt * a.Gt, rho = threadIdx.x % kSpan, c = blockIdx.x;
+    const int col = blockIdx.y * kJoinCols + threadIdx.x / kSpan * FEAT;
+    ptx::griddep_wait();
+    const JoinNote note = a.notes[c];
+    if (!note.cut || rho >= rows) return;
+    const size_t size = partial_floats(rows, a.d);
+    const int n = note.last - c + 1;                         // partials
+    float m = -INFINITY, l = 0.f, o[FEAT];
+#pragma unroll
+    for (int k = 0; k < FEAT; ++k) o[k] = 0.f;
+    for (int i0 = 0; i0 < n; i0 += 2) {
+        float mi[2], li[2], v[2][FEAT];
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            const int i = i0 + x;
+            const float *p = a.part + (size_t)(i == 0 ? 2 * c + 1 : 2 * (c + i)) * size + rho;
+            mi[x] = i < n ? p[0] : -INFINITY;
+            li[x] = i < n ? p[rows] : 0.f;
+#pragma unroll
+            for (int k = 0; k < FEAT; ++k) v[x][k] = i < n ? p[(2 + col + k) * rows] : 0.f;
+        }
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            if (i0 + x >= n) break;
+            const Merge w(m, mi[x]);
+            l = l * w.keep + li[x] * w.add;
+#pragma unroll
+            for (int k = 0; k < FEAT; ++k) o[k] = o[k] * w.keep + v[x][k] * w.add;
+        }
+    }
+    size_t at;
+    if (!row_at(a, note.req, unit_of(a, note.head, note.rt), rho, at)) return;
+    const float inv = 1.f / l;
+#pragma unroll
+    for (int k = 0; k < FEAT; ++k) o[k] *= inv;
+    T *out = static_cast<T *>(a.O) + at + col;
+    if constexpr (FEAT == 2) {
+        if constexpr (sizeof(T) == 4) *reinterpret_cast<float2 *>(out) = make_float2(o[0], o[1]);
+        else *reinterpret_cast<uint32_t *>(out) = pipe::pack_bf16x2(o[0], o[1]);
+    } else if constexpr (FEAT == 8 && sizeof(T) == 2) {
+        *reinterpret_cast<uint4 *>(out) = make_uint4(pipe::pack_bf16x2(o[0], o[1]), pipe::pack_bf16x2(o[2], o[3]),
+                                                     pipe::pack_bf16x2(o[4], o[5]), pipe::pack_bf16x2(o[6], o[7]));
+    } else {
+#pragma unroll
+        for (int k = 0; k < FEAT; k += 4) store4(out + k, make_float4(o[k], o[k + 1], o[k + 2], o[k + 3]));
     }
 }
 
@@ -444,12 +483,12 @@ __global__ __launch_bounds__(kThreads) void k_paged_join(const PagedArgs a)
 template <typename T> cudaError_t launch_join(const PagedArgs &a, cudaStream_t st)
 {
     if (a.n_cta == 1 || a.max_pages * a.page_size <= kTile) return cudaSuccess;
-    // few rows: little shared memory, so that the blocks are in place before the
-    // attention kernel ends
+    const dim3 grid(a.n_cta, a.d / kJoinCols), block(kThreads);
     const int rows = a.Bt * a.Gt;
-    if (rows <= 16)
-        return pipe::launch_early(k_paged_join<T, 16, 16>, dim3(a.n_cta, a.d / 16), dim3(kThreads), 0, st, a);
-    return pipe::launch_early(k_paged_join<T, 16, kMaxRows>, dim3(a.n_cta, a.d / 16), dim3(kThreads), 0, st, a);
+    if (rows <= 16) return pipe::launch_early(k_paged_join_few<T>, grid, block, 0, st, a);
+    if (rows <= 32) return pipe::launch_early(k_paged_join_many<T, 2>, grid, block, 0, st, a);
+    if (rows <= 64) return pipe::launch_early(k_paged_join_many<T, 4>, grid, block, 0, st, a);
+    return pipe::launch_early(k_paged_join_many<T, 8>, grid, block, 0, st, a);
 }
 
 template <int D> cudaError_t launch_f32(const PagedArgs &a, cudaStream_t st)
