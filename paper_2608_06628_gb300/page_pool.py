@@ -8,9 +8,21 @@ requests of the batch; a released row may take a new request at once.
 """
 from __future__ import annotations
 
+import contextlib
+
 import torch
 
 from . import hybrid as H
+
+
+def on_stream(stream):
+    """Torch's own work goes to a call's stream too (None: the current one, else torch's stream or a raw handle)."""
+    if stream is None:
+        return contextlib.nullcontext()
+    if not isinstance(stream, torch.cuda.Stream):
+        handle = stream if isinstance(stream, int) else stream.cuda_stream
+        stream = torch.cuda.ExternalStream(handle) if handle else torch.cuda.default_stream()
+    return torch.cuda.stream(stream)
 
 
 class PagePool:
@@ -25,7 +37,9 @@ class PagePool:
         self.device = torch.device(device)
         self.block_table = torch.full((n_req, self.pg.max_pages), -1, dtype=torch.int32, device=device)
         self.free_pages = torch.arange(n_pages, dtype=torch.int32, device=device)
-        self._lens = [torch.zeros(n_req, dtype=torch.int32, device=device) for _ in range(2)]
+        # the lengths and an entry more, which release() writes for rows that are not there
+        self._lens_all = [torch.zeros(n_req + 1, dtype=torch.int32, device=device) for _ in range(2)]
+        self._lens = [x[:n_req] for x in self._lens_all]
         self._ring = [torch.tensor([0, n_pages], dtype=torch.int32, device=device) for _ in range(2)]
         self.workspace_bytes = H.hybrid_paged_attn_workspace_bytes(cfg, self.pg, n_req)
         if self.workspace_bytes == 0:
@@ -51,12 +65,16 @@ class PagePool:
         H.hybrid_page_append(self.pg, self.n_req, self._lens[0], n_new, self.free_pages, self._ring[0], self.block_table,
                              slots, positions, n_tok, offsets, self._lens[1], self._ring[1], stream=stream)
         self._lens.reverse()
+        self._lens_all.reverse()
         self._ring.reverse()
         return slots, positions, offsets
 
     def release(self, rows: torch.Tensor, stream=None):
-        """Give back the pages of the requests in rows (int32, device, each once); their lengths become 0."""
+        """Give back the pages of the requests in rows (int32, device, each once); their lengths become 0, on the
+        same stream. A row out of range is left out, and reported by hybrid_check."""
         H.hybrid_page_release(self.pg, self.n_req, rows, rows.numel(), self._lens[0], self.block_table, self.free_pages,
                               self._ring[0], self._ring[1], stream=stream)
         self._ring.reverse()
-        self._lens[0][rows.long()] = 0
+        with on_stream(stream):
+            there = (rows >= 0) & (rows < self.n_req)
+            self._lens_all[0].index_fill_(0, torch.where(there, rows, self.n_req).long(), 0)
