@@ -15,14 +15,36 @@ import torch
 from . import hybrid as H
 
 
-def on_stream(stream):
-    """Torch's own work goes to a call's stream too (None: the current one, else torch's stream or a raw handle)."""
-    if stream is None:
-        return contextlib.nullcontext()
-    if not isinstance(stream, torch.cuda.Stream):
-        handle = stream if isinstance(stream, int) else stream.cuda_stream
-        stream = torch.cuda.ExternalStream(handle) if handle else torch.cuda.default_stream()
-    return torch.cuda.stream(stream)
+class OnStream:
+    """A call's work on its stream (None: the current one; else torch's stream or a raw handle): torch's own kernels
+    and allocations go there too. `used` is what the work reads and writes besides: its memory is not handed out again
+    before the work is done, whenever the caller drops it, and what returns() is given not before the caller's stream is
+    done with it. The order between the two streams (events, wait_stream) is the caller's."""
+
+    def __init__(self, stream, *used):
+        if stream is None:
+            self.caller, self.scope = None, contextlib.nullcontext()
+            return
+        if not isinstance(stream, torch.cuda.Stream):
+            handle = stream if isinstance(stream, int) else stream.cuda_stream
+            stream = torch.cuda.ExternalStream(handle) if handle else torch.cuda.default_stream()
+        self.caller, self.scope = torch.cuda.current_stream(), torch.cuda.stream(stream)
+        for x in used:
+            if x is not None:
+                x.record_stream(stream)
+
+    def __enter__(self):
+        self.scope.__enter__()
+        return self
+
+    def __exit__(self, *exc):
+        return self.scope.__exit__(*exc)
+
+    def returns(self, *made):
+        if self.caller is not None:
+            for x in made:
+                x.record_stream(self.caller)
+        return made[0] if len(made) == 1 else made
 
 
 class PagePool:
@@ -56,25 +78,29 @@ class PagePool:
         """{head, count} of the free pages."""
         return self._ring[0]
 
+    def _tables(self):
+        return (*self._lens, *self._ring, self.block_table, self.free_pages)
+
     def append(self, n_new: torch.Tensor, n_tok: int, stream=None):
         """Room for n_new [n_req] (int32, device) more tokens of each request, at most n_tok in all.
         Returns slots, positions [n_tok] and tok_offsets [n_req + 1] (int32); slots beyond the last
         token, and of requests that did not fit (see hybrid_check), are -1."""
         new = lambda n: torch.empty(n, dtype=torch.int32, device=self.device)  # noqa: E731
-        slots, positions, offsets = new(n_tok), new(n_tok), new(self.n_req + 1)
-        H.hybrid_page_append(self.pg, self.n_req, self._lens[0], n_new, self.free_pages, self._ring[0], self.block_table,
-                             slots, positions, n_tok, offsets, self._lens[1], self._ring[1], stream=stream)
-        self._lens.reverse()
-        self._lens_all.reverse()
-        self._ring.reverse()
-        return slots, positions, offsets
+        with OnStream(stream, n_new, *self._tables()) as on:
+            slots, positions, offsets = new(n_tok), new(n_tok), new(self.n_req + 1)
+            H.hybrid_page_append(self.pg, self.n_req, self._lens[0], n_new, self.free_pages, self._ring[0], self.block_table,
+                                 slots, positions, n_tok, offsets, self._lens[1], self._ring[1])
+            self._lens.reverse()
+            self._lens_all.reverse()
+            self._ring.reverse()
+            return on.returns(slots, positions, offsets)
 
     def release(self, rows: torch.Tensor, stream=None):
         """Give back the pages of the requests in rows (int32, device, each once); their lengths become 0, on the
         same stream. A row out of range is left out, and reported by hybrid_check."""
-        H.hybrid_page_release(self.pg, self.n_req, rows, rows.numel(), self._lens[0], self.block_table, self.free_pages,
-                              self._ring[0], self._ring[1], stream=stream)
-        self._ring.reverse()
-        with on_stream(stream):
+        with OnStream(stream, rows, *self._tables()):
+            H.hybrid_page_release(self.pg, self.n_req, rows, rows.numel(), self._lens[0], self.block_table, self.free_pages,
+                                  self._ring[0], self._ring[1])
+            self._ring.reverse()
             there = (rows >= 0) & (rows < self.n_req)
             self._lens_all[0].index_fill_(0, torch.where(there, rows, self.n_req).long(), 0)

@@ -9,7 +9,7 @@ from __future__ import annotations
 import torch
 
 from . import hybrid as H
-from .page_pool import PagePool
+from .page_pool import OnStream, PagePool
 
 
 class SoftmaxLayer:
@@ -27,18 +27,21 @@ class SoftmaxLayer:
     def write(self, qkv, pool: PagePool, layer: int, slots, positions, stream=None):
         """Normalise and rotate; keys and values go to their slots.  Returns the queries."""
         q, k, v = self.split(qkv)
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        H.hybrid_qk_norm_rope_cache(self.cfg, self.rope, pool.pg, q, q.stride(0), k, k.stride(0), v, v.stride(0), q.shape[0],
-                                    self.wq, self.wk, positions, self.freqs, slots, out, pool.k_cache[layer],
-                                    pool.v_cache[layer], stream=stream)
-        return out
+        kc, vc = pool.k_cache[layer], pool.v_cache[layer]
+        with OnStream(stream, qkv, slots, positions, self.wq, self.wk, self.freqs, kc, vc) as on:
+            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            H.hybrid_qk_norm_rope_cache(self.cfg, self.rope, pool.pg, q, q.stride(0), k, k.stride(0), v, v.stride(0), q.shape[0],
+                                        self.wq, self.wk, positions, self.freqs, slots, out, kc, vc)
+            return on.returns(out)
 
     def attend(self, q, pool: PagePool, layer: int, stream=None):
         """q [n_req * B, Hq, d] of the active blocks against the cache -> the same shape."""
-        out = torch.empty_like(q)
-        H.hybrid_paged_attn(self.cfg, pool.pg, q, pool.k_cache[layer], pool.v_cache[layer], pool.block_table, pool.lens,
-                            pool.n_req, self.window, self.n_sink, out, pool.workspace, pool.workspace_bytes, stream=stream)
-        return out
+        kc, vc = pool.k_cache[layer], pool.v_cache[layer]
+        with OnStream(stream, q, kc, vc, pool.block_table, pool.lens, pool.workspace) as on:
+            out = torch.empty_like(q)
+            H.hybrid_paged_attn(self.cfg, pool.pg, q, kc, vc, pool.block_table, pool.lens, pool.n_req, self.window, self.n_sink,
+                                out, pool.workspace, pool.workspace_bytes)
+            return on.returns(out)
 
     def step(self, qkv, pool: PagePool, layer: int, slots, positions, stream=None):
         """One denoising step of the active blocks (or, with B = 1, one token)."""

@@ -5,6 +5,7 @@ import torch
 
 from paper_2608_06628_gb300 import hybrid as H
 from paper_2608_06628_gb300.page_pool import PagePool
+from paper_2608_06628_gb300.softmax_layer import SoftmaxLayer
 
 pytestmark = pytest.mark.gpu
 BF, F32 = torch.bfloat16, torch.float32
@@ -72,3 +73,65 @@ def test_release_leaves_out_rows_that_are_not_there(rows, lens, free):
     pool.append(i32([3, 4, 2]), 9)
     H.hybrid_check()
     assert pool.lens.tolist() == [x + y for x, y in zip(lens, [3, 4, 2])]
+
+
+def layer_of(pool, **kw):
+    return SoftmaxLayer(pool.cfg, H.make_rope(pool.cfg.head_dim), **kw)
+
+
+def same_call(make):
+    """make(stream) on a late stream, its arguments and results dropped before it has run, while the current
+    stream takes memory of every size that they had: returns what the call gives on the current stream, on
+    the late one, and whether the other memory kept what was written to it."""
+    s = torch.cuda.Stream()
+    make(s)
+    want = [x.clone() for x in make(None)]
+    torch.cuda.synchronize()
+    late(s)
+    got = make(s)
+    kept = []
+    with torch.cuda.stream(s):
+        kept = [x.clone() for x in got]                      # of the late stream, behind the call
+    sizes = [x.nbytes for x in got]
+    del got
+    other = [torch.full((n // 4,), 55, dtype=torch.int32, device="cuda") for n in sizes for _ in range(4)]
+    torch.cuda.synchronize()
+    H.hybrid_check()
+    return want, kept, all(bool((x == 55).all()) for x in other)
+
+
+def test_append_on_another_stream_keeps_its_memory():
+    new = [1000, 1000, 48]
+
+    def append(stream):
+        pool = PagePool(H.make_cfg(64, 64, 2, 1, 4, F32), 3, 400, 4096, 16)
+        torch.cuda.current_stream().synchronize()
+        n_new = i32(new)
+        got = pool.append(n_new, 2048, stream=stream)
+        del n_new
+        torch.zeros(3, dtype=torch.int32, device="cuda")     # in the place of n_new, where that is free
+        return (*got, pool.lens)
+
+    want, got, intact = same_call(append)
+    assert intact and all(torch.equal(x, y) for x, y in zip(got, want))
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
+def test_layer_on_another_stream_keeps_its_memory(dt):
+    cfg = H.make_cfg(64, 64, 4, 2, 2, dt)
+    pool = pool_of([300, 200, 100], 60, cfg, 400)
+    pool.k_cache.normal_()
+    pool.v_cache.normal_()
+    layer = layer_of(pool)
+    slots, positions, _ = pool.append(i32([2, 2, 2]), 6)
+    x = torch.randn(6, 8 * 64, device="cuda").to(dt)
+    torch.cuda.synchronize()
+
+    def step(stream):
+        q = layer.write(x.clone(), pool, 0, slots.clone(), positions.clone(), stream)
+        torch.zeros_like(x), torch.zeros_like(slots), torch.zeros_like(slots)    # in the place of the copies
+        return q, layer.attend(q, pool, 0, stream), layer.step(x, pool, 0, slots, positions, stream)
+
+    # (the copies are made on the current stream, which has to be done before the late one begins: it is late)
+    want, got, intact = same_call(step)
+    assert intact and all(torch.equal(a, b) for a, b in zip(got, want))
