@@ -29,9 +29,8 @@ class OnStream:
             handle = stream if isinstance(stream, int) else stream.cuda_stream
             stream = torch.cuda.ExternalStream(handle) if handle else torch.cuda.default_stream()
         self.caller, self.scope = torch.cuda.current_stream(), torch.cuda.stream(stream)
-        for x in used:
-            if x is not None:
-                x.record_stream(stream)
+        self.stream = stream
+        self.uses(*used)
 
     def __enter__(self):
         self.scope.__enter__()
@@ -39,6 +38,12 @@ class OnStream:
 
     def __exit__(self, *exc):
         return self.scope.__exit__(*exc)
+
+    def uses(self, *used):
+        if self.caller is not None:
+            for x in used:
+                if x is not None:
+                    x.record_stream(self.stream)
 
     def returns(self, *made):
         if self.caller is not None:
@@ -67,6 +72,7 @@ class PagePool:
         if self.workspace_bytes == 0:
             raise ValueError(f"unsupported {cfg} with {self.pg}")
         self.workspace = torch.empty(self.workspace_bytes, dtype=torch.uint8, device=device)
+        self._workspaces = {}
 
     @property
     def lens(self) -> torch.Tensor:
@@ -80,6 +86,22 @@ class PagePool:
 
     def _tables(self):
         return (*self._lens, *self._ring, self.block_table, self.free_pages)
+
+    def workspace_of(self, cfg: H.hybrid_cfg, on: OnStream) -> torch.Tensor:
+        """Attention's workspace for a layer's cfg on the call's stream: calls on several streams may overlap, and need
+        one each. (Graphs captured on one stream share one: replays of them must not overlap.)"""
+        geometry = tuple(getattr(cfg, name) for name, _ in cfg._fields_)
+        key = (H._stream(None), geometry)
+        if key not in self._workspaces:
+            if not self._workspaces and geometry == tuple(getattr(self.cfg, name) for name, _ in cfg._fields_):
+                self._workspaces[key] = self.workspace
+            else:
+                n = H.hybrid_paged_attn_workspace_bytes(cfg, self.pg, self.n_req)
+                if n == 0:
+                    raise ValueError(f"unsupported {cfg} with {self.pg}")
+                self._workspaces[key] = torch.empty(n, dtype=torch.uint8, device=self.device)
+        on.uses(self._workspaces[key])
+        return self._workspaces[key]
 
     def append(self, n_new: torch.Tensor, n_tok: int, stream=None):
         """Room for n_new [n_req] (int32, device) more tokens of each request, at most n_tok in all.

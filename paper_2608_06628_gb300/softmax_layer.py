@@ -37,10 +37,10 @@ class SoftmaxLayer:
     def attend(self, q, pool: PagePool, layer: int, stream=None):
         """q [n_req * B, Hq, d] of the active blocks against the cache -> the same shape."""
         kc, vc = pool.k_cache[layer], pool.v_cache[layer]
-        with OnStream(stream, q, kc, vc, pool.block_table, pool.lens, pool.workspace) as on:
-            out = torch.empty_like(q)
+        with OnStream(stream, q, kc, vc, pool.block_table, pool.lens) as on:
+            out, workspace = torch.empty_like(q), pool.workspace_of(self.cfg, on)
             H.hybrid_paged_attn(self.cfg, pool.pg, q, kc, vc, pool.block_table, pool.lens, pool.n_req, self.window, self.n_sink,
-                                out, pool.workspace, pool.workspace_bytes)
+                                out, workspace, workspace.numel())
             return on.returns(out)
 
     def step(self, qkv, pool: PagePool, layer: int, slots, positions, stream=None):

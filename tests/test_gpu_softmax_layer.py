@@ -135,3 +135,59 @@ def test_layer_on_another_stream_keeps_its_memory(dt):
     # (the copies are made on the current stream, which has to be done before the late one begins: it is late)
     want, got, intact = same_call(step)
     assert intact and all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def filled(cfg, new, n_pages, max_len):
+    pool = pool_of(new, n_pages, cfg, max_len)
+    pool.k_cache.normal_()
+    pool.v_cache.normal_()
+    return pool
+
+
+def test_streams_have_workspaces_of_their_own(monkeypatch):
+    cfg = H.make_cfg(64, 64, 4, 2, 2, BF)
+    pool = filled(cfg, [300, 200, 100], 60, 400)
+    layer, q = layer_of(pool), torch.randn(6, 4, 64, device="cuda").to(BF)
+    seen, call = [], H.hybrid_paged_attn
+
+    def note(*args, **kw):
+        seen.append(args[11].data_ptr())
+        return call(*args, **kw)
+
+    monkeypatch.setattr(H, "hybrid_paged_attn", note)
+    a, b = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for s in (None, a, b, a, None, b):
+        layer.attend(q, pool, 0, s)
+    H.hybrid_check()
+    assert len(set(seen[:3])) == 3 and seen[3:] == [seen[1], seen[0], seen[2]]
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
+def test_attention_on_two_streams_at_once(dt):
+    """Contexts that are split over many blocks, so that every call has partial results in its workspace."""
+    cfg = H.make_cfg(128, 64, 8, 2, 16, dt)
+    pool = filled(cfg, [9000, 20000, 700], 1900, 20000)
+    layer = layer_of(pool)
+    q = [torch.randn(48, 8, 128, device="cuda").to(dt) for _ in range(2)]
+    want = [layer.attend(x, pool, 0) for x in q]
+    streams = [torch.cuda.Stream() for _ in q]
+    torch.cuda.synchronize()
+    got = [layer.attend(q[i], pool, 0, streams[i]) for _ in range(20) for i in range(2)]
+    torch.cuda.synchronize()
+    H.hybrid_check()
+    assert all(torch.equal(x, want[i % 2]) for i, x in enumerate(got))
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
+def test_attention_of_layers_with_other_rows_than_the_pool(dt):
+    """The pool is made for single tokens of 4 heads; the layer asks for blocks of 33 of 6 heads."""
+    import softmax_reference as R
+    from gpu_harness import assert_parity
+    pool = filled(H.make_cfg(64, 64, 4, 2, 1, dt), [300, 0, 5000], 400, 5000)
+    layer = SoftmaxLayer(H.make_cfg(64, 64, 6, 2, 33, dt), H.make_rope(64))
+    q = torch.randn(99, 6, 64, device="cuda").to(dt)
+    got = layer.attend(q, pool, 0)
+    H.hybrid_check()
+    want = R.paged_attention(q.view(3, 33, 6, 64), pool.k_cache[0], pool.v_cache[0], pool.block_table, pool.lens.tolist(), 0, 0)
+    assert_parity(got.view(want.shape).double().cpu().numpy(), want.cpu().numpy(), dt, "blocks of 33", units="out")
