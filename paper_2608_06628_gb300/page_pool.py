@@ -15,6 +15,15 @@ import torch
 from . import hybrid as H
 
 
+def expect(x, what: str, dtype, device, *shape, rows=False):
+    """ValueError unless x is a tensor of that type and shape on that device: dense, or (rows) with dense rows."""
+    if isinstance(x, torch.Tensor) and x.dtype == dtype and tuple(x.shape) == shape and x.device == device and \
+            (x.is_contiguous() or (rows and x.stride(-1) == 1)):
+        return
+    has = f"{x.dtype} {list(x.shape)}, strides {x.stride()}, on {x.device}" if isinstance(x, torch.Tensor) else type(x).__name__
+    raise ValueError(f"{what}: {has} where a dense {dtype} {list(shape)} on {device} is wanted")
+
+
 class OnStream:
     """A call's work on its stream (None: the current one; else torch's stream or a raw handle): torch's own kernels
     and allocations go there too. `used` is what the work reads and writes besides: its memory is not handed out again
@@ -61,7 +70,7 @@ class PagePool:
         shape = (n_layers, n_pages, cfg.n_kv_heads, page_size, cfg.head_dim)
         self.k_cache = torch.empty(shape, dtype=dtype, device=device)
         self.v_cache = torch.empty(shape, dtype=dtype, device=device)
-        self.device = torch.device(device)
+        self.device = self.k_cache.device
         self.block_table = torch.full((n_req, self.pg.max_pages), -1, dtype=torch.int32, device=device)
         self.free_pages = torch.arange(n_pages, dtype=torch.int32, device=device)
         # the lengths and an entry more, which release() writes for rows that are not there
@@ -107,6 +116,7 @@ class PagePool:
         """Room for n_new [n_req] (int32, device) more tokens of each request, at most n_tok in all.
         Returns slots, positions [n_tok] and tok_offsets [n_req + 1] (int32); slots beyond the last
         token, and of requests that did not fit (see hybrid_check), are -1."""
+        expect(n_new, "n_new", torch.int32, self.device, self.n_req)
         new = lambda n: torch.empty(n, dtype=torch.int32, device=self.device)  # noqa: E731
         with OnStream(stream, n_new, *self._tables()) as on:
             slots, positions, offsets = new(n_tok), new(n_tok), new(self.n_req + 1)
@@ -120,6 +130,7 @@ class PagePool:
     def release(self, rows: torch.Tensor, stream=None):
         """Give back the pages of the requests in rows (int32, device, each once); their lengths become 0, on the
         same stream. A row out of range is left out, and reported by hybrid_check."""
+        expect(rows, "rows", torch.int32, self.device, rows.numel())
         with OnStream(stream, rows, *self._tables()):
             H.hybrid_page_release(self.pg, self.n_req, rows, rows.numel(), self._lens[0], self.block_table, self.free_pages,
                                   self._ring[0], self._ring[1])

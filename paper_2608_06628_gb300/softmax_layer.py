@@ -2,14 +2,17 @@
 keys with the cache write in one pass, then attention over the paged cache.
 
 A layer works on the output of its fused projection, qkv [tokens, (Hq + 2 Hkv) d], and on a
-PagePool whose append() has made room for those tokens.
+PagePool whose append() has made room for those tokens. Shapes, types and layouts are checked
+(ValueError) before anything is launched.
 """
 from __future__ import annotations
+
+import math
 
 import torch
 
 from . import hybrid as H
-from .page_pool import OnStream, PagePool
+from .page_pool import OnStream, PagePool, expect
 
 
 class SoftmaxLayer:
@@ -17,6 +20,7 @@ class SoftmaxLayer:
         """rope: what hybrid.make_rope returns; wq, wk: norm weights [d] in the io type, or None."""
         self.cfg, (self.rope, self.freqs) = cfg, rope
         self.wq, self.wk, self.window, self.n_sink = wq, wk, window, n_sink
+        self.dtype = torch.bfloat16 if cfg.io_dtype == H.HYBRID_BF16 else torch.float32
 
     def split(self, qkv):
         """Q, K, V as views [tokens, heads, d] of the projection's output."""
@@ -26,16 +30,29 @@ class SoftmaxLayer:
 
     def write(self, qkv, pool: PagePool, layer: int, slots, positions, stream=None):
         """Normalise and rotate; keys and values go to their slots.  Returns the queries."""
+        c, dev, n_tok = self.cfg, pool.device, qkv.shape[0]
+        expect(qkv, "qkv", self.dtype, dev, n_tok, (c.n_q_heads + 2 * c.n_kv_heads) * c.head_dim, rows=True)
+        expect(slots, "slots", torch.int32, dev, max(n_tok, slots.numel()))
+        if self.rope.rot_dim:
+            expect(positions, "positions", torch.int32, dev, max(n_tok, positions.numel()))
+            expect(self.freqs, "freqs", torch.int64, dev, self.rope.rot_dim // 2)
+        for x, what in ((self.wq, "wq"), (self.wk, "wk")):
+            if x is not None:
+                expect(x, what, self.dtype, dev, c.head_dim)
         q, k, v = self.split(qkv)
+        step = qkv.stride(0) if n_tok > 1 else qkv.shape[1]      # (of a single row torch may report any)
         kc, vc = pool.k_cache[layer], pool.v_cache[layer]
         with OnStream(stream, qkv, slots, positions, self.wq, self.wk, self.freqs, kc, vc) as on:
             out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-            H.hybrid_qk_norm_rope_cache(self.cfg, self.rope, pool.pg, q, q.stride(0), k, k.stride(0), v, v.stride(0), q.shape[0],
-                                        self.wq, self.wk, positions, self.freqs, slots, out, kc, vc)
+            H.hybrid_qk_norm_rope_cache(self.cfg, self.rope, pool.pg, q, step, k, step, v, step, n_tok, self.wq, self.wk,
+                                        positions, self.freqs, slots, out, kc, vc)
             return on.returns(out)
 
     def attend(self, q, pool: PagePool, layer: int, stream=None):
         """q [n_req * B, Hq, d] of the active blocks against the cache -> the same shape."""
+        c, rows = self.cfg, pool.n_req * self.cfg.block_size
+        lead = q.shape[:-2] if math.prod(q.shape[:-2]) == rows else (rows,)
+        expect(q, "q", self.dtype, pool.device, *lead, c.n_q_heads, c.head_dim)
         kc, vc = pool.k_cache[layer], pool.v_cache[layer]
         with OnStream(stream, q, kc, vc, pool.block_table, pool.lens) as on:
             out, workspace = torch.empty_like(q), pool.workspace_of(self.cfg, on)

@@ -1,0 +1,114 @@
+"""The checks of the pool and the layer of the softmax layers on the host: what does not fit is refused before
+the library is called."""
+import pytest
+import torch
+
+from paper_2608_06628_gb300 import build as B
+from paper_2608_06628_gb300 import hybrid as H
+from paper_2608_06628_gb300.page_pool import PagePool
+from paper_2608_06628_gb300.softmax_layer import SoftmaxLayer
+
+BF, F32, I32 = torch.bfloat16, torch.float32, torch.int32
+HQ, HKV, D, BS, N = 4, 2, 64, 2, 3
+WIDTH = (HQ + 2 * HKV) * D
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _library():
+    B.build()
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    """The entry points that were reached, with their arguments."""
+    seen = []
+    for name in ("hybrid_page_append", "hybrid_page_release", "hybrid_qk_norm_rope_cache", "hybrid_paged_attn"):
+        monkeypatch.setattr(H, name, lambda *a, _name=name, **kw: seen.append((_name, a)))
+    monkeypatch.setattr(H, "_stream", lambda stream: 0 if stream is None else stream)
+    return seen
+
+
+def cfg(d=D, Hq=HQ, Hkv=HKV, Bs=BS, dt=F32):
+    return H.make_cfg(d, 64, Hq, Hkv, Bs, dt)
+
+
+def pool(**kw):
+    return PagePool(cfg(**kw), N, 20, 64, 16, device="cpu")
+
+
+def layer(c=None, rot=D, **kw):
+    return SoftmaxLayer(c or cfg(), H.make_rope(rot, device="cpu"), **kw)
+
+
+def ints(n, dtype=I32):
+    return torch.zeros(n, dtype=dtype)
+
+
+def wide(n):
+    """Every second entry of twice as many."""
+    return torch.zeros(2 * n, dtype=I32)[::2]
+
+
+@pytest.mark.parametrize("n_new", [ints(N, torch.int64), ints(N - 1), ints(N + 1), wide(N), ints(N).view(1, N), torch.zeros(N), [1, 2, 3]])
+def test_append_refuses(calls, n_new):
+    with pytest.raises(ValueError, match="n_new"):
+        pool().append(n_new, 6)
+    assert not calls
+
+
+@pytest.mark.parametrize("rows", [ints(2, torch.int64), wide(2), ints(2).view(2, 1), torch.zeros(2), torch.zeros(2, dtype=torch.bool)])
+def test_release_refuses(calls, rows):
+    with pytest.raises(ValueError, match="rows"):
+        pool().release(rows)
+    assert not calls
+
+
+@pytest.mark.parametrize("what,kw", [
+    ("qkv", dict(qkv=torch.zeros(6, WIDTH, dtype=BF))), ("qkv", dict(qkv=torch.zeros(6, WIDTH + 1))),
+    ("qkv", dict(qkv=torch.zeros(WIDTH, 6).t())), ("qkv", dict(qkv=torch.zeros(1, 6, WIDTH))), ("qkv", dict(qkv=torch.zeros(WIDTH))),
+    ("slots", dict(slots=ints(6, torch.int64))), ("slots", dict(slots=ints(5))), ("slots", dict(slots=wide(6))),
+    ("positions", dict(positions=ints(6, torch.int64))), ("positions", dict(positions=ints(5))),
+    ("positions", dict(positions=wide(6))),
+])
+def test_write_refuses(calls, what, kw):
+    args = dict(qkv=torch.zeros(6, WIDTH), slots=ints(6), positions=ints(6))
+    with pytest.raises(ValueError, match=what):
+        layer().write(pool=pool(), layer=0, **{**args, **kw})
+    assert not calls
+
+
+@pytest.mark.parametrize("what,kw", [("wq", dict(wq=torch.ones(D, dtype=BF))), ("wk", dict(wk=torch.ones(D + 1))),
+                                     ("wq", dict(wq=torch.ones(2 * D)[::2]))])
+def test_write_refuses_weights(calls, what, kw):
+    with pytest.raises(ValueError, match=what):
+        layer(**kw).write(torch.zeros(6, WIDTH), pool(), 0, ints(6), ints(6))
+    assert not calls
+
+
+@pytest.mark.parametrize("q", [torch.zeros(N * BS - 1, HQ, D), torch.zeros(N * BS + 1, HQ, D), torch.zeros(N * BS, HQ, D, dtype=BF),
+                               torch.zeros(N * BS, D, HQ).transpose(1, 2), torch.zeros(N * BS, HQ, 2 * D)[..., :D],
+                               torch.zeros(N * BS, HQ * D), torch.zeros(0, HQ, D)])
+def test_attend_refuses(calls, q):
+    with pytest.raises(ValueError, match="q:"):
+        layer().attend(q, pool(), 0)
+    assert not calls
+
+
+def test_step_refuses_part_of_a_batch(calls):
+    with pytest.raises(ValueError, match="q:"):
+        layer().step(torch.zeros(4, WIDTH), pool(), 0, ints(4), ints(4))
+
+
+def test_what_fits_goes_through(calls):
+    p = pool()
+    p.append(ints(N), 6)
+    p.release(ints(0))
+    out = layer(wq=torch.ones(D), wk=torch.ones(D)).write(torch.zeros(6, WIDTH + 8)[:, :WIDTH], p, 0, ints(9), ints(6))
+    assert out.shape == (6, HQ, D) and calls[-1][0] == "hybrid_qk_norm_rope_cache" and calls[-1][1][4] == WIDTH + 8
+    # one row, of which torch may report any stride; nothing rotated, so no positions
+    layer(rot=0).write(torch.zeros(WIDTH).expand(1, WIDTH), p, 0, ints(1), None)
+    assert calls[-1][1][4] == calls[-1][1][6] == calls[-1][1][8] == WIDTH
+    layer().write(torch.zeros(0, WIDTH), p, 0, ints(0), ints(0))
+    for lead in ((N * BS,), (N, BS)):
+        assert layer().attend(torch.zeros(*lead, HQ, D), p, 0).shape == (*lead, HQ, D)
+    assert [name for name, _ in calls].count("hybrid_paged_attn") == 2
