@@ -61,6 +61,24 @@ class OnStream:
         return made[0] if len(made) == 1 else made
 
 
+class BlockRows:
+    """Where the packed tokens of an append stand among the n_req * B query rows of attention, whose row r * B + i is
+    token i of request r: for batches where a request has fewer than B new tokens, or none."""
+
+    def __init__(self, offsets, n_req: int, n_tok: int, block: int):
+        self.n_tok, self.n_rows, dev = n_tok, n_req * block, offsets.device
+        offsets = offsets.long()
+        of_row = (offsets[:-1, None] + torch.arange(block, device=dev)).flatten()
+        # rows without a token repeat one: nothing reads what they give
+        self.token = of_row.clamp(0, max(n_tok - 1, 0))
+        t = torch.arange(n_tok, device=dev)
+        r = torch.searchsorted(offsets[1:].contiguous(), t, right=True)
+        i = t - offsets[r]
+        # the row of a token; beyond the last token n_rows, beyond its request's first B tokens n_rows + 1
+        row = torch.where(i < block, r * block + i, self.n_rows + 1)
+        self.row = torch.where(r < n_req, row, self.n_rows).clamp(0, self.n_rows + 1)
+
+
 class PagePool:
     def __init__(self, cfg: H.hybrid_cfg, n_req: int, n_pages: int, max_len: int, page_size: int = 32, n_layers: int = 1,
                  device="cuda"):
@@ -115,7 +133,8 @@ class PagePool:
     def append(self, n_new: torch.Tensor, n_tok: int, stream=None):
         """Room for n_new [n_req] (int32, device) more tokens of each request, at most n_tok in all.
         Returns slots, positions [n_tok] and tok_offsets [n_req + 1] (int32); slots beyond the last
-        token, and of requests that did not fit (see hybrid_check), are -1."""
+        token, and of requests that did not fit (see hybrid_check), are -1. Tokens are packed by request:
+        see block_rows where not every request has a whole block of them."""
         expect(n_new, "n_new", torch.int32, self.device, self.n_req)
         new = lambda n: torch.empty(n, dtype=torch.int32, device=self.device)  # noqa: E731
         with OnStream(stream, n_new, *self._tables()) as on:
@@ -126,6 +145,15 @@ class PagePool:
             self._lens_all.reverse()
             self._ring.reverse()
             return on.returns(slots, positions, offsets)
+
+    def block_rows(self, offsets: torch.Tensor, n_tok: int, block: int | None = None, stream=None) -> BlockRows:
+        """For SoftmaxLayer.attend and step, once per append: which query row each of its n_tok packed tokens has.
+        offsets: the append's tok_offsets; block: the layers' block size (None: the pool's)."""
+        expect(offsets, "offsets", torch.int32, self.device, self.n_req + 1)
+        with OnStream(stream, offsets) as on:
+            rows = BlockRows(offsets, self.n_req, n_tok, block or self.cfg.block_size)
+            on.returns(rows.token, rows.row)
+            return rows
 
     def release(self, rows: torch.Tensor, stream=None):
         """Give back the pages of the requests in rows (int32, device, each once); their lengths become 0, on the

@@ -4,6 +4,10 @@ keys with the cache write in one pass, then attention over the paged cache.
 A layer works on the output of its fused projection, qkv [tokens, (Hq + 2 Hkv) d], and on a
 PagePool whose append() has made room for those tokens. Shapes, types and layouts are checked
 (ValueError) before anything is launched.
+
+    slots, positions, offsets = pool.append(n_new, n_tok)
+    rows = pool.block_rows(offsets, n_tok)     # unless every request has a whole block of new tokens
+    out = layer.step(qkv, pool, i, slots, positions, rows=rows)
 """
 from __future__ import annotations
 
@@ -12,7 +16,7 @@ import math
 import torch
 
 from . import hybrid as H
-from .page_pool import OnStream, PagePool, expect
+from .page_pool import BlockRows, OnStream, PagePool, expect
 
 
 class SoftmaxLayer:
@@ -48,18 +52,37 @@ class SoftmaxLayer:
                                         positions, self.freqs, slots, out, kc, vc)
             return on.returns(out)
 
-    def attend(self, q, pool: PagePool, layer: int, stream=None):
-        """q [n_req * B, Hq, d] of the active blocks against the cache -> the same shape."""
-        c, rows = self.cfg, pool.n_req * self.cfg.block_size
-        lead = q.shape[:-2] if math.prod(q.shape[:-2]) == rows else (rows,)
+    def attend(self, q, pool: PagePool, layer: int, stream=None, rows: BlockRows | None = None):
+        """Queries of the active blocks against the cache -> the same shape.
+
+        q [n_req * B, Hq, d]: token i of request r in row r * B + i, so that every request has B tokens. With rows
+        (pool.block_rows), q [n_tok, Hq, d] is packed by request as pool.append packs it; outputs beyond the last token
+        are zeros, and of a request's tokens beyond its first B NaN: attention has no row for them."""
+        c, n_rows = self.cfg, pool.n_req * self.cfg.block_size
+        if rows is None:
+            lead = q.shape[:-2] if math.prod(q.shape[:-2]) == n_rows else (n_rows,)
+        elif rows.n_rows != n_rows:
+            raise ValueError(f"rows: made for {rows.n_rows} query rows, not for {n_rows}")
+        else:
+            lead = (rows.n_tok,)
         expect(q, "q", self.dtype, pool.device, *lead, c.n_q_heads, c.head_dim)
         kc, vc = pool.k_cache[layer], pool.v_cache[layer]
         with OnStream(stream, q, kc, vc, pool.block_table, pool.lens) as on:
-            out, workspace = torch.empty_like(q), pool.workspace_of(self.cfg, on)
-            H.hybrid_paged_attn(self.cfg, pool.pg, q, kc, vc, pool.block_table, pool.lens, pool.n_req, self.window, self.n_sink,
+            if rows is None:
+                out = torch.empty_like(q)
+            else:
+                on.uses(rows.token, rows.row)
+                if rows.n_tok == 0:
+                    return on.returns(torch.empty_like(q))
+                q = q.index_select(0, rows.token)
+                out = torch.empty((n_rows + 2, *q.shape[1:]), dtype=q.dtype, device=q.device)
+                out[n_rows].zero_()
+                out[n_rows + 1].fill_(math.nan)
+            workspace = pool.workspace_of(c, on)
+            H.hybrid_paged_attn(c, pool.pg, q, kc, vc, pool.block_table, pool.lens, pool.n_req, self.window, self.n_sink,
                                 out, workspace, workspace.numel())
-            return on.returns(out)
+            return on.returns(out if rows is None else out.index_select(0, rows.row))
 
-    def step(self, qkv, pool: PagePool, layer: int, slots, positions, stream=None):
-        """One denoising step of the active blocks (or, with B = 1, one token)."""
-        return self.attend(self.write(qkv, pool, layer, slots, positions, stream), pool, layer, stream)
+    def step(self, qkv, pool: PagePool, layer: int, slots, positions, stream=None, rows: BlockRows | None = None):
+        """One denoising step of the active blocks (or, with B = 1, one token); rows: see attend."""
+        return self.attend(self.write(qkv, pool, layer, slots, positions, stream), pool, layer, stream, rows)

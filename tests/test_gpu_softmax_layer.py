@@ -3,6 +3,8 @@ rows, graphs, and infinities in the cache."""
 import pytest
 import torch
 
+import softmax_reference as R
+from gpu_harness import assert_parity
 from paper_2608_06628_gb300 import hybrid as H
 from paper_2608_06628_gb300.page_pool import PagePool
 from paper_2608_06628_gb300.softmax_layer import SoftmaxLayer
@@ -182,8 +184,6 @@ def test_attention_on_two_streams_at_once(dt):
 @pytest.mark.parametrize("dt", [BF, F32])
 def test_attention_of_layers_with_other_rows_than_the_pool(dt):
     """The pool is made for single tokens of 4 heads; the layer asks for blocks of 33 of 6 heads."""
-    import softmax_reference as R
-    from gpu_harness import assert_parity
     pool = filled(H.make_cfg(64, 64, 4, 2, 1, dt), [300, 0, 5000], 400, 5000)
     layer = SoftmaxLayer(H.make_cfg(64, 64, 6, 2, 33, dt), H.make_rope(64))
     q = torch.randn(99, 6, 64, device="cuda").to(dt)
@@ -191,3 +191,40 @@ def test_attention_of_layers_with_other_rows_than_the_pool(dt):
     H.hybrid_check()
     want = R.paged_attention(q.view(3, 33, 6, 64), pool.k_cache[0], pool.v_cache[0], pool.block_table, pool.lens.tolist(), 0, 0)
     assert_parity(got.view(want.shape).double().cpu().numpy(), want.cpu().numpy(), dt, "blocks of 33", units="out")
+
+
+# ------------------------------------------------------------------ batches with idle rows
+
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("pad", [0, 3])
+def test_decoding_after_a_middle_and_the_last_row_are_released(dt, pad):
+    """Two blocks, the second for the requests that are left, one of which has fewer tokens than a block."""
+    B, n = 4, 5
+    cfg = H.make_cfg(64, 64, 4, 2, B, dt)
+    pool = PagePool(cfg, n, 200, 600, 16)
+    layer = layer_of(pool)
+
+    def block(new, n_tok):
+        slots, positions, offsets = pool.append(i32(new), n_tok)
+        x = torch.randn(n_tok, 8 * 64, device="cuda").to(dt)
+        if max(new) > B:
+            return layer.write(x, pool, 0, slots, positions)
+        rows = pool.block_rows(offsets, n_tok)
+        q = layer.write(x, pool, 0, slots, positions)
+        out = layer.attend(q, pool, 0, rows=rows)
+        assert torch.equal(out, layer.step(x, pool, 0, slots, positions, rows=rows))     # (writes the same again)
+        H.hybrid_check()
+        lens, at = pool.lens.tolist(), 0
+        for r, m in enumerate(new):
+            if m:
+                want = R.paged_attention(q[at:at + m][None], pool.k_cache[0], pool.v_cache[0], pool.block_table[r:r + 1], lens[r:r + 1], 0, 0)
+                assert_parity(out[at:at + m][None].double().cpu().numpy(), want.cpu().numpy(), dt, f"request {r}", units="out")
+            at += m
+        assert not bool(out[at:].any())
+
+    block([130, 7, 300, 16, 45], 498)
+    block([B] * n, n * B + pad)
+    pool.release(i32([2, 4]))
+    block([B, B - 1, 0, B, 0], 3 * B - 1 + pad)
+    block([B, B, 0, B, 0], n * B)                            # as many as query rows, but not in their places
+    block([0, 0, 0, 1, 0], 1 + pad)

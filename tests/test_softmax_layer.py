@@ -112,3 +112,50 @@ def test_what_fits_goes_through(calls):
     for lead in ((N * BS,), (N, BS)):
         assert layer().attend(torch.zeros(*lead, HQ, D), p, 0).shape == (*lead, HQ, D)
     assert [name for name, _ in calls].count("hybrid_paged_attn") == 2
+
+
+@pytest.mark.parametrize("new,n_tok", [([2, 0, 2], 4), ([2, 0, 2], 6), ([0, 1, 0], 1), ([1, 2, 1], 9), ([0, 0, 0], 3), ([0, 0, 0], 0),
+                                       ([3, 0, 5], 8), ([2, 2, 2], 6)])
+def test_packed_tokens_and_query_rows(calls, monkeypatch, new, n_tok):
+    """Attention that returns its queries: every token gets its own back, from the row of its request."""
+    taken = []
+
+    def same(cfg, pg, q, *args, **kw):
+        taken.append(q.clone())
+        args[7][:q.shape[0]] = q
+
+    monkeypatch.setattr(H, "hybrid_paged_attn", same)
+    p, offs = pool(), torch.tensor([0, *torch.tensor(new).cumsum(0).tolist()], dtype=I32)
+    rows = p.block_rows(offs, n_tok)
+    q = (torch.arange(n_tok * HQ * D, dtype=F32) + 1).view(n_tok, HQ, D)
+    out = layer().attend(q, p, 0, rows=rows)
+    assert out.shape == q.shape and len(taken) == (n_tok > 0)
+    t = 0
+    for r, n in enumerate(new):
+        for i in range(n):
+            if i < BS:
+                assert torch.equal(out[t], q[t]) and torch.equal(taken[0][r * BS + i], q[t])
+            else:
+                assert bool(out[t].isnan().all())
+            t += 1
+    assert not bool(out[t:].any())
+
+
+def test_packed_rows_refused(calls):
+    p, offs = pool(), torch.tensor([0, 2, 4, 6], dtype=I32)
+    for bad in (offs.long(), offs[:3], torch.zeros(8, dtype=I32)[::2]):
+        with pytest.raises(ValueError, match="offsets"):
+            p.block_rows(bad, 6)
+    with pytest.raises(ValueError, match="rows"):
+        layer().attend(torch.zeros(6, HQ, D), p, 0, rows=p.block_rows(offs, 6, 5))
+    with pytest.raises(ValueError, match="q:"):
+        layer().attend(torch.zeros(5, HQ, D), p, 0, rows=p.block_rows(offs, 6))
+    assert not calls
+
+
+def test_offsets_out_of_range_index_nothing(calls):
+    """Offsets that no append gives (they are the caller's memory) stay within the tensors."""
+    p = pool()
+    for offs in ([0, 900, -5, 2 ** 31 - 1], [-9, -7, -3, -1], [2 ** 31 - 1, 0, 0, 4]):
+        rows = p.block_rows(torch.tensor(offs, dtype=I32), 6)
+        assert 0 <= int(rows.token.min()) and int(rows.token.max()) < 6 and 0 <= int(rows.row.min()) and int(rows.row.max()) <= N * BS + 1
