@@ -26,6 +26,12 @@ class SoftmaxLayer:
         self.wq, self.wk, self.window, self.n_sink = wq, wk, window, n_sink
         self.dtype = torch.bfloat16 if cfg.io_dtype == H.HYBRID_BF16 else torch.float32
 
+    def _check_pool(self, pool: PagePool):
+        """The caches are laid out by the pool's cfg and read by the layer's."""
+        for name in ("head_dim", "n_kv_heads", "io_dtype"):
+            if getattr(self.cfg, name) != getattr(pool.cfg, name):
+                raise ValueError(f"pool: its caches are those of {pool.cfg}, the layer's of {self.cfg}")
+
     def split(self, qkv):
         """Q, K, V as views [tokens, heads, d] of the projection's output."""
         c = self.cfg
@@ -34,6 +40,7 @@ class SoftmaxLayer:
 
     def write(self, qkv, pool: PagePool, layer: int, slots, positions, stream=None):
         """Normalise and rotate; keys and values go to their slots.  Returns the queries."""
+        self._check_pool(pool)
         c, dev, n_tok = self.cfg, pool.device, qkv.shape[0]
         expect(qkv, "qkv", self.dtype, dev, n_tok, (c.n_q_heads + 2 * c.n_kv_heads) * c.head_dim, rows=True)
         expect(slots, "slots", torch.int32, dev, max(n_tok, slots.numel()))
@@ -58,6 +65,7 @@ class SoftmaxLayer:
         q [n_req * B, Hq, d]: token i of request r in row r * B + i, so that every request has B tokens. With rows
         (pool.block_rows), q [n_tok, Hq, d] is packed by request as pool.append packs it; outputs beyond the last token
         are zeros, and of a request's tokens beyond its first B NaN: attention has no row for them."""
+        self._check_pool(pool)
         c, n_rows = self.cfg, pool.n_req * self.cfg.block_size
         if rows is None:
             lead = q.shape[:-2] if math.prod(q.shape[:-2]) == n_rows else (n_rows,)

@@ -159,3 +159,24 @@ def test_offsets_out_of_range_index_nothing(calls):
     for offs in ([0, 900, -5, 2 ** 31 - 1], [-9, -7, -3, -1], [2 ** 31 - 1, 0, 0, 4]):
         rows = p.block_rows(torch.tensor(offs, dtype=I32), 6)
         assert 0 <= int(rows.token.min()) and int(rows.token.max()) < 6 and 0 <= int(rows.row.min()) and int(rows.row.max()) <= N * BS + 1
+
+
+@pytest.mark.parametrize("kw", [dict(d=128), dict(Hkv=4), dict(Hkv=1), dict(dt=BF)])
+def test_a_layer_of_other_caches_than_the_pools_is_refused(calls, kw):
+    """More key heads, or a wider type, would write beyond the pool's caches."""
+    c = cfg(**kw)
+    width, dt = (c.n_q_heads + 2 * c.n_kv_heads) * c.head_dim, kw.get("dt", F32)
+    lay = SoftmaxLayer(c, H.make_rope(c.head_dim, device="cpu"))
+    with pytest.raises(ValueError, match="pool"):
+        lay.write(torch.zeros(6, width, dtype=dt), pool(), 0, ints(6), ints(6))
+    with pytest.raises(ValueError, match="pool"):
+        lay.attend(torch.zeros(6, c.n_q_heads, c.head_dim, dtype=dt), pool(), 0)
+    assert not calls
+
+
+@pytest.mark.parametrize("kw", [dict(Bs=1), dict(Bs=64), dict(Hq=8), dict(Hq=2)])
+def test_a_layer_with_other_rows_than_the_pools_is_taken(calls, kw):
+    c = cfg(**kw)
+    SoftmaxLayer(c, H.make_rope(64, device="cpu")).attend(torch.zeros(N * c.block_size, c.n_q_heads, D), pool(), 0)
+    (name, args), = calls
+    assert name == "hybrid_paged_attn" and args[11].numel() == args[12] == H.hybrid_paged_attn_workspace_bytes(c, pool().pg, N)
