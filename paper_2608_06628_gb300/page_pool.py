@@ -1,10 +1,11 @@
 """Paged key-value caches of a model's softmax layers, and the tables that all layers share.
 
 The device holds everything: lengths, block table and the ring of free pages are
-int32 tensors that hybrid_page_append and hybrid_page_release read and write (they
-read one copy of lengths and ring and write another; the pool swaps them), so a
-serving loop never waits for the host to count pages.  Rows of the table are the
-requests of the batch; a released row may take a new request at once.
+int32 tensors that hybrid_page_append and hybrid_page_release read and write, so a
+serving loop never waits for the host to count pages.  Those calls read one copy of
+lengths and ring and write another, which the pool copies back: its tensors stay
+the same ones, and a captured graph may hold any number of calls.  Rows of the table
+are the requests of the batch; a released row may take a new request at once.
 """
 from __future__ import annotations
 
@@ -91,10 +92,10 @@ class PagePool:
         self.device = self.k_cache.device
         self.block_table = torch.full((n_req, self.pg.max_pages), -1, dtype=torch.int32, device=device)
         self.free_pages = torch.arange(n_pages, dtype=torch.int32, device=device)
-        # the lengths and an entry more, which release() writes for rows that are not there
-        self._lens_all = [torch.zeros(n_req + 1, dtype=torch.int32, device=device) for _ in range(2)]
-        self._lens = [x[:n_req] for x in self._lens_all]
-        self._ring = [torch.tensor([0, n_pages], dtype=torch.int32, device=device) for _ in range(2)]
+        # {head, count} of the ring, the lengths, and an entry that release() writes for rows that are not there; then
+        # the same as calls write it
+        self._state = torch.zeros(2, n_req + 3, dtype=torch.int32, device=device)
+        self._state[:, 1] = n_pages
         self.workspace_bytes = H.hybrid_paged_attn_workspace_bytes(cfg, self.pg, n_req)
         if self.workspace_bytes == 0:
             raise ValueError(f"unsupported {cfg} with {self.pg}")
@@ -104,15 +105,15 @@ class PagePool:
     @property
     def lens(self) -> torch.Tensor:
         """Tokens of each request, int32 [n_req]."""
-        return self._lens[0]
+        return self._state[0, 2:-1]
 
     @property
     def ring(self) -> torch.Tensor:
         """{head, count} of the free pages."""
-        return self._ring[0]
+        return self._state[0, :2]
 
     def _tables(self):
-        return (*self._lens, *self._ring, self.block_table, self.free_pages)
+        return self._state, self.block_table, self.free_pages
 
     def workspace_of(self, cfg: H.hybrid_cfg, on: OnStream) -> torch.Tensor:
         """Attention's workspace for a layer's cfg on the call's stream: calls on several streams may overlap, and need
@@ -139,11 +140,10 @@ class PagePool:
         new = lambda n: torch.empty(n, dtype=torch.int32, device=self.device)  # noqa: E731
         with OnStream(stream, n_new, *self._tables()) as on:
             slots, positions, offsets = new(n_tok), new(n_tok), new(self.n_req + 1)
-            H.hybrid_page_append(self.pg, self.n_req, self._lens[0], n_new, self.free_pages, self._ring[0], self.block_table,
-                                 slots, positions, n_tok, offsets, self._lens[1], self._ring[1])
-            self._lens.reverse()
-            self._lens_all.reverse()
-            self._ring.reverse()
+            now, then = self._state
+            H.hybrid_page_append(self.pg, self.n_req, now[2:], n_new, self.free_pages, now, self.block_table, slots, positions,
+                                 n_tok, offsets, then[2:], then)
+            now[:-1].copy_(then[:-1])
             return on.returns(slots, positions, offsets)
 
     def block_rows(self, offsets: torch.Tensor, n_tok: int, block: int | None = None, stream=None) -> BlockRows:
@@ -160,8 +160,8 @@ class PagePool:
         same stream. A row out of range is left out, and reported by hybrid_check."""
         expect(rows, "rows", torch.int32, self.device, rows.numel())
         with OnStream(stream, rows, *self._tables()):
-            H.hybrid_page_release(self.pg, self.n_req, rows, rows.numel(), self._lens[0], self.block_table, self.free_pages,
-                                  self._ring[0], self._ring[1])
-            self._ring.reverse()
+            now, then = self._state
+            H.hybrid_page_release(self.pg, self.n_req, rows, rows.numel(), now[2:], self.block_table, self.free_pages, now, then)
+            now[:2].copy_(then[:2])
             there = (rows >= 0) & (rows < self.n_req)
-            self._lens_all[0].index_fill_(0, torch.where(there, rows, self.n_req).long(), 0)
+            now[2:].index_fill_(0, torch.where(there, rows, self.n_req).long(), 0)

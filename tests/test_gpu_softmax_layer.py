@@ -228,3 +228,44 @@ def test_decoding_after_a_middle_and_the_last_row_are_released(dt, pad):
     block([B, B - 1, 0, B, 0], 3 * B - 1 + pad)
     block([B, B, 0, B, 0], n * B)                            # as many as query rows, but not in their places
     block([0, 0, 0, 1, 0], 1 + pad)
+
+
+# ------------------------------------------------------------------ graphs
+
+def test_a_captured_append_and_release_go_on_from_call_to_call():
+    """One append, and one append with one release, captured and replayed among eager calls: lengths, ring and
+    tables against the model."""
+    P, n, N = 16, 3, 60
+    cfg = H.make_cfg(64, 64, 4, 2, 2, F32)
+    pool = PagePool(cfg, n, N, 200, P)
+    model = R.Pool(P, N, pool.pg.max_pages, range(N), 0, N, [[-1] * pool.pg.max_pages for _ in range(n)])
+    lens, held = [0] * n, pool.lens
+    new, rows = i32([5, 17, 2]), i32([1])
+    pool.append(i32([0, 0, 0]), 24), pool.release(i32([]))
+    graphs = []
+    for release in (False, True):
+        g = torch.cuda.CUDAGraph()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(g):
+            out = pool.append(new, 24)
+            if release:
+                pool.release(rows)
+        graphs.append((g, out))
+
+    def check(out, n_new):
+        nonlocal lens
+        H.hybrid_check()
+        slots, pos, offs, lens, bad = model.append(lens, n_new, 24)
+        assert not bad and [x.tolist() for x in out] == [slots, pos, offs]
+
+    for what in (0, 0, 0, 1, 0, 2, 1, 1, 2, 2, 2, 0):        # the graphs, or an eager append
+        if what == 2:
+            check(pool.append(i32([1, 0, 4]), 24), [1, 0, 4])
+        else:
+            graphs[what][0].replay()
+            check(graphs[what][1], [5, 17, 2])
+        if what == 1:
+            model.release([1], lens)
+            lens[1] = 0
+        assert pool.lens.tolist() == held.tolist() == lens and pool.ring.tolist() == [model.head, model.count]
+        assert pool.block_table.tolist() == model.table
