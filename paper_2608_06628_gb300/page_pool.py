@@ -117,17 +117,17 @@ class PagePool:
 
     def workspace_of(self, cfg: H.hybrid_cfg, on: OnStream) -> torch.Tensor:
         """Attention's workspace for a layer's cfg on the call's stream: calls on several streams may overlap, and need
-        one each. (Graphs captured on one stream share one: replays of them must not overlap.)"""
-        geometry = tuple(getattr(cfg, name) for name, _ in cfg._fields_)
-        key = (H._stream(None), geometry)
+        one each. A captured call has one of its graph's memory, since the graph may be replayed beside any of them."""
+        n = H.hybrid_paged_attn_workspace_bytes(cfg, self.pg, self.n_req)
+        if n == 0:
+            raise ValueError(f"unsupported {cfg} with {self.pg}")
+        new = lambda: torch.empty(n, dtype=torch.uint8, device=self.device)  # noqa: E731
+        if self.device.type == "cuda" and torch.cuda.is_current_stream_capturing():
+            return new()
+        key = (H._stream(None), *(getattr(cfg, name) for name, _ in cfg._fields_))
         if key not in self._workspaces:
-            if not self._workspaces and geometry == tuple(getattr(self.cfg, name) for name, _ in cfg._fields_):
-                self._workspaces[key] = self.workspace
-            else:
-                n = H.hybrid_paged_attn_workspace_bytes(cfg, self.pg, self.n_req)
-                if n == 0:
-                    raise ValueError(f"unsupported {cfg} with {self.pg}")
-                self._workspaces[key] = torch.empty(n, dtype=torch.uint8, device=self.device)
+            first = not self._workspaces and n == self.workspace_bytes
+            self._workspaces[key] = self.workspace if first else new()
         on.uses(self._workspaces[key])
         return self._workspaces[key]
 

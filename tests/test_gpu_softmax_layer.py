@@ -269,3 +269,52 @@ def test_a_captured_append_and_release_go_on_from_call_to_call():
             lens[1] = 0
         assert pool.lens.tolist() == held.tolist() == lens and pool.ring.tolist() == [model.head, model.count]
         assert pool.block_table.tolist() == model.table
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
+def test_graphs_replayed_at_once(dt):
+    """Two captured attentions of contexts that are split, replayed on two streams beside eager calls on a third."""
+    cfg = H.make_cfg(128, 64, 8, 2, 16, dt)
+    pool = filled(cfg, [9000, 20000, 700], 1900, 20000)
+    layer = layer_of(pool)
+    q = [torch.randn(48, 8, 128, device="cuda").to(dt) for _ in range(3)]
+    want = [layer.attend(x, pool, 0) for x in q]
+    torch.cuda.synchronize()
+    graphs = []
+    for x in q[:2]:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            out = layer.attend(x, pool, 0)
+        graphs.append((g, out))
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for trial in range(30):
+        for s, (g, _) in zip(streams, graphs):
+            with torch.cuda.stream(s):
+                g.replay()
+        eager = layer.attend(q[2], pool, 0)
+        torch.cuda.synchronize()
+        assert torch.equal(eager, want[2]) and all(torch.equal(out, w) for (_, out), w in zip(graphs, want)), trial
+    H.hybrid_check()
+
+
+def test_captured_attention_has_a_workspace_of_its_graph(monkeypatch):
+    cfg = H.make_cfg(64, 64, 4, 2, 2, BF)
+    pool = filled(cfg, [300, 200, 100], 60, 400)
+    layer, q = layer_of(pool), torch.randn(6, 4, 64, device="cuda").to(BF)
+    seen, call = [], H.hybrid_paged_attn
+
+    def note(*args, **kw):
+        seen.append(args[11].data_ptr())
+        return call(*args, **kw)
+
+    monkeypatch.setattr(H, "hybrid_paged_attn", note)
+    s, graphs = torch.cuda.Stream(), []
+    torch.cuda.synchronize()
+    layer.attend(q, pool, 0, s)
+    torch.cuda.synchronize()
+    for _ in range(2):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1], stream=s):
+            layer.attend(q, pool, 0)
+    H.hybrid_check()
+    assert len(set(seen)) == 3
