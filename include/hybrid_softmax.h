@@ -179,6 +179,8 @@ hybrid_status hybrid_qk_norm_rope_backward(const hybrid_cfg *cfg, const hybrid_r
  * stay visible; n_sink is ignored without a window.)  A request without a visible
  * key gets zeros.  What lies in the cache at other places (NaN included) has no
  * effect, and pages and table entries that hold no visible key are not read.
+ * Infinities and NaN of visible keys and values give what the formula gives; a p_j
+ * below 2^-126 of the largest may count as zero (and zero times infinity is NaN).
  * The work of all requests is cut evenly over the GPU whatever their lengths are;
  * parts of one request are joined in a fixed order, so the same inputs give the
  * same bits on every call.  bfloat16: products on the tensor cores with float32

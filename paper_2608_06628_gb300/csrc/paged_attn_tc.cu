@@ -15,14 +15,16 @@
 // quarter share one scheduler.  With few rows (decoding) that would leave the whole
 // softmax to one scheduler, so the rows are copied: with at most 32 (64) rows, Q
 // stands 4 (2) times in the 128 rows of the product, and each copy takes a quarter
-// (half) of every tile's keys: its other columns of P stay zero, it has a reference
-// and a sum of its own, and O is the sum of the copies' rows, formed at the end of a
-// segment.  The products' padding costs nothing here: a tile's products take about
-// 0.6 us, its bytes 1.5 us at an SM's share of the memory bandwidth.  With more
-// rows, two threads share a row, 64 keys of every tile each, with a reference, a sum
-// and an accumulator O of its own; P then takes the place of the S it was made
-// from (Tensor Memory holds two S and two O), and the halves are added at the end of
-// a segment.  So no warp waits for another between the tiles of a segment.
+// (half) of every tile's keys: it has a reference and a sum of its own, and O is the
+// sum of the copies' rows, formed at the end of a segment.  The products of a copy's
+// keys with V write its lanes alone: with zeros in the other copies' P instead, an
+// infinite V would make NaN of their rows (one request of 777 keys 8.9 us, here 9.1; 64
+// requests of 256-8192 tokens 92.6 both).  The products' padding costs nothing: a
+// tile's products take about 0.6 us, its bytes 1.5 us at an SM's share of the memory
+// bandwidth.  With more rows, two threads share a row, 64 keys of every tile each, with
+// a reference, a sum and an accumulator O of its own; P then takes the place of the S
+// it was made from (Tensor Memory holds two S and two O), and the halves are added at
+// the end of a segment.  So no warp waits for another between the tiles of a segment.
 //
 // The cache is read once per row tile by TMA boxes of one page of one head (64
 // features x page_size rows, 128-byte swizzle), issued by one warp for K and one
@@ -289,29 +291,41 @@ __global__ void __launch_bounds__(Roles<kCopies>::kThreads, 1) k_paged_attn_tc(c
             while (ok && w.next(a)) {
                 // O is overwritten by a segment's first product: the last epilogue has read it
                 if (seg > 0) ok = wait_soon(ofree, (seg - 1) & 1u, fail);
-                uint32_t acc[kParts] = {};                 // whether the segment has written the accumulator
+                uint32_t acc[kParts * kCopies] = {};       // whether the segment has written the accumulator
                 for (int i = w.i0; ok && i < w.i1; ++i, ++n) {
                     const uint32_t b = n & 1;
                     const int j = key_tile(w.vis, i) * kTile;
                     const bool all = all_visible(w.vis, j);
-                    constexpr int kSteps = kTile / 16 / kParts;
+                    // steps of 16 keys of an accumulator: a half of O's, or a copy's lanes
+                    constexpr int kSteps = kTile / 16 / (kParts * kCopies);
                     ok = wait_soon(&full[NK + pos.slot], pos.phase, fail);
                     const uint64_t bv = v_desc + pos.slot * (kSlot >> 4);
 #pragma unroll
-                    for (int p = 0; p < kParts; ++p) {
-                        ok = ok && wait_soon(&pready[b * kParts + p], (n >> 1) & 1u, fail);
+                    for (int p = 0; p < kParts * kCopies; ++p) {
+                        if (kParts > 1 || p == 0) ok = ok && wait_soon(&pready[b * kParts + p], (n >> 1) & 1u, fail);
                         if (!ok) break;
-                        tc_fence_after();
-                        const uint32_t o = tmem + cO + 128 * p, pa = tmem + (kCopies > 1 ? cP + 64 * b : cS + 128 * b + 64 * p);
+                        if (kParts > 1 || p == 0) tc_fence_after();
+                        const uint32_t o = tmem + cO + (kCopies > 1 ? 0 : 128 * p);
+                        const uint32_t pa = tmem + (kCopies > 1 ? cP + 64 * b + 8 * kSteps * p : cS + 128 * b + 64 * p);
+                        auto product = [&](int g, uint32_t accumulate) {
+                            const uint64_t v = bv + (p * kSteps + g) * (2048 >> 4);
+                            if constexpr (kCopies > 1) {
+                                uint32_t off[4];
+#pragma unroll
+                                for (int x = 0; x < 4; ++x) off[x] = x * kCopies / 4 == p ? 0u : ~0u;
+                                mma_bf16_ts_lanes(o, pa + 8 * g, v, id, accumulate, off);
+                            } else {
+                                mma_bf16_ts(o, pa + 8 * g, v, id, accumulate);
+                            }
+                        };
                         if (all) {
 #pragma unroll
-                            for (int g = 0; g < kSteps; ++g)
-                                mma_bf16_ts(o, pa + 8 * g, bv + (p * kSteps + g) * (2048 >> 4), id, acc[p] | (g > 0));
+                            for (int g = 0; g < kSteps; ++g) product(g, acc[p] | (g > 0));
                             acc[p] = 1;
                         } else {
                             for (int g = 0; g < kSteps; ++g) {
                                 if (!any_visible(w.vis, j + 16 * (p * kSteps + g), 16)) continue;
-                                mma_bf16_ts(o, pa + 8 * g, bv + (p * kSteps + g) * (2048 >> 4), id, acc[p]);
+                                product(g, acc[p]);
                                 acc[p] = 1;
                             }
                         }
@@ -351,14 +365,6 @@ __global__ void __launch_bounds__(Roles<kCopies>::kThreads, 1) k_paged_attn_tc(c
             __syncwarp();
             if (lane == 0 && !bad) mbar_arrive(bar);
         };
-        if (kCopies > 1) {                                 // other copies' keys: P stays zero there
-            float zero[32];
-#pragma unroll
-            for (int y = 0; y < 32; ++y) zero[y] = 0.f;
-#pragma unroll
-            for (int x = 0; x < 4; ++x) tmem_st32(tmem + cP + 32 * x + lane_off, zero);
-            tmem_wait_st();
-        }
         while (w.next(a)) {     // left by a vote at a segment's end only, so that the warps of a row stay together
             float ref = -INFINITY;
             f32x2 l2 = pair2(0.f, 0.f);                    // the row's sum over this thread's keys, in two
@@ -511,11 +517,12 @@ __global__ void __launch_bounds__(Roles<kCopies>::kThreads, 1) k_paged_attn_tc(c
                         float o[32];
                         tmem_ld32(tmem + cO + x0 + x + lane_off, o);
                         tmem_wait_ld();
-                        if (row < rows) {
+                        if (row < rows) {                  // (a copy without a visible key has not written O)
 #pragma unroll
                             for (int y = 0; y < 32; y += 4)
                                 *reinterpret_cast<float4 *>(mine + x + y) =
-                                    make_float4(o[y] * f, o[y + 1] * f, o[y + 2] * f, o[y + 3] * f);
+                                    f != 0.f ? make_float4(o[y] * f, o[y + 1] * f, o[y + 2] * f, o[y + 3] * f)
+                                             : make_float4(0.f, 0.f, 0.f, 0.f);
                         }
                     }
                     if (x0 + span == D) arrive(ofree);

@@ -318,3 +318,50 @@ def test_captured_attention_has_a_workspace_of_its_graph(monkeypatch):
             layer.attend(q, pool, 0)
     H.hybrid_check()
     assert len(set(seen)) == 3
+
+
+# ------------------------------------------------------------------ infinities and NaN that queries see
+
+ROWS = [(1, 1), (1, 4), (8, 4), (33, 1), (16, 4), (9, 8), (24, 4), (32, 4), (33, 5)]     # (tokens, heads of a key head)
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("B,G", ROWS)
+def test_infinite_and_nan_values_that_queries_see(dt, B, G):
+    """One feature of some values is infinite or NaN: that feature of the outputs is what the formula gives (keys are
+    small, so that no weight vanishes), whatever the number of rows, and every other output is as without it."""
+    from test_gpu_softmax import attn_setup, run_attn
+    lens = [300, 128, 1000, 77, 4000]
+    s = attn_setup(dt, B, 2 * G, 2, 64, 16, lens, seed=3, k_scale=0.1)
+    clean = run_attn(s)
+    put = lambda r, j, h, c, x: s["vc"].__setitem__((int(s["table"][r, j // 16]), h, j % 16, c), x)  # noqa: E731
+    inf, nan = float("inf"), float("nan")
+    put(0, 200, 0, 5, inf), put(0, 299, 1, 63, -inf)         # a last, partial tile; its last key
+    put(1, 3, 0, 0, inf), put(1, 100, 0, 0, inf), put(1, 127, 0, 1, -inf)
+    put(2, 999, 1, 9, inf), put(2, 500, 1, 9, -inf)          # both signs: NaN
+    put(3, 0, 0, 7, nan), put(4, 2000, 0, 30, inf), put(4, 3999, 1, 31, nan)
+    got = run_attn(s)
+    want = R.paged_attention(s["q"], s["kc"], s["vc"], s["table"], lens, 0, 0)
+    odd = ~torch.isfinite(want)
+    assert int(odd.sum()) == 8 * B * G
+    assert torch.equal(got.double()[odd].nan_to_num(5.0, 1.0, -1.0), want[odd].nan_to_num(5.0, 1.0, -1.0))
+    assert torch.equal(got[~odd], clean[~odd])
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("B,G", ROWS)
+def test_infinite_and_nan_keys_and_queries(dt, B, G):
+    """A query with NaN gives NaN in its own row alone; a key with an infinity makes each score infinite: NaN where it
+    is positive, a weight of zero where it is negative."""
+    from test_gpu_softmax import attn_setup, run_attn
+    lens = [300, 128, 1000]
+    s = attn_setup(dt, B, 2 * G, 2, 64, 16, lens, seed=4)
+    s["kc"][int(s["table"][1, 3]), 1, 5, 2] = float("inf")
+    s["q"][1, :, G:, 2] = s["q"][1, :, G:, 2].abs() + 1
+    s["q"][1, 0, G, 2] *= -1
+    s["q"][2, B - 1, 0, 11] = float("nan")
+    got = run_attn(s)
+    want = R.paged_attention(s["q"], s["kc"], s["vc"], s["table"], lens, 0, 0)
+    odd = want.isnan()
+    assert int(odd.sum()) == 64 * (B * G - 1 + 1) and torch.equal(got.isnan(), odd)
+    assert_parity(got.double().nan_to_num(0.0).cpu().numpy(), want.nan_to_num(0.0).cpu().numpy(), dt, "the rest", units="out")
