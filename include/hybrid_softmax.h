@@ -77,8 +77,8 @@ hybrid_status hybrid_page_append(const hybrid_page_cfg *pg, int n_req, const int
  * entries.  lens [n_req] are the requests' lengths; the caller sets those of the
  * released rows to 0 before the next append.  Entries are written into
  * free_pages in place, outside the live part of ring_in.  A row or length out of
- * range is skipped, and what would overfill the ring is dropped; both are
- * reported by hybrid_check().  n_rows <= 65536. */
+ * range is skipped, a table entry out of range left out, and what would overfill the
+ * ring dropped; all are reported by hybrid_check().  n_rows <= 65536. */
 hybrid_status hybrid_page_release(const hybrid_page_cfg *pg, int n_req, const int *rows, int n_rows,
                                   const int *lens, const int *block_table, int *free_pages, const int *ring_in,
                                   int *ring_out, cudaStream_t stream);

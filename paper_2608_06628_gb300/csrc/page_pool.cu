@@ -237,8 +237,12 @@ struct ReleaseArgs {
     unsigned *err;
 };
 
+// Whether a released row has ever held an entry that is no page, on this device.
+__device__ unsigned g_bad_entry;
+
 // Page i of all released pages, in order, goes to the ring's entry head + count + i.
-// Blocks take runs of kThreads pages in turn.
+// Blocks take runs of kThreads pages in turn.  Entries that are no pages are taken out
+// again by k_page_release_drop.
 __global__ __launch_bounds__(kThreads) void k_page_release(const ReleaseArgs a)
 {
     __shared__ int s_row[kChunk];
@@ -297,7 +301,10 @@ __global__ __launch_bounds__(kThreads) void k_page_release(const ReleaseArgs a)
                     else y = m;
                 }
                 const int page = a.table[(size_t)s_row[x] * a.max_pages + (size_t)(i - s_first[x])];
-                if (page < 0 || page >= a.n_pages) bad = true;
+                if (page < 0 || page >= a.n_pages) {
+                    bad = true;
+                    *const_cast<volatile unsigned *>(&g_bad_entry) = 1u;
+                }
                 const long long to = (long long)head + count + i;      // < 2 n_pages
                 a.free_pages[to < a.n_pages ? to : to - a.n_pages] = page;
             }
@@ -310,6 +317,35 @@ __global__ __launch_bounds__(kThreads) void k_page_release(const ReleaseArgs a)
         a.ring_out[1] = ring_ok ? count + (int)(page0 < room ? page0 : room) : a.ring_in[1];
     }
     if (bad) raise_error(a.err, ERR_BAD_INDEX);
+}
+
+// The pages of the release just before it without the entries that are no pages, closed up
+// in order, by one block.  The healthy case is a look at a word that nothing sets, for a
+// launch (2 us of the host's time, 1 us on the GPU): the blocks of the release know of each
+// other's pages only when they are done, and the word outlives the call because calls on
+// several streams share it.
+__global__ __launch_bounds__(kThreads) void k_page_release_drop(const ReleaseArgs a)
+{
+    __shared__ Scan2 s_warp[kThreads / 32];
+    ptx::griddep_wait();
+    ptx::griddep_launch_dependents();
+    if (*const_cast<volatile unsigned *>(&g_bad_entry) == 0u) return;
+    int head, count;
+    if (!load_ring(a.ring_in, a.n_pages, head, count)) return;
+    const int n = a.ring_out[1] - count;                        // entries of the release
+    int kept = 0;
+    for (int i0 = 0; i0 < n; i0 += kThreads) {
+        const long long from = (long long)head + count + i0 + threadIdx.x;
+        const int page = i0 + (int)threadIdx.x < n ? a.free_pages[from < a.n_pages ? from : from - a.n_pages] : -1;
+        const bool keep = page >= 0 && page < a.n_pages;
+        Scan2 total;
+        const Scan2 at = block_scan({keep ? 1 : 0, 0}, total, s_warp);      // (a barrier behind the loads)
+        const long long to = (long long)head + count + kept + at.a;
+        if (keep) a.free_pages[to < a.n_pages ? to : to - a.n_pages] = page;
+        kept += (int)total.a;
+        __syncthreads();                                        // before the next entries are loaded
+    }
+    if (threadIdx.x == 0) a.ring_out[1] = count + kept;
 }
 
 // A thread per item (slots, a page) while that takes no more blocks than the GPU holds at once.
@@ -352,7 +388,9 @@ cudaError_t launch_page_release(const hybrid_page_cfg &pg, int n_req, const int 
     // at most the pool's pages move
     long long most = (long long)n_rows * pg.max_pages;
     if (most > pg.n_pages) most = pg.n_pages;
-    return pipe::launch_early(k_page_release, dim3(blocks_for(most)), dim3(kThreads), 0, st, a);
+    const cudaError_t e = pipe::launch_early(k_page_release, dim3(blocks_for(most)), dim3(kThreads), 0, st, a);
+    if (e != cudaSuccess || n_rows == 0) return e;
+    return pipe::launch_early(k_page_release_drop, dim3(1), dim3(kThreads), 0, st, a);
 }
 
 }  // namespace hyb

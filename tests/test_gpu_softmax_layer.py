@@ -193,6 +193,38 @@ def test_attention_of_layers_with_other_rows_than_the_pool(dt):
     assert_parity(got.view(want.shape).double().cpu().numpy(), want.cpu().numpy(), dt, "blocks of 33", units="out")
 
 
+# ------------------------------------------------------------------ entries that are no pages
+
+@pytest.mark.parametrize("n,pages,bad", [(1, 3, [0]), (3, 3, [2, 5]), (2, 400, [0, 255, 256, 700]), (300, 40, range(0, 12000, 7)),
+                                         (7, 100, range(700)), (5, 60, [])])
+def test_release_leaves_out_entries_that_are_no_pages(n, pages, bad):
+    """They stay out of the ring, the pages beside them go into it in order, and the calls behind are whole again."""
+    P, N = 16, n * pages + 9
+    order = torch.randperm(N, generator=torch.Generator().manual_seed(n)).to(torch.int32)
+    table = order[:n * pages].clone()
+    for k, i in enumerate(bad):
+        table[i] = [-1, N, 2 ** 31 - 1, -2 ** 31][k % 4]
+    good = [x for x in table.tolist() if 0 <= x < N]
+    head, free, ring = N - 5, torch.full((N,), -7, dtype=torch.int32), i32([0, 0])
+    free[torch.tensor([(head + i) % N for i in range(9)])] = order[n * pages:]
+    free, table = free.cuda(), table.view(n, pages).cuda()
+    lens = i32([pages * P - r % P for r in range(n)])
+    pg = H.make_page_cfg(P, N, pages)
+    H.hybrid_page_release(pg, n, i32(range(n)), n, lens, table, free, i32([head, 9]), ring)
+    assert H.hybrid_check(check=False) == (H.HYBRID_ERR_DEVICE if len(bad) else H.HYBRID_OK)
+    assert ring.tolist() == [head, 9 + len(good)]
+    live = [free.tolist()[(head + i) % N] for i in range(9 + len(good))]
+    assert live == order[n * pages:].tolist() + good
+    # without entries of that kind, the ring half full: in order, and all of them
+    half, again = n * pages // 2, i32([0, 0])
+    table = order[:n * pages].view(n, pages).cuda()
+    H.hybrid_page_release(pg, n, i32(range(n)), n, lens, table, free, i32([3, half]), again)
+    assert H.hybrid_check(check=False) == (H.HYBRID_OK if n * pages <= N - half else H.HYBRID_ERR_DEVICE)
+    m = min(n * pages, N - half)
+    assert again.tolist() == [3, half + m]
+    assert [free.tolist()[(3 + half + i) % N] for i in range(m)] == order[:m].tolist()
+
+
 # ------------------------------------------------------------------ batches with idle rows
 
 @pytest.mark.parametrize("dt", [BF, F32])
