@@ -148,7 +148,7 @@ def make_cfg(head_dim, feat_dim, n_q_heads, n_kv_heads, block_size, io_dtype) ->
 
 
 def _ptr(x):
-    if x is None or type(x) is int:
+    if x is None or isinstance(x, int):
         return x
     return x.data_ptr()
 
