@@ -50,8 +50,8 @@ typedef struct {
  *
  * The free pages form a ring: free_pages [n_pages] int, and a pair of ints
  * {head, count}: the free ones are free_pages[(head + i) % n_pages], i < count.
- * Calls read one pair and write another (ring_in and ring_out must not be the
- * same, nor may lens and lens_out), so a call can be replayed. */
+ * Calls read one pair and write another, so a call can be replayed.  No output may
+ * share memory with an input or another output (HYBRID_ERR_INVALID_ARG). */
 
 /* Room for n_new[r] >= 0 new tokens of each request, which has lens[r] already:
  * pages are taken from the ring's head, request by request in order, and

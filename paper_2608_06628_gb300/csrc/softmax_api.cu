@@ -11,6 +11,28 @@ bool aligned(const void *p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p
 bool good(const void *p, uintptr_t a) { return p && aligned(p, a); }
 bool good_or_null(const void *p, uintptr_t a) { return aligned(p, a); }
 
+// n ints of a call's argument
+struct Ints {
+    const int *p;
+    size_t n;
+};
+// Whether one of the outputs shares memory with an input or another output.  (The blocks of
+// a call do not wait for one another: one may write what another has yet to read.)
+template <int O, int I> bool overlap(const Ints (&out)[O], const Ints (&in)[I])
+{
+    auto meet = [](const Ints &a, const Ints &b) {
+        const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
+        return a.p && b.p && a.n && b.n && x < y + b.n * sizeof(int) && y < x + a.n * sizeof(int);
+    };
+    for (int i = 0; i < O; ++i) {
+        for (int j = 0; j < I; ++j)
+            if (meet(out[i], in[j])) return true;
+        for (int j = 0; j < i; ++j)
+            if (meet(out[i], out[j])) return true;
+    }
+    return false;
+}
+
 hybrid_status from_cuda(cudaError_t e) { return e == cudaSuccess ? HYBRID_OK : HYBRID_ERR_CUDA; }
 
 constexpr int kMaxRequests = 65536;
@@ -101,7 +123,11 @@ hybrid_status hybrid_page_append(const hybrid_page_cfg *pg, int n_req, const int
         return HYBRID_ERR_INVALID_ARG;
     if (n_slots > 0 && !good(slots, 4)) return HYBRID_ERR_INVALID_ARG;
     if (!good_or_null(positions, 4) || !good_or_null(tok_offsets, 4)) return HYBRID_ERR_INVALID_ARG;
-    if (ring_in == ring_out || (n_req > 0 && lens == lens_out)) return HYBRID_ERR_INVALID_ARG;
+    const size_t n = n_req, table = n * pg->max_pages;
+    if (overlap<6, 4>({{block_table, table}, {slots, (size_t)n_slots}, {positions, (size_t)n_slots}, {tok_offsets, n + 1},
+                       {lens_out, n}, {ring_out, 2}},
+                      {{lens, n}, {n_new, n}, {free_pages, (size_t)pg->n_pages}, {ring_in, 2}}))
+        return HYBRID_ERR_INVALID_ARG;
     unsigned *err = hyb::error_word();
     if (!err) return HYBRID_ERR_CUDA;
     return from_cuda(hyb::launch_page_append(*pg, n_req, lens, n_new, free_pages, ring_in, block_table, slots,
@@ -119,7 +145,9 @@ hybrid_status hybrid_page_release(const hybrid_page_cfg *pg, int n_req, const in
     if (n_rows == 0 && !ring_out) return HYBRID_OK;
     if (!good(free_pages, 4) || !good(ring_in, 4) || !good(ring_out, 4)) return HYBRID_ERR_INVALID_ARG;
     if (n_rows > 0 && (!good(rows, 4) || !good(lens, 4) || !good(block_table, 4))) return HYBRID_ERR_INVALID_ARG;
-    if (ring_in == ring_out) return HYBRID_ERR_INVALID_ARG;
+    if (overlap<2, 4>({{free_pages, (size_t)pg->n_pages}, {ring_out, 2}},
+                      {{rows, (size_t)n_rows}, {lens, (size_t)n_req}, {block_table, (size_t)n_req * pg->max_pages}, {ring_in, 2}}))
+        return HYBRID_ERR_INVALID_ARG;
     unsigned *err = hyb::error_word();
     if (!err) return HYBRID_ERR_CUDA;
     return from_cuda(hyb::launch_page_release(*pg, n_req, rows, n_rows, lens, block_table, free_pages, ring_in,
