@@ -18,9 +18,10 @@
 // (half) of every tile's keys: it has a reference and a sum of its own, and O is the
 // sum of the copies' rows, formed at the end of a segment.  The products of a copy's
 // keys with V write its lanes alone: with zeros in the other copies' P instead, an
-// infinite V would make NaN of their rows (one request of 777 keys 8.9 us, here 9.1; 64
-// requests of 256-8192 tokens 92.6 both).  The products' padding costs nothing: a
-// tile's products take about 0.6 us, its bytes 1.5 us at an SM's share of the memory
+// infinite V would make NaN of their rows, for the same time (64 requests of 256-8192
+// tokens 92.5 us both, 45 requests of 86-249 tokens with 16 key heads 34.5, here 34.7; 39.3
+// with a loop for each copy, which the instruction cache does not hold).  The products'
+// padding costs nothing: a tile's products take about 0.6 us, its bytes 1.5 us at an SM's share of the memory
 // bandwidth.  With more rows, two threads share a row, 64 keys of every tile each, with
 // a reference, a sum and an accumulator O of its own; P then takes the place of the S
 // it was made from (Tensor Memory holds two S and two O), and the halves are added at
@@ -291,42 +292,37 @@ __global__ void __launch_bounds__(Roles<kCopies>::kThreads, 1) k_paged_attn_tc(c
             while (ok && w.next(a)) {
                 // O is overwritten by a segment's first product: the last epilogue has read it
                 if (seg > 0) ok = wait_soon(ofree, (seg - 1) & 1u, fail);
-                uint32_t acc[kParts * kCopies] = {};       // whether the segment has written the accumulator
+                uint32_t acc = 0;                          // bits: accumulators, or copies, that the segment has written
                 for (int i = w.i0; ok && i < w.i1; ++i, ++n) {
                     const uint32_t b = n & 1;
                     const int j = key_tile(w.vis, i) * kTile;
                     const bool all = all_visible(w.vis, j);
-                    // steps of 16 keys of an accumulator: a half of O's, or a copy's lanes
-                    constexpr int kSteps = kTile / 16 / (kParts * kCopies);
+                    // steps of 16 keys: of a part, of a copy
+                    constexpr int kSteps = kTile / 16 / kParts, kOwn = kSteps / kCopies;
                     ok = wait_soon(&full[NK + pos.slot], pos.phase, fail);
                     const uint64_t bv = v_desc + pos.slot * (kSlot >> 4);
 #pragma unroll
-                    for (int p = 0; p < kParts * kCopies; ++p) {
-                        if (kParts > 1 || p == 0) ok = ok && wait_soon(&pready[b * kParts + p], (n >> 1) & 1u, fail);
+                    for (int p = 0; p < kParts; ++p) {
+                        ok = ok && wait_soon(&pready[b * kParts + p], (n >> 1) & 1u, fail);
                         if (!ok) break;
-                        if (kParts > 1 || p == 0) tc_fence_after();
-                        const uint32_t o = tmem + cO + (kCopies > 1 ? 0 : 128 * p);
-                        const uint32_t pa = tmem + (kCopies > 1 ? cP + 64 * b + 8 * kSteps * p : cS + 128 * b + 64 * p);
+                        tc_fence_after();
+                        const uint32_t o = tmem + cO + 128 * p, pa = tmem + (kCopies > 1 ? cP + 64 * b : cS + 128 * b + 64 * p);
                         auto product = [&](int g, uint32_t accumulate) {
                             const uint64_t v = bv + (p * kSteps + g) * (2048 >> 4);
-                            if constexpr (kCopies > 1) {
-                                uint32_t off[4];
-#pragma unroll
-                                for (int x = 0; x < 4; ++x) off[x] = x * kCopies / 4 == p ? 0u : ~0u;
-                                mma_bf16_ts_lanes(o, pa + 8 * g, v, id, accumulate, off);
-                            } else {
-                                mma_bf16_ts(o, pa + 8 * g, v, id, accumulate);
-                            }
+                            if constexpr (kCopies > 1) mma_bf16_ts_lanes(o, pa + 8 * g, v, id, accumulate, kCopies, g / kOwn);
+                            else mma_bf16_ts(o, pa + 8 * g, v, id, accumulate);
                         };
                         if (all) {
 #pragma unroll
-                            for (int g = 0; g < kSteps; ++g) product(g, acc[p] | (g > 0));
-                            acc[p] = 1;
+                            for (int g = 0; g < kSteps; ++g)
+                                product(g, g % kOwn > 0 ? 1u : acc >> (p + g / kOwn) & 1u);
+                            acc |= ((1u << kCopies) - 1) << p;
                         } else {
+#pragma unroll 1
                             for (int g = 0; g < kSteps; ++g) {
                                 if (!any_visible(w.vis, j + 16 * (p * kSteps + g), 16)) continue;
-                                product(g, acc[p]);
-                                acc[p] = 1;
+                                product(g, acc >> (p + g / kOwn) & 1u);
+                                acc |= 1u << (p + g / kOwn);
                             }
                         }
                     }

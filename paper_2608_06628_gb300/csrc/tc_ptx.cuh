@@ -410,10 +410,13 @@ __device__ __forceinline__ void mma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, ui
         "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
         : "memory");
 }
-// The same for some of D's lanes: a bit of `off` for each lane that keeps its value.
+// The same for part `part` of D's lanes, of 2 or 4 equal ones; the others keep their values.
 __device__ __forceinline__ void mma_bf16_ts_lanes(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc,
-                                                  uint32_t accumulate, const uint32_t (&off)[4])
+                                                  uint32_t accumulate, int parts, int part)
 {
+    uint32_t off[4];                        // a bit for each lane that is left alone
+#pragma unroll
+    for (int x = 0; x < 4; ++x) off[x] = x * parts / 4 == part ? 0u : ~0u;
     asm volatile(
         "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
         "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, {%5, %6, %7, %8}, p;\n\t}" ::"r"(d_tmem),
