@@ -10,6 +10,7 @@ are the requests of the batch; a released row may take a new request at once.
 from __future__ import annotations
 
 import contextlib
+import math
 
 import torch
 
@@ -68,16 +69,15 @@ class BlockRows:
 
     def __init__(self, offsets, n_req: int, n_tok: int, block: int):
         self.n_tok, self.n_rows, dev = n_tok, n_req * block, offsets.device
-        offsets = offsets.long()
-        of_row = (offsets[:-1, None] + torch.arange(block, device=dev)).flatten()
+        t = torch.arange(max(n_tok, block), dtype=torch.int32, device=dev)
         # rows without a token repeat one: nothing reads what they give
-        self.token = of_row.clamp(0, max(n_tok - 1, 0))
-        t = torch.arange(n_tok, device=dev)
-        r = torch.searchsorted(offsets[1:].contiguous(), t, right=True)
-        i = t - offsets[r]
-        # the row of a token; beyond the last token n_rows, beyond its request's first B tokens n_rows + 1
-        row = torch.where(i < block, r * block + i, self.n_rows + 1)
-        self.row = torch.where(r < n_req, row, self.n_rows).clamp(0, self.n_rows + 1)
+        self.token = (offsets[:-1, None] + t[:block]).view(-1).clamp_(0, max(n_tok - 1, 0))
+        t = t[:n_tok]
+        r = torch.searchsorted(offsets[1:], t, right=True, out_int32=True)
+        i = t - offsets.index_select(0, r)
+        # the row of a token; beyond its request's first B tokens n_rows + 1, beyond the last token n_rows
+        row = torch.where(i < block, torch.add(i, r, alpha=block), self.n_rows + 1)
+        self.row = torch.where(r < n_req, row, self.n_rows).clamp_(0, self.n_rows + 1)
 
 
 class PagePool:
@@ -96,21 +96,26 @@ class PagePool:
         # the same as calls write it
         self._state = torch.zeros(2, n_req + 3, dtype=torch.int32, device=device)
         self._state[:, 1] = n_pages
+        now, then = self._state
+        self._now, self._then, self._ring, self._lens = now[:-1], then[:-1], now[:2], now[2:-1]
+        self._then_ring, self._then_lens, self._lens_and_spare = then[:2], then[2:-1], now[2:]
         self.workspace_bytes = H.hybrid_paged_attn_workspace_bytes(cfg, self.pg, n_req)
         if self.workspace_bytes == 0:
             raise ValueError(f"unsupported {cfg} with {self.pg}")
         self.workspace = torch.empty(self.workspace_bytes, dtype=torch.uint8, device=device)
         self._workspaces = {}
+        # outputs of tokens without a query row: beyond the last token, beyond a request's first block of them
+        self.no_row = torch.tensor([[[0.0]], [[math.nan]]], dtype=dtype, device=device)
 
     @property
     def lens(self) -> torch.Tensor:
         """Tokens of each request, int32 [n_req]."""
-        return self._state[0, 2:-1]
+        return self._lens
 
     @property
     def ring(self) -> torch.Tensor:
         """{head, count} of the free pages."""
-        return self._state[0, :2]
+        return self._ring
 
     def _tables(self):
         return self._state, self.block_table, self.free_pages
@@ -118,18 +123,21 @@ class PagePool:
     def workspace_of(self, cfg: H.hybrid_cfg, on: OnStream) -> torch.Tensor:
         """Attention's workspace for a layer's cfg on the call's stream: calls on several streams may overlap, and need
         one each. A captured call has one of its graph's memory, since the graph may be replayed beside any of them."""
-        n = H.hybrid_paged_attn_workspace_bytes(cfg, self.pg, self.n_req)
-        if n == 0:
-            raise ValueError(f"unsupported {cfg} with {self.pg}")
-        new = lambda: torch.empty(n, dtype=torch.uint8, device=self.device)  # noqa: E731
-        if self.device.type == "cuda" and torch.cuda.is_current_stream_capturing():
-            return new()
-        key = (H._stream(None), *(getattr(cfg, name) for name, _ in cfg._fields_))
-        if key not in self._workspaces:
-            first = not self._workspaces and n == self.workspace_bytes
-            self._workspaces[key] = self.workspace if first else new()
-        on.uses(self._workspaces[key])
-        return self._workspaces[key]
+        key = (H._stream(None), cfg.head_dim, cfg.n_q_heads, cfg.n_kv_heads, cfg.block_size, cfg.io_dtype)
+        capturing = self.device.type == "cuda" and torch.cuda.is_current_stream_capturing()
+        made = None if capturing else self._workspaces.get(key)
+        if made is None:
+            n = H.hybrid_paged_attn_workspace_bytes(cfg, self.pg, self.n_req)
+            if n == 0:
+                raise ValueError(f"unsupported {cfg} with {self.pg}")
+            if not capturing and not self._workspaces and n == self.workspace_bytes:
+                made = self.workspace
+            else:
+                made = torch.empty(n, dtype=torch.uint8, device=self.device)
+            if not capturing:
+                self._workspaces[key] = made
+        on.uses(made)
+        return made
 
     def append(self, n_new: torch.Tensor, n_tok: int, stream=None):
         """Room for n_new [n_req] (int32, device) more tokens of each request, at most n_tok in all.
@@ -140,10 +148,9 @@ class PagePool:
         new = lambda n: torch.empty(n, dtype=torch.int32, device=self.device)  # noqa: E731
         with OnStream(stream, n_new, *self._tables()) as on:
             slots, positions, offsets = new(n_tok), new(n_tok), new(self.n_req + 1)
-            now, then = self._state
-            H.hybrid_page_append(self.pg, self.n_req, now[2:], n_new, self.free_pages, now, self.block_table, slots, positions,
-                                 n_tok, offsets, then[2:], then)
-            now[:-1].copy_(then[:-1])
+            H.hybrid_page_append(self.pg, self.n_req, self._lens, n_new, self.free_pages, self._ring, self.block_table, slots,
+                                 positions, n_tok, offsets, self._then_lens, self._then_ring)
+            self._now.copy_(self._then)
             return on.returns(slots, positions, offsets)
 
     def block_rows(self, offsets: torch.Tensor, n_tok: int, block: int | None = None, stream=None) -> BlockRows:
@@ -160,8 +167,8 @@ class PagePool:
         same stream. A row out of range is left out, and reported by hybrid_check."""
         expect(rows, "rows", torch.int32, self.device, rows.numel())
         with OnStream(stream, rows, *self._tables()):
-            now, then = self._state
-            H.hybrid_page_release(self.pg, self.n_req, rows, rows.numel(), now[2:], self.block_table, self.free_pages, now, then)
-            now[:2].copy_(then[:2])
-            there = (rows >= 0) & (rows < self.n_req)
-            now[2:].index_fill_(0, torch.where(there, rows, self.n_req).long(), 0)
+            H.hybrid_page_release(self.pg, self.n_req, rows, rows.numel(), self._lens, self.block_table, self.free_pages,
+                                  self._ring, self._then_ring)
+            self._ring.copy_(self._then_ring)
+            # rows below 0 and above the last all become the entry behind the lengths (-1 counts from the end)
+            self._lens_and_spare.index_fill_(0, rows.long().clamp_(-1, self.n_req), 0)

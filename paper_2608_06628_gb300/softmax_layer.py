@@ -50,13 +50,15 @@ class SoftmaxLayer:
         for x, what in ((self.wq, "wq"), (self.wk, "wk")):
             if x is not None:
                 expect(x, what, self.dtype, dev, c.head_dim)
-        q, k, v = self.split(qkv)
         step = qkv.stride(0) if n_tok > 1 else qkv.shape[1]      # (of a single row torch may report any)
+        q = qkv.data_ptr()
+        k = q + c.n_q_heads * c.head_dim * qkv.element_size()
+        v = k + c.n_kv_heads * c.head_dim * qkv.element_size()
         kc, vc = pool.k_cache[layer], pool.v_cache[layer]
         with OnStream(stream, qkv, slots, positions, self.wq, self.wk, self.freqs, kc, vc) as on:
-            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-            H.hybrid_qk_norm_rope_cache(self.cfg, self.rope, pool.pg, q, step, k, step, v, step, n_tok, self.wq, self.wk,
-                                        positions, self.freqs, slots, out, kc, vc)
+            out = torch.empty((n_tok, c.n_q_heads, c.head_dim), dtype=qkv.dtype, device=dev)
+            H.hybrid_qk_norm_rope_cache(c, self.rope, pool.pg, q, step, k, step, v, step, n_tok, self.wq, self.wk, positions,
+                                        self.freqs, slots, out, kc, vc)
             return on.returns(out)
 
     def attend(self, q, pool: PagePool, layer: int, stream=None, rows: BlockRows | None = None):
@@ -78,14 +80,13 @@ class SoftmaxLayer:
         with OnStream(stream, q, kc, vc, pool.block_table, pool.lens) as on:
             if rows is None:
                 out = torch.empty_like(q)
+            elif rows.n_tok == 0:
+                return on.returns(torch.empty_like(q))
             else:
-                on.uses(rows.token, rows.row)
-                if rows.n_tok == 0:
-                    return on.returns(torch.empty_like(q))
+                on.uses(rows.token, rows.row, pool.no_row)
                 q = q.index_select(0, rows.token)
                 out = torch.empty((n_rows + 2, *q.shape[1:]), dtype=q.dtype, device=q.device)
-                out[n_rows].zero_()
-                out[n_rows + 1].fill_(math.nan)
+                out[n_rows:].copy_(pool.no_row)
             workspace = pool.workspace_of(c, on)
             H.hybrid_paged_attn(c, pool.pg, q, kc, vc, pool.block_table, pool.lens, pool.n_req, self.window, self.n_sink,
                                 out, workspace, workspace.numel())
