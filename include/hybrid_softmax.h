@@ -107,7 +107,10 @@ typedef enum {
     HYBRID_ROPE_NTK = 2,      /* base * factor^(rot_dim / (rot_dim - 2)) in place of base */
     HYBRID_ROPE_YARN = 3      /* by parts: theta_i (1 - g) / factor + theta_i g, with
                                  g = clamp((r_i - beta_slow) / (beta_fast - beta_slow), 0, 1),
-                                 r_i = orig_len theta_i / 2 pi; scale = 0.1 ln(factor) + 1 */
+                                 r_i = orig_len theta_i / 2 pi; scale = 0.1 ln(factor) + 1.
+                                 The ramp is linear in the turns r_i.  (A model whose ramp is
+                                 linear in the pair's index i between the two bounds has other
+                                 frequencies between them: it brings freqs of its own.) */
 } hybrid_rope_kind;
 
 typedef struct {

@@ -321,7 +321,7 @@ __global__ __launch_bounds__(kThreads) void k_page_release(const ReleaseArgs a)
 
 // The pages of the release just before it without the entries that are no pages, closed up
 // in order, by one block.  The healthy case is a look at a word that nothing sets, for a
-// launch (2 us of the host's time, 1 us on the GPU): the blocks of the release know of each
+// launch (2 us of the host's time, 0.6 us on the GPU): the blocks of the release know of each
 // other's pages only when they are done, and the word outlives the call because calls on
 // several streams share it.
 __global__ __launch_bounds__(kThreads) void k_page_release_drop(const ReleaseArgs a)

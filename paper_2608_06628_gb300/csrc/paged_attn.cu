@@ -17,7 +17,7 @@
 //
 // Bound by reads of shared memory and the FMA pipe in turn (about 60% of the peak of
 // each): 64 requests of 256-8192 tokens, blocks of 32, 16 query and 4 key heads, d = 128
-// 1540 us (46 TFLOP/s), d = 64 852 us; with 8 rows x 2 keys and 4 x 4 to a thread, and a
+// 1530 us (47 TFLOP/s), d = 64 848 us; with 8 rows x 2 keys and 4 x 4 to a thread, and a
 // maximum of each row found for each tile, 2440 us.
 #include "paged_plan.cuh"
 #include "tc_pipeline.cuh"

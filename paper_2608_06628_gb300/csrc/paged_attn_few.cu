@@ -14,9 +14,9 @@
 // what it alone reads (cp.async, kStages - 1 steps ahead), so the loop has no barrier.
 //
 // Bound by memory with 4 rows: 64 requests of 256-8192 tokens, 4 key heads, d = 128
-// 176 us (6.3 TB/s), d = 64 92 us, where a version with chunks of 32 or 64 keys, two barriers
+// 173 us (6.4 TB/s), d = 64 92 us, where a version with chunks of 32 or 64 keys, two barriers
 // each and scores through shared memory took 297 us.  With 8 rows the queries and
-// outputs fill 128 registers, so one block to a multiprocessor, 177 and 99 us (one key
+// outputs fill 128 registers, so one block to a multiprocessor, 179 and 103 us (one key
 // to a step 223 and 121 us: 2 warps to a scheduler, and each step waits for its sums).
 #include "paged_plan.cuh"
 #include "tc_pipeline.cuh"

@@ -289,7 +289,8 @@ def make_page_cfg(page_size, n_pages, max_pages) -> hybrid_page_cfg:
 def make_rope(rot_dim, interleaved=False, eps=1e-6, base=10000.0, kind=HYBRID_ROPE_NONE, factor=1.0, orig_len=4096.0,
               beta_fast=32.0, beta_slow=1.0, device="cuda"):
     """The rotation of a model's layers: (hybrid_rope_cfg, freqs), freqs an int64
-    tensor that holds hybrid_rope_freqs' 64-bit fractions.  Made once per model."""
+    tensor that holds hybrid_rope_freqs' 64-bit fractions.  Made once per model.  (YaRN's ramp
+    is linear in a pair's turns over orig_len; for one linear in the pair's index, bring freqs.)"""
     import torch
     arr = (ctypes.c_ulonglong * max(1, int(rot_dim) // 2))()
     scale = ctypes.c_float(1.0)
