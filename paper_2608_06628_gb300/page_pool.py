@@ -38,7 +38,8 @@ class OnStream:
             return
         if not isinstance(stream, torch.cuda.Stream):
             handle = stream if isinstance(stream, int) else stream.cuda_stream
-            stream = torch.cuda.ExternalStream(handle) if handle else torch.cuda.default_stream()
+            # 0 and 1 (cudaStreamLegacy) both name the default stream
+            stream = torch.cuda.ExternalStream(handle) if handle > 1 else torch.cuda.default_stream()
         self.caller, self.scope = torch.cuda.current_stream(), torch.cuda.stream(stream)
         self.stream = stream
         self.uses(*used)

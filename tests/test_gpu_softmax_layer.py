@@ -64,6 +64,18 @@ def test_release_on_the_default_stream_by_its_handle():
     assert pool.ring.tolist() == [6, 17] and pool.lens.tolist() == [0, 33, 0]
 
 
+@pytest.mark.parametrize("handle", [1, 2])
+def test_release_on_the_runtimes_special_handles(handle):
+    """cudaStreamLegacy and cudaStreamPerThread, as the C entry points take them."""
+    pool = pool_of([20, 33, 5])
+    rows = i32([0, 2])
+    torch.cuda.synchronize()
+    pool.release(rows, stream=handle)
+    torch.cuda.synchronize()
+    H.hybrid_check()
+    assert pool.ring.tolist() == [6, 17] and pool.lens.tolist() == [0, 33, 0]
+
+
 @pytest.mark.parametrize("rows,lens,free", [([-1], [20, 33, 5], 14), ([3], [20, 33, 5], 14), ([2 ** 31 - 1, 1, -2 ** 31], [20, 0, 5], 17),
                                             ([], [20, 33, 5], 14)])
 def test_release_leaves_out_rows_that_are_not_there(rows, lens, free):
