@@ -203,6 +203,63 @@ hybrid_status hybrid_paged_attn(const hybrid_cfg *cfg, const hybrid_page_cfg *pg
                                 const int *kv_len, int n_req, int window, int n_sink, void *O, void *workspace,
                                 size_t workspace_bytes, cudaStream_t stream);
 
+/* ------------------------------------------------------------------------
+ * The cache in 8 bits.
+ *
+ *   K_cache, V_cache  [n_pages][Hkv][page_size][d] e4m3 codes, one byte each
+ *   K_scale, V_scale  [n_pages][Hkv][page_size / HYBRID_QUANT_TOKENS] float32
+ * A value is its code times the scale of its group: the HYBRID_QUANT_TOKENS tokens of
+ * one head whose places in a page have the same quotient by that number.  Scales are
+ * powers of two, so that a value is rounded once (to nearest even), and values above
+ * 2^-6 of the scale keep 4 significant bits:
+ *     scale = 2^E, E >= -126 the least with max |y| <= 448 * 2^E over the tokens written
+ * Infinities and NaN are left out of the maximum and become NaN.  Tables, slots and
+ * lengths are those of the cache above; half of a bfloat16 cache's bytes, a quarter of a
+ * float32 one's, and 4 bytes of scale for 16 d codes. */
+#define HYBRID_QUANT_TOKENS 16
+
+/* hybrid_qk_norm_rope_cache into such a cache.  Q and Qo may both be null (keys and
+ * values alone; with rot_dim = 0 and wk null they are written as they are).
+ * A call that writes the first slot of a group starts the group afresh: tokens of it
+ * that the call does not write become zeros, at the scale of those that it writes.  Any
+ * other call keeps the group's tokens: the scale is the larger of the old one and the one
+ * that the new tokens need, and where it grows the old tokens' codes are rounded again
+ * (which loses nothing above 2^-6 of the new scale).  So tokens appended in order of
+ * their positions, one or many at a time, and the active block written again at each
+ * denoising step, need nothing to be cleared first.
+ *   slots      the tokens of one group that a call writes stand next to one another (as
+ *              hybrid_page_append leaves them), among 16 of the call's tokens in a row, between
+ *              them at most tokens whose slots write nothing; otherwise the group's contents are
+ *              unspecified
+ *   K_scale, V_scale  4-byte aligned, read and written; of groups without a written
+ *              token left alone
+ * No output may share memory with another one, K, V or (but for Qo = Q) Q. */
+hybrid_status hybrid_qk_norm_rope_cache_quant(const hybrid_cfg *cfg, const hybrid_rope_cfg *rope,
+                                              const hybrid_page_cfg *pg, const void *Q, size_t q_stride,
+                                              const void *K, size_t k_stride, const void *V, size_t v_stride,
+                                              int n_tok, const void *wq, const void *wk, const int *positions,
+                                              const unsigned long long *freqs, const int *slots, void *Qo,
+                                              void *K_cache, void *V_cache, float *K_scale, float *V_scale,
+                                              cudaStream_t stream);
+
+/* Tokens read back: K, V [n_tok][Hkv][d] dense, of slots [n_tok] in any order.  io_dtype holds
+ * every value exactly (below 2^-126: rounded once).  A negative slot gives zeros; one beyond the
+ * pool gives zeros and is reported by hybrid_check().  Of cfg, n_q_heads is checked only;
+ * pg->max_pages is not read. */
+hybrid_status hybrid_cache_dequant(const hybrid_cfg *cfg, const hybrid_page_cfg *pg, const void *K_cache,
+                                   const void *V_cache, const float *K_scale, const float *V_scale,
+                                   const int *slots, int n_tok, void *K, void *V, cudaStream_t stream);
+
+/* hybrid_paged_attn over such a cache: the same arguments, limits and guarantees, Q and O in
+ * io_dtype.  Scales of groups without a visible key are not read.  The scales here may be any
+ * positive float32 numbers. */
+size_t hybrid_paged_attn_quant_workspace_bytes(const hybrid_cfg *cfg, const hybrid_page_cfg *pg, int n_req);
+hybrid_status hybrid_paged_attn_quant(const hybrid_cfg *cfg, const hybrid_page_cfg *pg, const void *Q,
+                                      const void *K_cache, const void *V_cache, const float *K_scale,
+                                      const float *V_scale, const int *block_table, const int *kv_len, int n_req,
+                                      int window, int n_sink, void *O, void *workspace, size_t workspace_bytes,
+                                      cudaStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -503,8 +503,7 @@ template <int D> cudaError_t launch_f32(const PagedArgs &a, cudaStream_t st)
 
 }  // namespace
 
-// Row tiles of at most `most` rows, of about equal size along the tokens.
-static void cut_rows(PagedArgs &a, int most)
+void paged_cut_rows(PagedArgs &a, int most)
 {
     a.Gt = a.G < most ? a.G : most;
     a.n_gt = (a.G + a.Gt - 1) / a.Gt;
@@ -522,14 +521,14 @@ void paged_geometry(const hybrid_cfg &c, PagedArgs &a)
     a.G = c.n_q_heads / c.n_kv_heads;
     a.d = c.head_dim;
     if (tc) {
-        cut_rows(a, kMaxRows);
+        paged_cut_rows(a, kMaxRows);
     } else {
         // The kernel of paged_attn_few.cu also for a few row tiles: 64 requests of 256-8192
         // tokens, 4 key heads, d = 128, here 786 us for any rows up to 64, there four tiles
         // of 8 rows 650 us, five 813, six 969 (one request of 777 tokens: 25 us here, 14
         // there).
-        cut_rows(a, kFewestRows);
-        if (a.n_gt * a.n_bt > 5) cut_rows(a, kRows);
+        paged_cut_rows(a, kFewestRows);
+        if (a.n_gt * a.n_bt > 5) paged_cut_rows(a, kRows);
     }
     const int rows = a.Bt * a.Gt;
     a.extra = tc && rows <= 64 ? 3 : 7;
@@ -555,8 +554,12 @@ cudaError_t launch_paged_attn(hybrid_dtype dt, const PagedArgs &a, cudaStream_t 
     if (bf16) e = launch_paged_attn_tc(a, st);
     else if (rows <= kFewestRows) e = launch_paged_attn_few(a, st);
     else e = a.d == 128 ? launch_f32<128>(a, st) : launch_f32<64>(a, st);
-    if (e != cudaSuccess) return e;
-    return bf16 ? launch_join<__nv_bfloat16>(a, st) : launch_join<float>(a, st);
+    return e != cudaSuccess ? e : launch_paged_join(dt, a, st);
+}
+
+cudaError_t launch_paged_join(hybrid_dtype dt, const PagedArgs &a, cudaStream_t st)
+{
+    return dt == HYBRID_BF16 ? launch_join<__nv_bfloat16>(a, st) : launch_join<float>(a, st);
 }
 
 }  // namespace hyb

@@ -22,9 +22,7 @@
 // memory's rate an SM has about 170 (backward 260) for the 512 (2 x 512) bytes of a
 // step, so what depends on the kind of row is set where the kind changes, and a
 // step only advances pointers.  Everything is float32; outputs are rounded once.
-#include "hybrid_common.cuh"
-#include "softmax_kernels.h"
-#include "tc_pipeline.cuh"
+#include "rope_rows.cuh"
 
 namespace hyb {
 namespace {
@@ -33,208 +31,9 @@ constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
 constexpr int kMaxBackwardBlocks = 512;     // partial sums of dw
 
-using ptx::f32x2;
-using ptx::pair2;
+using namespace rope;
 
-// 16 bytes of elements as pairs of float32.
-template <typename T> struct Vec {
-    static constexpr int E = 16 / sizeof(T);
-    __device__ static void unpack(const uint4 &v, f32x2 (&x)[E / 2]);
-    __device__ static uint4 pack(const f32x2 (&x)[E / 2]);
-};
-template <> __device__ __forceinline__ void Vec<float>::unpack(const uint4 &v, f32x2 (&x)[2])
-{
-    x[0] = pair2(__uint_as_float(v.x), __uint_as_float(v.y));
-    x[1] = pair2(__uint_as_float(v.z), __uint_as_float(v.w));
-}
-template <> __device__ __forceinline__ uint4 Vec<float>::pack(const f32x2 (&x)[2])
-{
-    float f[4];
-    ptx::unpair2(x[0], f[0], f[1]);
-    ptx::unpair2(x[1], f[2], f[3]);
-    return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
-}
-template <> __device__ __forceinline__ void Vec<__nv_bfloat16>::unpack(const uint4 &v, f32x2 (&x)[4])
-{
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = pair2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
-}
-template <> __device__ __forceinline__ uint4 Vec<__nv_bfloat16>::pack(const f32x2 (&x)[4])
-{
-    uint32_t w[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        float a, b;
-        ptx::unpair2(x[i], a, b);
-        w[i] = pipe::pack_bf16x2(a, b);
-    }
-    return make_uint4(w[0], w[1], w[2], w[3]);
-}
-
-// Sum over the L lanes of a head.
-template <int L> __device__ __forceinline__ float head_sum(float v)
-{
-#pragma unroll
-    for (int o = L / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-    return v;
-}
-
-constexpr int kMaxPairs = 64;
 constexpr int kDepth = 4;           // steps ahead
-
-// Layout of the pairs: interleaved, halves of part of the head, halves of all of it
-// (where the pieces' distance is known to the compiler).
-enum Layout { kInterleaved, kHalves, kAllHalves };
-
-// Where a lane's features lie in a row: two pieces of E / 2, in elements.
-template <int D, int E, Layout kLayout> struct Pieces {
-    int first, distance;            // the first piece, and from it to the second
-    int pair;                       // its first pair
-    bool on;                        // its pairs are rotated
-    __device__ Pieces(const RopeArgs &a, int l)
-    {
-        pair = l * (E / 2);
-        const int half = a.rot >> 1;
-        on = pair < half;
-        if (kLayout == kInterleaved) {
-            first = l * E;
-            distance = E / 2;
-        } else if (on) {
-            first = pair;
-            distance = half;
-        } else {                    // beyond the rotated part, halves of what is left
-            first = a.rot + (pair - half);
-            distance = D / 2 - half;
-        }
-    }
-    __device__ int apart() const { return kLayout == kAllHalves ? D / 2 : (kLayout == kInterleaved ? E / 2 : distance); }
-};
-
-// Copies of a lane's pieces; `row` points at its first piece.  No branch: a copy of
-// a row that is not there is predicated off.
-template <Layout kLayout, typename T>
-__device__ __forceinline__ void copy_async(uint32_t dst, const T *row, int apart, bool live)
-{
-    if (kLayout == kInterleaved) {
-        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %2, 0;\n\t@p cp.async.cg.shared.global [%0], [%1], 16;\n\t}" ::"r"(
-                         dst),
-                     "l"(row), "r"((int)live)
-                     : "memory");
-    } else {
-        asm volatile(
-            "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %3, 0;\n\t@p cp.async.ca.shared.global [%0], [%1], 8;\n\t"
-            "@p cp.async.ca.shared.global [%0 + 8], [%2], 8;\n\t}" ::"r"(dst),
-            "l"(row), "l"(row + apart), "r"((int)live)
-            : "memory");
-    }
-}
-template <Layout kLayout, typename T>
-__device__ __forceinline__ void store(T *row, int apart, const uint4 &v, bool live)
-{
-    if (kLayout == kInterleaved) {
-        if (live) *reinterpret_cast<uint4 *>(row) = v;
-    } else if (live) {
-        *reinterpret_cast<uint2 *>(row) = make_uint2(v.x, v.y);
-        *reinterpret_cast<uint2 *>(row + apart) = make_uint2(v.z, v.w);
-    }
-}
-template <Layout kLayout, typename T> __device__ __forceinline__ uint4 load(const T *row, int apart)
-{
-    if (kLayout == kInterleaved) return __ldg(reinterpret_cast<const uint4 *>(row));
-    const uint2 x = __ldg(reinterpret_cast<const uint2 *>(row));
-    const uint2 y = __ldg(reinterpret_cast<const uint2 *>(row + apart));
-    return make_uint4(x.x, x.y, y.x, y.y);
-}
-__device__ __forceinline__ uint4 ring_load(uint32_t at)
-{
-    uint4 v;
-    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at));
-    return v;
-}
-__device__ __forceinline__ void ring_store(uint32_t at, uint32_t v)
-{
-    asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(at), "r"(v) : "memory");
-}
-
-// Cosines and sines (times scale) of a lane's E / 2 pairs, as the packed arithmetic
-// wants them.  Half layout: c[i], s[i], ns[i] hold those of pairs 2 i and 2 i + 1
-// (i < E / 4).  Interleaved: c[i] = (cos, cos) and s[i] = (-sin, sin) of pair i.
-template <int E, bool kInter> struct Rotation {
-    static constexpr int N = kInter ? E / 2 : E / 4;
-    f32x2 c[N], s[N], ns[kInter ? 1 : N];
-};
-
-// The angles of token t, by the whole warp; `table` is the warp's own.  kInverse:
-// the rotation by -t.
-template <int E, bool kInter, bool kInverse>
-__device__ __forceinline__ void make_rotation(const RopeArgs &a, int t, int pair0, bool on, float2 *table,
-                                              Rotation<E, kInter> &r)
-{
-    const int lane = threadIdx.x & 31, half = a.rot >> 1;
-    if (half == 0) return;
-    __syncwarp();                                   // the last token's have been read
-    const unsigned long long p = (unsigned long long)(long long)__ldg(a.positions + t);
-#pragma unroll
-    for (int i = 0; i < kMaxPairs / 32; ++i) {
-        const int pair = lane + 32 * i;
-        if (pair < half) {
-            // fraction of a turn, exact modulo 1, as a signed number of half turns
-            const int frac = (int)(unsigned)((p * __ldg(a.freqs + pair)) >> 32);
-            float s, c;
-            sincospif((float)frac * 0x1p-31f, &s, &c);
-            table[pair] = make_float2(c * a.scale, (kInverse ? -s : s) * a.scale);
-        }
-    }
-    __syncwarp();
-    if (on) {
-        if (kInter) {
-#pragma unroll
-            for (int i = 0; i < E / 2; ++i) {
-                const float2 v = table[pair0 + i];
-                r.c[i] = pair2(v.x, v.x);
-                r.s[i] = pair2(-v.y, v.y);
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < E / 4; ++i) {
-                const float2 v = table[pair0 + 2 * i], w = table[pair0 + 2 * i + 1];
-                r.c[i] = pair2(v.x, w.x);
-                r.s[i] = pair2(v.y, w.y);
-                r.ns[i] = pair2(-v.y, -w.y);
-            }
-        }
-    }
-}
-
-// x <- R x for a lane whose pairs are rotated.
-template <int E, bool kInter> __device__ __forceinline__ void rotate(f32x2 (&x)[E / 2], const Rotation<E, kInter> &r)
-{
-    if (kInter) {
-#pragma unroll
-        for (int i = 0; i < E / 2; ++i) {
-            float a, b;
-            ptx::unpair2(x[i], a, b);
-            x[i] = ptx::fma2(pair2(b, a), r.s[i], ptx::mul2(x[i], r.c[i]));
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < E / 4; ++i) {
-            f32x2 &a = x[i], &b = x[E / 4 + i];
-            const f32x2 a0 = a;
-            a = ptx::fma2(b, r.ns[i], ptx::mul2(a0, r.c[i]));
-            b = ptx::fma2(a0, r.s[i], ptx::mul2(b, r.c[i]));
-        }
-    }
-}
-
-// Sum of the two halves.
-__device__ __forceinline__ float both(const f32x2 &x)
-{
-    float a, b;
-    ptx::unpair2(x, a, b);
-    return a + b;
-}
 
 // The rows of a token in steps of RPW: kinds 0 (Q), 1 (K) and, with the cache, 2
 // (V), each padded to whole steps.  The steps of all tokens are shared out evenly:
@@ -584,7 +383,7 @@ int split_rows(const RopeArgs &a, int rpw, int per_sm, bool waves, Split &s)
 {
     s.steps_q = (a.Hq + rpw - 1) / rpw;
     s.steps_k = (a.Hkv + rpw - 1) / rpw;
-    s.n_kinds = a.slots ? 3 : 2;
+    s.n_kinds = a.slots ? 3 : (a.K ? 2 : 1);
     s.steps = s.steps_q + (s.n_kinds - 1) * s.steps_k;
     const long long total = (long long)a.n_tok * s.steps, held = (long long)per_sm * pipe::sm_count() * kWarps;
     long long warps = total < held ? total : held;

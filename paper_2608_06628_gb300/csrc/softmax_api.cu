@@ -59,10 +59,10 @@ hybrid_status check_pages(const hybrid_page_cfg *p)
     return HYBRID_OK;
 }
 
-// Checks shared by the three rotation entry points, for n_tok > 0.
+// Checks shared by the rotation entry points, for n_tok > 0.
 hybrid_status check_rope(const hybrid_cfg *cfg, const hybrid_rope_cfg *rope, const void *Q, size_t q_stride,
                          const void *K, size_t k_stride, int n_tok, const void *wq, const void *wk,
-                         const int *positions, const unsigned long long *freqs)
+                         const int *positions, const unsigned long long *freqs, bool needs_q = true)
 {
     hybrid_status s = check_cfg(cfg);
     if (s != HYBRID_OK) return s;
@@ -72,12 +72,27 @@ hybrid_status check_rope(const hybrid_cfg *cfg, const hybrid_rope_cfg *rope, con
     if (!(rope->eps >= 0.f) || !std::isfinite(rope->eps) || !std::isfinite(rope->scale)) return HYBRID_ERR_INVALID_ARG;
     if (n_tok == 0) return HYBRID_OK;
     const size_t unit = cfg->io_dtype == HYBRID_BF16 ? 8 : 4;   // elements of 16 bytes
-    if (q_stride % unit != 0 || k_stride % unit != 0) return HYBRID_ERR_INVALID_ARG;
-    if (q_stride < (size_t)cfg->n_q_heads * cfg->head_dim || k_stride < (size_t)cfg->n_kv_heads * cfg->head_dim)
+    if ((needs_q && q_stride % unit != 0) || k_stride % unit != 0) return HYBRID_ERR_INVALID_ARG;
+    if ((needs_q && q_stride < (size_t)cfg->n_q_heads * cfg->head_dim) || k_stride < (size_t)cfg->n_kv_heads * cfg->head_dim)
         return HYBRID_ERR_INVALID_ARG;
-    if (!good(Q, 16) || !good(K, 16) || !good_or_null(wq, 16) || !good_or_null(wk, 16)) return HYBRID_ERR_INVALID_ARG;
+    if (!good(K, 16) || (needs_q && !good(Q, 16)) || !good_or_null(wq, 16) || !good_or_null(wk, 16)) return HYBRID_ERR_INVALID_ARG;
     if (rope->rot_dim > 0 && (!good(positions, 4) || !good(freqs, 8))) return HYBRID_ERR_INVALID_ARG;
     return HYBRID_OK;
+}
+
+// Whether one of the first `outs` of n pieces of memory shares some with another piece.
+struct Piece {
+    const void *p;
+    size_t bytes;
+};
+bool outputs_overlap(const Piece *x, int n, int outs)
+{
+    for (int i = 0; i < outs; ++i)
+        for (int j = i + 1; j < n; ++j) {
+            const uintptr_t a = reinterpret_cast<uintptr_t>(x[i].p), b = reinterpret_cast<uintptr_t>(x[j].p);
+            if (a && b && a < b + x[j].bytes && b < a + x[i].bytes) return true;
+        }
+    return false;
 }
 
 hyb::RopeArgs rope_args(const hybrid_cfg *cfg, const hybrid_rope_cfg *rope, const void *Q, size_t q_stride,
@@ -102,6 +117,60 @@ hyb::RopeArgs rope_args(const hybrid_cfg *cfg, const hybrid_rope_cfg *rope, cons
     a.scale = rope->scale;
     a.eps = rope->eps;
     return a;
+}
+
+// What the two kinds of paged attention share; `geometry` cuts a call's rows.
+using Geometry = void (*)(const hybrid_cfg &, hyb::PagedArgs &);
+
+size_t workspace_bytes_of(const hybrid_cfg *cfg, const hybrid_page_cfg *pg, int n_req, Geometry geometry)
+{
+    if (check_cfg(cfg) != HYBRID_OK || check_pages(pg) != HYBRID_OK || n_req < 0 || n_req > kMaxRequests) return 0;
+    if (cfg->block_size < 1 || cfg->block_size > 128) return 0;
+    hyb::PagedArgs a{};
+    geometry(*cfg, a);
+    return hyb::paged_workspace_bytes(a);
+}
+
+// The checks of a call and its description, the scales left to the caller (`scales`: whether they are in order).
+hybrid_status attn_args(const hybrid_cfg *cfg, const hybrid_page_cfg *pg, const void *Q, const void *K_cache, const void *V_cache,
+                        const int *block_table, const int *kv_len, int n_req, int window, int n_sink, void *O, void *workspace,
+                        size_t workspace_bytes, Geometry geometry, bool scales, hyb::PagedArgs &a)
+{
+    hybrid_status s = check_cfg(cfg);
+    if (s != HYBRID_OK) return s;
+    s = check_pages(pg);
+    if (s != HYBRID_OK) return s;
+    if (cfg->block_size < 1 || cfg->block_size > 128) return HYBRID_ERR_UNSUPPORTED;
+    if (n_req < 0 || window < 0 || n_sink < 0) return HYBRID_ERR_INVALID_ARG;
+    if (n_req > kMaxRequests) return HYBRID_ERR_UNSUPPORTED;
+    if (n_req == 0) return HYBRID_OK;
+    if (!good(Q, 16) || !good(K_cache, 16) || !good(V_cache, 16) || !scales || !good(O, 16) || !good(block_table, 4) ||
+        !good(kv_len, 4) || !good(workspace, 16))
+        return HYBRID_ERR_INVALID_ARG;
+    geometry(*cfg, a);
+    if (workspace_bytes < hyb::paged_workspace_bytes(a)) return HYBRID_ERR_INVALID_ARG;
+    // the kernels count quarters of tiles of 128 keys, of all row tiles, in an int
+    const long long quarters = 4 * (((long long)pg->max_pages * pg->page_size + 127) / 128) + a.extra;
+    if (quarters * n_req > 0x7fffffffll / ((long long)a.Hkv * a.n_gt * a.n_bt)) return HYBRID_ERR_UNSUPPORTED;
+    // no more blocks than the longest possible contexts give work, four quarters each
+    const long long most = quarters * n_req * a.Hkv * a.n_gt * a.n_bt / 4;
+    if (most < a.n_cta) a.n_cta = (int)most;
+    a.err = hyb::error_word();
+    if (!a.err) return HYBRID_ERR_CUDA;
+    a.Q = Q;
+    a.K = K_cache;
+    a.V = V_cache;
+    a.table = block_table;
+    a.lens = kv_len;
+    a.O = O;
+    hyb::paged_set_workspace(a, workspace);
+    a.n_req = n_req;
+    a.page_size = pg->page_size;
+    a.n_pages = pg->n_pages;
+    a.max_pages = pg->max_pages;
+    a.window = window;
+    a.sink = n_sink;
+    return HYBRID_OK;
 }
 
 }  // namespace
@@ -266,11 +335,7 @@ hybrid_status hybrid_qk_norm_rope_backward(const hybrid_cfg *cfg, const hybrid_r
 
 size_t hybrid_paged_attn_workspace_bytes(const hybrid_cfg *cfg, const hybrid_page_cfg *pg, int n_req)
 {
-    if (check_cfg(cfg) != HYBRID_OK || check_pages(pg) != HYBRID_OK || n_req < 0 || n_req > kMaxRequests) return 0;
-    if (cfg->block_size < 1 || cfg->block_size > 128) return 0;
-    hyb::PagedArgs a{};
-    hyb::paged_geometry(*cfg, a);
-    return hyb::paged_workspace_bytes(a);
+    return workspace_bytes_of(cfg, pg, n_req, hyb::paged_geometry);
 }
 
 hybrid_status hybrid_paged_attn(const hybrid_cfg *cfg, const hybrid_page_cfg *pg, const void *Q,
@@ -278,43 +343,113 @@ hybrid_status hybrid_paged_attn(const hybrid_cfg *cfg, const hybrid_page_cfg *pg
                                 const int *kv_len, int n_req, int window, int n_sink, void *O, void *workspace,
                                 size_t workspace_bytes, cudaStream_t stream)
 {
+    hyb::PagedArgs a{};
+    const hybrid_status s = attn_args(cfg, pg, Q, K_cache, V_cache, block_table, kv_len, n_req, window, n_sink, O, workspace,
+                                      workspace_bytes, hyb::paged_geometry, true, a);
+    if (s != HYBRID_OK || n_req == 0) return s;
+    return from_cuda(hyb::launch_paged_attn(cfg->io_dtype, a, stream));
+}
+
+hybrid_status hybrid_qk_norm_rope_cache_quant(const hybrid_cfg *cfg, const hybrid_rope_cfg *rope,
+                                              const hybrid_page_cfg *pg, const void *Q, size_t q_stride,
+                                              const void *K, size_t k_stride, const void *V, size_t v_stride,
+                                              int n_tok, const void *wq, const void *wk, const int *positions,
+                                              const unsigned long long *freqs, const int *slots, void *Qo,
+                                              void *K_cache, void *V_cache, float *K_scale, float *V_scale,
+                                              cudaStream_t stream)
+{
+    const bool queries = Q || Qo;
+    hybrid_status s = check_rope(cfg, rope, Q, q_stride, K, k_stride, n_tok, wq, wk, positions, freqs, queries);
+    if (s != HYBRID_OK) return s;
+    s = check_pages(pg);
+    if (s != HYBRID_OK || n_tok == 0) return s;
+    if (!good(V, 16) || !good(slots, 4) || (queries && !good(Qo, 16)) || !good(K_cache, 16) || !good(V_cache, 16) ||
+        !good(K_scale, 4) || !good(V_scale, 4))
+        return HYBRID_ERR_INVALID_ARG;
+    const size_t es = cfg->io_dtype == HYBRID_BF16 ? 2 : 4, d = cfg->head_dim, kv = cfg->n_kv_heads * d, q = cfg->n_q_heads * d;
+    if (v_stride % (16 / es) != 0 || v_stride < kv) return HYBRID_ERR_INVALID_ARG;
+    if (queries && Qo == Q && q_stride != q) return HYBRID_ERR_INVALID_ARG;
+    const size_t codes = (size_t)pg->n_pages * pg->page_size * kv, scales = codes / d / HYBRID_QUANT_TOKENS * sizeof(float);
+    const size_t last = n_tok - 1;
+    const Piece pieces[] = {{Qo, n_tok * q * es}, {K_cache, codes}, {V_cache, codes}, {K_scale, scales}, {V_scale, scales},
+                            {K, (last * k_stride + kv) * es}, {V, (last * v_stride + kv) * es},
+                            {Qo == Q ? nullptr : Q, (last * q_stride + q) * es}};
+    // (rows of Q, K and V interleave in a projection's output: a strided input is a piece with gaps, and no output
+    // may lie in them)
+    if (outputs_overlap(pieces, 8, 5)) return HYBRID_ERR_INVALID_ARG;
+    unsigned *err = hyb::error_word();
+    if (!err) return HYBRID_ERR_CUDA;
+    hyb::RopeArgs a = rope_args(cfg, rope, Q, q_stride, K, k_stride, n_tok, wq, wk, positions, freqs);
+    a.V = V;
+    a.v_stride = v_stride;
+    a.slots = slots;
+    a.Qo = Qo;
+    a.K_cache = K_cache;
+    a.V_cache = V_cache;
+    a.K_scale = K_scale;
+    a.V_scale = V_scale;
+    a.page_size = pg->page_size;
+    a.n_pages = pg->n_pages;
+    a.err = err;
+    return from_cuda(hyb::launch_qk_norm_rope_cache_quant(cfg->io_dtype, a, stream));
+}
+
+hybrid_status hybrid_cache_dequant(const hybrid_cfg *cfg, const hybrid_page_cfg *pg, const void *K_cache,
+                                   const void *V_cache, const float *K_scale, const float *V_scale,
+                                   const int *slots, int n_tok, void *K, void *V, cudaStream_t stream)
+{
     hybrid_status s = check_cfg(cfg);
     if (s != HYBRID_OK) return s;
     s = check_pages(pg);
     if (s != HYBRID_OK) return s;
-    if (cfg->block_size < 1 || cfg->block_size > 128) return HYBRID_ERR_UNSUPPORTED;
-    if (n_req < 0 || window < 0 || n_sink < 0) return HYBRID_ERR_INVALID_ARG;
-    if (n_req > kMaxRequests) return HYBRID_ERR_UNSUPPORTED;
-    if (n_req == 0) return HYBRID_OK;
-    if (!good(Q, 16) || !good(K_cache, 16) || !good(V_cache, 16) || !good(O, 16) || !good(block_table, 4) ||
-        !good(kv_len, 4) || !good(workspace, 16))
+    if (n_tok < 0) return HYBRID_ERR_INVALID_ARG;
+    if (n_tok == 0) return HYBRID_OK;
+    if (!good(K_cache, 16) || !good(V_cache, 16) || !good(K_scale, 4) || !good(V_scale, 4) || !good(slots, 4) ||
+        !good(K, 16) || !good(V, 16))
         return HYBRID_ERR_INVALID_ARG;
-    hyb::PagedArgs a{};
-    hyb::paged_geometry(*cfg, a);
-    if (workspace_bytes < hyb::paged_workspace_bytes(a)) return HYBRID_ERR_INVALID_ARG;
-    // the kernels count quarters of tiles of 128 keys, of all row tiles, in an int
-    const long long quarters = 4 * (((long long)pg->max_pages * pg->page_size + 127) / 128) + a.extra;
-    if (quarters * n_req > 0x7fffffffll / ((long long)a.Hkv * a.n_gt * a.n_bt)) return HYBRID_ERR_UNSUPPORTED;
-    // no more blocks than the longest possible contexts give work, four quarters each
-    const long long most = quarters * n_req * a.Hkv * a.n_gt * a.n_bt / 4;
-    if (most < a.n_cta) a.n_cta = (int)most;
+    const size_t kv = (size_t)cfg->n_kv_heads * cfg->head_dim, out = n_tok * kv * (cfg->io_dtype == HYBRID_BF16 ? 2 : 4);
+    const size_t codes = (size_t)pg->n_pages * pg->page_size * kv, scales = codes / cfg->head_dim / HYBRID_QUANT_TOKENS * sizeof(float);
+    const Piece pieces[] = {{K, out}, {V, out}, {K_cache, codes}, {V_cache, codes}, {K_scale, scales}, {V_scale, scales},
+                            {slots, n_tok * sizeof(int)}};
+    if (outputs_overlap(pieces, 7, 2)) return HYBRID_ERR_INVALID_ARG;
     unsigned *err = hyb::error_word();
     if (!err) return HYBRID_ERR_CUDA;
-    a.Q = Q;
-    a.K = K_cache;
-    a.V = V_cache;
-    a.table = block_table;
-    a.lens = kv_len;
-    a.O = O;
-    hyb::paged_set_workspace(a, workspace);
-    a.n_req = n_req;
+    hyb::DequantArgs a{};
+    a.K_cache = K_cache;
+    a.V_cache = V_cache;
+    a.K_scale = K_scale;
+    a.V_scale = V_scale;
+    a.slots = slots;
+    a.K = K;
+    a.V = V;
+    a.n_tok = n_tok;
+    a.Hkv = cfg->n_kv_heads;
+    a.d = cfg->head_dim;
     a.page_size = pg->page_size;
     a.n_pages = pg->n_pages;
-    a.max_pages = pg->max_pages;
-    a.window = window;
-    a.sink = n_sink;
     a.err = err;
-    return from_cuda(hyb::launch_paged_attn(cfg->io_dtype, a, stream));
+    return from_cuda(hyb::launch_cache_dequant(cfg->io_dtype, a, stream));
+}
+
+size_t hybrid_paged_attn_quant_workspace_bytes(const hybrid_cfg *cfg, const hybrid_page_cfg *pg, int n_req)
+{
+    return workspace_bytes_of(cfg, pg, n_req, hyb::paged_quant_geometry);
+}
+
+hybrid_status hybrid_paged_attn_quant(const hybrid_cfg *cfg, const hybrid_page_cfg *pg, const void *Q,
+                                      const void *K_cache, const void *V_cache, const float *K_scale,
+                                      const float *V_scale, const int *block_table, const int *kv_len, int n_req,
+                                      int window, int n_sink, void *O, void *workspace, size_t workspace_bytes,
+                                      cudaStream_t stream)
+{
+    hyb::PagedArgs a{};
+    const bool scales = good(K_scale, 4) && good(V_scale, 4);
+    const hybrid_status s = attn_args(cfg, pg, Q, K_cache, V_cache, block_table, kv_len, n_req, window, n_sink, O, workspace,
+                                      workspace_bytes, hyb::paged_quant_geometry, scales, a);
+    if (s != HYBRID_OK || n_req == 0) return s;
+    a.K_scale = K_scale;
+    a.V_scale = V_scale;
+    return from_cuda(hyb::launch_paged_attn_quant(cfg->io_dtype, a, stream));
 }
 
 }  // extern "C"

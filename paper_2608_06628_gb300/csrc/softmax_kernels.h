@@ -22,7 +22,7 @@ cudaError_t launch_page_release(const hybrid_page_cfg &pg, int n_req, const int 
 
 // qk_norm_rope.cu
 struct RopeArgs {
-    const void *Q, *K, *V;            // V: cache writes only
+    const void *Q, *K, *V;            // K null: queries alone; V: cache writes only
     size_t q_stride, k_stride, v_stride;
     const void *wq, *wk;              // null: no norm
     const int *positions;
@@ -33,6 +33,7 @@ struct RopeArgs {
     const void *dQo, *dKo;            // backward
     float *partial;                   // backward: [blocks][2][d]
     float *dwq, *dwk;
+    float *K_scale, *V_scale;         // 8-bit caches
     int n_tok, Hq, Hkv, d;
     int rot, interleaved, page_size, n_pages;
     float scale, eps;
@@ -42,12 +43,25 @@ cudaError_t launch_qk_norm_rope(hybrid_dtype dt, const RopeArgs &a, cudaStream_t
 cudaError_t launch_qk_norm_rope_backward(hybrid_dtype dt, const RopeArgs &a, cudaStream_t st);
 size_t qk_norm_rope_partial_bytes(int d, int n_tok);
 
+// cache_quant.cu
+cudaError_t launch_qk_norm_rope_cache_quant(hybrid_dtype dt, const RopeArgs &a, cudaStream_t st);   // Q may be null
+struct DequantArgs {
+    const void *K_cache, *V_cache;
+    const float *K_scale, *V_scale;
+    const int *slots;
+    void *K, *V;
+    int n_tok, Hkv, d, page_size, n_pages;
+    unsigned *err;
+};
+cudaError_t launch_cache_dequant(hybrid_dtype dt, const DequantArgs &a, cudaStream_t st);
+
 // paged_attn.cu (float32, and the join of split requests), paged_attn_tc.cu (bfloat16)
 namespace paged {
 struct JoinNote;
 }
 struct PagedArgs {
     const void *Q, *K, *V;
+    const float *K_scale, *V_scale;   // 8-bit caches
     const int *table, *lens;
     void *O;
     paged::JoinNote *notes;           // workspace, see paged_plan.cuh
@@ -69,5 +83,12 @@ cudaError_t launch_paged_attn_tc(const PagedArgs &a, cudaStream_t st);
 constexpr int kFewestRows = 8;
 cudaError_t launch_paged_attn_few(const PagedArgs &a, cudaStream_t st);
 cudaError_t launch_paged_attn(hybrid_dtype dt, const PagedArgs &a, cudaStream_t st);
+// The join of a call whose attention kernel was launched just before.
+cudaError_t launch_paged_join(hybrid_dtype dt, const PagedArgs &a, cudaStream_t st);
+// paged_attn_quant.cu: the same over an 8-bit cache
+void paged_quant_geometry(const hybrid_cfg &c, PagedArgs &a);
+cudaError_t launch_paged_attn_quant(hybrid_dtype dt, const PagedArgs &a, cudaStream_t st);
+// Row tiles of at most `most` rows, of about equal size along the tokens.
+void paged_cut_rows(PagedArgs &a, int most);
 
 }  // namespace hyb

@@ -34,7 +34,11 @@ EXPORTED = (
     "hybrid_page_append", "hybrid_page_release", "hybrid_rope_freqs", "hybrid_qk_norm_rope",
     "hybrid_qk_norm_rope_cache", "hybrid_qk_norm_rope_workspace_bytes", "hybrid_qk_norm_rope_backward",
     "hybrid_paged_attn_workspace_bytes", "hybrid_paged_attn",
+    "hybrid_qk_norm_rope_cache_quant", "hybrid_cache_dequant", "hybrid_paged_attn_quant_workspace_bytes",
+    "hybrid_paged_attn_quant",
 )
+
+HYBRID_QUANT_TOKENS = 16      # tokens of a head that share a scale in an 8-bit cache
 
 HYBRID_ROPE_NONE = 0
 HYBRID_ROPE_LINEAR = 1
@@ -131,9 +135,15 @@ def lib(path: str | None = None):
     L.hybrid_paged_attn_workspace_bytes.argtypes = [cfgp, pgp, I]
     L.hybrid_paged_attn_workspace_bytes.restype = S
     L.hybrid_paged_attn.argtypes = [cfgp, pgp, P, P, P, P, P, I, I, I, P, P, S, P]
+    L.hybrid_qk_norm_rope_cache_quant.argtypes = [cfgp, ropep, pgp, P, S, P, S, P, S, I, P, P, P, P, P, P, P, P, P, P, P]
+    L.hybrid_cache_dequant.argtypes = [cfgp, pgp, P, P, P, P, P, I, P, P, P]
+    L.hybrid_paged_attn_quant_workspace_bytes.argtypes = [cfgp, pgp, I]
+    L.hybrid_paged_attn_quant_workspace_bytes.restype = S
+    L.hybrid_paged_attn_quant.argtypes = [cfgp, pgp, P, P, P, P, P, P, P, I, I, I, P, P, S, P]
     for name in EXPORTED:
         if name not in ("hybrid_state_bytes", "hybrid_status_str", "hybrid_train_workspace_bytes",
-                        "hybrid_qk_norm_rope_workspace_bytes", "hybrid_paged_attn_workspace_bytes"):
+                        "hybrid_qk_norm_rope_workspace_bytes", "hybrid_paged_attn_workspace_bytes",
+                        "hybrid_paged_attn_quant_workspace_bytes"):
             getattr(L, name).restype = ctypes.c_int
     if path == _build.LIB_PATH:
         _lib = L
@@ -359,3 +369,31 @@ def hybrid_paged_attn(cfg, pg, Q, K_cache, V_cache, block_table, kv_len, n_req, 
     st = lib().hybrid_paged_attn(cfg, pg, _ptr(Q), _ptr(K_cache), _ptr(V_cache), _ptr(block_table), _ptr(kv_len),
                                  n_req, window, n_sink, _ptr(O), _ptr(workspace), workspace_bytes, _stream(stream))
     return _ret(st, "hybrid_paged_attn", check)
+
+
+# ---------------------------------------------------------------- the cache in 8 bits
+
+def hybrid_qk_norm_rope_cache_quant(cfg, rope, pg, Q, q_stride, K, k_stride, V, v_stride, n_tok, wq, wk, positions, freqs,
+                                    slots, Qo, K_cache, V_cache, K_scale, V_scale, stream=None, check=True):
+    st = lib().hybrid_qk_norm_rope_cache_quant(cfg, rope, pg, _ptr(Q), q_stride, _ptr(K), k_stride, _ptr(V), v_stride, n_tok,
+                                               _ptr(wq), _ptr(wk), _ptr(positions), _ptr(freqs), _ptr(slots), _ptr(Qo),
+                                               _ptr(K_cache), _ptr(V_cache), _ptr(K_scale), _ptr(V_scale), _stream(stream))
+    return _ret(st, "hybrid_qk_norm_rope_cache_quant", check)
+
+
+def hybrid_cache_dequant(cfg, pg, K_cache, V_cache, K_scale, V_scale, slots, n_tok, K, V, stream=None, check=True):
+    st = lib().hybrid_cache_dequant(cfg, pg, _ptr(K_cache), _ptr(V_cache), _ptr(K_scale), _ptr(V_scale), _ptr(slots), n_tok,
+                                    _ptr(K), _ptr(V), _stream(stream))
+    return _ret(st, "hybrid_cache_dequant", check)
+
+
+def hybrid_paged_attn_quant_workspace_bytes(cfg, pg, n_req) -> int:
+    return int(lib().hybrid_paged_attn_quant_workspace_bytes(cfg, pg, n_req))
+
+
+def hybrid_paged_attn_quant(cfg, pg, Q, K_cache, V_cache, K_scale, V_scale, block_table, kv_len, n_req, window, n_sink, O,
+                            workspace, workspace_bytes, stream=None, check=True):
+    st = lib().hybrid_paged_attn_quant(cfg, pg, _ptr(Q), _ptr(K_cache), _ptr(V_cache), _ptr(K_scale), _ptr(V_scale),
+                                       _ptr(block_table), _ptr(kv_len), n_req, window, n_sink, _ptr(O), _ptr(workspace),
+                                       workspace_bytes, _stream(stream))
+    return _ret(st, "hybrid_paged_attn_quant", check)

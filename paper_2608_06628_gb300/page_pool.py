@@ -6,6 +6,10 @@ serving loop never waits for the host to count pages.  Those calls read one copy
 lengths and ring and write another, which the pool copies back: its tensors stay
 the same ones, and a captured graph may hold any number of calls.  Rows of the table
 are the requests of the batch; a released row may take a new request at once.
+
+With quant=True keys and values are held in 8 bits (e4m3 codes, and a float32 scale for each
+16 tokens of a head in k_scale, v_scale): SoftmaxLayer writes and reads such a pool like any
+other, and load() and store() bring tokens out of it and into it.
 """
 from __future__ import annotations
 
@@ -83,14 +87,20 @@ class BlockRows:
 
 class PagePool:
     def __init__(self, cfg: H.hybrid_cfg, n_req: int, n_pages: int, max_len: int, page_size: int = 32, n_layers: int = 1,
-                 device="cuda"):
-        self.cfg, self.n_req, self.n_layers = cfg, n_req, n_layers
+                 device="cuda", quant: bool = False):
+        self.cfg, self.n_req, self.n_layers, self.quant = cfg, n_req, n_layers, quant
         self.pg = H.make_page_cfg(page_size, n_pages, -(-max_len // page_size))
         dtype = torch.bfloat16 if cfg.io_dtype == H.HYBRID_BF16 else torch.float32
         shape = (n_layers, n_pages, cfg.n_kv_heads, page_size, cfg.head_dim)
-        self.k_cache = torch.empty(shape, dtype=dtype, device=device)
-        self.v_cache = torch.empty(shape, dtype=dtype, device=device)
-        self.device = self.k_cache.device
+        held = torch.float8_e4m3fn if quant else dtype
+        self.k_cache = torch.empty(shape, dtype=held, device=device)
+        self.v_cache = torch.empty(shape, dtype=held, device=device)
+        self.dtype, self.device = dtype, self.k_cache.device
+        self.k_scale = self.v_scale = None
+        if quant:
+            scales = (*shape[:3], page_size // H.HYBRID_QUANT_TOKENS)
+            self.k_scale = torch.empty(scales, dtype=torch.float32, device=device)
+            self.v_scale = torch.empty(scales, dtype=torch.float32, device=device)
         self.block_table = torch.full((n_req, self.pg.max_pages), -1, dtype=torch.int32, device=device)
         self.free_pages = torch.arange(n_pages, dtype=torch.int32, device=device)
         # {head, count} of the ring, the lengths, and an entry that release() writes for rows that are not there; then
@@ -100,7 +110,8 @@ class PagePool:
         now, then = self._state
         self._now, self._then, self._ring, self._lens = now[:-1], then[:-1], now[:2], now[2:-1]
         self._then_ring, self._then_lens, self._lens_and_spare = then[:2], then[2:-1], now[2:]
-        self.workspace_bytes = H.hybrid_paged_attn_workspace_bytes(cfg, self.pg, n_req)
+        self._attn_bytes = H.hybrid_paged_attn_quant_workspace_bytes if quant else H.hybrid_paged_attn_workspace_bytes
+        self.workspace_bytes = self._attn_bytes(cfg, self.pg, n_req)
         if self.workspace_bytes == 0:
             raise ValueError(f"unsupported {cfg} with {self.pg}")
         self.workspace = torch.empty(self.workspace_bytes, dtype=torch.uint8, device=device)
@@ -128,7 +139,7 @@ class PagePool:
         capturing = self.device.type == "cuda" and torch.cuda.is_current_stream_capturing()
         made = None if capturing else self._workspaces.get(key)
         if made is None:
-            n = H.hybrid_paged_attn_workspace_bytes(cfg, self.pg, self.n_req)
+            n = self._attn_bytes(cfg, self.pg, self.n_req)
             if n == 0:
                 raise ValueError(f"unsupported {cfg} with {self.pg}")
             if not capturing and not self._workspaces and n == self.workspace_bytes:
@@ -139,6 +150,11 @@ class PagePool:
                 self._workspaces[key] = made
         on.uses(made)
         return made
+
+    def caches(self, layer: int):
+        """A layer's memory as the entry points take it: K and V, then the scales of an 8-bit pool."""
+        kv = (self.k_cache[layer], self.v_cache[layer])
+        return (*kv, self.k_scale[layer], self.v_scale[layer]) if self.quant else kv
 
     def append(self, n_new: torch.Tensor, n_tok: int, stream=None):
         """Room for n_new [n_req] (int32, device) more tokens of each request, at most n_tok in all.
@@ -173,3 +189,43 @@ class PagePool:
             self._ring.copy_(self._then_ring)
             # rows below 0 and above the last all become the entry behind the lengths (-1 counts from the end)
             self._lens_and_spare.index_fill_(0, rows.long().clamp_(-1, self.n_req), 0)
+
+    def slots_of(self, row: int, start: int, stop: int) -> torch.Tensor:
+        """Slots (int32) of the tokens start ... stop - 1 of a request, which the cache holds."""
+        P = self.pg.page_size
+        if not (0 <= row < self.n_req and 0 <= start <= stop <= self.pg.max_pages * P):
+            raise ValueError(f"tokens {start} ... {stop} of row {row}: {self.n_req} rows of {self.pg.max_pages * P} tokens")
+        j = torch.arange(start, stop, dtype=torch.int32, device=self.device)
+        return self.block_table[row].index_select(0, j // P) * P + j % P
+
+    def _quantised(self, layer, slots, what: str):
+        """The layer's memory and the number of slots, for load and store."""
+        if not self.quant:
+            raise ValueError(f"{what}: of an 8-bit pool (quant=True); others are indexed as tensors")
+        if not isinstance(layer, int) or not 0 <= layer < self.n_layers:
+            raise IndexError(f"layer {layer} of {self.n_layers}")
+        n = slots.numel() if isinstance(slots, torch.Tensor) else 0
+        expect(slots, "slots", torch.int32, self.device, n)
+        return self.caches(layer), n
+
+    def load(self, layer: int, slots: torch.Tensor, stream=None):
+        """Keys and values [n, Hkv, d] (io type) of the tokens in slots (int32, device) of an 8-bit pool, in any
+        order; zeros for negative slots."""
+        caches, n = self._quantised(layer, slots, "load")
+        shape = (n, self.cfg.n_kv_heads, self.cfg.head_dim)
+        with OnStream(stream, slots, *caches) as on:
+            k, v = (torch.empty(shape, dtype=self.dtype, device=self.device) for _ in range(2))
+            H.hybrid_cache_dequant(self.cfg, self.pg, *caches, slots, n, k, v)
+            return on.returns(k, v)
+
+    def store(self, layer: int, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, stream=None):
+        """Keys and values [n, Hkv, d] as they are (rotated already) into slots of an 8-bit pool. Tokens of 16 slots that
+        share a scale stand next to one another, as append and slots_of leave them."""
+        caches, n = self._quantised(layer, slots, "store")
+        c = self.cfg
+        for x, what in ((k, "k"), (v, "v")):
+            expect(x, what, self.dtype, self.device, n, c.n_kv_heads, c.head_dim)
+        row, as_is = c.n_kv_heads * c.head_dim, H.hybrid_rope_cfg(0, 0, 1.0, 0.0)
+        with OnStream(stream, k, v, slots, *caches):
+            H.hybrid_qk_norm_rope_cache_quant(c, as_is, self.pg, None, 0, k, row, v, row, n, None, None, None, None, slots, None,
+                                              *caches)

@@ -8,6 +8,9 @@ PagePool whose append() has made room for those tokens. Shapes, types and layout
     slots, positions, offsets = pool.append(n_new, n_tok)
     rows = pool.block_rows(offsets, n_tok)     # unless every request has a whole block of new tokens
     out = layer.step(qkv, pool, i, slots, positions, rows=rows)
+
+An 8-bit pool (quant=True) is used in the same way: keys and values are rounded as they are
+written, and attention reads the codes.
 """
 from __future__ import annotations
 
@@ -54,11 +57,12 @@ class SoftmaxLayer:
         q = qkv.data_ptr()
         k = q + c.n_q_heads * c.head_dim * qkv.element_size()
         v = k + c.n_kv_heads * c.head_dim * qkv.element_size()
-        kc, vc = pool.k_cache[layer], pool.v_cache[layer]
-        with OnStream(stream, qkv, slots, positions, self.wq, self.wk, self.freqs, kc, vc) as on:
+        caches = pool.caches(layer)
+        into = H.hybrid_qk_norm_rope_cache_quant if pool.quant else H.hybrid_qk_norm_rope_cache
+        with OnStream(stream, qkv, slots, positions, self.wq, self.wk, self.freqs, *caches) as on:
             out = torch.empty((n_tok, c.n_q_heads, c.head_dim), dtype=qkv.dtype, device=dev)
-            H.hybrid_qk_norm_rope_cache(c, self.rope, pool.pg, q, step, k, step, v, step, n_tok, self.wq, self.wk, positions,
-                                        self.freqs, slots, out, kc, vc)
+            into(c, self.rope, pool.pg, q, step, k, step, v, step, n_tok, self.wq, self.wk, positions, self.freqs, slots, out,
+                 *caches)
             return on.returns(out)
 
     def attend(self, q, pool: PagePool, layer: int, stream=None, rows: BlockRows | None = None):
@@ -76,8 +80,9 @@ class SoftmaxLayer:
         else:
             lead = (rows.n_tok,)
         expect(q, "q", self.dtype, pool.device, *lead, c.n_q_heads, c.head_dim)
-        kc, vc = pool.k_cache[layer], pool.v_cache[layer]
-        with OnStream(stream, q, kc, vc, pool.block_table, pool.lens) as on:
+        caches = pool.caches(layer)
+        attention = H.hybrid_paged_attn_quant if pool.quant else H.hybrid_paged_attn
+        with OnStream(stream, q, *caches, pool.block_table, pool.lens) as on:
             if rows is None:
                 out = torch.empty_like(q)
             elif rows.n_tok == 0:
@@ -88,8 +93,8 @@ class SoftmaxLayer:
                 out = torch.empty((n_rows + 2, *q.shape[1:]), dtype=q.dtype, device=q.device)
                 out[n_rows:].copy_(pool.no_row)
             workspace = pool.workspace_of(c, on)
-            H.hybrid_paged_attn(c, pool.pg, q, kc, vc, pool.block_table, pool.lens, pool.n_req, self.window, self.n_sink,
-                                out, workspace, workspace.numel())
+            attention(c, pool.pg, q, *caches, pool.block_table, pool.lens, pool.n_req, self.window, self.n_sink, out, workspace,
+                      workspace.numel())
             return on.returns(out if rows is None else out.index_select(0, rows.row))
 
     def step(self, qkv, pool: PagePool, layer: int, slots, positions, stream=None, rows: BlockRows | None = None):

@@ -1,0 +1,737 @@
+"""The 8-bit paged cache on the GPU against its definition in 64 bits (quant_reference.py).
+
+Bounds, from the arithmetic (eps32 = 2^-24):
+  codes      half an e4m3 step: 2^-4 of the value, 2^-10 of the scale below 2^-6 of it; where keys are
+             normalised and rotated, also that operator's 32 eps32 = 2e-6 of the row's largest entry,
+             which may carry a value over a step's border (a step of up to 2^-3 in the place of half
+             of one: the bound adds 1.07 times the error itself, since both borders move with it), and
+             the same relative error of the group's largest entry at a border of its scale.  Kept and
+             moved codes are equal.
+  read       codes times a power of two: exact in both types.
+  attention  the bounds of attention over the 16/32-bit cache (gpu_harness.TOL).
+"""
+import math
+import random
+
+import numpy as np
+import pytest
+import torch
+
+import quant_reference as Q
+import softmax_reference as R
+from gpu_harness import assert_parity
+from paper_2608_06628_gb300 import hybrid as H
+from paper_2608_06628_gb300.page_pool import PagePool
+from paper_2608_06628_gb300.softmax_layer import SoftmaxLayer
+from quant_reference import F8, GROUP
+
+pytestmark = pytest.mark.gpu
+BF, F32 = torch.bfloat16, torch.float32
+EPS = 1e-6
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _device():
+    if not torch.cuda.is_available():
+        pytest.skip("no CUDA device")
+    from paper_2608_06628_gb300 import build
+    build.build()
+    torch.cuda.set_device(0)
+
+
+def i32(v):
+    return torch.tensor(v, dtype=torch.int32, device="cuda")
+
+
+def gen(seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return g
+
+
+def random_cache(n_pages, Hkv, P, d, seed, spread=2):
+    """Any codes but NaN, and scales 2^-spread ... 2^spread."""
+    g = gen(seed)
+    codes = torch.randint(0, 256, (n_pages, Hkv, P, d), generator=g, device="cuda").to(torch.uint8)
+    codes[(codes & 0x7f) == Q.NAN] = 0
+    scales = torch.exp2(torch.randint(-spread, spread + 1, (n_pages, Hkv, P // GROUP), generator=g, device="cuda").float())
+    return codes.view(F8), scales
+
+
+def copies(*tensors):
+    return [t.view(torch.uint8).clone().view(t.dtype) if t.dtype == F8 else t.clone() for t in tensors]
+
+
+# ------------------------------------------------------------------ writes
+
+def packed_slots(rng, P, ranges):
+    """Slots of tokens start ... start + new - 1 of each request, with pages of its own, and the number of pages."""
+    used = [[(s + n - 1) // P - s // P + 1 if n else 0 for s, n in ranges]][0]
+    ids = list(range(sum(used) + 2))
+    rng.shuffle(ids)
+    slots, pos = [], []
+    for (start, n), k in zip(ranges, used):
+        pages = [ids.pop() for _ in range(k)]
+        for p in range(start, start + n):
+            slots.append(pages[p // P - start // P] * P + p % P)
+            pos.append(p)
+    return slots, pos, sum(used) + 2
+
+
+def write_setup(dt, ranges, Hq, Hkv, d, P, rot=None, inter=False, norm=True, seed=0, scale=1.0):
+    rng, g = random.Random(seed), gen(seed)
+    slots, pos, n_pages = packed_slots(rng, P, ranges)
+    T, rot = len(slots), d if rot is None else rot
+    width = (Hq + 2 * Hkv) * d
+    wide = (torch.randn(T, width + 16, generator=g, device="cuda") * scale).to(dt)[:, :width].unflatten(1, (-1, d))
+    w = (1 + 0.1 * torch.randn(2, d, generator=g, device="cuda")).to(dt)
+    rope, freqs = H.make_rope(rot, inter, eps=EPS, base=10000.0, device="cuda")
+    kc, ks = random_cache(n_pages, Hkv, P, d, seed + 1)
+    vc, vs = random_cache(n_pages, Hkv, P, d, seed + 2)
+    return dict(dt=dt, T=T, Hq=Hq, Hkv=Hkv, d=d, P=P, rot=rot, inter=inter, q=wide[:, :Hq], k=wide[:, Hq:Hq + Hkv], v=wide[:, Hq + Hkv:],
+                stride=width + 16, wq=w[0] if norm else None, wk=w[1] if norm else None, rope=rope, freqs=freqs, pos=i32(pos),
+                slots=i32(slots), cfg=H.make_cfg(d, 64, Hq, Hkv, 1, dt), pg=H.make_page_cfg(P, n_pages, 1), n_pages=n_pages,
+                cache=[kc, vc, ks, vs])
+
+
+def run_write(s, queries=True, stream=None):
+    qo = torch.full((s["T"], s["Hq"], s["d"]), 7.0, dtype=s["dt"], device="cuda")
+    H.hybrid_qk_norm_rope_cache_quant(s["cfg"], s["rope"], s["pg"], s["q"] if queries else None, s["stride"] if queries else 0, s["k"],
+                                      s["stride"], s["v"], s["stride"], s["T"], s["wq"], s["wk"], s["pos"] if s["rot"] else None,
+                                      s["freqs"] if s["rot"] else None, s["slots"], qo if queries else None, *s["cache"], stream=stream)
+    return qo
+
+
+def keys_of(s):
+    t, scale = R.turns(s["rot"]) if s["rot"] else ([], 1.0)
+    return R.norm_rotate(s["k"].double(), None if s["wk"] is None else s["wk"].double(), s["pos"], t, scale, s["inter"], EPS)
+
+
+def check_write(s, before, what):
+    slots = s["slots"].tolist()
+    kc, vc, ks, vs = s["cache"]
+    exact = s["wk"] is None and s["rot"] == 0
+    Q.check_write((before[0], before[2]), (kc, ks), keys_of(s), slots, 0.0 if exact else 2e-6, what + " keys")
+    Q.check_write((before[1], before[3]), (vc, vs), s["v"].double(), slots, 0.0, what + " values")
+
+
+RANGES = [
+    [(0, 1)], [(5, 1), (0, 3), (15, 1), (16, 1), (31, 2)], [(0, 16), (0, 17), (3, 45), (15, 2), (14, 100), (130, 129)],
+    [(x, 32) for x in (0, 7, 16, 100, 127)], [(x, 1) for x in range(70)], [(0, 0), (9, 300), (0, 0)],
+]
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("ranges", RANGES, ids=str)
+@pytest.mark.parametrize("Hq,Hkv,d,P,rot,inter,norm", [(16, 4, 128, 16, 128, False, True), (3, 3, 64, 64, 48, True, False),
+                                                       (10, 2, 128, 128, 80, False, True), (4, 1, 64, 32, 0, False, True)])
+def test_writes(dt, ranges, Hq, Hkv, d, P, rot, inter, norm):
+    s = write_setup(dt, ranges, Hq, Hkv, d, P, rot, inter, norm, seed=len(ranges))
+    before = copies(*s["cache"])
+    qo = run_write(s)
+    H.hybrid_check()
+    check_write(s, before, f"{dt} P{P}")
+    # the queries are those of the dense operator
+    want, ko = torch.empty_like(qo), torch.empty(s["T"], Hkv, d, dtype=dt, device="cuda")
+    H.hybrid_qk_norm_rope(s["cfg"], s["rope"], s["q"], s["stride"], s["k"], s["stride"], s["T"], s["wq"], s["wk"], s["pos"],
+                          s["freqs"], want, ko)
+    assert torch.equal(qo, want)
+    # keys and values alone, from the same beginning, give the same bits
+    after = s["cache"]
+    s["cache"] = before
+    run_write(s, queries=False)
+    H.hybrid_check()
+    for x, y in zip(s["cache"], after):
+        assert torch.equal(x.view(torch.uint8), y.view(torch.uint8))
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
+def test_writes_of_many_tokens(dt):
+    rng = random.Random(3)
+    s = write_setup(dt, [(rng.randint(0, 50), rng.randint(1, 150)) for _ in range(80)], 2, 2, 64, 32, seed=9)
+    before = copies(*s["cache"])
+    run_write(s)
+    H.hybrid_check()
+    check_write(s, before, "many")
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("Hkv", [1, 16, 80])
+def test_writes_as_they_are(dt, Hkv):
+    s = write_setup(dt, [(0, 40), (7, 9), (3, 1)], Hkv, Hkv, 64, 16, rot=0, norm=False, seed=Hkv, scale=30.0)
+    before = copies(*s["cache"])
+    run_write(s, queries=False)
+    H.hybrid_check()
+    check_write(s, before, "as they are")
+
+
+def test_values_at_the_ends_of_the_range():
+    """Zeros, subnormals, the largest numbers, infinities and NaN; scales at both ends and at their borders."""
+    d, P = 64, 16
+    rows = [torch.zeros(d), torch.full((d,), 1e-45), torch.full((d,), 2.0 ** -126), torch.full((d,), 448.0), torch.full((d,), 448.0 + 2 ** -15),
+            torch.full((d,), 3.4e38), torch.full((d,), math.inf), torch.full((d,), -math.inf), torch.full((d,), math.nan),
+            torch.full((d,), 448.0 * 2.0 ** -126), torch.full((d,), 2.0 ** 120), torch.linspace(-1, 1, d), torch.linspace(-500, 500, d)]
+    for i in (6, 7, 8):                                      # beside finite ones
+        rows.append(torch.where(torch.arange(d) % 7 == 0, rows[i], torch.linspace(-3, 3, d)))
+    # a group for each row alone, then groups of all rows, of which the scale is the largest one's
+    ranges = [(0, 1)] * len(rows) + [(0, 16), (5, 11)]
+    s = write_setup(F32, ranges, 1, 1, d, P, rot=0, norm=False)
+    x = torch.stack(rows + rows + rows[:11])
+    assert len(rows) == 16 and len(x) == s["T"]
+    s["k"].copy_(x[:, None])
+    s["v"].copy_(x.flip(1)[:, None])
+    before = copies(*s["cache"])
+    run_write(s, queries=False)
+    H.hybrid_check()
+    check_write(s, before, "ends of the range")
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("steps", [[1] * 50, [7] * 7, [3, 1, 40, 6], [16, 16, 18]])
+def test_appending_in_parts(dt, steps):
+    """Tokens written one or many at a time, into pages that held something else: as written at once, but for values up to
+    2^-6 of the scale, which may be rounded twice (an error of one step of 2^-9 of it instead of half)."""
+    T, Hkv, d, P = sum(steps), 2, 64, 32
+    s = write_setup(dt, [(0, T)], 4, Hkv, d, P, seed=T)
+    # tokens that grow, so that scales move
+    grow = torch.exp2(torch.arange(T, device="cuda") % 16 * 0.5)[:, None, None]
+    s["k"].copy_((s["k"].float() * grow).to(dt))
+    s["v"].copy_((s["v"].float() * grow).to(dt))
+    s["wk"] = s["wq"] = None
+    parts = dict(s, cache=copies(*s["cache"]))
+    run_write(s)
+    at = 0
+    for n in steps:
+        part = dict(parts, T=n, **{x: s[x][at:at + n] for x in ("q", "k", "v", "pos", "slots")})
+        run_write(part)
+        at += n
+    H.hybrid_check()
+    for c in (0, 1):
+        assert torch.equal(s["cache"][c + 2], parts["cache"][c + 2])
+        a, b = Q.values(s["cache"][c], s["cache"][c + 2]), Q.values(parts["cache"][c], parts["cache"][c + 2])
+        scale = s["cache"][c + 2].double().repeat_interleave(GROUP, 2)[..., None]
+        assert bool(((a - b).abs() <= torch.where(a.abs() <= scale * 2.0 ** -6, scale * 2.0 ** -9, 0.0)).all())
+
+
+def test_the_active_block_again():
+    """Each denoising step writes the block's tokens again: groups that the block begins start afresh, the scale of the
+    one that it shares with the prompt stays or grows."""
+    s = write_setup(BF, [(21, 32)], 4, 2, 128, 32, seed=4)
+    for i in range(4):
+        s["v"].mul_(0.5 if i % 2 else 4.0)
+        s["k"].copy_(torch.randn(s["k"].shape, generator=gen(i), device="cuda"))
+        before = copies(*s["cache"])
+        run_write(s)
+        H.hybrid_check()
+        check_write(s, before, f"step {i}")
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
+def test_slots_that_are_not_there(dt):
+    s = write_setup(dt, [(3, 40), (0, 9), (30, 5)], 2, 2, 64, 32, seed=8)
+    s["slots"][::5] = -1
+    s["slots"][1] = -2 ** 31
+    before = copies(*s["cache"])
+    run_write(s)
+    H.hybrid_check()
+    check_write(s, before, "padding")
+    s["slots"][7], s["slots"][20] = s["n_pages"] * s["P"], 2 ** 31 - 1
+    before = copies(*s["cache"])
+    run_write(s)
+    assert H.hybrid_check(check=False) == H.HYBRID_ERR_DEVICE and H.hybrid_check(check=False) == H.HYBRID_OK
+    check_write(s, before, "beyond the pool")
+    s["slots"].fill_(-1)
+    before = copies(*s["cache"])
+    run_write(s)
+    H.hybrid_check()
+    check_write(s, before, "padding alone")
+
+
+def test_repeated_slots_stay_in_bounds():
+    """The same slots more than once, side by side or apart: unspecified there, nothing else written."""
+    s = write_setup(BF, [(0, 64)], 2, 2, 64, 16, seed=8)
+    s["slots"][:40] = s["slots"][0]
+    s["slots"][50] = s["slots"][63]
+    before = copies(*s["cache"])
+    run_write(s)
+    H.hybrid_check()
+    touched = {x // 16 for x in s["slots"].tolist()}
+    for x, y in zip(s["cache"], before):
+        for page in range(s["n_pages"]):
+            if page not in touched:
+                assert torch.equal(x[page].view(torch.uint8), y[page].view(torch.uint8))
+
+
+def test_write_in_place_and_same_bits():
+    s = write_setup(BF, [(5, 70), (0, 3)], 4, 2, 128, 16, seed=5)
+    dense = s["q"].contiguous()
+    first, want = copies(*s["cache"]), None
+    for stream in (None, torch.cuda.Stream()):
+        s["cache"] = copies(*first)
+        torch.cuda.synchronize()
+        q = dense.clone()
+        torch.cuda.synchronize()
+        H.hybrid_qk_norm_rope_cache_quant(s["cfg"], s["rope"], s["pg"], q, 4 * 128, s["k"], s["stride"], s["v"], s["stride"], s["T"],
+                                          s["wq"], s["wk"], s["pos"], s["freqs"], s["slots"], q, *s["cache"], stream=stream)
+        torch.cuda.synchronize()
+        H.hybrid_check()
+        got = [q.view(torch.uint8)] + [x.view(torch.uint8) for x in s["cache"]]
+        want = want or got
+        assert all(torch.equal(x, y) for x, y in zip(got, want))
+    s["cache"] = copies(*first)
+    assert torch.equal(run_write(s).view(torch.uint8), want[0])
+
+
+# ------------------------------------------------------------------ reading back
+
+def read(cfg, pg, cache, slots, dt):
+    k, v = (torch.full((slots.numel(), cfg.n_kv_heads, cfg.head_dim), 7.0, dtype=dt, device="cuda") for _ in range(2))
+    H.hybrid_cache_dequant(cfg, pg, *cache, slots, slots.numel(), k, v)
+    return k, v
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("T,Hkv,d,P", [(1, 1, 64, 16), (333, 4, 64, 16), (1000, 3, 128, 128), (20000, 2, 128, 32)])
+def test_reading_back(dt, T, Hkv, d, P):
+    n_pages = 40
+    kc, ks = random_cache(n_pages, Hkv, P, d, 1, 100)
+    vc, vs = random_cache(n_pages, Hkv, P, d, 2, 100)
+    kc.view(torch.uint8)[3] = torch.arange(P * d, device="cuda").view(P, d).to(torch.uint8)     # every code
+    slots = torch.randint(0, n_pages * P, (T,), generator=gen(T), device="cuda").to(torch.int32)
+    if T > 1:
+        slots[::7] = -1
+        slots[1:12] = torch.arange(3 * P, 3 * P + 11, device="cuda")
+    cfg, pg = H.make_cfg(d, 64, Hkv, Hkv, 1, dt), H.make_page_cfg(P, n_pages, 1)
+    k, v = read(cfg, pg, (kc, vc, ks, vs), slots, dt)
+    H.hybrid_check()
+    sl = slots.clamp(min=0).long()
+    for got, codes, scales in ((k, kc, ks), (v, vc, vs)):
+        want = Q.values(codes, scales)[sl // P, :, sl % P]
+        want[slots < 0] = 0.0
+        assert torch.equal(got.double().nan_to_num(nan=12345.0), want.nan_to_num(nan=12345.0))
+    slots[0] = n_pages * P
+    slots[T // 2] = 2 ** 31 - 1
+    k2, v2 = read(cfg, pg, (kc, vc, ks, vs), slots, dt)
+    assert H.hybrid_check(check=False) == H.HYBRID_ERR_DEVICE and H.hybrid_check(check=False) == H.HYBRID_OK
+    assert not k2[0].any() and not v2[T // 2].any()
+    if T > 2:
+        assert torch.equal(k2[1].view(torch.uint8), k[1].view(torch.uint8))
+
+
+def test_far_pages():
+    """A cache of more than 2^31 codes: writes, reads and attention at its end."""
+    P, d, n_pages = 128, 128, 140000
+    assert n_pages * P * d > 2 ** 31
+    kc, vc = (torch.empty(n_pages, 1, P, d, dtype=F8, device="cuda") for _ in range(2))
+    ks, vs = (torch.empty(n_pages, 1, P // GROUP, device="cuda") for _ in range(2))
+    cfg, pg = H.make_cfg(d, 64, 4, 1, 1, BF), H.make_page_cfg(P, n_pages, 4)
+    table = i32([[n_pages - 1, n_pages - 50, n_pages - 3, -1]])
+    j = torch.arange(300, device="cuda")
+    slots = (table[0][j // P] * P + j % P).to(torch.int32)
+    k, v = torch.randn(2, 300, 1, d, generator=gen(0), device="cuda").to(BF)
+    H.hybrid_qk_norm_rope_cache_quant(cfg, H.hybrid_rope_cfg(0, 0, 1.0, 0.0), pg, None, 0, k, d, v, d, 300, None, None, None, None, slots,
+                                      None, kc, vc, ks, vs)
+    k2, v2 = read(cfg, pg, (kc, vc, ks, vs), slots, BF)
+    for x, y in ((k, k2), (v, v2)):
+        assert bool(((x.float() - y.float()).abs() <= (x.float().abs() * 2 ** -4).clamp(min=2.0 ** -10 * x.float().abs().max() / 224)).all())
+    for B in (1, 8, 16, 32):
+        cfg = H.make_cfg(d, 64, 4, 1, B, BF)
+        q = torch.randn(1, B, 4, d, generator=gen(B), device="cuda").to(BF)
+        o = attend(cfg, pg, q, (kc, vc, ks, vs), table, i32([300]))
+        H.hybrid_check()
+        x = torch.einsum("bhd,kd->bhk", q[0].double(), k2[:, 0].double()) / math.sqrt(d)
+        want = torch.einsum("bhk,kd->bhd", torch.softmax(x, -1), v2[:, 0].double())[None]
+        assert_parity(o.double().cpu().numpy(), want.cpu().numpy(), BF, f"far pages, {B} tokens", units="out")
+
+
+# ------------------------------------------------------------------ attention
+
+def attend(cfg, pg, q, cache, table, lens, window=0, sink=0, stream=None):
+    n = lens.numel()
+    o = torch.full_like(q, 3.0)
+    nb = H.hybrid_paged_attn_quant_workspace_bytes(cfg, pg, n)
+    ws = torch.full((nb,), 255, dtype=torch.uint8, device="cuda")
+    if stream is not None:
+        stream.wait_stream(torch.cuda.current_stream())
+    H.hybrid_paged_attn_quant(cfg, pg, q, *cache, table, lens, n, window, sink, o, ws, nb, stream=stream)
+    return o
+
+
+def attn_setup(dt, B, Hq, Hkv, d, P, lens, window=0, sink=0, seed=0, k_scale=1.0, poison=True, spread=2):
+    """Every place that no query sees holds a code of NaN, groups without a visible key a scale of NaN; pages without one
+    are not in the pool, and their table entries out of range."""
+    g, rng = gen(seed), random.Random(seed)
+    n, max_pages = len(lens), max(1, -(-max(lens) // P)) + 1
+    seen = [R.visible(x, window, sink) for x in lens]
+    pages = [sorted({j // P for j in v}) for v in seen]
+    n_pages = sum(map(len, pages)) + 2
+    ids = list(range(n_pages))
+    rng.shuffle(ids)
+    table = torch.full((n, max_pages), -77 if seed % 2 else 2 ** 30, dtype=torch.int32)
+    cache = []
+    see = torch.zeros(n_pages, P, dtype=torch.bool)
+    for r in range(n):
+        for j in pages[r]:
+            table[r, j] = ids.pop()
+        j = torch.tensor(seen[r], dtype=torch.long)
+        see[table[r][j // P].long(), j % P] = True
+    see = see.cuda()
+    for size in (k_scale, 1.0):
+        x = torch.randn(n_pages, Hkv, P, d, generator=g, device="cuda") * size
+        x = x * torch.exp2(torch.randint(-spread, spread + 1, (n_pages, Hkv, P // GROUP, 1), generator=g, device="cuda").float()
+                           ).repeat_interleave(GROUP, 2) / 2.0 ** (spread // 2)
+        x = x.view(n_pages, Hkv, P // GROUP, GROUP, d)
+        scale = torch.exp2(torch.ceil(torch.log2(x.abs().amax((-1, -2)) / 448)))
+        codes = (x / scale[..., None, None]).view(n_pages, Hkv, P, d).to(F8)
+        if poison:
+            codes.view(torch.uint8)[~see[:, None, :].expand(-1, Hkv, -1)] = Q.NAN
+            scale[~see.view(n_pages, 1, -1, GROUP).any(-1).expand(-1, Hkv, -1)] = math.nan
+        cache += [codes, scale]
+    return dict(cfg=H.make_cfg(d, 64, Hq, Hkv, B, dt), pg=H.make_page_cfg(P, n_pages, max_pages),
+                cache=[cache[0], cache[2], cache[1], cache[3]], q=torch.randn(n, B, Hq, d, generator=g, device="cuda").to(dt),
+                table=table.cuda(), lens=i32(lens), window=window, sink=sink, dt=dt)
+
+
+def run_attn(s, stream=None):
+    return attend(s["cfg"], s["pg"], s["q"], s["cache"], s["table"], s["lens"], s["window"], s["sink"], stream)
+
+
+def want_attn(s):
+    kc, vc, ks, vs = s["cache"]
+    return R.paged_attention(s["q"], Q.values(kc, ks), Q.values(vc, vs), s["table"], s["lens"].tolist(), s["window"], s["sink"])
+
+
+def check_attn(s, what=""):
+    o = run_attn(s)
+    H.hybrid_check()
+    got, want = o.double().cpu().numpy(), want_attn(s).cpu().numpy()
+    assert_parity(got, want, s["dt"], what, units="out")
+    for r, x in enumerate(s["lens"].tolist()):
+        if not R.visible(x, s["window"], s["sink"]):
+            assert not np.any(got[r]), "zeros without a visible key"
+    return o
+
+
+EDGES = [0, 1, 2, 15, 16, 17, 31, 33, 63, 64, 65, 127, 128, 129, 255, 256, 257, 300, 1000]
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("B,Hq,Hkv,d,P", [
+    (1, 16, 4, 128, 16), (1, 1, 1, 64, 128), (32, 16, 4, 128, 32), (16, 2, 2, 64, 64), (33, 6, 2, 128, 16), (128, 4, 4, 64, 32),
+    (1, 32, 1, 128, 64), (5, 35, 5, 64, 16), (3, 160, 1, 128, 16), (2, 256, 1, 64, 128), (64, 16, 4, 128, 128), (8, 32, 8, 64, 16),
+])
+def test_attention_edges_of_pages_and_tiles(dt, B, Hq, Hkv, d, P):
+    check_attn(attn_setup(dt, B, Hq, Hkv, d, P, EDGES, seed=B + Hq), f"B{B} Hq{Hq} Hkv{Hkv} d{d} P{P}")
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("B,G", [(1, 1), (1, 5), (7, 1), (2, 4), (1, 8), (9, 1), (1, 11), (16, 1), (17, 1), (5, 5), (8, 4), (33, 1), (10, 4),
+                                 (12, 5), (16, 4), (13, 5), (24, 4), (128, 1), (129 // 3, 3), (60, 3)])
+def test_attention_rows_of_a_tile(dt, B, G, d):
+    check_attn(attn_setup(dt, B, 2 * G, 2, d, 32, [1, 40, 0, 300, 129, 1500], seed=B), f"B{B} G{G}")
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("window,sink", [(1, 0), (1, 1), (16, 4), (100, 0), (128, 128), (129, 33), (1000, 130), (257, 500), (5, 100000),
+                                         (2147483647, 7)])
+def test_attention_window_and_first_tokens(dt, window, sink):
+    lens = [0, 1, 5, 16, 100, 129, 140, 256, 260, 385, 512, 777, 1500, 4000]
+    for B, Hq, Hkv, d, P in ((1, 8, 2, 128, 16), (32, 4, 1, 64, 64), (8, 12, 3, 128, 32)):
+        check_attn(attn_setup(dt, B, Hq, Hkv, d, P, lens, window, sink, seed=window % 97 + sink % 31), f"window {window} sink {sink}")
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
+def test_attention_long_and_split(dt):
+    """Requests split over many blocks beside short ones."""
+    check_attn(attn_setup(dt, 1, 8, 2, 128, 64, [40001, 3, 17000, 0, 128]), "long, one token")
+    check_attn(attn_setup(dt, 32, 4, 1, 128, 32, [20011, 1, 9000]), "long, block")
+    check_attn(attn_setup(dt, 16, 8, 2, 64, 16, [20011, 1, 9000]), "long, block of small heads")
+    check_attn(attn_setup(dt, 1, 1, 1, 64, 16, [9999]), "one head")
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
+def test_attention_many_requests(dt):
+    rng = random.Random(1)
+    lens = [rng.choice([0, 1, 16, rng.randint(0, 200)]) for _ in range(3000)]
+    check_attn(attn_setup(dt, 1, 4, 2, 64, 16, lens), "3000 requests")
+    check_attn(attn_setup(dt, 16, 4, 1, 64, 16, lens[:700]), "700 requests, 64 rows")
+    check_attn(attn_setup(dt, 1, 4, 2, 64, 16, [0] * 300 + [5] + [0] * 300), "mostly empty")
+    check_attn(attn_setup(dt, 4, 4, 2, 64, 16, [0] * 40), "all empty")
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
+def test_attention_row_tiles_of_many_requests(dt):
+    rng = random.Random(2)
+    for n in (3, 128, 129, 400):
+        lens = [rng.choice([0, 1, 127, 128, rng.randint(0, 400)]) for _ in range(n)]
+        check_attn(attn_setup(dt, 40, 14, 2, 64, 32, lens, seed=n), f"{n} requests, 280 rows")
+    check_attn(attn_setup(dt, 128, 8, 1, 128, 16, [3000, 0, 50], 700, 30), "1024 rows, window")
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("max_len", [16, 128, 144])
+def test_attention_of_contexts_that_fit_a_tile(dt, max_len):
+    lens = [0, 1, max_len, max_len - 1, 7, max_len // 2]
+    for Hkv, Hq, B in ((1, 4, 1), (3, 6, 20)):
+        s = attn_setup(dt, B, Hq, Hkv, 64, 16, lens, seed=max_len)
+        s["table"] = s["table"][:, :max_len // 16].contiguous()
+        s["pg"] = H.make_page_cfg(16, s["pg"].n_pages, max_len // 16)
+        check_attn(s, f"{B} tokens")
+
+
+SHAPES = [(1, 8, 2, 128, 16), (1, 8, 2, 64, 32), (4, 8, 2, 128, 32), (8, 8, 2, 64, 16), (32, 4, 1, 128, 32), (16, 8, 2, 128, 64), (32, 8, 2, 64, 64)]
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+def test_attention_large_and_rising_scores(dt, shape):
+    B, Hq, Hkv, d, P = shape
+    check_attn(attn_setup(dt, B, Hq, Hkv, d, P, [700, 33, 4000], k_scale=8.0), "k x 8")
+    s = attn_setup(dt, B, Hq, Hkv, d, P, [3000, 17], poison=False, spread=0)
+    # scores that rise along the cache, so that every tile raises the maximum
+    for r, n in ((0, 3000), (1, 17)):
+        j = torch.arange(n, device="cuda")
+        page, sub = s["table"][r][j // P].long(), j % P // GROUP
+        s["cache"][2][page, :, sub] = torch.exp2(-8 + 5 * (j // GROUP) / (n // GROUP))[:, None]
+    s["q"] = s["q"].abs()
+    s["cache"][0].view(torch.uint8).bitwise_and_(0x7f)
+    check_attn(s, "rising scores")
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+def test_attention_scales_far_apart(dt, shape):
+    """Scales of values over 2^-60 ... 2^60, rising or falling along the cache; keys whose scores are small beside
+    values whose scale is large; a first token that takes nearly all of the softmax and has values near zero."""
+    B, Hq, Hkv, d, P = shape
+    for turn in (1, -1):
+        s = attn_setup(dt, B, Hq, Hkv, d, P, [1000, 130, 3], poison=False)
+        for r, n in ((0, 1000), (1, 130), (2, 3)):
+            j = torch.arange(n, device="cuda")
+            page, sub = s["table"][r][j // P].long(), j % P // GROUP
+            s["cache"][3][page, :, sub] = torch.exp2((turn * (120 * (j // GROUP) // (n // GROUP + 1) - 60)).float())[:, None]
+        o, want = run_attn(s), want_attn(s)
+        H.hybrid_check()
+        # beside values of up to 2^60 the absolute bound of float32 outputs has no meaning: rows to unit size
+        size = want.abs().amax(-1, keepdim=True)
+        assert_parity((o.double() / size).cpu().numpy(), (want / size).cpu().numpy(), dt, "scales of values", units="out")
+    s = attn_setup(dt, B, Hq, Hkv, d, P, [2000, 40], poison=False, spread=0)
+    page = s["table"][:, 0].long()
+    s["cache"][2].mul_(2.0 ** -3)
+    s["cache"][2][page, :, 0] = 2.0 ** -3
+    s["cache"][0].view(torch.uint8)[page, :, :GROUP] = 0
+    s["cache"][0].view(torch.uint8)[page, :, 0] = 0x78         # the first key: large
+    s["cache"][3][page, :, 0] = 2.0 ** -40
+    s["q"] = s["q"].abs() * 0.25
+    check_attn(s, "a first token of large score and no value")
+
+
+def test_attention_any_scale():
+    """Scales that are no powers of two, and the smallest and largest ones."""
+    for dt in (BF, F32):
+        for B, Hq, Hkv, d, P in SHAPES:
+            s = attn_setup(dt, B, Hq, Hkv, d, P, [777, 40])
+            for x in s["cache"][2:]:
+                x.mul_(torch.rand(x.shape, generator=gen(3), device="cuda") + 0.5)
+            check_attn(s, "any scale")
+            s = attn_setup(dt, B, Hq, Hkv, d, P, [300, 16], poison=False)
+            s["cache"][2].fill_(2.0 ** -126)                    # every key alike
+            check_attn(s, "smallest scale of keys")
+            s["cache"][3].fill_(2.0 ** -126)
+            for x in s["cache"][:2]:
+                x.view(torch.uint8).fill_(0)
+            assert not bool(run_attn(s).any())
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+def test_attention_queries_of_every_size(dt, shape):
+    """Query rows of zeros, of one large entry beside small ones that decide, very small and very large ones."""
+    B, Hq, Hkv, d, P = shape
+    s = attn_setup(dt, B, Hq, Hkv, d, P, [500, 129], poison=False, spread=0)
+    s["q"][0, 0, 0] = 0.0
+    s["q"][0, 0, 1] *= 2.0 ** -100
+    s["q"][1, 0, 0, 5] = 30000.0
+    s["cache"][0].view(torch.uint8)[..., 5] = 0                 # the feature that it meets
+    check_attn(s, "sizes of queries")
+    s["q"].mul_(2.0 ** 90)
+    s["cache"][2].mul_(2.0 ** -90)
+    check_attn(s, "large queries and small keys")
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+def test_attention_nan_stays_where_it_is(dt, shape):
+    """NaN in one feature of a visible value: that feature of its head's outputs, nothing else.  In a key, or in a query's
+    infinities: those rows."""
+    B, Hq, Hkv, d, P = shape
+    s = attn_setup(dt, B, Hq, Hkv, d, P, [500, 129, 40], poison=False)
+    want = want_attn(s)
+    page, at = int(s["table"][1, 100 // P]), 100 % P
+    s["cache"][1].view(torch.uint8)[page, 0, at, 7] = Q.NAN
+    s["cache"][0].view(torch.uint8)[int(s["table"][2, 0]), 0, 5, 3] = Q.NAN | 0x80
+    s["q"][0, B - 1, Hq - 1, 9] = math.inf
+    o = run_attn(s)
+    H.hybrid_check()
+    G, bad = Hq // Hkv, torch.zeros(o.shape, dtype=torch.bool, device="cuda")
+    bad[1, :, :G, 7] = True
+    bad[2, :, :G] = True
+    bad[0, B - 1, Hq - 1] = True
+    # (a row whose infinity meets keys of one sign alone may be finite; with 500 keys of both it is not)
+    assert torch.equal(o.isnan(), bad)
+    keep = ~bad
+    assert_parity((o * keep).nan_to_num().double().cpu().numpy(), (want * keep).cpu().numpy(), dt, "beside NaN")
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
+def test_attention_same_bits_and_another_stream(dt):
+    for B, Hq, d in ((1, 8, 128), (8, 8, 128), (32, 8, 64)):
+        s = attn_setup(dt, B, Hq, 2, d, 16, [5000, 77, 1234])
+        a, stream = run_attn(s), torch.cuda.Stream()
+        b = run_attn(s, stream)
+        H.hybrid_check(stream=stream)
+        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("B,d", [(2, 64), (2, 128), (32, 128)])
+def test_attention_reports_bad_pages_and_lengths(dt, B, d):
+    for what, value in (("table", -1), ("table", 10 ** 6), ("lens", -5), ("lens", 2 ** 31 - 1)):
+        s = attn_setup(dt, B, 4, 2, d, 16, [300, 200, 100], poison=False)
+        want = want_attn(s)
+        if what == "table":
+            s["table"][0, 3] = value
+        else:
+            s["table"].clamp_(0, s["pg"].n_pages - 1)
+            s["lens"][0] = value
+        o = run_attn(s)
+        assert H.hybrid_check(check=False) == H.HYBRID_ERR_DEVICE and H.hybrid_check(check=False) == H.HYBRID_OK
+        assert_parity(o[1:].double().cpu().numpy(), want[1:].cpu().numpy(), dt, f"beside a bad {what}", units="out")
+
+
+# ------------------------------------------------------------------ together
+
+def cache_of(pool, layer):
+    return [Q.values(c[layer], s[layer]) for c, s in ((pool.k_cache, pool.k_scale), (pool.v_cache, pool.v_scale))]
+
+
+def check_layer(layer, pool, i, q, o, dt, what):
+    n, c = pool.n_req, layer.cfg
+    want = R.paged_attention(q.view(n, -1, c.n_q_heads, c.head_dim), *cache_of(pool, i), pool.block_table, pool.lens.tolist(),
+                             layer.window, layer.n_sink)
+    assert_parity(o.view(want.shape).double().cpu().numpy(), want.cpu().numpy(), dt, what, units="out")
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("B", [1, 8, 32])
+def test_decoding_with_a_pool(dt, B):
+    """Prompts, then blocks of which each is written several times, requests that leave and others that take their pages."""
+    Hq, Hkv, d, P, n = 8, 2, 128, 32, 3
+    pool = PagePool(H.make_cfg(d, 64, Hq, Hkv, B, dt), n, 60, 400, P, n_layers=2, quant=True)
+    pool.k_cache.view(torch.uint8).fill_(Q.NAN)
+    pool.v_cache.view(torch.uint8).fill_(Q.NAN)
+    pool.k_scale.fill_(math.nan)
+    pool.v_scale.fill_(math.nan)
+    layer = SoftmaxLayer(pool.cfg, H.make_rope(d))
+    width = (Hq + 2 * Hkv) * d
+    for turn, new in enumerate(([40, 129, 1], [B] * n, [B] * n, [0, 0, 77], [B] * n)):
+        if turn == 3:
+            pool.release(i32([2]))
+        slots, pos, _ = pool.append(i32(new), sum(new) + 3)
+        for again in range(2 if new == [B] * n else 1):
+            x = torch.randn(sum(new) + 3, width, generator=gen(10 * turn + again), device="cuda").to(dt)
+            q = layer.write(x, pool, turn % 2, slots, pos)
+            H.hybrid_check()
+        if new == [B] * n:
+            for i in range(2):
+                if i != turn % 2:                               # the other layer has the same tokens
+                    layer.write(x, pool, i, slots, pos)
+        else:
+            layer.write(x, pool, 1 - turn % 2, slots, pos)
+        if new == [B] * n:
+            for i in range(2):
+                o = layer.attend(q[:n * B], pool, i)
+                H.hybrid_check()
+                check_layer(layer, pool, i, q[:n * B], o, dt, f"turn {turn} layer {i}")
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
+def test_contexts_leave_and_come_back(dt):
+    """A request's tokens read back, its pages released, and stored in other ones: the same values, on another stream too."""
+    pool = PagePool(H.make_cfg(64, 64, 4, 2, 1, dt), 2, 40, 320, 16, quant=True)
+    slots, pos, _ = pool.append(i32([150, 77]), 227)
+    layer = SoftmaxLayer(pool.cfg, H.make_rope(64))
+    layer.write(torch.randn(227, 8 * 64, generator=gen(1), device="cuda").to(dt), pool, 0, slots, pos)
+    k, v = pool.load(0, pool.slots_of(0, 0, 150))
+    want = cache_of(pool, 0)
+    sl = slots[:150].long()
+    assert torch.equal(k.double(), want[0][sl // 16, :, sl % 16]) and torch.equal(v.double(), want[1][sl // 16, :, sl % 16])
+    pool.release(i32([0]))
+    pool.append(i32([0, 30]), 30)
+    pool.append(i32([150, 0]), 150)
+    stream = torch.cuda.Stream()
+    back = pool.slots_of(0, 0, 150)
+    stream.wait_stream(torch.cuda.current_stream())
+    pool.store(0, k, v, back, stream=stream)
+    k2, v2 = pool.load(0, back, stream=stream)
+    torch.cuda.current_stream().wait_stream(stream)
+    H.hybrid_check()
+    assert torch.equal(k2, k) and torch.equal(v2, v)
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("B", [1, 16])
+def test_decoding_in_two_graphs(dt, B):
+    """Writes and attention captured for two layers in a graph each, replayed at the same time on two streams."""
+    n, Hq, Hkv, d = 5, 8, 2, 128
+    pool = PagePool(H.make_cfg(d, 64, Hq, Hkv, B, dt), n, 120, 600, 16, n_layers=2, quant=True)
+    layer = SoftmaxLayer(pool.cfg, H.make_rope(d))
+    width = (Hq + 2 * Hkv) * d
+    new = [300, 1, 129, 40, 16]
+    for i, (slots, pos, _) in enumerate([pool.append(i32(new), sum(new))] * 2):
+        layer.write(torch.randn(sum(new), width, generator=gen(i), device="cuda").to(dt), pool, i, slots, pos)
+    slots, pos, _ = pool.append(i32([B] * n), B * n)
+    x = [torch.randn(B * n, width, generator=gen(5 + i), device="cuda").to(dt) for i in range(2)]
+    layer.step(x[0], pool, 0, slots, pos)
+    graphs, outs = [], []
+    for i in range(2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            q = layer.write(x[i], pool, i, slots, pos)
+            outs.append((q, layer.attend(q, pool, i)))
+        graphs.append(g)
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for turn in range(3):
+        for i in range(2):
+            x[i].copy_(torch.randn(x[i].shape, generator=gen(20 + 2 * turn + i), device="cuda"))
+        torch.cuda.synchronize()
+        for i in range(2):
+            with torch.cuda.stream(streams[i]):
+                graphs[i].replay()
+        torch.cuda.synchronize()
+        H.hybrid_check()
+        for i in range(2):
+            check_layer(layer, pool, i, *outs[i], dt, f"turn {turn} layer {i}")
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
+def test_batches_with_idle_rows(dt):
+    B, n, Hq, Hkv, d = 4, 4, 4, 2, 64
+    pool = PagePool(H.make_cfg(d, 64, Hq, Hkv, B, dt), n, 60, 200, 16, quant=True)
+    layer = SoftmaxLayer(pool.cfg, H.make_rope(d), window=50, n_sink=3)
+    for new in ([60, 0, 100, 7], [4, 0, 2, 1]):
+        T = sum(new) + 2
+        slots, pos, offs = pool.append(i32(new), T)
+        q = layer.write(torch.randn(T, (Hq + 2 * Hkv) * d, generator=gen(T), device="cuda").to(dt), pool, 0, slots, pos)
+    o = layer.attend(q, pool, 0, rows=pool.block_rows(offs, T))
+    H.hybrid_check()
+    qs = torch.zeros(n, B, Hq, d, dtype=dt, device="cuda")
+    at = 0
+    for r, x in enumerate(new):
+        qs[r, :x] = q[at:at + x]
+        at += x
+    want = R.paged_attention(qs, *cache_of(pool, 0), pool.block_table, pool.lens.tolist(), 50, 3)
+    want = torch.cat([want[r, :x] for r, x in enumerate(new)])
+    assert_parity(o[:sum(new)].double().cpu().numpy(), want.cpu().numpy(), dt, "idle rows")
+    assert not bool(o[sum(new):].any())

@@ -1,0 +1,220 @@
+"""The 8-bit cache's entry points and its pool on the host, without a GPU: what does not fit is refused before
+the device is touched."""
+import ctypes
+
+import pytest
+import torch
+
+import test_softmax_abi as A
+from paper_2608_06628_gb300 import build as B
+from paper_2608_06628_gb300 import hybrid as H
+from paper_2608_06628_gb300.page_pool import PagePool
+from paper_2608_06628_gb300.softmax_layer import SoftmaxLayer
+from quant_reference import F8, least_scale
+
+OK, BAD, UNSUP = H.HYBRID_OK, H.HYBRID_ERR_INVALID_ARG, H.HYBRID_ERR_UNSUPPORTED
+WRITE, READ, ATTN = "hybrid_qk_norm_rope_cache_quant", "hybrid_cache_dequant", "hybrid_paged_attn_quant"
+MB = 1 << 20
+# As test_softmax_abi.ARGS; pointers are a megabyte apart, so that outputs of these sizes do not meet.
+ARGS = {
+    WRITE: ((A.cfg, A.rope, A.pg), ["p16", "i:2048", "p16", "i:512", "p16", "i:512", "i:3", "o16", "o16", "p4", "p8", "p4", "p16",
+                                    "p16", "p16", "p4", "p4", "s"]),
+    READ: ((A.cfg, A.pg), ["p16", "p16", "p4", "p4", "p4", "i:3", "p16", "p16", "s"]),
+    ATTN: ((A.cfg, A.pg), ["p16", "p16", "p16", "p4", "p4", "p4", "p4", "i:2", "i:0", "i:0", "p16", "p16", "i:1000000000", "s"]),
+}
+
+
+@pytest.fixture(scope="module")
+def L():
+    B.build()
+    return H.lib()
+
+
+def at(i):
+    return (i + 1) * 16 * MB
+
+
+def call(L, name, make=None, override=None):
+    cfgs, roles = ARGS[name]
+    made = [(make or {}).get(f, f)() for f in cfgs]
+    args = []
+    for i, r in enumerate(roles):
+        if override and i in override:
+            args.append(override[i])
+        else:
+            args.append(None if r == "s" else int(r[2:]) if r.startswith("i:") else at(i))
+    return getattr(L, name)(*[ctypes.byref(m) if m is not None else None for m in made], *args)
+
+
+@pytest.mark.parametrize("name", sorted(ARGS))
+def test_every_pointer_is_checked(L, name):
+    cfgs, roles = ARGS[name]
+    assert len(cfgs) + len(roles) == len(getattr(L, name).argtypes)
+    for i, r in enumerate(roles):
+        if r[0] not in "po":
+            continue
+        assert call(L, name, override={i: at(i) + int(r[1:]) // 2}) == BAD, (name, i, "misaligned")
+        if r[0] == "p":
+            assert call(L, name, override={i: None}) == BAD, (name, i, "null")
+    for f in cfgs:
+        assert call(L, name, {f: lambda: None}) == BAD
+
+
+@pytest.mark.parametrize("name", sorted(ARGS))
+@pytest.mark.parametrize("f,bad,code", [
+    (A.cfg, dict(d=96), UNSUP), (A.cfg, dict(dt=7), UNSUP), (A.cfg, dict(Hq=257, Hkv=257), UNSUP), (A.cfg, dict(Hq=6, Hkv=4), BAD),
+    (A.cfg, dict(Hkv=0), UNSUP), (A.pg, dict(P=24), UNSUP), (A.pg, dict(P=8), UNSUP), (A.pg, dict(n=0), BAD), (A.pg, dict(n=2 ** 26), UNSUP),
+    (A.rope, dict(rot=24), UNSUP), (A.rope, dict(inter=2), BAD), (A.rope, dict(eps=-1.0), BAD)])
+def test_configurations_outside_the_set(L, name, f, bad, code):
+    if f in ARGS[name][0]:
+        assert call(L, name, {f: lambda: f(**bad)}) == code
+
+
+def test_numbers_and_strides(L):
+    for name, over, code in [
+        (WRITE, {6: -1}, BAD), (WRITE, {1: 2040}, BAD), (WRITE, {1: 2052}, BAD), (WRITE, {3: 504}, BAD), (WRITE, {5: 504}, BAD),
+        (WRITE, {5: 515}, BAD), (WRITE, {0: None}, BAD), (WRITE, {12: None}, BAD), (WRITE, {0: None, 12: None, 2: None}, BAD),
+        (WRITE, {12: at(0), 1: 4096}, BAD),             # in place on a strided input
+        (READ, {5: -1}, BAD),
+        (ATTN, {7: -1}, BAD), (ATTN, {7: 65537}, UNSUP), (ATTN, {8: -1}, BAD), (ATTN, {9: -1}, BAD), (ATTN, {12: 100}, BAD),
+    ]:
+        assert call(L, name, override=over) == code, (name, over)
+    for Bs in (0, 129):
+        assert call(L, ATTN, {A.cfg: lambda Bs=Bs: A.cfg(Bs=Bs)}) == UNSUP
+
+
+@pytest.mark.parametrize("name,outs,ins", [(WRITE, [12, 13, 14, 15, 16], [2, 4]), (READ, [6, 7], [0, 1, 2, 3, 4])])
+def test_outputs_that_share_memory(L, name, outs, ins):
+    for o in outs:
+        for x in outs + ins:
+            if x != o:
+                assert call(L, name, override={o: at(x)}) == BAD, (name, o, x)
+    if name == WRITE:
+        for o in outs[1:]:
+            assert call(L, name, override={o: at(0)}) == BAD, (name, o, "Q")
+
+
+def test_nothing_to_do(L):
+    for name, count in ((WRITE, 6), (READ, 5), (ATTN, 7)):
+        over = {i: None for i, r in enumerate(ARGS[name][1]) if r[0] in "po"}
+        over[count] = 0
+        assert call(L, name, override=over) == OK
+        assert call(L, name, {A.cfg: lambda: A.cfg(d=96)}, over) == UNSUP
+
+
+def test_workspace_sizes():
+    c = A.cfg()
+    assert H.hybrid_paged_attn_quant_workspace_bytes(c, A.pg(), 3) > 0
+    for bad in (dict(d=96), dict(Bs=0), dict(Bs=129), dict(dt=5)):
+        assert H.hybrid_paged_attn_quant_workspace_bytes(A.cfg(**bad), A.pg(), 3) == 0
+    assert H.hybrid_paged_attn_quant_workspace_bytes(c, A.pg(P=24), 3) == 0
+    assert H.hybrid_paged_attn_quant_workspace_bytes(c, A.pg(), -1) == 0
+
+
+def test_least_scale():
+    """The reference's own scale, at its borders."""
+    for e in (-126, -7, 0, 100):
+        s = 2.0 ** e
+        assert least_scale(448 * s) == s and least_scale(448 * s * (1 + 2.0 ** -40)) == 2 * s
+    assert least_scale(0.0) == least_scale(1e-45) == 2.0 ** -126 and least_scale(224.0) == 0.5
+
+
+# ------------------------------------------------------------------ the pool and the layer
+
+HQ, HKV, D, N, P = 4, 2, 64, 3, 32
+BF, F32, I32 = torch.bfloat16, torch.float32, torch.int32
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    seen = []
+    for name in ("hybrid_page_append", "hybrid_qk_norm_rope_cache", "hybrid_paged_attn", WRITE, READ, ATTN):
+        monkeypatch.setattr(H, name, lambda *a, _name=name, **kw: seen.append((_name, a)))
+    monkeypatch.setattr(H, "_stream", lambda stream: 0 if stream is None else stream)
+    return seen
+
+
+def pool(dt=F32, quant=True):
+    return PagePool(H.make_cfg(D, 64, HQ, HKV, 2, dt), N, 20, 64, P, n_layers=2, device="cpu", quant=quant)
+
+
+def ints(n, dtype=I32):
+    return torch.zeros(n, dtype=dtype)
+
+
+def test_shapes_of_an_8_bit_pool(calls):
+    p = pool()
+    assert p.k_cache.dtype == p.v_cache.dtype == F8 and p.k_cache.shape == (2, 20, HKV, P, D)
+    assert p.k_scale.dtype == F32 and p.k_scale.shape == p.v_scale.shape == (2, 20, HKV, P // 16)
+    assert [c.data_ptr() for c in p.caches(1)] == [x[1].data_ptr() for x in (p.k_cache, p.v_cache, p.k_scale, p.v_scale)]
+    assert pool(quant=False).k_scale is None and len(pool(quant=False).caches(0)) == 2
+
+
+def test_the_layer_takes_the_pools_entry_points(calls):
+    layer = SoftmaxLayer(pool().cfg, H.make_rope(D, device="cpu"))
+    for quant, names in ((True, [WRITE, ATTN]), (False, ["hybrid_qk_norm_rope_cache", "hybrid_paged_attn"])):
+        p = pool(quant=quant)
+        calls.clear()
+        q = layer.write(torch.zeros(N * 2, (HQ + 2 * HKV) * D), p, 1, ints(N * 2), ints(N * 2))
+        layer.attend(q, p, 1)
+        assert [name for name, _ in calls] == names
+
+
+def test_load_and_store(calls):
+    p = pool(BF)
+    k, v = p.load(1, ints(5))
+    assert k.dtype == v.dtype == BF and k.shape == v.shape == (5, HKV, D) and calls[-1][0] == READ
+    p.store(1, k, v, ints(5))
+    assert calls[-1][0] == WRITE and calls[-1][1][3] is None and calls[-1][1][4] == 0
+    p.store(0, k[:1], v[:1].expand(1, HKV, D), ints(1))             # one token, whose stride torch may report as any
+    assert calls[-1][1][6] == calls[-1][1][8] == HKV * D
+    p.load(0, ints(0))
+    p.store(0, k[:0], v[:0], ints(0))
+
+
+@pytest.mark.parametrize("slots", [ints(5, torch.int64), ints(10)[::2], ints(6).view(2, 3), torch.zeros(5), [0] * 5, None])
+def test_load_and_store_refuse_slots(calls, slots):
+    x = torch.zeros(5, HKV, D)
+    with pytest.raises(ValueError, match="slots"):
+        pool().load(0, slots)
+    with pytest.raises(ValueError, match="slots"):
+        pool().store(0, x, x, slots)
+    assert not calls
+
+
+@pytest.mark.parametrize("x", [torch.zeros(5, HKV, D, dtype=BF), torch.zeros(4, HKV, D), torch.zeros(5, HKV + 1, D), torch.zeros(5, HKV * D),
+                               torch.zeros(5, HKV, 2 * D)[..., ::2], torch.zeros(5, D, HKV).transpose(1, 2)])
+def test_store_refuses_tensors(calls, x):
+    good = torch.zeros(5, HKV, D)
+    for k, v, what in ((x, good, "k"), (good, x, "v")):
+        with pytest.raises(ValueError, match=what):
+            pool().store(0, k, v, ints(5))
+    assert not calls
+
+
+@pytest.mark.parametrize("layer", [-1, 2, 1.0, None])
+def test_layers_that_are_not_there(calls, layer):
+    with pytest.raises((IndexError, TypeError)):
+        pool().load(layer, ints(5))
+    x = torch.zeros(5, HKV, D)
+    with pytest.raises((IndexError, TypeError)):
+        pool().store(layer, x, x, ints(5))
+    assert not calls
+
+
+def test_other_pools_are_indexed_as_tensors(calls):
+    x = torch.zeros(5, HKV, D)
+    for f in (lambda p: p.load(0, ints(5)), lambda p: p.store(0, x, x, ints(5))):
+        with pytest.raises(ValueError, match="8-bit"):
+            f(pool(quant=False))
+    assert not calls
+
+
+def test_slots_of():
+    p = pool()
+    p.block_table[1, :2] = torch.tensor([7, 3], dtype=I32)
+    assert p.slots_of(1, 30, 35).tolist() == [7 * P + 30, 7 * P + 31, 3 * P, 3 * P + 1, 3 * P + 2]
+    assert p.slots_of(1, 5, 5).numel() == 0 and p.slots_of(1, 0, 1).dtype == I32
+    for row, start, stop in ((3, 0, 1), (-1, 0, 1), (0, -1, 1), (0, 2, 1), (0, 0, 65)):
+        with pytest.raises((ValueError, IndexError)):
+            p.slots_of(row, start, stop)
