@@ -1,0 +1,463 @@
+// paged_attn_quant.cu -- attention over the 8-bit paged cache with few query rows
+// (hybrid_paged_attn_quant): decoding, of one or several new tokens.
+//
+// With so few rows the codes' bytes bound it, so what counts is that nothing else does: no
+// block-wide step, and few instructions to a code.  A warp has a run of 16 keys of each tile,
+// which is one group, and forms, transposed so that the rows are the narrow side,
+//     S^T = K Q^T           x = S ks log2(e) / sqrt(d)
+//     p = 2^(x - m),   l += p
+//     O^T += V^T P^T        P = p vs, relative to a reference of its own
+// by mma.m16n8k16 from registers: codes become half precision, exactly, on their way from shared
+// memory into the operands, and the scales ks, vs of the group stay with S and P.  The features
+// (of S) and the keys (of O) that an operand's place stands for are chosen so that a lane finds
+// its own in 16 bytes of a key.
+//
+// Half precision and its range.  A query row is brought to 2^14 ... 2^15 at its largest entry by
+// a power of two: entries below 2^-29 of it lose bits, in units of 2^-39 of it.  P is held
+// relative to a running reference of x + log2(vs), apart from the reference m of p and l (a token
+// that takes most of the softmax may have values near zero): 11 bits, and below 2^-21 of the
+// largest p vs of its row units of 2^-31 of that.  float32: two such numbers for each entry of Q
+// and P, 22 bits.
+//
+// The codes come by cp.async into a ring of the warp, 16 bytes at a time, permuted so that
+// neither operand's reads meet in a bank.
+#include "paged_plan.cuh"
+#include "quant.cuh"
+#include "tc_pipeline.cuh"
+
+namespace hyb {
+namespace {
+
+using namespace paged;
+using ptx::f32x2;
+using ptx::pair2;
+
+constexpr int kThreads = 256;
+constexpr int kWarps = kThreads / 32;
+constexpr int kRun = kTile / kWarps;            // keys of a warp in a tile, side by side: of one group
+constexpr float kSlack = 8.f;                   // log2 of how far a reference may be exceeded
+constexpr float kTop = 7.f;                     // log2 of P at its reference
+constexpr float kMax = 3.402823466e38f;
+
+static_assert(kRun == quant::kGroup, "two scales a run");
+
+__device__ __forceinline__ uint32_t decode_lo(uint32_t v)
+{
+    const __half2 h = quant::decode2(v);
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
+__device__ __forceinline__ uint32_t decode_hi(uint32_t v) { return decode_lo(v >> 16); }
+__device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi)
+{
+    const __half2 h = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
+// What half precision leaves of a pair.
+__device__ __forceinline__ uint32_t rest_f16x2(uint32_t h, float lo, float hi)
+{
+    const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&h));
+    return pack_f16x2(lo - f.x, hi - f.y);
+}
+// D += A B, A 16 x 16, B 16 x 8 of half precision
+__device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose8(uint32_t v)      // of an 8 x 8 matrix of half precision over the warp
+{
+    uint32_t r;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+    return r;
+}
+__device__ __forceinline__ float lg2(float x)
+{
+    float y;
+    asm("lg2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ void copy_codes(uint32_t dst, const uint8_t *src, int bytes)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void copy_scale(uint32_t dst, const float *src)
+{
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+}
+
+// Places in a run's codes of one kind: [key][16 bytes], permuted.  Row r of S^T is key key_of(r).
+template <int D> struct Place;
+template <> struct Place<128> {
+    __device__ static int key_of(int r) { return r ^ ((r & 1) << 2); }
+    __device__ static uint32_t chunk(int key, int c) { return key * 128 + ((c ^ (key & 7)) << 4); }
+};
+template <> struct Place<64> {
+    __device__ static int key_of(int r) { return (r & 8) | (r & 2) << 1 | (r & 4) >> 1 | ((r ^ r >> 1) & 1); }
+    __device__ static uint32_t chunk(int key, int c) { return key * 64 + ((c ^ (key & 2)) << 4); }
+};
+
+// NT: row tiles of 8 rows
+template <int D, int NT> struct Smem {
+    static constexpr int kStages = NT * D <= 128 ? 3 : 4;
+    static constexpr int kScales = kStages + 1;
+    static constexpr int kPasses = 4, kPass = D / kPasses;  // features of the output at a time
+    uint8_t ring[kWarps][kStages][2][kRun * D];             // K, then V
+    float o[kWarps][8 * NT][kPass + 4];
+    float scales[kWarps][kScales][2];
+    float m[kWarps][8 * NT], l[kWarps][8 * NT];
+    PlanSmem plan;
+};
+
+template <typename T, int D, int NT>
+__global__ __launch_bounds__(kThreads, NT == 1 ? 2 : 1) void k_paged_attn_quant(const PagedArgs a, int page_lg)
+{
+    using S = Smem<D, NT>;
+    constexpr int kStages = S::kStages, kScales = S::kScales;
+    constexpr int kParts = sizeof(T) == 2 ? 1 : 2;          // halves that hold a number
+    constexpr int KS = D / 16, MT = D / 16;                 // steps of S over the features, tiles of O
+    constexpr int kCopies = kRun * D / 16 / 32;             // of a lane, of K and of V
+    extern __shared__ __align__(16) unsigned char raw[];
+    S &s = *reinterpret_cast<S *>(raw);
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int g = lane >> 2, c = lane & 3;
+    const int rows = a.Bt * a.Gt;
+    const float to_log2 = pipe::kLog2e * rsqrtf((float)D);
+    const uint8_t *K = static_cast<const uint8_t *>(a.K), *V = static_cast<const uint8_t *>(a.V);
+    const uint32_t ring = ptx::smem_u32(&s.ring[warp]);
+    const int key0 = Place<D>::key_of(g);                   // of rows g and g + 8 of S^T: key0, key0 + 8
+
+    ptx::griddep_wait();
+    ptx::griddep_launch_dependents();
+    Walk w;
+    Shares sh(0, 1);
+    const bool work = find_share<kThreads>(a, s.plan, w, sh);
+    bool go = work && w.next(a);
+    // the copies, of the segment w: tile, stage
+    int i = 0, slot = 0, to_scale = 0;
+    int ahead = 0;                                          // page of the next run
+    auto look_up = [&](int tile) {
+        ahead = 0;
+        if (tile >= w.i1) return;
+        const int j = key_tile(w.vis, tile) * kTile + warp * kRun;
+        if (any_visible(w.vis, j, kRun)) ahead = __ldg(a.table + (size_t)w.req * a.max_pages + (j >> page_lg));
+    };
+    auto fetch = [&]() {
+        if (i < w.i1) {
+            const int j = key_tile(w.vis, i) * kTile + warp * kRun;
+            int page = ahead;
+            look_up(++i);
+            if (any_visible(w.vis, j, kRun)) {
+                if (page < 0 || page >= a.n_pages) {
+                    raise_error(a.err, ERR_BAD_INDEX);
+                    page = 0;
+                }
+                const size_t run = (((size_t)page * a.Hkv + w.head) << page_lg) + (j & ((1 << page_lg) - 1));
+                if (lane < 2) copy_scale(ptx::smem_u32(&s.scales[warp][to_scale][lane]), (lane ? a.V_scale : a.K_scale) + run / kRun);
+#pragma unroll
+                for (int x = 0; x < kCopies; ++x) {
+                    const int at = lane + 32 * x, key = at / (D / 16);
+                    const int bytes = key_visible(w.vis, j + key) ? 16 : 0;     // masked keys and values are zeros
+                    const uint32_t dst = ring + slot * (2 * kRun * D) + Place<D>::chunk(key, at % (D / 16));
+                    copy_codes(dst, K + run * D + 16 * at, bytes);
+                    copy_codes(dst + kRun * D, V + run * D + 16 * at, bytes);
+                }
+            }
+            to_scale = to_scale + 1 == kScales ? 0 : to_scale + 1;
+        }
+        slot = slot + 1 == kStages ? 0 : slot + 1;
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    auto first_page = [&]() {
+        i = w.i0;
+        slot = to_scale = 0;
+        look_up(i);
+    };
+    auto first_steps = [&]() {
+#pragma unroll
+        for (int x = 0; x < kStages - 1; ++x) fetch();
+    };
+    if (go) {
+        first_page();
+        first_steps();
+    }
+    while (go) {
+        const Unit u = unit_of(a, w.head, w.rt);
+        // Q: step t of the features has, in this lane, 4 t % 16 ... of its 16-byte piece c + 4 (t / 4)
+        uint32_t q[NT][KS][kParts][2];
+        float kc[NT][2];                                    // of rows 2 c, 2 c + 1: log2(e) / sqrt(d) over the row's factor
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            size_t from;
+            const bool live = row_at(a, w.req, u, 8 * nt + g, from);
+            float v[KS][4];
+            uint32_t top = 0;
+#pragma unroll
+            for (int t = 0; t < KS; ++t) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[t][e] = 0.f;
+                if (live) {
+                    const T *src = static_cast<const T *>(a.Q) + from + 16 * (c + 4 * (t / 4)) + 4 * (t % 4);
+                    if constexpr (sizeof(T) == 2) {
+                        const uint2 p = __ldg(reinterpret_cast<const uint2 *>(src));
+                        v[t][0] = __uint_as_float(p.x << 16);
+                        v[t][1] = __uint_as_float(p.x & 0xffff0000u);
+                        v[t][2] = __uint_as_float(p.y << 16);
+                        v[t][3] = __uint_as_float(p.y & 0xffff0000u);
+                    } else {
+                        const float4 p = __ldg(reinterpret_cast<const float4 *>(src));
+                        v[t][0] = p.x, v[t][1] = p.y, v[t][2] = p.z, v[t][3] = p.w;
+                    }
+                }
+            }
+#pragma unroll
+            for (int t = 0; t < KS; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const uint32_t b = __float_as_uint(v[t][e]) & 0x7fffffffu;
+                    if (b < 0x7f800000u) top = max(top, b);
+                }
+            top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+            top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+            int e2 = (int)(top >> 23) - 127 - 14;           // the row over 2^e2 is below 2^15
+            if (e2 < -126) e2 = -126;
+            const float over = __uint_as_float((uint32_t)(127 - e2) << 23);
+            const float back = __uint_as_float((uint32_t)(127 + e2) << 23) * to_log2;
+            kc[nt][0] = __shfl_sync(0xffffffffu, back, 8 * c);
+            kc[nt][1] = __shfl_sync(0xffffffffu, back, 8 * c + 4);
+#pragma unroll
+            for (int t = 0; t < KS; ++t)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const float lo = v[t][2 * h] * over, hi = v[t][2 * h + 1] * over;
+                    q[nt][t][0][h] = pack_f16x2(lo, hi);
+                    if constexpr (kParts == 2) q[nt][t][1][h] = rest_f16x2(q[nt][t][0][h], lo, hi);
+                }
+        }
+        float o[NT][MT][4], m[NT][2], mo[NT][2], l[NT][2];  // l of this lane's keys
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+            for (int t = 0; t < MT; ++t) o[nt][t][0] = o[nt][t][1] = o[nt][t][2] = o[nt][t][3] = 0.f;
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+                m[nt][y] = mo[nt][y] = -INFINITY;
+                l[nt][y] = 0.f;
+            }
+        }
+        for (int n = w.i0, b = 0, scale = 0; n < w.i1; ++n, b = b + 1 == kStages ? 0 : b + 1, scale = scale + 1 == kScales ? 0 : scale + 1) {
+            fetch();                                        // into the stage of the step before
+            asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
+            __syncwarp();                                   // other lanes' copies too
+            const int j = key_tile(w.vis, n) * kTile + warp * kRun;
+            if (any_visible(w.vis, j, kRun)) {
+                const unsigned char *codes = s.ring[warp][b][0];
+                const float ks = s.scales[warp][scale][0], vs = s.scales[warp][scale][1], lv = lg2(vs);
+                float x[NT][4];
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) x[nt][0] = x[nt][1] = x[nt][2] = x[nt][3] = 0.f;
+#pragma unroll
+                for (int t4 = 0; t4 < KS / 4; ++t4) {
+                    const uint4 k0 = *reinterpret_cast<const uint4 *>(codes + Place<D>::chunk(key0, c + 4 * t4));
+                    const uint4 k1 = *reinterpret_cast<const uint4 *>(codes + Place<D>::chunk(key0 + 8, c + 4 * t4));
+                    const uint32_t w0[4] = {k0.x, k0.y, k0.z, k0.w}, w1[4] = {k1.x, k1.y, k1.z, k1.w};
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) {
+                        const uint32_t f[4] = {decode_lo(w0[t]), decode_lo(w1[t]), decode_hi(w0[t]), decode_hi(w1[t])};
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                            for (int p = 0; p < kParts; ++p) mma(x[nt], f, q[nt][4 * t4 + t][p][0], q[nt][4 * t4 + t][p][1]);
+                    }
+                }
+                const bool v0 = key_visible(w.vis, j + key0), v1 = key_visible(w.vis, j + key0 + 8);
+                bool above = false;
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) {
+                        const float f = fminf(ks * kc[nt][y], kMax);
+                        x[nt][y] = v0 ? x[nt][y] * f : -INFINITY;
+                        x[nt][2 + y] = v1 ? x[nt][2 + y] * f : -INFINITY;
+                        const float top = fmaxf(x[nt][y], x[nt][2 + y]);
+                        above |= top > m[nt][y] + kSlack || top + lv > mo[nt][y] + kSlack;
+                    }
+                if (__any_sync(0xffffffffu, above)) {
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int y = 0; y < 2; ++y) {
+                            float top = fmaxf(x[nt][y], x[nt][2 + y]);
+#pragma unroll
+                            for (int z = 4; z < 32; z <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, z));
+                            if (top > m[nt][y] + kSlack) {
+                                l[nt][y] *= m[nt][y] == -INFINITY ? 1.f : pipe::ex2(m[nt][y] - top);    // (zero, or NaN)
+                                m[nt][y] = top;
+                            }
+                            if (top + lv > mo[nt][y] + kSlack) {
+                                const float f = mo[nt][y] == -INFINITY ? 1.f : pipe::ex2(mo[nt][y] - (top + lv));
+                                mo[nt][y] = top + lv;
+#pragma unroll
+                                for (int t = 0; t < MT; ++t) {
+                                    o[nt][t][y] *= f;
+                                    o[nt][t][2 + y] *= f;
+                                }
+                            }
+                        }
+                }
+                uint32_t p[NT][kParts][2];                  // keys 0 ... 7, 8 ... 15 in S^T's order
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    float pv[4];
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) {
+                        const float base = m[nt][y] == -INFINITY ? 0.f : m[nt][y], base_o = mo[nt][y] == -INFINITY ? 0.f : mo[nt][y];
+                        const float gain = pipe::ex2(fminf(lv + base - base_o + kTop, 127.f));
+                        const float p0 = pipe::ex2(x[nt][y] - base), p1 = pipe::ex2(x[nt][2 + y] - base);
+                        l[nt][y] += p0 + p1;
+                        pv[y] = p0 * gain;
+                        pv[2 + y] = p1 * gain;
+                    }
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const uint32_t hi = pack_f16x2(pv[2 * h], pv[2 * h + 1]);
+                        p[nt][0][h] = transpose8(hi);
+                        if constexpr (kParts == 2) p[nt][1][h] = transpose8(rest_f16x2(hi, pv[2 * h], pv[2 * h + 1]));
+                    }
+                }
+                // V: this lane has D / 8 features from D / 8 g, of keys 2 c, 2 c + 1, 2 c + 8, 2 c + 9 in that order
+                const unsigned char *values = codes + kRun * D;
+                const int ka = Place<D>::key_of(2 * c), kb = Place<D>::key_of(2 * c + 1);
+                constexpr int kWords = D / 32;
+                uint32_t r[4][kWords];
+#pragma unroll
+                for (int y = 0; y < 4; ++y) {
+                    const int key = (y & 1 ? kb : ka) + (y & 2 ? 8 : 0);
+                    if constexpr (D == 128) {
+                        const uint4 v = *reinterpret_cast<const uint4 *>(values + Place<D>::chunk(key, g));
+                        r[y][0] = v.x, r[y][1] = v.y, r[y][2] = v.z, r[y][3] = v.w;
+                    } else {
+                        const uint2 v = *reinterpret_cast<const uint2 *>(values + Place<D>::chunk(key, g >> 1) + 8 * (g & 1));
+                        r[y][0] = v.x, r[y][1] = v.y;
+                    }
+                }
+#pragma unroll
+                for (int t = 0; t < MT; ++t) {              // features 2 t, 2 t + 1 of the lane's
+                    const uint32_t sel = t & 1 ? 0x7362u : 0x5140u;
+                    const uint32_t lo = __byte_perm(r[0][t / 2], r[1][t / 2], sel), hi = __byte_perm(r[2][t / 2], r[3][t / 2], sel);
+                    const uint32_t f[4] = {decode_lo(lo), decode_hi(lo), decode_lo(hi), decode_hi(hi)};
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int z = 0; z < kParts; ++z) mma(o[nt][t], f, p[nt][z][0], p[nt][z][1]);
+                }
+            }
+            __syncwarp();                                   // the stage has been read
+        }
+        // the segment after this one: its first copies are under way meanwhile
+        const bool whole = w.whole();
+        const int req = w.req;
+        float *part = a.part + w.slot() * partial_floats(rows, D);
+        go = w.next(a);
+        if (go) {
+            first_page();
+            first_steps();
+        }
+        float back[NT][2];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+#pragma unroll
+                for (int z = 4; z < 32; z <<= 1) l[nt][y] += __shfl_xor_sync(0xffffffffu, l[nt][y], z);
+                if (g == 0) {
+                    s.m[warp][8 * nt + 2 * c + y] = m[nt][y];
+                    s.l[warp][8 * nt + 2 * c + y] = l[nt][y];
+                }
+                // O relative to m
+                back[nt][y] = m[nt][y] == -INFINITY ? 0.f : pipe::ex2(mo[nt][y] - m[nt][y] - kTop);
+            }
+#pragma unroll
+        for (int pass = 0; pass < S::kPasses; ++pass) {     // D / 32 features of each lane's
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int y = 0; y < 2; ++y)
+#pragma unroll
+                    for (int t = 0; t < MT / S::kPasses; ++t) {
+                        const float(&from)[4] = o[nt][pass * (MT / S::kPasses) + t];
+                        *reinterpret_cast<float2 *>(&s.o[warp][8 * nt + 2 * c + y][g * (D / 32) + 2 * t]) =
+                            make_float2(from[y] * back[nt][y], from[2 + y] * back[nt][y]);
+                    }
+            __syncthreads();
+            // the warps
+            for (int x = tid; x < rows * S::kPass; x += kThreads) {
+                const int rho = x / S::kPass, at = x % S::kPass;
+                const int col = at / (D / 32) * (D / 8) + pass * (D / 32) + at % (D / 32);
+                float top = s.m[0][rho], sum = 0.f, out = 0.f;
+#pragma unroll
+                for (int y = 1; y < kWarps; ++y) top = fmaxf(top, s.m[y][rho]);
+                const float base = top == -INFINITY ? 0.f : top;
+#pragma unroll
+                for (int y = 0; y < kWarps; ++y) {
+                    const float f = pipe::ex2(s.m[y][rho] - base);
+                    sum = fmaf(f, s.l[y][rho], sum);
+                    out = fmaf(f, s.o[y][rho][at], out);
+                }
+                if (whole) {
+                    size_t to;
+                    if (row_at(a, req, u, rho, to)) static_cast<T *>(a.O)[to + col] = from_f32<T>(out / sum);
+                } else {
+                    part[2 * rows + (size_t)col * rows + rho] = out;
+                    if (pass == 0 && at == 0) {
+                        part[rho] = top;
+                        part[rows + rho] = sum;
+                    }
+                }
+            }
+            __syncthreads();                                // before the next pass, or segment
+        }
+    }
+    if (tid == 0) write_note(a, work, w, sh);
+    write_empty<T, kThreads>(a, tid);
+}
+
+template <typename T, int D, int NT> cudaError_t launch(const PagedArgs &a, cudaStream_t st)
+{
+    using S = Smem<D, NT>;
+    static_assert(sizeof(S) <= (NT == 1 ? 115200 : 232448), "blocks of a multiprocessor");
+    static std::atomic<unsigned long long> opted{0};
+    const cudaError_t e = pipe::opt_in(reinterpret_cast<const void *>(&k_paged_attn_quant<T, D, NT>), (int)sizeof(S), opted);
+    if (e != cudaSuccess) return e;
+    int lg = 4;
+    while ((1 << lg) < a.page_size) ++lg;
+    return pipe::launch_early(k_paged_attn_quant<T, D, NT>, dim3(a.n_cta), dim3(kThreads), sizeof(S), st, a, lg);
+}
+template <typename T> cudaError_t launch(const PagedArgs &a, cudaStream_t st)
+{
+    const int rows = a.Bt * a.Gt;
+    if (a.d == 128) return rows <= 8 ? launch<T, 128, 1>(a, st) : launch<T, 128, 2>(a, st);
+    return rows <= 8 ? launch<T, 64, 1>(a, st) : (rows <= 16 ? launch<T, 64, 2>(a, st) : launch<T, 64, 4>(a, st));
+}
+
+}  // namespace
+
+void paged_quant_geometry(const hybrid_cfg &c, PagedArgs &a)
+{
+    a.B = c.block_size;
+    a.Hq = c.n_q_heads;
+    a.Hkv = c.n_kv_heads;
+    a.G = c.n_q_heads / c.n_kv_heads;
+    a.d = c.head_dim;
+    paged_cut_rows(a, c.head_dim == 128 ? 16 : 32);
+    a.extra = 7;
+    a.n_cta = (a.Bt * a.Gt > 8 ? 1 : 2) * pipe::sm_count();  // resident blocks
+}
+
+cudaError_t launch_paged_attn_quant(hybrid_dtype dt, const PagedArgs &a, cudaStream_t st)
+{
+    const cudaError_t e = dt == HYBRID_BF16 ? launch<__nv_bfloat16>(a, st) : launch<float>(a, st);
+    return e != cudaSuccess ? e : launch_paged_join(dt, a, st);
+}
+
+}  // namespace hyb
