@@ -437,10 +437,12 @@ template <typename T> cudaError_t launch(const PagedArgs &a, cudaStream_t st)
 {
     const int rows = a.Bt * a.Gt;
     if (a.d == 128) return rows <= 8 ? launch<T, 128, 1>(a, st) : launch<T, 128, 2>(a, st);
-    return rows <= 8 ? launch<T, 64, 1>(a, st) : (rows <= 16 ? launch<T, 64, 2>(a, st) : launch<T, 64, 4>(a, st));
+    return rows <= 8 ? launch<T, 64, 1>(a, st) : launch<T, 64, 2>(a, st);
 }
 
 }  // namespace
+
+constexpr int kMostRows = 16;                   // of a warp; bfloat16 calls with more rows go to the tensor cores
 
 void paged_quant_geometry(const hybrid_cfg &c, PagedArgs &a)
 {
@@ -449,14 +451,18 @@ void paged_quant_geometry(const hybrid_cfg &c, PagedArgs &a)
     a.Hkv = c.n_kv_heads;
     a.G = c.n_q_heads / c.n_kv_heads;
     a.d = c.head_dim;
-    paged_cut_rows(a, c.head_dim == 128 ? 16 : 32);
+    const bool tc = c.io_dtype == HYBRID_BF16 && a.G * a.B > kMostRows;
+    paged_cut_rows(a, tc ? 128 : kMostRows);
     a.extra = 7;
     a.n_cta = (a.Bt * a.Gt > 8 ? 1 : 2) * pipe::sm_count();  // resident blocks
 }
 
 cudaError_t launch_paged_attn_quant(hybrid_dtype dt, const PagedArgs &a, cudaStream_t st)
 {
-    const cudaError_t e = dt == HYBRID_BF16 ? launch<__nv_bfloat16>(a, st) : launch<float>(a, st);
+    cudaError_t e;
+    if (dt == HYBRID_F32) e = launch<float>(a, st);
+    else if (a.G * a.B > kMostRows) e = launch_paged_attn_quant_tc(a, st);
+    else e = launch<__nv_bfloat16>(a, st);
     return e != cudaSuccess ? e : launch_paged_join(dt, a, st);
 }
 

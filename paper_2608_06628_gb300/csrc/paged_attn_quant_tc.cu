@@ -1,0 +1,712 @@
+// paged_attn_quant_tc.cu -- attention over the 8-bit paged cache on the tensor cores, bfloat16
+// queries with more rows than a warp takes (hybrid_paged_attn_quant: blocks of tokens).
+//
+// As paged_attn_tc.cu: a row tile of up to 128 query rows is the M of the products, tiles of 128
+// keys, one block per SM that walks its share of all requests' tiles (paged_plan.cuh), copies of
+// the rows where they are few, references that move only when they are exceeded by more than 8.
+// What the codes change:
+//     S = Q C_K^T           half precision, C the codes; x = S ks log2(e) / sqrt(d)
+//     p = 2^(x - m),   l += p
+//     O += (p vs / 2^(r - m)) C_V,   r a reference of x + log2(vs)
+// Codes are exact in half precision.  So is a row of Q over a power of two that brings its
+// largest entry to 2^14 ... 2^15 (entries below 2^-29 of it in units of 2^-39 of it).  P has 11
+// bits, relative to a reference of its own (a token that takes most of the softmax may have
+// values near zero), and below 2^-21 of the row's largest p vs units of 2^-31 of that.
+//
+// Eight warps bring the codes from the ring that TMA fills (a page of a head is one box) to
+// half precision, 64 keys at a time, in the layout of the products' operands: 3 such pieces of K
+// and of V, so that a product never waits for the one before it to free its operand.  Q stays in
+// Tensor Memory, which keeps 32 KB a tile off shared memory: what is left, codes written and read
+// once, pieces written and read once, is 192 KB a tile, 1500 cycles, about as long as the codes'
+// 33 KB take at an SM's share of the memory bandwidth (1400).  P takes the place of the S that it
+// was made from.
+//
+// Keys that no query sees: pages and scales without a visible key are not loaded, masked scores
+// are replaced before use, masked rows of V are zeros in the operand.
+//
+// Warps: softmax and epilogue (4), converters of K (4) and V (4), producers of K with the scales,
+// and of V, issuers of S and of O.  Every wait is bounded (tc_pipeline.cuh).
+#include "paged_plan.cuh"
+#include "quant.cuh"
+#include "tc_pipeline.cuh"
+
+namespace hyb {
+namespace {
+
+using namespace paged;
+using namespace pipe;
+
+constexpr int kSmemLimit = 232448;
+constexpr int kMaxSlots = 12;
+constexpr int kPieces = 3;                // of K, and of V, in half precision
+constexpr int kPieceKeys = 64;
+constexpr int kScaleTiles = 32;           // tiles whose scales are held (see the producer)
+constexpr uint32_t kBarBytes = 1024;      // barriers, TMEM address, failure flag, the plan's scratch
+constexpr uint32_t kScaleBytes = kScaleTiles * 16 * 4;
+constexpr uint32_t kExchange = 1024;      // two floats a row
+// with copies: 64 inverse sums, and 128 rows of 32 + 4 features (a quarter of the rows: 128 + 4)
+constexpr uint32_t kStage = 256 + 128 * 36 * 4;
+constexpr float kSlack = 8.f;             // log2 of how far a reference may be exceeded
+constexpr float kTop = 7.f;               // log2 of P at its reference
+constexpr float kMax = 3.402823466e38f;
+constexpr int kThreads = 512;
+enum Role { kSoft = 0, kConvertK = 4, kConvertV = 8, kLoadK = 12, kLoadV = 13, kIssueS = 14, kIssueO = 15 };
+
+struct TcArgs {
+    CUtensorMap tmK, tmV;
+    PagedArgs p;
+    int NK, NV;                           // slots of the codes of K, then of V
+    uint32_t off_bar, off_stage, bytes;
+};
+
+__device__ __forceinline__ float lg2(float x)
+{
+    float y;
+    asm("lg2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi)
+{
+    const __half2 h = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
+
+// Keys 16 v ... 16 v + 15 of a piece (64 keys from `codes` on) to half precision, by a warp.  A
+// group of 8 lanes has 64 features of two keys that differ in bits 0 and 2: neither its reads nor
+// its writes meet in a bank.  kMasked: `see` tells which keys are visible, others become zeros.
+template <int D, bool kMasked, typename See>
+__device__ __forceinline__ void convert(const uint8_t *codes, uint8_t *piece, int v, int lane, See see)
+{
+    constexpr int kHalves = D / 64;
+    const int c = lane & 3, octet = lane >> 3 ^ (lane & 4 ? 5 : 0);
+    uint4 x[2][kHalves];
+#pragma unroll
+    for (int o = 0; o < 2; ++o) {
+        const int key = 16 * v + 8 * o + octet;
+#pragma unroll
+        for (int p = 0; p < kHalves; ++p)
+            x[o][p] = *reinterpret_cast<const uint4 *>(codes + key * D + (D == 128 ? ((4 * p + c) ^ octet) << 4 : c << 4));
+    }
+#pragma unroll
+    for (int o = 0; o < 2; ++o) {
+        const int key = 16 * v + 8 * o + octet;
+        const bool keep = !kMasked || see(key);
+#pragma unroll
+        for (int p = 0; p < kHalves; ++p) {
+            const uint32_t w[4] = {x[o][p].x, x[o][p].y, x[o][p].z, x[o][p].w};
+            uint32_t f[8];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t code = keep ? w[i] : 0u;
+                const __half2 lo = quant::decode2(code), hi = quant::decode2(code >> 16);
+                f[2 * i] = *reinterpret_cast<const uint32_t *>(&lo);
+                f[2 * i + 1] = *reinterpret_cast<const uint32_t *>(&hi);
+            }
+            uint8_t *row = piece + p * (kPieceKeys * 128) + key * 128;
+            *reinterpret_cast<uint4 *>(row + ((2 * c ^ octet) << 4)) = make_uint4(f[0], f[1], f[2], f[3]);
+            *reinterpret_cast<uint4 *>(row + (((2 * c + 1) ^ octet) << 4)) = make_uint4(f[4], f[5], f[6], f[7]);
+        }
+    }
+}
+
+// kCopies: 4, 2 or 1 copies of the rows (at most 32, 64, 128 of them).
+template <int D, int kCopies>
+__global__ void __launch_bounds__(kThreads, 1) k_paged_attn_quant_tc(const __grid_constant__ TcArgs ta)
+{
+    using namespace ptx;
+    constexpr int kHalves = D / 64;                        // 64-feature panels of a piece
+    constexpr uint32_t kPanel = kPieceKeys * 128;          // bytes of one panel
+    constexpr uint32_t kPiece = kHalves * kPanel, kCodes = kTile * D;
+    constexpr int kCopyRows = 128 / kCopies;
+    // Tensor Memory columns: S (2 x 128; then P in the first 64 of each), O, Q
+    constexpr uint32_t cS = 0, cO = 256, cQ = 384;
+    const PagedArgs &a = ta.p;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, NK = ta.NK, NV = ta.NV;
+    const int rows = a.Bt * a.Gt;
+    const int n_soft = kCopies > 1 ? 4 : (rows + 31) / 32; // softmax warps at work
+
+    uint8_t *piece_k = smem, *piece_v = smem + kPieces * kPiece, *ring = smem + 2 * kPieces * kPiece;
+    uint64_t *bars = reinterpret_cast<uint64_t *>(smem + ta.off_bar);
+    uint64_t *full = bars;               // [NK + NV] the codes have landed
+    uint64_t *empty = full + kMaxSlots;  // [NK + NV] they are converted
+    uint64_t *kfull = empty + kMaxSlots; // [3] a piece of K is in place
+    uint64_t *kempty = kfull + kPieces;  // [3] its products are done
+    uint64_t *vfull = kempty + kPieces;
+    uint64_t *vempty = vfull + kPieces;
+    uint64_t *sready = vempty + kPieces; // [2] S is formed
+    uint64_t *pready = sready + 2;       // [2] P is written (and O rescaled)
+    uint64_t *pvdone = pready + 2;       // [2] O includes the tile's P V
+    uint64_t *qready = pvdone + 2;       // the segment's Q is in place
+    uint64_t *ofree = qready + 1;        // the epilogue has read O
+    uint64_t *drained = ofree + 1;       // [2] every MMA of an issuer has completed
+    uint32_t *tmem_holder = reinterpret_cast<uint32_t *>(drained + 2);
+    volatile int *fail = reinterpret_cast<volatile int *>(tmem_holder + 1);
+    PlanSmem *plan_smem = reinterpret_cast<PlanSmem *>(tmem_holder + 2);
+    float *scales = reinterpret_cast<float *>(smem + ta.off_bar + kBarBytes);     // [kScaleTiles][8 of K, 8 of V]
+    float *exchange = scales + kScaleBytes / 4;            // [2][128]
+    float *inv_of = exchange + 256;                        // [64], with copies
+
+    if (warp == kIssueS) {
+        tmem_alloc(tmem_holder, 512);
+        tmem_relinquish();
+    }
+    if (warp == kLoadK && lane == 0) {
+        prefetch_tensormap(&ta.tmK);
+        prefetch_tensormap(&ta.tmV);
+        for (int i = 0; i < NK + NV; ++i) {
+            mbar_init(&full[i], i < NK ? 33 : 1);          // the producer's lanes for their scales, and the boxes
+            mbar_init(&empty[i], 4);
+        }
+        for (int i = 0; i < kPieces; ++i) {
+            mbar_init(&kfull[i], 4);
+            mbar_init(&kempty[i], 1);
+            mbar_init(&vfull[i], 4);
+            mbar_init(&vempty[i], 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&sready[i], 1);
+            mbar_init(&pready[i], n_soft);
+            mbar_init(&pvdone[i], 1);
+            mbar_init(&drained[i], 1);
+        }
+        mbar_init(qready, n_soft);
+        mbar_init(ofree, n_soft);
+        *fail = 0;
+        fence_mbar_init();
+    }
+    tc_fence_before();
+    __syncthreads();                                       // barriers and Tensor Memory are in place
+    tc_fence_after();
+    // what comes before in the stream is complete from here on
+    griddep_wait();
+    griddep_launch_dependents();
+    Walk w;
+    Shares sh(0, 1);
+    const bool work = find_share<kThreads>(a, *plan_smem, w, sh);
+    const uint32_t tmem = *tmem_holder;
+
+    if (warp == kLoadK || warp == kLoadV) {
+        // ------------------------------------------------------ producers of the codes
+        const bool is_v = warp == kLoadV;
+        if (work) {
+            const int P = a.page_size, per = kTile / P;    // pages of a tile
+            const uint32_t page_bytes = (uint32_t)P * D, n_slots = is_v ? NV : NK;
+            const CUtensorMap *map = is_v ? &ta.tmV : &ta.tmK;
+            uint64_t *my_full = is_v ? full + NK : full, *my_empty = is_v ? empty + NK : empty;
+            uint8_t *my_ring = is_v ? ring + (size_t)NK * kCodes : ring;
+            // a cache that is read once need not push tables, lengths and partials out of L2
+            const bool once = row_tiles(a) == 1;
+            const uint64_t policy = policy_evict_first();
+            // lanes 0 ... 7, 8 ... 15: scales of K, V of the 8 groups of a tile
+            const int group = 16 * (lane & 7), lg = 31 - __clz(P);
+            const float *my_scale = lane < 8 ? a.K_scale : a.V_scale;
+            uint32_t n = 0;                                // tiles issued
+            RingPos pos{0, 1};                             // phase of `empty`: the first round is free
+            bool ok = true;
+            while (ok && w.next(a)) {
+                const int head = w.head;
+                const int *pages = a.table + (size_t)w.req * a.max_pages;
+                auto page_at = [&](int i) -> int {         // this lane's page of tile i, -1: nothing visible in it
+                    if (i >= w.i1 || lane >= per) return -1;
+                    const int j = key_tile(w.vis, i) * per + lane;
+                    if (!any_visible(w.vis, j * P, P)) return -1;
+                    const int page = __ldg(pages + j);
+                    if (page >= 0 && page < a.n_pages) return page;
+                    raise_error(a.err, ERR_BAD_INDEX);
+                    return 0;
+                };
+                int next_page = page_at(w.i0);
+                for (int i = w.i0; i < w.i1; ++i) {
+                    const int page = next_page;
+                    next_page = page_at(i + 1);            // a tile ahead of its use
+                    const uint32_t bytes = page_bytes * __popc(__ballot_sync(0xffffffffu, page >= 0));
+                    ok = wait_soon(&my_empty[pos.slot], pos.phase, fail);
+                    if (__any_sync(0xffffffffu, !ok)) {
+                        ok = false;
+                        break;
+                    }
+                    if (lane == 0) mbar_arrive_expect_tx(&my_full[pos.slot], bytes);
+                    __syncwarp();
+                    if (page >= 0) {
+                        uint8_t *dst = my_ring + (size_t)pos.slot * kCodes + lane * P * D;
+                        if (once) tma_load_4d_policy(dst, map, 0, 0, head, page, &my_full[pos.slot], policy);
+                        else tma_load_4d(dst, map, 0, 0, head, page, &my_full[pos.slot]);
+                    }
+                    if (!is_v) {
+                        // Zeros for groups without a visible key.  The place was that of 32 tiles ago, whose softmax
+                        // is done: the slot's last tile, at most 12 ago, is converted, so the products of the piece
+                        // 3 before it are done, and so is the softmax that freed their S, 3 tiles before that at most.
+                        const int of = __shfl_sync(0xffffffffu, page, group >> lg);
+                        const bool see = any_visible(w.vis, key_tile(w.vis, i) * kTile + group, 16);
+                        if (lane < 16) {
+                            const float *src = my_scale + (see ? (((size_t)of * a.Hkv + head) << lg | (group & (P - 1))) / 16 : 0);
+                            asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(
+                                             smem_u32(scales + n % kScaleTiles * 16 + lane)),
+                                         "l"(src), "r"(see ? 4 : 0)
+                                         : "memory");
+                        }
+                        cp_async_arrive_noinc(&my_full[pos.slot]);
+                    }
+                    pos.step(n_slots);
+                    ++n;
+                }
+            }
+            cp_async_wait_all();
+            if (*fail && lane == 0) {
+                // let copies in flight land before the block exits
+                for (uint32_t s = 0; s < n_slots; ++s) {
+                    const uint32_t k = n / n_slots + (s < n % n_slots ? 1u : 0u);
+                    if (k) mbar_wait(&my_full[s], (k - 1) & 1u, kWaitNs);
+                }
+            }
+        }
+        if (is_v) {
+            if (lane == 0) write_note(a, work, w, sh);
+            write_empty<bf16, 32>(a, lane);
+        }
+    } else if (work && warp >= kConvertK && warp < kLoadK) {
+        // ------------------------------------------------------ converters
+        const bool is_v = warp >= kConvertV;
+        const int v = warp & 3;
+        const uint32_t n_slots = is_v ? NV : NK;
+        uint64_t *my_full = is_v ? full + NK : full, *my_empty = is_v ? empty + NK : empty;
+        uint64_t *done = is_v ? vfull : kfull, *free = is_v ? vempty : kempty;
+        uint8_t *my_ring = is_v ? ring + (size_t)NK * kCodes : ring, *my_piece = is_v ? piece_v : piece_k;
+        RingPos pos{0, 0}, to{0, 1};
+        bool ok = true;
+        while (ok && w.next(a)) {
+            for (int i = w.i0; i < w.i1; ++i) {
+                const int j0 = key_tile(w.vis, i) * kTile;
+                const bool edge = is_v && !all_visible(w.vis, j0);
+                ok = wait_soon(&my_full[pos.slot], pos.phase, fail);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    ok = ok && wait_soon(&free[to.slot], to.phase, fail);
+                    if (__any_sync(0xffffffffu, !ok)) {
+                        ok = false;
+                        break;
+                    }
+                    const uint8_t *codes = my_ring + (size_t)pos.slot * kCodes + h * kPieceKeys * D;
+                    uint8_t *piece = my_piece + to.slot * kPiece;
+                    const int j = j0 + h * kPieceKeys;
+                    if (edge) convert<D, true>(codes, piece, v, lane, [&](int key) { return key_visible(w.vis, j + key); });
+                    else convert<D, false>(codes, piece, v, lane, [](int) { return true; });
+                    fence_proxy_async_smem();
+                    __syncwarp();
+                    if (lane == 0) {
+                        mbar_arrive(&done[to.slot]);
+                        if (h == 1) mbar_arrive(&my_empty[pos.slot]);
+                    }
+                    to.step(kPieces);
+                }
+                if (!ok) break;
+                pos.step(n_slots);
+            }
+        }
+    } else if (work && warp == kIssueS) {
+        // --------------------------------------------- issuer of S = Q K^T
+        if (lane == 0) {
+            const uint32_t id = instr_desc(FMT_F16, FMT_F16, false, false, 128, kPieceKeys);
+            const uint64_t k_desc = smem_desc(smem_u32(piece_k), 16, 1024, SWZ_128B);
+            uint32_t n = 0, seg = 0;                       // tiles and segments so far
+            RingPos pos{0, 0};
+            bool ok = true;
+            while (ok && w.next(a)) {
+                ok = wait_soon(qready, seg & 1u, fail);
+                ++seg;
+                for (int i = w.i0; ok && i < w.i1; ++i, ++n) {
+                    const uint32_t b = n & 1;
+                    ok = wait_soon(&pvdone[b], ((n >> 1) & 1u) ^ 1u, fail);     // P in S's buffer is multiplied
+                    for (int h = 0; ok && h < 2; ++h) {
+                        ok = wait_soon(&kfull[pos.slot], pos.phase, fail);
+                        if (!ok) break;
+                        tc_fence_after();
+                        const uint64_t bk = k_desc + pos.slot * (kPiece >> 4);
+#pragma unroll
+                        for (int k = 0; k < D / 16; ++k)
+                            mma_bf16_ts(tmem + cS + 128 * b + 64 * h, tmem + cQ + 8 * k, bk + (k >> 2) * (kPanel >> 4) + (k & 3) * 2, id,
+                                        k > 0);
+                        mma_commit(&kempty[pos.slot]);
+                        pos.step(kPieces);
+                    }
+                    if (ok) mma_commit(&sready[b]);
+                }
+            }
+            mma_commit(&drained[0]);
+            mbar_wait(&drained[0], 0, kWaitNs);
+        }
+    } else if (work && warp == kIssueO) {
+        // ------------------------------------------------------ issuer of O += P V
+        if (lane == 0) {
+            const uint32_t id = instr_desc(FMT_F16, FMT_F16, false, true, 128, D);
+            const uint64_t v_desc = smem_desc(smem_u32(piece_v), kPanel, 1024, SWZ_128B);
+            constexpr int kOwn = kTile / 16 / kCopies;     // steps of 16 keys of a copy
+            uint32_t n = 0, seg = 0;
+            RingPos pos{0, 0};
+            bool ok = true;
+            while (ok && w.next(a)) {
+                // O is overwritten by a segment's first product: the last epilogue has read it
+                if (seg > 0) ok = wait_soon(ofree, (seg - 1) & 1u, fail);
+                ++seg;
+                for (int i = w.i0; ok && i < w.i1; ++i, ++n) {
+                    const uint32_t b = n & 1;
+                    ok = wait_soon(&pready[b], (n >> 1) & 1u, fail);
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        ok = ok && wait_soon(&vfull[pos.slot], pos.phase, fail);
+                        if (!ok) break;
+                        tc_fence_after();
+                        const uint64_t bv = v_desc + pos.slot * (kPiece >> 4);
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) {
+                            const int g = 4 * h + x;
+                            const uint32_t from = tmem + cS + 128 * b + 8 * g, acc = i > w.i0 || g % kOwn > 0;
+                            if constexpr (kCopies > 1) mma_bf16_ts_lanes(tmem + cO, from, bv + x * (2048 >> 4), id, acc, kCopies, g / kOwn);
+                            else mma_bf16_ts(tmem + cO, from, bv + x * (2048 >> 4), id, acc);
+                        }
+                        mma_commit(&vempty[pos.slot]);
+                        pos.step(kPieces);
+                    }
+                    if (ok) mma_commit(&pvdone[b]);
+                }
+            }
+            mma_commit(&drained[1]);
+            mbar_wait(&drained[1], 0, kWaitNs);
+        }
+    } else if (work && warp < n_soft) {
+        // --------------------------------------------------- Q, softmax, epilogue
+        constexpr int kKeys = kTile / kCopies;              // keys of a tile of this thread
+        constexpr int kGroups = kKeys / 16;
+        constexpr bool kKeep = kKeys <= 64;                 // scores stay in registers between the passes
+        const int copy = tid / kCopyRows, row = tid % kCopyRows, key0 = kKeys * copy;
+        const uint32_t lane_off = (uint32_t)(32 * warp) << 16;
+        const float to_log2 = kLog2e * rsqrtf((float)D);
+        float *stage = reinterpret_cast<float *>(smem + ta.off_stage);   // with copies
+        uint32_t n = 0;                                     // tiles so far
+        bool bad = false;                                   // a wait gave up: leave at the next vote
+        auto wait = [&](uint64_t *bar, uint32_t parity) {
+            bad = __any_sync(0xffffffffu, bad || !wait_soon(bar, parity, fail));
+        };
+        // arrival of the warp, after its Tensor Memory accesses
+        auto arrive = [&](uint64_t *bar) {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0 && !bad) mbar_arrive(bar);
+        };
+        while (w.next(a)) {     // left by a vote at a segment's end only, so that the warps of a row stay together
+            const Unit u = unit_of(a, w.head, w.rt);
+            size_t at;
+            const bool live = row_at(a, w.req, u, row, at), whole = w.whole();
+            float kc;                                       // log2(e) / sqrt(d) over the row's factor
+            {   // Q.  (The last segment's products with it are done: its last S has been read.)
+                const bf16 *src = static_cast<const bf16 *>(a.Q) + at;
+                uint4 v[D / 8];
+#pragma unroll
+                for (int x = 0; x < D / 8; ++x)
+                    v[x] = live ? __ldg(reinterpret_cast<const uint4 *>(src) + x) : make_uint4(0, 0, 0, 0);
+                uint32_t top = 0;
+#pragma unroll
+                for (int x = 0; x < D / 8; ++x) {
+                    const uint32_t q4[4] = {v[x].x, v[x].y, v[x].z, v[x].w};
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) {
+                        const uint32_t lo = q4[y] & 0x7fffu, hi = q4[y] >> 16 & 0x7fffu;
+                        if (lo < 0x7f80u) top = max(top, lo);
+                        if (hi < 0x7f80u) top = max(top, hi);
+                    }
+                }
+                int e2 = (int)(top >> 7) - 127 - 14;        // the row over 2^e2 is below 2^15
+                if (e2 < -126) e2 = -126;
+                const float over = __uint_as_float((uint32_t)(127 - e2) << 23);
+                kc = __uint_as_float((uint32_t)(127 + e2) << 23) * to_log2;
+                tc_fence_after();
+#pragma unroll
+                for (int x = 0; x < D / 32; ++x) {
+                    float f[16];
+#pragma unroll
+                    for (int y = 0; y < 16; ++y) {
+                        const uint4 &q4 = v[4 * x + y / 4];
+                        const uint32_t q2 = y % 4 == 0 ? q4.x : (y % 4 == 1 ? q4.y : (y % 4 == 2 ? q4.z : q4.w));
+                        f[y] = __uint_as_float(pack_f16x2(__uint_as_float(q2 << 16) * over, __uint_as_float(q2 & 0xffff0000u) * over));
+                    }
+                    tmem_st16(tmem + cQ + 16 * x + lane_off, f);
+                }
+                tmem_wait_st();
+                arrive(qready);
+            }
+            float m = -INFINITY, mo = -INFINITY;            // references of l and of O
+            f32x2 l2 = pair2(0.f, 0.f);                     // the row's sum over this thread's keys, in two
+            for (int i = w.i0; i < w.i1; ++i, ++n) {
+                const uint32_t b = n & 1;
+                const int j0 = key_tile(w.vis, i) * kTile;
+                const bool edge = !all_visible(w.vis, j0);
+                const int k0 = j0 + key0, hi = w.vis.len - k0, lo = w.vis.lo - k0, sink = w.vis.sink - k0;
+                auto seen = [&](int k) { return k < hi && (k >= lo || k < sink); };
+                wait(&sready[b], (n >> 1) & 1u);
+                tc_fence_after();
+                const float *my_scales = scales + n % kScaleTiles * 16 + kGroups * copy;
+                float fk[kGroups], lv[kGroups];
+#pragma unroll
+                for (int g = 0; g < kGroups; ++g) {
+                    fk[g] = fminf(my_scales[g] * kc, kMax);
+                    lv[g] = lg2(my_scales[8 + g]);
+                }
+                const uint32_t my_s = tmem + cS + 128 * b + lane_off;
+                float s[kKeep ? kKeys / 32 : 1][32];
+                float mx = -INFINITY, my = -INFINITY;       // of x, of x + log2(vs)
+#pragma unroll
+                for (int x = 0; x < kKeys / 32; ++x) {
+                    float(&v)[32] = s[kKeep ? x : 0];
+                    tmem_ld32(my_s + key0 + 32 * x, v);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const int g = 2 * x + h;
+                        float top = -INFINITY;
+                        if (edge) {
+#pragma unroll
+                            for (int y = 0; y < 16; ++y)
+                                if (seen(16 * g + y)) top = fmaxf(top, v[16 * h + y]);
+                        } else {
+                            float t[2] = {v[16 * h], v[16 * h + 1]};
+#pragma unroll
+                            for (int y = 2; y < 16; ++y) t[y & 1] = fmaxf(t[y & 1], v[16 * h + y]);
+                            top = fmaxf(t[0], t[1]);
+                        }
+                        top *= fk[g];                       // (NaN without a visible key)
+                        mx = fmaxf(mx, top);
+                        my = fmaxf(my, top + lv[g]);
+                    }
+                }
+                float f = 1.f;
+                if (mx > m + kSlack) {                      // from -inf: whenever a key is visible
+                    if (m != -INFINITY) {                   // (else the sum is zero)
+                        const float fl = ex2(m - mx);
+                        l2 = mul2(l2, pair2(fl, fl));
+                    }
+                    m = mx;
+                }
+                if (my > mo + kSlack) {
+                    if (mo != -INFINITY) f = ex2(mo - my);
+                    mo = my;
+                }
+                // O is at rest once earlier products are done
+                if (__any_sync(0xffffffffu, f != 1.f && row < rows)) {
+                    wait(&pvdone[(n - 1) & 1], ((n - 1) >> 1) & 1u);
+                    tc_fence_after();
+#pragma unroll 1
+                    for (int x = 0; x < D / 16; ++x) {
+                        float o[16];
+                        tmem_ld16(tmem + cO + 16 * x + lane_off, o);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int y = 0; y < 16; ++y) o[y] *= f;
+                        tmem_st16(tmem + cO + 16 * x + lane_off, o);
+                    }
+                }
+                const float base = m == -INFINITY ? 0.f : m, to_o = base - (mo == -INFINITY ? 0.f : mo) + kTop;
+                const f32x2 base2 = pair2(-base, -base);
+#pragma unroll
+                for (int x = 0; x < kKeys / 32; ++x) {
+                    float(&v)[32] = s[kKeep ? x : 0];
+                    if (!kKeep) {
+                        tmem_ld32(my_s + key0 + 32 * x, v);
+                        tmem_wait_ld();
+                    }
+                    float p[16];                            // pairs of half precision
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const int g = 2 * x + h;
+                        const float gain = ex2(fminf(lv[g] + to_o, 127.f));
+                        const f32x2 f2 = pair2(fk[g], fk[g]), gain2 = pair2(gain, gain);
+#pragma unroll
+                        for (int y = 0; y < 16; y += 2) {
+                            float p0, p1;
+                            unpair2(fma2(pair2(v[16 * h + y], v[16 * h + y + 1]), f2, base2), p0, p1);
+                            if (edge) {
+                                if (!seen(16 * g + y)) p0 = -INFINITY;
+                                if (!seen(16 * g + y + 1)) p1 = -INFINITY;
+                            }
+                            const f32x2 pp = pair2(ex2(p0), ex2(p1));
+                            l2 = add2(l2, pp);
+                            unpair2(mul2(pp, gain2), p0, p1);
+                            p[8 * h + y / 2] = __uint_as_float(pack_f16x2(p0, p1));
+                        }
+                    }
+                    tmem_st16(my_s + key0 / 2 + 16 * x, p);
+                }
+                tmem_wait_st();
+                arrive(&pready[b]);
+            }
+            // the segment's output
+            bf16 *out = static_cast<bf16 *>(a.O) + at;
+            float *partial = a.part + w.slot() * partial_floats(rows, D);
+            float l, l_odd;
+            unpair2(l2, l, l_odd);
+            l += l_odd;
+            if (kCopies > 1) {
+                // reference and sum of the row over its copies
+                exchange[tid] = m;
+                exchange[128 + tid] = l;
+                if (group_sync_failed(1, 128, bad)) break;
+                m = exchange[row];
+#pragma unroll
+                for (int c = 1; c < kCopies; ++c) m = fmaxf(m, exchange[c * kCopyRows + row]);
+                const float base = m == -INFINITY ? 0.f : m;
+                l = 0.f;
+#pragma unroll
+                for (int c = 0; c < kCopies; ++c)
+                    l = fmaf(exchange[128 + c * kCopyRows + row], ex2(exchange[c * kCopyRows + row] - base), l);
+                if (copy == 0) inv_of[row] = 1.f / l;               // read after the next barrier
+            }
+            const float f = ex2(mo - kTop - (m == -INFINITY ? 0.f : m));    // O relative to m
+            if (!whole && row < rows && copy == 0) {
+                partial[row] = m;
+                partial[rows + row] = l;
+            }
+            wait(&pvdone[(n - 1) & 1], ((n - 1) >> 1) & 1u);
+            tc_fence_after();
+            if constexpr (kCopies > 1) {
+                // The copies' rows are added in order, in shared memory, as many features
+                // (32, 64 or 128) at a time as it holds of these rows: [copy][row][width + 4].
+                const int width = rows <= kCopyRows / 4 ? 128 : (rows <= kCopyRows / 2 ? 64 : 32);
+                const int span = width < D ? width : D, pitch = span + 4;
+#pragma unroll 1
+                for (int x0 = 0; x0 < D; x0 += span) {
+                    float *mine = stage + (copy * rows + row) * pitch;
+#pragma unroll 1
+                    for (int x = 0; x < span; x += 32) {
+                        float o[32];
+                        tmem_ld32(tmem + cO + x0 + x + lane_off, o);
+                        tmem_wait_ld();
+                        if (row < rows) {
+#pragma unroll
+                            for (int y = 0; y < 32; y += 4)
+                                *reinterpret_cast<float4 *>(mine + x + y) =
+                                    f != 0.f ? make_float4(o[y] * f, o[y + 1] * f, o[y + 2] * f, o[y + 3] * f)
+                                             : make_float4(0.f, 0.f, 0.f, 0.f);
+                        }
+                    }
+                    if (x0 + span == D) arrive(ofree);
+                    group_sync_failed(1, 128, false);
+                    if (!bad) {
+                        if (whole) {                       // eight features of a row
+                            for (int x = tid; x < rows * (span / 8); x += 128) {
+                                const int r = x / (span / 8), col = x % (span / 8) * 8;
+                                const float *src = stage + r * pitch + col;
+                                float4 v0 = make_float4(0.f, 0.f, 0.f, 0.f), v1 = v0;
+#pragma unroll
+                                for (int c = 0; c < kCopies; ++c) {
+                                    const float4 s0 = *reinterpret_cast<const float4 *>(src + c * rows * pitch);
+                                    const float4 s1 = *reinterpret_cast<const float4 *>(src + c * rows * pitch + 4);
+                                    v0 = make_float4(v0.x + s0.x, v0.y + s0.y, v0.z + s0.z, v0.w + s0.w);
+                                    v1 = make_float4(v1.x + s1.x, v1.y + s1.y, v1.z + s1.z, v1.w + s1.w);
+                                }
+                                const float k = inv_of[r];
+                                size_t to;
+                                if (row_at(a, w.req, u, r, to))
+                                    *reinterpret_cast<uint4 *>(static_cast<bf16 *>(a.O) + to + x0 + col) = make_uint4(
+                                        pack_bf16x2(v0.x * k, v0.y * k), pack_bf16x2(v0.z * k, v0.w * k),
+                                        pack_bf16x2(v1.x * k, v1.y * k), pack_bf16x2(v1.z * k, v1.w * k));
+                            }
+                        } else {                           // feature-major, as the join reads it
+                            for (int x = tid; x < rows * span; x += 128) {
+                                const int r = x % rows, col = x / rows;
+                                float v = 0.f;
+#pragma unroll
+                                for (int c = 0; c < kCopies; ++c) v += stage[(c * rows + r) * pitch + col];
+                                partial[2 * rows + (size_t)x0 * rows + x] = v;
+                            }
+                        }
+                    }
+                    group_sync_failed(1, 128, false);
+                }
+            } else {
+                const float k = whole ? f / l : f;
+#pragma unroll 1
+                for (int x = 0; x < D / 32; ++x) {
+                    float o[32];
+                    tmem_ld32(tmem + cO + 32 * x + lane_off, o);
+                    tmem_wait_ld();
+                    if (x == D / 32 - 1) arrive(ofree);
+                    if (bad) continue;
+#pragma unroll
+                    for (int y = 0; y < 32; ++y) o[y] *= k;
+                    if (whole) {
+                        if (live) {
+#pragma unroll
+                            for (int y = 0; y < 32; y += 8)
+                                *reinterpret_cast<uint4 *>(out + 32 * x + y) =
+                                    make_uint4(pack_bf16x2(o[y], o[y + 1]), pack_bf16x2(o[y + 2], o[y + 3]),
+                                               pack_bf16x2(o[y + 4], o[y + 5]), pack_bf16x2(o[y + 6], o[y + 7]));
+                        }
+                    } else if (row < rows) {
+                        float *po = partial + 2 * rows + (size_t)(32 * x) * rows + row;
+#pragma unroll
+                        for (int y = 0; y < 32; ++y) po[(size_t)y * rows] = o[y];
+                    }
+                }
+                if (group_sync_failed(1, 32 * n_soft, bad)) break;
+            }
+        }
+        if (tid == 0 && *fail) raise_error(a.err, ERR_WAIT_TIMEOUT);
+    }
+    __syncthreads();
+    if (warp == kIssueS) {
+        tc_fence_after();
+        tmem_dealloc(tmem, 512);
+    }
+}
+
+// Codes as bytes, boxes of one page of one head; rows of 128 bytes in the 128-byte swizzle.
+bool encode_codes(CUtensorMap *m, const void *base, const PagedArgs &a)
+{
+    PFN_cuTensorMapEncodeTiled_v12000 fn = encode_fn();
+    if (!fn) return false;
+    const cuuint64_t d = a.d, dims[4] = {d, (cuuint64_t)a.page_size, (cuuint64_t)a.Hkv, (cuuint64_t)a.n_pages};
+    const cuuint64_t strides[3] = {d, a.page_size * d, a.Hkv * a.page_size * d};
+    const cuuint32_t box[4] = {(cuuint32_t)d, (cuuint32_t)a.page_size, 1, 1}, es[4] = {1, 1, 1, 1};
+    return fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, const_cast<void *>(base), dims, strides, box, es,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, d == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE,
+              CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int D, int kCopies> cudaError_t launch(const PagedArgs &a, cudaStream_t st)
+{
+    TcArgs ta;
+    ta.p = a;
+    // pieces, codes, barriers, scales, exchange, stage (with copies), and 1 KB for alignment
+    const uint32_t pieces = 2 * kPieces * kPieceKeys * D * 2, slot = kTile * D;
+    const uint32_t tail = kBarBytes + kScaleBytes + kExchange + (kCopies > 1 ? kStage : 0) + 1024;
+    int ns = (int)((kSmemLimit - tail - pieces) / slot);
+    if (ns > kMaxSlots) ns = kMaxSlots;
+    ta.NK = ns / 2;
+    ta.NV = ns - ta.NK;
+    ta.off_bar = pieces + ns * slot;
+    ta.off_stage = ta.off_bar + kBarBytes + kScaleBytes + kExchange + 256;
+    ta.bytes = ta.off_bar + tail;
+    if (!encode_codes(&ta.tmK, a.K, a) || !encode_codes(&ta.tmV, a.V, a)) return cudaErrorInvalidValue;
+    static std::atomic<unsigned long long> opted{0};
+    const cudaError_t e = opt_in(reinterpret_cast<const void *>(&k_paged_attn_quant_tc<D, kCopies>), kSmemLimit, opted);
+    if (e != cudaSuccess) return e;
+    return pipe::launch_early(k_paged_attn_quant_tc<D, kCopies>, dim3(a.n_cta), dim3(kThreads), ta.bytes, st, ta);
+}
+
+template <int D> cudaError_t launch_rows(const PagedArgs &a, cudaStream_t st)
+{
+    // as many copies of the rows as fit in 128
+    const int rows = a.Bt * a.Gt;
+    if (rows <= 32) return launch<D, 4>(a, st);
+    return rows <= 64 ? launch<D, 2>(a, st) : launch<D, 1>(a, st);
+}
+
+}  // namespace
+
+cudaError_t launch_paged_attn_quant_tc(const PagedArgs &a, cudaStream_t st)
+{
+    return a.d == 128 ? launch_rows<128>(a, st) : launch_rows<64>(a, st);
+}
+
+}  // namespace hyb

@@ -69,32 +69,6 @@ struct TcArgs {
     uint32_t off_bar, off_stage, bytes;
 };
 
-// As wait_bar, but reads the timer only after some tries: its latency would delay
-// the common short wait.
-__device__ __forceinline__ bool wait_soon(uint64_t *bar, uint32_t parity, volatile int *fail)
-{
-    for (int i = 0; i < 32; ++i)
-        if (ptx::mbar_try_wait(bar, parity)) return true;
-    return wait_bar(bar, parity, fail);
-}
-
-// Position in a ring: slot and phase of the next item.
-struct RingPos {
-    uint32_t slot, phase;
-    __device__ void step(uint32_t n_slots)
-    {
-        if (++slot == n_slots) {
-            slot = 0;
-            phase ^= 1u;
-        }
-    }
-};
-
-__device__ __forceinline__ bool all_visible(const Visible &v, int j)
-{
-    return (j >= v.lo && j + kTile <= v.len) || j + kTile <= v.sink;
-}
-
 // kCopies: 4, 2 or 1 copies of the rows (at most 32, 64, 128 of them).
 template <int kCopies> struct Roles {
     static constexpr int kParts = kCopies == 1 ? 2 : 1;    // threads per row of a copy

@@ -64,6 +64,12 @@ __device__ __forceinline__ bool length_ok(const PagedArgs &a, int len)
 __device__ __forceinline__ int key_tile(const Visible &v, int i) { return i < v.ns ? i : v.first + (i - v.ns); }
 __device__ __forceinline__ bool key_visible(const Visible &v, int j) { return j < v.len && (j >= v.lo || j < v.sink); }
 
+// Whether every key of the tile from j is.
+__device__ __forceinline__ bool all_visible(const Visible &v, int j)
+{
+    return (j >= v.lo && j + kTile <= v.len) || j + kTile <= v.sink;
+}
+
 // Whether the n keys from j hold a visible one.
 __device__ __forceinline__ bool any_visible(const Visible &v, int j, int n)
 {

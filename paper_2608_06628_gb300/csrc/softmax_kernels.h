@@ -85,8 +85,9 @@ cudaError_t launch_paged_attn_few(const PagedArgs &a, cudaStream_t st);
 cudaError_t launch_paged_attn(hybrid_dtype dt, const PagedArgs &a, cudaStream_t st);
 // The join of a call whose attention kernel was launched just before.
 cudaError_t launch_paged_join(hybrid_dtype dt, const PagedArgs &a, cudaStream_t st);
-// paged_attn_quant.cu: the same over an 8-bit cache
+// The same over an 8-bit cache: paged_attn_quant.cu (float32, and few rows), paged_attn_quant_tc.cu
 void paged_quant_geometry(const hybrid_cfg &c, PagedArgs &a);
+cudaError_t launch_paged_attn_quant_tc(const PagedArgs &a, cudaStream_t st);     // without the join
 cudaError_t launch_paged_attn_quant(hybrid_dtype dt, const PagedArgs &a, cudaStream_t st);
 // Row tiles of at most `most` rows, of about equal size along the tokens.
 void paged_cut_rows(PagedArgs &a, int most);

@@ -52,6 +52,27 @@ __device__ __forceinline__ bool wait_bar(uint64_t *bar, uint32_t parity, volatil
     }
 }
 
+// As wait_bar, but reads the timer only after some tries: its latency would delay
+// the common short wait.
+__device__ __forceinline__ bool wait_soon(uint64_t *bar, uint32_t parity, volatile int *fail)
+{
+    for (int i = 0; i < 32; ++i)
+        if (ptx::mbar_try_wait(bar, parity)) return true;
+    return wait_bar(bar, parity, fail);
+}
+
+// Position in a ring: slot and phase of the next item.
+struct RingPos {
+    uint32_t slot, phase;
+    __device__ void step(uint32_t n_slots)
+    {
+        if (++slot == n_slots) {
+            slot = 0;
+            phase ^= 1u;
+        }
+    }
+};
+
 // Barrier over a group of warps that also ORs a failure flag across it, so
 // that every thread of the group takes the same branch afterwards.
 __device__ __forceinline__ bool group_sync_failed(uint32_t id, uint32_t nthreads, bool local_fail)
