@@ -73,8 +73,8 @@ __device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi)
 
 // Keys 16 v ... 16 v + 15 of a piece (64 keys from `codes` on) to half precision, by a warp.  A
 // group of 8 lanes has 64 features of two keys that differ in bits 0 and 2: neither its reads nor
-// its writes meet in a bank.  kMasked: `see` tells which keys are visible, others become zeros.
-template <int D, bool kMasked, typename See>
+// its writes meet in a bank.  Keys for which see() is false become zeros.
+template <int D, typename See>
 __device__ __forceinline__ void convert(const uint8_t *codes, uint8_t *piece, int v, int lane, See see)
 {
     constexpr int kHalves = D / 64;
@@ -90,7 +90,7 @@ __device__ __forceinline__ void convert(const uint8_t *codes, uint8_t *piece, in
 #pragma unroll
     for (int o = 0; o < 2; ++o) {
         const int key = 16 * v + 8 * o + octet;
-        const bool keep = !kMasked || see(key);
+        const bool keep = see(key);
 #pragma unroll
         for (int p = 0; p < kHalves; ++p) {
             const uint32_t w[4] = {x[o][p].x, x[o][p].y, x[o][p].z, x[o][p].w};
@@ -281,7 +281,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_quant_tc(const __gri
                 const int j0 = key_tile(w.vis, i) * kTile;
                 const bool edge = is_v && !all_visible(w.vis, j0);
                 ok = wait_soon(&my_full[pos.slot], pos.phase, fail);
-#pragma unroll
+#pragma unroll 1
                 for (int h = 0; h < 2; ++h) {
                     ok = ok && wait_soon(&free[to.slot], to.phase, fail);
                     if (__any_sync(0xffffffffu, !ok)) {
@@ -291,8 +291,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_quant_tc(const __gri
                     const uint8_t *codes = my_ring + (size_t)pos.slot * kCodes + h * kPieceKeys * D;
                     uint8_t *piece = my_piece + to.slot * kPiece;
                     const int j = j0 + h * kPieceKeys;
-                    if (edge) convert<D, true>(codes, piece, v, lane, [&](int key) { return key_visible(w.vis, j + key); });
-                    else convert<D, false>(codes, piece, v, lane, [](int) { return true; });
+                    convert<D>(codes, piece, v, lane, [&](int key) { return !edge || key_visible(w.vis, j + key); });
                     fence_proxy_async_smem();
                     __syncwarp();
                     if (lane == 0) {
@@ -319,6 +318,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_quant_tc(const __gri
                 for (int i = w.i0; ok && i < w.i1; ++i, ++n) {
                     const uint32_t b = n & 1;
                     ok = wait_soon(&pvdone[b], ((n >> 1) & 1u) ^ 1u, fail);     // P in S's buffer is multiplied
+#pragma unroll 1
                     for (int h = 0; ok && h < 2; ++h) {
                         ok = wait_soon(&kfull[pos.slot], pos.phase, fail);
                         if (!ok) break;
@@ -353,7 +353,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_quant_tc(const __gri
                 for (int i = w.i0; ok && i < w.i1; ++i, ++n) {
                     const uint32_t b = n & 1;
                     ok = wait_soon(&pready[b], (n >> 1) & 1u, fail);
-#pragma unroll
+#pragma unroll 1
                     for (int h = 0; h < 2; ++h) {
                         ok = ok && wait_soon(&vfull[pos.slot], pos.phase, fail);
                         if (!ok) break;
@@ -379,7 +379,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_quant_tc(const __gri
         // --------------------------------------------------- Q, softmax, epilogue
         constexpr int kKeys = kTile / kCopies;              // keys of a tile of this thread
         constexpr int kGroups = kKeys / 16;
-        constexpr bool kKeep = kKeys <= 64;                 // scores stay in registers between the passes
         const int copy = tid / kCopyRows, row = tid % kCopyRows, key0 = kKeys * copy;
         const uint32_t lane_off = (uint32_t)(32 * warp) << 16;
         const float to_log2 = kLog2e * rsqrtf((float)D);
@@ -406,15 +405,22 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_quant_tc(const __gri
 #pragma unroll
                 for (int x = 0; x < D / 8; ++x)
                     v[x] = live ? __ldg(reinterpret_cast<const uint4 *>(src) + x) : make_uint4(0, 0, 0, 0);
-                uint32_t top = 0;
+                uint32_t top2 = 0;                          // largest magnitudes of the even and the odd entries
+                auto larger = [](uint32_t p, uint32_t q) {
+                    const __nv_bfloat162 r = __hmax2(*reinterpret_cast<__nv_bfloat162 *>(&p), *reinterpret_cast<__nv_bfloat162 *>(&q));
+                    return *reinterpret_cast<const uint32_t *>(&r);
+                };
 #pragma unroll
-                for (int x = 0; x < D / 8; ++x) {
-                    const uint32_t q4[4] = {v[x].x, v[x].y, v[x].z, v[x].w};
-#pragma unroll
-                    for (int y = 0; y < 4; ++y) {
-                        const uint32_t lo = q4[y] & 0x7fffu, hi = q4[y] >> 16 & 0x7fffu;
-                        if (lo < 0x7f80u) top = max(top, lo);
-                        if (hi < 0x7f80u) top = max(top, hi);
+                for (int x = 0; x < D / 8; ++x)
+                    top2 = larger(top2, larger(larger(v[x].x & 0x7fff7fffu, v[x].y & 0x7fff7fffu),
+                                               larger(v[x].z & 0x7fff7fffu, v[x].w & 0x7fff7fffu)));
+                uint32_t top = max(top2 & 0xffffu, top2 >> 16);
+                if (top >= 0x7f80u) {                       // infinities are left out
+                    top = 0;
+#pragma unroll 1
+                    for (int x = 0; x < D; ++x) {
+                        const uint32_t q1 = __ldg(reinterpret_cast<const unsigned short *>(src) + x) & 0x7fffu;
+                        if (q1 < 0x7f80u) top = max(top, q1);
                     }
                 }
                 int e2 = (int)(top >> 7) - 127 - 14;        // the row over 2^e2 is below 2^15
@@ -443,41 +449,36 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_quant_tc(const __gri
                 const int j0 = key_tile(w.vis, i) * kTile;
                 const bool edge = !all_visible(w.vis, j0);
                 const int k0 = j0 + key0, hi = w.vis.len - k0, lo = w.vis.lo - k0, sink = w.vis.sink - k0;
-                auto seen = [&](int k) { return k < hi && (k >= lo || k < sink); };
+                auto below = [](int k) { return k >= 32 ? ~0u : (k <= 0 ? 0u : (1u << k) - 1); };
                 wait(&sready[b], (n >> 1) & 1u);
                 tc_fence_after();
                 const float *my_scales = scales + n % kScaleTiles * 16 + kGroups * copy;
-                float fk[kGroups], lv[kGroups];
-#pragma unroll
-                for (int g = 0; g < kGroups; ++g) {
-                    fk[g] = fminf(my_scales[g] * kc, kMax);
-                    lv[g] = lg2(my_scales[8 + g]);
-                }
                 const uint32_t my_s = tmem + cS + 128 * b + lane_off;
-                float s[kKeep ? kKeys / 32 : 1][32];
-                float mx = -INFINITY, my = -INFINITY;       // of x, of x + log2(vs)
-#pragma unroll
-                for (int x = 0; x < kKeys / 32; ++x) {
-                    float(&v)[32] = s[kKeep ? x : 0];
-                    tmem_ld32(my_s + key0 + 32 * x, v);
+                float s[32];                                // 32 keys at a time, twice: they fill the registers
+                // scores of keys 32 x ... from Tensor Memory, the masked ones replaced
+                auto scores = [&](int x) {
+                    tmem_ld32(my_s + key0 + 32 * x, s);
                     tmem_wait_ld();
+                    if (edge) {
+                        const unsigned see = below(hi - 32 * x) & (~below(lo - 32 * x) | below(sink - 32 * x));
+#pragma unroll
+                        for (int y = 0; y < 32; ++y) s[y] = see >> y & 1u ? s[y] : -INFINITY;
+                    }
+                };
+                // (bounded away from zero: it meets the infinities of masked scores)
+                auto factor = [&](int g) { return fminf(fmaxf(my_scales[g] * kc, 0x1p-126f), kMax); };
+                float mx = -INFINITY, my = -INFINITY;       // of x, of x + log2(vs)
+#pragma unroll 1
+                for (int x = 0; x < kKeys / 32; ++x) {
+                    scores(x);
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
-                        const int g = 2 * x + h;
-                        float top = -INFINITY;
-                        if (edge) {
+                        float t[2] = {s[16 * h], s[16 * h + 1]};
 #pragma unroll
-                            for (int y = 0; y < 16; ++y)
-                                if (seen(16 * g + y)) top = fmaxf(top, v[16 * h + y]);
-                        } else {
-                            float t[2] = {v[16 * h], v[16 * h + 1]};
-#pragma unroll
-                            for (int y = 2; y < 16; ++y) t[y & 1] = fmaxf(t[y & 1], v[16 * h + y]);
-                            top = fmaxf(t[0], t[1]);
-                        }
-                        top *= fk[g];                       // (NaN without a visible key)
+                        for (int y = 2; y < 16; ++y) t[y & 1] = fmaxf(t[y & 1], s[16 * h + y]);
+                        const float top = fmaxf(t[0], t[1]) * factor(2 * x + h);
                         mx = fmaxf(mx, top);
-                        my = fmaxf(my, top + lv[g]);
+                        my = fmaxf(my, top + lg2(my_scales[8 + 2 * x + h]));
                     }
                 }
                 float f = 1.f;
@@ -508,27 +509,18 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_quant_tc(const __gri
                 }
                 const float base = m == -INFINITY ? 0.f : m, to_o = base - (mo == -INFINITY ? 0.f : mo) + kTop;
                 const f32x2 base2 = pair2(-base, -base);
-#pragma unroll
+#pragma unroll 1
                 for (int x = 0; x < kKeys / 32; ++x) {
-                    float(&v)[32] = s[kKeep ? x : 0];
-                    if (!kKeep) {
-                        tmem_ld32(my_s + key0 + 32 * x, v);
-                        tmem_wait_ld();
-                    }
+                    if (kKeys > 32) scores(x);
                     float p[16];                            // pairs of half precision
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
-                        const int g = 2 * x + h;
-                        const float gain = ex2(fminf(lv[g] + to_o, 127.f));
-                        const f32x2 f2 = pair2(fk[g], fk[g]), gain2 = pair2(gain, gain);
+                        const float gain = ex2(fminf(lg2(my_scales[8 + 2 * x + h]) + to_o, 127.f)), fk = factor(2 * x + h);
+                        const f32x2 f2 = pair2(fk, fk), gain2 = pair2(gain, gain);
 #pragma unroll
                         for (int y = 0; y < 16; y += 2) {
                             float p0, p1;
-                            unpair2(fma2(pair2(v[16 * h + y], v[16 * h + y + 1]), f2, base2), p0, p1);
-                            if (edge) {
-                                if (!seen(16 * g + y)) p0 = -INFINITY;
-                                if (!seen(16 * g + y + 1)) p1 = -INFINITY;
-                            }
+                            unpair2(fma2(pair2(s[16 * h + y], s[16 * h + y + 1]), f2, base2), p0, p1);
                             const f32x2 pp = pair2(ex2(p0), ex2(p1));
                             l2 = add2(l2, pp);
                             unpair2(mul2(pp, gain2), p0, p1);

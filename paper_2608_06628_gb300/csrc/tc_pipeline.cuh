@@ -56,6 +56,7 @@ __device__ __forceinline__ bool wait_bar(uint64_t *bar, uint32_t parity, volatil
 // the common short wait.
 __device__ __forceinline__ bool wait_soon(uint64_t *bar, uint32_t parity, volatile int *fail)
 {
+#pragma unroll 1
     for (int i = 0; i < 32; ++i)
         if (ptx::mbar_try_wait(bar, parity)) return true;
     return wait_bar(bar, parity, fail);
