@@ -312,11 +312,11 @@ __global__ __launch_bounds__(kThreads, NT == 1 ? 2 : 1) void k_paged_attn_quant(
 #pragma unroll
                     for (int y = 0; y < 2; ++y) {
                         const float base = m[nt][y] == -INFINITY ? 0.f : m[nt][y], base_o = mo[nt][y] == -INFINITY ? 0.f : mo[nt][y];
-                        const float gain = pipe::ex2(fminf(lv + base - base_o + kTop, 127.f));
-                        const float p0 = pipe::ex2(x[nt][y] - base), p1 = pipe::ex2(x[nt][2 + y] - base);
-                        l[nt][y] += p0 + p1;
-                        pv[y] = p0 * gain;
-                        pv[2 + y] = p1 * gain;
+                        // P at once: l, from its sum.  (Below 2^-60 half precision has zeros, and float32 still has p.)
+                        const float gain = fminf(fmaxf(lv + base - base_o + kTop, -60.f), 126.f);
+                        pv[y] = pipe::ex2(x[nt][y] - base + gain);
+                        pv[2 + y] = pipe::ex2(x[nt][2 + y] - base + gain);
+                        l[nt][y] = fmaf(pv[y] + pv[2 + y], pipe::ex2(-gain), l[nt][y]);
                     }
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {

@@ -38,19 +38,20 @@ using namespace pipe;
 
 constexpr int kSmemLimit = 232448;
 constexpr int kMaxSlots = 12;
-constexpr int kPieces = 3;                // of K, and of V, in half precision
+constexpr int kTiles = 2;                 // of K in half precision
+constexpr int kPieces = 3;                // of V, of 64 keys
 constexpr int kPieceKeys = 64;
 constexpr int kScaleTiles = 32;           // tiles whose scales are held (see the producer)
 constexpr uint32_t kBarBytes = 1024;      // barriers, TMEM address, failure flag, the plan's scratch
 constexpr uint32_t kScaleBytes = kScaleTiles * 16 * 4;
-constexpr uint32_t kExchange = 1024;      // two floats a row
+constexpr uint32_t kExchange = 2048;      // two floats a thread of the softmax
 // with copies: 64 inverse sums, and 128 rows of 32 + 4 features (a quarter of the rows: 128 + 4)
 constexpr uint32_t kStage = 256 + 128 * 36 * 4;
 constexpr float kSlack = 8.f;             // log2 of how far a reference may be exceeded
 constexpr float kTop = 7.f;               // log2 of P at its reference
 constexpr float kMax = 3.402823466e38f;
-constexpr int kThreads = 512;
-enum Role { kSoft = 0, kConvertK = 4, kConvertV = 8, kLoadK = 12, kLoadV = 13, kIssueS = 14, kIssueO = 15 };
+constexpr int kThreads = 640;
+enum Role { kSoft = 0, kConvertK = 8, kConvertV = 12, kLoadK = 16, kLoadV = 17, kIssueS = 18, kIssueO = 19 };
 
 struct TcArgs {
     CUtensorMap tmK, tmV;
@@ -71,26 +72,39 @@ __device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi)
     return *reinterpret_cast<const uint32_t *>(&h);
 }
 
-// Keys 16 v ... 16 v + 15 of a piece (64 keys from `codes` on) to half precision, by a warp.  A
-// group of 8 lanes has 64 features of two keys that differ in bits 0 and 2: neither its reads nor
-// its writes meet in a bank.  Keys for which see() is false become zeros.
+__device__ __forceinline__ float max3(float x, float y, float z)
+{
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(x), "f"(y), "f"(z));
+    return r;
+}
+__device__ __forceinline__ void tmem_st8(uint32_t taddr, const float (&v)[8])
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr),
+                 "r"(__float_as_uint(v[0])), "r"(__float_as_uint(v[1])), "r"(__float_as_uint(v[2])), "r"(__float_as_uint(v[3])),
+                 "r"(__float_as_uint(v[4])), "r"(__float_as_uint(v[5])), "r"(__float_as_uint(v[6])), "r"(__float_as_uint(v[7]))
+                 : "memory");
+}
+
+// 16 keys from `codes` on to half precision, from row `row` (a multiple of 16) of an operand with
+// panels of `panel` bytes, by a warp.  A group of 8 lanes has 64 features of two keys that differ
+// in bits 0 and 2: neither its reads nor its writes meet in a bank.  Keys for which see() is false
+// become zeros.
 template <int D, typename See>
-__device__ __forceinline__ void convert(const uint8_t *codes, uint8_t *piece, int v, int lane, See see)
+__device__ __forceinline__ void convert(const uint8_t *codes, uint8_t *to, uint32_t panel, int lane, See see)
 {
     constexpr int kHalves = D / 64;
     const int c = lane & 3, octet = lane >> 3 ^ (lane & 4 ? 5 : 0);
     uint4 x[2][kHalves];
 #pragma unroll
     for (int o = 0; o < 2; ++o) {
-        const int key = 16 * v + 8 * o + octet;
 #pragma unroll
         for (int p = 0; p < kHalves; ++p)
-            x[o][p] = *reinterpret_cast<const uint4 *>(codes + key * D + (D == 128 ? ((4 * p + c) ^ octet) << 4 : c << 4));
+            x[o][p] = *reinterpret_cast<const uint4 *>(codes + (8 * o + octet) * D + (D == 128 ? ((4 * p + c) ^ octet) << 4 : c << 4));
     }
 #pragma unroll
     for (int o = 0; o < 2; ++o) {
-        const int key = 16 * v + 8 * o + octet;
-        const bool keep = see(key);
+        const bool keep = see(8 * o + octet);
 #pragma unroll
         for (int p = 0; p < kHalves; ++p) {
             const uint32_t w[4] = {x[o][p].x, x[o][p].y, x[o][p].z, x[o][p].w};
@@ -102,7 +116,7 @@ __device__ __forceinline__ void convert(const uint8_t *codes, uint8_t *piece, in
                 f[2 * i] = *reinterpret_cast<const uint32_t *>(&lo);
                 f[2 * i + 1] = *reinterpret_cast<const uint32_t *>(&hi);
             }
-            uint8_t *row = piece + p * (kPieceKeys * 128) + key * 128;
+            uint8_t *row = to + p * panel + (8 * o + octet) * 128;
             *reinterpret_cast<uint4 *>(row + ((2 * c ^ octet) << 4)) = make_uint4(f[0], f[1], f[2], f[3]);
             *reinterpret_cast<uint4 *>(row + (((2 * c + 1) ^ octet) << 4)) = make_uint4(f[4], f[5], f[6], f[7]);
         }
@@ -114,26 +128,27 @@ template <int D, int kCopies>
 __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_quant_tc(const __grid_constant__ TcArgs ta)
 {
     using namespace ptx;
-    constexpr int kHalves = D / 64;                        // 64-feature panels of a piece
-    constexpr uint32_t kPanel = kPieceKeys * 128;          // bytes of one panel
-    constexpr uint32_t kPiece = kHalves * kPanel, kCodes = kTile * D;
+    constexpr int kHalves = D / 64;                        // 64-feature panels of a tile of K, a piece of V
+    constexpr uint32_t kPanelK = kTile * 128, kPanelV = kPieceKeys * 128;      // bytes of one panel
+    constexpr uint32_t kTileK = kHalves * kPanelK, kPieceV = kHalves * kPanelV, kCodes = kTile * D;
     constexpr int kCopyRows = 128 / kCopies;
-    // Tensor Memory columns: S (2 x 128; then P in the first 64 of each), O, Q
+    // Tensor Memory columns: S (2 x 128; then P in the first 32 of each half), O, Q
     constexpr uint32_t cS = 0, cO = 256, cQ = 384;
     const PagedArgs &a = ta.p;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, NK = ta.NK, NV = ta.NV;
     const int rows = a.Bt * a.Gt;
-    const int n_soft = kCopies > 1 ? 4 : (rows + 31) / 32; // softmax warps at work
+    // quarters of the lanes with rows, softmax warps at work
+    const int n_quads = kCopies > 1 ? 4 : (rows + 31) / 32, n_soft = 2 * n_quads;
 
-    uint8_t *piece_k = smem, *piece_v = smem + kPieces * kPiece, *ring = smem + 2 * kPieces * kPiece;
+    uint8_t *tile_k = smem, *piece_v = smem + kTiles * kTileK, *ring = piece_v + kPieces * kPieceV;
     uint64_t *bars = reinterpret_cast<uint64_t *>(smem + ta.off_bar);
     uint64_t *full = bars;               // [NK + NV] the codes have landed
     uint64_t *empty = full + kMaxSlots;  // [NK + NV] they are converted
-    uint64_t *kfull = empty + kMaxSlots; // [3] a piece of K is in place
-    uint64_t *kempty = kfull + kPieces;  // [3] its products are done
-    uint64_t *vfull = kempty + kPieces;
+    uint64_t *kfull = empty + kMaxSlots; // [2] a tile of K is in place
+    uint64_t *kempty = kfull + kTiles;   // [2] its products are done
+    uint64_t *vfull = kempty + kTiles;   // [3] a piece of V
     uint64_t *vempty = vfull + kPieces;
     uint64_t *sready = vempty + kPieces; // [2] S is formed
     uint64_t *pready = sready + 2;       // [2] P is written (and O rescaled)
@@ -145,8 +160,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_quant_tc(const __gri
     volatile int *fail = reinterpret_cast<volatile int *>(tmem_holder + 1);
     PlanSmem *plan_smem = reinterpret_cast<PlanSmem *>(tmem_holder + 2);
     float *scales = reinterpret_cast<float *>(smem + ta.off_bar + kBarBytes);     // [kScaleTiles][8 of K, 8 of V]
-    float *exchange = scales + kScaleBytes / 4;            // [2][128]
-    float *inv_of = exchange + 256;                        // [64], with copies
+    float *exchange = scales + kScaleBytes / 4;            // [2][2][128]
+    float *inv_of = exchange + 512;                        // [64], with copies
 
     if (warp == kIssueS) {
         tmem_alloc(tmem_holder, 512);
@@ -159,9 +174,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_quant_tc(const __gri
             mbar_init(&full[i], i < NK ? 33 : 1);          // the producer's lanes for their scales, and the boxes
             mbar_init(&empty[i], 4);
         }
-        for (int i = 0; i < kPieces; ++i) {
+        for (int i = 0; i < kTiles; ++i) {
             mbar_init(&kfull[i], 4);
             mbar_init(&kempty[i], 1);
+        }
+        for (int i = 0; i < kPieces; ++i) {
             mbar_init(&vfull[i], 4);
             mbar_init(&vempty[i], 1);
         }
@@ -236,8 +253,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_quant_tc(const __gri
                     }
                     if (!is_v) {
                         // Zeros for groups without a visible key.  The place was that of 32 tiles ago, whose softmax
-                        // is done: the slot's last tile, at most 12 ago, is converted, so the products of the piece
-                        // 3 before it are done, and so is the softmax that freed their S, 3 tiles before that at most.
+                        // is done: the slot's last tile, at most 6 ago, is converted, so S of the second tile before
+                        // that one is formed, and that waited for the softmax of the second tile before it.
                         const int of = __shfl_sync(0xffffffffu, page, group >> lg);
                         const bool see = any_visible(w.vis, key_tile(w.vis, i) * kTile + group, 16);
                         if (lane < 16) {
@@ -272,8 +289,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_quant_tc(const __gri
         const int v = warp & 3;
         const uint32_t n_slots = is_v ? NV : NK;
         uint64_t *my_full = is_v ? full + NK : full, *my_empty = is_v ? empty + NK : empty;
-        uint64_t *done = is_v ? vfull : kfull, *free = is_v ? vempty : kempty;
-        uint8_t *my_ring = is_v ? ring + (size_t)NK * kCodes : ring, *my_piece = is_v ? piece_v : piece_k;
+        uint8_t *my_ring = is_v ? ring + (size_t)NK * kCodes : ring;
         RingPos pos{0, 0}, to{0, 1};
         bool ok = true;
         while (ok && w.next(a)) {
@@ -281,24 +297,29 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_quant_tc(const __gri
                 const int j0 = key_tile(w.vis, i) * kTile;
                 const bool edge = is_v && !all_visible(w.vis, j0);
                 ok = wait_soon(&my_full[pos.slot], pos.phase, fail);
+                const uint8_t *codes = my_ring + (size_t)pos.slot * kCodes;
+                // K: the warp has 32 keys of the tile; V: 16 of each of its two pieces
 #pragma unroll 1
                 for (int h = 0; h < 2; ++h) {
-                    ok = ok && wait_soon(&free[to.slot], to.phase, fail);
+                    uint64_t *free = is_v ? &vempty[to.slot] : &kempty[to.slot];
+                    if (is_v || h == 0) ok = ok && wait_soon(free, to.phase, fail);
                     if (__any_sync(0xffffffffu, !ok)) {
                         ok = false;
                         break;
                     }
-                    const uint8_t *codes = my_ring + (size_t)pos.slot * kCodes + h * kPieceKeys * D;
-                    uint8_t *piece = my_piece + to.slot * kPiece;
-                    const int j = j0 + h * kPieceKeys;
-                    convert<D>(codes, piece, v, lane, [&](int key) { return !edge || key_visible(w.vis, j + key); });
-                    fence_proxy_async_smem();
-                    __syncwarp();
-                    if (lane == 0) {
-                        mbar_arrive(&done[to.slot]);
-                        if (h == 1) mbar_arrive(&my_empty[pos.slot]);
+                    const int key = is_v ? kPieceKeys * h + 16 * v : 32 * v + 16 * h;
+                    uint8_t *row = is_v ? piece_v + to.slot * kPieceV + 16 * v * 128 : tile_k + to.slot * kTileK + key * 128;
+                    convert<D>(codes + key * D, row, is_v ? kPanelV : kPanelK, lane,
+                               [&](int x) { return !edge || key_visible(w.vis, j0 + key + x); });
+                    if (is_v || h == 1) {
+                        fence_proxy_async_smem();
+                        __syncwarp();
+                        if (lane == 0) {
+                            mbar_arrive(is_v ? &vfull[to.slot] : &kfull[to.slot]);
+                            if (h == 1) mbar_arrive(&my_empty[pos.slot]);
+                        }
+                        to.step(is_v ? kPieces : kTiles);
                     }
-                    to.step(kPieces);
                 }
                 if (!ok) break;
                 pos.step(n_slots);
@@ -307,31 +328,25 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_quant_tc(const __gri
     } else if (work && warp == kIssueS) {
         // --------------------------------------------- issuer of S = Q K^T
         if (lane == 0) {
-            const uint32_t id = instr_desc(FMT_F16, FMT_F16, false, false, 128, kPieceKeys);
-            const uint64_t k_desc = smem_desc(smem_u32(piece_k), 16, 1024, SWZ_128B);
+            const uint32_t id = instr_desc(FMT_F16, FMT_F16, false, false, 128, kTile);
+            const uint64_t k_desc = smem_desc(smem_u32(tile_k), 16, 1024, SWZ_128B);
             uint32_t n = 0, seg = 0;                       // tiles and segments so far
-            RingPos pos{0, 0};
             bool ok = true;
             while (ok && w.next(a)) {
                 ok = wait_soon(qready, seg & 1u, fail);
                 ++seg;
                 for (int i = w.i0; ok && i < w.i1; ++i, ++n) {
                     const uint32_t b = n & 1;
-                    ok = wait_soon(&pvdone[b], ((n >> 1) & 1u) ^ 1u, fail);     // P in S's buffer is multiplied
-#pragma unroll 1
-                    for (int h = 0; ok && h < 2; ++h) {
-                        ok = wait_soon(&kfull[pos.slot], pos.phase, fail);
-                        if (!ok) break;
-                        tc_fence_after();
-                        const uint64_t bk = k_desc + pos.slot * (kPiece >> 4);
+                    // P in S's buffer is multiplied, the tile is in place
+                    ok = wait_soon(&pvdone[b], ((n >> 1) & 1u) ^ 1u, fail) && wait_soon(&kfull[b], (n >> 1) & 1u, fail);
+                    if (!ok) break;
+                    tc_fence_after();
+                    const uint64_t bk = k_desc + b * (kTileK >> 4);
 #pragma unroll
-                        for (int k = 0; k < D / 16; ++k)
-                            mma_bf16_ts(tmem + cS + 128 * b + 64 * h, tmem + cQ + 8 * k, bk + (k >> 2) * (kPanel >> 4) + (k & 3) * 2, id,
-                                        k > 0);
-                        mma_commit(&kempty[pos.slot]);
-                        pos.step(kPieces);
-                    }
-                    if (ok) mma_commit(&sready[b]);
+                    for (int k = 0; k < D / 16; ++k)
+                        mma_bf16_ts(tmem + cS + 128 * b, tmem + cQ + 8 * k, bk + (k >> 2) * (kPanelK >> 4) + (k & 3) * 2, id, k > 0);
+                    mma_commit(&sready[b]);
+                    mma_commit(&kempty[b]);
                 }
             }
             mma_commit(&drained[0]);
@@ -341,7 +356,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_quant_tc(const __gri
         // ------------------------------------------------------ issuer of O += P V
         if (lane == 0) {
             const uint32_t id = instr_desc(FMT_F16, FMT_F16, false, true, 128, D);
-            const uint64_t v_desc = smem_desc(smem_u32(piece_v), kPanel, 1024, SWZ_128B);
+            const uint64_t v_desc = smem_desc(smem_u32(piece_v), kPanelV, 1024, SWZ_128B);
             constexpr int kOwn = kTile / 16 / kCopies;     // steps of 16 keys of a copy
             uint32_t n = 0, seg = 0;
             RingPos pos{0, 0};
@@ -358,11 +373,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_quant_tc(const __gri
                         ok = ok && wait_soon(&vfull[pos.slot], pos.phase, fail);
                         if (!ok) break;
                         tc_fence_after();
-                        const uint64_t bv = v_desc + pos.slot * (kPiece >> 4);
+                        const uint64_t bv = v_desc + pos.slot * (kPieceV >> 4);
 #pragma unroll
                         for (int x = 0; x < 4; ++x) {
                             const int g = 4 * h + x;
-                            const uint32_t from = tmem + cS + 128 * b + 8 * g, acc = i > w.i0 || g % kOwn > 0;
+                            const uint32_t from = tmem + cS + 128 * b + 64 * h + 8 * x, acc = i > w.i0 || g % kOwn > 0;
                             if constexpr (kCopies > 1) mma_bf16_ts_lanes(tmem + cO, from, bv + x * (2048 >> 4), id, acc, kCopies, g / kOwn);
                             else mma_bf16_ts(tmem + cO, from, bv + x * (2048 >> 4), id, acc);
                         }
@@ -375,14 +390,19 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_quant_tc(const __gri
             mma_commit(&drained[1]);
             mbar_wait(&drained[1], 0, kWaitNs);
         }
-    } else if (work && warp < n_soft) {
+    } else if (work && warp < kConvertK && (warp & 3) < n_quads) {
         // --------------------------------------------------- Q, softmax, epilogue
-        constexpr int kKeys = kTile / kCopies;              // keys of a tile of this thread
-        constexpr int kGroups = kKeys / 16;
-        const int copy = tid / kCopyRows, row = tid % kCopyRows, key0 = kKeys * copy;
-        const uint32_t lane_off = (uint32_t)(32 * warp) << 16;
+        // two threads to a lane of Tensor Memory: halves of its keys, and of the features
+        constexpr int kKeys = kTile / kCopies / 2;          // keys of a tile of this thread
+        constexpr int kSpan = kKeys < 32 ? kKeys : 32;      // of them at a time
+        constexpr int kFeat = D / 2;
+        const int quad = warp & 3, part = warp >> 2, at_lane = 32 * quad + lane;
+        const int copy = at_lane / kCopyRows, row = at_lane % kCopyRows, key0 = kKeys * (2 * copy + part);
+        const uint32_t lane_off = (uint32_t)(32 * quad) << 16;
+        const uint32_t pair_bar = 1 + quad;
         const float to_log2 = kLog2e * rsqrtf((float)D);
         float *stage = reinterpret_cast<float *>(smem + ta.off_stage);   // with copies
+        float *mine = exchange + 128 * part + at_lane, *others = exchange + 128 * (part ^ 1) + at_lane;
         uint32_t n = 0;                                     // tiles so far
         bool bad = false;                                   // a wait gave up: leave at the next vote
         auto wait = [&](uint64_t *bar, uint32_t parity) {
@@ -400,10 +420,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_quant_tc(const __gri
             const bool live = row_at(a, w.req, u, row, at), whole = w.whole();
             float kc;                                       // log2(e) / sqrt(d) over the row's factor
             {   // Q.  (The last segment's products with it are done: its last S has been read.)
-                const bf16 *src = static_cast<const bf16 *>(a.Q) + at;
-                uint4 v[D / 8];
+                const bf16 *src = static_cast<const bf16 *>(a.Q) + at + kFeat * part;
+                uint4 v[kFeat / 8];
 #pragma unroll
-                for (int x = 0; x < D / 8; ++x)
+                for (int x = 0; x < kFeat / 8; ++x)
                     v[x] = live ? __ldg(reinterpret_cast<const uint4 *>(src) + x) : make_uint4(0, 0, 0, 0);
                 uint32_t top2 = 0;                          // largest magnitudes of the even and the odd entries
                 auto larger = [](uint32_t p, uint32_t q) {
@@ -411,25 +431,28 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_quant_tc(const __gri
                     return *reinterpret_cast<const uint32_t *>(&r);
                 };
 #pragma unroll
-                for (int x = 0; x < D / 8; ++x)
+                for (int x = 0; x < kFeat / 8; ++x)
                     top2 = larger(top2, larger(larger(v[x].x & 0x7fff7fffu, v[x].y & 0x7fff7fffu),
                                                larger(v[x].z & 0x7fff7fffu, v[x].w & 0x7fff7fffu)));
                 uint32_t top = max(top2 & 0xffffu, top2 >> 16);
                 if (top >= 0x7f80u) {                       // infinities are left out
                     top = 0;
 #pragma unroll 1
-                    for (int x = 0; x < D; ++x) {
+                    for (int x = 0; x < kFeat; ++x) {
                         const uint32_t q1 = __ldg(reinterpret_cast<const unsigned short *>(src) + x) & 0x7fffu;
                         if (q1 < 0x7f80u) top = max(top, q1);
                     }
                 }
+                *mine = __uint_as_float(top);
+                group_sync_failed(pair_bar, 64, false);
+                top = max(top, __float_as_uint(*others));
                 int e2 = (int)(top >> 7) - 127 - 14;        // the row over 2^e2 is below 2^15
                 if (e2 < -126) e2 = -126;
                 const float over = __uint_as_float((uint32_t)(127 - e2) << 23);
                 kc = __uint_as_float((uint32_t)(127 + e2) << 23) * to_log2;
                 tc_fence_after();
 #pragma unroll
-                for (int x = 0; x < D / 32; ++x) {
+                for (int x = 0; x < kFeat / 32; ++x) {
                     float f[16];
 #pragma unroll
                     for (int y = 0; y < 16; ++y) {
@@ -437,13 +460,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_quant_tc(const __gri
                         const uint32_t q2 = y % 4 == 0 ? q4.x : (y % 4 == 1 ? q4.y : (y % 4 == 2 ? q4.z : q4.w));
                         f[y] = __uint_as_float(pack_f16x2(__uint_as_float(q2 << 16) * over, __uint_as_float(q2 & 0xffff0000u) * over));
                     }
-                    tmem_st16(tmem + cQ + 16 * x + lane_off, f);
+                    tmem_st16(tmem + cQ + kFeat / 2 * part + 16 * x + lane_off, f);
                 }
                 tmem_wait_st();
                 arrive(qready);
             }
-            float m = -INFINITY, mo = -INFINITY;            // references of l and of O
-            f32x2 l2 = pair2(0.f, 0.f);                     // the row's sum over this thread's keys, in two
+            float m = -INFINITY, mo = -INFINITY;            // references of l (this thread's), and of O (the row's)
+            float l = 0.f;                                  // sum over this thread's keys
             for (int i = w.i0; i < w.i1; ++i, ++n) {
                 const uint32_t b = n & 1;
                 const int j0 = key_tile(w.vis, i) * kTile;
@@ -452,111 +475,127 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_quant_tc(const __gri
                 auto below = [](int k) { return k >= 32 ? ~0u : (k <= 0 ? 0u : (1u << k) - 1); };
                 wait(&sready[b], (n >> 1) & 1u);
                 tc_fence_after();
-                const float *my_scales = scales + n % kScaleTiles * 16 + kGroups * copy;
+                const float *my_scales = scales + n % kScaleTiles * 16 + key0 / 16;
                 const uint32_t my_s = tmem + cS + 128 * b + lane_off;
-                float s[32];                                // 32 keys at a time, twice: they fill the registers
-                // scores of keys 32 x ... from Tensor Memory, the masked ones replaced
+                // P lies in the half of S that its keys have: where it meets scores of the lane's other thread, they have
+                // been read before the vote below, and those of its own that are read twice lie ahead of it
+                const uint32_t my_p = my_s + key0 / 64 * 64 + key0 % 64 / 2;
+                float s[kSpan];
+                // scores of keys kSpan x ... from Tensor Memory, the masked ones replaced
                 auto scores = [&](int x) {
-                    tmem_ld32(my_s + key0 + 32 * x, s);
+                    if constexpr (kSpan == 32) tmem_ld32(my_s + key0 + 32 * x, s);
+                    else tmem_ld16(my_s + key0, s);
                     tmem_wait_ld();
                     if (edge) {
                         const unsigned see = below(hi - 32 * x) & (~below(lo - 32 * x) | below(sink - 32 * x));
 #pragma unroll
-                        for (int y = 0; y < 32; ++y) s[y] = see >> y & 1u ? s[y] : -INFINITY;
+                        for (int y = 0; y < kSpan; ++y) s[y] = see >> y & 1u ? s[y] : -INFINITY;
                     }
                 };
                 // (bounded away from zero: it meets the infinities of masked scores)
                 auto factor = [&](int g) { return fminf(fmaxf(my_scales[g] * kc, 0x1p-126f), kMax); };
                 float mx = -INFINITY, my = -INFINITY;       // of x, of x + log2(vs)
 #pragma unroll 1
-                for (int x = 0; x < kKeys / 32; ++x) {
+                for (int x = 0; x < kKeys / kSpan; ++x) {
                     scores(x);
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        float t[2] = {s[16 * h], s[16 * h + 1]};
+                    for (int h = 0; h < kSpan / 16; ++h) {
+                        float t = max3(s[16 * h], s[16 * h + 1], s[16 * h + 2]), t2 = max3(s[16 * h + 3], s[16 * h + 4], s[16 * h + 5]);
 #pragma unroll
-                        for (int y = 2; y < 16; ++y) t[y & 1] = fmaxf(t[y & 1], s[16 * h + y]);
-                        const float top = fmaxf(t[0], t[1]) * factor(2 * x + h);
+                        for (int y = 6; y < 14; y += 4) {
+                            t = max3(t, s[16 * h + y], s[16 * h + y + 1]);
+                            t2 = max3(t2, s[16 * h + y + 2], s[16 * h + y + 3]);
+                        }
+                        t = max3(t, s[16 * h + 14], s[16 * h + 15]);
+                        const float top = fmaxf(t, t2) * factor(2 * x + h);
                         mx = fmaxf(mx, top);
                         my = fmaxf(my, top + lg2(my_scales[8 + 2 * x + h]));
                     }
                 }
-                float f = 1.f;
                 if (mx > m + kSlack) {                      // from -inf: whenever a key is visible
-                    if (m != -INFINITY) {                   // (else the sum is zero)
-                        const float fl = ex2(m - mx);
-                        l2 = mul2(l2, pair2(fl, fl));
-                    }
+                    if (m != -INFINITY) l *= ex2(m - mx);   // (else it is zero)
                     m = mx;
                 }
-                if (my > mo + kSlack) {
-                    if (mo != -INFINITY) f = ex2(mo - my);
-                    mo = my;
-                }
-                // O is at rest once earlier products are done
-                if (__any_sync(0xffffffffu, f != 1.f && row < rows)) {
-                    wait(&pvdone[(n - 1) & 1], ((n - 1) >> 1) & 1u);
-                    tc_fence_after();
+                // the row's threads move its reference together
+                if (group_sync_failed(pair_bar, 64, my > mo + kSlack && row < rows)) {
+                    *mine = my;
+                    group_sync_failed(pair_bar, 64, false);
+                    my = fmaxf(my, *others);
+                    float f = 1.f;
+                    if (my > mo + kSlack) {
+                        if (mo != -INFINITY) f = ex2(mo - my);
+                        mo = my;
+                    }
+                    if (__any_sync(0xffffffffu, f != 1.f && row < rows)) {
+                        wait(&pvdone[(n - 1) & 1], ((n - 1) >> 1) & 1u);       // O is at rest
+                        tc_fence_after();
 #pragma unroll 1
-                    for (int x = 0; x < D / 16; ++x) {
-                        float o[16];
-                        tmem_ld16(tmem + cO + 16 * x + lane_off, o);
-                        tmem_wait_ld();
+                        for (int x = 0; x < kFeat / 32; ++x) {
+                            float o[32];
+                            tmem_ld32(tmem + cO + kFeat * part + 32 * x + lane_off, o);
+                            tmem_wait_ld();
 #pragma unroll
-                        for (int y = 0; y < 16; ++y) o[y] *= f;
-                        tmem_st16(tmem + cO + 16 * x + lane_off, o);
+                            for (int y = 0; y < 32; ++y) o[y] *= f;
+                            tmem_st32(tmem + cO + kFeat * part + 32 * x + lane_off, o);
+                        }
                     }
                 }
                 const float base = m == -INFINITY ? 0.f : m, to_o = base - (mo == -INFINITY ? 0.f : mo) + kTop;
-                const f32x2 base2 = pair2(-base, -base);
 #pragma unroll 1
-                for (int x = 0; x < kKeys / 32; ++x) {
-                    if (kKeys > 32) scores(x);
-                    float p[16];                            // pairs of half precision
+                for (int x = 0; x < kKeys / kSpan; ++x) {
+                    if (kKeys > kSpan) scores(x);
+                    float p[kSpan / 2];                     // pairs of half precision
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const float gain = ex2(fminf(lg2(my_scales[8 + 2 * x + h]) + to_o, 127.f)), fk = factor(2 * x + h);
-                        const f32x2 f2 = pair2(fk, fk), gain2 = pair2(gain, gain);
+                    for (int h = 0; h < kSpan / 16; ++h) {
+                        // P at once: l, from its sum.  (Below 2^-60 half precision has zeros, and float32 still has p.)
+                        const float gain = fminf(fmaxf(lg2(my_scales[8 + 2 * x + h]) + to_o, -60.f), 126.f), fk = factor(2 * x + h);
+                        const f32x2 f2 = pair2(fk, fk), add = pair2(gain - base, gain - base);
+                        f32x2 sum[4];                       // (one alone would be a chain of latencies)
 #pragma unroll
-                        for (int y = 0; y < 16; y += 2) {
+                        for (int y = 0; y < 8; ++y) {
                             float p0, p1;
-                            unpair2(fma2(pair2(s[16 * h + y], s[16 * h + y + 1]), f2, base2), p0, p1);
-                            const f32x2 pp = pair2(ex2(p0), ex2(p1));
-                            l2 = add2(l2, pp);
-                            unpair2(mul2(pp, gain2), p0, p1);
-                            p[8 * h + y / 2] = __uint_as_float(pack_f16x2(p0, p1));
+                            unpair2(fma2(pair2(s[16 * h + 2 * y], s[16 * h + 2 * y + 1]), f2, add), p0, p1);
+                            p0 = ex2(p0);
+                            p1 = ex2(p1);
+                            sum[y & 3] = y < 4 ? pair2(p0, p1) : add2(sum[y & 3], pair2(p0, p1));
+                            p[8 * h + y] = __uint_as_float(pack_f16x2(p0, p1));
                         }
+                        float p0, p1;
+                        unpair2(add2(add2(sum[0], sum[1]), add2(sum[2], sum[3])), p0, p1);
+                        l = fmaf(p0 + p1, ex2(-gain), l);
                     }
-                    tmem_st16(my_s + key0 / 2 + 16 * x, p);
+                    if constexpr (kSpan == 32) tmem_st16(my_p + 16 * x, p);
+                    else tmem_st8(my_p, p);
                 }
                 tmem_wait_st();
                 arrive(&pready[b]);
             }
-            // the segment's output
+            // the segment's output: reference and sum of the row over its threads
             bf16 *out = static_cast<bf16 *>(a.O) + at;
             float *partial = a.part + w.slot() * partial_floats(rows, D);
-            float l, l_odd;
-            unpair2(l2, l, l_odd);
-            l += l_odd;
-            if (kCopies > 1) {
-                // reference and sum of the row over its copies
-                exchange[tid] = m;
-                exchange[128 + tid] = l;
-                if (group_sync_failed(1, 128, bad)) break;
-                m = exchange[row];
+            *mine = m;
+            mine[256] = l;
+            if (group_sync_failed(kCopies > 1 ? 5 : pair_bar, kCopies > 1 ? 256 : 64, bad)) break;
+            {
+                float top = -INFINITY, sum = 0.f;
 #pragma unroll
-                for (int c = 1; c < kCopies; ++c) m = fmaxf(m, exchange[c * kCopyRows + row]);
-                const float base = m == -INFINITY ? 0.f : m;
-                l = 0.f;
+                for (int c = 0; c < 2 * kCopies; ++c) top = fmaxf(top, exchange[(c & 1) * 128 + (c >> 1) * kCopyRows + row]);
+                m = top;
+                if (top == -INFINITY) top = 0.f;
 #pragma unroll
-                for (int c = 0; c < kCopies; ++c)
-                    l = fmaf(exchange[128 + c * kCopyRows + row], ex2(exchange[c * kCopyRows + row] - base), l);
-                if (copy == 0) inv_of[row] = 1.f / l;               // read after the next barrier
+                for (int c = 0; c < 2 * kCopies; ++c) {
+                    const float *e = exchange + (c & 1) * 128 + (c >> 1) * kCopyRows + row;
+                    sum = fmaf(e[256], ex2(e[0] - top), sum);
+                }
+                l = sum;
             }
             const float f = ex2(mo - kTop - (m == -INFINITY ? 0.f : m));    // O relative to m
-            if (!whole && row < rows && copy == 0) {
-                partial[row] = m;
-                partial[rows + row] = l;
+            if (part == 0 && copy == 0 && row < rows) {
+                if (kCopies > 1) inv_of[row] = 1.f / l;                     // read after the next barrier
+                if (!whole) {
+                    partial[row] = m;
+                    partial[rows + row] = l;
+                }
             }
             wait(&pvdone[(n - 1) & 1], ((n - 1) >> 1) & 1u);
             tc_fence_after();
@@ -567,25 +606,25 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_quant_tc(const __gri
                 const int span = width < D ? width : D, pitch = span + 4;
 #pragma unroll 1
                 for (int x0 = 0; x0 < D; x0 += span) {
-                    float *mine = stage + (copy * rows + row) * pitch;
+                    float *to = stage + (copy * rows + row) * pitch;
 #pragma unroll 1
-                    for (int x = 0; x < span; x += 32) {
-                        float o[32];
-                        tmem_ld32(tmem + cO + x0 + x + lane_off, o);
+                    for (int x = 16 * part; x < span; x += 32) {
+                        float o[16];
+                        tmem_ld16(tmem + cO + x0 + x + lane_off, o);
                         tmem_wait_ld();
                         if (row < rows) {
 #pragma unroll
-                            for (int y = 0; y < 32; y += 4)
-                                *reinterpret_cast<float4 *>(mine + x + y) =
+                            for (int y = 0; y < 16; y += 4)
+                                *reinterpret_cast<float4 *>(to + x + y) =
                                     f != 0.f ? make_float4(o[y] * f, o[y + 1] * f, o[y + 2] * f, o[y + 3] * f)
                                              : make_float4(0.f, 0.f, 0.f, 0.f);
                         }
                     }
                     if (x0 + span == D) arrive(ofree);
-                    group_sync_failed(1, 128, false);
+                    group_sync_failed(5, 256, false);
                     if (!bad) {
                         if (whole) {                       // eight features of a row
-                            for (int x = tid; x < rows * (span / 8); x += 128) {
+                            for (int x = tid; x < rows * (span / 8); x += 256) {
                                 const int r = x / (span / 8), col = x % (span / 8) * 8;
                                 const float *src = stage + r * pitch + col;
                                 float4 v0 = make_float4(0.f, 0.f, 0.f, 0.f), v1 = v0;
@@ -597,14 +636,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_quant_tc(const __gri
                                     v1 = make_float4(v1.x + s1.x, v1.y + s1.y, v1.z + s1.z, v1.w + s1.w);
                                 }
                                 const float k = inv_of[r];
-                                size_t to;
-                                if (row_at(a, w.req, u, r, to))
-                                    *reinterpret_cast<uint4 *>(static_cast<bf16 *>(a.O) + to + x0 + col) = make_uint4(
+                                size_t dst;
+                                if (row_at(a, w.req, u, r, dst))
+                                    *reinterpret_cast<uint4 *>(static_cast<bf16 *>(a.O) + dst + x0 + col) = make_uint4(
                                         pack_bf16x2(v0.x * k, v0.y * k), pack_bf16x2(v0.z * k, v0.w * k),
                                         pack_bf16x2(v1.x * k, v1.y * k), pack_bf16x2(v1.z * k, v1.w * k));
                             }
                         } else {                           // feature-major, as the join reads it
-                            for (int x = tid; x < rows * span; x += 128) {
+                            for (int x = tid; x < rows * span; x += 256) {
                                 const int r = x % rows, col = x / rows;
                                 float v = 0.f;
 #pragma unroll
@@ -613,16 +652,17 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_quant_tc(const __gri
                             }
                         }
                     }
-                    group_sync_failed(1, 128, false);
+                    group_sync_failed(5, 256, false);
                 }
             } else {
                 const float k = whole ? f / l : f;
 #pragma unroll 1
-                for (int x = 0; x < D / 32; ++x) {
+                for (int x = 0; x < kFeat / 32; ++x) {
+                    const int col = kFeat * part + 32 * x;
                     float o[32];
-                    tmem_ld32(tmem + cO + 32 * x + lane_off, o);
+                    tmem_ld32(tmem + cO + col + lane_off, o);
                     tmem_wait_ld();
-                    if (x == D / 32 - 1) arrive(ofree);
+                    if (x == kFeat / 32 - 1) arrive(ofree);
                     if (bad) continue;
 #pragma unroll
                     for (int y = 0; y < 32; ++y) o[y] *= k;
@@ -630,17 +670,17 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_quant_tc(const __gri
                         if (live) {
 #pragma unroll
                             for (int y = 0; y < 32; y += 8)
-                                *reinterpret_cast<uint4 *>(out + 32 * x + y) =
+                                *reinterpret_cast<uint4 *>(out + col + y) =
                                     make_uint4(pack_bf16x2(o[y], o[y + 1]), pack_bf16x2(o[y + 2], o[y + 3]),
                                                pack_bf16x2(o[y + 4], o[y + 5]), pack_bf16x2(o[y + 6], o[y + 7]));
                         }
                     } else if (row < rows) {
-                        float *po = partial + 2 * rows + (size_t)(32 * x) * rows + row;
+                        float *po = partial + 2 * rows + (size_t)col * rows + row;
 #pragma unroll
                         for (int y = 0; y < 32; ++y) po[(size_t)y * rows] = o[y];
                     }
                 }
-                if (group_sync_failed(1, 32 * n_soft, bad)) break;
+                group_sync_failed(pair_bar, 64, false);     // the exchange has been read
             }
         }
         if (tid == 0 && *fail) raise_error(a.err, ERR_WAIT_TIMEOUT);
@@ -670,7 +710,7 @@ template <int D, int kCopies> cudaError_t launch(const PagedArgs &a, cudaStream_
     TcArgs ta;
     ta.p = a;
     // pieces, codes, barriers, scales, exchange, stage (with copies), and 1 KB for alignment
-    const uint32_t pieces = 2 * kPieces * kPieceKeys * D * 2, slot = kTile * D;
+    const uint32_t pieces = (kTiles * kTile + kPieces * kPieceKeys) * D * 2, slot = kTile * D;
     const uint32_t tail = kBarBytes + kScaleBytes + kExchange + (kCopies > 1 ? kStage : 0) + 1024;
     int ns = (int)((kSmemLimit - tail - pieces) / slot);
     if (ns > kMaxSlots) ns = kMaxSlots;
