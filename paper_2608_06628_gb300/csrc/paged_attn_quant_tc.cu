@@ -38,9 +38,7 @@ using namespace pipe;
 
 constexpr int kSmemLimit = 232448;
 constexpr int kMaxSlots = 12;
-constexpr int kTiles = 2;                 // of K in half precision
-constexpr int kPieces = 3;                // of V, of 64 keys
-constexpr int kPieceKeys = 64;
+constexpr int kTiles = 2;                 // of K, and of V, in half precision
 constexpr int kScaleTiles = 32;           // tiles whose scales are held (see the producer)
 constexpr uint32_t kBarBytes = 1024;      // barriers, TMEM address, failure flag, the plan's scratch
 constexpr uint32_t kScaleBytes = kScaleTiles * 16 * 4;
@@ -128,9 +126,8 @@ template <int D, int kCopies>
 __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_quant_tc(const __grid_constant__ TcArgs ta)
 {
     using namespace ptx;
-    constexpr int kHalves = D / 64;                        // 64-feature panels of a tile of K, a piece of V
-    constexpr uint32_t kPanelK = kTile * 128, kPanelV = kPieceKeys * 128;      // bytes of one panel
-    constexpr uint32_t kTileK = kHalves * kPanelK, kPieceV = kHalves * kPanelV, kCodes = kTile * D;
+    constexpr uint32_t kPanel = kTile * 128;               // bytes of 64 features of a tile
+    constexpr uint32_t kHalf = D / 64 * kPanel, kCodes = kTile * D;            // of a tile in half precision, and of its codes
     constexpr int kCopyRows = 128 / kCopies;
     // Tensor Memory columns: S (2 x 128; then P in the first 32 of each half), O, Q
     constexpr uint32_t cS = 0, cO = 256, cQ = 384;
@@ -142,15 +139,15 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_quant_tc(const __gri
     // quarters of the lanes with rows, softmax warps at work
     const int n_quads = kCopies > 1 ? 4 : (rows + 31) / 32, n_soft = 2 * n_quads;
 
-    uint8_t *tile_k = smem, *piece_v = smem + kTiles * kTileK, *ring = piece_v + kPieces * kPieceV;
+    uint8_t *tile_k = smem, *tile_v = smem + kTiles * kHalf, *ring = tile_v + kTiles * kHalf;
     uint64_t *bars = reinterpret_cast<uint64_t *>(smem + ta.off_bar);
     uint64_t *full = bars;               // [NK + NV] the codes have landed
     uint64_t *empty = full + kMaxSlots;  // [NK + NV] they are converted
     uint64_t *kfull = empty + kMaxSlots; // [2] a tile of K is in place
     uint64_t *kempty = kfull + kTiles;   // [2] its products are done
-    uint64_t *vfull = kempty + kTiles;   // [3] a piece of V
-    uint64_t *vempty = vfull + kPieces;
-    uint64_t *sready = vempty + kPieces; // [2] S is formed
+    uint64_t *vfull = kempty + kTiles;
+    uint64_t *vempty = vfull + kTiles;
+    uint64_t *sready = vempty + kTiles;  // [2] S is formed
     uint64_t *pready = sready + 2;       // [2] P is written (and O rescaled)
     uint64_t *pvdone = pready + 2;       // [2] O includes the tile's P V
     uint64_t *qready = pvdone + 2;       // the segment's Q is in place
@@ -177,8 +174,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_quant_tc(const __gri
         for (int i = 0; i < kTiles; ++i) {
             mbar_init(&kfull[i], 4);
             mbar_init(&kempty[i], 1);
-        }
-        for (int i = 0; i < kPieces; ++i) {
             mbar_init(&vfull[i], 4);
             mbar_init(&vempty[i], 1);
         }
@@ -298,30 +293,21 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_quant_tc(const __gri
                 const bool edge = is_v && !all_visible(w.vis, j0);
                 ok = wait_soon(&my_full[pos.slot], pos.phase, fail);
                 const uint8_t *codes = my_ring + (size_t)pos.slot * kCodes;
-                // K: the warp has 32 keys of the tile; V: 16 of each of its two pieces
-#pragma unroll 1
-                for (int h = 0; h < 2; ++h) {
-                    uint64_t *free = is_v ? &vempty[to.slot] : &kempty[to.slot];
-                    if (is_v || h == 0) ok = ok && wait_soon(free, to.phase, fail);
-                    if (__any_sync(0xffffffffu, !ok)) {
-                        ok = false;
-                        break;
-                    }
-                    const int key = is_v ? kPieceKeys * h + 16 * v : 32 * v + 16 * h;
-                    uint8_t *row = is_v ? piece_v + to.slot * kPieceV + 16 * v * 128 : tile_k + to.slot * kTileK + key * 128;
-                    convert<D>(codes + key * D, row, is_v ? kPanelV : kPanelK, lane,
-                               [&](int x) { return !edge || key_visible(w.vis, j0 + key + x); });
-                    if (is_v || h == 1) {
-                        fence_proxy_async_smem();
-                        __syncwarp();
-                        if (lane == 0) {
-                            mbar_arrive(is_v ? &vfull[to.slot] : &kfull[to.slot]);
-                            if (h == 1) mbar_arrive(&my_empty[pos.slot]);
-                        }
-                        to.step(is_v ? kPieces : kTiles);
-                    }
-                }
+                ok = ok && wait_soon(is_v ? &vempty[to.slot] : &kempty[to.slot], to.phase, fail);
+                if (__any_sync(0xffffffffu, !ok)) ok = false;
                 if (!ok) break;
+                uint8_t *rows_of = (is_v ? tile_v : tile_k) + to.slot * kHalf;
+#pragma unroll 1
+                for (int key = 32 * v; key < 32 * v + 32; key += 16)
+                    convert<D>(codes + key * D, rows_of + key * 128, kPanel, lane,
+                               [&](int x) { return !edge || key_visible(w.vis, j0 + key + x); });
+                fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) {
+                    mbar_arrive(is_v ? &vfull[to.slot] : &kfull[to.slot]);
+                    mbar_arrive(&my_empty[pos.slot]);
+                }
+                to.step(kTiles);
                 pos.step(n_slots);
             }
         }
@@ -341,10 +327,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_quant_tc(const __gri
                     ok = wait_soon(&pvdone[b], ((n >> 1) & 1u) ^ 1u, fail) && wait_soon(&kfull[b], (n >> 1) & 1u, fail);
                     if (!ok) break;
                     tc_fence_after();
-                    const uint64_t bk = k_desc + b * (kTileK >> 4);
+                    const uint64_t bk = k_desc + b * (kHalf >> 4);
 #pragma unroll
                     for (int k = 0; k < D / 16; ++k)
-                        mma_bf16_ts(tmem + cS + 128 * b, tmem + cQ + 8 * k, bk + (k >> 2) * (kPanelK >> 4) + (k & 3) * 2, id, k > 0);
+                        mma_bf16_ts(tmem + cS + 128 * b, tmem + cQ + 8 * k, bk + (k >> 2) * (kPanel >> 4) + (k & 3) * 2, id, k > 0);
                     mma_commit(&sready[b]);
                     mma_commit(&kempty[b]);
                 }
@@ -356,35 +342,30 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_quant_tc(const __gri
         // ------------------------------------------------------ issuer of O += P V
         if (lane == 0) {
             const uint32_t id = instr_desc(FMT_F16, FMT_F16, false, true, 128, D);
-            const uint64_t v_desc = smem_desc(smem_u32(piece_v), kPanelV, 1024, SWZ_128B);
+            const uint64_t v_desc = smem_desc(smem_u32(tile_v), kPanel, 1024, SWZ_128B);
             constexpr int kOwn = kTile / 16 / kCopies;     // steps of 16 keys of a copy
             uint32_t n = 0, seg = 0;
-            RingPos pos{0, 0};
             bool ok = true;
             while (ok && w.next(a)) {
                 // O is overwritten by a segment's first product: the last epilogue has read it
                 if (seg > 0) ok = wait_soon(ofree, (seg - 1) & 1u, fail);
                 ++seg;
                 for (int i = w.i0; ok && i < w.i1; ++i, ++n) {
-                    const uint32_t b = n & 1;
-                    ok = wait_soon(&pready[b], (n >> 1) & 1u, fail);
-#pragma unroll 1
-                    for (int h = 0; h < 2; ++h) {
-                        ok = ok && wait_soon(&vfull[pos.slot], pos.phase, fail);
-                        if (!ok) break;
-                        tc_fence_after();
-                        const uint64_t bv = v_desc + pos.slot * (kPieceV >> 4);
+                    const uint32_t b = n & 1, first = i > w.i0;
+                    ok = wait_soon(&vfull[b], (n >> 1) & 1u, fail) && wait_soon(&pready[b], (n >> 1) & 1u, fail);
+                    if (!ok) break;
+                    tc_fence_after();
+                    const uint64_t bv = v_desc + b * (kHalf >> 4);
+                    const uint32_t from = tmem + cS + 128 * b;
 #pragma unroll
-                        for (int x = 0; x < 4; ++x) {
-                            const int g = 4 * h + x;
-                            const uint32_t from = tmem + cS + 128 * b + 64 * h + 8 * x, acc = i > w.i0 || g % kOwn > 0;
-                            if constexpr (kCopies > 1) mma_bf16_ts_lanes(tmem + cO, from, bv + x * (2048 >> 4), id, acc, kCopies, g / kOwn);
-                            else mma_bf16_ts(tmem + cO, from, bv + x * (2048 >> 4), id, acc);
-                        }
-                        mma_commit(&vempty[pos.slot]);
-                        pos.step(kPieces);
+                    for (int g = 0; g < kTile / 16; ++g) {
+                        const uint32_t acc = g % kOwn > 0 ? 1u : first;
+                        if constexpr (kCopies > 1)
+                            mma_bf16_ts_lanes(tmem + cO, from + 64 * (g / 4) + 8 * (g % 4), bv + g * (2048 >> 4), id, acc, kCopies, g / kOwn);
+                        else mma_bf16_ts(tmem + cO, from + 64 * (g / 4) + 8 * (g % 4), bv + g * (2048 >> 4), id, acc);
                     }
-                    if (ok) mma_commit(&pvdone[b]);
+                    mma_commit(&pvdone[b]);
+                    mma_commit(&vempty[b]);
                 }
             }
             mma_commit(&drained[1]);
@@ -395,6 +376,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_quant_tc(const __gri
         // two threads to a lane of Tensor Memory: halves of its keys, and of the features
         constexpr int kKeys = kTile / kCopies / 2;          // keys of a tile of this thread
         constexpr int kSpan = kKeys < 32 ? kKeys : 32;      // of them at a time
+        constexpr int kGroups = kKeys / 16;
         constexpr int kFeat = D / 2;
         const int quad = warp & 3, part = warp >> 2, at_lane = 32 * quad + lane;
         const int copy = at_lane / kCopyRows, row = at_lane % kCopyRows, key0 = kKeys * (2 * copy + part);
@@ -480,6 +462,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_quant_tc(const __gri
                 // P lies in the half of S that its keys have: where it meets scores of the lane's other thread, they have
                 // been read before the vote below, and those of its own that are read twice lie ahead of it
                 const uint32_t my_p = my_s + key0 / 64 * 64 + key0 % 64 / 2;
+                // factors of S (bounded away from zero: they meet the infinities of masked scores), log2(vs)
+                float fk[kGroups], lv[kGroups];
+#pragma unroll
+                for (int g = 0; g < kGroups; ++g) {
+                    fk[g] = fminf(fmaxf(my_scales[g] * kc, 0x1p-126f), kMax);
+                    lv[g] = lg2(my_scales[8 + g]);
+                }
                 float s[kSpan];
                 // scores of keys kSpan x ... from Tensor Memory, the masked ones replaced
                 auto scores = [&](int x) {
@@ -492,11 +481,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_quant_tc(const __gri
                         for (int y = 0; y < kSpan; ++y) s[y] = see >> y & 1u ? s[y] : -INFINITY;
                     }
                 };
-                // (bounded away from zero: it meets the infinities of masked scores)
-                auto factor = [&](int g) { return fminf(fmaxf(my_scales[g] * kc, 0x1p-126f), kMax); };
+                // of group h of span x
+                auto of = [&](const float (&v)[kGroups], int x, int h) { return kGroups == 4 && x > 0 ? v[(2 + h) % kGroups] : v[h]; };
                 float mx = -INFINITY, my = -INFINITY;       // of x, of x + log2(vs)
 #pragma unroll 1
-                for (int x = 0; x < kKeys / kSpan; ++x) {
+                for (int x = kKeys / kSpan - 1; x >= 0; --x) {              // (span 0 stays in registers for the second pass)
                     scores(x);
 #pragma unroll
                     for (int h = 0; h < kSpan / 16; ++h) {
@@ -507,9 +496,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_quant_tc(const __gri
                             t2 = max3(t2, s[16 * h + y + 2], s[16 * h + y + 3]);
                         }
                         t = max3(t, s[16 * h + 14], s[16 * h + 15]);
-                        const float top = fmaxf(t, t2) * factor(2 * x + h);
+                        const float top = fmaxf(t, t2) * of(fk, x, h);
                         mx = fmaxf(mx, top);
-                        my = fmaxf(my, top + lg2(my_scales[8 + 2 * x + h]));
+                        my = fmaxf(my, top + of(lv, x, h));
                     }
                 }
                 if (mx > m + kSlack) {                      // from -inf: whenever a key is visible
@@ -543,13 +532,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_quant_tc(const __gri
                 const float base = m == -INFINITY ? 0.f : m, to_o = base - (mo == -INFINITY ? 0.f : mo) + kTop;
 #pragma unroll 1
                 for (int x = 0; x < kKeys / kSpan; ++x) {
-                    if (kKeys > kSpan) scores(x);
+                    if (x > 0) scores(x);
                     float p[kSpan / 2];                     // pairs of half precision
 #pragma unroll
                     for (int h = 0; h < kSpan / 16; ++h) {
                         // P at once: l, from its sum.  (Below 2^-60 half precision has zeros, and float32 still has p.)
-                        const float gain = fminf(fmaxf(lg2(my_scales[8 + 2 * x + h]) + to_o, -60.f), 126.f), fk = factor(2 * x + h);
-                        const f32x2 f2 = pair2(fk, fk), add = pair2(gain - base, gain - base);
+                        const float gain = fminf(fmaxf(of(lv, x, h) + to_o, -60.f), 126.f), f = of(fk, x, h);
+                        const f32x2 f2 = pair2(f, f), add = pair2(gain - base, gain - base);
                         f32x2 sum[4];                       // (one alone would be a chain of latencies)
 #pragma unroll
                         for (int y = 0; y < 8; ++y) {
@@ -709,14 +698,14 @@ template <int D, int kCopies> cudaError_t launch(const PagedArgs &a, cudaStream_
 {
     TcArgs ta;
     ta.p = a;
-    // pieces, codes, barriers, scales, exchange, stage (with copies), and 1 KB for alignment
-    const uint32_t pieces = (kTiles * kTile + kPieces * kPieceKeys) * D * 2, slot = kTile * D;
+    // half precision, codes, barriers, scales, exchange, stage (with copies), and 1 KB for alignment
+    const uint32_t halves = 2 * kTiles * kTile * D * 2, slot = kTile * D;
     const uint32_t tail = kBarBytes + kScaleBytes + kExchange + (kCopies > 1 ? kStage : 0) + 1024;
-    int ns = (int)((kSmemLimit - tail - pieces) / slot);
+    int ns = (int)((kSmemLimit - tail - halves) / slot);
     if (ns > kMaxSlots) ns = kMaxSlots;
     ta.NK = ns / 2;
     ta.NV = ns - ta.NK;
-    ta.off_bar = pieces + ns * slot;
+    ta.off_bar = halves + ns * slot;
     ta.off_stage = ta.off_bar + kBarBytes + kScaleBytes + kExchange + 256;
     ta.bytes = ta.off_bar + tail;
     if (!encode_codes(&ta.tmK, a.K, a) || !encode_codes(&ta.tmV, a.V, a)) return cudaErrorInvalidValue;
