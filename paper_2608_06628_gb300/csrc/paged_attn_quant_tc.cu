@@ -199,6 +199,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_quant_tc(const __gri
     const bool work = find_share<kThreads>(a, *plan_smem, w, sh);
     const uint32_t tmem = *tmem_holder;
 
+    // The scores of a tile fill the softmax's registers: 96 + 2 * 64 + 2 * 128 = 5 * 96 for the groups of four warps.
+    if (warp >= kLoadK) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
     if (warp == kLoadK || warp == kLoadV) {
         // ------------------------------------------------------ producers of the codes
         const bool is_v = warp == kLoadV;
@@ -278,39 +281,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_quant_tc(const __gri
             if (lane == 0) write_note(a, work, w, sh);
             write_empty<bf16, 32>(a, lane);
         }
-    } else if (work && warp >= kConvertK && warp < kLoadK) {
-        // ------------------------------------------------------ converters
-        const bool is_v = warp >= kConvertV;
-        const int v = warp & 3;
-        const uint32_t n_slots = is_v ? NV : NK;
-        uint64_t *my_full = is_v ? full + NK : full, *my_empty = is_v ? empty + NK : empty;
-        uint8_t *my_ring = is_v ? ring + (size_t)NK * kCodes : ring;
-        RingPos pos{0, 0}, to{0, 1};
-        bool ok = true;
-        while (ok && w.next(a)) {
-            for (int i = w.i0; i < w.i1; ++i) {
-                const int j0 = key_tile(w.vis, i) * kTile;
-                const bool edge = is_v && !all_visible(w.vis, j0);
-                ok = wait_soon(&my_full[pos.slot], pos.phase, fail);
-                const uint8_t *codes = my_ring + (size_t)pos.slot * kCodes;
-                ok = ok && wait_soon(is_v ? &vempty[to.slot] : &kempty[to.slot], to.phase, fail);
-                if (__any_sync(0xffffffffu, !ok)) ok = false;
-                if (!ok) break;
-                uint8_t *rows_of = (is_v ? tile_v : tile_k) + to.slot * kHalf;
-#pragma unroll 1
-                for (int key = 32 * v; key < 32 * v + 32; key += 16)
-                    convert<D>(codes + key * D, rows_of + key * 128, kPanel, lane,
-                               [&](int x) { return !edge || key_visible(w.vis, j0 + key + x); });
-                fence_proxy_async_smem();
-                __syncwarp();
-                if (lane == 0) {
-                    mbar_arrive(is_v ? &vfull[to.slot] : &kfull[to.slot]);
-                    mbar_arrive(&my_empty[pos.slot]);
-                }
-                to.step(kTiles);
-                pos.step(n_slots);
-            }
-        }
     } else if (work && warp == kIssueS) {
         // --------------------------------------------- issuer of S = Q K^T
         if (lane == 0) {
@@ -371,7 +341,46 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_quant_tc(const __gri
             mma_commit(&drained[1]);
             mbar_wait(&drained[1], 0, kWaitNs);
         }
-    } else if (work && warp < kConvertK && (warp & 3) < n_quads) {
+    }
+    } else if (warp >= kConvertK) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+        if (work) {
+        // ------------------------------------------------------ converters
+        const bool is_v = warp >= kConvertV;
+        const int v = warp & 3;
+        const uint32_t n_slots = is_v ? NV : NK;
+        uint64_t *my_full = is_v ? full + NK : full, *my_empty = is_v ? empty + NK : empty;
+        uint8_t *my_ring = is_v ? ring + (size_t)NK * kCodes : ring;
+        RingPos pos{0, 0}, to{0, 1};
+        bool ok = true;
+        while (ok && w.next(a)) {
+            for (int i = w.i0; i < w.i1; ++i) {
+                const int j0 = key_tile(w.vis, i) * kTile;
+                const bool edge = is_v && !all_visible(w.vis, j0);
+                ok = wait_soon(&my_full[pos.slot], pos.phase, fail);
+                const uint8_t *codes = my_ring + (size_t)pos.slot * kCodes;
+                ok = ok && wait_soon(is_v ? &vempty[to.slot] : &kempty[to.slot], to.phase, fail);
+                if (__any_sync(0xffffffffu, !ok)) ok = false;
+                if (!ok) break;
+                uint8_t *rows_of = (is_v ? tile_v : tile_k) + to.slot * kHalf;
+#pragma unroll 1
+                for (int key = 32 * v; key < 32 * v + 32; key += 16)
+                    convert<D>(codes + key * D, rows_of + key * 128, kPanel, lane,
+                               [&](int x) { return !edge || key_visible(w.vis, j0 + key + x); });
+                fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) {
+                    mbar_arrive(is_v ? &vfull[to.slot] : &kfull[to.slot]);
+                    mbar_arrive(&my_empty[pos.slot]);
+                }
+                to.step(kTiles);
+                pos.step(n_slots);
+            }
+        }
+        }
+    } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 128;");
+        if (work && (warp & 3) < n_quads) {
         // --------------------------------------------------- Q, softmax, epilogue
         // two threads to a lane of Tensor Memory: halves of its keys, and of the features
         constexpr int kKeys = kTile / kCopies / 2;          // keys of a tile of this thread
@@ -469,37 +478,35 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_quant_tc(const __gri
                     fk[g] = fminf(fmaxf(my_scales[g] * kc, 0x1p-126f), kMax);
                     lv[g] = lg2(my_scales[8 + g]);
                 }
-                float s[kSpan];
-                // scores of keys kSpan x ... from Tensor Memory, the masked ones replaced
-                auto scores = [&](int x) {
-                    if constexpr (kSpan == 32) tmem_ld32(my_s + key0 + 32 * x, s);
-                    else tmem_ld16(my_s + key0, s);
-                    tmem_wait_ld();
-                    if (edge) {
+                // scores from Tensor Memory, the masked ones replaced
+                float s[kKeys / kSpan][kSpan];
+#pragma unroll
+                for (int x = 0; x < kKeys / kSpan; ++x) {
+                    if constexpr (kSpan == 32) tmem_ld32(my_s + key0 + 32 * x, s[x]);
+                    else tmem_ld16(my_s + key0, s[x]);
+                }
+                tmem_wait_ld();
+                if (edge) {
+#pragma unroll
+                    for (int x = 0; x < kKeys / kSpan; ++x) {
                         const unsigned see = below(hi - 32 * x) & (~below(lo - 32 * x) | below(sink - 32 * x));
 #pragma unroll
-                        for (int y = 0; y < kSpan; ++y) s[y] = see >> y & 1u ? s[y] : -INFINITY;
+                        for (int y = 0; y < kSpan; ++y) s[x][y] = see >> y & 1u ? s[x][y] : -INFINITY;
                     }
-                };
-                // of group h of span x
-                auto of = [&](const float (&v)[kGroups], int x, int h) { return kGroups == 4 && x > 0 ? v[(2 + h) % kGroups] : v[h]; };
+                }
                 float mx = -INFINITY, my = -INFINITY;       // of x, of x + log2(vs)
-#pragma unroll 1
-                for (int x = kKeys / kSpan - 1; x >= 0; --x) {              // (span 0 stays in registers for the second pass)
-                    scores(x);
 #pragma unroll
-                    for (int h = 0; h < kSpan / 16; ++h) {
-                        float t = max3(s[16 * h], s[16 * h + 1], s[16 * h + 2]), t2 = max3(s[16 * h + 3], s[16 * h + 4], s[16 * h + 5]);
+                for (int g = 0; g < kGroups; ++g) {
+                    const float *v = &s[g / 2][g % 2 * 16];
+                    float t = max3(v[0], v[1], v[2]), t2 = max3(v[3], v[4], v[5]);
 #pragma unroll
-                        for (int y = 6; y < 14; y += 4) {
-                            t = max3(t, s[16 * h + y], s[16 * h + y + 1]);
-                            t2 = max3(t2, s[16 * h + y + 2], s[16 * h + y + 3]);
-                        }
-                        t = max3(t, s[16 * h + 14], s[16 * h + 15]);
-                        const float top = fmaxf(t, t2) * of(fk, x, h);
-                        mx = fmaxf(mx, top);
-                        my = fmaxf(my, top + of(lv, x, h));
+                    for (int y = 6; y < 14; y += 4) {
+                        t = max3(t, v[y], v[y + 1]);
+                        t2 = max3(t2, v[y + 2], v[y + 3]);
                     }
+                    const float top = fmaxf(max3(t, v[14], v[15]), t2) * fk[g];
+                    mx = fmaxf(mx, top);
+                    my = fmaxf(my, top + lv[g]);
                 }
                 if (mx > m + kSlack) {                      // from -inf: whenever a key is visible
                     if (m != -INFINITY) l *= ex2(m - mx);   // (else it is zero)
@@ -519,31 +526,31 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_quant_tc(const __gri
                         wait(&pvdone[(n - 1) & 1], ((n - 1) >> 1) & 1u);       // O is at rest
                         tc_fence_after();
 #pragma unroll 1
-                        for (int x = 0; x < kFeat / 32; ++x) {
-                            float o[32];
-                            tmem_ld32(tmem + cO + kFeat * part + 32 * x + lane_off, o);
+                        for (int x = 0; x < kFeat / 16; ++x) {
+                            float o[16];
+                            tmem_ld16(tmem + cO + kFeat * part + 16 * x + lane_off, o);
                             tmem_wait_ld();
 #pragma unroll
-                            for (int y = 0; y < 32; ++y) o[y] *= f;
-                            tmem_st32(tmem + cO + kFeat * part + 32 * x + lane_off, o);
+                            for (int y = 0; y < 16; ++y) o[y] *= f;
+                            tmem_st16(tmem + cO + kFeat * part + 16 * x + lane_off, o);
                         }
                     }
                 }
                 const float base = m == -INFINITY ? 0.f : m, to_o = base - (mo == -INFINITY ? 0.f : mo) + kTop;
-#pragma unroll 1
+#pragma unroll
                 for (int x = 0; x < kKeys / kSpan; ++x) {
-                    if (x > 0) scores(x);
                     float p[kSpan / 2];                     // pairs of half precision
 #pragma unroll
                     for (int h = 0; h < kSpan / 16; ++h) {
                         // P at once: l, from its sum.  (Below 2^-60 half precision has zeros, and float32 still has p.)
-                        const float gain = fminf(fmaxf(of(lv, x, h) + to_o, -60.f), 126.f), f = of(fk, x, h);
-                        const f32x2 f2 = pair2(f, f), add = pair2(gain - base, gain - base);
+                        const int g = 2 * x + h;
+                        const float gain = fminf(fmaxf(lv[g] + to_o, -60.f), 126.f);
+                        const f32x2 f2 = pair2(fk[g], fk[g]), add = pair2(gain - base, gain - base);
                         f32x2 sum[4];                       // (one alone would be a chain of latencies)
 #pragma unroll
                         for (int y = 0; y < 8; ++y) {
                             float p0, p1;
-                            unpair2(fma2(pair2(s[16 * h + 2 * y], s[16 * h + 2 * y + 1]), f2, add), p0, p1);
+                            unpair2(fma2(pair2(s[x][16 * h + 2 * y], s[x][16 * h + 2 * y + 1]), f2, add), p0, p1);
                             p0 = ex2(p0);
                             p1 = ex2(p1);
                             sum[y & 3] = y < 4 ? pair2(p0, p1) : add2(sum[y & 3], pair2(p0, p1));
@@ -673,6 +680,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_quant_tc(const __gri
             }
         }
         if (tid == 0 && *fail) raise_error(a.err, ERR_WAIT_TIMEOUT);
+    }
     }
     __syncthreads();
     if (warp == kIssueS) {
