@@ -76,6 +76,12 @@ __device__ __forceinline__ float max3(float x, float y, float z)
     asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(x), "f"(y), "f"(z));
     return r;
 }
+__device__ __forceinline__ bool elect_one()
+{
+    uint32_t one;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(one));
+    return one != 0;
+}
 __device__ __forceinline__ void tmem_st8(uint32_t taddr, const float (&v)[8])
 {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr),
@@ -89,7 +95,7 @@ __device__ __forceinline__ void tmem_st8(uint32_t taddr, const float (&v)[8])
 // in bits 0 and 2: neither its reads nor its writes meet in a bank.  Keys for which see() is false
 // become zeros.
 template <int D, typename See>
-__device__ __forceinline__ void convert(const uint8_t *codes, uint8_t *to, uint32_t panel, int lane, See see)
+__device__ __forceinline__ void convert(uint32_t codes, uint32_t to, uint32_t panel, int lane, See see)
 {
     constexpr int kHalves = D / 64;
     const int c = lane & 3, octet = lane >> 3 ^ (lane & 4 ? 5 : 0);
@@ -97,8 +103,12 @@ __device__ __forceinline__ void convert(const uint8_t *codes, uint8_t *to, uint3
 #pragma unroll
     for (int o = 0; o < 2; ++o) {
 #pragma unroll
-        for (int p = 0; p < kHalves; ++p)
-            x[o][p] = *reinterpret_cast<const uint4 *>(codes + (8 * o + octet) * D + (D == 128 ? ((4 * p + c) ^ octet) << 4 : c << 4));
+        for (int p = 0; p < kHalves; ++p) {
+            const uint32_t at = codes + (8 * o + octet) * D + (D == 128 ? ((4 * p + c) ^ octet) << 4 : c << 4);
+            asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
+                         : "=r"(x[o][p].x), "=r"(x[o][p].y), "=r"(x[o][p].z), "=r"(x[o][p].w)
+                         : "r"(at));
+        }
     }
 #pragma unroll
     for (int o = 0; o < 2; ++o) {
@@ -114,9 +124,12 @@ __device__ __forceinline__ void convert(const uint8_t *codes, uint8_t *to, uint3
                 f[2 * i] = *reinterpret_cast<const uint32_t *>(&lo);
                 f[2 * i + 1] = *reinterpret_cast<const uint32_t *>(&hi);
             }
-            uint8_t *row = to + p * panel + (8 * o + octet) * 128;
-            *reinterpret_cast<uint4 *>(row + ((2 * c ^ octet) << 4)) = make_uint4(f[0], f[1], f[2], f[3]);
-            *reinterpret_cast<uint4 *>(row + (((2 * c + 1) ^ octet) << 4)) = make_uint4(f[4], f[5], f[6], f[7]);
+            const uint32_t row = to + p * panel + (8 * o + octet) * 128;
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(row + (((2 * c + i) ^ octet) << 4)), "r"(f[4 * i]),
+                             "r"(f[4 * i + 1]), "r"(f[4 * i + 2]), "r"(f[4 * i + 3])
+                             : "memory");
         }
     }
 }
@@ -283,50 +296,58 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_quant_tc(const __gri
         }
     } else if (work && warp == kIssueS) {
         // --------------------------------------------- issuer of S = Q K^T
-        if (lane == 0) {
-            const uint32_t id = instr_desc(FMT_F16, FMT_F16, false, false, 128, kTile);
-            const uint64_t k_desc = smem_desc(smem_u32(tile_k), 16, 1024, SWZ_128B);
-            uint32_t n = 0, seg = 0;                       // tiles and segments so far
-            bool ok = true;
-            while (ok && w.next(a)) {
-                ok = wait_soon(qready, seg & 1u, fail);
-                ++seg;
-                for (int i = w.i0; ok && i < w.i1; ++i, ++n) {
-                    const uint32_t b = n & 1;
-                    // P in S's buffer is multiplied, the tile is in place
-                    ok = wait_soon(&pvdone[b], ((n >> 1) & 1u) ^ 1u, fail) && wait_soon(&kfull[b], (n >> 1) & 1u, fail);
-                    if (!ok) break;
-                    tc_fence_after();
-                    const uint64_t bk = k_desc + b * (kHalf >> 4);
+        // (Branches on votes: the compiler then knows that the warp goes one way, and keeps what the products are told
+        // in uniform registers, where they want it.)
+        const bool one = elect_one();
+        const uint32_t id = instr_desc(FMT_F16, FMT_F16, false, false, 128, kTile);
+        const uint64_t k_desc = smem_desc(smem_u32(tile_k), 16, 1024, SWZ_128B);
+        uint32_t n = 0, seg = 0;                           // tiles and segments so far
+        bool ok = true;
+        while (__all_sync(0xffffffffu, ok && w.next(a))) {
+            ok = wait_soon(qready, seg & 1u, fail);
+            ++seg;
+            for (int i = w.i0; __all_sync(0xffffffffu, ok && i < w.i1); ++i, ++n) {
+                const uint32_t b = n & 1;
+                // P in S's buffer is multiplied, the tile is in place
+                ok = wait_soon(&pvdone[b], ((n >> 1) & 1u) ^ 1u, fail) && wait_soon(&kfull[b], (n >> 1) & 1u, fail);
+                if (!__all_sync(0xffffffffu, ok)) break;
+                tc_fence_after();
+                const uint64_t bk = k_desc + b * (kHalf >> 4);
+                if (one) {
 #pragma unroll
                     for (int k = 0; k < D / 16; ++k)
                         mma_bf16_ts(tmem + cS + 128 * b, tmem + cQ + 8 * k, bk + (k >> 2) * (kPanel >> 4) + (k & 3) * 2, id, k > 0);
                     mma_commit(&sready[b]);
                     mma_commit(&kempty[b]);
                 }
+                __syncwarp();
             }
+        }
+        if (one) {
             mma_commit(&drained[0]);
             mbar_wait(&drained[0], 0, kWaitNs);
         }
     } else if (work && warp == kIssueO) {
         // ------------------------------------------------------ issuer of O += P V
-        if (lane == 0) {
-            const uint32_t id = instr_desc(FMT_F16, FMT_F16, false, true, 128, D);
-            const uint64_t v_desc = smem_desc(smem_u32(tile_v), kPanel, 1024, SWZ_128B);
-            constexpr int kOwn = kTile / 16 / kCopies;     // steps of 16 keys of a copy
-            uint32_t n = 0, seg = 0;
-            bool ok = true;
-            while (ok && w.next(a)) {
-                // O is overwritten by a segment's first product: the last epilogue has read it
-                if (seg > 0) ok = wait_soon(ofree, (seg - 1) & 1u, fail);
-                ++seg;
-                for (int i = w.i0; ok && i < w.i1; ++i, ++n) {
-                    const uint32_t b = n & 1, first = i > w.i0;
-                    ok = wait_soon(&vfull[b], (n >> 1) & 1u, fail) && wait_soon(&pready[b], (n >> 1) & 1u, fail);
-                    if (!ok) break;
-                    tc_fence_after();
-                    const uint64_t bv = v_desc + b * (kHalf >> 4);
-                    const uint32_t from = tmem + cS + 128 * b;
+        const bool one = elect_one();
+        const uint32_t id = instr_desc(FMT_F16, FMT_F16, false, true, 128, D);
+        const uint64_t v_desc = smem_desc(smem_u32(tile_v), kPanel, 1024, SWZ_128B);
+        constexpr int kOwn = kTile / 16 / kCopies;         // steps of 16 keys of a copy
+        uint32_t n = 0, seg = 0;
+        bool ok = true;
+        while (__all_sync(0xffffffffu, ok && w.next(a))) {
+            // O is overwritten by a segment's first product: the last epilogue has read it
+            if (seg > 0) ok = wait_soon(ofree, (seg - 1) & 1u, fail);
+            ++seg;
+            uint32_t first = 0;                            // accumulate: not in the segment's first tile
+            for (int i = w.i0; __all_sync(0xffffffffu, ok && i < w.i1); ++i, ++n) {
+                const uint32_t b = n & 1;
+                ok = wait_soon(&vfull[b], (n >> 1) & 1u, fail) && wait_soon(&pready[b], (n >> 1) & 1u, fail);
+                if (!__all_sync(0xffffffffu, ok)) break;
+                tc_fence_after();
+                const uint64_t bv = v_desc + b * (kHalf >> 4);
+                const uint32_t from = tmem + cS + 128 * b;
+                if (one) {
 #pragma unroll
                     for (int g = 0; g < kTile / 16; ++g) {
                         const uint32_t acc = g % kOwn > 0 ? 1u : first;
@@ -337,7 +358,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_quant_tc(const __gri
                     mma_commit(&pvdone[b]);
                     mma_commit(&vempty[b]);
                 }
+                __syncwarp();
+                first = 1;
             }
+        }
+        if (one) {
             mma_commit(&drained[1]);
             mbar_wait(&drained[1], 0, kWaitNs);
         }
@@ -350,7 +375,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_quant_tc(const __gri
         const int v = warp & 3;
         const uint32_t n_slots = is_v ? NV : NK;
         uint64_t *my_full = is_v ? full + NK : full, *my_empty = is_v ? empty + NK : empty;
-        uint8_t *my_ring = is_v ? ring + (size_t)NK * kCodes : ring;
+        const uint32_t my_ring = smem_u32(is_v ? ring + (size_t)NK * kCodes : ring), my_tiles = smem_u32(is_v ? tile_v : tile_k);
         RingPos pos{0, 0}, to{0, 1};
         bool ok = true;
         while (ok && w.next(a)) {
@@ -358,14 +383,12 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_quant_tc(const __gri
                 const int j0 = key_tile(w.vis, i) * kTile;
                 const bool edge = is_v && !all_visible(w.vis, j0);
                 ok = wait_soon(&my_full[pos.slot], pos.phase, fail);
-                const uint8_t *codes = my_ring + (size_t)pos.slot * kCodes;
                 ok = ok && wait_soon(is_v ? &vempty[to.slot] : &kempty[to.slot], to.phase, fail);
                 if (__any_sync(0xffffffffu, !ok)) ok = false;
                 if (!ok) break;
-                uint8_t *rows_of = (is_v ? tile_v : tile_k) + to.slot * kHalf;
 #pragma unroll 1
                 for (int key = 32 * v; key < 32 * v + 32; key += 16)
-                    convert<D>(codes + key * D, rows_of + key * 128, kPanel, lane,
+                    convert<D>(my_ring + pos.slot * kCodes + key * D, my_tiles + to.slot * kHalf + key * 128, kPanel, lane,
                                [&](int x) { return !edge || key_visible(w.vis, j0 + key + x); });
                 fence_proxy_async_smem();
                 __syncwarp();
