@@ -41,12 +41,6 @@ constexpr float kMax = 3.402823466e38f;
 
 static_assert(kRun == quant::kGroup, "two scales a run");
 
-__device__ __forceinline__ uint32_t decode_lo(uint32_t v)
-{
-    const __half2 h = quant::decode2(v);
-    return *reinterpret_cast<const uint32_t *>(&h);
-}
-__device__ __forceinline__ uint32_t decode_hi(uint32_t v) { return decode_lo(v >> 16); }
 __device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi)
 {
     const __half2 h = __floats2half2_rn(lo, hi);
@@ -263,7 +257,9 @@ __global__ __launch_bounds__(kThreads, NT == 1 ? 2 : 1) void k_paged_attn_quant(
                     const uint32_t w0[4] = {k0.x, k0.y, k0.z, k0.w}, w1[4] = {k1.x, k1.y, k1.z, k1.w};
 #pragma unroll
                     for (int t = 0; t < 4; ++t) {
-                        const uint32_t f[4] = {decode_lo(w0[t]), decode_lo(w1[t]), decode_hi(w0[t]), decode_hi(w1[t])};
+                        uint32_t f[4];
+                        quant::decode4(w0[t], f[0], f[2]);
+                        quant::decode4(w1[t], f[1], f[3]);
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -345,7 +341,9 @@ __global__ __launch_bounds__(kThreads, NT == 1 ? 2 : 1) void k_paged_attn_quant(
                 for (int t = 0; t < MT; ++t) {              // features 2 t, 2 t + 1 of the lane's
                     const uint32_t sel = t & 1 ? 0x7362u : 0x5140u;
                     const uint32_t lo = __byte_perm(r[0][t / 2], r[1][t / 2], sel), hi = __byte_perm(r[2][t / 2], r[3][t / 2], sel);
-                    const uint32_t f[4] = {decode_lo(lo), decode_hi(lo), decode_lo(hi), decode_hi(hi)};
+                    uint32_t f[4];
+                    quant::decode4(lo, f[0], f[1]);
+                    quant::decode4(hi, f[2], f[3]);
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll

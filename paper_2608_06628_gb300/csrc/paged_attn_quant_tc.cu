@@ -76,6 +76,18 @@ __device__ __forceinline__ float max3(float x, float y, float z)
     asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(x), "f"(y), "f"(z));
     return r;
 }
+template <int N> __device__ __forceinline__ void read_scales(const float *p, float (&v)[N])
+{
+    if constexpr (N == 4) {
+        const float4 x = *reinterpret_cast<const float4 *>(p);
+        v[0] = x.x, v[1] = x.y, v[2] = x.z, v[3] = x.w;
+    } else if constexpr (N == 2) {
+        const float2 x = *reinterpret_cast<const float2 *>(p);
+        v[0] = x.x, v[1] = x.y;
+    } else {
+        v[0] = *p;
+    }
+}
 __device__ __forceinline__ bool elect_one()
 {
     uint32_t one;
@@ -92,9 +104,9 @@ __device__ __forceinline__ void tmem_st8(uint32_t taddr, const float (&v)[8])
 
 // 16 keys from `codes` on to half precision, from row `row` (a multiple of 16) of an operand with
 // panels of `panel` bytes, by a warp.  A group of 8 lanes has 64 features of two keys that differ
-// in bits 0 and 2: neither its reads nor its writes meet in a bank.  Keys for which see() is false
-// become zeros.
-template <int D, typename See>
+// in bits 0 and 2: neither its reads nor its writes meet in a bank.  With kMasked, keys for which
+// see() is false become zeros.
+template <int D, bool kMasked, typename See>
 __device__ __forceinline__ void convert(uint32_t codes, uint32_t to, uint32_t panel, int lane, See see)
 {
     constexpr int kHalves = D / 64;
@@ -112,17 +124,14 @@ __device__ __forceinline__ void convert(uint32_t codes, uint32_t to, uint32_t pa
     }
 #pragma unroll
     for (int o = 0; o < 2; ++o) {
-        const bool keep = see(8 * o + octet);
+        const bool keep = !kMasked || see(8 * o + octet);
 #pragma unroll
         for (int p = 0; p < kHalves; ++p) {
             const uint32_t w[4] = {x[o][p].x, x[o][p].y, x[o][p].z, x[o][p].w};
             uint32_t f[8];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const uint32_t code = keep ? w[i] : 0u;
-                const __half2 lo = quant::decode2(code), hi = quant::decode2(code >> 16);
-                f[2 * i] = *reinterpret_cast<const uint32_t *>(&lo);
-                f[2 * i + 1] = *reinterpret_cast<const uint32_t *>(&hi);
+                quant::decode4(kMasked && !keep ? 0u : w[i], f[2 * i], f[2 * i + 1]);
             }
             const uint32_t row = to + p * panel + (8 * o + octet) * 128;
 #pragma unroll
@@ -169,7 +178,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_quant_tc(const __gri
     uint32_t *tmem_holder = reinterpret_cast<uint32_t *>(drained + 2);
     volatile int *fail = reinterpret_cast<volatile int *>(tmem_holder + 1);
     PlanSmem *plan_smem = reinterpret_cast<PlanSmem *>(tmem_holder + 2);
-    float *scales = reinterpret_cast<float *>(smem + ta.off_bar + kBarBytes);     // [kScaleTiles][8 of K, 8 of V]
+    float *scales = reinterpret_cast<float *>(smem + ta.off_bar + kBarBytes);     // [kScaleTiles][8 of K, 8 of V (then their log2)]
     float *exchange = scales + kScaleBytes / 4;            // [2][2][128]
     float *inv_of = exchange + 512;                        // [64], with copies
 
@@ -308,8 +317,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_quant_tc(const __gri
             ++seg;
             for (int i = w.i0; __all_sync(0xffffffffu, ok && i < w.i1); ++i, ++n) {
                 const uint32_t b = n & 1;
-                // P in S's buffer is multiplied, the tile is in place
-                ok = wait_soon(&pvdone[b], ((n >> 1) & 1u) ^ 1u, fail) && wait_soon(&kfull[b], (n >> 1) & 1u, fail);
+                // the tile is in place, P in S's buffer is multiplied
+                ok = wait_soon(&kfull[b], (n >> 1) & 1u, fail) && wait_soon(&pvdone[b], ((n >> 1) & 1u) ^ 1u, fail);
                 if (!__all_sync(0xffffffffu, ok)) break;
                 tc_fence_after();
                 const uint64_t bk = k_desc + b * (kHalf >> 4);
@@ -377,6 +386,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_quant_tc(const __gri
         uint64_t *my_full = is_v ? full + NK : full, *my_empty = is_v ? empty + NK : empty;
         const uint32_t my_ring = smem_u32(is_v ? ring + (size_t)NK * kCodes : ring), my_tiles = smem_u32(is_v ? tile_v : tile_k);
         RingPos pos{0, 0}, to{0, 1};
+        uint32_t n = 0;                                    // tiles so far
         bool ok = true;
         while (ok && w.next(a)) {
             for (int i = w.i0; i < w.i1; ++i) {
@@ -386,10 +396,19 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_quant_tc(const __gri
                 ok = ok && wait_soon(is_v ? &vempty[to.slot] : &kempty[to.slot], to.phase, fail);
                 if (__any_sync(0xffffffffu, !ok)) ok = false;
                 if (!ok) break;
+                const uint32_t codes = my_ring + pos.slot * kCodes + 32 * v * D, rows_of = my_tiles + to.slot * kHalf + 32 * v * 128;
 #pragma unroll 1
-                for (int key = 32 * v; key < 32 * v + 32; key += 16)
-                    convert<D>(my_ring + pos.slot * kCodes + key * D, my_tiles + to.slot * kHalf + key * 128, kPanel, lane,
-                               [&](int x) { return !edge || key_visible(w.vis, j0 + key + x); });
+                for (int key = 0; key < 32; key += 16) {
+                    const int j = j0 + 32 * v + key;
+                    if (edge) convert<D, true>(codes + key * D, rows_of + key * 128, kPanel, lane, [&](int x) { return key_visible(w.vis, j + x); });
+                    else convert<D, false>(codes + key * D, rows_of + key * 128, kPanel, lane, [](int) { return true; });
+                }
+                // log2 of the scales of V, for the softmax
+                if (warp == kConvertK && lane < 8) {
+                    float *vs = scales + n % kScaleTiles * 16 + 8 + lane;
+                    *vs = lg2(*vs);
+                }
+                ++n;
                 fence_proxy_async_smem();
                 __syncwarp();
                 if (lane == 0) {
@@ -428,57 +447,59 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_quant_tc(const __gri
             __syncwarp();
             if (lane == 0 && !bad) mbar_arrive(bar);
         };
-        while (w.next(a)) {     // left by a vote at a segment's end only, so that the warps of a row stay together
-            const Unit u = unit_of(a, w.head, w.rt);
-            size_t at;
-            const bool live = row_at(a, w.req, u, row, at), whole = w.whole();
-            float kc;                                       // log2(e) / sqrt(d) over the row's factor
-            {   // Q.  (The last segment's products with it are done: its last S has been read.)
-                const bf16 *src = static_cast<const bf16 *>(a.Q) + at + kFeat * part;
-                uint4 v[kFeat / 8];
+        // Q of the segment w; returns log2(e) / sqrt(d) over the row's factor
+        auto load_q = [&]() -> float {
+            size_t from;
+            const bool live = row_at(a, w.req, unit_of(a, w.head, w.rt), row, from);
+            const bf16 *src = static_cast<const bf16 *>(a.Q) + from + kFeat * part;
+            uint4 v[kFeat / 8];
 #pragma unroll
-                for (int x = 0; x < kFeat / 8; ++x)
-                    v[x] = live ? __ldg(reinterpret_cast<const uint4 *>(src) + x) : make_uint4(0, 0, 0, 0);
-                uint32_t top2 = 0;                          // largest magnitudes of the even and the odd entries
-                auto larger = [](uint32_t p, uint32_t q) {
-                    const __nv_bfloat162 r = __hmax2(*reinterpret_cast<__nv_bfloat162 *>(&p), *reinterpret_cast<__nv_bfloat162 *>(&q));
-                    return *reinterpret_cast<const uint32_t *>(&r);
-                };
+            for (int x = 0; x < kFeat / 8; ++x)
+                v[x] = live ? __ldg(reinterpret_cast<const uint4 *>(src) + x) : make_uint4(0, 0, 0, 0);
+            uint32_t top2 = 0;                              // largest magnitudes of the even and the odd entries
+            auto larger = [](uint32_t p, uint32_t q) {
+                const __nv_bfloat162 r = __hmax2(*reinterpret_cast<__nv_bfloat162 *>(&p), *reinterpret_cast<__nv_bfloat162 *>(&q));
+                return *reinterpret_cast<const uint32_t *>(&r);
+            };
 #pragma unroll
-                for (int x = 0; x < kFeat / 8; ++x)
-                    top2 = larger(top2, larger(larger(v[x].x & 0x7fff7fffu, v[x].y & 0x7fff7fffu),
-                                               larger(v[x].z & 0x7fff7fffu, v[x].w & 0x7fff7fffu)));
-                uint32_t top = max(top2 & 0xffffu, top2 >> 16);
-                if (top >= 0x7f80u) {                       // infinities are left out
-                    top = 0;
+            for (int x = 0; x < kFeat / 8; ++x)
+                top2 = larger(top2, larger(larger(v[x].x & 0x7fff7fffu, v[x].y & 0x7fff7fffu),
+                                           larger(v[x].z & 0x7fff7fffu, v[x].w & 0x7fff7fffu)));
+            uint32_t top = max(top2 & 0xffffu, top2 >> 16);
+            if (top >= 0x7f80u) {                           // infinities are left out
+                top = 0;
 #pragma unroll 1
-                    for (int x = 0; x < kFeat; ++x) {
-                        const uint32_t q1 = __ldg(reinterpret_cast<const unsigned short *>(src) + x) & 0x7fffu;
-                        if (q1 < 0x7f80u) top = max(top, q1);
-                    }
+                for (int x = 0; x < kFeat; ++x) {
+                    const uint32_t q1 = __ldg(reinterpret_cast<const unsigned short *>(src) + x) & 0x7fffu;
+                    if (q1 < 0x7f80u) top = max(top, q1);
                 }
-                *mine = __uint_as_float(top);
-                group_sync_failed(pair_bar, 64, false);
-                top = max(top, __float_as_uint(*others));
-                int e2 = (int)(top >> 7) - 127 - 14;        // the row over 2^e2 is below 2^15
-                if (e2 < -126) e2 = -126;
-                const float over = __uint_as_float((uint32_t)(127 - e2) << 23);
-                kc = __uint_as_float((uint32_t)(127 + e2) << 23) * to_log2;
-                tc_fence_after();
-#pragma unroll
-                for (int x = 0; x < kFeat / 32; ++x) {
-                    float f[16];
-#pragma unroll
-                    for (int y = 0; y < 16; ++y) {
-                        const uint4 &q4 = v[4 * x + y / 4];
-                        const uint32_t q2 = y % 4 == 0 ? q4.x : (y % 4 == 1 ? q4.y : (y % 4 == 2 ? q4.z : q4.w));
-                        f[y] = __uint_as_float(pack_f16x2(__uint_as_float(q2 << 16) * over, __uint_as_float(q2 & 0xffff0000u) * over));
-                    }
-                    tmem_st16(tmem + cQ + kFeat / 2 * part + 16 * x + lane_off, f);
-                }
-                tmem_wait_st();
-                arrive(qready);
             }
+            *mine = __uint_as_float(top);
+            group_sync_failed(pair_bar, 64, false);
+            top = max(top, __float_as_uint(*others));
+            group_sync_failed(pair_bar, 64, false);         // read before the exchange is used again
+            int e2 = (int)(top >> 7) - 127 - 14;            // the row over 2^e2 is below 2^15
+            if (e2 < -126) e2 = -126;
+            const float over = __uint_as_float((uint32_t)(127 - e2) << 23);
+            tc_fence_after();                               // (all S of the last segment have been read)
+#pragma unroll
+            for (int x = 0; x < kFeat / 32; ++x) {
+                float f[16];
+#pragma unroll
+                for (int y = 0; y < 16; ++y) {
+                    const uint4 &q4 = v[4 * x + y / 4];
+                    const uint32_t q2 = y % 4 == 0 ? q4.x : (y % 4 == 1 ? q4.y : (y % 4 == 2 ? q4.z : q4.w));
+                    f[y] = __uint_as_float(pack_f16x2(__uint_as_float(q2 << 16) * over, __uint_as_float(q2 & 0xffff0000u) * over));
+                }
+                tmem_st16(tmem + cQ + kFeat / 2 * part + 16 * x + lane_off, f);
+            }
+            tmem_wait_st();
+            arrive(qready);
+            return __uint_as_float((uint32_t)(127 + e2) << 23) * to_log2;
+        };
+        bool go = w.next(a);
+        float kc = go ? load_q() : 0.f;
+        while (go) {            // left by a vote at a segment's end only, so that the warps of a row stay together
             float m = -INFINITY, mo = -INFINITY;            // references of l (this thread's), and of O (the row's)
             float l = 0.f;                                  // sum over this thread's keys
             for (int i = w.i0; i < w.i1; ++i, ++n) {
@@ -496,11 +517,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_quant_tc(const __gri
                 const uint32_t my_p = my_s + key0 / 64 * 64 + key0 % 64 / 2;
                 // factors of S (bounded away from zero: they meet the infinities of masked scores), log2(vs)
                 float fk[kGroups], lv[kGroups];
+                read_scales(my_scales, fk);
+                read_scales(my_scales + 8, lv);
 #pragma unroll
-                for (int g = 0; g < kGroups; ++g) {
-                    fk[g] = fminf(fmaxf(my_scales[g] * kc, 0x1p-126f), kMax);
-                    lv[g] = lg2(my_scales[8 + g]);
-                }
+                for (int g = 0; g < kGroups; ++g) fk[g] = fminf(fmaxf(fk[g] * kc, 0x1p-126f), kMax);
                 // scores from Tensor Memory, the masked ones replaced
                 float s[kKeys / kSpan][kSpan];
 #pragma unroll
@@ -589,9 +609,16 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_quant_tc(const __gri
                 tmem_wait_st();
                 arrive(&pready[b]);
             }
+            // the next segment's Q: its first products are formed beside the output of this one
+            const Walk done = w;
+            go = w.next(a);
+            if (go) kc = load_q();
             // the segment's output: reference and sum of the row over its threads
+            const Unit u = unit_of(a, done.head, done.rt);
+            size_t at;
+            const bool live = row_at(a, done.req, u, row, at), whole = done.whole();
             bf16 *out = static_cast<bf16 *>(a.O) + at;
-            float *partial = a.part + w.slot() * partial_floats(rows, D);
+            float *partial = a.part + done.slot() * partial_floats(rows, D);
             *mine = m;
             mine[256] = l;
             if (group_sync_failed(kCopies > 1 ? 5 : pair_bar, kCopies > 1 ? 256 : 64, bad)) break;
@@ -656,7 +683,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_quant_tc(const __gri
                                 }
                                 const float k = inv_of[r];
                                 size_t dst;
-                                if (row_at(a, w.req, u, r, dst))
+                                if (row_at(a, done.req, u, r, dst))
                                     *reinterpret_cast<uint4 *>(static_cast<bf16 *>(a.O) + dst + x0 + col) = make_uint4(
                                         pack_bf16x2(v0.x * k, v0.y * k), pack_bf16x2(v0.z * k, v0.w * k),
                                         pack_bf16x2(v1.x * k, v1.y * k), pack_bf16x2(v1.z * k, v1.w * k));

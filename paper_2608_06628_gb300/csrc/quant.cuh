@@ -25,16 +25,19 @@ __device__ __forceinline__ uint32_t encode4(float a, float b, float c, float d)
 {
     return encode2(a, b) | encode2(c, d) << 16;
 }
-// The two values of the low 16 bits, exact in half precision.
-__device__ __forceinline__ __half2 decode2(uint32_t v)
+// Four values, exact in half precision: pairs of the low and of the high 16 bits (which the
+// conversion picks by itself).
+__device__ __forceinline__ void decode4(uint32_t v, uint32_t &lo, uint32_t &hi)
 {
-    uint32_t r;
-    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"((uint16_t)v));
-    return *reinterpret_cast<const __half2 *>(&r);
+    asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}"
+        : "=r"(lo), "=r"(hi)
+        : "r"(v));
 }
 __device__ __forceinline__ void decode4(uint32_t v, float (&x)[4])
 {
-    const float2 a = __half22float2(decode2(v)), b = __half22float2(decode2(v >> 16));
+    uint32_t lo, hi;
+    decode4(v, lo, hi);
+    const float2 a = __half22float2(*reinterpret_cast<const __half2 *>(&lo)), b = __half22float2(*reinterpret_cast<const __half2 *>(&hi));
     x[0] = a.x;
     x[1] = a.y;
     x[2] = b.x;
