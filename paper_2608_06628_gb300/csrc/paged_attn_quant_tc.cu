@@ -61,7 +61,7 @@ struct TcArgs {
 __device__ __forceinline__ float lg2(float x)
 {
     float y;
-    asm("lg2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+    asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
 __device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi)
@@ -69,6 +69,28 @@ __device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi)
     const __half2 h = __floats2half2_rn(lo, hi);
     return *reinterpret_cast<const uint32_t *>(&h);
 }
+
+// Key tiles of a segment in order, and whether all of a tile is visible, in a few instructions a tile.
+struct Tiles {
+    int i, i1, tile, ns, first, whole_from, whole_to, whole_sink;
+    __device__ void begin(const Walk &w)
+    {
+        i = w.i0;
+        i1 = w.i1;
+        ns = w.vis.ns;
+        first = w.vis.first;
+        tile = key_tile(w.vis, i);
+        whole_from = (w.vis.lo + kTile - 1) / kTile;
+        whole_to = w.vis.len / kTile;
+        whole_sink = w.vis.sink / kTile;
+    }
+    __device__ bool whole() const { return (tile >= whole_from && tile < whole_to) || tile < whole_sink; }
+    __device__ bool step()
+    {
+        tile = ++i == ns ? first : tile + 1;
+        return i < i1;
+    }
+};
 
 __device__ __forceinline__ float max3(float x, float y, float z)
 {
@@ -100,47 +122,6 @@ __device__ __forceinline__ void tmem_st8(uint32_t taddr, const float (&v)[8])
                  "r"(__float_as_uint(v[0])), "r"(__float_as_uint(v[1])), "r"(__float_as_uint(v[2])), "r"(__float_as_uint(v[3])),
                  "r"(__float_as_uint(v[4])), "r"(__float_as_uint(v[5])), "r"(__float_as_uint(v[6])), "r"(__float_as_uint(v[7]))
                  : "memory");
-}
-
-// 16 keys from `codes` on to half precision, from row `row` (a multiple of 16) of an operand with
-// panels of `panel` bytes, by a warp.  A group of 8 lanes has 64 features of two keys that differ
-// in bits 0 and 2: neither its reads nor its writes meet in a bank.  With kMasked, keys for which
-// see() is false become zeros.
-template <int D, bool kMasked, typename See>
-__device__ __forceinline__ void convert(uint32_t codes, uint32_t to, uint32_t panel, int lane, See see)
-{
-    constexpr int kHalves = D / 64;
-    const int c = lane & 3, octet = lane >> 3 ^ (lane & 4 ? 5 : 0);
-    uint4 x[2][kHalves];
-#pragma unroll
-    for (int o = 0; o < 2; ++o) {
-#pragma unroll
-        for (int p = 0; p < kHalves; ++p) {
-            const uint32_t at = codes + (8 * o + octet) * D + (D == 128 ? ((4 * p + c) ^ octet) << 4 : c << 4);
-            asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
-                         : "=r"(x[o][p].x), "=r"(x[o][p].y), "=r"(x[o][p].z), "=r"(x[o][p].w)
-                         : "r"(at));
-        }
-    }
-#pragma unroll
-    for (int o = 0; o < 2; ++o) {
-        const bool keep = !kMasked || see(8 * o + octet);
-#pragma unroll
-        for (int p = 0; p < kHalves; ++p) {
-            const uint32_t w[4] = {x[o][p].x, x[o][p].y, x[o][p].z, x[o][p].w};
-            uint32_t f[8];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                quant::decode4(kMasked && !keep ? 0u : w[i], f[2 * i], f[2 * i + 1]);
-            }
-            const uint32_t row = to + p * panel + (8 * o + octet) * 128;
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-                asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(row + (((2 * c + i) ^ octet) << 4)), "r"(f[4 * i]),
-                             "r"(f[4 * i + 1]), "r"(f[4 * i + 2]), "r"(f[4 * i + 3])
-                             : "memory");
-        }
-    }
 }
 
 // kCopies: 4, 2 or 1 copies of the rows (at most 32, 64, 128 of them).
@@ -178,7 +159,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_quant_tc(const __gri
     uint32_t *tmem_holder = reinterpret_cast<uint32_t *>(drained + 2);
     volatile int *fail = reinterpret_cast<volatile int *>(tmem_holder + 1);
     PlanSmem *plan_smem = reinterpret_cast<PlanSmem *>(tmem_holder + 2);
-    float *scales = reinterpret_cast<float *>(smem + ta.off_bar + kBarBytes);     // [kScaleTiles][8 of K, 8 of V (then their log2)]
+    float *scales = reinterpret_cast<float *>(smem + ta.off_bar + kBarBytes);     // [kScaleTiles][8 of K, 8 of V]
     float *exchange = scales + kScaleBytes / 4;            // [2][2][128]
     float *inv_of = exchange + 512;                        // [64], with copies
 
@@ -221,9 +202,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_quant_tc(const __gri
     const bool work = find_share<kThreads>(a, *plan_smem, w, sh);
     const uint32_t tmem = *tmem_holder;
 
-    // The scores of a tile fill the softmax's registers: 96 + 2 * 64 + 2 * 128 = 5 * 96 for the groups of four warps.
+    // The scores of a tile fill the softmax's registers: 80 + 2 * 72 + 2 * 128 = 5 * 96 for the groups of four warps.
     if (warp >= kLoadK) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
     if (warp == kLoadK || warp == kLoadV) {
         // ------------------------------------------------------ producers of the codes
         const bool is_v = warp == kLoadV;
@@ -245,20 +226,30 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_quant_tc(const __gri
             while (ok && w.next(a)) {
                 const int head = w.head;
                 const int *pages = a.table + (size_t)w.req * a.max_pages;
-                auto page_at = [&](int i) -> int {         // this lane's page of tile i, -1: nothing visible in it
-                    if (i >= w.i1 || lane >= per) return -1;
-                    const int j = key_tile(w.vis, i) * per + lane;
-                    if (!any_visible(w.vis, j * P, P)) return -1;
-                    const int page = __ldg(pages + j);
-                    if (page >= 0 && page < a.n_pages) return page;
-                    raise_error(a.err, ERR_BAD_INDEX);
-                    return 0;
+                Tiles at;
+                at.begin(w);
+                // this lane's page of the tile, -1: nothing visible in it
+                auto page_of = [&]() -> int {
+                    const int j = at.tile * per + lane;
+                    return lane < per && (at.whole() || any_visible(w.vis, j * P, P)) ? __ldg(pages + j) : -1;
                 };
-                int next_page = page_at(w.i0);
-                for (int i = w.i0; i < w.i1; ++i) {
-                    const int page = next_page;
-                    next_page = page_at(i + 1);            // a tile ahead of its use
-                    const uint32_t bytes = page_bytes * __popc(__ballot_sync(0xffffffffu, page >= 0));
+                auto sees = [&]() { return lane < per && (at.whole() || any_visible(w.vis, at.tile * kTile + lane * P, P)); };
+                int next_page = page_of();
+                bool next_see = sees();
+                for (bool more = true; more;) {
+                    const int tile = at.tile;
+                    const bool whole = at.whole(), mine = next_see;
+                    int page = next_page;                  // (looked at here, a tile after its load)
+                    if (mine && (page < 0 || page >= a.n_pages)) {
+                        raise_error(a.err, ERR_BAD_INDEX);
+                        page = 0;
+                    }
+                    more = at.step();
+                    if (more) {
+                        next_page = page_of();
+                        next_see = sees();
+                    }
+                    const uint32_t bytes = page_bytes * __popc(__ballot_sync(0xffffffffu, mine));
                     ok = wait_soon(&my_empty[pos.slot], pos.phase, fail);
                     if (__any_sync(0xffffffffu, !ok)) {
                         ok = false;
@@ -266,7 +257,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_quant_tc(const __gri
                     }
                     if (lane == 0) mbar_arrive_expect_tx(&my_full[pos.slot], bytes);
                     __syncwarp();
-                    if (page >= 0) {
+                    if (mine) {
                         uint8_t *dst = my_ring + (size_t)pos.slot * kCodes + lane * P * D;
                         if (once) tma_load_4d_policy(dst, map, 0, 0, head, page, &my_full[pos.slot], policy);
                         else tma_load_4d(dst, map, 0, 0, head, page, &my_full[pos.slot]);
@@ -276,7 +267,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_quant_tc(const __gri
                         // is done: the slot's last tile, at most 6 ago, is converted, so S of the second tile before
                         // that one is formed, and that waited for the softmax of the second tile before it.
                         const int of = __shfl_sync(0xffffffffu, page, group >> lg);
-                        const bool see = any_visible(w.vis, key_tile(w.vis, i) * kTile + group, 16);
+                        const bool see = whole || any_visible(w.vis, tile * kTile + group, 16);
                         if (lane < 16) {
                             const float *src = my_scale + (see ? (((size_t)of * a.Hkv + head) << lg | (group & (P - 1))) / 16 : 0);
                             asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(
@@ -377,47 +368,64 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_quant_tc(const __gri
         }
     }
     } else if (warp >= kConvertK) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
         if (work) {
         // ------------------------------------------------------ converters
         const bool is_v = warp >= kConvertV;
-        const int v = warp & 3;
+        // The warp has 32 keys of each tile.  In a step, 8 keys and 64 features, 8 lanes have two keys that differ in bits
+        // 0 and 2, so that neither their reads nor their writes meet in a bank.
+        constexpr int kUnits = D / 16, kPanels = D / 64;
+        const int c = lane & 3, octet = lane >> 3 ^ (lane & 4 ? 5 : 0), key0 = 32 * (warp & 3);
         const uint32_t n_slots = is_v ? NV : NK;
         uint64_t *my_full = is_v ? full + NK : full, *my_empty = is_v ? empty + NK : empty;
-        const uint32_t my_ring = smem_u32(is_v ? ring + (size_t)NK * kCodes : ring), my_tiles = smem_u32(is_v ? tile_v : tile_k);
-        RingPos pos{0, 0}, to{0, 1};
-        uint32_t n = 0;                                    // tiles so far
+        uint64_t *done = is_v ? vfull : kfull, *free = is_v ? vempty : kempty;
+        const uint32_t my_ring = smem_u32(is_v ? ring + (size_t)NK * kCodes : ring) + (key0 + octet) * D;
+        const uint32_t my_tile = smem_u32(is_v ? tile_v : tile_k) + (key0 + octet) * 128;
+        RingPos pos{0, 0};
+        uint32_t n = 0;                                     // tiles so far
         bool ok = true;
         while (ok && w.next(a)) {
-            for (int i = w.i0; i < w.i1; ++i) {
-                const int j0 = key_tile(w.vis, i) * kTile;
-                const bool edge = is_v && !all_visible(w.vis, j0);
+            Tiles at;
+            at.begin(w);
+            do {
+                const uint32_t b = n & 1;
                 ok = wait_soon(&my_full[pos.slot], pos.phase, fail);
-                ok = ok && wait_soon(is_v ? &vempty[to.slot] : &kempty[to.slot], to.phase, fail);
+                uint4 v[kUnits];
+#pragma unroll
+                for (int x = 0; x < kUnits; ++x)
+                    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
+                                 : "=r"(v[x].x), "=r"(v[x].y), "=r"(v[x].z), "=r"(v[x].w)
+                                 : "r"(my_ring + pos.slot * kCodes + x / kPanels * (8 * D) + (D == 128 ? (4 * (x % kPanels) + c ^ octet) << 4 : c << 4)));
+                if (is_v && !at.whole()) {                  // masked keys are zeros
+#pragma unroll
+                    for (int x = 0; x < kUnits; ++x)
+                        if (!key_visible(w.vis, at.tile * kTile + key0 + 8 * (x / kPanels) + octet)) v[x] = make_uint4(0, 0, 0, 0);
+                }
+                ok = ok && wait_soon(&free[b], ((n >> 1) & 1u) ^ 1u, fail);
                 if (__any_sync(0xffffffffu, !ok)) ok = false;
                 if (!ok) break;
-                const uint32_t codes = my_ring + pos.slot * kCodes + 32 * v * D, rows_of = my_tiles + to.slot * kHalf + 32 * v * 128;
-#pragma unroll 1
-                for (int key = 0; key < 32; key += 16) {
-                    const int j = j0 + 32 * v + key;
-                    if (edge) convert<D, true>(codes + key * D, rows_of + key * 128, kPanel, lane, [&](int x) { return key_visible(w.vis, j + x); });
-                    else convert<D, false>(codes + key * D, rows_of + key * 128, kPanel, lane, [](int) { return true; });
+#pragma unroll
+                for (int x = 0; x < kUnits; ++x) {
+                    const uint32_t word[4] = {v[x].x, v[x].y, v[x].z, v[x].w};
+                    uint32_t f[8];
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) quant::decode4(word[y], f[2 * y], f[2 * y + 1]);
+                    const uint32_t row = my_tile + b * kHalf + x % kPanels * kPanel + x / kPanels * 1024;
+#pragma unroll
+                    for (int y = 0; y < 2; ++y)
+                        asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(row + (((2 * c + y) ^ octet) << 4)), "r"(f[4 * y]),
+                                     "r"(f[4 * y + 1]), "r"(f[4 * y + 2]), "r"(f[4 * y + 3])
+                                     : "memory");
                 }
-                // log2 of the scales of V, for the softmax
-                if (warp == kConvertK && lane < 8) {
-                    float *vs = scales + n % kScaleTiles * 16 + 8 + lane;
-                    *vs = lg2(*vs);
-                }
-                ++n;
                 fence_proxy_async_smem();
                 __syncwarp();
                 if (lane == 0) {
-                    mbar_arrive(is_v ? &vfull[to.slot] : &kfull[to.slot]);
+                    mbar_arrive(&done[b]);
                     mbar_arrive(&my_empty[pos.slot]);
                 }
-                to.step(kTiles);
                 pos.step(n_slots);
-            }
+                ++n;
+            } while (at.step());
         }
         }
     } else {
@@ -502,11 +510,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_quant_tc(const __gri
         while (go) {            // left by a vote at a segment's end only, so that the warps of a row stay together
             float m = -INFINITY, mo = -INFINITY;            // references of l (this thread's), and of O (the row's)
             float l = 0.f;                                  // sum over this thread's keys
-            for (int i = w.i0; i < w.i1; ++i, ++n) {
+            Tiles tiles;
+            tiles.begin(w);
+            do {
                 const uint32_t b = n & 1;
-                const int j0 = key_tile(w.vis, i) * kTile;
-                const bool edge = !all_visible(w.vis, j0);
-                const int k0 = j0 + key0, hi = w.vis.len - k0, lo = w.vis.lo - k0, sink = w.vis.sink - k0;
                 auto below = [](int k) { return k >= 32 ? ~0u : (k <= 0 ? 0u : (1u << k) - 1); };
                 wait(&sready[b], (n >> 1) & 1u);
                 tc_fence_after();
@@ -520,7 +527,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_quant_tc(const __gri
                 read_scales(my_scales, fk);
                 read_scales(my_scales + 8, lv);
 #pragma unroll
-                for (int g = 0; g < kGroups; ++g) fk[g] = fminf(fmaxf(fk[g] * kc, 0x1p-126f), kMax);
+                for (int g = 0; g < kGroups; ++g) {
+                    fk[g] = fminf(fmaxf(fk[g] * kc, 0x1p-126f), kMax);
+                    lv[g] = lg2(lv[g]);
+                }
                 // scores from Tensor Memory, the masked ones replaced
                 float s[kKeys / kSpan][kSpan];
 #pragma unroll
@@ -529,7 +539,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_quant_tc(const __gri
                     else tmem_ld16(my_s + key0, s[x]);
                 }
                 tmem_wait_ld();
-                if (edge) {
+                if (!tiles.whole()) {
+                    const int k0 = tiles.tile * kTile + key0, hi = w.vis.len - k0, lo = w.vis.lo - k0, sink = w.vis.sink - k0;
 #pragma unroll
                     for (int x = 0; x < kKeys / kSpan; ++x) {
                         const unsigned see = below(hi - 32 * x) & (~below(lo - 32 * x) | below(sink - 32 * x));
@@ -608,7 +619,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_quant_tc(const __gri
                 }
                 tmem_wait_st();
                 arrive(&pready[b]);
-            }
+                ++n;
+            } while (tiles.step());
             // the next segment's Q: its first products are formed beside the output of this one
             const Walk done = w;
             go = w.next(a);
