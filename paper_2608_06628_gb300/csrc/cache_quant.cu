@@ -1,17 +1,21 @@
 // cache_quant.cu -- the paged cache in 8 bits: keys and values rounded as they are written, with
-// the keys' norm and rotation in the same pass (hybrid_qk_norm_rope_cache_quant), and tokens read
-// back (hybrid_cache_dequant).  The format is in quant.cuh.
+// the norms and rotations of keys and queries in the same pass (hybrid_qk_norm_rope_cache_quant),
+// and tokens read back (hybrid_cache_dequant).  The format is in quant.cuh.
 //
 // Write.  A scale belongs to 16 tokens of a head, so the tokens of one group that a call writes
-// (a run: they stand side by side, but for tokens without a slot) are held together: a warp has a run's rows of one head, of K
-// or of V, in registers, up to 16 rows of d float32 (64 registers a lane at d = 128), and
+// (a run: they stand side by side, but for tokens without a slot) are held together: a warp has a
+// run's rows of one head, of K or of V, and
 //     y = norm and rotation of x (K),   amax = max |y| over the run
 //     E = least power of two with amax <= 448 * 2^E; no less than the group's old one, unless
 //         the run has the group's first slot
 //     code = e4m3(y / 2^E)
-// then brings the group's other tokens to 2^E (zeros where the group starts afresh).  A block
-// takes a window of the packed tokens and the runs that begin in it, one after another; its warps
-// share a run's angles and take its heads.  Queries go through qk_norm_rope.cu's kernel.
+// then brings the group's other tokens to 2^E (zeros where the group starts afresh).  A block has
+// a window of the packed tokens: its queries, and the runs that begin in it.  It forms the window's
+// angles once; its warps share the pieces of work (a run's head; some steps of queries), and each
+// copies the rows of its next piece to shared memory while it works on one (cp.async, a lane
+// only what it reads itself).  A run's rows are formed twice, for the maximum and for the codes: that
+// costs less than 64 registers a lane to keep them, and loops over the steps instead of unrolled
+// ones keep the code within the instruction cache.
 #include "quant.cuh"
 #include "rope_rows.cuh"
 
@@ -33,101 +37,111 @@ struct Run {
     __device__ bool has(int r) const { return members >> r & 1u; }
 };
 
-// One head of a run, K (kLayout: of the rotated pairs) or V (norm and rotation left out).
-template <typename T, int D, Layout kLayout, bool kKey>
-__device__ __forceinline__ void write_head(const RopeArgs &a, const Run &run, int head, const float2 *angles)
-{
-    constexpr int E = Vec<T>::E, L = D / E, RPW = 32 / L, kSteps = kGroup / RPW;
-    const int lane = threadIdx.x & 31, sub = lane / L;
-    const Pieces<D, E, kLayout> piece(a, lane % L);
-    const int apart = piece.apart();
-    const T *src = static_cast<const T *>(kKey ? a.K : a.V) + (size_t)head * D + piece.first;
-    const size_t stride = kKey ? a.k_stride : a.v_stride;
+template <typename T, int D> struct Rows {
+    static constexpr int E = Vec<T>::E, L = D / E, RPW = 32 / L;        // elements of a lane, lanes of a row, rows of a step
+    static constexpr int kSteps = kGroup / RPW;                         // of a run, and of a piece of queries
+    static constexpr int kStage = kSteps * 512;                         // bytes of a warp's rows
+    static constexpr int kAngles = (2 * kGroup - 1) * kMaxPairs;
+    static constexpr int kBytes = kWarps * 2 * kStage + kAngles * (int)sizeof(float2);
+};
 
-    uint4 raw[kSteps];
+// A row's norm (w: the weights, null without) and rotation.
+template <int D, int E, bool kInter>
+__device__ __forceinline__ void norm_rotate(f32x2 (&x)[E / 2], bool norm, const f32x2 (&w)[E / 2], float eps, bool turn,
+                                            const float2 *angles, int pair)
+{
+    if (norm) {
+        f32x2 ss = ptx::mul2(x[0], x[0]);
 #pragma unroll
-    for (int i = 0; i < kSteps; ++i) {
-        const int r = i * RPW + sub;
-        raw[i] = run.has(r) ? load<kLayout>(src + (size_t)(run.t + r) * stride, apart) : make_uint4(0, 0, 0, 0);
+        for (int k = 1; k < E / 2; ++k) ss = ptx::fma2(x[k], x[k], ss);
+        const float r = rsqrtf(head_sum<D / E>(both(ss)) * (1.f / D) + eps);
+        const f32x2 rr = pair2(r, r);
+#pragma unroll
+        for (int k = 0; k < E / 2; ++k) x[k] = ptx::mul2(ptx::mul2(x[k], rr), w[k]);
     }
-    f32x2 x[kSteps][E / 2];
+    if (turn) {
+        Rotation<E, kInter> rot;
+        read_rotation(angles, pair, rot);
+        rotate<E, kInter>(x, rot);
+    }
+}
+
+// One head of a run, K or V (norm and rotation left out), into the cache.  `rows`: this lane's place in its stage;
+// `angles`: of the run's first token.
+template <typename T, int D, Layout kLayout>
+__device__ __forceinline__ void write_head(const RopeArgs &a, const Run &run, bool key, int head, uint32_t rows, const float2 *angles)
+{
+    using R = Rows<T, D>;
+    constexpr int E = R::E;
+    const int lane = threadIdx.x & 31, sub = lane / R::L;
+    const Pieces<D, E, kLayout> piece(a, lane % R::L);
+    const int apart = piece.apart();
+    const size_t row = (((size_t)run.page * a.Hkv + head) * a.page_size + run.off);     // the group's first token
+    float *scale = (key ? a.K_scale : a.V_scale) + row / kGroup;
+    uint8_t *codes = static_cast<uint8_t *>(key ? a.K_cache : a.V_cache) + row * D;
+    const bool fresh = run.written & 1u;
+    const float old = fresh ? 0.f : *scale;                 // under way beside the arithmetic
+    const bool norm = key && a.wk, turn = key && a.rot > 0 && piece.on;
+    f32x2 w[E / 2];
+    if (norm) Vec<T>::unpack(load<kLayout>(static_cast<const T *>(a.wk) + piece.first, apart), w);
+    const int steps = (run.n + R::RPW - 1) / R::RPW;
+    // this lane's part of row step * RPW + sub (zeros where the run has none)
+    auto form = [&](int step, float (&y)[E]) {
+        const int r = step * R::RPW + sub;
+        f32x2 x[E / 2];
+        Vec<T>::unpack(ring_load(rows + 512 * step), x);
+        norm_rotate<D, E, kLayout == kInterleaved>(x, norm, w, a.eps, turn, angles + r * kMaxPairs, piece.pair);
+        const bool has = run.has(r);
 #pragma unroll
-    for (int i = 0; i < kSteps; ++i) Vec<T>::unpack(raw[i], x[i]);
-    if (kKey && a.wk) {
-        f32x2 w[E / 2];
-        Vec<T>::unpack(load<kLayout>(static_cast<const T *>(a.wk) + piece.first, apart), w);
-#pragma unroll
-        for (int i = 0; i < kSteps; ++i) {
-            if (i * RPW >= run.n) break;
-            f32x2 ss = ptx::mul2(x[i][0], x[i][0]);
-#pragma unroll
-            for (int k = 1; k < E / 2; ++k) ss = ptx::fma2(x[i][k], x[i][k], ss);
-            const float r = rsqrtf(head_sum<L>(both(ss)) * (1.f / D) + a.eps);
-            const f32x2 rr = pair2(r, r);
-#pragma unroll
-            for (int k = 0; k < E / 2; ++k) x[i][k] = ptx::mul2(ptx::mul2(x[i][k], rr), w[k]);
+        for (int k = 0; k < E / 2; ++k) {
+            ptx::unpair2(x[k], y[2 * k], y[2 * k + 1]);
+            if (!has) y[2 * k] = y[2 * k + 1] = 0.f;
         }
-    }
-    if (kKey && a.rot > 0 && piece.on) {
-#pragma unroll
-        for (int i = 0; i < kSteps; ++i) {
-            const int r = i * RPW + sub;
-            if (!run.has(r)) continue;
-            Rotation<E, kLayout == kInterleaved> rot;
-            read_rotation(angles + r * kMaxPairs, piece.pair, rot);
-            rotate<E, kLayout == kInterleaved>(x[i], rot);
-        }
-    }
-    // the largest magnitude, as bits; beyond 0x7f7fffff there are infinities or NaN, which are left out
-    uint32_t amax = 0;
-    auto each = [&](auto f) {
-#pragma unroll
-        for (int i = 0; i < kSteps; ++i)
-            if (run.has(i * RPW + sub))
-#pragma unroll
-                for (int k = 0; k < E / 2; ++k) {
-                    float lo, hi;
-                    ptx::unpair2(x[i][k], lo, hi);
-                    f(lo, hi);
-                    x[i][k] = pair2(lo, hi);
-                }
     };
     auto magnitude = [](float v) { return __float_as_uint(v) & 0x7fffffffu; };
-    each([&](float &lo, float &hi) { amax = max(amax, max(magnitude(lo), magnitude(hi))); });
+    // the largest magnitude, as bits; from 0x7f800000 on there are infinities or NaN, which are left out
+    uint32_t amax = 0;
+#pragma unroll 2
+    for (int i = 0; i < steps; ++i) {
+        float y[E];
+        form(i, y);
+#pragma unroll
+        for (int k = 0; k < E; ++k) amax = max(amax, magnitude(y[k]));
+    }
     amax = __reduce_max_sync(0xffffffffu, amax);
-    if (amax >= 0x7f800000u) {
+    const bool wild = amax >= 0x7f800000u;
+    if (wild) {
         amax = 0;
-        each([&](float &lo, float &hi) {
-            for (float *v : {&lo, &hi}) {
-                if (magnitude(*v) < 0x7f800000u) amax = max(amax, magnitude(*v));
-                else *v = __uint_as_float(0x7fc00000u);
-            }
-        });
+#pragma unroll 1
+        for (int i = 0; i < steps; ++i) {
+            float y[E];
+            form(i, y);
+#pragma unroll
+            for (int k = 0; k < E; ++k)
+                if (magnitude(y[k]) < 0x7f800000u) amax = max(amax, magnitude(y[k]));
+        }
         amax = __reduce_max_sync(0xffffffffu, amax);
     }
-    const size_t row = (((size_t)run.page * a.Hkv + head) * a.page_size + run.off);     // the group's first token
-    float *scale = (kKey ? a.K_scale : a.V_scale) + row / kGroup;
-    uint8_t *codes = static_cast<uint8_t *>(kKey ? a.K_cache : a.V_cache) + row * D;
-    const bool fresh = run.written & 1u;
     int e = scale_of_amax(amax), has = e;
     if (!fresh) {
-        has = scale_of_bits(__float_as_uint(*scale));
+        has = scale_of_bits(__float_as_uint(old));
         e = max(e, has);
     }
     const float inv = scale_inverse(e);
-#pragma unroll
-    for (int i = 0; i < kSteps; ++i) {
-        const int r = i * RPW + sub;
-        const int to = __shfl_sync(0xffffffffu, run.slot, r) % kGroup;
-        if (!run.has(r)) continue;
+#pragma unroll 2
+    for (int i = 0; i < steps; ++i) {
+        const int r = i * R::RPW + sub, to = __shfl_sync(0xffffffffu, run.slot, r & 31) % kGroup;
+        float y[E];
+        form(i, y);
         uint32_t c[E / 4];
 #pragma unroll
-        for (int k = 0; k < E / 2; k += 2) {
-            float v0, v1, v2, v3;
-            ptx::unpair2(x[i][k], v0, v1);
-            ptx::unpair2(x[i][k + 1], v2, v3);
-            c[k / 2] = encode4(v0 * inv, v1 * inv, v2 * inv, v3 * inv);
+        for (int k = 0; k < E; ++k) {
+            if (wild && magnitude(y[k]) >= 0x7f800000u) y[k] = __uint_as_float(0x7fc00000u);
+            y[k] *= inv;
         }
+#pragma unroll
+        for (int k = 0; k < E; k += 4) c[k / 4] = encode4(y[k], y[k + 1], y[k + 2], y[k + 3]);
+        if (!run.has(r)) continue;
         uint8_t *dst = codes + to * D + piece.first;
         if constexpr (E == 8) {
             if (kLayout == kInterleaved) {
@@ -164,48 +178,146 @@ __device__ __forceinline__ void write_head(const RopeArgs &a, const Run &run, in
     if (lane == 0 && (fresh || e != has)) *scale = scale_value(e);
 }
 
+// Steps of queries of a window: step s has RPW heads of its token s / steps.
+struct Steps {
+    int token, head;
+    __device__ Steps(int s, int steps, int rpw, int sub)
+    {
+        token = s / steps;
+        head = (s - token * steps) * rpw + sub;
+    }
+    __device__ void next(int heads, int rpw, int sub)       // (`head` may lie behind the last: a padded step)
+    {
+        head += rpw;
+        if (head - sub >= heads) {
+            head = sub;
+            ++token;
+        }
+    }
+};
+
 template <typename T, int D, Layout kLayout>
-__global__ __launch_bounds__(kThreads, 2) void k_cache_quant(const RopeArgs a, int window)
+__global__ __launch_bounds__(kThreads, 2) void k_cache_write(const RopeArgs a, int window)
 {
-    __shared__ float2 s_angles[kGroup * kMaxPairs];
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int t0 = blockIdx.x * window, t1 = min(t0 + window, a.n_tok);
+    using R = Rows<T, D>;
+    constexpr int E = R::E, RPW = R::RPW;
+    extern __shared__ __align__(16) unsigned char s_raw[];
+    float2 *s_angles = reinterpret_cast<float2 *>(s_raw + kWarps * 2 * R::kStage);
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, sub = lane / R::L;
+    const int t0 = blockIdx.x * window, n_win = min(window, a.n_tok - t0);
+    const uint32_t stage0 = ptx::smem_u32(s_raw) + warp * (2 * R::kStage) + 16 * lane;
+    const Pieces<D, E, kLayout> piece(a, lane % R::L);
     ptx::griddep_wait();
     ptx::griddep_launch_dependents();
-    for (int t = t0; t < t1; ++t) {
-        // the run that begins at token t
-        // tokens t ... t + 15, and in the upper lanes t - 16 ... t - 1
-        const int token = lane < kGroup ? t + lane : t - 32 + lane;
+    // Groups of the tokens t0 - 16 ... t0 + 15 and t0 + 16 ... t0 + 31, -1 without a slot; each warp for itself.
+    auto slot_at = [&](int t) { return t >= 0 && t < a.n_tok ? __ldg(a.slots + t) : -1; };
+    const int slot0 = slot_at(t0 - kGroup + lane), slot1 = lane < kGroup ? slot_at(t0 + kGroup + lane) : -1;
+    const int slots = a.n_pages * a.page_size;
+    const int of0 = slot0 >= 0 && slot0 < slots ? slot0 / kGroup : -1, of1 = slot1 >= 0 && slot1 < slots ? slot1 / kGroup : -1;
+    if (blockIdx.y == 0 && warp == 0 && lane >= kGroup && lane < kGroup + n_win && slot0 >= slots) raise_error(a.err, ERR_BAD_INDEX);
+    // A run begins at a token of the window unless the last token with a slot before it, of the 15 before, is of its group.
+    const unsigned live = __ballot_sync(0xffffffffu, of0 >= 0);
+    const unsigned earlier = live & ((1u << lane) - 1);
+    const int last = earlier ? 31 - __clz(earlier) : 0;
+    const int group_before = __shfl_sync(0xffffffffu, of0, last);
+    const unsigned starts = __ballot_sync(0xffffffffu, of0 >= 0 && lane >= kGroup && lane < kGroup + n_win &&
+                                                           !(earlier && lane - last < kGroup && group_before == of0));
+    auto run_from = [&](int at) {                           // lane `at` of of0
         Run run;
-        run.slot = token >= 0 && token < a.n_tok ? __ldg(a.slots + token) : -1;
-        const int of = run.slot >= 0 && run.slot < a.n_pages * a.page_size ? run.slot / kGroup : -1;
-        const int group = __shfl_sync(0xffffffffu, of, 0);
-        if (group < 0) {
-            if (tid == 0 && run.slot >= 0) raise_error(a.err, ERR_BAD_INDEX);
-            continue;
-        }
-        // no token of the group in the 15 before, up to the last one of another group
-        const unsigned same = __ballot_sync(0xffffffffu, of == group), other = __ballot_sync(0xffffffffu, of >= 0 && of != group);
-        const unsigned before = other >> 16;
-        if ((same >> 17 & ~0u << (before ? 31 - __clz(before) : 0)) != 0) continue;
-        run.members = same & 0xffffu & ((other & 0xffffu) != 0 ? (1u << (__ffs(other) - 1)) - 1 : 0xffffu);
-        run.t = t;
+        const int group = __shfl_sync(0xffffffffu, of0, at), from = at + lane;          // tokens t ... t + 15
+        const int g0 = __shfl_sync(0xffffffffu, of0, from & 31), g1 = __shfl_sync(0xffffffffu, of1, from & 31);
+        const int s0 = __shfl_sync(0xffffffffu, slot0, from & 31), s1 = __shfl_sync(0xffffffffu, slot1, from & 31);
+        const int of = from < 32 ? g0 : g1;
+        run.slot = from < 32 ? s0 : s1;
+        const unsigned same = __ballot_sync(0xffffffffu, lane < kGroup && of == group);
+        const unsigned other = __ballot_sync(0xffffffffu, lane < kGroup && of >= 0 && of != group);
+        run.members = other ? same & ((1u << (__ffs(other) - 1)) - 1) : same;
+        run.t = t0 + at - kGroup;
         run.n = 32 - __clz(run.members);
         run.written = __reduce_or_sync(0xffffffffu, lane < kGroup && run.has(lane) ? 1u << run.slot % kGroup : 0u);
         run.page = group * kGroup / a.page_size;
         run.off = group * kGroup - run.page * a.page_size;
-        const int half = a.rot >> 1;
-        if (half > 0) {
-            __syncthreads();                        // the last run's have been read
-            for (int x = tid; x < run.n * kMaxPairs; x += kThreads) {
-                const int pair = x % kMaxPairs;
-                if (pair < half && run.has(x / kMaxPairs)) s_angles[x] = angle(a, t + x / kMaxPairs, pair);
+        return run;
+    };
+    const int heads = 2 * a.Hkv, n_heads = __popc(starts) * heads;
+    const int steps = (a.Hq + RPW - 1) / RPW, n_steps = a.Q ? n_win * steps : 0;
+    const int n_work = n_heads + (n_steps + R::kSteps - 1) / R::kSteps;
+    // the run of a piece of work that is a head
+    auto run_of = [&](int work, int &head) {
+        const int nth = work / heads;
+        unsigned left = starts;
+        for (int x = 0; x < nth; ++x) left &= left - 1;
+        head = work - nth * heads;
+        return run_from(__ffs(left) - 1);
+    };
+    // copies of a piece's rows, as one group of them
+    auto copy = [&](int work, uint32_t to) {
+        if (work < n_heads) {
+            int head;
+            const Run run = run_of(work, head);
+            const bool key = head < a.Hkv;
+            const size_t stride = key ? a.k_stride : a.v_stride;
+            const T *src = static_cast<const T *>(key ? a.K : a.V) + (size_t)(run.t + sub) * stride +
+                           (size_t)(key ? head : head - a.Hkv) * D + piece.first;
+#pragma unroll 4
+            for (int i = 0; i * RPW < run.n; ++i) {
+                copy_async<kLayout>(to + 512 * i, src, piece.apart(), run.has(i * RPW + sub));
+                src += RPW * stride;
             }
-            __syncthreads();
+        } else if (work < n_work) {
+            const int s0 = (work - n_heads) * R::kSteps, n = min(R::kSteps, n_steps - s0);
+            Steps at(s0, steps, RPW, sub);
+#pragma unroll 4
+            for (int i = 0; i < n; ++i) {
+                const T *src = static_cast<const T *>(a.Q) + (size_t)(t0 + at.token) * a.q_stride + (size_t)at.head * D + piece.first;
+                copy_async<kLayout>(to + 512 * i, src, piece.apart(), at.head < a.Hq);
+                at.next(a.Hq, RPW, sub);
+            }
         }
-        for (int x = blockIdx.y * kWarps + warp; x < 2 * a.Hkv; x += gridDim.y * kWarps) {
-            if (x < a.Hkv) write_head<T, D, kLayout, true>(a, run, x, s_angles);
-            else write_head<T, D, kInterleaved, false>(a, run, x - a.Hkv, s_angles);
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    int work = blockIdx.y * kWarps + warp, b = 0;
+    copy(work, stage0);
+    const int half = a.rot >> 1;
+    if (half > 0) {
+        // the tokens whose angles are used: the window's for queries, the runs' for keys
+        int n_angles = a.Q ? n_win : 0;
+        if (starts) {
+            const Run tail = run_from(31 - __clz(starts));
+            n_angles = max(n_angles, tail.t - t0 + tail.n);
+        }
+        for (int x = tid; x < n_angles * kMaxPairs; x += kThreads) {
+            const int pair = x % kMaxPairs;
+            if (pair < half) s_angles[x] = angle(a, t0 + x / kMaxPairs, pair);
+        }
+        __syncthreads();
+    }
+#pragma unroll 1
+    for (; work < n_work; b ^= 1) {
+        const int now = work;
+        const uint32_t rows = stage0 + b * R::kStage;
+        work += gridDim.y * kWarps;
+        copy(work, stage0 + (b ^ 1) * R::kStage);
+        asm volatile("cp.async.wait_group 1;" ::: "memory");
+        if (now < n_heads) {
+            int head;
+            const Run run = run_of(now, head);
+            const bool key = head < a.Hkv;
+            write_head<T, D, kLayout>(a, run, key, key ? head : head - a.Hkv, rows, s_angles + (run.t - t0) * kMaxPairs);
+        } else {
+            const int s0 = (now - n_heads) * R::kSteps, n = min(R::kSteps, n_steps - s0);
+            f32x2 w[E / 2];
+            if (a.wq) Vec<T>::unpack(load<kLayout>(static_cast<const T *>(a.wq) + piece.first, piece.apart()), w);
+            Steps at(s0, steps, RPW, sub);
+#pragma unroll 4
+            for (int i = 0; i < n; ++i) {
+                f32x2 x[E / 2];
+                Vec<T>::unpack(ring_load(rows + 512 * i), x);
+                norm_rotate<D, E, kLayout == kInterleaved>(x, a.wq, w, a.eps, a.rot > 0 && piece.on, s_angles + at.token * kMaxPairs, piece.pair);
+                store<kLayout>(static_cast<T *>(a.Qo) + ((size_t)(t0 + at.token) * a.Hq + at.head) * D + piece.first, piece.apart(),
+                               Vec<T>::pack(x), at.head < a.Hq);
+                at.next(a.Hq, RPW, sub);
+            }
         }
     }
 }
@@ -217,10 +329,15 @@ template <typename T, int D, Layout kLayout> cudaError_t launch_write(const Rope
     const int held = 2 * pipe::sm_count();
     int window = (a.n_tok + held - 1) / held;
     if (window > kGroup) window = kGroup;
-    const int blocks = (a.n_tok + window - 1) / window, rounds = (2 * a.Hkv + kWarps - 1) / kWarps;
+    const int blocks = (a.n_tok + window - 1) / window;
+    const int steps = a.Q ? (a.Hq + Rows<T, D>::RPW - 1) / Rows<T, D>::RPW * window : 0;
+    const int pieces = 2 * a.Hkv + (steps + Rows<T, D>::kSteps - 1) / Rows<T, D>::kSteps, rounds = (pieces + kWarps - 1) / kWarps;
     int y = held / blocks;
     y = y < 1 ? 1 : (y > rounds ? rounds : y);
-    return pipe::launch_early(k_cache_quant<T, D, kLayout>, dim3(blocks, y), dim3(kThreads), 0, st, a, window);
+    static std::atomic<unsigned long long> opted{0};
+    const cudaError_t e = pipe::opt_in(reinterpret_cast<const void *>(&k_cache_write<T, D, kLayout>), Rows<T, D>::kBytes, opted);
+    if (e != cudaSuccess) return e;
+    return pipe::launch_early(k_cache_write<T, D, kLayout>, dim3(blocks, y), dim3(kThreads), Rows<T, D>::kBytes, st, a, window);
 }
 template <typename T, int D> cudaError_t launch_write(const RopeArgs &a, cudaStream_t st)
 {
@@ -281,13 +398,6 @@ template <typename T, int D> cudaError_t launch_read(const DequantArgs &a, cudaS
 
 cudaError_t launch_qk_norm_rope_cache_quant(hybrid_dtype dt, const RopeArgs &a, cudaStream_t st)
 {
-    if (a.Q) {
-        RopeArgs q = a;                             // the queries alone
-        q.K = nullptr;
-        q.slots = nullptr;
-        const cudaError_t e = launch_qk_norm_rope(dt, q, st);
-        if (e != cudaSuccess) return e;
-    }
     if (dt == HYBRID_BF16) return a.d == 128 ? launch_write<__nv_bfloat16, 128>(a, st) : launch_write<__nv_bfloat16, 64>(a, st);
     return a.d == 128 ? launch_write<float, 128>(a, st) : launch_write<float, 64>(a, st);
 }
