@@ -27,6 +27,8 @@ using namespace quant;
 
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
+constexpr int kWindow = 48;             // most tokens of a window
+constexpr int kReach = kWindow + kGroup - 1;    // and of the runs that begin in it
 
 struct Run {
     int t, n;                   // first token, and tokens up to the last one
@@ -37,39 +39,72 @@ struct Run {
     __device__ bool has(int r) const { return members >> r & 1u; }
 };
 
+constexpr int kTable = 3 * kMaxPairs;    // floats of a token's angles: cosines, sines, and sines with the other sign
+
 template <typename T, int D> struct Rows {
     static constexpr int E = Vec<T>::E, L = D / E, RPW = 32 / L;        // elements of a lane, lanes of a row, rows of a step
     static constexpr int kSteps = kGroup / RPW;                         // of a run, and of a piece of queries
-    static constexpr int kStage = kSteps * 512;                         // bytes of a warp's rows
-    static constexpr int kAngles = (2 * kGroup - 1) * kMaxPairs;
-    static constexpr int kBytes = kWarps * 2 * kStage + kAngles * (int)sizeof(float2);
+    static constexpr int kKeys = kGroup * D;                            // floats of a run's keys
+    static constexpr int kBytes = (kWarps * kKeys + kReach * kTable) * (int)sizeof(float);
 };
 
-// A row's norm (w: the weights, null without) and rotation.
-template <int D, int E, bool kInter>
-__device__ __forceinline__ void norm_rotate(f32x2 (&x)[E / 2], bool norm, const f32x2 (&w)[E / 2], float eps, bool turn,
-                                            const float2 *angles, int pair)
+// This lane's pairs of a token's angles, from pair0 on.
+template <int E, bool kInter> __device__ __forceinline__ void read_angles(const float *table, int pair0, Rotation<E, kInter> &r)
 {
-    if (norm) {
-        f32x2 ss = ptx::mul2(x[0], x[0]);
+    if constexpr (kInter) {
 #pragma unroll
-        for (int k = 1; k < E / 2; ++k) ss = ptx::fma2(x[k], x[k], ss);
-        const float r = rsqrtf(head_sum<D / E>(both(ss)) * (1.f / D) + eps);
-        const f32x2 rr = pair2(r, r);
-#pragma unroll
-        for (int k = 0; k < E / 2; ++k) x[k] = ptx::mul2(ptx::mul2(x[k], rr), w[k]);
-    }
-    if (turn) {
-        Rotation<E, kInter> rot;
-        read_rotation(angles, pair, rot);
-        rotate<E, kInter>(x, rot);
+        for (int i = 0; i < E / 2; ++i) {
+            const float c = table[pair0 + i], s = table[kMaxPairs + pair0 + i], ns = table[2 * kMaxPairs + pair0 + i];
+            r.c[i] = pair2(c, c);
+            r.s[i] = pair2(ns, s);
+        }
+    } else if constexpr (E == 8) {
+        auto two = [](const float *p, f32x2 (&v)[2]) {
+            const ulonglong2 x = *reinterpret_cast<const ulonglong2 *>(p);
+            v[0].v = x.x;
+            v[1].v = x.y;
+        };
+        two(table + pair0, r.c);
+        two(table + kMaxPairs + pair0, r.s);
+        two(table + 2 * kMaxPairs + pair0, r.ns);
+    } else {
+        r.c[0].v = *reinterpret_cast<const unsigned long long *>(table + pair0);
+        r.s[0].v = *reinterpret_cast<const unsigned long long *>(table + kMaxPairs + pair0);
+        r.ns[0].v = *reinterpret_cast<const unsigned long long *>(table + 2 * kMaxPairs + pair0);
     }
 }
 
-// One head of a run, K or V (norm and rotation left out), into the cache.  `rows`: this lane's place in its stage;
-// `angles`: of the run's first token.
-template <typename T, int D, Layout kLayout>
-__device__ __forceinline__ void write_head(const RopeArgs &a, const Run &run, bool key, int head, uint32_t rows, const float2 *angles)
+__device__ __forceinline__ float max3_nan(float x, float y, float z)
+{
+    float r;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(x), "f"(y), "f"(z));
+    return r;
+}
+// 1 / norm of a row, and the row times that and the weights.
+template <int D, int E> __device__ __forceinline__ float row_factor(const f32x2 (&x)[E / 2], float eps)
+{
+    f32x2 ss = ptx::mul2(x[0], x[0]);
+#pragma unroll
+    for (int k = 1; k < E / 2; ++k) ss = ptx::fma2(x[k], x[k], ss);
+    return rsqrtf(head_sum<D / E>(both(ss)) * (1.f / D) + eps);
+}
+template <int E> __device__ __forceinline__ void scale_row(f32x2 (&x)[E / 2], float r, const f32x2 (&w)[E / 2])
+{
+    const f32x2 rr = pair2(r, r);
+#pragma unroll
+    for (int k = 0; k < E / 2; ++k) x[k] = ptx::mul2(ptx::mul2(x[k], rr), w[k]);
+}
+
+// Whether a magnitude, as bits, is infinite or NaN.
+__device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7fffffffu; }
+__device__ __forceinline__ bool wild(uint32_t magnitude) { return magnitude >= 0x7f800000u; }
+
+// One head of a run, K or V, into the cache, from its rows; the keys' norm and rotation first (`angles`: of the run's first
+// token).  The keys wait in shared memory (`mine`: a lane's own part of a step is 16 bytes of every 512) for the
+// scale that their maximum decides; the values in their registers.
+template <typename T, int D, Layout kLayout, bool kKey>
+__device__ __forceinline__ void write_head(const RopeArgs &a, const Run &run, int head, const uint4 (&raw)[Rows<T, D>::kSteps],
+                                           const float *angles, uint32_t mine)
 {
     using R = Rows<T, D>;
     constexpr int E = R::E;
@@ -77,48 +112,67 @@ __device__ __forceinline__ void write_head(const RopeArgs &a, const Run &run, bo
     const Pieces<D, E, kLayout> piece(a, lane % R::L);
     const int apart = piece.apart();
     const size_t row = (((size_t)run.page * a.Hkv + head) * a.page_size + run.off);     // the group's first token
-    float *scale = (key ? a.K_scale : a.V_scale) + row / kGroup;
-    uint8_t *codes = static_cast<uint8_t *>(key ? a.K_cache : a.V_cache) + row * D;
+    float *scale = (kKey ? a.K_scale : a.V_scale) + row / kGroup;
+    uint8_t *codes = static_cast<uint8_t *>(kKey ? a.K_cache : a.V_cache) + row * D;
     const bool fresh = run.written & 1u;
     const float old = fresh ? 0.f : *scale;                 // under way beside the arithmetic
-    const bool norm = key && a.wk, turn = key && a.rot > 0 && piece.on;
     f32x2 w[E / 2];
-    if (norm) Vec<T>::unpack(load<kLayout>(static_cast<const T *>(a.wk) + piece.first, apart), w);
-    const int steps = (run.n + R::RPW - 1) / R::RPW;
-    // this lane's part of row step * RPW + sub (zeros where the run has none)
-    auto form = [&](int step, float (&y)[E]) {
-        const int r = step * R::RPW + sub;
-        f32x2 x[E / 2];
-        Vec<T>::unpack(ring_load(rows + 512 * step), x);
-        norm_rotate<D, E, kLayout == kInterleaved>(x, norm, w, a.eps, turn, angles + r * kMaxPairs, piece.pair);
-        const bool has = run.has(r);
+    if (kKey && a.wk) Vec<T>::unpack(load<kLayout>(static_cast<const T *>(a.wk) + piece.first, apart), w);
+    // the largest magnitude, infinity or NaN if there is one of them.  (Rows that the run does not have are zeros.)
+    float top = 0.f;
+    auto greatest = [&](const f32x2 (&x)[E / 2]) {
 #pragma unroll
         for (int k = 0; k < E / 2; ++k) {
-            ptx::unpair2(x[k], y[2 * k], y[2 * k + 1]);
-            if (!has) y[2 * k] = y[2 * k + 1] = 0.f;
+            float lo, hi;
+            ptx::unpair2(x[k], lo, hi);
+            top = max3_nan(top, fabsf(lo), fabsf(hi));
         }
     };
-    auto magnitude = [](float v) { return __float_as_uint(v) & 0x7fffffffu; };
-    // the largest magnitude, as bits; from 0x7f800000 on there are infinities or NaN, which are left out
-    uint32_t amax = 0;
-#pragma unroll 2
-    for (int i = 0; i < steps; ++i) {
-        float y[E];
-        form(i, y);
+    auto key_part = [&](int step) { return mine + step * (E * 128); };
 #pragma unroll
-        for (int k = 0; k < E; ++k) amax = max(amax, magnitude(y[k]));
+    for (int i = 0; i < R::kSteps; ++i) {
+        if (i * R::RPW >= run.n) break;
+        f32x2 x[E / 2];
+        Vec<T>::unpack(raw[i], x);
+        if constexpr (kKey) {
+            const int r = i * R::RPW + sub;
+            if (a.wk) {
+                const float f = row_factor<D, E>(x, a.eps);
+                scale_row<E>(x, run.has(r) ? f : 0.f, w);
+            }
+            if (a.rot > 0 && piece.on) {
+                Rotation<E, kLayout == kInterleaved> rot;
+                read_angles(angles + r * kTable, piece.pair, rot);
+                rotate<E, kLayout == kInterleaved>(x, rot);
+            }
+#pragma unroll
+            for (int k = 0; k < E / 4; ++k)
+                asm volatile("st.shared.v2.b64 [%0], {%1, %2};" ::"r"(key_part(i) + 512 * k), "l"(x[2 * k].v), "l"(x[2 * k + 1].v) : "memory");
+        }
+        greatest(x);
     }
-    amax = __reduce_max_sync(0xffffffffu, amax);
-    const bool wild = amax >= 0x7f800000u;
-    if (wild) {
-        amax = 0;
-#pragma unroll 1
-        for (int i = 0; i < steps; ++i) {
-            float y[E];
-            form(i, y);
+    auto read_key = [&](int step, f32x2 (&x)[E / 2]) {
 #pragma unroll
-            for (int k = 0; k < E; ++k)
-                if (magnitude(y[k]) < 0x7f800000u) amax = max(amax, magnitude(y[k]));
+        for (int k = 0; k < E / 4; ++k)
+            asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(x[2 * k].v), "=l"(x[2 * k + 1].v) : "r"(key_part(step) + 512 * k) : "memory");
+    };
+    uint32_t amax = __reduce_max_sync(0xffffffffu, magnitude(top));
+    const bool some_wild = wild(amax);                      // infinities and NaN are left out
+    if (some_wild) {
+        amax = 0;
+#pragma unroll
+        for (int i = 0; i < R::kSteps; ++i) {
+            if (i * R::RPW >= run.n) break;
+            f32x2 x[E / 2];
+            if constexpr (kKey) read_key(i, x);
+            else Vec<T>::unpack(raw[i], x);
+#pragma unroll
+            for (int k = 0; k < E / 2; ++k) {
+                float lo, hi;
+                ptx::unpair2(x[k], lo, hi);
+                if (!wild(magnitude(lo))) amax = max(amax, magnitude(lo));
+                if (!wild(magnitude(hi))) amax = max(amax, magnitude(hi));
+            }
         }
         amax = __reduce_max_sync(0xffffffffu, amax);
     }
@@ -127,22 +181,25 @@ __device__ __forceinline__ void write_head(const RopeArgs &a, const Run &run, bo
         has = scale_of_bits(__float_as_uint(old));
         e = max(e, has);
     }
-    const float inv = scale_inverse(e);
-#pragma unroll 2
-    for (int i = 0; i < steps; ++i) {
+    const f32x2 inv = pair2(scale_inverse(e), scale_inverse(e));
+    auto encode = [&](int i, f32x2 (&x)[E / 2]) {
         const int r = i * R::RPW + sub, to = __shfl_sync(0xffffffffu, run.slot, r & 31) % kGroup;
         float y[E];
-        form(i, y);
+#pragma unroll
+        for (int k = 0; k < E / 2; ++k) {
+            x[k] = ptx::mul2(x[k], inv);
+            ptx::unpair2(x[k], y[2 * k], y[2 * k + 1]);
+        }
+        if (some_wild) {                                    // (what is finite is at most 448 now)
+#pragma unroll
+            for (int k = 0; k < E; ++k)
+                if (wild(magnitude(y[k]))) y[k] = __uint_as_float(0x7fc00000u);
+        }
         uint32_t c[E / 4];
 #pragma unroll
-        for (int k = 0; k < E; ++k) {
-            if (wild && magnitude(y[k]) >= 0x7f800000u) y[k] = __uint_as_float(0x7fc00000u);
-            y[k] *= inv;
-        }
-#pragma unroll
         for (int k = 0; k < E; k += 4) c[k / 4] = encode4(y[k], y[k + 1], y[k + 2], y[k + 3]);
-        if (!run.has(r)) continue;
         uint8_t *dst = codes + to * D + piece.first;
+        if (!run.has(r)) return;
         if constexpr (E == 8) {
             if (kLayout == kInterleaved) {
                 *reinterpret_cast<uint2 *>(dst) = make_uint2(c[0], c[1]);
@@ -157,6 +214,22 @@ __device__ __forceinline__ void write_head(const RopeArgs &a, const Run &run, bo
                 *reinterpret_cast<uint16_t *>(dst) = (uint16_t)c[0];
                 *reinterpret_cast<uint16_t *>(dst + apart) = (uint16_t)(c[0] >> 16);
             }
+        }
+    };
+    if constexpr (kKey) {
+#pragma unroll 2
+        for (int i = 0; i * R::RPW < run.n; ++i) {
+            f32x2 x[E / 2];
+            read_key(i, x);
+            encode(i, x);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < R::kSteps; ++i) {
+            if (i * R::RPW >= run.n) break;
+            f32x2 x[E / 2];
+            Vec<T>::unpack(raw[i], x);
+            encode(i, x);
         }
     }
     if (run.written != 0xffffu && (fresh || e != has)) {
@@ -178,158 +251,202 @@ __device__ __forceinline__ void write_head(const RopeArgs &a, const Run &run, bo
     if (lane == 0 && (fresh || e != has)) *scale = scale_value(e);
 }
 
+// Quotients of x by a number n, x n < 2^32, without a division.
+struct Over {
+    unsigned by;                // 2^32 / n, rounded up; 0: n is 1
+    __host__ static Over of(int n) { return Over{n == 1 ? 0u : (unsigned)(((1ull << 32) + n - 1) / n)}; }
+    __device__ int operator()(int x) const { return by ? (int)__umulhi((unsigned)x, by) : x; }
+};
+
 // Steps of queries of a window: step s has RPW heads of its token s / steps.
 struct Steps {
     int token, head;
-    __device__ Steps(int s, int steps, int rpw, int sub)
+    __device__ Steps(int s, int steps, const Over &over, int rpw, int sub)
     {
-        token = s / steps;
+        token = over(s);
         head = (s - token * steps) * rpw + sub;
     }
-    __device__ void next(int heads, int rpw, int sub)       // (`head` may lie behind the last: a padded step)
+    __device__ bool next(int heads, int rpw, int sub)       // whether a token begins (`head` may lie behind the last: a padded step)
     {
         head += rpw;
-        if (head - sub >= heads) {
-            head = sub;
-            ++token;
-        }
+        if (head - sub < heads) return false;
+        head = sub;
+        ++token;
+        return true;
     }
 };
 
 template <typename T, int D, Layout kLayout>
-__global__ __launch_bounds__(kThreads, 2) void k_cache_write(const RopeArgs a, int window)
+__global__ __launch_bounds__(kThreads, 2) void k_cache_write(const RopeArgs a, int share, int window, int page_lg,
+                                                             const Over over_steps, const Over over_heads)
 {
     using R = Rows<T, D>;
     constexpr int E = R::E, RPW = R::RPW;
-    extern __shared__ __align__(16) unsigned char s_raw[];
-    float2 *s_angles = reinterpret_cast<float2 *>(s_raw + kWarps * 2 * R::kStage);
+    extern __shared__ __align__(16) float s_keys[];         // of each warp's run, then the window's angles
+    float *s_angles = s_keys + kWarps * R::kKeys;
+    __shared__ int s_slot[kGroup + kReach + 1];             // of the tokens from 16 before the window on
+    __shared__ int s_run[kWindow];                          // first tokens of the runs that begin in the window
+    __shared__ int s_runs, s_end;                           // their number, and the end of the last
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, sub = lane / R::L;
-    const int t0 = blockIdx.x * window, n_win = min(window, a.n_tok - t0);
-    const uint32_t stage0 = ptx::smem_u32(s_raw) + warp * (2 * R::kStage) + 16 * lane;
+    const int slots = a.n_pages * a.page_size;
+    const uint32_t mine = ptx::smem_u32(s_keys + warp * R::kKeys) + 16 * lane;
     const Pieces<D, E, kLayout> piece(a, lane % R::L);
     ptx::griddep_wait();
     ptx::griddep_launch_dependents();
-    // Groups of the tokens t0 - 16 ... t0 + 15 and t0 + 16 ... t0 + 31, -1 without a slot; each warp for itself.
-    auto slot_at = [&](int t) { return t >= 0 && t < a.n_tok ? __ldg(a.slots + t) : -1; };
-    const int slot0 = slot_at(t0 - kGroup + lane), slot1 = lane < kGroup ? slot_at(t0 + kGroup + lane) : -1;
-    const int slots = a.n_pages * a.page_size;
-    const int of0 = slot0 >= 0 && slot0 < slots ? slot0 / kGroup : -1, of1 = slot1 >= 0 && slot1 < slots ? slot1 / kGroup : -1;
-    if (blockIdx.y == 0 && warp == 0 && lane >= kGroup && lane < kGroup + n_win && slot0 >= slots) raise_error(a.err, ERR_BAD_INDEX);
-    // A run begins at a token of the window unless the last token with a slot before it, of the 15 before, is of its group.
-    const unsigned live = __ballot_sync(0xffffffffu, of0 >= 0);
-    const unsigned earlier = live & ((1u << lane) - 1);
-    const int last = earlier ? 31 - __clz(earlier) : 0;
-    const int group_before = __shfl_sync(0xffffffffu, of0, last);
-    const unsigned starts = __ballot_sync(0xffffffffu, of0 >= 0 && lane >= kGroup && lane < kGroup + n_win &&
-                                                           !(earlier && lane - last < kGroup && group_before == of0));
-    auto run_from = [&](int at) {                           // lane `at` of of0
+    const int t_begin = blockIdx.x * share, t_end = a.n_tok - t_begin < share ? a.n_tok : t_begin + share;
+    auto slot_at = [&](int t0) {                            // this thread's of the window at t0
+        const long long t = (long long)t0 - kGroup + tid;
+        return tid < kGroup + kReach && t >= 0 && t < a.n_tok ? __ldg(a.slots + t) : -1;
+    };
+    int next_slot = slot_at(t_begin);
+#pragma unroll 1
+    for (int t0 = t_begin, n_win; t0 < t_end; t0 += n_win) {
+    n_win = min(window, t_end - t0);
+    __syncthreads();                                        // the last window is done
+    if (tid < kGroup + kReach) s_slot[tid] = next_slot;
+    if (tid == 0) s_runs = s_end = 0;
+    if (n_win < t_end - t0) next_slot = slot_at(t0 + n_win);
+    __syncthreads();
+    auto group_of = [&](int i) {                            // of token t0 + i, -1 without a slot
+        const int slot = s_slot[kGroup + i];
+        return slot >= 0 && slot < slots ? slot / kGroup : -1;
+    };
+    if (tid < n_win) {
+        // A run begins here unless the last token with a slot before this one, of the 15 before, is of its group.
+        const int mine = group_of(tid);
+        if (mine < 0 && s_slot[kGroup + tid] >= slots && blockIdx.y == 0) raise_error(a.err, ERR_BAD_INDEX);
+        bool begins = mine >= 0;
+        for (int i = 1; begins && i < kGroup; ++i) {
+            const int g = group_of(tid - i);
+            if (g >= 0) {
+                begins = g != mine;
+                break;
+            }
+        }
+        if (begins) {
+            s_run[atomicAdd(&s_runs, 1)] = tid;
+            int end = tid + 1;                              // (in shared memory there is room for 15 tokens behind the window)
+            for (int i = tid + 1; i < tid + kGroup && i < kReach; ++i) {
+                const int g = group_of(i);
+                if (g == mine) end = i + 1;
+                else if (g >= 0) break;
+            }
+            atomicMax(&s_end, end);
+        }
+    }
+    __syncthreads();
+    auto run_from = [&](int at) {                           // the run that begins at token t0 + at
         Run run;
-        const int group = __shfl_sync(0xffffffffu, of0, at), from = at + lane;          // tokens t ... t + 15
-        const int g0 = __shfl_sync(0xffffffffu, of0, from & 31), g1 = __shfl_sync(0xffffffffu, of1, from & 31);
-        const int s0 = __shfl_sync(0xffffffffu, slot0, from & 31), s1 = __shfl_sync(0xffffffffu, slot1, from & 31);
-        const int of = from < 32 ? g0 : g1;
-        run.slot = from < 32 ? s0 : s1;
-        const unsigned same = __ballot_sync(0xffffffffu, lane < kGroup && of == group);
-        const unsigned other = __ballot_sync(0xffffffffu, lane < kGroup && of >= 0 && of != group);
-        run.members = other ? same & ((1u << (__ffs(other) - 1)) - 1) : same;
-        run.t = t0 + at - kGroup;
+        run.slot = lane < kGroup ? s_slot[kGroup + at + lane] : -1;
+        const int of = run.slot >= 0 && run.slot < slots ? run.slot / kGroup : -1, group = __shfl_sync(0xffffffffu, of, 0);
+        const unsigned same = __ballot_sync(0xffffffffu, of == group), other = __ballot_sync(0xffffffffu, of >= 0 && of != group);
+        run.members = (other ? same & ((1u << (__ffs(other) - 1)) - 1) : same) & 0xffffu;
+        run.t = t0 + at;
         run.n = 32 - __clz(run.members);
         run.written = __reduce_or_sync(0xffffffffu, lane < kGroup && run.has(lane) ? 1u << run.slot % kGroup : 0u);
-        run.page = group * kGroup / a.page_size;
-        run.off = group * kGroup - run.page * a.page_size;
+        run.page = group * kGroup >> page_lg;
+        run.off = group * kGroup & (a.page_size - 1);
         return run;
     };
-    const int heads = 2 * a.Hkv, n_heads = __popc(starts) * heads;
+    const int heads = 2 * a.Hkv, n_heads = s_runs * heads;
     const int steps = (a.Hq + RPW - 1) / RPW, n_steps = a.Q ? n_win * steps : 0;
     const int n_work = n_heads + (n_steps + R::kSteps - 1) / R::kSteps;
     // the run of a piece of work that is a head
     auto run_of = [&](int work, int &head) {
-        const int nth = work / heads;
-        unsigned left = starts;
-        for (int x = 0; x < nth; ++x) left &= left - 1;
+        const int nth = over_heads(work);
         head = work - nth * heads;
-        return run_from(__ffs(left) - 1);
+        return run_from(s_run[nth]);
     };
-    // copies of a piece's rows, as one group of them
-    auto copy = [&](int work, uint32_t to) {
+    // a piece's rows
+    uint4 raw[R::kSteps];
+    Run run;
+    int head = 0, s0 = 0, n = 0;
+    auto load_rows = [&](int work) {
         if (work < n_heads) {
-            int head;
-            const Run run = run_of(work, head);
+            run = run_of(work, head);
             const bool key = head < a.Hkv;
             const size_t stride = key ? a.k_stride : a.v_stride;
             const T *src = static_cast<const T *>(key ? a.K : a.V) + (size_t)(run.t + sub) * stride +
                            (size_t)(key ? head : head - a.Hkv) * D + piece.first;
-#pragma unroll 4
-            for (int i = 0; i * RPW < run.n; ++i) {
-                copy_async<kLayout>(to + 512 * i, src, piece.apart(), run.has(i * RPW + sub));
+#pragma unroll
+            for (int i = 0; i < R::kSteps; ++i) {
+                raw[i] = run.has(i * RPW + sub) ? load<kLayout>(src, piece.apart()) : make_uint4(0, 0, 0, 0);
                 src += RPW * stride;
             }
         } else if (work < n_work) {
-            const int s0 = (work - n_heads) * R::kSteps, n = min(R::kSteps, n_steps - s0);
-            Steps at(s0, steps, RPW, sub);
-#pragma unroll 4
-            for (int i = 0; i < n; ++i) {
-                const T *src = static_cast<const T *>(a.Q) + (size_t)(t0 + at.token) * a.q_stride + (size_t)at.head * D + piece.first;
-                copy_async<kLayout>(to + 512 * i, src, piece.apart(), at.head < a.Hq);
-                at.next(a.Hq, RPW, sub);
+            s0 = (work - n_heads) * R::kSteps;
+            n = min(R::kSteps, n_steps - s0);
+            Steps at(s0, steps, over_steps, RPW, sub);
+            const T *src = static_cast<const T *>(a.Q) + (size_t)(t0 + at.token) * a.q_stride + (size_t)at.head * D + piece.first;
+            const long long wrap = (long long)a.q_stride - steps * RPW * D;
+#pragma unroll
+            for (int i = 0; i < R::kSteps; ++i) {
+                raw[i] = i < n && at.head < a.Hq ? load<kLayout>(src, piece.apart()) : make_uint4(0, 0, 0, 0);
+                src += RPW * D;
+                if (at.next(a.Hq, RPW, sub)) src += wrap;
             }
         }
-        asm volatile("cp.async.commit_group;" ::: "memory");
     };
-    int work = blockIdx.y * kWarps + warp, b = 0;
-    copy(work, stage0);
+    int work = blockIdx.y * kWarps + warp;
+    load_rows(work);                                        // (the first piece's beside the angles)
     const int half = a.rot >> 1;
     if (half > 0) {
-        // the tokens whose angles are used: the window's for queries, the runs' for keys
-        int n_angles = a.Q ? n_win : 0;
-        if (starts) {
-            const Run tail = run_from(31 - __clz(starts));
-            n_angles = max(n_angles, tail.t - t0 + tail.n);
-        }
+        // of the window's tokens for queries, of the runs' for keys
+        const int n_angles = a.Q ? max(n_win, s_end) : s_end;
         for (int x = tid; x < n_angles * kMaxPairs; x += kThreads) {
             const int pair = x % kMaxPairs;
-            if (pair < half) s_angles[x] = angle(a, t0 + x / kMaxPairs, pair);
+            if (pair < half) {
+                const float2 v = angle(a, t0 + x / kMaxPairs, pair);
+                s_angles[x / kMaxPairs * kTable + pair] = v.x;
+                s_angles[x / kMaxPairs * kTable + kMaxPairs + pair] = v.y;
+                s_angles[x / kMaxPairs * kTable + 2 * kMaxPairs + pair] = -v.y;
+            }
         }
         __syncthreads();
     }
 #pragma unroll 1
-    for (; work < n_work; b ^= 1) {
-        const int now = work;
-        const uint32_t rows = stage0 + b * R::kStage;
-        work += gridDim.y * kWarps;
-        copy(work, stage0 + (b ^ 1) * R::kStage);
-        asm volatile("cp.async.wait_group 1;" ::: "memory");
-        if (now < n_heads) {
-            int head;
-            const Run run = run_of(now, head);
-            const bool key = head < a.Hkv;
-            write_head<T, D, kLayout>(a, run, key, key ? head : head - a.Hkv, rows, s_angles + (run.t - t0) * kMaxPairs);
+    while (work < n_work) {
+        if (work < n_heads) {
+            if (head < a.Hkv) write_head<T, D, kLayout, true>(a, run, head, raw, s_angles + (run.t - t0) * kTable, mine);
+            else write_head<T, D, kLayout, false>(a, run, head - a.Hkv, raw, nullptr, 0);
         } else {
-            const int s0 = (now - n_heads) * R::kSteps, n = min(R::kSteps, n_steps - s0);
             f32x2 w[E / 2];
             if (a.wq) Vec<T>::unpack(load<kLayout>(static_cast<const T *>(a.wq) + piece.first, piece.apart()), w);
-            Steps at(s0, steps, RPW, sub);
-#pragma unroll 4
-            for (int i = 0; i < n; ++i) {
+            Steps at(s0, steps, over_steps, RPW, sub);
+            const bool turn = a.rot > 0 && piece.on;
+            Rotation<E, kLayout == kInterleaved> rot;
+            T *dst = static_cast<T *>(a.Qo) + ((size_t)(t0 + at.token) * a.Hq + at.head) * D + piece.first;
+            const int wrap = (a.Hq - steps * RPW) * D;      // a token's last step may be padded
+            int token = -1;
+#pragma unroll
+            for (int i = 0; i < R::kSteps; ++i) {
+                if (i >= n) break;
+                if (turn && at.token != token) {
+                    read_angles(s_angles + at.token * kTable, piece.pair, rot);
+                    token = at.token;
+                }
                 f32x2 x[E / 2];
-                Vec<T>::unpack(ring_load(rows + 512 * i), x);
-                norm_rotate<D, E, kLayout == kInterleaved>(x, a.wq, w, a.eps, a.rot > 0 && piece.on, s_angles + at.token * kMaxPairs, piece.pair);
-                store<kLayout>(static_cast<T *>(a.Qo) + ((size_t)(t0 + at.token) * a.Hq + at.head) * D + piece.first, piece.apart(),
-                               Vec<T>::pack(x), at.head < a.Hq);
-                at.next(a.Hq, RPW, sub);
+                Vec<T>::unpack(raw[i], x);
+                if (a.wq) scale_row<E>(x, row_factor<D, E>(x, a.eps), w);
+                if (turn) rotate<E, kLayout == kInterleaved>(x, rot);
+                store<kLayout>(dst, piece.apart(), Vec<T>::pack(x), at.head < a.Hq);
+                dst += RPW * D;
+                if (at.next(a.Hq, RPW, sub)) dst += wrap;
             }
         }
+        work += gridDim.y * kWarps;
+        load_rows(work);
+    }
     }
 }
 
 template <typename T, int D, Layout kLayout> cudaError_t launch_write(const RopeArgs &a, cudaStream_t st)
 {
-    // A block to a token while the GPU holds them (each may be a run of its own), else windows
-    // of up to 16, in which about one run of a prompt begins.
+    // A block to a token while the GPU holds them (each may be a run of its own), else a share of the tokens to each of the
+    // blocks that it holds, in windows of about equal size.
     const int held = 2 * pipe::sm_count();
-    int window = (a.n_tok + held - 1) / held;
-    if (window > kGroup) window = kGroup;
-    const int blocks = (a.n_tok + window - 1) / window;
+    const int share = (a.n_tok + held - 1) / held, windows = (share + kWindow - 1) / kWindow, window = (share + windows - 1) / windows;
+    const int blocks = (a.n_tok + share - 1) / share;
     const int steps = a.Q ? (a.Hq + Rows<T, D>::RPW - 1) / Rows<T, D>::RPW * window : 0;
     const int pieces = 2 * a.Hkv + (steps + Rows<T, D>::kSteps - 1) / Rows<T, D>::kSteps, rounds = (pieces + kWarps - 1) / kWarps;
     int y = held / blocks;
@@ -337,7 +454,10 @@ template <typename T, int D, Layout kLayout> cudaError_t launch_write(const Rope
     static std::atomic<unsigned long long> opted{0};
     const cudaError_t e = pipe::opt_in(reinterpret_cast<const void *>(&k_cache_write<T, D, kLayout>), Rows<T, D>::kBytes, opted);
     if (e != cudaSuccess) return e;
-    return pipe::launch_early(k_cache_write<T, D, kLayout>, dim3(blocks, y), dim3(kThreads), Rows<T, D>::kBytes, st, a, window);
+    int lg = 4;
+    while ((1 << lg) < a.page_size) ++lg;
+    return pipe::launch_early(k_cache_write<T, D, kLayout>, dim3(blocks, y), dim3(kThreads), Rows<T, D>::kBytes, st, a, share, window, lg,
+                              Over::of((a.Hq + Rows<T, D>::RPW - 1) / Rows<T, D>::RPW), Over::of(2 * a.Hkv));
 }
 template <typename T, int D> cudaError_t launch_write(const RopeArgs &a, cudaStream_t st)
 {
