@@ -155,6 +155,21 @@ def test_writes_of_many_tokens(dt):
     check_write(s, before, "many")
 
 
+def test_writes_of_more_tokens_than_one_launch_takes():
+    """Queries go through a launch of their own where there are many tokens."""
+    rng = random.Random(5)
+    s = write_setup(BF, [(rng.randint(0, 50), rng.randint(1, 2000)) for _ in range(40)], 2, 1, 64, 64, seed=9)
+    assert s["T"] > 30000
+    before = copies(*s["cache"])
+    qo = run_write(s)
+    H.hybrid_check()
+    check_write(s, before, "many in two launches")
+    want, ko = torch.empty_like(qo), torch.empty(s["T"], 1, 64, dtype=BF, device="cuda")
+    H.hybrid_qk_norm_rope(s["cfg"], s["rope"], s["q"], s["stride"], s["k"], s["stride"], s["T"], s["wq"], s["wk"], s["pos"],
+                          s["freqs"], want, ko)
+    assert torch.equal(qo, want)
+
+
 @pytest.mark.parametrize("dt", [BF, F32])
 @pytest.mark.parametrize("Hkv", [1, 16, 80])
 def test_writes_as_they_are(dt, Hkv):
