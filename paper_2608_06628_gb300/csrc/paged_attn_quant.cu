@@ -68,7 +68,7 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t v)      // of an 8 x 8 m
 __device__ __forceinline__ float lg2(float x)
 {
     float y;
-    asm("lg2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+    asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
 __device__ __forceinline__ void copy_codes(uint32_t dst, const uint8_t *src, int bytes)
@@ -83,10 +83,13 @@ __device__ __forceinline__ void copy_scale(uint32_t dst, const float *src)
 // Places in a run's codes of one kind: [key][16 bytes], permuted.  Row r of S^T is key key_of(r).
 template <int D> struct Place;
 template <> struct Place<128> {
+    // pair of features of a row in a stage that holds outputs
+    __device__ static int pair(int r, int p) { return p ^ ((r >> 1 & 3) | (p >> 2 & 4)); }
     __device__ static int key_of(int r) { return r ^ ((r & 1) << 2); }
     __device__ static uint32_t chunk(int key, int c) { return key * 128 + ((c ^ (key & 7)) << 4); }
 };
 template <> struct Place<64> {
+    __device__ static int pair(int r, int p) { return p ^ (r >> 1 & 3); }
     __device__ static int key_of(int r) { return (r & 8) | (r & 2) << 1 | (r & 4) >> 1 | ((r ^ r >> 1) & 1); }
     __device__ static uint32_t chunk(int key, int c) { return key * 64 + ((c ^ (key & 2)) << 4); }
 };
@@ -94,11 +97,9 @@ template <> struct Place<64> {
 // NT: row tiles of 8 rows
 template <int D, int NT> struct Smem {
     static constexpr int kStages = NT * D <= 128 ? 3 : 4;
-    static constexpr int kScales = kStages + 1;
-    static constexpr int kPasses = 4, kPass = D / kPasses;  // features of the output at a time
+    static constexpr int kPasses = NT, kPass = D / kPasses; // features of the output at a time: those of 8 NT rows fill a stage
     uint8_t ring[kWarps][kStages][2][kRun * D];             // K, then V
-    float o[kWarps][8 * NT][kPass + 4];
-    float scales[kWarps][kScales][2];
+    float2 scales[kWarps][kStages];                         // of K, of V
     float m[kWarps][8 * NT], l[kWarps][8 * NT];
     PlanSmem plan;
 };
@@ -107,7 +108,7 @@ template <typename T, int D, int NT>
 __global__ __launch_bounds__(kThreads, NT == 1 ? 2 : 1) void k_paged_attn_quant(const PagedArgs a, int page_lg)
 {
     using S = Smem<D, NT>;
-    constexpr int kStages = S::kStages, kScales = S::kScales;
+    constexpr int kStages = S::kStages;
     constexpr int kParts = sizeof(T) == 2 ? 1 : 2;          // halves that hold a number
     constexpr int KS = D / 16, MT = D / 16;                 // steps of S over the features, tiles of O
     constexpr int kCopies = kRun * D / 16 / 32;             // of a lane, of K and of V
@@ -118,63 +119,76 @@ __global__ __launch_bounds__(kThreads, NT == 1 ? 2 : 1) void k_paged_attn_quant(
     const int rows = a.Bt * a.Gt;
     const float to_log2 = pipe::kLog2e * rsqrtf((float)D);
     const uint8_t *K = static_cast<const uint8_t *>(a.K), *V = static_cast<const uint8_t *>(a.V);
-    const uint32_t ring = ptx::smem_u32(&s.ring[warp]);
+    const uint32_t ring = ptx::smem_u32(&s.ring[warp]), scales = ptx::smem_u32(&s.scales[warp]) + 4 * lane;
     const int key0 = Place<D>::key_of(g);                   // of rows g and g + 8 of S^T: key0, key0 + 8
+    // A run's codes are 512 bytes after another, a copy of the warp each: places of this lane's in an even and an odd one.
+    uint32_t place[2];
+#pragma unroll
+    for (int x = 0; x < 2; ++x) place[x] = ring + Place<D>::chunk((lane + 32 * x) / (D / 16), lane % (D / 16));
+    constexpr int kTwo = 2 * 512;                           // bytes of an even and an odd one
 
     ptx::griddep_wait();
     ptx::griddep_launch_dependents();
-    Walk w;
+    Walk w;                                                 // of the segment at work
     Shares sh(0, 1);
     const bool work = find_share<kThreads>(a, s.plan, w, sh);
     bool go = work && w.next(a);
-    // the copies, of the segment w: tile, stage
-    int i = 0, slot = 0, to_scale = 0;
-    int ahead = 0;                                          // page of the next run
-    auto look_up = [&](int tile) {
-        ahead = 0;
-        if (tile >= w.i1) return;
-        const int j = key_tile(w.vis, tile) * kTile + warp * kRun;
-        if (any_visible(w.vis, j, kRun)) ahead = __ldg(a.table + (size_t)w.req * a.max_pages + (j >> page_lg));
+    // The copies go on from segment to segment, ahead of the work: their walk, the next tile, its stage and its page.
+    Walk fw = w;
+    bool more = go;
+    Tiles at;
+    int slot = 0, ahead[2] = {0, 0};                        // pages of the next tile and of the one behind it
+    const int *pages = nullptr;
+    size_t head = 0;
+    auto page_of = [&](const Tiles &t) -> int {
+        const int j = t.tile * kTile + warp * kRun;
+        return t.whole() || any_visible(fw.vis, j, kRun) ? __ldg(pages + (j >> page_lg)) : 0;
+    };
+    auto begin_copies = [&]() {
+        at.begin(fw);
+        pages = a.table + (size_t)fw.req * a.max_pages;
+        head = fw.head;
+        ahead[0] = page_of(at);
+        Tiles next = at;
+        if (next.step()) ahead[1] = page_of(next);
     };
     auto fetch = [&]() {
-        if (i < w.i1) {
-            const int j = key_tile(w.vis, i) * kTile + warp * kRun;
-            int page = ahead;
-            look_up(++i);
-            if (any_visible(w.vis, j, kRun)) {
-                if (page < 0 || page >= a.n_pages) {
+        if (more) {
+            const int j = at.tile * kTile + warp * kRun;
+            const bool whole = at.whole();
+            if (whole || any_visible(fw.vis, j, kRun)) {
+                int page = ahead[0];
+                if ((unsigned)page >= (unsigned)a.n_pages) {
                     raise_error(a.err, ERR_BAD_INDEX);
                     page = 0;
                 }
-                const size_t run = (((size_t)page * a.Hkv + w.head) << page_lg) + (j & ((1 << page_lg) - 1));
-                if (lane < 2) copy_scale(ptx::smem_u32(&s.scales[warp][to_scale][lane]), (lane ? a.V_scale : a.K_scale) + run / kRun);
+                const size_t run = (((size_t)page * a.Hkv + head) << page_lg) + (j & ((1 << page_lg) - 1));
+                if (lane < 2) copy_scale(scales + 8 * slot, (lane ? a.V_scale : a.K_scale) + run / kRun);
+                const uint8_t *from_k = K + run * D + 16 * lane, *from_v = V + run * D + 16 * lane;
+                const uint32_t stage = slot * (2 * kRun * D);
 #pragma unroll
-                for (int x = 0; x < kCopies; ++x) {
-                    const int at = lane + 32 * x, key = at / (D / 16);
-                    const int bytes = key_visible(w.vis, j + key) ? 16 : 0;     // masked keys and values are zeros
-                    const uint32_t dst = ring + slot * (2 * kRun * D) + Place<D>::chunk(key, at % (D / 16));
-                    copy_codes(dst, K + run * D + 16 * at, bytes);
-                    copy_codes(dst + kRun * D, V + run * D + 16 * at, bytes);
+                for (int x = 0; x < kCopies; ++x) {         // masked keys and values are zeros
+                    const int bytes = whole || key_visible(fw.vis, j + (lane + 32 * x) / (D / 16)) ? 16 : 0;
+                    const uint32_t dst = place[x & 1] + stage + x / 2 * kTwo;
+                    copy_codes(dst, from_k + 512 * x, bytes);
+                    copy_codes(dst + kRun * D, from_v + 512 * x, bytes);
                 }
             }
-            to_scale = to_scale + 1 == kScales ? 0 : to_scale + 1;
+            if (at.step()) {
+                ahead[0] = ahead[1];
+                Tiles next = at;
+                if (next.step()) ahead[1] = page_of(next);
+            } else if ((more = fw.next(a))) {
+                begin_copies();
+            }
         }
         slot = slot + 1 == kStages ? 0 : slot + 1;
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
-    auto first_page = [&]() {
-        i = w.i0;
-        slot = to_scale = 0;
-        look_up(i);
-    };
-    auto first_steps = [&]() {
-#pragma unroll
-        for (int x = 0; x < kStages - 1; ++x) fetch();
-    };
-    if (go) {
-        first_page();
-        first_steps();
-    }
+    if (go) begin_copies();
+#pragma unroll 1
+    for (int x = 0; x < kStages - 1; ++x) fetch();
+    int b = 0;                                              // stage at work
     while (go) {
         const Unit u = unit_of(a, w.head, w.rt);
         // Q: step t of the features has, in this lane, 4 t % 16 ... of its 16-byte piece c + 4 (t / 4)
@@ -228,7 +242,8 @@ __global__ __launch_bounds__(kThreads, NT == 1 ? 2 : 1) void k_paged_attn_quant(
                     if constexpr (kParts == 2) q[nt][t][1][h] = rest_f16x2(q[nt][t][0][h], lo, hi);
                 }
         }
-        float o[NT][MT][4], m[NT][2], mo[NT][2], l[NT][2];  // l of this lane's keys
+        float o[NT][MT][4], m[NT][2], mo[NT][2], l[NT][2];  // references of l and of O; l of this lane's keys
+        float base[NT][2], to_o[NT][2];                     // m and kTop + m - mo, with zeros for a reference that is not there yet
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
@@ -236,17 +251,22 @@ __global__ __launch_bounds__(kThreads, NT == 1 ? 2 : 1) void k_paged_attn_quant(
 #pragma unroll
             for (int y = 0; y < 2; ++y) {
                 m[nt][y] = mo[nt][y] = -INFINITY;
-                l[nt][y] = 0.f;
+                base[nt][y] = l[nt][y] = 0.f;
+                to_o[nt][y] = kTop;
             }
         }
-        for (int n = w.i0, b = 0, scale = 0; n < w.i1; ++n, b = b + 1 == kStages ? 0 : b + 1, scale = scale + 1 == kScales ? 0 : scale + 1) {
+        Tiles now;
+        now.begin(w);
+        do {
             fetch();                                        // into the stage of the step before
             asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
             __syncwarp();                                   // other lanes' copies too
-            const int j = key_tile(w.vis, n) * kTile + warp * kRun;
-            if (any_visible(w.vis, j, kRun)) {
+            const int j = now.tile * kTile + warp * kRun;
+            const bool whole = now.whole();
+            if (whole || any_visible(w.vis, j, kRun)) {
                 const unsigned char *codes = s.ring[warp][b][0];
-                const float ks = s.scales[warp][scale][0], vs = s.scales[warp][scale][1], lv = lg2(vs);
+                const float2 kv = s.scales[warp][b];
+                const float lv = lg2(kv.y);
                 float x[NT][4];
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) x[nt][0] = x[nt][1] = x[nt][2] = x[nt][3] = 0.f;
@@ -266,39 +286,49 @@ __global__ __launch_bounds__(kThreads, NT == 1 ? 2 : 1) void k_paged_attn_quant(
                             for (int p = 0; p < kParts; ++p) mma(x[nt], f, q[nt][4 * t4 + t][p][0], q[nt][4 * t4 + t][p][1]);
                     }
                 }
-                const bool v0 = key_visible(w.vis, j + key0), v1 = key_visible(w.vis, j + key0 + 8);
+                if (!whole) {
+                    const bool v0 = key_visible(w.vis, j + key0), v1 = key_visible(w.vis, j + key0 + 8);
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int y = 0; y < 2; ++y) {
+                            if (!v0) x[nt][y] = -INFINITY;
+                            if (!v1) x[nt][2 + y] = -INFINITY;
+                        }
+                }
+                // factors of S (bounded away from zero: they meet the infinities of masked scores)
+                float f[NT][2], top[NT][2];
                 bool above = false;
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                     for (int y = 0; y < 2; ++y) {
-                        const float f = fminf(ks * kc[nt][y], kMax);
-                        x[nt][y] = v0 ? x[nt][y] * f : -INFINITY;
-                        x[nt][2 + y] = v1 ? x[nt][2 + y] * f : -INFINITY;
-                        const float top = fmaxf(x[nt][y], x[nt][2 + y]);
-                        above |= top > m[nt][y] + kSlack || top + lv > mo[nt][y] + kSlack;
+                        f[nt][y] = fminf(fmaxf(kv.x * kc[nt][y], 0x1p-126f), kMax);
+                        top[nt][y] = fmaxf(x[nt][y], x[nt][2 + y]) * f[nt][y];
+                        above |= top[nt][y] > m[nt][y] + kSlack || top[nt][y] + lv > mo[nt][y] + kSlack;
                     }
                 if (__any_sync(0xffffffffu, above)) {
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                         for (int y = 0; y < 2; ++y) {
-                            float top = fmaxf(x[nt][y], x[nt][2 + y]);
+                            float t = top[nt][y];
 #pragma unroll
-                            for (int z = 4; z < 32; z <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, z));
-                            if (top > m[nt][y] + kSlack) {
-                                l[nt][y] *= m[nt][y] == -INFINITY ? 1.f : pipe::ex2(m[nt][y] - top);    // (zero, or NaN)
-                                m[nt][y] = top;
+                            for (int z = 4; z < 32; z <<= 1) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, z));
+                            if (t > m[nt][y] + kSlack) {
+                                l[nt][y] *= m[nt][y] == -INFINITY ? 1.f : pipe::ex2(m[nt][y] - t);      // (zero, or NaN)
+                                base[nt][y] = m[nt][y] = t;
                             }
-                            if (top + lv > mo[nt][y] + kSlack) {
-                                const float f = mo[nt][y] == -INFINITY ? 1.f : pipe::ex2(mo[nt][y] - (top + lv));
-                                mo[nt][y] = top + lv;
+                            if (t + lv > mo[nt][y] + kSlack) {
+                                const float f = mo[nt][y] == -INFINITY ? 1.f : pipe::ex2(mo[nt][y] - (t + lv));
+                                mo[nt][y] = t + lv;
 #pragma unroll
                                 for (int t = 0; t < MT; ++t) {
                                     o[nt][t][y] *= f;
                                     o[nt][t][2 + y] *= f;
                                 }
                             }
+                            to_o[nt][y] = base[nt][y] - (mo[nt][y] == -INFINITY ? 0.f : mo[nt][y]) + kTop;
                         }
                 }
                 uint32_t p[NT][kParts][2];                  // keys 0 ... 7, 8 ... 15 in S^T's order
@@ -307,11 +337,10 @@ __global__ __launch_bounds__(kThreads, NT == 1 ? 2 : 1) void k_paged_attn_quant(
                     float pv[4];
 #pragma unroll
                     for (int y = 0; y < 2; ++y) {
-                        const float base = m[nt][y] == -INFINITY ? 0.f : m[nt][y], base_o = mo[nt][y] == -INFINITY ? 0.f : mo[nt][y];
                         // P at once: l, from its sum.  (Below 2^-60 half precision has zeros, and float32 still has p.)
-                        const float gain = fminf(fmaxf(lv + base - base_o + kTop, -60.f), 126.f);
-                        pv[y] = pipe::ex2(x[nt][y] - base + gain);
-                        pv[2 + y] = pipe::ex2(x[nt][2 + y] - base + gain);
+                        const float gain = fminf(fmaxf(lv + to_o[nt][y], -60.f), 126.f), add = gain - base[nt][y];
+                        pv[y] = pipe::ex2(fmaf(x[nt][y], f[nt][y], add));
+                        pv[2 + y] = pipe::ex2(fmaf(x[nt][2 + y], f[nt][y], add));
                         l[nt][y] = fmaf(pv[y] + pv[2 + y], pipe::ex2(-gain), l[nt][y]);
                     }
 #pragma unroll
@@ -351,16 +380,13 @@ __global__ __launch_bounds__(kThreads, NT == 1 ? 2 : 1) void k_paged_attn_quant(
                 }
             }
             __syncwarp();                                   // the stage has been read
-        }
-        // the segment after this one: its first copies are under way meanwhile
+            b = b + 1 == kStages ? 0 : b + 1;
+        } while (now.step());
+        // the output; the next segment's first copies are under way already
         const bool whole = w.whole();
         const int req = w.req;
         float *part = a.part + w.slot() * partial_floats(rows, D);
         go = w.next(a);
-        if (go) {
-            first_page();
-            first_steps();
-        }
         float back[NT][2];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
@@ -375,47 +401,60 @@ __global__ __launch_bounds__(kThreads, NT == 1 ? 2 : 1) void k_paged_attn_quant(
                 // O relative to m
                 back[nt][y] = m[nt][y] == -INFINITY ? 0.f : pipe::ex2(mo[nt][y] - m[nt][y] - kTop);
             }
+        // each warp's into the stage that it worked on last, [row][pair of features, permuted], D / 8 / kPasses of each lane's
+        constexpr int kPer = MT / S::kPasses, kPairs = S::kPass / 2;
+        const int stage = b == 0 ? kStages - 1 : b - 1;
+        auto outputs = [&](int y) { return reinterpret_cast<float2 *>(s.ring[y][stage][0]); };
 #pragma unroll
-        for (int pass = 0; pass < S::kPasses; ++pass) {     // D / 32 features of each lane's
+        for (int pass = 0; pass < S::kPasses; ++pass) {
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                 for (int y = 0; y < 2; ++y)
 #pragma unroll
-                    for (int t = 0; t < MT / S::kPasses; ++t) {
-                        const float(&from)[4] = o[nt][pass * (MT / S::kPasses) + t];
-                        *reinterpret_cast<float2 *>(&s.o[warp][8 * nt + 2 * c + y][g * (D / 32) + 2 * t]) =
-                            make_float2(from[y] * back[nt][y], from[2 + y] * back[nt][y]);
+                    for (int t = 0; t < kPer; ++t) {
+                        const float(&from)[4] = o[nt][pass * kPer + t];
+                        const int r = 8 * nt + 2 * c + y;
+                        outputs(warp)[r * kPairs + Place<D>::pair(r, g * kPer + t)] = make_float2(from[y] * back[nt][y], from[2 + y] * back[nt][y]);
                     }
             __syncthreads();
             // the warps
-            for (int x = tid; x < rows * S::kPass; x += kThreads) {
-                const int rho = x / S::kPass, at = x % S::kPass;
-                const int col = at / (D / 32) * (D / 8) + pass * (D / 32) + at % (D / 32);
-                float top = s.m[0][rho], sum = 0.f, out = 0.f;
+            for (int x = tid; x < rows * kPairs; x += kThreads) {
+                const int rho = x / kPairs, at_pair = x % kPairs;
+                const int col = at_pair / kPer * (D / 8) + 2 * (pass * kPer + at_pair % kPer);
+                float top = s.m[0][rho], sum = 0.f;
+                float2 out = make_float2(0.f, 0.f);
 #pragma unroll
                 for (int y = 1; y < kWarps; ++y) top = fmaxf(top, s.m[y][rho]);
-                const float base = top == -INFINITY ? 0.f : top;
+                const float to = top == -INFINITY ? 0.f : top;
 #pragma unroll
                 for (int y = 0; y < kWarps; ++y) {
-                    const float f = pipe::ex2(s.m[y][rho] - base);
+                    const float f = pipe::ex2(s.m[y][rho] - to);
+                    const float2 v = outputs(y)[rho * kPairs + Place<D>::pair(rho, at_pair)];
                     sum = fmaf(f, s.l[y][rho], sum);
-                    out = fmaf(f, s.o[y][rho][at], out);
+                    out.x = fmaf(f, v.x, out.x);
+                    out.y = fmaf(f, v.y, out.y);
                 }
                 if (whole) {
-                    size_t to;
-                    if (row_at(a, req, u, rho, to)) static_cast<T *>(a.O)[to + col] = from_f32<T>(out / sum);
+                    size_t dst;
+                    if (row_at(a, req, u, rho, dst)) {
+                        T *po = static_cast<T *>(a.O) + dst + col;
+                        if constexpr (sizeof(T) == 2) *reinterpret_cast<uint32_t *>(po) = pipe::pack_bf16x2(out.x / sum, out.y / sum);
+                        else *reinterpret_cast<float2 *>(po) = make_float2(out.x / sum, out.y / sum);
+                    }
                 } else {
-                    part[2 * rows + (size_t)col * rows + rho] = out;
-                    if (pass == 0 && at == 0) {
+                    part[2 * rows + (size_t)col * rows + rho] = out.x;
+                    part[2 * rows + (size_t)(col + 1) * rows + rho] = out.y;
+                    if (pass == 0 && at_pair == 0) {
                         part[rho] = top;
                         part[rows + rho] = sum;
                     }
                 }
             }
-            __syncthreads();                                // before the next pass, or segment
+            __syncthreads();                                // before the next pass, or copies into the stages
         }
     }
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
     if (tid == 0) write_note(a, work, w, sh);
     write_empty<T, kThreads>(a, tid);
 }
@@ -451,7 +490,10 @@ void paged_quant_geometry(const hybrid_cfg &c, PagedArgs &a)
     a.d = c.head_dim;
     const bool tc = c.io_dtype == HYBRID_BF16 && a.G * a.B > kMostRows;
     paged_cut_rows(a, tc ? 128 : kMostRows);
-    a.extra = 7;
+    // Quarters of a tile that a change of units costs: 64 requests of 256-8192 tokens, one token 61.9 us with 7, 58.9 with
+    // 10 and 14 (float32, 16 requests: 25.2, 25.3, 26.5); blocks of 32 tokens 96 with 7, 89 with 14, 88 with 20, blocks of 8
+    // with d = 64 70, 64 and 66.
+    a.extra = tc ? 14 : 10;
     a.n_cta = (a.Bt * a.Gt > 8 ? 1 : 2) * pipe::sm_count();  // resident blocks
 }
 

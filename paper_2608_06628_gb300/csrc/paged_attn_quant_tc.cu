@@ -70,28 +70,6 @@ __device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi)
     return *reinterpret_cast<const uint32_t *>(&h);
 }
 
-// Key tiles of a segment in order, and whether all of a tile is visible, in a few instructions a tile.
-struct Tiles {
-    int i, i1, tile, ns, first, whole_from, whole_to, whole_sink;
-    __device__ void begin(const Walk &w)
-    {
-        i = w.i0;
-        i1 = w.i1;
-        ns = w.vis.ns;
-        first = w.vis.first;
-        tile = key_tile(w.vis, i);
-        whole_from = (w.vis.lo + kTile - 1) / kTile;
-        whole_to = w.vis.len / kTile;
-        whole_sink = w.vis.sink / kTile;
-    }
-    __device__ bool whole() const { return (tile >= whole_from && tile < whole_to) || tile < whole_sink; }
-    __device__ bool step()
-    {
-        tile = ++i == ns ? first : tile + 1;
-        return i < i1;
-    }
-};
-
 __device__ __forceinline__ float max3(float x, float y, float z)
 {
     float r;

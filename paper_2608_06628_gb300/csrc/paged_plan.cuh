@@ -154,6 +154,28 @@ struct Walk {
     __device__ int slot() const { return 2 * (int)blockIdx.x + (i0 == 0 ? 1 : 0); }
 };
 
+// Key tiles of a segment in order, and whether all of a tile is visible, in a few instructions a tile.
+struct Tiles {
+    int i, i1, tile, ns, first, whole_from, whole_to, whole_sink;
+    __device__ void begin(const Walk &w)
+    {
+        i = w.i0;
+        i1 = w.i1;
+        ns = w.vis.ns;
+        first = w.vis.first;
+        tile = key_tile(w.vis, i);
+        whole_from = (w.vis.lo + kTile - 1) / kTile;
+        whole_to = w.vis.len / kTile;
+        whole_sink = w.vis.sink / kTile;
+    }
+    __device__ bool whole() const { return (tile >= whole_from && tile < whole_to) || tile < whole_sink; }
+    __device__ bool step()
+    {
+        tile = ++i == ns ? first : tile + 1;
+        return i < i1;
+    }
+};
+
 // The walk up to the request, which the caller fills in; returns the first quarter's
 // place in its row tile (of `total` quarters per key head).
 __device__ __forceinline__ int start_walk(const PagedArgs &a, int total, const Shares &sh, Walk &w)
