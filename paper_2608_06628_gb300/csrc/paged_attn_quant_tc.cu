@@ -24,8 +24,8 @@
 // Keys that no query sees: pages and scales without a visible key are not loaded, masked scores
 // are replaced before use, masked rows of V are zeros in the operand.
 //
-// Warps: softmax and epilogue (4), converters of K (4) and V (4), producers of K with the scales,
-// and of V, issuers of S and of O.  Every wait is bounded (tc_pipeline.cuh).
+// Warps: softmax and epilogue (8), converters of K (4) and V (4), producers of the even and the odd
+// tiles, issuers of S and of O.  Every wait is bounded (tc_pipeline.cuh).
 #include "paged_plan.cuh"
 #include "quant.cuh"
 #include "tc_pipeline.cuh"
@@ -49,7 +49,7 @@ constexpr float kSlack = 8.f;             // log2 of how far a reference may be 
 constexpr float kTop = 7.f;               // log2 of P at its reference
 constexpr float kMax = 3.402823466e38f;
 constexpr int kThreads = 640;
-enum Role { kSoft = 0, kConvertK = 8, kConvertV = 12, kLoadK = 16, kLoadV = 17, kIssueS = 18, kIssueO = 19 };
+enum Role { kSoft = 0, kConvertK = 8, kConvertV = 12, kLoad0 = 16, kLoad1 = 17, kIssueS = 18, kIssueO = 19 };
 
 struct TcArgs {
     CUtensorMap tmK, tmV;
@@ -145,7 +145,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_quant_tc(const __gri
         tmem_alloc(tmem_holder, 512);
         tmem_relinquish();
     }
-    if (warp == kLoadK && lane == 0) {
+    if (warp == kLoad0 && lane == 0) {
         prefetch_tensormap(&ta.tmK);
         prefetch_tensormap(&ta.tmV);
         for (int i = 0; i < NK + NV; ++i) {
@@ -181,94 +181,96 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_quant_tc(const __gri
     const uint32_t tmem = *tmem_holder;
 
     // The scores of a tile fill the softmax's registers: 80 + 2 * 72 + 2 * 128 = 5 * 96 for the groups of four warps.
-    if (warp >= kLoadK) {
+    if (warp >= kLoad0) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
-    if (warp == kLoadK || warp == kLoadV) {
-        // ------------------------------------------------------ producers of the codes
-        const bool is_v = warp == kLoadV;
+    if (warp == kLoad0 || warp == kLoad1) {
+        // ------------------------------------------ producers of the codes and scales: even tiles, odd ones
+        const uint32_t parity = warp - kLoad0;
         if (work) {
             const int P = a.page_size, per = kTile / P;    // pages of a tile
-            const uint32_t page_bytes = (uint32_t)P * D, n_slots = is_v ? NV : NK;
-            const CUtensorMap *map = is_v ? &ta.tmV : &ta.tmK;
-            uint64_t *my_full = is_v ? full + NK : full, *my_empty = is_v ? empty + NK : empty;
-            uint8_t *my_ring = is_v ? ring + (size_t)NK * kCodes : ring;
+            const uint32_t page_bytes = (uint32_t)P * D;
             // a cache that is read once need not push tables, lengths and partials out of L2
             const bool once = row_tiles(a) == 1;
             const uint64_t policy = policy_evict_first();
             // lanes 0 ... 7, 8 ... 15: scales of K, V of the 8 groups of a tile
             const int group = 16 * (lane & 7), lg = 31 - __clz(P);
             const float *my_scale = lane < 8 ? a.K_scale : a.V_scale;
-            uint32_t n = 0;                                // tiles issued
-            RingPos pos{0, 1};                             // phase of `empty`: the first round is free
+            uint32_t n = 0, last = ~0u;                    // tiles before the segment, the last one that this warp has issued
             bool ok = true;
-            while (ok && w.next(a)) {
+            for (; ok && w.next(a); n += w.i1 - w.i0) {
                 const int head = w.head;
                 const int *pages = a.table + (size_t)w.req * a.max_pages;
                 Tiles at;
                 at.begin(w);
-                // this lane's page of the tile, -1: nothing visible in it
-                auto page_of = [&]() -> int {
-                    const int j = at.tile * per + lane;
-                    return lane < per && (at.whole() || any_visible(w.vis, j * P, P)) ? __ldg(pages + j) : -1;
-                };
+                // this lane's page of the tile, if it has one with something visible in it
                 auto sees = [&]() { return lane < per && (at.whole() || any_visible(w.vis, at.tile * kTile + lane * P, P)); };
-                int next_page = page_of();
-                bool next_see = sees();
-                for (bool more = true; more;) {
+                uint32_t tile_n = n;
+                bool more = (n & 1) == parity || (++tile_n, at.step()), next_see = more && sees();
+                int next_page = next_see ? __ldg(pages + at.tile * per + lane) : 0;
+                while (more) {
+                    const uint32_t now = tile_n;
                     const int tile = at.tile;
                     const bool whole = at.whole(), mine = next_see;
-                    int page = next_page;                  // (looked at here, a tile after its load)
-                    if (mine && (page < 0 || page >= a.n_pages)) {
+                    int page = next_page;                  // (looked at here, a tile of this warp's after its load)
+                    if (mine && (unsigned)page >= (unsigned)a.n_pages) {
                         raise_error(a.err, ERR_BAD_INDEX);
                         page = 0;
                     }
-                    more = at.step();
+                    more = at.step() && at.step();
+                    tile_n += 2;
                     if (more) {
-                        next_page = page_of();
                         next_see = sees();
+                        if (next_see) next_page = __ldg(pages + at.tile * per + lane);
                     }
                     const uint32_t bytes = page_bytes * __popc(__ballot_sync(0xffffffffu, mine));
-                    ok = wait_soon(&my_empty[pos.slot], pos.phase, fail);
+                    const uint32_t sk = now % NK, sv = NK + now % NV;
+                    ok = wait_soon(&empty[sk], (now / NK & 1u) ^ 1u, fail) && wait_soon(&empty[sv], (now / NV & 1u) ^ 1u, fail);
                     if (__any_sync(0xffffffffu, !ok)) {
                         ok = false;
                         break;
                     }
-                    if (lane == 0) mbar_arrive_expect_tx(&my_full[pos.slot], bytes);
+                    last = now;
+                    if (lane == 0) {
+                        mbar_arrive_expect_tx(&full[sk], bytes);
+                        mbar_arrive_expect_tx(&full[sv], bytes);
+                    }
                     __syncwarp();
                     if (mine) {
-                        uint8_t *dst = my_ring + (size_t)pos.slot * kCodes + lane * P * D;
-                        if (once) tma_load_4d_policy(dst, map, 0, 0, head, page, &my_full[pos.slot], policy);
-                        else tma_load_4d(dst, map, 0, 0, head, page, &my_full[pos.slot]);
-                    }
-                    if (!is_v) {
-                        // Zeros for groups without a visible key.  The place was that of 32 tiles ago, whose softmax
-                        // is done: the slot's last tile, at most 6 ago, is converted, so S of the second tile before
-                        // that one is formed, and that waited for the softmax of the second tile before it.
-                        const int of = __shfl_sync(0xffffffffu, page, group >> lg);
-                        const bool see = whole || any_visible(w.vis, tile * kTile + group, 16);
-                        if (lane < 16) {
-                            const float *src = my_scale + (see ? (((size_t)of * a.Hkv + head) << lg | (group & (P - 1))) / 16 : 0);
-                            asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(
-                                             smem_u32(scales + n % kScaleTiles * 16 + lane)),
-                                         "l"(src), "r"(see ? 4 : 0)
-                                         : "memory");
+                        uint8_t *dst_k = ring + (size_t)sk * kCodes + lane * P * D, *dst_v = ring + (size_t)sv * kCodes + lane * P * D;
+                        if (once) {
+                            tma_load_4d_policy(dst_k, &ta.tmK, 0, 0, head, page, &full[sk], policy);
+                            tma_load_4d_policy(dst_v, &ta.tmV, 0, 0, head, page, &full[sv], policy);
+                        } else {
+                            tma_load_4d(dst_k, &ta.tmK, 0, 0, head, page, &full[sk]);
+                            tma_load_4d(dst_v, &ta.tmV, 0, 0, head, page, &full[sv]);
                         }
-                        cp_async_arrive_noinc(&my_full[pos.slot]);
                     }
-                    pos.step(n_slots);
-                    ++n;
+                    // Zeros for groups without a visible key.  The place was that of 32 tiles ago, whose softmax is done:
+                    // the slot's last tile, at most 6 ago, is converted, so S of the second tile before that one is
+                    // formed, and that waited for the softmax of the second tile before it.
+                    const int of = __shfl_sync(0xffffffffu, page, group >> lg);
+                    const bool see = whole || any_visible(w.vis, tile * kTile + group, 16);
+                    if (lane < 16) {
+                        const float *src = my_scale + (see ? (((size_t)of * a.Hkv + head) << lg | (group & (P - 1))) / 16 : 0);
+                        asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(smem_u32(scales + now % kScaleTiles * 16 + lane)),
+                                     "l"(src), "r"(see ? 4 : 0)
+                                     : "memory");
+                    }
+                    cp_async_arrive_noinc(&full[sk]);
                 }
             }
             cp_async_wait_all();
             if (*fail && lane == 0) {
                 // let copies in flight land before the block exits
-                for (uint32_t s = 0; s < n_slots; ++s) {
-                    const uint32_t k = n / n_slots + (s < n % n_slots ? 1u : 0u);
-                    if (k) mbar_wait(&my_full[s], (k - 1) & 1u, kWaitNs);
+                for (uint32_t x = 0; last != ~0u && x < (uint32_t)(NK > NV ? NK : NV) && 2 * x <= last; ++x) {
+                    const uint32_t t = last - 2 * x;
+                    if (2 * x < (uint32_t)NK) mbar_wait(&full[t % NK], t / NK & 1u, kWaitNs);
+                    if (2 * x < (uint32_t)NV) mbar_wait(&full[NK + t % NV], t / NV & 1u, kWaitNs);
                 }
             }
         }
-        if (is_v) {
+        if (parity == 1) {
+            while (work && w.next(a)) {}                   // (the note is of the last segment)
             if (lane == 0) write_note(a, work, w, sh);
             write_empty<bf16, 32>(a, lane);
         }
@@ -751,8 +753,7 @@ template <int D, int kCopies> cudaError_t launch(const PagedArgs &a, cudaStream_
     const uint32_t tail = kBarBytes + kScaleBytes + kExchange + (kCopies > 1 ? kStage : 0) + 1024;
     int ns = (int)((kSmemLimit - tail - halves) / slot);
     if (ns > kMaxSlots) ns = kMaxSlots;
-    ta.NK = ns / 2;
-    ta.NV = ns - ta.NK;
+    ta.NK = ta.NV = ns / 4 * 2;           // even: a slot has tiles of one producer only, which sees every phase of it
     ta.off_bar = halves + ns * slot;
     ta.off_stage = ta.off_bar + kBarBytes + kScaleBytes + kExchange + 256;
     ta.bytes = ta.off_bar + tail;

@@ -52,12 +52,16 @@ __device__ __forceinline__ bool wait_bar(uint64_t *bar, uint32_t parity, volatil
     }
 }
 
-// As wait_bar, for waits that are short or over: nothing but the tries before a wait of 0.2 ms (a
-// wait that is over costs 68 cycles; 208 with a loop around the tries, of the compiler's making).
+// As wait_bar, for waits that are short or over: the first try apart (a wait that is over costs 68
+// cycles; 208 with a loop around all tries, of the compiler's making), then tries with nothing between
+// them: a waiting warp takes issue slots from those at work, and the timer and the flag are a dozen
+// instructions.
 __device__ __forceinline__ bool wait_soon(uint64_t *bar, uint32_t parity, volatile int *fail)
 {
     if (ptx::mbar_try_wait(bar, parity)) return true;
-    if (ptx::mbar_try_wait_sleep(bar, parity, 200000u)) return true;
+#pragma unroll 1
+    for (int i = 0; i < 256; ++i)
+        if (ptx::mbar_try_wait_sleep(bar, parity, 1000000u)) return true;
     return wait_bar(bar, parity, fail);
 }
 
