@@ -16,6 +16,8 @@
 // only what it reads itself).  A run's rows are formed twice, for the maximum and for the codes: that
 // costs less than 64 registers a lane to keep them, and loops over the steps instead of unrolled
 // ones keep the code within the instruction cache.
+#include <type_traits>
+
 #include "quant.cuh"
 #include "rope_rows.cuh"
 
@@ -465,43 +467,55 @@ template <typename T, int D> cudaError_t launch_write(const RopeArgs &a, cudaStr
     return a.rot == D ? launch_write<T, D, kAllHalves>(a, st) : launch_write<T, D, kHalves>(a, st);
 }
 
-// Reading back: a thread has 8 features of a token's head, of K and of V.
-template <typename T, int D> __global__ __launch_bounds__(kThreads) void k_cache_dequant(const DequantArgs a)
+// Reading back: a thread has 16 bytes of output of a token's head, of K and of V, kAhead of them under way at a time; a block
+// has `share` tokens.
+template <typename T, int D> __global__ __launch_bounds__(kThreads) void k_cache_dequant(const DequantArgs a, int share, int page_lg, const Over over)
 {
-    constexpr int kPer = D / 8;
+    constexpr int E = Vec<T>::E, kPer = D / E, kAhead = 4;
     ptx::griddep_wait();
     ptx::griddep_launch_dependents();
-    const size_t total = (size_t)a.n_tok * a.Hkv * kPer;
-    for (size_t x = (size_t)blockIdx.x * kThreads + threadIdx.x; x < total; x += (size_t)gridDim.x * kThreads) {
-        const int c = (int)(x % kPer);
-        const size_t th = x / kPer;
-        const int h = (int)(th % a.Hkv), t = (int)(th / a.Hkv);
-        const int slot = __ldg(a.slots + t), page = slot / a.page_size;
-        const bool there = slot >= 0 && page < a.n_pages;
-        if (slot >= 0 && !there) raise_error(a.err, ERR_BAD_INDEX);
-        const size_t row = there ? ((size_t)page * a.Hkv + h) * a.page_size + slot % a.page_size : 0;
+    const int t0 = blockIdx.x * share, n = min(share, a.n_tok - t0), units = a.Hkv * kPer, total = n * units;
+    using Codes = typename std::conditional<E == 8, uint2, uint32_t>::type;
+    auto codes_of = [](const Codes &c, int i) -> uint32_t {
+        if constexpr (E == 8) return i == 0 ? c.x : c.y;
+        else return c;
+    };
+    for (int x0 = threadIdx.x; x0 < total; x0 += kAhead * kThreads) {
+        Codes k[kAhead], v[kAhead];
+        float ks[kAhead], vs[kAhead];
 #pragma unroll
-        for (int y = 0; y < 2; ++y) {
-            float f[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-            if (there) {
-                const uint2 v = __ldg(reinterpret_cast<const uint2 *>(static_cast<const uint8_t *>(y ? a.V_cache : a.K_cache) + row * D + 8 * c));
-                const float s = __ldg((y ? a.V_scale : a.K_scale) + row / kGroup);
-                float lo[4], hi[4];
-                decode4(v.x, lo);
-                decode4(v.y, hi);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    f[i] = lo[i] * s;
-                    f[i + 4] = hi[i] * s;
-                }
+        for (int i = 0; i < kAhead; ++i) {
+            const int x = x0 + i * kThreads, t = over(x), u = x - t * units, h = u / kPer;
+            const int slot = x < total ? __ldg(a.slots + t0 + t) : -1, page = slot >> page_lg;
+            k[i] = v[i] = Codes{};
+            ks[i] = vs[i] = 0.f;
+            if (slot >= 0 && page < a.n_pages) {
+                const size_t row = (((size_t)page * a.Hkv + h) << page_lg) + (slot & ((1 << page_lg) - 1)), at = row * D + u % kPer * E;
+                k[i] = __ldg(reinterpret_cast<const Codes *>(static_cast<const uint8_t *>(a.K_cache) + at));
+                v[i] = __ldg(reinterpret_cast<const Codes *>(static_cast<const uint8_t *>(a.V_cache) + at));
+                ks[i] = __ldg(a.K_scale + row / kGroup);
+                vs[i] = __ldg(a.V_scale + row / kGroup);
+            } else if (slot >= 0) {
+                raise_error(a.err, ERR_BAD_INDEX);
             }
-            T *out = static_cast<T *>(y ? a.V : a.K) + x * 8;
-            if constexpr (sizeof(T) == 2) {
-                *reinterpret_cast<uint4 *>(out) = make_uint4(pipe::pack_bf16x2(f[0], f[1]), pipe::pack_bf16x2(f[2], f[3]),
-                                                             pipe::pack_bf16x2(f[4], f[5]), pipe::pack_bf16x2(f[6], f[7]));
-            } else {
-                *reinterpret_cast<float4 *>(out) = make_float4(f[0], f[1], f[2], f[3]);
-                *reinterpret_cast<float4 *>(out + 4) = make_float4(f[4], f[5], f[6], f[7]);
+        }
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const int x = x0 + i * kThreads;
+            if (x >= total) break;
+            const size_t to = ((size_t)t0 * units + x) * E;
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+                const float s = y ? vs[i] : ks[i];
+                f32x2 out[E / 2];
+#pragma unroll
+                for (int z = 0; z < E / 4; ++z) {
+                    float f[4];
+                    decode4(codes_of(y ? v[i] : k[i], z), f);
+                    out[2 * z] = pair2(f[0] * s, f[1] * s);
+                    out[2 * z + 1] = pair2(f[2] * s, f[3] * s);
+                }
+                *reinterpret_cast<uint4 *>(static_cast<T *>(y ? a.V : a.K) + to) = Vec<T>::pack(out);
             }
         }
     }
@@ -509,9 +523,15 @@ template <typename T, int D> __global__ __launch_bounds__(kThreads) void k_cache
 
 template <typename T, int D> cudaError_t launch_read(const DequantArgs &a, cudaStream_t st)
 {
-    const size_t total = (size_t)a.n_tok * a.Hkv * (D / 8), most = (size_t)8 * pipe::sm_count();
-    const size_t blocks = (total + kThreads - 1) / kThreads;
-    return pipe::launch_early(k_cache_dequant<T, D>, dim3((unsigned)(blocks < most ? blocks : most)), dim3(kThreads), 0, st, a);
+    // a block has a round of its threads at least; of many tokens, one in 16 blocks to a multiprocessor
+    const int units = a.Hkv * (D / Vec<T>::E), least = (kThreads + units - 1) / units, held = 16 * pipe::sm_count();
+    int share = (a.n_tok + held - 1) / held;
+    if (share < least) share = least;
+    // (their quotients are taken by multiplication: 2^18 of them, of at most 2^13 units a token)
+    if (share > (1 << 18) / units) share = (1 << 18) / units;
+    int lg = 4;
+    while ((1 << lg) < a.page_size) ++lg;
+    return pipe::launch_early(k_cache_dequant<T, D>, dim3((a.n_tok + share - 1) / share), dim3(kThreads), 0, st, a, share, lg, Over::of(units));
 }
 
 }  // namespace
