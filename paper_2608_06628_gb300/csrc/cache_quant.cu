@@ -253,6 +253,11 @@ __device__ __forceinline__ void write_head(const RopeArgs &a, const Run &run, in
     if (lane == 0 && (fresh || e != has)) *scale = scale_value(e);
 }
 
+__device__ __forceinline__ void prefetch_l2(const void *p, uint32_t bytes)
+{
+    asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(__cvta_generic_to_global(p)), "r"(bytes) : "memory");
+}
+
 // Quotients of x by a number n, x n < 2^32, without a division.
 struct Over {
     unsigned by;                // 2^32 / n, rounded up; 0: n is 1
@@ -287,6 +292,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_cache_write(const RopeArgs a, i
     extern __shared__ __align__(16) float s_keys[];         // of each warp's run, then the window's angles
     float *s_angles = s_keys + kWarps * R::kKeys;
     __shared__ int s_slot[kGroup + kReach + 1];             // of the tokens from 16 before the window on
+    __shared__ int s_pos[kReach];                           // positions of the window's tokens
     __shared__ int s_run[kWindow];                          // first tokens of the runs that begin in the window
     __shared__ int s_runs, s_end;                           // their number, and the end of the last
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, sub = lane / R::L;
@@ -300,23 +306,34 @@ __global__ __launch_bounds__(kThreads, 2) void k_cache_write(const RopeArgs a, i
         const long long t = (long long)t0 - kGroup + tid;
         return tid < kGroup + kReach && t >= 0 && t < a.n_tok ? __ldg(a.slots + t) : -1;
     };
-    int next_slot = slot_at(t_begin);
+    auto position_at = [&](int t0) {
+        return a.rot > 0 && tid < kReach && tid < a.n_tok - t0 ? __ldg(a.positions + t0 + tid) : 0;
+    };
+    // A window's rows on their way to L2 while the one before it is worked on: a thread has a token's keys or values.
+    auto prefetch = [&](int t0) {
+        if (tid >= 2 * min(window, t_end - t0)) return;
+        const size_t t = t0 + (tid >> 1);
+        prefetch_l2(tid & 1 ? static_cast<const T *>(a.V) + t * a.v_stride : static_cast<const T *>(a.K) + t * a.k_stride,
+                    (uint32_t)(a.Hkv * D * sizeof(T)));
+    };
+    int next_slot = slot_at(t_begin), next_pos = position_at(t_begin);
+    if (window < share) prefetch(t_begin);
 #pragma unroll 1
     for (int t0 = t_begin, n_win; t0 < t_end; t0 += n_win) {
     n_win = min(window, t_end - t0);
     __syncthreads();                                        // the last window is done
     if (tid < kGroup + kReach) s_slot[tid] = next_slot;
+    if (tid < kReach) s_pos[tid] = next_pos;
     if (tid == 0) s_runs = s_end = 0;
-    if (n_win < t_end - t0) next_slot = slot_at(t0 + n_win);
     __syncthreads();
     auto group_of = [&](int i) {                            // of token t0 + i, -1 without a slot
         const int slot = s_slot[kGroup + i];
         return slot >= 0 && slot < slots ? slot / kGroup : -1;
     };
+    if (tid < kReach && s_slot[kGroup + tid] >= slots && blockIdx.y == 0) raise_error(a.err, ERR_BAD_INDEX);
     if (tid < n_win) {
         // A run begins here unless the last token with a slot before this one, of the 15 before, is of its group.
         const int mine = group_of(tid);
-        if (mine < 0 && s_slot[kGroup + tid] >= slots && blockIdx.y == 0) raise_error(a.err, ERR_BAD_INDEX);
         bool begins = mine >= 0;
         for (int i = 1; begins && i < kGroup; ++i) {
             const int g = group_of(tid - i);
@@ -337,6 +354,12 @@ __global__ __launch_bounds__(kThreads, 2) void k_cache_write(const RopeArgs a, i
         }
     }
     __syncthreads();
+    n_win = max(n_win, min(s_end, t_end - t0));             // the next window begins behind the last run
+    if (n_win < t_end - t0) {
+        next_slot = slot_at(t0 + n_win);
+        next_pos = position_at(t0 + n_win);
+        prefetch(t0 + n_win);
+    }
     auto run_from = [&](int at) {                           // the run that begins at token t0 + at
         Run run;
         run.slot = lane < kGroup ? s_slot[kGroup + at + lane] : -1;
@@ -350,26 +373,23 @@ __global__ __launch_bounds__(kThreads, 2) void k_cache_write(const RopeArgs a, i
         run.off = group * kGroup & (a.page_size - 1);
         return run;
     };
-    const int heads = 2 * a.Hkv, n_heads = s_runs * heads;
+    const int n_keys = s_runs * a.Hkv, n_heads = 2 * n_keys;     // (keys take longer: first)
     const int steps = (a.Hq + RPW - 1) / RPW, n_steps = a.Q ? n_win * steps : 0;
     const int n_work = n_heads + (n_steps + R::kSteps - 1) / R::kSteps;
-    // the run of a piece of work that is a head
-    auto run_of = [&](int work, int &head) {
-        const int nth = over_heads(work);
-        head = work - nth * heads;
-        return run_from(s_run[nth]);
-    };
     // a piece's rows
     uint4 raw[R::kSteps];
     Run run;
+    bool key = false;
     int head = 0, s0 = 0, n = 0;
     auto load_rows = [&](int work) {
         if (work < n_heads) {
-            run = run_of(work, head);
-            const bool key = head < a.Hkv;
+            key = work < n_keys;
+            const int at = key ? work : work - n_keys, nth = over_heads(at);
+            run = run_from(s_run[nth]);
+            head = at - nth * a.Hkv;
             const size_t stride = key ? a.k_stride : a.v_stride;
             const T *src = static_cast<const T *>(key ? a.K : a.V) + (size_t)(run.t + sub) * stride +
-                           (size_t)(key ? head : head - a.Hkv) * D + piece.first;
+                           (size_t)head * D + piece.first;
 #pragma unroll
             for (int i = 0; i < R::kSteps; ++i) {
                 raw[i] = run.has(i * RPW + sub) ? load<kLayout>(src, piece.apart()) : make_uint4(0, 0, 0, 0);
@@ -398,7 +418,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_cache_write(const RopeArgs a, i
         for (int x = tid; x < n_angles * kMaxPairs; x += kThreads) {
             const int pair = x % kMaxPairs;
             if (pair < half) {
-                const float2 v = angle(a, t0 + x / kMaxPairs, pair);
+                const float2 v = angle_at(a, (unsigned long long)(long long)s_pos[x / kMaxPairs], pair);
                 s_angles[x / kMaxPairs * kTable + pair] = v.x;
                 s_angles[x / kMaxPairs * kTable + kMaxPairs + pair] = v.y;
                 s_angles[x / kMaxPairs * kTable + 2 * kMaxPairs + pair] = -v.y;
@@ -409,8 +429,8 @@ __global__ __launch_bounds__(kThreads, 2) void k_cache_write(const RopeArgs a, i
 #pragma unroll 1
     while (work < n_work) {
         if (work < n_heads) {
-            if (head < a.Hkv) write_head<T, D, kLayout, true>(a, run, head, raw, s_angles + (run.t - t0) * kTable, mine);
-            else write_head<T, D, kLayout, false>(a, run, head - a.Hkv, raw, nullptr, 0);
+            if (key) write_head<T, D, kLayout, true>(a, run, head, raw, s_angles + (run.t - t0) * kTable, mine);
+            else write_head<T, D, kLayout, false>(a, run, head, raw, nullptr, 0);
         } else {
             f32x2 w[E / 2];
             if (a.wq) Vec<T>::unpack(load<kLayout>(static_cast<const T *>(a.wq) + piece.first, piece.apart()), w);
@@ -459,7 +479,7 @@ template <typename T, int D, Layout kLayout> cudaError_t launch_write(const Rope
     int lg = 4;
     while ((1 << lg) < a.page_size) ++lg;
     return pipe::launch_early(k_cache_write<T, D, kLayout>, dim3(blocks, y), dim3(kThreads), Rows<T, D>::kBytes, st, a, share, window, lg,
-                              Over::of((a.Hq + Rows<T, D>::RPW - 1) / Rows<T, D>::RPW), Over::of(2 * a.Hkv));
+                              Over::of((a.Hq + Rows<T, D>::RPW - 1) / Rows<T, D>::RPW), Over::of(a.Hkv));
 }
 template <typename T, int D> cudaError_t launch_write(const RopeArgs &a, cudaStream_t st)
 {
