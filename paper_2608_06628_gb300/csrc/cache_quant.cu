@@ -253,11 +253,6 @@ __device__ __forceinline__ void write_head(const RopeArgs &a, const Run &run, in
     if (lane == 0 && (fresh || e != has)) *scale = scale_value(e);
 }
 
-__device__ __forceinline__ void prefetch_l2(const void *p, uint32_t bytes)
-{
-    asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(__cvta_generic_to_global(p)), "r"(bytes) : "memory");
-}
-
 // Quotients of x by a number n, x n < 2^32, without a division.
 struct Over {
     unsigned by;                // 2^32 / n, rounded up; 0: n is 1
@@ -309,15 +304,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_cache_write(const RopeArgs a, i
     auto position_at = [&](int t0) {
         return a.rot > 0 && tid < kReach && tid < a.n_tok - t0 ? __ldg(a.positions + t0 + tid) : 0;
     };
-    // A window's rows on their way to L2 while the one before it is worked on: a thread has a token's keys or values.
-    auto prefetch = [&](int t0) {
-        if (tid >= 2 * min(window, t_end - t0)) return;
-        const size_t t = t0 + (tid >> 1);
-        prefetch_l2(tid & 1 ? static_cast<const T *>(a.V) + t * a.v_stride : static_cast<const T *>(a.K) + t * a.k_stride,
-                    (uint32_t)(a.Hkv * D * sizeof(T)));
-    };
     int next_slot = slot_at(t_begin), next_pos = position_at(t_begin);
-    if (window < share) prefetch(t_begin);
 #pragma unroll 1
     for (int t0 = t_begin, n_win; t0 < t_end; t0 += n_win) {
     n_win = min(window, t_end - t0);
@@ -358,7 +345,6 @@ __global__ __launch_bounds__(kThreads, 2) void k_cache_write(const RopeArgs a, i
     if (n_win < t_end - t0) {
         next_slot = slot_at(t0 + n_win);
         next_pos = position_at(t0 + n_win);
-        prefetch(t0 + n_win);
     }
     auto run_from = [&](int at) {                           // the run that begins at token t0 + at
         Run run;
