@@ -29,7 +29,7 @@ using namespace quant;
 
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
-constexpr int kWindow = 48;             // most tokens of a window
+constexpr int kWindow = 80;             // most tokens of a window
 constexpr int kReach = kWindow + kGroup - 1;    // and of the runs that begin in it
 
 struct Run {
@@ -41,7 +41,7 @@ struct Run {
     __device__ bool has(int r) const { return members >> r & 1u; }
 };
 
-constexpr int kTable = 3 * kMaxPairs;    // floats of a token's angles: cosines, sines, and sines with the other sign
+constexpr int kTable = 2 * kMaxPairs;    // floats of a token's angles: cosines, sines
 
 template <typename T, int D> struct Rows {
     static constexpr int E = Vec<T>::E, L = D / E, RPW = 32 / L;        // elements of a lane, lanes of a row, rows of a step
@@ -56,9 +56,9 @@ template <int E, bool kInter> __device__ __forceinline__ void read_angles(const 
     if constexpr (kInter) {
 #pragma unroll
         for (int i = 0; i < E / 2; ++i) {
-            const float c = table[pair0 + i], s = table[kMaxPairs + pair0 + i], ns = table[2 * kMaxPairs + pair0 + i];
+            const float c = table[pair0 + i], s = table[kMaxPairs + pair0 + i];
             r.c[i] = pair2(c, c);
-            r.s[i] = pair2(ns, s);
+            r.s[i] = pair2(-s, s);
         }
     } else if constexpr (E == 8) {
         auto two = [](const float *p, f32x2 (&v)[2]) {
@@ -68,11 +68,13 @@ template <int E, bool kInter> __device__ __forceinline__ void read_angles(const 
         };
         two(table + pair0, r.c);
         two(table + kMaxPairs + pair0, r.s);
-        two(table + 2 * kMaxPairs + pair0, r.ns);
     } else {
         r.c[0].v = *reinterpret_cast<const unsigned long long *>(table + pair0);
         r.s[0].v = *reinterpret_cast<const unsigned long long *>(table + kMaxPairs + pair0);
-        r.ns[0].v = *reinterpret_cast<const unsigned long long *>(table + 2 * kMaxPairs + pair0);
+    }
+    if constexpr (!kInter) {
+#pragma unroll
+        for (int i = 0; i < E / 4; ++i) r.ns[i].v = r.s[i].v ^ 0x8000000080000000ull;
     }
 }
 
@@ -407,7 +409,6 @@ __global__ __launch_bounds__(kThreads, 2) void k_cache_write(const RopeArgs a, i
                 const float2 v = angle_at(a, (unsigned long long)(long long)s_pos[x / kMaxPairs], pair);
                 s_angles[x / kMaxPairs * kTable + pair] = v.x;
                 s_angles[x / kMaxPairs * kTable + kMaxPairs + pair] = v.y;
-                s_angles[x / kMaxPairs * kTable + 2 * kMaxPairs + pair] = -v.y;
             }
         }
         __syncthreads();
