@@ -29,7 +29,7 @@ using namespace quant;
 
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
-constexpr int kWindow = 80;             // most tokens of a window
+constexpr int kWindow = 48;             // most tokens of a window
 constexpr int kReach = kWindow + kGroup - 1;    // and of the runs that begin in it
 
 struct Run {
