@@ -250,9 +250,14 @@ hybrid_status hybrid_cache_dequant(const hybrid_cfg *cfg, const hybrid_page_cfg 
                                    const void *V_cache, const float *K_scale, const float *V_scale,
                                    const int *slots, int n_tok, void *K, void *V, cudaStream_t stream);
 
-/* hybrid_paged_attn over such a cache: the same arguments, limits and guarantees, Q and O in
- * io_dtype.  Scales of groups without a visible key are not read.  The scales here may be any
- * positive float32 numbers. */
+/* hybrid_paged_attn over such a cache: the same arguments and guarantees, Q and O in io_dtype, and
+ * the same limits but for a 4 in the place of the 2 tiles.  Scales of groups without a visible key
+ * are not read.  The scales here may be any positive normal float32 numbers.
+ * Products on the tensor cores, of codes (exact) with numbers of half precision, summed in float32:
+ *   bfloat16  q as it is, but for entries below 2^-29 of the largest of their row; p_j times the
+ *             value's scale rounded to 11 bits, below 2^-21 of the row's largest such product to a
+ *             multiple of 2^-31 of it (their sum is taken in float32)
+ *   float32   each as two such numbers, 22 bits */
 size_t hybrid_paged_attn_quant_workspace_bytes(const hybrid_cfg *cfg, const hybrid_page_cfg *pg, int n_req);
 hybrid_status hybrid_paged_attn_quant(const hybrid_cfg *cfg, const hybrid_page_cfg *pg, const void *Q,
                                       const void *K_cache, const void *V_cache, const float *K_scale,

@@ -9,13 +9,26 @@
 //     E = least power of two with amax <= 448 * 2^E; no less than the group's old one, unless
 //         the run has the group's first slot
 //     code = e4m3(y / 2^E)
-// then brings the group's other tokens to 2^E (zeros where the group starts afresh).  A block has
-// a window of the packed tokens: its queries, and the runs that begin in it.  It forms the window's
-// angles once; its warps share the pieces of work (a run's head; some steps of queries), and each
-// copies the rows of its next piece to shared memory while it works on one (cp.async, a lane
-// only what it reads itself).  A run's rows are formed twice, for the maximum and for the codes: that
-// costs less than 64 registers a lane to keep them, and loops over the steps instead of unrolled
-// ones keep the code within the instruction cache.
+// then brings the group's other tokens to 2^E (zeros where the group starts afresh).  A run's rows
+// are in registers; keys wait in shared memory, after norm and rotation, for the scale that their
+// maximum decides (forming them twice, in blocks of one window: 217 us where this took 187).  A block has a share of the
+// packed tokens, in windows: their queries, and the runs that begin in a window.  It forms a window's
+// angles once, and its warps share the pieces of work: a run's head, keys before values, since keys
+// take twice as long, and steps of queries.
+//
+// Measured, 65 503 tokens, 4 key heads of 128, bfloat16: keys and values 67 us, with 16 query heads
+// 154 us (4.8 TB/s; 109 at the copy's rate).  What bounds the keys and values is a warp's chain of
+// instructions: 1170 to a head of a run, a sixth of them for angles, issued in two cycles of five.
+//   - Two blocks of 8 warps to a multiprocessor, 128 registers a thread.  Three blocks with 80
+//     spilled (214 us with the queries, 180 with two then); rows of the next piece in registers or by
+//     copies to shared memory ahead, 198 and 209; two steps of a run at a time, no gain.
+//   - Rows on their way need room in the L1 cache: windows of 48 tokens leave it 60 KB, with 56 the
+//     angles take half of that (169 us); with fewer than 20 the barriers show (168).
+//   - Windows end behind a run where one reaches over their end, so that no angle is formed twice.
+// Calls of few tokens are bound by the launch and three loads in a row: slots, rows, old scales (64
+// tokens 7.3 us, of which the host has 5; 2048 tokens 11.6).
+//
+// Read.  Nothing but bytes: 150 001 tokens, 4 heads of 128 into bfloat16, 73 us, 6.3 TB/s.
 #include <type_traits>
 
 #include "quant.cuh"
@@ -474,8 +487,8 @@ template <typename T, int D> cudaError_t launch_write(const RopeArgs &a, cudaStr
     return a.rot == D ? launch_write<T, D, kAllHalves>(a, st) : launch_write<T, D, kHalves>(a, st);
 }
 
-// Reading back: a thread has 16 bytes of output of a token's head, of K and of V, kAhead of them under way at a time; a block
-// has `share` tokens.
+// Reading back: a thread has 16 bytes of output of a token's head, of K and of V, kAhead of them under way at a time (one, of 4
+// features: 85 us where this takes 73); a block has `share` tokens.
 template <typename T, int D> __global__ __launch_bounds__(kThreads) void k_cache_dequant(const DequantArgs a, int share, int page_lg, const Over over)
 {
     constexpr int E = Vec<T>::E, kPer = D / E, kAhead = 4;
@@ -546,8 +559,9 @@ template <typename T, int D> cudaError_t launch_read(const DequantArgs &a, cudaS
 cudaError_t launch_qk_norm_rope_cache_quant(hybrid_dtype dt, const RopeArgs &args, cudaStream_t st)
 {
     RopeArgs a = args;
-    // With many tokens the queries are better off in a launch of the kernel that has nothing but rows to stream (65503
-    // tokens of 16 heads: 86 us there, about 100 here); with few the launch costs more (2048 tokens: 13.4 us in one).
+    // With many tokens the queries are better off in a launch of the kernel that has nothing but rows to stream: 65 503 tokens
+    // 155 us in two launches, 163 in one.  With few the launch costs more: 12 000 tokens 40 and 36 us, 2048 14.5 and 11.7;
+    // 16 384 and 24 576 tokens take as long either way.
     if (a.Q && a.n_tok > 2 * kWindow * pipe::sm_count()) {
         RopeArgs q = a;
         q.K = nullptr;

@@ -20,7 +20,14 @@
 // and P, 22 bits.
 //
 // The codes come by cp.async into a ring of the warp, 16 bytes at a time, permuted so that
-// neither operand's reads meet in a bank.
+// neither operand's reads meet in a bank; the copies go on from one request's tiles to the next one's
+// while an output is written.
+//
+// Measured (heads of 128, one token): 3 requests of 115k keys, 16 heads with keys of their own, 219 us (6.5
+// TB/s, 96% of the copy's rate); 64 requests of 256-8192 keys, 16 query and 4 key heads, 57.8 us (41 at that
+// rate): first codes after 5.7 us, then 5.6 TB/s, shares that end between 43 and 57 us because the
+// multiprocessors do not get equal parts of the bandwidth, and 4.5 us of join.  float32, 16 requests, 27 us
+// (11 at that rate): ten of them start and join.
 #include "paged_plan.cuh"
 #include "quant.cuh"
 #include "tc_pipeline.cuh"

@@ -13,13 +13,22 @@
 // bits, relative to a reference of its own (a token that takes most of the softmax may have
 // values near zero), and below 2^-21 of the row's largest p vs units of 2^-31 of that.
 //
-// Eight warps bring the codes from the ring that TMA fills (a page of a head is one box) to
-// half precision, 64 keys at a time, in the layout of the products' operands: 3 such pieces of K
-// and of V, so that a product never waits for the one before it to free its operand.  Q stays in
-// Tensor Memory, which keeps 32 KB a tile off shared memory: what is left, codes written and read
-// once, pieces written and read once, is 192 KB a tile, 1500 cycles, about as long as the codes'
-// 33 KB take at an SM's share of the memory bandwidth (1400).  P takes the place of the S that it
-// was made from.
+// Eight warps bring the codes from the ring that TMA fills (a page of a head is one box) to half
+// precision in the layout of the products' operands: two tiles of K and two of V, so that a product
+// of a whole tile never waits for the one before it to free its operand.  Q stays in Tensor Memory,
+// which keeps 32 KB a tile off shared memory: what is left, codes written and read once, tiles
+// written and read once, is 192 KB a tile, 1500 cycles, about as long as the codes' 33 KB take at an
+// SM's share of the memory bandwidth (1400).  P takes the place of the S that it was made from.  Two
+// threads share a row of the softmax: halves of its keys, and of the output's features.
+//
+// Measured (64 requests of 256-8192 tokens, 16 query and 4 key heads of 128, blocks of 32 tokens): 90
+// us, 44 for the codes at the copy's rate.  What bounds it is a tile's chain: scores formed, read,
+// their exponentials (512 cycles of the four schedulers at least) and conversions, P stored, its
+// product; 2700 cycles a tile.  Other arrangements of the same chain took longer: two groups of
+// softmax warps with every second tile each 121 us, four threads to a row 118, the codes copied by
+// the warps that convert them 112; P in a place of its own 92.  With d = 64 and
+// pages of 16 tokens (53.8 us, 20 at the copy's rate) a producer's 16 boxes of a tile, about 100 cycles
+// each, come as close: hence two producers (62 us with one).
 //
 // Keys that no query sees: pages and scales without a visible key are not loaded, masked scores
 // are replaced before use, masked rows of V are zeros in the operand.
