@@ -297,6 +297,43 @@ def test_write_in_place_and_same_bits():
     assert torch.equal(run_write(s).view(torch.uint8), want[0])
 
 
+@pytest.mark.parametrize("dt,inter", [(BF, False), (F32, True)])
+def test_padding_within_the_runs_of_many_tokens(dt, inter):
+    """Tokens without a slot anywhere, the ends of the blocks' windows and shares among them."""
+    rng = random.Random(11)
+    s = write_setup(dt, [(rng.randint(0, 50), rng.randint(1, 1500)) for _ in range(40)], 2, 1, 64, 16, rot=32, inter=inter, seed=7)
+    assert s["T"] > 20000
+    gone = torch.rand(s["T"], generator=gen(3), device="cuda") < 0.2
+    s["slots"][gone] = -1
+    before = copies(*s["cache"])
+    run_write(s)
+    H.hybrid_check()
+    check_write(s, before, "padding within runs")
+
+
+def test_a_slot_beyond_the_pool_is_reported_wherever_it_is():
+    s = write_setup(BF, [(5, 16000)], 1, 1, 64, 128, seed=2)
+    slots, last = s["slots"].clone(), s["T"] - 1
+    for at in [0, last - 1, last, *range(90, 170)]:
+        s["slots"].copy_(slots)
+        s["slots"][at] = s["n_pages"] * s["P"]
+        run_write(s, queries=at % 2 == 0)
+        assert H.hybrid_check(check=False) == H.HYBRID_ERR_DEVICE, at
+        assert H.hybrid_check(check=False) == H.HYBRID_OK
+
+
+def test_many_queries_in_place():
+    s = write_setup(BF, [(9, 20000), (0, 11000)], 2, 1, 64, 64, seed=6)
+    q, first = s["q"].contiguous(), copies(*s["cache"])
+    want = run_write(s)
+    after, s["cache"] = s["cache"], first
+    H.hybrid_qk_norm_rope_cache_quant(s["cfg"], s["rope"], s["pg"], q, 2 * 64, s["k"], s["stride"], s["v"], s["stride"], s["T"], s["wq"],
+                                      s["wk"], s["pos"], s["freqs"], s["slots"], q, *s["cache"])
+    H.hybrid_check()
+    for x, y in zip((q, *s["cache"]), (want, *after)):
+        assert torch.equal(x.view(torch.uint8), y.view(torch.uint8))
+
+
 # ------------------------------------------------------------------ reading back
 
 def read(cfg, pg, cache, slots, dt):
