@@ -17,13 +17,13 @@
 // take twice as long, and steps of queries.
 //
 // Measured, 65 503 tokens, 4 key heads of 128, bfloat16: keys and values 67 us, with 16 query heads
-// 154 us (4.8 TB/s; 109 at the copy's rate).  What bounds the keys and values is a warp's chain of
+// 144 us (5.1 TB/s; 109 at the copy's rate).  What bounds the keys and values is a warp's chain of
 // instructions: 1170 to a head of a run, a sixth of them for angles, issued in two cycles of five.
 //   - Two blocks of 8 warps to a multiprocessor, 128 registers a thread.  Three blocks with 80
 //     spilled (214 us with the queries, 180 with two then); rows of the next piece in registers or by
 //     copies to shared memory ahead, 198 and 209; two steps of a run at a time, no gain.
 //   - Rows on their way need room in the L1 cache: windows of 48 tokens leave it 60 KB, with 56 the
-//     angles take half of that (169 us); with fewer than 20 the barriers show (168).
+//     angles take half of that (74 us, with the queries 155); with fewer than 20 the barriers show (82).
 //   - Windows end behind a run where one reaches over their end, so that no angle is formed twice.
 // Calls of few tokens are bound by the launch and three loads in a row: slots, rows, old scales (64
 // tokens 7.3 us, of which the host has 5; 2048 tokens 11.6).
@@ -462,11 +462,12 @@ __global__ __launch_bounds__(kThreads, 2) void k_cache_write(const RopeArgs a, i
     }
 }
 
-template <typename T, int D, Layout kLayout> cudaError_t launch_write(const RopeArgs &a, cudaStream_t st)
+template <typename T, int D, Layout kLayout> cudaError_t launch_write(const RopeArgs &a, bool beside, cudaStream_t st)
 {
+    // `beside`: the queries' kernel has the other half of each multiprocessor.
     // A block to a token while the GPU holds them (each may be a run of its own), else a share of the tokens to each of the
     // blocks that it holds, in windows of about equal size.
-    const int held = 2 * pipe::sm_count();
+    const int held = (beside ? 1 : 2) * pipe::sm_count();
     const int share = (a.n_tok + held - 1) / held, windows = (share + kWindow - 1) / kWindow, window = (share + windows - 1) / windows;
     const int blocks = (a.n_tok + share - 1) / share;
     const int steps = a.Q ? (a.Hq + Rows<T, D>::RPW - 1) / Rows<T, D>::RPW * window : 0;
@@ -481,10 +482,10 @@ template <typename T, int D, Layout kLayout> cudaError_t launch_write(const Rope
     return pipe::launch_early(k_cache_write<T, D, kLayout>, dim3(blocks, y), dim3(kThreads), Rows<T, D>::kBytes, st, a, share, window, lg,
                               Over::of((a.Hq + Rows<T, D>::RPW - 1) / Rows<T, D>::RPW), Over::of(a.Hkv));
 }
-template <typename T, int D> cudaError_t launch_write(const RopeArgs &a, cudaStream_t st)
+template <typename T, int D> cudaError_t launch_write(const RopeArgs &a, bool beside, cudaStream_t st)
 {
-    if (a.interleaved) return launch_write<T, D, kInterleaved>(a, st);
-    return a.rot == D ? launch_write<T, D, kAllHalves>(a, st) : launch_write<T, D, kHalves>(a, st);
+    if (a.interleaved) return launch_write<T, D, kInterleaved>(a, beside, st);
+    return a.rot == D ? launch_write<T, D, kAllHalves>(a, beside, st) : launch_write<T, D, kHalves>(a, beside, st);
 }
 
 // Reading back: a thread has 16 bytes of output of a token's head, of K and of V, kAhead of them under way at a time (one, of 4
@@ -559,19 +560,20 @@ template <typename T, int D> cudaError_t launch_read(const DequantArgs &a, cudaS
 cudaError_t launch_qk_norm_rope_cache_quant(hybrid_dtype dt, const RopeArgs &args, cudaStream_t st)
 {
     RopeArgs a = args;
-    // With many tokens the queries are better off in a launch of the kernel that has nothing but rows to stream: 65 503 tokens
-    // 155 us in two launches, 163 in one.  With few the launch costs more: 12 000 tokens 40 and 36 us, 2048 14.5 and 11.7;
-    // 16 384 and 24 576 tokens take as long either way.
-    if (a.Q && a.n_tok > 2 * kWindow * pipe::sm_count()) {
-        RopeArgs q = a;
-        q.K = nullptr;
-        q.slots = nullptr;
-        const cudaError_t e = launch_qk_norm_rope(dt, q, st);
-        if (e != cudaSuccess) return e;
-        a.Q = nullptr;
-    }
-    if (dt == HYBRID_BF16) return a.d == 128 ? launch_write<__nv_bfloat16, 128>(a, st) : launch_write<__nv_bfloat16, 64>(a, st);
-    return a.d == 128 ? launch_write<float, 128>(a, st) : launch_write<float, 64>(a, st);
+    // Queries of many tokens take the kernel that has nothing but rows to stream, beside this one: memory bounds the one, its
+    // warps' latencies the other (65 503 tokens: 144 us, 154 one after the other, 162 in one launch; 12 000: 34 and 36). Up to
+    // 64 tokens a multiprocessor one launch takes as long (8192 tokens 25 us either way), and less of the host's time.
+    const bool beside = a.Q && a.n_tok > 64 * pipe::sm_count();
+    if (beside) a.Q = nullptr;
+    cudaError_t e;
+    if (dt == HYBRID_BF16) e = a.d == 128 ? launch_write<__nv_bfloat16, 128>(a, beside, st) : launch_write<__nv_bfloat16, 64>(a, beside, st);
+    else e = a.d == 128 ? launch_write<float, 128>(a, beside, st) : launch_write<float, 64>(a, beside, st);
+    if (!beside || e != cudaSuccess) return e;
+    RopeArgs q = args;
+    q.K = nullptr;
+    q.slots = nullptr;
+    q.beside = true;
+    return launch_qk_norm_rope(dt, q, st);
 }
 
 cudaError_t launch_cache_dequant(hybrid_dtype dt, const DequantArgs &a, cudaStream_t st)

@@ -117,7 +117,9 @@ __global__ __launch_bounds__(kThreads, 4) void k_qk_norm_rope(const RopeArgs a, 
     const Pieces<D, E, kLayout> piece(a, lane % L);
     const int apart = piece.apart();
     const uint32_t ring0 = ptx::smem_u32(&s_ring[tid]), ring_end = ring0 + kDepth * kSlot;
-    ptx::griddep_wait();
+    // `beside`: each block of the kernel before this one has waited for what comes before both by the time that this one starts,
+    // and this one does not need its results.  Its end is awaited by the last block, so that what follows finds both done.
+    if (!a.beside) ptx::griddep_wait();
     ptx::griddep_launch_dependents();
     Cursor<RPW> at;
     if (!at.begin(split, blockIdx.x * kWarps + warp)) return;
@@ -208,6 +210,7 @@ __global__ __launch_bounds__(kThreads, 4) void k_qk_norm_rope(const RopeArgs a, 
             advance(Vec<T>::pack(x));
         }
     } while (at.next(split));
+    if (a.beside && blockIdx.x == gridDim.x - 1) ptx::griddep_wait();
 }
 
 template <typename T, int D, Layout kLayout>

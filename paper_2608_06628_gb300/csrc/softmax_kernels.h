@@ -38,6 +38,7 @@ struct RopeArgs {
     int rot, interleaved, page_size, n_pages;
     float scale, eps;
     unsigned *err;
+    bool beside;                      // runs beside the kernel before it in the stream (see qk_norm_rope.cu)
 };
 cudaError_t launch_qk_norm_rope(hybrid_dtype dt, const RopeArgs &a, cudaStream_t st);
 cudaError_t launch_qk_norm_rope_backward(hybrid_dtype dt, const RopeArgs &a, cudaStream_t st);

@@ -334,6 +334,49 @@ def test_many_queries_in_place():
         assert torch.equal(x.view(torch.uint8), y.view(torch.uint8))
 
 
+@pytest.mark.parametrize("captured", [False, True])
+def test_what_follows_a_write_of_many_tokens_finds_it_done(captured):
+    """Keys and values are written beside the queries: reading, and the next write, begin when both are done."""
+    s = write_setup(BF, [(0, 9000), (0, 16001)], 4, 4, 128, 64, seed=6)
+    first, T = copies(*s["cache"]), s["T"]
+    x = [torch.randn(T, 12 * 128 + 16, generator=gen(i), device="cuda").to(BF) for i in range(3)]
+    wide = torch.empty_like(x[0])
+    rows = wide[:, :12 * 128].unflatten(1, (-1, 128))
+    s.update(q=rows[:, :4], k=rows[:, 4:8], v=rows[:, 8:], stride=wide.shape[1])
+
+    def chain():
+        """Writes, each read at once; the last one's queries too."""
+        out = []
+        for y in x:
+            wide.copy_(y)
+            qo = run_write(s)
+            out += [*read(s["cfg"], s["pg"], s["cache"], s["slots"], BF), qo + 0]
+        return out
+
+    want = []
+    for y in x:                                             # the same, one after the other
+        wide.copy_(y)
+        torch.cuda.synchronize()
+        qo = run_write(s)
+        torch.cuda.synchronize()
+        want += [*read(s["cfg"], s["pg"], s["cache"], s["slots"], BF), qo]
+        torch.cuda.synchronize()
+    for c, f in zip(s["cache"], first):
+        c.view(torch.uint8).copy_(f.view(torch.uint8))
+    if captured:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            out = chain()
+    for _ in range(5):
+        if captured:
+            graph.replay()
+        else:
+            out = chain()
+        H.hybrid_check()
+        for got, w in zip(out, want):
+            assert torch.equal(got, w)
+
+
 # ------------------------------------------------------------------ reading back
 
 def read(cfg, pg, cache, slots, dt):
