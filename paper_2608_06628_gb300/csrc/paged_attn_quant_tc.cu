@@ -48,9 +48,9 @@ using namespace pipe;
 constexpr int kSmemLimit = 232448;
 constexpr int kMaxSlots = 12;
 constexpr int kTiles = 2;                 // of K, and of V, in half precision
-constexpr int kScaleTiles = 32;           // tiles whose scales are held (see the producer)
-constexpr uint32_t kBarBytes = 1024;      // barriers, TMEM address, failure flag, the plan's scratch
-constexpr uint32_t kScaleBytes = kScaleTiles * 16 * 4;
+constexpr uint32_t kBarBytes = 512;       // barriers, TMEM address, failure flag, the plan's scratch
+template <int D> constexpr int kScaleTiles = D == 128 ? 8 : 16;      // tiles whose scales are held: NK + 4 (see the producer)
+template <int D> constexpr uint32_t kScaleBytes = kScaleTiles<D> * 16 * 4;
 constexpr uint32_t kExchange = 2048;      // two floats a thread of the softmax
 // with copies: 64 inverse sums, and 128 rows of 32 + 4 features (a quarter of the rows: 128 + 4)
 constexpr uint32_t kStage = 256 + 128 * 36 * 4;
@@ -122,8 +122,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_quant_tc(const __gri
     // Tensor Memory columns: S (2 x 128; then P in the first 32 of each half), O, Q
     constexpr uint32_t cS = 0, cO = 256, cQ = 384;
     const PagedArgs &a = ta.p;
-    extern __shared__ uint8_t smem_raw[];
-    uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    extern __shared__ __align__(1024) uint8_t smem[];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, NK = ta.NK, NV = ta.NV;
     const int rows = a.Bt * a.Gt;
     // quarters of the lanes with rows, softmax warps at work
@@ -146,8 +145,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_quant_tc(const __gri
     uint32_t *tmem_holder = reinterpret_cast<uint32_t *>(drained + 2);
     volatile int *fail = reinterpret_cast<volatile int *>(tmem_holder + 1);
     PlanSmem *plan_smem = reinterpret_cast<PlanSmem *>(tmem_holder + 2);
+    static_assert((2 * kMaxSlots + 4 * kTiles + 10) * 8 + 8 + sizeof(PlanSmem) <= kBarBytes, "room for the barriers");
     float *scales = reinterpret_cast<float *>(smem + ta.off_bar + kBarBytes);     // [kScaleTiles][8 of K, 8 of V]
-    float *exchange = scales + kScaleBytes / 4;            // [2][2][128]
+    float *exchange = scales + kScaleBytes<D> / 4;            // [2][2][128]
     float *inv_of = exchange + 512;                        // [64], with copies
 
     if (warp == kIssueS) {
@@ -254,14 +254,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_quant_tc(const __gri
                             tma_load_4d(dst_v, &ta.tmV, 0, 0, head, page, &full[sv]);
                         }
                     }
-                    // Zeros for groups without a visible key.  The place was that of 32 tiles ago, whose softmax is done:
-                    // the slot's last tile, at most 6 ago, is converted, so S of the second tile before that one is
-                    // formed, and that waited for the softmax of the second tile before it.
+                    // Zeros for groups without a visible key.  The place was that of NK + 4 tiles ago or an earlier one, whose
+                    // softmax is done: the slot's last tile, NK ago, is converted, so S of the second tile before that one is
+                    // formed, and that waited for the product with P of the second tile before it.
                     const int of = __shfl_sync(0xffffffffu, page, group >> lg);
                     const bool see = whole || any_visible(w.vis, tile * kTile + group, 16);
                     if (lane < 16) {
                         const float *src = my_scale + (see ? (((size_t)of * a.Hkv + head) << lg | (group & (P - 1))) / 16 : 0);
-                        asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(smem_u32(scales + now % kScaleTiles * 16 + lane)),
+                        asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(smem_u32(scales + now % kScaleTiles<D> * 16 + lane)),
                                      "l"(src), "r"(see ? 4 : 0)
                                      : "memory");
                     }
@@ -506,7 +506,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn_quant_tc(const __gri
                 auto below = [](int k) { return k >= 32 ? ~0u : (k <= 0 ? 0u : (1u << k) - 1); };
                 wait(&sready[b], (n >> 1) & 1u);
                 tc_fence_after();
-                const float *my_scales = scales + n % kScaleTiles * 16 + key0 / 16;
+                const float *my_scales = scales + n % kScaleTiles<D> * 16 + key0 / 16;
                 const uint32_t my_s = tmem + cS + 128 * b + lane_off;
                 // P lies in the half of S that its keys have: where it meets scores of the lane's other thread, they have
                 // been read before the vote below, and those of its own that are read twice lie ahead of it
@@ -757,14 +757,18 @@ template <int D, int kCopies> cudaError_t launch(const PagedArgs &a, cudaStream_
 {
     TcArgs ta;
     ta.p = a;
-    // half precision, codes, barriers, scales, exchange, stage (with copies), and 1 KB for alignment
+    // half precision, codes, barriers, scales, exchange, stage (with copies)
     const uint32_t halves = 2 * kTiles * kTile * D * 2, slot = kTile * D;
-    const uint32_t tail = kBarBytes + kScaleBytes + kExchange + (kCopies > 1 ? kStage : 0) + 1024;
+    const uint32_t tail = kBarBytes + kScaleBytes<D> + kExchange + (kCopies > 1 ? kStage : 0);
     int ns = (int)((kSmemLimit - tail - halves) / slot);
     if (ns > kMaxSlots) ns = kMaxSlots;
-    ta.NK = ta.NV = ns / 4 * 2;           // even: a slot has tiles of one producer only, which sees every phase of it
+    // (A slot's tiles may be now of one producer and now of the other.  Waits for its barriers are told apart by their parity
+    // all the same: a producer's last tile waited for a slot whose last tile is later than the second last one of this.)
+    ta.NV = ns / 2;
+    ta.NK = ns - ta.NV;
+    if (ta.NV < 2 || ta.NK + 4 > kScaleTiles<D>) return cudaErrorInvalidConfiguration;
     ta.off_bar = halves + ns * slot;
-    ta.off_stage = ta.off_bar + kBarBytes + kScaleBytes + kExchange + 256;
+    ta.off_stage = ta.off_bar + kBarBytes + kScaleBytes<D> + kExchange + 256;
     ta.bytes = ta.off_bar + tail;
     if (!encode_codes(&ta.tmK, a.K, a) || !encode_codes(&ta.tmV, a.V, a)) return cudaErrorInvalidValue;
     static std::atomic<unsigned long long> opted{0};
