@@ -23,8 +23,8 @@
 // neither operand's reads meet in a bank; the copies go on from one request's tiles to the next one's
 // while an output is written.
 //
-// Measured (heads of 128, one token): 3 requests of 115k keys, 16 heads with keys of their own, 219 us (6.5
-// TB/s, 96% of the copy's rate); 64 requests of 256-8192 keys, 16 query and 4 key heads, 57.8 us (41 at that
+// Measured (heads of 128, one token): 3 requests of 115k keys, 16 heads with keys of their own, 216 us (6.6
+// TB/s, 97% of the copy's rate); 64 requests of 256-8192 keys, 16 query and 4 key heads, 58 us (41 at that
 // rate): first codes after 5.7 us, then 5.6 TB/s, shares that end between 43 and 57 us because the
 // multiprocessors do not get equal parts of the bandwidth, and 4.5 us of join.  float32, 16 requests, 27 us
 // (11 at that rate): ten of them start and join.

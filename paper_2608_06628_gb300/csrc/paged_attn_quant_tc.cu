@@ -21,13 +21,15 @@
 // SM's share of the memory bandwidth (1400).  P takes the place of the S that it was made from.  Two
 // threads share a row of the softmax: halves of its keys, and of the output's features.
 //
-// Measured (64 requests of 256-8192 tokens, 16 query and 4 key heads of 128, blocks of 32 tokens): 90
-// us, 44 for the codes at the copy's rate.  What bounds it is a tile's chain: scores formed, read,
-// their exponentials (512 cycles of the four schedulers at least) and conversions, P stored, its
-// product; 2700 cycles a tile.  Other arrangements of the same chain took longer: two groups of
+// Measured (64 requests of 256-8192 tokens, 16 query and 4 key heads of 128, blocks of 32 tokens): 85
+// us, 44 for the codes at the copy's rate.  What bounds it is a tile's chain: scores read and compared
+// (430 cycles), a reference agreed on (330), exponentials (512 of the special unit at least) and P
+// (910 together), the wait for the next scores (480); and a change of units, 8000 cycles, half of them
+// for code that the instruction cache has lost.  Three tiles of codes of each kind are on their way, as
+// many as shared memory holds (two: 92 us).  Other arrangements of the same chain took longer: two groups of
 // softmax warps with every second tile each 121 us, four threads to a row 118, the codes copied by
 // the warps that convert them 112; P in a place of its own 92.  With d = 64 and
-// pages of 16 tokens (53.8 us, 20 at the copy's rate) a producer's 16 boxes of a tile, about 100 cycles
+// pages of 16 tokens (53 us, 20 at the copy's rate) a producer's 16 boxes of a tile, about 100 cycles
 // each, come as close: hence two producers (62 us with one).
 //
 // Keys that no query sees: pages and scales without a visible key are not loaded, masked scores
